@@ -1,0 +1,405 @@
+"""Cases of the 8-bit KV cache operators: query / key norms with rotation and the cache write (bf16 and 8-bit cache),
+the way back to bf16, and ragged attention over the 8-bit cache.
+
+Shapes are the ones this repository serves: 28 query heads on 4 kv heads and 32 on 32 at head_dim 128, 4 on 4 at
+head_dim 64; blocks of 32 tokens; prompts and contexts of a few hundred to a few thousand tokens, and long single-token
+contexts.  The 8-bit cache holds e4m3 codes in blocks of 32 cache rows, [block][kv head][32][head_dim], with one
+power-of-two scale for each block and head."""
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+BLK = 32                 # cache rows that share a scale
+TOP = 448.0              # largest e4m3 value
+KMIN, KMAX = -40, 40     # exponents a scale may have
+
+
+# ---- cases -------------------------------------------------------------------------------------------------
+
+def listed():
+    return [
+        # one token for each of four short rows of the smallest model: a call whose cost is latency
+        dict(name="attn 4x1 mha dh64", op="attn", hq=4, hkv=4, dh=64, rows=4, nq=1, lo=9, hi=160, empty=1, mix=1),
+        # single-token serving of a full batch, grouped heads, contexts of one to four thousand tokens
+        dict(name="attn 64x1 gqa", op="attn", hq=28, hkv=4, dh=128, rows=64, nq=1, lo=1024, hi=4096, empty=0, mix=2),
+        # two very long rows, single tokens: few work items, the keys have to be split
+        dict(name="attn 2x1 gqa 64k", op="attn", hq=28, hkv=4, dh=128, rows=2, nq=1, lo=50001, hi=65536, empty=0, mix=3),
+        # a block step (32 tokens a row) of a model without grouped heads
+        dict(name="attn 64x32 mha", op="attn", hq=32, hkv=32, dh=128, rows=64, nq=32, lo=96, hi=1024, empty=0, mix=4),
+        # the block step of the benchmark's model and batch
+        dict(name="attn 16x32 gqa", op="attn", hq=28, hkv=4, dh=128, rows=16, nq=32, lo=320, hi=800, empty=1, mix=5),
+        # block-start refresh: whole rows as queries, bound by arithmetic
+        dict(name="attn 6 rows whole gqa", op="attn", hq=28, hkv=4, dh=128, rows=6, nq=0, lo=1200, hi=2304, empty=0, mix=6),
+        # single-token step of a batch: norms, rotation, bf16 cache
+        dict(name="norm 64x1 gqa", op="norm", hq=28, hkv=4, dh=128, rows=64, nq=1, lo=64, hi=4096, empty=0, mix=7),
+        # refresh of a batch of whole rows, bf16 cache
+        dict(name="norm 16 rows whole gqa", op="norm", hq=28, hkv=4, dh=128, rows=16, nq=0, lo=320, hi=1024, empty=0, mix=8),
+        # a block step rewrites 32 rows inside each slab of the 8-bit cache: most blocks are partly kept
+        dict(name="write 16x32 gqa", op="write", hq=28, hkv=4, dh=128, rows=16, nq=32, lo=320, hi=800, empty=0, mix=9,
+             append=False),
+        # refresh of whole rows into the 8-bit cache, no grouped heads
+        dict(name="write 16 rows whole mha", op="write", hq=32, hkv=32, dh=128, rows=16, nq=0, lo=128, hi=1024, empty=0,
+             mix=10, append=True),
+        # reading a few blocks back (a row handed to a bf16 cache)
+        dict(name="read 4x160 mha dh64", op="read", hq=4, hkv=4, dh=64, rows=4, nq=0, lo=33, hi=160, empty=0, mix=11),
+        # reading a batch of long rows back
+        dict(name="read 16 rows mha", op="read", hq=32, hkv=32, dh=128, rows=16, nq=0, lo=700, hi=2304, empty=0, mix=12),
+    ]
+
+
+HEADS = [(4, 4, 64), (8, 2, 64), (28, 4, 128), (28, 4, 128), (32, 32, 128), (32, 8, 128), (6, 2, 128)]
+
+
+def _log(rng, a, b):
+    return max(a, min(b, int(round(math.exp(rng.uniform(math.log(a), math.log(b)))))))
+
+
+def draw(rng):
+    hq, hkv, dh = rng.choice(HEADS)
+    op = rng.choice(["attn", "attn", "attn", "norm", "write", "read"])
+    c = dict(op=op, hq=hq, hkv=hkv, dh=dh, rows=_log(rng, 1, 96), nq=rng.choice([0, 1, 1, _log(rng, 2, 64), 32]),
+             hi=_log(rng, 16, 2304), empty=0, mix=rng.randrange(1 << 20))
+    if op == "attn" and c["nq"] == 1 and rng.random() < 0.5:
+        c["hi"] = _log(rng, 2048, 65536)
+    if op == "read":
+        c["nq"] = 0
+    c["lo"] = max(1, int(c["hi"] * rng.uniform(0.02, 1.0)))
+    if op == "attn" and rng.random() < 0.3:
+        c["empty"] = min(c["rows"] - 1, rng.randrange(1, 4))
+    if op == "write":
+        c["append"] = rng.random() < 0.5
+    most = max(_cost(x) for x in listed() if x["op"] == op)
+    room = max(work(x)["bytes"] for x in listed() if x["op"] == op)
+    big = lambda: _cost(c) > most or work(c)["bytes"] > room   # noqa: E731
+    while c["rows"] > 1 and big():
+        c["rows"] = max(1, c["rows"] * 3 // 4)
+        c["empty"] = min(c["empty"], c["rows"] - 1)
+    while big():
+        c["hi"] = max(1, c["hi"] * 3 // 4)
+        c["lo"] = min(c["lo"], c["hi"])
+    return c
+
+
+def _cost(case):
+    w = work(case)
+    return max(w["bytes"], w["flops"] / 50)
+
+
+def _plan(case):
+    """Row lengths of a case: queries n, visible cache rows vis, first written position at, rows valid before the call had;
+    slabs of whole blocks in shuffled order with gaps."""
+    r = np.random.RandomState(case["mix"])
+    rows = case["rows"]
+    vis = r.randint(case["lo"], case["hi"] + 1, rows).astype(np.int64)
+    if case["nq"] == 0:
+        n = vis.copy()
+    else:
+        n = np.minimum(vis, case["nq"])
+        short = r.rand(rows) < 0.15                      # a ragged last block here and there
+        n = np.where(short, 1 + (n - 1) * r.rand(rows), n).astype(np.int64)
+    at = np.floor((vis - n + 1) * r.rand(rows)).astype(np.int64)
+    if case.get("append"):
+        at = vis - n
+    had = at.copy() if case.get("append") else vis.copy()
+    for i in range(case["empty"]):                       # rows that see nothing
+        vis[i] = 0
+    blocks = (np.maximum(vis, at + n) + BLK - 1) // BLK
+    base = np.zeros(rows, np.int64)
+    free = 1
+    for i in r.permutation(rows):
+        base[i] = free * BLK
+        free += int(blocks[i]) + int(r.randint(0, 2))
+    cu = np.concatenate([[0], np.cumsum(n)])
+    return dict(n=n, vis=vis, at=at, had=had, base=base, cu=cu, n_blocks=free + 1)
+
+
+def _touched(p):
+    """(cache block, row, first position) of every block that a write touches."""
+    first, last = p["at"] // BLK, (p["at"] + np.maximum(p["n"], 1) - 1) // BLK
+    count = np.where(p["n"] > 0, last - first + 1, 0)
+    row = np.repeat(np.arange(len(count)), count)
+    k = np.arange(len(row)) - np.repeat(np.cumsum(count) - count, count)
+    pos = (first[row] + k) * BLK
+    return (p["base"][row] + pos) // BLK, row, pos
+
+
+def work(case):
+    p, hq, hkv, dh = _plan(case), case["hq"], case["hkv"], case["dh"]
+    m, seen = int(p["n"].sum()), int(p["vis"].sum())
+    nblk = int(((p["vis"] + BLK - 1) // BLK).sum())
+    if case["op"] == "attn":
+        return {"bytes": seen * hkv * dh * 2 + nblk * hkv * 8 + 2 * m * hq * dh * 2,
+                "flops": 4 * hq * dh * int((p["n"] * p["vis"]).sum())}
+    if case["op"] == "read":
+        return {"bytes": seen * hkv * dh * 2 * 3 + nblk * hkv * 8, "flops": 2 * seen * hkv * dh}
+    table = 4 * dh * m
+    if case["op"] == "norm":
+        return {"bytes": 4 * m * (hq + 2 * hkv) * dh + table, "flops": 10 * m * (hq + hkv) * dh}
+    blk, row, pos = _touched(p)
+    lo, hi = np.maximum(pos, p["at"][row]), np.minimum(pos + BLK, (p["at"] + p["n"])[row])
+    kept = np.maximum(0, np.minimum(pos + BLK, p["had"][row]) - pos) - np.maximum(
+        0, np.minimum(hi, p["had"][row]) - lo)
+    return {"bytes": 2 * m * (hq + 2 * hkv) * dh + 2 * m * hq * dh + 2 * m * hkv * dh + table
+            + 2 * int(kept.sum()) * hkv * dh + 16 * len(blk) * hkv, "flops": 10 * m * (hq + 2 * hkv) * dh}
+
+
+# ---- inputs ------------------------------------------------------------------------------------------------
+
+def _cache(n_blocks, hkv, dh, g):
+    """Codes and scales of normally distributed values whose spread differs between blocks and heads."""
+    spread = torch.exp2(torch.randint(-2, 3, (n_blocks, hkv, 1, 1), generator=g, device="cuda").float())
+    x = torch.randn(n_blocks, hkv, BLK, dh, generator=g, device="cuda") * spread
+    s = torch.ldexp(torch.ones(n_blocks, hkv, device="cuda"), torch.ceil(torch.log2(x.abs().amax((2, 3)) / TOP)).int())
+    return (x / s[:, :, None, None]).clamp(-TOP, TOP).to(torch.float8_e4m3fn), s
+
+
+def prepare(case, seed):
+    p, hq, hkv, dh = _plan(case), case["hq"], case["hkv"], case["dh"]
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    ints = lambda a: torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).cuda()   # noqa: E731
+    m = int(p["cu"][-1])
+    st = dict(case=case, m=m, rows=case["rows"], max_nq=int(p["n"].max()), max_vis=int(p["vis"].max()),
+              base=ints(p["base"]), cu=ints(p["cu"]), vis=ints(p["vis"]), kv_rows=p["n_blocks"] * BLK)
+    if case["op"] == "attn":
+        st["q"] = torch.randn(m, hq * dh, generator=g, device="cuda").mul_(1.5).bfloat16()
+    if case["op"] in ("attn", "read", "write"):
+        st["k8"], st["ks"] = _cache(p["n_blocks"], hkv, dh, g)
+        st["v8"], st["vs"] = _cache(p["n_blocks"], hkv, dh, g)
+    if case["op"] == "read":
+        st["total"] = int(p["vis"].sum())
+        st["start"] = torch.zeros_like(st["base"])
+    if case["op"] in ("norm", "write"):
+        st["qkv"] = torch.randn(m, (hq + 2 * hkv) * dh, generator=g, device="cuda").mul_(1.5).bfloat16()
+        st["gq"] = (1 + 0.1 * torch.randn(dh, generator=g, device="cuda")).bfloat16()
+        st["gk"] = (1 + 0.1 * torch.randn(dh, generator=g, device="cuda")).bfloat16()
+        row = np.repeat(np.arange(case["rows"]), p["n"])
+        pos = p["at"][row] + np.arange(m) - p["cu"][row]
+        st["pos"], st["tok_kv"] = ints(pos), ints(p["base"][row] + pos)
+        rows_of_table = int(case["hi"]) + BLK
+        angle = torch.arange(rows_of_table, device="cuda", dtype=torch.float64)[:, None] * torch.pow(
+            10000.0, -2.0 * torch.arange(dh // 2, device="cuda", dtype=torch.float64) / dh)
+        st["table"] = torch.stack([angle.cos(), angle.sin()], -1).float().contiguous()
+        st["q_out"] = torch.empty(m, hq * dh, dtype=torch.bfloat16, device="cuda")
+    if case["op"] == "norm":
+        st["kc"] = torch.randn(st["kv_rows"], hkv, dh, generator=g, device="cuda").bfloat16()
+        st["vc"] = torch.randn(st["kv_rows"], hkv, dh, generator=g, device="cuda").bfloat16()
+    if case["op"] == "write":
+        blk, brow, bpos = _touched(p)
+        st["at"], st["had"] = ints(p["at"]), ints(p["had"])
+        st["blk"] = torch.from_numpy(blk).cuda()
+        st["brow"], st["bpos"] = torch.from_numpy(brow).cuda(), torch.from_numpy(bpos).cuda()
+    return st
+
+
+# ---- one pass ----------------------------------------------------------------------------------------------
+
+def run(state):
+    op = state["case"]["op"]
+    if own:
+        return _own(state)
+    return {"attn": _attn, "read": _read, "norm": _norm, "write": _write}[op](state)
+
+
+def _own(s):
+    from paper_2607_08930_b200 import binding as B
+    c = s["case"]
+    hq, hkv, dh = c["hq"], c["hkv"], c["dh"]
+    if c["op"] == "attn":
+        return B.op_attention_kv8(s["q"], s["k8"], s["v8"], s["ks"], s["vs"], s["cu"], s["base"], s["vis"], hq,
+                                  max_nq=s["max_nq"], max_vis=s["max_vis"])
+    if c["op"] == "read":
+        return B.op_kv8_read(s["k8"], s["v8"], s["ks"], s["vs"], s["base"], s["start"], s["vis"], s["total"])
+    if c["op"] == "norm":
+        q = B.op_qk_norm_rope_kv(s["qkv"], s["gq"], s["gk"], 1e-6, s["pos"], s["tok_kv"], s["kc"], s["vc"], hq, hkv, dh,
+                                 s["table"], q_out=s["q_out"])
+        return q, s["kc"], s["vc"]
+    q = B.op_qk_norm_rope_kv8(s["qkv"], s["gq"], s["gk"], 1e-6, s["pos"], s["cu"], s["base"], s["at"], s["had"],
+                              s["k8"], s["v8"], s["ks"], s["vs"], hq, hkv, dh, s["table"], q_out=s["q_out"])
+    return q, s["k8"], s["v8"], s["ks"], s["vs"]
+
+
+def _values(codes, scales, blocks):
+    """fp32 values of the given cache blocks: [..., kv head, row of the block, dim]."""
+    x = codes.view(torch.uint8)[blocks].view(torch.float8_e4m3fn).float()
+    return x * scales[blocks][..., None, None]
+
+
+def _attn(s):
+    c = s["case"]
+    hq, hkv, dh, rows, nq = c["hq"], c["hkv"], c["dh"], s["rows"], s["max_nq"]
+    nb = max(1, (s["max_vis"] + BLK - 1) // BLK)
+    vis, base = s["vis"].long(), s["base"].long()
+    blocks = torch.arange(nb, device="cuda")[None]
+    inside = blocks * BLK < vis[:, None]
+    at = torch.where(inside, base[:, None] // BLK + blocks, 0)
+    k = _values(s["k8"], s["ks"], at).transpose(1, 2).reshape(rows, hkv, 1, nb * BLK, dh)
+    j = torch.arange(nq, device="cuda")[None]
+    start, n = s["cu"][:-1].long(), (s["cu"][1:] - s["cu"][:-1]).long()
+    real = j < n[:, None]
+    tok = torch.where(real, start[:, None] + j, 0)
+    q = s["q"][tok].float().reshape(rows, nq, hkv, hq // hkv, dh).permute(0, 2, 3, 1, 4).reshape(rows, hkv, 1, -1, dh)
+    z = torch.matmul(q, k.transpose(3, 4)) / math.sqrt(dh)
+    key = torch.arange(nb * BLK, device="cuda")
+    seen = (key[None] < vis[:, None])[:, None, None, None]
+    z = z.masked_fill(~seen, -math.inf)
+    top = z.amax(-1, keepdim=True)
+    e = torch.exp(z - torch.where(top > -math.inf, top, 0.0))
+    del z, k
+    v = _values(s["v8"], s["vs"], at).transpose(1, 2).reshape(rows, hkv, 1, nb * BLK, dh)
+    v = torch.where(seen.transpose(3, 4), v, 0.0)
+    total = e.sum(-1, keepdim=True)
+    o = torch.matmul(e, v) / torch.where(total > 0, total, 1.0)
+    o = o.reshape(rows, hkv, hq // hkv, nq, dh).permute(0, 3, 1, 2, 4).reshape(rows * nq, hq * dh)
+    # packed token t of row i is padded token i * nq + (t - start_i)
+    t = torch.arange(s["m"], device="cuda")
+    r = torch.searchsorted(s["cu"][1:].long(), t, right=True)
+    return o[r * nq + t - start[r]].bfloat16()
+
+
+def _read(s):
+    t = torch.arange(s["total"], device="cuda")
+    end = torch.cumsum(s["vis"].long(), 0)
+    r = torch.searchsorted(end, t, right=True)
+    at = s["base"].long()[r] + t - (end[r] - s["vis"].long()[r]) + s["start"].long()[r]
+    k = s["k8"].view(torch.uint8)[at // BLK, :, at % BLK].view(torch.float8_e4m3fn).float() * s["ks"][at // BLK][..., None]
+    v = s["v8"].view(torch.uint8)[at // BLK, :, at % BLK].view(torch.float8_e4m3fn).float() * s["vs"][at // BLK][..., None]
+    return k.bfloat16(), v.bfloat16()
+
+
+def _normed(x, gain, table):
+    """RMS norm over the head's dims, gain, rotation of the pairs (j, j + dh / 2): x [m, heads, dh] in fp32."""
+    x = x / torch.sqrt((x * x).mean(-1, keepdim=True) + 1e-6) * gain.float()
+    a, b = x.chunk(2, -1)
+    cos, sin = table[:, None, :, 0], table[:, None, :, 1]
+    return torch.cat([a * cos - b * sin, b * cos + a * sin], -1)
+
+
+def _parts(s):
+    c = s["case"]
+    hq, hkv, dh = c["hq"], c["hkv"], c["dh"]
+    x = s["qkv"].float().reshape(s["m"], hq + 2 * hkv, dh)
+    table = s["table"][s["pos"].long()]
+    return (_normed(x[:, :hq], s["gq"], table), _normed(x[:, hq:hq + hkv], s["gk"], table), x[:, hq + hkv:])
+
+
+def _norm(s):
+    q, k, v = _parts(s)
+    s["q_out"].copy_(q.reshape(s["m"], -1))
+    s["kc"][s["tok_kv"].long()] = k.bfloat16()
+    s["vc"][s["tok_kv"].long()] = v.bfloat16()
+    return s["q_out"], s["kc"], s["vc"]
+
+
+def _store(s, codes, scales, new):
+    """Blocks s["blk"] of one cache take the rows `new` [m, kv head, dh]; rows that were valid stay."""
+    old_codes = codes.view(torch.uint8)[s["blk"]]
+    old = old_codes.view(torch.float8_e4m3fn).float() * scales[s["blk"]][:, :, None, None]
+    pos = s["bpos"][:, None] + torch.arange(BLK, device="cuda")
+    at, n, had = s["at"].long()[s["brow"]][:, None], (s["cu"][1:] - s["cu"][:-1]).long()[s["brow"]][:, None], s["had"].long()[s["brow"]][:, None]
+    fresh = (pos >= at) & (pos < at + n)
+    kept = (pos < had) & ~fresh
+    tok = torch.where(fresh, s["cu"].long()[s["brow"]][:, None] + pos - at, 0)
+    x = torch.where(fresh[:, None, :, None], new[tok].transpose(1, 2), old)
+    valid = (fresh | kept)[:, None, :, None]
+    top = torch.where(valid, x.abs(), 0.0).amax((2, 3))
+    m, e = torch.frexp(top)
+    k = torch.where(m <= TOP / 512, e - 9, e - 8)
+    k = torch.where(top > 0, k, KMIN).clamp(KMIN, KMAX)
+    scale = torch.ldexp(torch.ones_like(top), k)
+    put = (x / scale[:, :, None, None]).clamp(-TOP, TOP).to(torch.float8_e4m3fn).view(torch.uint8)
+    codes.view(torch.uint8)[s["blk"]] = torch.where(valid, put, old_codes)
+    scales[s["blk"]] = scale
+
+
+def _write(s):
+    q, k, v = _parts(s)
+    s["q_out"].copy_(q.reshape(s["m"], -1))
+    _store(s, s["k8"], s["ks"], k)
+    _store(s, s["v8"], s["vs"], v)
+    return s["q_out"], s["k8"], s["v8"], s["ks"], s["vs"]
+
+
+# ---- the same in 64 bits, from the definitions -------------------------------------------------------------
+
+def exact(case, seed):
+    s, p = prepare(case, seed), _plan(case)
+    hq, hkv, dh = case["hq"], case["hkv"], case["dh"]
+    group = hq // hkv
+    real = {}
+    if "k8" in s:                                          # a code is sign, exponent and mantissa; read it as such
+        for name, scale in (("k8", "ks"), ("v8", "vs")):
+            b = s[name].view(torch.uint8).long()
+            ex, man = (b >> 3) & 15, (b & 7).double()
+            mag = torch.where(ex > 0, (1 + man / 8) * torch.exp2((ex - 7).double()), man / 8 * 2.0 ** -6)
+            mag = torch.where((b & 127) == 127, torch.nan, mag)
+            real[name] = torch.where(b > 127, -mag, mag) * s[scale].double()[:, :, None, None]
+    if case["op"] == "attn":
+        out = torch.zeros(s["m"], hq, dh, dtype=torch.float64, device="cuda")
+        for i in range(case["rows"]):
+            n, vis, t0, b0 = int(p["n"][i]), int(p["vis"][i]), int(p["cu"][i]), int(p["base"][i]) // BLK
+            if vis == 0 or n == 0:
+                continue
+            some = slice(b0, b0 + (vis + BLK - 1) // BLK)
+            kk = real["k8"][some].permute(1, 0, 2, 3).reshape(hkv, -1, dh)[:, :vis]
+            vv = real["v8"][some].permute(1, 0, 2, 3).reshape(hkv, -1, dh)[:, :vis]
+            q = s["q"][t0:t0 + n].double().reshape(n, hq, dh)
+            for h in range(hq):
+                w = torch.softmax(q[:, h] @ kk[h // group].T * dh ** -0.5, 1)
+                out[t0:t0 + n, h] = w @ vv[h // group]
+        return out.reshape(s["m"], hq * dh)
+    if case["op"] == "read":
+        got = []
+        for name in ("k8", "v8"):
+            flat = real[name].permute(0, 2, 1, 3).reshape(-1, hkv, dh)
+            got.append(torch.cat([flat[int(b):int(b) + int(n)] for b, n in zip(p["base"], p["vis"])]))
+        return tuple(got)
+    x = s["qkv"].double().reshape(s["m"], -1, dh)
+    pos = s["pos"].double()
+    freq = torch.tensor([10000.0 ** (-2.0 * j / dh) for j in range(dh // 2)], dtype=torch.float64, device="cuda")
+    turn = torch.polar(torch.ones(s["m"], 1, dh // 2, dtype=torch.float64, device="cuda"), (pos[:, None] * freq)[:, None])
+
+    def rotated(y, gain):
+        y = gain.double() * y * torch.rsqrt(y.square().mean(2, keepdim=True) + 1e-6)
+        z = torch.complex(y[..., :dh // 2].contiguous(), y[..., dh // 2:].contiguous()) * turn
+        return torch.cat([z.real, z.imag], 2)
+
+    q, k, v = rotated(x[:, :hq], s["gq"]), rotated(x[:, hq:hq + hkv], s["gk"]), x[:, hq + hkv:]
+    if case["op"] == "norm":
+        kc, vc = s["kc"].double(), s["vc"].double()
+        for i in range(case["rows"]):
+            a, b, to = int(p["cu"][i]), int(p["cu"][i + 1]), int(p["base"][i] + p["at"][i])
+            kc[to:to + b - a], vc[to:to + b - a] = k[a:b], v[a:b]
+        return q.reshape(s["m"], -1), kc, vc
+
+    def quantised(y, scale):                               # to the nearest e4m3 value, halves to the even one
+        y = y / scale
+        ex = torch.floor(torch.log2(y.abs().clamp_min(2.0 ** -6)))
+        step = torch.exp2(ex - 3)
+        return torch.round(y / step) * step
+
+    outs = [q.reshape(s["m"], -1)]
+    scales = []
+    for name, scale, new in (("k8", "ks", k), ("v8", "vs", v)):
+        codes = s[name].double()
+        sc = s[scale].double()
+        flat = real[name].permute(0, 2, 1, 3).reshape(-1, hkv, dh).clone()      # by cache row
+        for i in range(case["rows"]):
+            a, b, to = int(p["cu"][i]), int(p["cu"][i + 1]), int(p["base"][i] + p["at"][i])
+            flat[to:to + b - a] = new[a:b]
+        blk, row, first = _touched(p)
+        live = np.maximum(p["had"], p["at"] + p["n"])[row] - first               # rows of the block that hold something
+        # (rows between `had` and `at` do not occur here: a write starts at or before the end of what was there)
+        x3 = flat.reshape(-1, BLK, hkv, dh)[torch.from_numpy(blk).cuda()].transpose(1, 2)
+        on = (torch.arange(BLK, device="cuda") < torch.from_numpy(live).cuda()[:, None])[:, None, :, None]
+        top = torch.where(on, x3.abs(), 0.0).amax((2, 3))
+        ladder = torch.exp2(torch.arange(KMIN, KMAX + 1, device="cuda", dtype=torch.float64))
+        new_sc = ladder[torch.searchsorted(ladder * TOP, top).clamp(max=KMAX - KMIN)]
+        where = torch.from_numpy(blk).cuda()
+        codes[where] = torch.where(on, quantised(x3, new_sc[:, :, None, None]), codes[where])
+        sc[where] = new_sc
+        outs.append(codes)
+        scales.append(sc)
+    return tuple(outs + scales)
