@@ -211,7 +211,7 @@ def _own(s):
         return B.op_attention_kv8(s["q"], s["k8"], s["v8"], s["ks"], s["vs"], s["cu"], s["base"], s["vis"], hq,
                                   max_nq=s["max_nq"], max_vis=s["max_vis"])
     if c["op"] == "read":
-        return B.op_kv8_read(s["k8"], s["v8"], s["ks"], s["vs"], s["base"], s["start"], s["vis"], s["total"])
+        return B.op_kv8_read(s["k8"], s["v8"], s["ks"], s["vs"], s["cu"], s["base"], s["start"], s["total"])
     if c["op"] == "norm":
         q = B.op_qk_norm_rope_kv(s["qkv"], s["gq"], s["gk"], 1e-6, s["pos"], s["tok_kv"], s["kc"], s["vc"], hq, hkv, dh,
                                  s["table"], q_out=s["q_out"])
