@@ -319,6 +319,71 @@ int bs_op_lm_head_confidence(const void* hf, int lda, const void* W, int M, int 
                              int mask_id, void* scratch, size_t scratch_bytes, int* tok, float* conf,
                              float* logits /* nullable */, int* error_flag /* nullable */, void* stream);
 
+/* ---- per-head norms with the rotation, and an 8-bit KV cache ------------- *
+ * No counterpart in the paper (its runs hold the cache in 16 bits and its models have no per-head norms): for models
+ * that normalise every query and key head, and for batches whose cache has to fit half the bytes.
+ *
+ * The 8-bit cache.  K and V are e4m3 codes [kv_rows / 32][n_kv_heads][32][head_dim] (the 32 cache rows of a block, one
+ * head after the other), each with fp32 scales [kv_rows / 32][n_kv_heads]: value = code * scale.  kv_rows is a
+ * multiple of BS_KV8_BLOCK.  Slabs start at multiples of BS_KV8_BLOCK rows (kv_base[i]), so that no block holds rows of
+ * two requests; two rows of one call must not name overlapping slabs.  A scale is the smallest power of two 2^k,
+ * -40 <= k <= 40, with max |x| <= 448 * 2^k over the block's valid rows; larger values saturate, infinities with them,
+ * NaN stays NaN.  Values written are rounded once (nearest even), from fp32.  Scales that a reader finds outside
+ * [2^-40, 2^40] are taken as the nearer bound.
+ *
+ * Common to the four operators below: head_dim 64 or 128; n_q_heads a multiple of n_kv_heads; device pointers are
+ * 16-byte aligned (scratch 256); row i owns packed tokens [cu[i], cu[i+1]), cu[0] = 0, non-decreasing; tokens at and
+ * behind cu[n_rows] belong to no row and their outputs are left as they were.  Indices are checked on the device: a
+ * token or row whose position, cache row or span lies outside the stated sizes is skipped, and error_flag (device int,
+ * nullable, only ever raised) gets 100 or more.  Calls allocate nothing and may be captured into graphs; calls that
+ * share scratch must be ordered (same stream, or events). */
+enum { BS_KV8_BLOCK = 32, BS_KV8_MAX_ROWS = 1024 };
+
+/* cos / sin table of the rotation, [max_pos][head_dim / 2][2], evaluated in double and rounded once, into HOST memory
+ * (copy it to the device once; the operators below and every layer share it). */
+int bs_rope_table(float* host_table, int max_pos, int head_dim, float theta);
+
+/* Norms of every query and key head, rotation, K/V scatter in one pass over qkv bf16 [M][(Hq + 2 Hkv) * head_dim]:
+ *   y = gain * x / sqrt(mean(x^2) + eps) over the head's dims, then the pairs (y_j, y_{j + head_dim/2}) turned by the
+ *   angle of the token's position id (rope_table, device memory), all in fp32 and rounded once to bf16.
+ * Query heads go to q_out (row stride q_ld elements, a multiple of 8; q_out = qkv with q_ld = (Hq + 2 Hkv) * head_dim
+ * rotates in place), k and v to cache row tok_kv[t] of the bf16 caches [kv_rows][Hkv][head_dim]; tok_kv[t] < 0: the
+ * token belongs to no row and is skipped.  q_gain / k_gain: bf16 [head_dim], or both NULL (rotation only).
+ * Tokens of one call must name different cache rows. */
+int bs_op_qk_norm_rope_kv(const void* qkv, const void* q_gain, const void* k_gain, float eps, const int* tok_pos,
+                          const int* tok_kv, void* q_out, int q_ld, void* kcache, void* vcache, long long kv_rows, int M,
+                          int n_q_heads, int n_kv_heads, int head_dim, const float* rope_table, int max_pos,
+                          int* error_flag, void* stream);
+
+/* The same pass with the 8-bit cache.  The tokens of row i are written to its cache positions kv_at[i],
+ * kv_at[i] + 1, ... (offsets from kv_base[i]); positions [0, kv_len[i]) held valid rows before the call.  Blocks that
+ * the span touches get the scale of everything that is valid in them afterwards - the new rows and the ones that stay -
+ * and rows that stay are re-encoded if their scale moved; codes at other positions are left as they were.
+ * (Block step: kv_len = the row's visible length.  Append: kv_at = kv_len.  Whole-row refresh: kv_at = kv_len = 0.) */
+int bs_op_qk_norm_rope_kv8(const void* qkv, const void* q_gain, const void* k_gain, float eps, const int* tok_pos,
+                           const int* cu_q, const int* kv_base, const int* kv_at, const int* kv_len, int n_rows,
+                           void* q_out, int q_ld, void* k8, void* v8, float* k_scale, float* v_scale, long long kv_rows,
+                           int M, int n_q_heads, int n_kv_heads, int head_dim, const float* rope_table, int max_pos,
+                           int* error_flag, void* stream);
+
+/* Reads cache positions [kv_at[i], kv_at[i] + n_i), n_i = cu[i+1] - cu[i], of every row back: bf16 [total][Hkv][head_dim]
+ * K and V (exact for the scales that the writer stores).  total >= cu[n_rows] is the size of the outputs. */
+int bs_op_kv8_read(const void* k8, const void* v8, const float* k_scale, const float* v_scale, long long kv_rows,
+                   const int* cu, const int* kv_base, const int* kv_at, int n_rows, int total, int n_kv_heads,
+                   int head_dim, void* k_out, void* v_out, int* error_flag, void* stream);
+
+/* Ragged bidirectional attention over the 8-bit cache: the queries of row i attend to cache positions [0, vis[i]) of
+ * its slab (no causal or padding mask); out bf16 [M][Hq * head_dim]; vis[i] = 0 gives zeros.  Codes behind vis[i] may
+ * be anything, NaN included.  q bf16, row stride q_ld elements (a multiple of 8): q_out of the operators above, or
+ * the query part of a qkv buffer.  max_nq (0: unknown) and max_vis (0: unknown) are the largest query count and vis of
+ * a row; they choose the kernel, not the result's meaning.  At most BS_KV8_MAX_ROWS rows and 32 query heads per kv
+ * head.  scratch: bs_op_attention_kv8_scratch_bytes bytes of device memory, overwritten. */
+size_t bs_op_attention_kv8_scratch_bytes(int n_q_heads, int n_kv_heads, int head_dim);
+int bs_op_attention_kv8(const void* q, int q_ld, const void* k8, const void* v8, const float* k_scale,
+                        const float* v_scale, long long kv_rows, void* out, const int* cu_q, const int* kv_base,
+                        const int* vis, int n_rows, int M, int max_nq, int max_vis, int n_q_heads, int n_kv_heads,
+                        int head_dim, void* scratch, size_t scratch_bytes, int* error_flag, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

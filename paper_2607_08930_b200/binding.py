@@ -66,7 +66,8 @@ EXPORTS = ["bs_query_sizes", "bs_init_model", "bs_admit", "bs_evict_refill", "bs
            "bs_read_tokens", "bs_get_stats", "bs_set_profiling", "bs_get_profile", "bs_destroy", "bs_last_error", "bs_build_flags", "bs_debug_read", "bs_debug_inject_timeout",
            "bs_debug_force_commit", "bs_debug_snapshot", "bs_debug_restore", "bs_op_gemm", "bs_op_gemm_cluster_splits",
            "bs_op_rmsnorm", "bs_op_rope_kv", "bs_op_rope_kv_static", "bs_op_attention_q_tile", "bs_op_attention", "bs_op_confidence",
-           "bs_op_lm_head_confidence", "bs_op_lm_head_confidence_scratch_bytes"]
+           "bs_op_lm_head_confidence", "bs_op_lm_head_confidence_scratch_bytes", "bs_rope_table", "bs_op_qk_norm_rope_kv",
+           "bs_op_qk_norm_rope_kv8", "bs_op_kv8_read", "bs_op_attention_kv8", "bs_op_attention_kv8_scratch_bytes"]
 
 _lib = None
 
@@ -112,6 +113,15 @@ def lib() -> C.CDLL:
         L.bs_op_lm_head_confidence_scratch_bytes.argtypes = [i, i]
         L.bs_op_lm_head_confidence_scratch_bytes.restype = C.c_size_t
         L.bs_op_lm_head_confidence.argtypes = [vp, i, vp, i, i, i, vp, i, vp, C.c_size_t, vp, vp, vp, vp, vp]
+        L.bs_rope_table.argtypes = [vp, i, i, f]
+        L.bs_op_qk_norm_rope_kv.argtypes = [vp, vp, vp, f, vp, vp, vp, i, vp, vp, ll, i, i, i, i, vp, i, vp, vp]
+        L.bs_op_qk_norm_rope_kv8.argtypes = [vp, vp, vp, f, vp, vp, vp, vp, vp, i, vp, i, vp, vp, vp, vp, ll, i, i, i, i,
+                                             vp, i, vp, vp]
+        L.bs_op_kv8_read.argtypes = [vp, vp, vp, vp, ll, vp, vp, vp, i, i, i, i, vp, vp, vp, vp]
+        L.bs_op_attention_kv8_scratch_bytes.argtypes = [i, i, i]
+        L.bs_op_attention_kv8_scratch_bytes.restype = C.c_size_t
+        L.bs_op_attention_kv8.argtypes = [vp, i, vp, vp, vp, vp, ll, vp, vp, vp, vp, i, i, i, i, i, i, i, vp, C.c_size_t,
+                                          vp, vp]
         _lib = L
     return _lib
 
@@ -432,3 +442,178 @@ def op_confidence(logits: torch.Tensor, mask_id: int):
     _check_op(lib().bs_op_confidence(logits.data_ptr(), n, V, mask_id, tok.data_ptr(), conf.data_ptr(), _stream()),
               "bs_op_confidence")
     return tok, conf
+
+
+# ---- per-head norms with the rotation, and the 8-bit KV cache -----------------------------------------------------
+
+KV8_BLOCK, KV8_MAX_ROWS = 32, 1024
+_BF16, _F32, _I32, _E4M3 = torch.bfloat16, torch.float32, torch.int32, torch.float8_e4m3fn
+
+
+def _refuse(name: str, why: str) -> None:
+    raise BlockServeError(BS_E_ARG, f"{name}: {why}")
+
+
+def _tensors(name: str, device: torch.device, *what) -> None:
+    """what: (argument name, tensor, dtype, least number of elements): contiguous, on `device`."""
+    for arg, t, dtype, least in what:
+        if t.dtype is not dtype or t.device != device or not t.is_contiguous() or t.numel() < least:
+            _refuse(name, f"{arg} must be a contiguous {dtype} tensor of at least {least} elements on {device}, "
+                          f"got {tuple(t.shape)} {t.dtype} on {t.device}")
+
+
+def _call(name: str, device: torch.device, fn, *args) -> None:
+    """The library's kernels go to the device's current stream, whatever device is current."""
+    if device.type != "cuda":
+        _refuse(name, "the operators run on CUDA tensors only")
+    if torch.cuda.current_device() == device.index:
+        rc = fn(*args, torch.cuda.current_stream().cuda_stream)
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, torch.cuda.current_stream().cuda_stream)
+    if rc != BS_OK:
+        _check_op(rc, name)
+
+
+def rope_table(max_pos: int, dh: int, theta: float, device="cuda") -> torch.Tensor:
+    """cos / sin table [max_pos, dh / 2, 2] of the operators below (angles evaluated in double): built once per model."""
+    t = torch.empty(max_pos, dh // 2, 2, dtype=_F32)
+    _check_op(lib().bs_rope_table(t.data_ptr(), max_pos, dh, theta), "bs_rope_table")
+    return t.to(device)
+
+
+def kv8_cache(kv_rows: int, hkv: int, dh: int, device="cuda"):
+    """(k8, v8, k_scale, v_scale) of an 8-bit cache: e4m3 codes [kv_rows / 32, hkv, 32, dh] and one power-of-two scale
+    for each block of 32 rows and head.  kv_rows is rounded up to whole blocks; the contents are not initialised (rows
+    are valid once written)."""
+    n = (kv_rows + KV8_BLOCK - 1) // KV8_BLOCK
+    return (torch.empty(n, hkv, KV8_BLOCK, dh, dtype=_E4M3, device=device),
+            torch.empty(n, hkv, KV8_BLOCK, dh, dtype=_E4M3, device=device),
+            torch.empty(n, hkv, dtype=_F32, device=device), torch.empty(n, hkv, dtype=_F32, device=device))
+
+
+def _kv8_rows(name: str, device, k8, v8, k_scale, v_scale) -> int:
+    if k8.dim() != 4 or k8.shape[2] != KV8_BLOCK or v8.shape != k8.shape or k_scale.shape != k8.shape[:2] or \
+            v_scale.shape != k8.shape[:2]:
+        _refuse(name, "an 8-bit cache is codes [blocks, kv heads, 32, head_dim] and scales [blocks, kv heads]")
+    _tensors(name, device, ("k8", k8, _E4M3, 1), ("v8", v8, _E4M3, 1), ("k_scale", k_scale, _F32, 1),
+             ("v_scale", v_scale, _F32, 1))
+    return k8.shape[0] * KV8_BLOCK
+
+
+def _rows_of(name: str, t: torch.Tensor, arg: str, device, least: int) -> int:
+    """Row stride of a bf16 matrix whose rows are dense."""
+    if t.dim() != 2 or t.dtype is not _BF16 or t.device != device or t.shape[1] < least or \
+            (t.stride(1) != 1 and t.numel() > 0):
+        _refuse(name, f"{arg} must be a bfloat16 matrix on {device} with rows of at least {least} adjacent elements")
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _norm_inputs(name: str, qkv, q_gain, k_gain, tok_pos, hq, hkv, dh, rope, q_out):
+    dev, M, width = qkv.device, qkv.shape[0], (hq + 2 * hkv) * dh
+    if qkv.dim() != 2 or qkv.shape[1] != width or rope.dim() != 3 or rope.shape[1:] != (dh // 2, 2):
+        _refuse(name, f"qkv must be [M, {width}] and rope_table [max_pos, {dh // 2}, 2]")
+    _tensors(name, dev, ("qkv", qkv, _BF16, 0), ("tok_pos", tok_pos, _I32, M), ("rope_table", rope, _F32, dh))
+    if (q_gain is None) != (k_gain is None):
+        _refuse(name, "q_gain and k_gain are given together or not at all")
+    if q_gain is not None:
+        _tensors(name, dev, ("q_gain", q_gain, _BF16, dh), ("k_gain", k_gain, _BF16, dh))
+    if q_out is None:
+        q_out = torch.empty(M, hq * dh, dtype=_BF16, device=dev)
+    ld = _rows_of(name, q_out, "q_out", dev, hq * dh)
+    if q_out.shape[0] < M:
+        _refuse(name, f"q_out needs {M} rows")
+    return dev, M, q_out, ld
+
+
+def op_qk_norm_rope_kv(qkv, q_gain, k_gain, eps: float, tok_pos, tok_kv, kcache, vcache, hq: int, hkv: int, dh: int,
+                       rope_table, q_out: Optional[torch.Tensor] = None,
+                       error_flag: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """RMS norm of every query and key head (gains bf16 [dh], or None for both: no norm), rotation at tok_pos, K / V to
+    rows tok_kv of the bf16 caches [kv_rows, hkv, dh] (tok_kv < 0: the token is skipped).  Returns the queries
+    [M, hq * dh]; q_out = qkv rotates in place.  error_flag (int32 [1]) gets >= 100 where an index was out of range."""
+    name = "bs_op_qk_norm_rope_kv"
+    dev, M, q_out, ld = _norm_inputs(name, qkv, q_gain, k_gain, tok_pos, hq, hkv, dh, rope_table, q_out)
+    if kcache.dim() != 3 or kcache.shape[1:] != (hkv, dh) or vcache.shape != kcache.shape:
+        _refuse(name, f"the caches must be [kv_rows, {hkv}, {dh}]")
+    _tensors(name, dev, ("kcache", kcache, _BF16, 1), ("vcache", vcache, _BF16, 1), ("tok_kv", tok_kv, _I32, M))
+    if error_flag is not None:
+        _tensors(name, dev, ("error_flag", error_flag, _I32, 1))
+    _call(name, dev, lib().bs_op_qk_norm_rope_kv, qkv.data_ptr(), _ptr(q_gain), _ptr(k_gain), eps, tok_pos.data_ptr(),
+          tok_kv.data_ptr(), q_out.data_ptr(), ld, kcache.data_ptr(), vcache.data_ptr(), kcache.shape[0], M, hq, hkv, dh,
+          rope_table.data_ptr(), rope_table.shape[0], _ptr(error_flag))
+    return q_out
+
+
+def op_qk_norm_rope_kv8(qkv, q_gain, k_gain, eps: float, tok_pos, cu_q, kv_base, kv_at, kv_len, k8, v8, k_scale, v_scale,
+                        hq: int, hkv: int, dh: int, rope_table, q_out: Optional[torch.Tensor] = None,
+                        error_flag: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """op_qk_norm_rope_kv with the 8-bit cache of kv8_cache(): row i's tokens [cu_q[i], cu_q[i+1]) go to cache positions
+    kv_at[i].. of its slab (kv_base[i], a multiple of 32), where positions [0, kv_len[i]) held valid rows before.
+    Blocks it touches are re-scaled over everything valid in them."""
+    name = "bs_op_qk_norm_rope_kv8"
+    dev, M, q_out, ld = _norm_inputs(name, qkv, q_gain, k_gain, tok_pos, hq, hkv, dh, rope_table, q_out)
+    rows = _kv8_rows(name, dev, k8, v8, k_scale, v_scale)
+    if k8.shape[1] != hkv or k8.shape[3] != dh:
+        _refuse(name, f"the cache holds {k8.shape[1]} heads of {k8.shape[3]}, not {hkv} of {dh}")
+    n = cu_q.numel() - 1
+    _tensors(name, dev, ("cu_q", cu_q, _I32, 1), ("kv_base", kv_base, _I32, n), ("kv_at", kv_at, _I32, n),
+             ("kv_len", kv_len, _I32, n))
+    if error_flag is not None:
+        _tensors(name, dev, ("error_flag", error_flag, _I32, 1))
+    _call(name, dev, lib().bs_op_qk_norm_rope_kv8, qkv.data_ptr(), _ptr(q_gain), _ptr(k_gain), eps, tok_pos.data_ptr(),
+          cu_q.data_ptr(), kv_base.data_ptr(), kv_at.data_ptr(), kv_len.data_ptr(), n, q_out.data_ptr(), ld, k8.data_ptr(),
+          v8.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), rows, M, hq, hkv, dh, rope_table.data_ptr(),
+          rope_table.shape[0], _ptr(error_flag))
+    return q_out
+
+
+def op_kv8_read(k8, v8, k_scale, v_scale, cu, kv_base, kv_at, total: int, k_out: Optional[torch.Tensor] = None,
+                v_out: Optional[torch.Tensor] = None, error_flag: Optional[torch.Tensor] = None):
+    """Cache positions [kv_at[i], kv_at[i] + cu[i+1] - cu[i]) of every row, packed: bf16 (K, V) [total, hkv, dh]."""
+    name = "bs_op_kv8_read"
+    dev = k8.device
+    rows = _kv8_rows(name, dev, k8, v8, k_scale, v_scale)
+    hkv, dh, n = k8.shape[1], k8.shape[3], cu.numel() - 1
+    _tensors(name, dev, ("cu", cu, _I32, 1), ("kv_base", kv_base, _I32, n), ("kv_at", kv_at, _I32, n))
+    if k_out is None:
+        k_out = torch.empty(total, hkv, dh, dtype=_BF16, device=dev)
+    if v_out is None:
+        v_out = torch.empty(total, hkv, dh, dtype=_BF16, device=dev)
+    _tensors(name, dev, ("k_out", k_out, _BF16, total * hkv * dh), ("v_out", v_out, _BF16, total * hkv * dh))
+    if error_flag is not None:
+        _tensors(name, dev, ("error_flag", error_flag, _I32, 1))
+    _call(name, dev, lib().bs_op_kv8_read, k8.data_ptr(), v8.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), rows,
+          cu.data_ptr(), kv_base.data_ptr(), kv_at.data_ptr(), n, total, hkv, dh, k_out.data_ptr(), v_out.data_ptr(),
+          _ptr(error_flag))
+    return k_out, v_out
+
+
+def attention_kv8_scratch(hq: int, hkv: int, dh: int, device="cuda") -> torch.Tensor:
+    """Scratch of op_attention_kv8, for callers that keep it (calls that share it must be ordered)."""
+    return torch.empty(max(256, lib().bs_op_attention_kv8_scratch_bytes(hq, hkv, dh)), dtype=torch.uint8, device=device)
+
+
+def op_attention_kv8(q, k8, v8, k_scale, v_scale, cu_q, kv_base, vis, hq: int, max_nq: int = 0, max_vis: int = 0,
+                     scratch: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                     error_flag: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of packed queries (q [M, >= hq * dh]: q_out of the operators above, or a qkv buffer) over their rows'
+    cache positions [0, vis[i]) of the 8-bit cache; rows with vis = 0 give zeros.  max_nq / max_vis (0: unknown): the
+    largest number of query tokens and of visible positions of a row.  Without `scratch` it comes from torch's allocator."""
+    name = "bs_op_attention_kv8"
+    dev = q.device
+    rows = _kv8_rows(name, dev, k8, v8, k_scale, v_scale)
+    hkv, dh, n, M = k8.shape[1], k8.shape[3], cu_q.numel() - 1, q.shape[0]
+    ld = _rows_of(name, q, "q", dev, hq * dh)
+    _tensors(name, dev, ("cu_q", cu_q, _I32, 1), ("kv_base", kv_base, _I32, n), ("vis", vis, _I32, n))
+    if out is None:
+        out = torch.empty(M, hq * dh, dtype=_BF16, device=dev)
+    if scratch is None:
+        scratch = attention_kv8_scratch(hq, hkv, dh, dev)
+    _tensors(name, dev, ("out", out, _BF16, M * hq * dh), ("scratch", scratch, torch.uint8, 0))
+    if error_flag is not None:
+        _tensors(name, dev, ("error_flag", error_flag, _I32, 1))
+    _call(name, dev, lib().bs_op_attention_kv8, q.data_ptr(), ld, k8.data_ptr(), v8.data_ptr(), k_scale.data_ptr(),
+          v_scale.data_ptr(), rows, out.data_ptr(), cu_q.data_ptr(), kv_base.data_ptr(), vis.data_ptr(), n, M, max_nq,
+          max_vis, hq, hkv, dh, scratch.data_ptr(), scratch.numel(), _ptr(error_flag))
+    return out

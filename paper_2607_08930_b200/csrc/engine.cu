@@ -3,12 +3,13 @@
 #include <algorithm>
 #include <cstdio>
 #include <cstring>
+#include <initializer_list>
 #include <string>
 #include <unordered_map>
 #include <vector>
 
 #include "../../include/blockserve.h"
-#include "common.cuh"
+#include "kv8.cuh"
 
 using namespace bs;
 
@@ -957,6 +958,105 @@ int bs_op_confidence(const float* logits, int n_rows, int vocab, int mask_id, in
   if (!logits || !tok || !conf || n_rows < 0 || vocab < 2) return BS_E_ARG;
   return launch_confidence(logits, n_rows, vocab, mask_id, tok, conf, (cudaStream_t)stream) == cudaSuccess ? BS_OK
                                                                                                            : BS_E_CUDA;
+}
+
+// ---- per-head norms with the rotation, and the 8-bit KV cache -------------------------------------------------
+
+static bool kv8_shape_ok(int hq, int hkv, int dh) {
+  return hkv >= 1 && hkv <= 65535 && hq >= 1 && hq % hkv == 0 && hq / hkv <= 32 && (dh == 64 || dh == 128) &&
+         (long long)(hq + 2ll * hkv) * dh <= (1 << 24);
+}
+static bool aligned16(std::initializer_list<const void*> ps) {
+  for (const void* p : ps)
+    if (!p || ((uintptr_t)p & 15)) return false;
+  return true;
+}
+static bool kv8_cache_of(const void* k8, const void* v8, const float* ks, const float* vs, long long kv_rows, Kv8Cache* c) {
+  if (!aligned16({k8, v8, ks, vs}) || kv_rows < kKv8Block || kv_rows % kKv8Block || kv_rows > 0x7fffffffll) return false;
+  *c = Kv8Cache{(unsigned char*)k8, (unsigned char*)v8, (float*)ks, (float*)vs, kv_rows / kKv8Block};
+  return true;
+}
+static bool qk_norm_args(const void* qkv, const void* q_gain, const void* k_gain, float eps, const int* tok_pos, void* q_out,
+                         int q_ld, int M, int hq, int hkv, int dh, const float* table, int max_pos, int* error_flag,
+                         QkNormArgs* a) {
+  if (M < 0 || !kv8_shape_ok(hq, hkv, dh) || max_pos < 1 || !(eps >= 0.f) || !tok_pos) return false;
+  if (!aligned16({qkv, q_out, table}) || q_ld < hq * dh || q_ld % 8 || (!q_gain != !k_gain)) return false;
+  if (q_gain && !aligned16({q_gain, k_gain})) return false;
+  *a = QkNormArgs{(const bf16*)qkv, (bf16*)q_out, q_ld, (const bf16*)q_gain, (const bf16*)k_gain, eps, tok_pos,
+                  table, max_pos, M, hq, hkv, dh, error_flag};
+  return true;
+}
+
+int bs_rope_table(float* host_table, int max_pos, int head_dim, float theta) {
+  if (!host_table || max_pos < 1 || head_dim < 2 || head_dim % 2 || !(theta > 0.f)) return BS_E_ARG;
+  build_rope_table(host_table, max_pos, head_dim, theta);
+  return BS_OK;
+}
+
+int bs_op_qk_norm_rope_kv(const void* qkv, const void* q_gain, const void* k_gain, float eps, const int* tok_pos,
+                          const int* tok_kv, void* q_out, int q_ld, void* kcache, void* vcache, long long kv_rows, int M,
+                          int n_q_heads, int n_kv_heads, int head_dim, const float* rope_table, int max_pos,
+                          int* error_flag, void* stream) {
+  if (M == 0) return BS_OK;
+  QkNormArgs a;
+  if (!qk_norm_args(qkv, q_gain, k_gain, eps, tok_pos, q_out, q_ld, M, n_q_heads, n_kv_heads, head_dim, rope_table, max_pos,
+                    error_flag, &a) || !tok_kv || !aligned16({kcache, vcache}) || kv_rows < 1)
+    return BS_E_ARG;
+  return launch_qk_norm_rope_kv(a, tok_kv, (bf16*)kcache, (bf16*)vcache, kv_rows, (cudaStream_t)stream) == cudaSuccess
+             ? BS_OK : BS_E_CUDA;
+}
+
+int bs_op_qk_norm_rope_kv8(const void* qkv, const void* q_gain, const void* k_gain, float eps, const int* tok_pos,
+                           const int* cu_q, const int* kv_base, const int* kv_at, const int* kv_len, int n_rows,
+                           void* q_out, int q_ld, void* k8, void* v8, float* k_scale, float* v_scale, long long kv_rows,
+                           int M, int n_q_heads, int n_kv_heads, int head_dim, const float* rope_table, int max_pos,
+                           int* error_flag, void* stream) {
+  if (M == 0 || n_rows == 0) return BS_OK;
+  QkNormArgs a;
+  Kv8Cache c;
+  if (!qk_norm_args(qkv, q_gain, k_gain, eps, tok_pos, q_out, q_ld, M, n_q_heads, n_kv_heads, head_dim, rope_table, max_pos,
+                    error_flag, &a) || !kv8_cache_of(k8, v8, k_scale, v_scale, kv_rows, &c) ||
+      !cu_q || !kv_base || !kv_at || !kv_len || n_rows < 1)
+    return BS_E_ARG;
+  cudaError_t r = launch_qk_norm_rope_kv8(a, cu_q, kv_base, kv_at, kv_len, n_rows, c, (cudaStream_t)stream);
+  return r == cudaSuccess ? BS_OK : (r == cudaErrorInvalidValue ? BS_E_ARG : BS_E_CUDA);
+}
+
+int bs_op_kv8_read(const void* k8, const void* v8, const float* k_scale, const float* v_scale, long long kv_rows,
+                   const int* cu, const int* kv_base, const int* kv_at, int n_rows, int total, int n_kv_heads,
+                   int head_dim, void* k_out, void* v_out, int* error_flag, void* stream) {
+  if (total == 0 || n_rows == 0) return BS_OK;
+  Kv8Cache c;
+  if (total < 0 || n_rows < 1 || !kv8_shape_ok(n_kv_heads, n_kv_heads, head_dim) || !aligned16({k_out, v_out}) || !cu ||
+      !kv_base || !kv_at || !kv8_cache_of(k8, v8, k_scale, v_scale, kv_rows, &c))
+    return BS_E_ARG;
+  return launch_kv8_read(c, cu, kv_base, kv_at, n_rows, total, n_kv_heads, head_dim, (bf16*)k_out, (bf16*)v_out, error_flag,
+                         (cudaStream_t)stream) == cudaSuccess ? BS_OK : BS_E_CUDA;
+}
+
+size_t bs_op_attention_kv8_scratch_bytes(int n_q_heads, int n_kv_heads, int head_dim) {
+  if (!kv8_shape_ok(n_q_heads, n_kv_heads, head_dim)) return 0;
+  return attention_kv8_scratch_bytes(n_q_heads, n_kv_heads, head_dim);
+}
+
+int bs_op_attention_kv8(const void* q, int q_ld, const void* k8, const void* v8, const float* k_scale,
+                        const float* v_scale, long long kv_rows, void* out, const int* cu_q, const int* kv_base,
+                        const int* vis, int n_rows, int M, int max_nq, int max_vis, int n_q_heads, int n_kv_heads,
+                        int head_dim, void* scratch, size_t scratch_bytes, int* error_flag, void* stream) {
+  if (M == 0 || n_rows == 0) return BS_OK;
+  AttnKv8Args a;
+  if (M < 0 || n_rows < 1 || n_rows > kAttnKv8MaxRows || max_nq < 0 || max_vis < 0 ||
+      !kv8_shape_ok(n_q_heads, n_kv_heads, head_dim) || q_ld < n_q_heads * head_dim || q_ld % 8 ||
+      !aligned16({q, out, scratch}) || ((uintptr_t)scratch & 255) || !cu_q || !kv_base || !vis ||
+      scratch_bytes < attention_kv8_scratch_bytes(n_q_heads, n_kv_heads, head_dim) ||
+      !kv8_cache_of(k8, v8, k_scale, v_scale, kv_rows, &a.cache))
+    return BS_E_ARG;
+  a.q = (const bf16*)q; a.q_ld = q_ld; a.out = (bf16*)out;
+  a.cu_q = cu_q; a.kv_base = kv_base; a.vis = vis;
+  a.n_rows = n_rows; a.M = M; a.max_nq = max_nq; a.max_vis = max_vis;
+  a.hq = n_q_heads; a.hkv = n_kv_heads; a.dh = head_dim;
+  a.scratch = scratch; a.scratch_bytes = scratch_bytes; a.error_flag = error_flag;
+  return launch_attention_kv8(a, (cudaStream_t)stream) == cudaSuccess ? BS_OK : BS_E_CUDA;
 }
 
 }  // extern "C"
