@@ -86,16 +86,18 @@ def span(codes: np.ndarray, scales: np.ndarray, base: int, at: int, n: int) -> n
 
 
 def attention(q: np.ndarray, k: np.ndarray, v: np.ndarray):
-    """q [n, hq, dh], k / v [vis, hkv, dh] -> (out [n, hq, dh], sum_j p_j |v_j|, largest sum_d |q_d k_jd| / sqrt(dh))."""
+    """q [n, hq, dh], k / v [vis, hkv, dh] -> (out [n, hq, dh], sum_j p_j |v_j|, largest sum_d |q_d k_jd| / sqrt(dh),
+    largest max_d |q_d| sum_d |k_jd| / sqrt(dh))."""
     n, hq, dh = q.shape
-    out, mag, dot = np.zeros(q.shape), np.zeros(q.shape), 0.0
+    out, mag, dot, flat = np.zeros(q.shape), np.zeros(q.shape), 0.0, 0.0
     if len(k) == 0:
-        return out, mag, dot
+        return out, mag, dot, flat
     g = hq // k.shape[1]
     for h in range(hq):
         z = q[:, h] @ k[:, h // g].T / np.sqrt(dh)
         dot = max(dot, float((np.abs(q[:, h]) @ np.abs(k[:, h // g]).T).max() / np.sqrt(dh)))
+        flat = max(flat, float(np.abs(q[:, h]).max() * np.abs(k[:, h // g]).sum(1).max() / np.sqrt(dh)))
         p = np.exp(z - z.max(1, keepdims=True))
         p /= p.sum(1, keepdims=True)
         out[:, h], mag[:, h] = p @ v[:, h // g], p @ np.abs(v[:, h // g])
-    return out, mag, dot
+    return out, mag, dot, flat

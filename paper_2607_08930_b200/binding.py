@@ -7,6 +7,7 @@ creating an engine without a CUDA device, raises: there is no CPU path.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import Dict, Optional, Sequence
 
@@ -447,30 +448,32 @@ def op_confidence(logits: torch.Tensor, mask_id: int):
 # ---- per-head norms with the rotation, and the 8-bit KV cache -----------------------------------------------------
 
 KV8_BLOCK, KV8_MAX_ROWS = 32, 1024
-_BF16, _F32, _I32, _E4M3 = torch.bfloat16, torch.float32, torch.int32, torch.float8_e4m3fn
+_BF16, _F32, _I32, _E4M3, _U8 = torch.bfloat16, torch.float32, torch.int32, torch.float8_e4m3fn, torch.uint8
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda dev: torch.cuda.current_stream(dev).cuda_stream)      # the handle alone: a fiftieth of the Stream object's cost
 
 
 def _refuse(name: str, why: str) -> None:
     raise BlockServeError(BS_E_ARG, f"{name}: {why}")
 
 
-def _tensors(name: str, device: torch.device, *what) -> None:
-    """what: (argument name, tensor, dtype, least number of elements): contiguous, on `device`."""
-    for arg, t, dtype, least in what:
-        if t.dtype is not dtype or t.device != device or not t.is_contiguous() or t.numel() < least:
-            _refuse(name, f"{arg} must be a contiguous {dtype} tensor of at least {least} elements on {device}, "
-                          f"got {tuple(t.shape)} {t.dtype} on {t.device}")
+def _need(name: str, dev: int, dtype: torch.dtype, least: int, args: str, *tensors) -> None:
+    """Every tensor (named by the words of `args`): contiguous, on device `dev`, `dtype`, at least `least` elements."""
+    for i, t in enumerate(tensors):
+        if t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous() or t.numel() < least:
+            _refuse(name, f"{args.split()[i]} must be a contiguous {dtype} tensor of at least {least} elements on the "
+                          f"operator's device, got {tuple(t.shape)} {t.dtype} on {t.device}")
 
 
-def _call(name: str, device: torch.device, fn, *args) -> None:
-    """The library's kernels go to the device's current stream, whatever device is current."""
-    if device.type != "cuda":
+def _call(name: str, dev: int, fn, *args) -> None:
+    """The library's kernels go to the current stream of the tensors' device, whatever device is current."""
+    if dev < 0:
         _refuse(name, "the operators run on CUDA tensors only")
-    if torch.cuda.current_device() == device.index:
-        rc = fn(*args, torch.cuda.current_stream().cuda_stream)
+    if torch.cuda.current_device() == dev:
+        rc = fn(*args, _raw_stream(dev))
     else:
-        with torch.cuda.device(device):
-            rc = fn(*args, torch.cuda.current_stream().cuda_stream)
+        with torch.cuda.device(dev):
+            rc = fn(*args, _raw_stream(dev))
     if rc != BS_OK:
         _check_op(rc, name)
 
@@ -492,38 +495,42 @@ def kv8_cache(kv_rows: int, hkv: int, dh: int, device="cuda"):
             torch.empty(n, hkv, dtype=_F32, device=device), torch.empty(n, hkv, dtype=_F32, device=device))
 
 
-def _kv8_rows(name: str, device, k8, v8, k_scale, v_scale) -> int:
-    if k8.dim() != 4 or k8.shape[2] != KV8_BLOCK or v8.shape != k8.shape or k_scale.shape != k8.shape[:2] or \
-            v_scale.shape != k8.shape[:2]:
+def _kv8_shape(name: str, dev: int, k8, v8, k_scale, v_scale):
+    """(kv_rows, kv heads, head_dim) of an 8-bit cache."""
+    shape = k8.shape
+    if len(shape) != 4 or shape[2] != KV8_BLOCK or v8.shape != shape or k_scale.shape != shape[:2] or \
+            v_scale.shape != shape[:2]:
         _refuse(name, "an 8-bit cache is codes [blocks, kv heads, 32, head_dim] and scales [blocks, kv heads]")
-    _tensors(name, device, ("k8", k8, _E4M3, 1), ("v8", v8, _E4M3, 1), ("k_scale", k_scale, _F32, 1),
-             ("v_scale", v_scale, _F32, 1))
-    return k8.shape[0] * KV8_BLOCK
+    _need(name, dev, _E4M3, 1, "k8 v8", k8, v8)
+    _need(name, dev, _F32, 1, "k_scale v_scale", k_scale, v_scale)
+    return shape[0] * KV8_BLOCK, shape[1], shape[3]
 
 
-def _rows_of(name: str, t: torch.Tensor, arg: str, device, least: int) -> int:
-    """Row stride of a bf16 matrix whose rows are dense."""
-    if t.dim() != 2 or t.dtype is not _BF16 or t.device != device or t.shape[1] < least or \
+def _row_stride(name: str, dev: int, arg: str, t: torch.Tensor, rows: int, width: int) -> int:
+    """Row stride of a bf16 matrix of at least `rows` rows of `width` adjacent elements."""
+    if t.dim() != 2 or t.dtype is not _BF16 or t.get_device() != dev or t.shape[0] < rows or t.shape[1] < width or \
             (t.stride(1) != 1 and t.numel() > 0):
-        _refuse(name, f"{arg} must be a bfloat16 matrix on {device} with rows of at least {least} adjacent elements")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+        _refuse(name, f"{arg} must be a bfloat16 matrix of at least {rows} rows of {width} adjacent elements on the "
+                      f"operator's device, got {tuple(t.shape)} {t.dtype} on {t.device}")
+    return t.stride(0) if rows > 1 else max(t.stride(0), t.shape[1])
 
 
-def _norm_inputs(name: str, qkv, q_gain, k_gain, tok_pos, hq, hkv, dh, rope, q_out):
-    dev, M, width = qkv.device, qkv.shape[0], (hq + 2 * hkv) * dh
+def _norm_inputs(name: str, dev: int, qkv, q_gain, k_gain, tok_pos, hq, hkv, dh, rope, q_out, error_flag):
+    M, width = qkv.shape[0], (hq + 2 * hkv) * dh
     if qkv.dim() != 2 or qkv.shape[1] != width or rope.dim() != 3 or rope.shape[1:] != (dh // 2, 2):
         _refuse(name, f"qkv must be [M, {width}] and rope_table [max_pos, {dh // 2}, 2]")
-    _tensors(name, dev, ("qkv", qkv, _BF16, 0), ("tok_pos", tok_pos, _I32, M), ("rope_table", rope, _F32, dh))
+    _need(name, dev, _BF16, 0, "qkv", qkv)
+    _need(name, dev, _I32, M, "tok_pos", tok_pos)
+    _need(name, dev, _F32, dh, "rope_table", rope)
     if (q_gain is None) != (k_gain is None):
         _refuse(name, "q_gain and k_gain are given together or not at all")
     if q_gain is not None:
-        _tensors(name, dev, ("q_gain", q_gain, _BF16, dh), ("k_gain", k_gain, _BF16, dh))
+        _need(name, dev, _BF16, dh, "q_gain k_gain", q_gain, k_gain)
+    if error_flag is not None:
+        _need(name, dev, _I32, 1, "error_flag", error_flag)
     if q_out is None:
-        q_out = torch.empty(M, hq * dh, dtype=_BF16, device=dev)
-    ld = _rows_of(name, q_out, "q_out", dev, hq * dh)
-    if q_out.shape[0] < M:
-        _refuse(name, f"q_out needs {M} rows")
-    return dev, M, q_out, ld
+        q_out = torch.empty(M, hq * dh, dtype=_BF16, device=qkv.device)
+    return M, q_out, _row_stride(name, dev, "q_out", q_out, M, hq * dh)
 
 
 def op_qk_norm_rope_kv(qkv, q_gain, k_gain, eps: float, tok_pos, tok_kv, kcache, vcache, hq: int, hkv: int, dh: int,
@@ -532,16 +539,15 @@ def op_qk_norm_rope_kv(qkv, q_gain, k_gain, eps: float, tok_pos, tok_kv, kcache,
     """RMS norm of every query and key head (gains bf16 [dh], or None for both: no norm), rotation at tok_pos, K / V to
     rows tok_kv of the bf16 caches [kv_rows, hkv, dh] (tok_kv < 0: the token is skipped).  Returns the queries
     [M, hq * dh]; q_out = qkv rotates in place.  error_flag (int32 [1]) gets >= 100 where an index was out of range."""
-    name = "bs_op_qk_norm_rope_kv"
-    dev, M, q_out, ld = _norm_inputs(name, qkv, q_gain, k_gain, tok_pos, hq, hkv, dh, rope_table, q_out)
+    name, dev = "bs_op_qk_norm_rope_kv", qkv.get_device()
+    M, q_out, ld = _norm_inputs(name, dev, qkv, q_gain, k_gain, tok_pos, hq, hkv, dh, rope_table, q_out, error_flag)
     if kcache.dim() != 3 or kcache.shape[1:] != (hkv, dh) or vcache.shape != kcache.shape:
         _refuse(name, f"the caches must be [kv_rows, {hkv}, {dh}]")
-    _tensors(name, dev, ("kcache", kcache, _BF16, 1), ("vcache", vcache, _BF16, 1), ("tok_kv", tok_kv, _I32, M))
-    if error_flag is not None:
-        _tensors(name, dev, ("error_flag", error_flag, _I32, 1))
-    _call(name, dev, lib().bs_op_qk_norm_rope_kv, qkv.data_ptr(), _ptr(q_gain), _ptr(k_gain), eps, tok_pos.data_ptr(),
-          tok_kv.data_ptr(), q_out.data_ptr(), ld, kcache.data_ptr(), vcache.data_ptr(), kcache.shape[0], M, hq, hkv, dh,
-          rope_table.data_ptr(), rope_table.shape[0], _ptr(error_flag))
+    _need(name, dev, _BF16, 1, "kcache vcache", kcache, vcache)
+    _need(name, dev, _I32, M, "tok_kv", tok_kv)
+    _call(name, dev, (_lib or lib()).bs_op_qk_norm_rope_kv, qkv.data_ptr(), _ptr(q_gain), _ptr(k_gain), eps,
+          tok_pos.data_ptr(), tok_kv.data_ptr(), q_out.data_ptr(), ld, kcache.data_ptr(), vcache.data_ptr(),
+          kcache.shape[0], M, hq, hkv, dh, rope_table.data_ptr(), rope_table.shape[0], _ptr(error_flag))
     return q_out
 
 
@@ -551,47 +557,52 @@ def op_qk_norm_rope_kv8(qkv, q_gain, k_gain, eps: float, tok_pos, cu_q, kv_base,
     """op_qk_norm_rope_kv with the 8-bit cache of kv8_cache(): row i's tokens [cu_q[i], cu_q[i+1]) go to cache positions
     kv_at[i].. of its slab (kv_base[i], a multiple of 32), where positions [0, kv_len[i]) held valid rows before.
     Blocks it touches are re-scaled over everything valid in them."""
-    name = "bs_op_qk_norm_rope_kv8"
-    dev, M, q_out, ld = _norm_inputs(name, qkv, q_gain, k_gain, tok_pos, hq, hkv, dh, rope_table, q_out)
-    rows = _kv8_rows(name, dev, k8, v8, k_scale, v_scale)
-    if k8.shape[1] != hkv or k8.shape[3] != dh:
-        _refuse(name, f"the cache holds {k8.shape[1]} heads of {k8.shape[3]}, not {hkv} of {dh}")
+    name, dev = "bs_op_qk_norm_rope_kv8", qkv.get_device()
+    M, q_out, ld = _norm_inputs(name, dev, qkv, q_gain, k_gain, tok_pos, hq, hkv, dh, rope_table, q_out, error_flag)
+    rows, heads, width = _kv8_shape(name, dev, k8, v8, k_scale, v_scale)
+    if heads != hkv or width != dh:
+        _refuse(name, f"the cache holds {heads} heads of {width}, not {hkv} of {dh}")
     n = cu_q.numel() - 1
-    _tensors(name, dev, ("cu_q", cu_q, _I32, 1), ("kv_base", kv_base, _I32, n), ("kv_at", kv_at, _I32, n),
-             ("kv_len", kv_len, _I32, n))
-    if error_flag is not None:
-        _tensors(name, dev, ("error_flag", error_flag, _I32, 1))
-    _call(name, dev, lib().bs_op_qk_norm_rope_kv8, qkv.data_ptr(), _ptr(q_gain), _ptr(k_gain), eps, tok_pos.data_ptr(),
-          cu_q.data_ptr(), kv_base.data_ptr(), kv_at.data_ptr(), kv_len.data_ptr(), n, q_out.data_ptr(), ld, k8.data_ptr(),
-          v8.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), rows, M, hq, hkv, dh, rope_table.data_ptr(),
-          rope_table.shape[0], _ptr(error_flag))
+    _need(name, dev, _I32, 1, "cu_q", cu_q)
+    _need(name, dev, _I32, n, "kv_base kv_at kv_len", kv_base, kv_at, kv_len)
+    _call(name, dev, (_lib or lib()).bs_op_qk_norm_rope_kv8, qkv.data_ptr(), _ptr(q_gain), _ptr(k_gain), eps,
+          tok_pos.data_ptr(), cu_q.data_ptr(), kv_base.data_ptr(), kv_at.data_ptr(), kv_len.data_ptr(), n,
+          q_out.data_ptr(), ld, k8.data_ptr(), v8.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), rows, M, hq, hkv, dh,
+          rope_table.data_ptr(), rope_table.shape[0], _ptr(error_flag))
     return q_out
 
 
 def op_kv8_read(k8, v8, k_scale, v_scale, cu, kv_base, kv_at, total: int, k_out: Optional[torch.Tensor] = None,
                 v_out: Optional[torch.Tensor] = None, error_flag: Optional[torch.Tensor] = None):
     """Cache positions [kv_at[i], kv_at[i] + cu[i+1] - cu[i]) of every row, packed: bf16 (K, V) [total, hkv, dh]."""
-    name = "bs_op_kv8_read"
-    dev = k8.device
-    rows = _kv8_rows(name, dev, k8, v8, k_scale, v_scale)
-    hkv, dh, n = k8.shape[1], k8.shape[3], cu.numel() - 1
-    _tensors(name, dev, ("cu", cu, _I32, 1), ("kv_base", kv_base, _I32, n), ("kv_at", kv_at, _I32, n))
+    name, dev = "bs_op_kv8_read", k8.get_device()
+    rows, hkv, dh = _kv8_shape(name, dev, k8, v8, k_scale, v_scale)
+    n = cu.numel() - 1
+    _need(name, dev, _I32, 1, "cu", cu)
+    _need(name, dev, _I32, n, "kv_base kv_at", kv_base, kv_at)
+    if total < 0:
+        _refuse(name, "total must not be negative")
     if k_out is None:
-        k_out = torch.empty(total, hkv, dh, dtype=_BF16, device=dev)
+        k_out = torch.empty(total, hkv, dh, dtype=_BF16, device=k8.device)
     if v_out is None:
-        v_out = torch.empty(total, hkv, dh, dtype=_BF16, device=dev)
-    _tensors(name, dev, ("k_out", k_out, _BF16, total * hkv * dh), ("v_out", v_out, _BF16, total * hkv * dh))
+        v_out = torch.empty(total, hkv, dh, dtype=_BF16, device=k8.device)
+    _need(name, dev, _BF16, total * hkv * dh, "k_out v_out", k_out, v_out)
     if error_flag is not None:
-        _tensors(name, dev, ("error_flag", error_flag, _I32, 1))
-    _call(name, dev, lib().bs_op_kv8_read, k8.data_ptr(), v8.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), rows,
-          cu.data_ptr(), kv_base.data_ptr(), kv_at.data_ptr(), n, total, hkv, dh, k_out.data_ptr(), v_out.data_ptr(),
+        _need(name, dev, _I32, 1, "error_flag", error_flag)
+    _call(name, dev, (_lib or lib()).bs_op_kv8_read, k8.data_ptr(), v8.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
+          rows, cu.data_ptr(), kv_base.data_ptr(), kv_at.data_ptr(), n, total, hkv, dh, k_out.data_ptr(), v_out.data_ptr(),
           _ptr(error_flag))
     return k_out, v_out
 
 
+@functools.lru_cache(maxsize=None)
+def attention_kv8_scratch_bytes(hq: int, hkv: int, dh: int) -> int:
+    return max(256, lib().bs_op_attention_kv8_scratch_bytes(hq, hkv, dh))
+
+
 def attention_kv8_scratch(hq: int, hkv: int, dh: int, device="cuda") -> torch.Tensor:
     """Scratch of op_attention_kv8, for callers that keep it (calls that share it must be ordered)."""
-    return torch.empty(max(256, lib().bs_op_attention_kv8_scratch_bytes(hq, hkv, dh)), dtype=torch.uint8, device=device)
+    return torch.empty(attention_kv8_scratch_bytes(hq, hkv, dh), dtype=_U8, device=device)
 
 
 def op_attention_kv8(q, k8, v8, k_scale, v_scale, cu_q, kv_base, vis, hq: int, max_nq: int = 0, max_vis: int = 0,
@@ -600,20 +611,23 @@ def op_attention_kv8(q, k8, v8, k_scale, v_scale, cu_q, kv_base, vis, hq: int, m
     """Attention of packed queries (q [M, >= hq * dh]: q_out of the operators above, or a qkv buffer) over their rows'
     cache positions [0, vis[i]) of the 8-bit cache; rows with vis = 0 give zeros.  max_nq / max_vis (0: unknown): the
     largest number of query tokens and of visible positions of a row.  Without `scratch` it comes from torch's allocator."""
-    name = "bs_op_attention_kv8"
-    dev = q.device
-    rows = _kv8_rows(name, dev, k8, v8, k_scale, v_scale)
-    hkv, dh, n, M = k8.shape[1], k8.shape[3], cu_q.numel() - 1, q.shape[0]
-    ld = _rows_of(name, q, "q", dev, hq * dh)
-    _tensors(name, dev, ("cu_q", cu_q, _I32, 1), ("kv_base", kv_base, _I32, n), ("vis", vis, _I32, n))
+    name, dev = "bs_op_attention_kv8", q.get_device()
+    rows, hkv, dh = _kv8_shape(name, dev, k8, v8, k_scale, v_scale)
+    n, M = cu_q.numel() - 1, q.shape[0]
+    ld = _row_stride(name, dev, "q", q, M, hq * dh)
+    _need(name, dev, _I32, 1, "cu_q", cu_q)
+    _need(name, dev, _I32, n, "kv_base vis", kv_base, vis)
     if out is None:
-        out = torch.empty(M, hq * dh, dtype=_BF16, device=dev)
+        out = torch.empty(M, hq * dh, dtype=_BF16, device=q.device)
+    else:
+        _need(name, dev, _BF16, M * hq * dh, "out", out)
     if scratch is None:
-        scratch = attention_kv8_scratch(hq, hkv, dh, dev)
-    _tensors(name, dev, ("out", out, _BF16, M * hq * dh), ("scratch", scratch, torch.uint8, 0))
+        scratch = torch.empty(attention_kv8_scratch_bytes(hq, hkv, dh), dtype=_U8, device=q.device)
+    else:
+        _need(name, dev, _U8, 0, "scratch", scratch)
     if error_flag is not None:
-        _tensors(name, dev, ("error_flag", error_flag, _I32, 1))
-    _call(name, dev, lib().bs_op_attention_kv8, q.data_ptr(), ld, k8.data_ptr(), v8.data_ptr(), k_scale.data_ptr(),
-          v_scale.data_ptr(), rows, out.data_ptr(), cu_q.data_ptr(), kv_base.data_ptr(), vis.data_ptr(), n, M, max_nq,
-          max_vis, hq, hkv, dh, scratch.data_ptr(), scratch.numel(), _ptr(error_flag))
+        _need(name, dev, _I32, 1, "error_flag", error_flag)
+    _call(name, dev, (_lib or lib()).bs_op_attention_kv8, q.data_ptr(), ld, k8.data_ptr(), v8.data_ptr(),
+          k_scale.data_ptr(), v_scale.data_ptr(), rows, out.data_ptr(), cu_q.data_ptr(), kv_base.data_ptr(), vis.data_ptr(),
+          n, M, max_nq, max_vis, hq, hkv, dh, scratch.data_ptr(), scratch.numel(), _ptr(error_flag))
     return out

@@ -3,11 +3,12 @@
 //
 //   s_j = q . k_j / sqrt(dh),   out = sum_j e^(s_j - m) v_j / sum_j e^(s_j - m)
 //
-// with k_j = ks_b c_j and v_j = vs_b c'_j for the codes c, c' and the two scales of cache block b.  The codes go to the
-// tensor cores as fp16 (exact: e4m3 needs 4 significant bits and 2^-9 .. 448); ks_b multiplies the finished fp32 scores
-// and vs_b the output accumulator, so no scale is ever rounded into an operand.  Queries become fp16 after a power of
-// two per query row has brought their largest element into [1, 2): bf16's 8 bits fit fp16's 11, what drops below 2^-24
-// of the row's largest element is far below the fp32 sum's own rounding.
+// with k_j = ks_b c_j and v_j = vs_b c'_j for the codes c, c' and the two scales of cache block b.  No scale is rounded
+// into an operand: ks_b multiplies the finished fp32 scores, and the weight that meets the codes of V is
+//
+//   w_j = vs_b e^(s_j - m) = 2^(t_j - M),   t_j = log2(e) s_j + log2(vs_b),   M: running maximum of t
+//
+// so that weights are largest where the summands w_j c'_j are; the denominator takes w_j / vs_b.
 #include <math.h>
 
 #include <algorithm>
@@ -20,10 +21,21 @@ namespace bs {
 
 namespace {
 
-__device__ __forceinline__ void mma_f16(float* c, const uint4& a, unsigned b0, unsigned b1) {
+__device__ __forceinline__ void mma_f16(float* c, const unsigned* a, unsigned b0, unsigned b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-               : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1));
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_e4m3(float* c, unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0, unsigned b1) {
+  asm volatile("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// 8 x 8 fp16 matrix across the warp (lane (g, c): row g, columns 2c, 2c + 1), transposed
+__device__ __forceinline__ unsigned transpose8x8(unsigned x) {
+  unsigned r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
 }
 __device__ __forceinline__ unsigned pack_f16(float a, float b) {
   const __half2 h = __floats2half2_rn(a, b);
@@ -34,34 +46,53 @@ __device__ __forceinline__ float exp2_fast(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-__device__ __forceinline__ uint4 load_stream(const void* p) {
+__device__ __forceinline__ float log2_fast(float x) {      // exact for powers of two
+  float y;
+  asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// 16 bytes to shared memory, or zeros (`real` = false; the source is then not read)
+__device__ __forceinline__ void copy_async16(unsigned dst, const void* src, bool real) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ uint4 lds128(unsigned at) {
   uint4 v;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
   return v;
 }
-__device__ __forceinline__ uint2 load_stream2(const void* p) {
+__device__ __forceinline__ uint2 lds64(unsigned at) {
   uint2 v;
-  asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
+  asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at));
   return v;
 }
 
 // ---- streaming kernel ---------------------------------------------------------------------------------------
 //
 // Few query rows per kv head (single tokens, block steps without grouped heads): bound by the bytes of the cache.
-// A work item is (row, kv head, tile of 16 MT flattened (token, head-in-group) query rows); its cost is the row's
-// number of cache blocks.  All items' blocks form one line, which the CTAs of a single resident wave share evenly:
-// CTA c takes blocks [c T / G, (c + 1) T / G), whatever the rows' lengths are.  An item that a CTA holds whole is
-// written out directly; a cut one leaves partial (output, maximum, sum) parts, at most two per CTA, that a second small
-// kernel merges in order.
+// A work item is (row, kv head, tile of 8 NQ flattened (token, head-in-group) query rows).  All items' cache blocks
+// form one line - an item counts kItemCost blocks more than it has, about what starting and ending it costs - which the
+// CTAs of a single resident wave share evenly: CTA c takes units [c T / G, (c + 1) T / G), whatever the rows' lengths
+// are.  An item that a CTA holds whole is written out directly; a cut one leaves partial (output, reference, sum) parts,
+// at most two per CTA, that a second small kernel merges in order.
 //
-// Inside a CTA every warp takes whole cache blocks (32 keys) on its own, straight from global memory into registers:
-// the order of the dims in the scores' k index and of the dims in the output's n index is free, and is chosen so that
-// a lane's 16-byte loads are its mma.sync operand registers - no shared memory, no barrier, no shuffle of K or V.
+// Inside a CTA every warp takes whole cache blocks (32 keys) on its own, through a ring of shared-memory stages that
+// no other warp touches (cp.async, no barrier): the next blocks are on their way while this one is computed.  Rows
+// behind the row's end arrive as zeros, whatever the cache holds there.
+//
+// Keys are the rows (M) of both products and the queries their columns (N), so that 8 query rows - a group of heads of
+// one token - fill an instruction.  Scores: the codes of K go to the tensor cores as they are (e4m3); a query element,
+// after a power of two per query row has brought the row's largest into [128, 256), is the sum of two e4m3 values: the
+// nearest one and the rest (4 + 4 significant bits, bf16 has 8; exact above 2^-10 of the row's largest element, and
+// within 2^-17 of that element below).  Output: V's codes as fp16 (exact) against weights in fp16, transposed in
+// registers (movmatrix).  The order of the dims in the scores' k index and of the dims in the output's m index is free,
+// and is chosen so that a lane's 16-byte shared-memory loads are its operand registers; a 16-byte chunk's place in its
+// 128-byte line is turned by the line's number, which keeps those loads free of bank conflicts.
 constexpr int kStreamWarps = 4;
 constexpr int kStreamThreads = kStreamWarps * 32;
-constexpr int kMaxStreamCtas = 512;
-// Probabilities are formed against a reference kBias below the running maximum (log2 units), which is moved only when
-// the maximum has grown kGrow above it: they stay below 2^kGrow in fp16 and keep full precision down to 2^-20 of the
+constexpr int kMaxStreamCtas = 592;
+constexpr int kItemCost = 8;
+// Weights are formed against a reference kBias below the running maximum (log2 units), which is moved only when the
+// maximum has grown kGrow above it: they stay below 2^kGrow in fp16 and keep full precision down to 2^-20 of the
 // largest one.
 constexpr float kBias = 6.f, kGrow = 14.f;
 
@@ -74,13 +105,19 @@ struct StreamParams {
   const int* kv_base;
   const int* vis;
   int n_rows, M, hq, hkv, tq;
-  long long* prefix;     // scratch: [n_rows + 1] blocks before each row, then the number of CTAs that share them
-  float* part_o;         // scratch: [2 CTAs][16 MT][DH]
-  float2* part_ml;       // scratch: [2 CTAs][16 MT]
+  long long* prefix;     // scratch: [n_rows + 1] units before each row, then the number of CTAs that share them
+  float* part_o;         // scratch: [2 CTAs][8 NQ][DH]
+  float2* part_ml;       // scratch: [2 CTAs][8 NQ]
   int* error_flag;
 };
 
-struct RowInfo { int t0, n, vis, nb, tiles; long long base; };
+struct RowInfo {
+  int t0, n, vis, nb, tiles;
+  long long base;
+  // units of one item, and of the row
+  __device__ __forceinline__ int item_units() const { return nb > 0 ? nb + kItemCost : 0; }
+  __device__ __forceinline__ long long units(int hkv) const { return (long long)tiles * hkv * item_units(); }
+};
 
 __device__ __forceinline__ bool row_info(const int* cu_q, const int* kv_base, const int* vis, long long n_blocks, int M,
                                          int tq, int r, RowInfo& w) {
@@ -98,47 +135,58 @@ __device__ __forceinline__ bool row_info(const int* cu_q, const int* kv_base, co
   return ok;
 }
 
-// First block of CTA c's share, and the CTA that holds block u.
+// First unit of CTA c's share, and the CTA that holds unit u.
 __device__ __forceinline__ long long share_start(long long c, long long total, long long ctas) { return c * total / ctas; }
 __device__ __forceinline__ int share_of(long long u, long long total, long long ctas) { return (int)(((u + 1) * ctas - 1) / total); }
 
-template <int DH, int MT>
-constexpr int stream_smem() {
-  return MT * (DH / 16) * 32 * 16 +                                   // query fragments
-         kStreamWarps / 2 * 16 * MT * (DH + 4) * 4 +                  // outputs of half the warps
-         kStreamWarps * 16 * MT * 8 + 16 * MT * 4 +                   // (reference, sum) per warp and row; query scales
-         (kAttnKv8MaxRows + 1) * 8;                                   // prefix
-}
+template <int DH>
+constexpr int kTileBytes = kKv8Block * DH;           // one block of one head, K or V
+template <int DH, int NQ, int STAGES>
+struct StreamSmem {
+  static constexpr int R = 8 * NQ, LDO = DH + 4;
+  static constexpr int ring = kStreamWarps * STAGES * 2 * kTileBytes<DH>;
+  static constexpr int merge = kStreamWarps * R * LDO * 4;         // the warps' outputs, over the ring when it is idle
+  static constexpr int front = ring > merge ? ring : merge;
+  static constexpr int q = NQ * (DH / 32) * 32 * 16;               // query fragments
+  static constexpr int total = 128 + front + q + kStreamWarps * R * 8 + R * 4;
+};
+constexpr int kRowsPerThread = kAttnKv8MaxRows / kStreamThreads;
 
-template <int DH, int MT>
-__global__ void __launch_bounds__(kStreamThreads, 2) k_attention_kv8_stream(StreamParams p) {
-  constexpr int KS = DH / 16;            // k steps of the scores = 32-bit words of K per lane and key
-  constexpr int NT = DH / 8;             // n tiles of the output
-  constexpr int R = 16 * MT;
-  constexpr int LDO = DH + 4;
-  extern __shared__ __align__(16) unsigned char smem[];
-  uint4* s_q = reinterpret_cast<uint4*>(smem);                               // [MT][KS][32]
-  float* s_o = reinterpret_cast<float*>(s_q + MT * KS * 32);                 // [warps / 2][R][LDO]
-  float2* s_ml = reinterpret_cast<float2*>(s_o + kStreamWarps / 2 * R * LDO);   // [warps][R]
+template <int DH, int NQ, int STAGES, int MINB>
+__global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(StreamParams p) {
+  using L = StreamSmem<DH, NQ, STAGES>;
+  constexpr int KS = DH / 32;            // k steps of the scores
+  constexpr int MD = DH / 16;            // m tiles of the output
+  constexpr int kHalves = NQ == 1 ? 2 : 1;             // (unrolled, the wider instantiations do not fit their registers)
+  constexpr int R = L::R, LDO = L::LDO, TB = kTileBytes<DH>;
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* smem = smem_raw + ((128u - (tc::smem_u32(smem_raw) & 127u)) & 127u);
+  float* s_o = reinterpret_cast<float*>(smem);                               // [warps][R][LDO]
+  uint4* s_q = reinterpret_cast<uint4*>(smem + L::front);                    // [NQ][KS][32]
+  float2* s_ml = reinterpret_cast<float2*>(smem + L::front + L::q);          // [warps][R]
   float* s_sc = reinterpret_cast<float*>(s_ml + kStreamWarps * R);           // [R]
-  long long* s_pre = reinterpret_cast<long long*>(s_sc + R);                 // [n_rows + 1]
   __shared__ long long s_warp[kStreamWarps];
+  __shared__ long long s_first;          // units before s_row
+  __shared__ int s_row;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int g = lane >> 2, c4 = lane & 3;
   const int G = p.hq / p.hkv;
   pdl_wait();
   pdl_trigger();
 
-  // ---- blocks before every row (exclusive prefix) ----
+  // ---- units before every row (exclusive prefix); the row that holds this CTA's first unit ----
+  long long before[kRowsPerThread], cost[kRowsPerThread];
   long long total = 0;
-  for (int base = 0; base < p.n_rows; base += kStreamThreads) {
-    const int r = base + tid;
+#pragma unroll
+  for (int i = 0; i < kRowsPerThread; ++i) {
+    if (i * kStreamThreads >= p.n_rows) break;
+    const int r = i * kStreamThreads + tid;
     long long w = 0;
     if (r < p.n_rows) {
       RowInfo ri;
       if (!row_info(p.cu_q, p.kv_base, p.vis, p.c.n_blocks, p.M, p.tq, r, ri) && blockIdx.x == 0 && p.error_flag)
         atomicMax(p.error_flag, 100 + SITE_ATTN_KV8);
-      w = (long long)ri.tiles * p.hkv * ri.nb;
+      w = ri.units(p.hkv);
     }
     long long inc = w;
 #pragma unroll
@@ -148,333 +196,314 @@ __global__ void __launch_bounds__(kStreamThreads, 2) k_attention_kv8_stream(Stre
     }
     if (lane == 31) s_warp[warp] = inc;
     __syncthreads();
-    long long before = total;
+    long long b = total;
+#pragma unroll
     for (int k = 0; k < kStreamWarps; ++k) {
-      if (k < warp) before += s_warp[k];
+      if (k < warp) b += s_warp[k];
       total += s_warp[k];
     }
-    if (r < p.n_rows) s_pre[r] = before + inc - w;
+    before[i] = b + inc - w;
+    cost[i] = w;
     __syncthreads();
   }
-  if (tid == 0) s_pre[p.n_rows] = total;
-  __syncthreads();
-  // a share of fewer blocks than warps would leave warps idle
-  const long long ctas = max(1ll, min((long long)gridDim.x, (total + kStreamWarps - 1) / kStreamWarps));
-  if (blockIdx.x == 0) {
-    for (int r = tid; r <= p.n_rows; r += kStreamThreads) p.prefix[r] = s_pre[r];
-    if (tid == 0) p.prefix[p.n_rows + 1] = ctas;
+  // a share holds one block per warp at least
+  const long long ctas = max(1ll, min((long long)gridDim.x, total / (kItemCost + kStreamWarps)));
+  const long long u0 = share_start(blockIdx.x, total, ctas), u1 = share_start((long long)blockIdx.x + 1, total, ctas);
+#pragma unroll
+  for (int i = 0; i < kRowsPerThread; ++i) {
+    if (i * kStreamThreads >= p.n_rows) break;
+    const int r = i * kStreamThreads + tid;
+    if (r < p.n_rows) {
+      if (blockIdx.x == 0) p.prefix[r] = before[i];
+      if (before[i] <= u0 && u0 < before[i] + cost[i]) { s_row = r; s_first = before[i]; }   // one thread at most
+    }
+  }
+  if (blockIdx.x == 0 && tid == 0) {
+    p.prefix[p.n_rows] = total;
+    p.prefix[p.n_rows + 1] = ctas;
   }
   if (total == 0 || (long long)blockIdx.x >= ctas) return;
-  const long long u0 = share_start(blockIdx.x, total, ctas), u1 = share_start((long long)blockIdx.x + 1, total, ctas);
+  __syncthreads();
+  int row = s_row;
+  long long first = s_first;
+  RowInfo ri;
+  row_info(p.cu_q, p.kv_base, p.vis, p.c.n_blocks, p.M, p.tq, row, ri);
 
-  int row = 0;
-  {   // the row that holds block u0: the last one whose prefix is <= u0 (rows without blocks share a prefix with the next)
-    int lo = 0, hi = p.n_rows;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (s_pre[mid] <= u0) lo = mid; else hi = mid;
+  // this warp's ring, and this lane's part of a block's copy: 16 bytes i * 512 + lane * 16 of K and of V
+  const unsigned ring = tc::smem_u32(smem) + (unsigned)warp * STAGES * 2 * TB;
+  const unsigned put0 = (unsigned)((lane >> 3) * 128 + (((lane & 7) ^ (lane >> 3)) << 4));
+  const unsigned put1 = (unsigned)((lane >> 3) * 128 + (((lane & 7) ^ (4 + (lane >> 3))) << 4));
+  auto fetch = [&](int stage, int b, int head) {
+    const size_t at = ((size_t)(ri.base + b) * p.hkv + head) * TB + lane * 16;
+    const unsigned dst = ring + (unsigned)stage * 2 * TB;
+    const int rows = ri.vis - b * kKv8Block;
+#pragma unroll
+    for (int i = 0; i < TB / 512; ++i) {
+      const bool real = (i * 512 + lane * 16) / DH < rows;
+      const unsigned to = dst + i * 512 + ((i & 1) ? put1 : put0);
+      copy_async16(to, p.c.k + at + i * 512, real);
+      copy_async16(to + TB, p.c.v + at + i * 512, real);
     }
-    row = lo;
-  }
+  };
 
   for (long long u = u0; u < u1;) {
-    while (s_pre[row + 1] <= u) ++row;
-    RowInfo ri;
-    row_info(p.cu_q, p.kv_base, p.vis, p.c.n_blocks, p.M, p.tq, row, ri);
-    const long long local = u - s_pre[row];
-    const int item = (int)(local / ri.nb), b0 = (int)(local % ri.nb);
+    while (u - first >= ri.units(p.hkv)) {
+      first += ri.units(p.hkv);
+      ++row;
+      row_info(p.cu_q, p.kv_base, p.vis, p.c.n_blocks, p.M, p.tq, row, ri);
+    }
+    const long long local = u - first;
+    const int per = ri.item_units(), item = (int)(local / per), at = (int)(local % per);
+    const int b0 = max(0, at - kItemCost);                        // an item's first kItemCost units hold no block
+    const int b1 = (int)min((long long)ri.nb, max(0ll, at + (u1 - u) - kItemCost));
+    const bool opens = u == u0;                                   // (the partial slot of this segment)
+    u += per - at;
+    if (b1 <= b0) continue;
     const int head = item / ri.tiles, tile = item % ri.tiles;
-    const int b1 = (int)min((long long)ri.nb, b0 + (u1 - u));
     const int t0 = ri.t0 + tile * p.tq, nt = min(p.tq, ri.t0 + ri.n - t0), nrows = nt * G;
 
-    // ---- queries: fp16 fragments in shared memory ----
-    __syncthreads();                     // the previous segment's fragments and sums are no longer read
-    for (int mt = warp; mt < MT; mt += kStreamWarps) {
-      uint2 raw[2][KS];
-      float top[2] = {0.f, 0.f};
+    __syncthreads();                     // the previous segment's fragments, sums and outputs are no longer read
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const int f = mt * 16 + g + 8 * x;
-        const bool valid = f < nrows;
-        const bf16* src = p.q + (size_t)(t0 + (valid ? f / G : 0)) * p.q_ld + (head * G + (valid ? f % G : 0)) * DH;
-#pragma unroll
-        for (int k = 0; k < KS; ++k) {
-          // k step k of lane c4 stands for dims (k / 4) 64 + 16 c4 + 4 (k % 4) ..+ 3
-          raw[x][k] = valid ? *reinterpret_cast<const uint2*>(src + (k >> 2) * 64 + c4 * 16 + (k & 3) * 4) : make_uint2(0, 0);
-          const float2 a = __bfloat1622float2(*reinterpret_cast<__nv_bfloat162*>(&raw[x][k].x));
-          const float2 b = __bfloat1622float2(*reinterpret_cast<__nv_bfloat162*>(&raw[x][k].y));
-          top[x] = fmaxf(fmaxf(top[x], fmaxf(fabsf(a.x), fabsf(a.y))), fmaxf(fabsf(b.x), fabsf(b.y)));
-        }
-        top[x] = fmaxf(top[x], __shfl_xor_sync(0xffffffffu, top[x], 1));
-        top[x] = fmaxf(top[x], __shfl_xor_sync(0xffffffffu, top[x], 2));
-      }
-      float inv[2];
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const int e = min(max((int)(__float_as_uint(top[x]) >> 23) - 127, -100), 100);
-        inv[x] = pow2i(-e);
-        if (c4 == 0) s_sc[mt * 16 + g + 8 * x] = pow2i(e) * (1.4426950408889634f * rsqrtf((float)DH));
-      }
-#pragma unroll
-      for (int k = 0; k < KS; ++k) {
-        unsigned w[2][2];
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const float2 a = __bfloat1622float2(*reinterpret_cast<__nv_bfloat162*>(&raw[x][k].x));
-          const float2 b = __bfloat1622float2(*reinterpret_cast<__nv_bfloat162*>(&raw[x][k].y));
-          w[x][0] = pack_f16(a.x * inv[x], a.y * inv[x]);
-          w[x][1] = pack_f16(b.x * inv[x], b.y * inv[x]);
-        }
-        s_q[(mt * KS + k) * 32 + lane] = make_uint4(w[0][0], w[1][0], w[0][1], w[1][1]);
-      }
+    for (int i = 0; i < STAGES - 1; ++i) {
+      if (b0 + warp + i * kStreamWarps < b1) fetch(i, b0 + warp + i * kStreamWarps, head);
+      asm volatile("cp.async.commit_group;\n" ::: "memory");
     }
-    __syncthreads();
-
-    float o[MT][NT][4];
-    float ref[MT][2], sum[MT][2], sc[MT][2];
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-#pragma unroll
-      for (int i = 0; i < NT; ++i) o[mt][i][0] = o[mt][i][1] = o[mt][i][2] = o[mt][i][3] = 0.f;
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        ref[mt][x] = -INFINITY;
-        sum[mt][x] = 0.f;
-        sc[mt][x] = s_sc[mt * 16 + g + 8 * x];
-      }
+    float ks_next = 1.f, vs_next = 1.f;
+    if (b0 + warp < b1) {
+      const size_t sa = (size_t)(ri.base + b0 + warp) * p.hkv + head;
+      ks_next = __ldg(p.c.k_scale + sa);
+      vs_next = __ldg(p.c.v_scale + sa);
     }
-    float vs_cur = 1.f;                  // the accumulator is in units of this V scale
-
-    for (int b = b0 + warp; b < b1; b += kStreamWarps) {
-      const size_t tile_at = (size_t)(ri.base + b) * p.hkv + head;
-      const unsigned char* kt = p.c.k + tile_at * (kKv8Block * DH);
-      const unsigned char* vt = p.c.v + tile_at * (kKv8Block * DH);
-      const float ks = kv8_clamp_scale(__ldg(p.c.k_scale + tile_at));
-      const float vs = kv8_clamp_scale(__ldg(p.c.v_scale + tile_at));
-      unsigned kr[4][KS];                // [key group of 8][word]
+    // ---- queries: two e4m3 fragments (nearest value, rest) of every row in shared memory ----
+    for (int nq = warp; nq < NQ; nq += kStreamWarps) {
+      const int f = nq * 8 + g;          // query row of this lane (n index of the scores)
+      const bool valid = f < nrows;
+      const bf16* src = p.q + (size_t)(t0 + (valid ? f / G : 0)) * p.q_ld + (head * G + (valid ? f % G : 0)) * DH + c4 * (DH / 4);
+      uint4 raw[KS];
+      float top = 0.f;
 #pragma unroll
-      for (int n = 0; n < 4; ++n) {
-#pragma unroll
-        for (int h = 0; h < KS / 4; ++h) {
-          const uint4 v = load_stream(kt + (n * 8 + g) * DH + h * 64 + c4 * 16);
-          kr[n][h * 4] = v.x; kr[n][h * 4 + 1] = v.y; kr[n][h * 4 + 2] = v.z; kr[n][h * 4 + 3] = v.w;
-        }
-      }
-      unsigned vr[2][4][NT / 4];         // [16 keys][key 2c, 2c+1, 2c+8, 2c+9][word]: dims g NT ..
-#pragma unroll
-      for (int n = 0; n < 2; ++n)
+      for (int k = 0; k < KS; ++k) {     // k step k of lane c4 stands for dims c4 DH / 4 + 8 k .. + 7
+        raw[k] = valid ? *reinterpret_cast<const uint4*>(src + k * 8) : make_uint4(0, 0, 0, 0);
+        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&raw[k]);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const unsigned char* src = vt + (n * 16 + 2 * c4 + (j & 1) + (j >> 1) * 8) * DH + g * NT;
-          if (NT == 16) {
-            const uint4 v = load_stream(src);
-            vr[n][j][0] = v.x; vr[n][j][1] = v.y;
-            vr[n][j][NT / 4 - 2] = v.z; vr[n][j][NT / 4 - 1] = v.w;
-          } else {
-            const uint2 v = load_stream2(src);
-            vr[n][j][0] = v.x; vr[n][j][1] = v.y;
-          }
+          const float2 x = __bfloat1622float2(h[j]);
+          top = fmaxf(top, fmaxf(fabsf(x.x), fabsf(x.y)));
         }
-      float s[MT][4][4];
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-        for (int n = 0; n < 4; ++n) s[mt][n][0] = s[mt][n][1] = s[mt][n][2] = s[mt][n][3] = 0.f;
+      }
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 100);
+      const float up = pow2i(7 - e);
+      if (c4 == 0) s_sc[f] = pow2i(e - 7) * (1.4426950408889634f * rsqrtf((float)DH));
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
-        uint4 a[MT];
+        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&raw[k]);
+        unsigned hi[2] = {0u, 0u}, lo[2] = {0u, 0u};
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) a[mt] = s_q[(mt * KS + k) * 32 + lane];
-#pragma unroll
-        for (int n = 0; n < 4; ++n) {
-          unsigned x0, x1;
-          kv8_decode4(kr[n][k], x0, x1);
-#pragma unroll
-          for (int mt = 0; mt < MT; ++mt) mma_f16(s[mt][n], a[mt], x0, x1);
+        for (int j = 0; j < 4; ++j) {
+          float2 x = __bfloat1622float2(h[j]);
+          x.x *= up;
+          x.y *= up;
+          const unsigned near = kv8_encode2(x.x, x.y);
+          const unsigned back = kv8_decode2((unsigned short)near);
+          const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&back));
+          hi[j >> 1] |= near << (16 * (j & 1));
+          lo[j >> 1] |= kv8_encode2(x.x - y.x, x.y - y.y) << (16 * (j & 1));
         }
+        s_q[(nq * KS + k) * 32 + lane] = make_uint4(hi[0], hi[1], lo[0], lo[1]);
       }
-      const int left = ri.vis - b * kKv8Block;         // keys of this block that the row sees (> 0)
-      unsigned pr[MT][4][2];                           // probabilities as A fragments
+    }
+    __syncthreads();
+
+    float o[NQ][MD][4];
+    float ref[NQ][2], sum[NQ][2], sc[NQ][2];         // of query rows nq * 8 + 2 c4 + {0, 1}
+    uint4 qf[NQ == 1 ? KS : 1];
+    if (NQ == 1) {
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-        float mx[2] = {-INFINITY, -INFINITY};
+      for (int k = 0; k < KS; ++k) qf[NQ == 1 ? k : 0] = s_q[k * 32 + lane];
+    }
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const float f = sc[mt][x] * ks;
+    for (int nq = 0; nq < NQ; ++nq) {
 #pragma unroll
-          for (int n = 0; n < 4; ++n)
+      for (int i = 0; i < MD; ++i) o[nq][i][0] = o[nq][i][1] = o[nq][i][2] = o[nq][i][3] = 0.f;
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              float& v = s[mt][n][2 * x + j];
-              v = n * 8 + 2 * c4 + j < left ? v * f : -INFINITY;
-              mx[x] = fmaxf(mx[x], v);
-            }
-          mx[x] = fmaxf(mx[x], __shfl_xor_sync(0xffffffffu, mx[x], 1));
-          mx[x] = fmaxf(mx[x], __shfl_xor_sync(0xffffffffu, mx[x], 2));
-        }
-        const bool grow0 = mx[0] > ref[mt][0] + kGrow, grow1 = mx[1] > ref[mt][1] + kGrow;
-        if (__any_sync(0xffffffffu, grow0 || grow1 || vs != vs_cur)) {
-          const float turn = vs_cur / vs;              // exact: both are powers of two
-          float f0 = 1.f, f1 = 1.f;
-          if (grow0) { f0 = exp2_fast(ref[mt][0] - (mx[0] - kBias)); ref[mt][0] = mx[0] - kBias; }
-          if (grow1) { f1 = exp2_fast(ref[mt][1] - (mx[1] - kBias)); ref[mt][1] = mx[1] - kBias; }
-          sum[mt][0] *= f0;
-          sum[mt][1] *= f1;
-          f0 *= turn;
-          f1 *= turn;
-#pragma unroll
-          for (int i = 0; i < NT; ++i) {
-            o[mt][i][0] *= f0; o[mt][i][1] *= f0;
-            o[mt][i][2] *= f1; o[mt][i][3] *= f1;
-          }
-        }
-#pragma unroll
-        for (int n = 0; n < 4; ++n) {
-#pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            const float e0 = exp2_fast(s[mt][n][2 * x] - ref[mt][x]), e1 = exp2_fast(s[mt][n][2 * x + 1] - ref[mt][x]);
-            sum[mt][x] += e0 + e1;
-            pr[mt][n][x] = pack_f16(e0, e1);
-          }
-        }
-      }
-      vs_cur = vs;
-      if (left < kKv8Block) {                          // codes behind the row's end may be anything: none of them counts
-#pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (n * 16 + 2 * c4 + (j & 1) + (j >> 1) * 8 >= left) {
-#pragma unroll
-              for (int w = 0; w < NT / 4; ++w) vr[n][j][w] = 0u;
-            }
-      }
-#pragma unroll
-      for (int n = 0; n < 2; ++n) {
-#pragma unroll
-        for (int w = 0; w < NT / 4; ++w) {
-          // bytes of two keys side by side: (key 2c, key 2c + 1) for each of four dims
-          unsigned b0w[4], b1w[4];
-          kv8_decode4(__byte_perm(vr[n][0][w], vr[n][1][w], 0x5140), b0w[0], b0w[1]);
-          kv8_decode4(__byte_perm(vr[n][0][w], vr[n][1][w], 0x7362), b0w[2], b0w[3]);
-          kv8_decode4(__byte_perm(vr[n][2][w], vr[n][3][w], 0x5140), b1w[0], b1w[1]);
-          kv8_decode4(__byte_perm(vr[n][2][w], vr[n][3][w], 0x7362), b1w[2], b1w[3]);
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
-              mma_f16(o[mt][w * 4 + i],
-                      make_uint4(pr[mt][2 * n][0], pr[mt][2 * n][1], pr[mt][2 * n + 1][0], pr[mt][2 * n + 1][1]),
-                      b0w[i], b1w[i]);
-        }
+      for (int y = 0; y < 2; ++y) {
+        ref[nq][y] = -INFINITY;
+        sum[nq][y] = 0.f;
+        sc[nq][y] = s_sc[nq * 8 + 2 * c4 + y];
       }
     }
 
-    // ---- the warps' parts of this segment become one: (reference, sum) of every warp, then the outputs in two steps ----
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        float l = sum[mt][x];
-        l += __shfl_xor_sync(0xffffffffu, l, 1);
-        l += __shfl_xor_sync(0xffffffffu, l, 2);
-        sum[mt][x] = l;
-        if (c4 == 0) s_ml[warp * R + mt * 16 + g + 8 * x] = make_float2(ref[mt][x], l);
-      }
-    __syncthreads();
-    float m_all[MT][2], l_all[MT][2];
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const int f = mt * 16 + g + 8 * x;
-        float m = -INFINITY, l = 0.f;
-#pragma unroll
-        for (int w = 0; w < kStreamWarps; ++w) m = fmaxf(m, s_ml[w * R + f].x);
-#pragma unroll
-        for (int w = 0; w < kStreamWarps; ++w) {
-          const float2 v = s_ml[w * R + f];
-          if (v.x > -INFINITY) l += v.y * exp2_fast(v.x - m);
-        }
-        m_all[mt][x] = m;
-        l_all[mt][x] = l;
-        const float f2 = ref[mt][x] > -INFINITY ? exp2_fast(ref[mt][x] - m) * vs_cur : 0.f;
-#pragma unroll
-        for (int i = 0; i < NT; ++i) {
-          o[mt][i][2 * x] *= f2;
-          o[mt][i][2 * x + 1] *= f2;
+    int stage = 0;
+    for (int b = b0 + warp; b < b1; b += kStreamWarps) {
+      const float ks = kv8_clamp_scale(ks_next), vs = kv8_clamp_scale(vs_next);
+      {
+        const int nb = b + (STAGES - 1) * kStreamWarps;
+        if (nb < b1) fetch(stage == 0 ? STAGES - 1 : stage - 1, nb, head);
+        asm volatile("cp.async.commit_group;\n" ::: "memory");
+        if (b + kStreamWarps < b1) {
+          const size_t sa = (size_t)(ri.base + b + kStreamWarps) * p.hkv + head;
+          ks_next = __ldg(p.c.k_scale + sa);
+          vs_next = __ldg(p.c.v_scale + sa);
         }
       }
+      const float lv = log2_fast(vs), inv_vs = 1.0f / vs;
+      const int left = ri.vis - b * kKv8Block;         // keys of this block that the row sees (> 0)
+      asm volatile("cp.async.wait_group %0;\n" ::"n"(STAGES - 1) : "memory");
+      __syncwarp();
+      const unsigned kt = ring + (unsigned)stage * 2 * TB, vt = kt + TB;
+#pragma unroll kHalves
+      for (int m = 0; m < 2; ++m) {                    // 16 keys: rows 16 m + g and 16 m + g + 8 of this lane
+        float s[NQ][4];
 #pragma unroll
-    for (int half = kStreamWarps / 2; half > 0; half >>= 1) {
-      // lane (g, c4) holds dims [2 c4 NT, 2 c4 NT + NT) in component 0 and the NT after them in component 1
-      if (warp >= half && warp < 2 * half) {
-        float* dst = s_o + (warp - half) * R * LDO;
+        for (int nq = 0; nq < NQ; ++nq) s[nq][0] = s[nq][1] = s[nq][2] = s[nq][3] = 0.f;
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int h = 0; h < KS / 2; ++h) {             // 16 bytes of both keys: two k steps
+          uint4 kr[2];
 #pragma unroll
-          for (int x = 0; x < 2; ++x)
+          for (int x = 0; x < 2; ++x) {
+            const int key = m * 16 + g + 8 * x;
+            // dh 128: line = key, chunk 2 c4 + h; dh 64: two keys per line, chunk 4 (key & 1) + c4
+            const int line = DH == 128 ? key : key >> 1, chunk = DH == 128 ? 2 * c4 + h : 4 * (key & 1) + c4;
+            kr[x] = lds128(kt + line * 128 + ((chunk ^ (line & 7)) << 4));
+          }
 #pragma unroll
-            for (int y = 0; y < 2; ++y)
-#pragma unroll
-              for (int i = 0; i < NT; i += 4)
-                *reinterpret_cast<float4*>(dst + (mt * 16 + g + 8 * x) * LDO + (2 * c4 + y) * NT + i) =
-                    make_float4(o[mt][i][2 * x + y], o[mt][i + 1][2 * x + y], o[mt][i + 2][2 * x + y], o[mt][i + 3][2 * x + y]);
-      }
-      __syncthreads();
-      if (warp < half) {
-        const float* src = s_o + warp * R * LDO;
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-          for (int x = 0; x < 2; ++x)
-#pragma unroll
-            for (int y = 0; y < 2; ++y)
-#pragma unroll
-              for (int i = 0; i < NT; i += 4) {
-                const float4 v = *reinterpret_cast<const float4*>(src + (mt * 16 + g + 8 * x) * LDO + (2 * c4 + y) * NT + i);
-                o[mt][i][2 * x + y] += v.x; o[mt][i + 1][2 * x + y] += v.y;
-                o[mt][i + 2][2 * x + y] += v.z; o[mt][i + 3][2 * x + y] += v.w;
-              }
-      }
-      if (half > 1) __syncthreads();
-    }
-    if (warp == 0) {
-      const bool whole = b0 == 0 && b1 == ri.nb;
-      const size_t slot = 2 * (size_t)blockIdx.x + (u > u0 ? 1 : 0);
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const int f = mt * 16 + g + 8 * x;
-          if (f >= nrows) continue;
-          if (whole) {
-            const float inv = 1.0f / l_all[mt][x];
-            bf16* dst = p.out + (size_t)(t0 + f / G) * (p.hq * DH) + (head * G + f % G) * DH + 2 * c4 * NT;
-#pragma unroll
-            for (int y = 0; y < 2; ++y)
-#pragma unroll
-              for (int i = 0; i < NT; i += 8) {
-                uint4 w;
-                __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&w);
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                  h[j] = __floats2bfloat162_rn(o[mt][i + 2 * j][2 * x + y] * inv, o[mt][i + 2 * j + 1][2 * x + y] * inv);
-                *reinterpret_cast<uint4*>(dst + y * NT + i) = w;
-              }
-          } else {
-            float* dst = p.part_o + (slot * R + f) * DH + 2 * c4 * NT;
-#pragma unroll
-            for (int y = 0; y < 2; ++y)
-#pragma unroll
-              for (int i = 0; i < NT; i += 4)
-                *reinterpret_cast<float4*>(dst + y * NT + i) =
-                    make_float4(o[mt][i][2 * x + y], o[mt][i + 1][2 * x + y], o[mt][i + 2][2 * x + y], o[mt][i + 3][2 * x + y]);
-            if (c4 == 0) p.part_ml[slot * R + f] = make_float2(m_all[mt][x], l_all[mt][x]);
+          for (int nq = 0; nq < NQ; ++nq) {
+            const uint4 qa = NQ == 1 ? qf[NQ == 1 ? 2 * h : 0] : s_q[(nq * KS + 2 * h) * 32 + lane];
+            const uint4 qb = NQ == 1 ? qf[NQ == 1 ? 2 * h + 1 : 0] : s_q[(nq * KS + 2 * h + 1) * 32 + lane];
+            mma_e4m3(s[nq], kr[0].x, kr[1].x, kr[0].y, kr[1].y, qa.x, qa.y);
+            mma_e4m3(s[nq], kr[0].x, kr[1].x, kr[0].y, kr[1].y, qa.z, qa.w);
+            mma_e4m3(s[nq], kr[0].z, kr[1].z, kr[0].w, kr[1].w, qb.x, qb.y);
+            mma_e4m3(s[nq], kr[0].z, kr[1].z, kr[0].w, kr[1].w, qb.z, qb.w);
           }
         }
+        unsigned pr[NQ][2];
+        bool grow = false;
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {                // j & 1: query row, j >> 1: key
+            s[nq][j] = m * 16 + g + 8 * (j >> 1) < left ? fmaf(s[nq][j], sc[nq][j & 1] * ks, lv) : -INFINITY;
+            grow = grow || s[nq][j] > ref[nq][j & 1] + kGrow;
+          }
+        }
+        if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+          for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+              float mx = fmaxf(s[nq][y], s[nq][2 + y]);
+              mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+              mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+              mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+              if (mx > ref[nq][y] + kGrow) {
+                const float f = exp2_fast(ref[nq][y] - (mx - kBias));
+                ref[nq][y] = mx - kBias;
+                sum[nq][y] *= f;
+#pragma unroll
+                for (int i = 0; i < MD; ++i) {
+                  o[nq][i][y] *= f;
+                  o[nq][i][2 + y] *= f;
+                }
+              }
+            }
+        }
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq) {
+          const float e0 = exp2_fast(s[nq][0] - ref[nq][0]), e1 = exp2_fast(s[nq][1] - ref[nq][1]);
+          const float e2 = exp2_fast(s[nq][2] - ref[nq][0]), e3 = exp2_fast(s[nq][3] - ref[nq][1]);
+          sum[nq][0] = fmaf(e0 + e2, inv_vs, sum[nq][0]);
+          sum[nq][1] = fmaf(e1 + e3, inv_vs, sum[nq][1]);
+          pr[nq][0] = transpose8x8(pack_f16(e0, e1));
+          pr[nq][1] = transpose8x8(pack_f16(e2, e3));
+        }
+        // ---- output: dims g DH / 8 + 2 i (row g of m tile i) and + 1 (row g + 8) ----
+        unsigned vr[4][DH / 32];         // keys 16 m + 2 c4, + 1, + 8, + 9
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int key = m * 16 + 2 * c4 + (j & 1) + (j >> 1) * 8;
+          if (DH == 128) {
+            const uint4 v = lds128(vt + key * 128 + ((g ^ (key & 7)) << 4));
+            vr[j][0] = v.x; vr[j][1] = v.y;
+            vr[j][DH / 32 - 2] = v.z; vr[j][DH / 32 - 1] = v.w;
+          } else {
+            const int line = key >> 1, chunk = 4 * (key & 1) + (g >> 1);
+            const uint2 v = lds64(vt + line * 128 + ((chunk ^ (line & 7)) << 4) + (g & 1) * 8);
+            vr[j][0] = v.x; vr[j][1] = v.y;
+          }
+        }
+#pragma unroll
+        for (int w = 0; w < DH / 32; ++w)
+#pragma unroll
+          for (int z = 0; z < 2; ++z) {                // dims 4 w + 2 z, + 1: bytes of two keys side by side
+            unsigned a[4];
+            kv8_decode4(__byte_perm(vr[0][w], vr[1][w], z ? 0x7362 : 0x5140), a[0], a[1]);
+            kv8_decode4(__byte_perm(vr[2][w], vr[3][w], z ? 0x7362 : 0x5140), a[2], a[3]);
+#pragma unroll
+            for (int nq = 0; nq < NQ; ++nq) mma_f16(o[nq][2 * w + z], a, pr[nq][0], pr[nq][1]);
+          }
+      }
+      stage = stage + 1 == STAGES ? 0 : stage + 1;
+      __syncwarp();                      // the stage may be filled again
     }
-    u += b1 - b0;
+
+    // ---- the warps' parts of this segment become one ----
+#pragma unroll
+    for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        float l = sum[nq][y];
+        l += __shfl_xor_sync(0xffffffffu, l, 4);
+        l += __shfl_xor_sync(0xffffffffu, l, 8);
+        l += __shfl_xor_sync(0xffffffffu, l, 16);
+        if (g == 0) s_ml[warp * R + nq * 8 + 2 * c4 + y] = make_float2(ref[nq][y], l);
+      }
+    __syncthreads();                     // (the ring is idle from here on)
+#pragma unroll
+    for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        const int f = nq * 8 + 2 * c4 + y;
+        float m = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < kStreamWarps; ++w) m = fmaxf(m, s_ml[w * R + f].x);
+        // a warp without blocks has an output of zeros; one that met nothing but NaN has NaN, and keeps it
+        const float turn = ref[nq][y] > -INFINITY ? exp2_fast(ref[nq][y] - m) : 1.f;
+        float* dst = s_o + (warp * R + f) * LDO + g * (DH / 8);
+#pragma unroll
+        for (int i = 0; i < MD; i += 2)
+          *reinterpret_cast<float4*>(dst + 2 * i) = make_float4(o[nq][i][y] * turn, o[nq][i][2 + y] * turn,
+                                                                o[nq][i + 1][y] * turn, o[nq][i + 1][2 + y] * turn);
+      }
+    __syncthreads();
+    const bool whole = b0 == 0 && b1 == ri.nb;
+    const size_t slot = 2 * (size_t)blockIdx.x + (opens ? 0 : 1);
+    for (int v = tid; v < nrows * (DH / 4); v += kStreamThreads) {
+      const int f = v / (DH / 4), d = v % (DH / 4) * 4;
+      float m = -INFINITY, l = 0.f;
+#pragma unroll
+      for (int w = 0; w < kStreamWarps; ++w) m = fmaxf(m, s_ml[w * R + f].x);
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < kStreamWarps; ++w) {
+        const float2 ml = s_ml[w * R + f];
+        l += ml.x > -INFINITY ? ml.y * exp2_fast(ml.x - m) : ml.y;
+        const float4 x = *reinterpret_cast<const float4*>(s_o + (w * R + f) * LDO + d);
+        acc.x += x.x; acc.y += x.y; acc.z += x.z; acc.w += x.w;
+      }
+      if (whole) {
+        const float inv = 1.0f / l;
+        uint2 w;
+        __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&w);
+        h[0] = __floats2bfloat162_rn(acc.x * inv, acc.y * inv);
+        h[1] = __floats2bfloat162_rn(acc.z * inv, acc.w * inv);
+        *reinterpret_cast<uint2*>(p.out + (size_t)(t0 + f / G) * (p.hq * DH) + (head * G + f % G) * DH + d) = w;
+      } else {
+        *reinterpret_cast<float4*>(p.part_o + (slot * R + f) * DH + d) = acc;
+        if (d == 0) p.part_ml[slot * R + f] = make_float2(m, l);
+      }
+    }
   }
 }
 
@@ -494,14 +523,15 @@ __global__ void __launch_bounds__(256) k_attention_kv8_merge(StreamParams p, int
   const int G = p.hq / p.hkv, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int t0 = ri.t0 + tile * p.tq, nrows = min(p.tq, ri.t0 + ri.n - t0) * G;
   const long long total = p.prefix[p.n_rows], ctas = p.prefix[p.n_rows + 1];
-  const long long first = p.prefix[row] + ((long long)head * ri.tiles + tile) * ri.nb;
+  // the item's blocks are units [first, first + nb) of the line
+  const long long first = p.prefix[row] + ((long long)head * ri.tiles + tile) * ri.item_units() + kItemCost;
   int c0 = 0, c1 = -1;
   if (ri.nb > 0) {
     c0 = share_of(first, total, ctas);
     c1 = share_of(first + ri.nb - 1, total, ctas);
     if (c0 == c1) return;                  // held whole by one CTA, which wrote it
   }
-  for (int f = warp + 8 * blockIdx.z; f < nrows; f += 8 * gridDim.z) {
+  for (int f = warp; f < nrows; f += 8) {
     float acc[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) acc[j] = 0.f;
@@ -512,9 +542,9 @@ __global__ void __launch_bounds__(256) k_attention_kv8_merge(StreamParams p, int
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const int cc = min(c + k, c1);
-        const size_t at = ((size_t)2 * cc + (first > share_start(cc, total, ctas) ? 1 : 0)) * R + f;
+        // a CTA's first segment is in its even slot: the item this CTA began with, if it began inside the item's units
+        const size_t at = ((size_t)2 * cc + (first - kItemCost > share_start(cc, total, ctas) ? 1 : 0)) * R + f;
         ml[k] = p.part_ml[at];
-        if (c + k > c1) ml[k] = make_float2(-INFINITY, 0.f);
         const float* src = p.part_o + at * DH + lane * V;
         if (V == 4) {
           const float4 w = *reinterpret_cast<const float4*>(src);
@@ -526,15 +556,15 @@ __global__ void __launch_bounds__(256) k_attention_kv8_merge(StreamParams p, int
       }
       float nm = m;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) nm = fmaxf(nm, ml[k].x);
-      const float f0 = m > -INFINITY ? exp2_fast(m - nm) : 0.f;
+      for (int k = 0; k < 4; ++k) nm = fmaxf(nm, ml[k].x);      // (a part listed twice changes nothing here)
+      const float f0 = m > -INFINITY ? exp2_fast(m - nm) : 1.f;
       l *= f0;
 #pragma unroll
       for (int j = 0; j < V; ++j) acc[j] *= f0;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         if (c + k > c1) continue;
-        const float w = ml[k].x > -INFINITY ? exp2_fast(ml[k].x - nm) : 1.f;   // (NaN sums stay NaN)
+        const float w = ml[k].x > -INFINITY ? exp2_fast(ml[k].x - nm) : 1.f;   // (sums of NaN stay NaN)
         l += w * ml[k].y;
 #pragma unroll
         for (int j = 0; j < V; ++j) acc[j] += w * v[k][j];
@@ -550,39 +580,33 @@ __global__ void __launch_bounds__(256) k_attention_kv8_merge(StreamParams p, int
 }
 
 // Per device: how many CTAs of each instantiation one wave holds (0: not asked yet).
-struct DeviceInfo { int wave[4]; };
+struct DeviceInfo { int wave[6]; };
 DeviceInfo g_dev[kMaxDevices];
 std::mutex g_mutex;
 
-template <int DH, int MT>
-cudaError_t prepare_stream(int* wave) {
-  int dev = 0, sms = 0, per = 0;
-  cudaError_t r = cudaGetDevice(&dev);
-  if (r == cudaSuccess) r = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-  if (r == cudaSuccess)
-    r = cudaFuncSetAttribute(k_attention_kv8_stream<DH, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, stream_smem<DH, MT>());
-  if (r == cudaSuccess)
-    r = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, k_attention_kv8_stream<DH, MT>, kStreamThreads, stream_smem<DH, MT>());
-  if (r != cudaSuccess) return r;
-  if (sms < 1 || per < 1) return cudaErrorInvalidDevice;
-  *wave = std::min(sms * per, kMaxStreamCtas);
-  return cudaSuccess;
-}
-
-template <int DH, int MT>
+template <int DH, int NQ, int STAGES, int MINB>
 cudaError_t run_stream(StreamParams p, int index, cudaStream_t s) {
+  constexpr auto kernel = k_attention_kv8_stream<DH, NQ, STAGES, MINB>;
+  constexpr int smem = StreamSmem<DH, NQ, STAGES>::total;
   DeviceInfo* d = device_slot(g_dev);
   if (!d) return cudaErrorInvalidDevice;
   {
     std::lock_guard<std::mutex> lock(g_mutex);
-    if (!d->wave[index])
-      if (cudaError_t r = prepare_stream<DH, MT>(&d->wave[index])) return r;
+    if (!d->wave[index]) {
+      int dev = 0, sms = 0, per = 0;
+      cudaError_t r = cudaGetDevice(&dev);
+      if (r == cudaSuccess) r = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+      if (r == cudaSuccess) r = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+      if (r == cudaSuccess) r = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, kernel, kStreamThreads, smem);
+      if (r != cudaSuccess) return r;
+      if (sms < 1 || per < 1) return cudaErrorInvalidDevice;
+      d->wave[index] = std::min(sms * per, kMaxStreamCtas);
+    }
   }
-  cudaError_t r = launch_pdl(k_attention_kv8_stream<DH, MT>, dim3(d->wave[index]), dim3(kStreamThreads),
-                             (size_t)stream_smem<DH, MT>(), s, p);
+  cudaError_t r = launch_pdl(kernel, dim3(d->wave[index]), dim3(kStreamThreads), (size_t)smem, s, p);
   if (r != cudaSuccess) return r;
   const long long slots = (long long)p.M / p.tq + p.n_rows;
-  return launch_pdl(k_attention_kv8_merge<DH>, dim3((unsigned)slots, p.hkv), dim3(256), 0, s, p, 16 * MT);
+  return launch_pdl(k_attention_kv8_merge<DH>, dim3((unsigned)slots, p.hkv), dim3(256), 0, s, p, 8 * NQ);
 }
 
 inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
@@ -599,11 +623,11 @@ cudaError_t launch_attention_kv8(const AttnKv8Args& a, cudaStream_t s) {
   if (a.M <= 0 || a.n_rows <= 0) return cudaSuccess;
   const int G = a.hq / a.hkv;
   const long long widest = (long long)(a.max_nq > 0 ? a.max_nq : a.M) * G;
-  const int mt = widest <= 16 ? 1 : 2;
+  const int nq = widest <= 8 ? 1 : widest <= 16 ? 2 : 4;
   StreamParams p;
   p.q = a.q; p.q_ld = a.q_ld; p.c = a.cache; p.out = a.out;
   p.cu_q = a.cu_q; p.kv_base = a.kv_base; p.vis = a.vis;
-  p.n_rows = a.n_rows; p.M = a.M; p.hq = a.hq; p.hkv = a.hkv; p.tq = 16 * mt / G;
+  p.n_rows = a.n_rows; p.M = a.M; p.hq = a.hq; p.hkv = a.hkv; p.tq = 8 * nq / G;
   p.error_flag = a.error_flag;
   char* at = static_cast<char*>(a.scratch);
   p.prefix = reinterpret_cast<long long*>(at);
@@ -611,8 +635,9 @@ cudaError_t launch_attention_kv8(const AttnKv8Args& a, cudaStream_t s) {
   p.part_o = reinterpret_cast<float*>(at);
   at += up256((size_t)2 * kMaxStreamCtas * 32 * a.dh * sizeof(float));
   p.part_ml = reinterpret_cast<float2*>(at);
-  if (a.dh == 128) return mt == 1 ? run_stream<128, 1>(p, 0, s) : run_stream<128, 2>(p, 1, s);
-  return mt == 1 ? run_stream<64, 1>(p, 2, s) : run_stream<64, 2>(p, 3, s);
+  if (a.dh == 128)
+    return nq == 1 ? run_stream<128, 1, 2, 3>(p, 0, s) : nq == 2 ? run_stream<128, 2, 2, 3>(p, 1, s) : run_stream<128, 4, 2, 2>(p, 2, s);
+  return nq == 1 ? run_stream<64, 1, 2, 3>(p, 3, s) : nq == 2 ? run_stream<64, 2, 2, 3>(p, 4, s) : run_stream<64, 4, 2, 3>(p, 5, s);
 }
 
 }  // namespace bs

@@ -333,12 +333,13 @@ def attn_inputs(rng, hq, hkv, dh, rows, spread=4, qscale=1.0):
     return n, vis, base, (ck, sk), (cv, sv), q
 
 
-def attn_bound(out, mag, dot, vmax, n_keys, dh):
-    """How far a correct kernel may be: the output's rounding to bf16; scores in fp32 (dh products of exact factors, a
-    relative 2^-23 per accumulation, the scale and the base-2 exponent's argument 4 more), their error e^d - 1 on every
-    weight; weights rounded to fp16 (2^-11, or 2^-30 of the largest weight where they are subnormal), exponentials 2^-21;
-    fp32 sums over the keys in chunks of 16."""
-    d = dot * (dh + 4) * 2.0 ** -23
+def attn_bound(out, mag, dot, flat, vmax, n_keys, dh):
+    """How far a correct kernel may be: the output's rounding to bf16; a query element held to 2^-17 of its row's largest
+    element at worst (as two e4m3 values: the largest lies in [2^7, 2^8), the second value's step is 2^-9 at least);
+    scores in fp32 (dh products, a relative 2^-23 per accumulation, the scale and the base-2 exponent's argument 4 more),
+    their error e^d - 1 on every weight; weights rounded to fp16 (2^-11, or 2^-30 of the largest weight where they are
+    subnormal), exponentials 2^-21; fp32 sums over the keys in chunks of 16."""
+    d = dot * (dh + 4) * 2.0 ** -23 + flat * 2.0 ** -17
     w = np.expm1(2 * d) + 2.0 ** -11 + 2.0 ** -20 + (n_keys / 16 + 16) * 2.0 ** -23
     return (np.abs(out) * HALF_BF16 + mag * w + n_keys * 2.0 ** -30 * vmax) * (1 + 2.0 ** -7) + 1e-37
 
@@ -353,8 +354,8 @@ def check_attention(got, q, hq, dh, n, vis, base, kc, vc):
             assert (g == 0).all(), f"row {i} sees nothing"
             continue
         k, v = K.span(*kc, base[i], 0, vis[i]), K.span(*vc, base[i], 0, vis[i])
-        ref, mag, dot = K.attention(host(q)[cu[i]:cu[i + 1]].reshape(n[i], hq, dh), k, v)
-        err, tol = np.abs(g - ref), attn_bound(ref, mag, dot, np.abs(v).max(), vis[i], dh)
+        ref, mag, dot, flat = K.attention(host(q)[cu[i]:cu[i + 1]].reshape(n[i], hq, dh), k, v)
+        err, tol = np.abs(g - ref), attn_bound(ref, mag, dot, flat, np.abs(v).max(), vis[i], dh)
         assert (err <= tol).all(), f"row {i}: error {err.max()} at most {(err / tol).max()} of the bound"
 
 
@@ -462,8 +463,8 @@ def test_offsets_beyond_32_bits(B, nq):
     # the scale of a block can be twice what a value alone would need: half a step of e4m3, or half a subnormal step
     top = np.abs(x[:, 64:]).max()
     assert (np.abs(v - x[:, 64:]) <= np.maximum(np.abs(x[:, 64:]) * 2.0 ** -4, top / 224 * 2.0 ** -10)).all()
-    ref, mag, dot = K.attention(host(q).reshape(nq, hq, dh), k, v)
-    assert (np.abs(host(out).reshape(nq, hq, dh) - ref) <= attn_bound(ref, mag, dot, np.abs(v).max(), M, dh)).all()
+    ref, mag, dot, flat = K.attention(host(q).reshape(nq, hq, dh), k, v)
+    assert (np.abs(host(out).reshape(nq, hq, dh) - ref) <= attn_bound(ref, mag, dot, flat, np.abs(v).max(), M, dh)).all()
 
 
 def test_a_step_of_serving(B):
@@ -504,9 +505,9 @@ def test_a_step_of_serving(B):
         got, at_row = host(o8), prefix(length)
         for i in range(3):
             ki, vi = k[at_row[i]:at_row[i + 1]], v[at_row[i]:at_row[i + 1]]
-            ref, mag, dot = K.attention(host(q8)[cu[i]:cu[i + 1]].reshape(-1, hq, dh), ki, vi)
+            ref, mag, dot, flat = K.attention(host(q8)[cu[i]:cu[i + 1]].reshape(-1, hq, dh), ki, vi)
             err = np.abs(got[cu[i]:cu[i + 1]].reshape(-1, hq, dh) - ref)
-            assert (err <= attn_bound(ref, mag, dot, np.abs(vi).max(), len(ki), dh)).all(), (name, i)
+            assert (err <= attn_bound(ref, mag, dot, flat, np.abs(vi).max(), len(ki), dh)).all(), (name, i)
         # 8 bits move a key's dims by at most 2^-4 of themselves, in all directions: the outputs stay alike
         a, b = got, host(o16)
         assert np.linalg.norm(a - b) < 0.1 * np.linalg.norm(b), name
