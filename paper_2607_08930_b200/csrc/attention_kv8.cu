@@ -26,11 +26,6 @@ __device__ __forceinline__ void mma_f16(float* c, const unsigned* a, unsigned b0
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ void mma_e4m3(float* c, unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0, unsigned b1) {
-  asm volatile("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
-               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
 // 8 x 8 fp16 matrix across the warp (lane (g, c): row g, columns 2c, 2c + 1), transposed
 __device__ __forceinline__ unsigned transpose8x8(unsigned x) {
   unsigned r;
@@ -80,13 +75,14 @@ __device__ __forceinline__ uint2 lds64(unsigned at) {
 // behind the row's end arrive as zeros, whatever the cache holds there.
 //
 // Keys are the rows (M) of both products and the queries their columns (N), so that 8 query rows - a group of heads of
-// one token - fill an instruction.  Scores: the codes of K go to the tensor cores as they are (e4m3); a query element,
-// after a power of two per query row has brought the row's largest into [128, 256), is the sum of two e4m3 values: the
-// nearest one and the rest (4 + 4 significant bits, bf16 has 8; exact above 2^-10 of the row's largest element, and
-// within 2^-17 of that element below).  Output: V's codes as fp16 (exact) against weights in fp16, transposed in
-// registers (movmatrix).  The order of the dims in the scores' k index and of the dims in the output's m index is free,
-// and is chosen so that a lane's 16-byte shared-memory loads are its operand registers; a 16-byte chunk's place in its
-// 128-byte line is turned by the line's number, which keeps those loads free of bank conflicts.
+// one token - fill an instruction.  Codes go to the tensor cores as fp16, which holds every e4m3 value (the warp-level
+// e4m3 product is no way around that: measured on B200, it runs as conversions and two fp16 products, 25 clk against 8).
+// Queries become fp16 after a power of two per query row has brought their largest element into [1, 2): bf16's 8 bits
+// fit fp16's 11, and what drops below 2^-24 of the row's largest element is below the fp32 sum's own rounding.  Weights
+// are fp16, transposed in registers (movmatrix).  The order of the dims in the scores' k index and of the dims in the
+// output's m index is free, and is chosen so that a lane's 16-byte shared-memory loads hold its operand registers; a
+// 16-byte chunk's place in its 128-byte line is turned by the line's number, which keeps those loads free of bank
+// conflicts.
 constexpr int kStreamWarps = 4;
 constexpr int kStreamThreads = kStreamWarps * 32;
 constexpr int kMaxStreamCtas = 592;
@@ -147,7 +143,7 @@ struct StreamSmem {
   static constexpr int ring = kStreamWarps * STAGES * 2 * kTileBytes<DH>;
   static constexpr int merge = kStreamWarps * R * LDO * 4;         // the warps' outputs, over the ring when it is idle
   static constexpr int front = ring > merge ? ring : merge;
-  static constexpr int q = NQ * (DH / 32) * 32 * 16;               // query fragments
+  static constexpr int q = NQ * (DH / 32) * 32 * 16;               // query fragments, two k steps in 16 bytes
   static constexpr int total = 128 + front + q + kStreamWarps * R * 8 + R * 4;
 };
 constexpr int kRowsPerThread = kAttnKv8MaxRows / kStreamThreads;
@@ -155,7 +151,7 @@ constexpr int kRowsPerThread = kAttnKv8MaxRows / kStreamThreads;
 template <int DH, int NQ, int STAGES, int MINB>
 __global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(StreamParams p) {
   using L = StreamSmem<DH, NQ, STAGES>;
-  constexpr int KS = DH / 32;            // k steps of the scores
+  constexpr int KP = DH / 32;            // pairs of k steps of the scores
   constexpr int MD = DH / 16;            // m tiles of the output
   constexpr int kHalves = NQ == 1 ? 2 : 1;             // (unrolled, the wider instantiations do not fit their registers)
   constexpr int R = L::R, LDO = L::LDO, TB = kTileBytes<DH>;
@@ -222,6 +218,15 @@ __global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(S
     p.prefix[p.n_rows] = total;
     p.prefix[p.n_rows + 1] = ctas;
   }
+  // rows that see nothing: zeros
+  for (int r = blockIdx.x; r < p.n_rows; r += gridDim.x) {
+    RowInfo z;
+    row_info(p.cu_q, p.kv_base, p.vis, p.c.n_blocks, p.M, p.tq, r, z);
+    if (z.nb == 0) {
+      uint4* dst = reinterpret_cast<uint4*>(p.out + (size_t)z.t0 * (p.hq * DH));
+      for (long long i = tid; i < (long long)z.n * (p.hq * DH / 8); i += kStreamThreads) dst[i] = make_uint4(0, 0, 0, 0);
+    }
+  }
   if (total == 0 || (long long)blockIdx.x >= ctas) return;
   __syncthreads();
   int row = s_row;
@@ -274,15 +279,15 @@ __global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(S
       ks_next = __ldg(p.c.k_scale + sa);
       vs_next = __ldg(p.c.v_scale + sa);
     }
-    // ---- queries: two e4m3 fragments (nearest value, rest) of every row in shared memory ----
+    // ---- queries: fp16 fragments in shared memory ----
     for (int nq = warp; nq < NQ; nq += kStreamWarps) {
       const int f = nq * 8 + g;          // query row of this lane (n index of the scores)
       const bool valid = f < nrows;
       const bf16* src = p.q + (size_t)(t0 + (valid ? f / G : 0)) * p.q_ld + (head * G + (valid ? f % G : 0)) * DH + c4 * (DH / 4);
-      uint4 raw[KS];
+      uint4 raw[KP];
       float top = 0.f;
 #pragma unroll
-      for (int k = 0; k < KS; ++k) {     // k step k of lane c4 stands for dims c4 DH / 4 + 8 k .. + 7
+      for (int k = 0; k < KP; ++k) {     // k step i of lane c4 stands for dims c4 DH / 4 + 4 i .. + 3
         raw[k] = valid ? *reinterpret_cast<const uint4*>(src + k * 8) : make_uint4(0, 0, 0, 0);
         const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&raw[k]);
 #pragma unroll
@@ -294,34 +299,28 @@ __global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(S
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
       const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 100);
-      const float up = pow2i(7 - e);
-      if (c4 == 0) s_sc[f] = pow2i(e - 7) * (1.4426950408889634f * rsqrtf((float)DH));
+      const float up = pow2i(-e);
+      if (c4 == 0) s_sc[f] = pow2i(e) * (1.4426950408889634f * rsqrtf((float)DH));
 #pragma unroll
-      for (int k = 0; k < KS; ++k) {
+      for (int k = 0; k < KP; ++k) {
         const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&raw[k]);
-        unsigned hi[2] = {0u, 0u}, lo[2] = {0u, 0u};
+        unsigned w[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          float2 x = __bfloat1622float2(h[j]);
-          x.x *= up;
-          x.y *= up;
-          const unsigned near = kv8_encode2(x.x, x.y);
-          const unsigned back = kv8_decode2((unsigned short)near);
-          const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&back));
-          hi[j >> 1] |= near << (16 * (j & 1));
-          lo[j >> 1] |= kv8_encode2(x.x - y.x, x.y - y.y) << (16 * (j & 1));
+          const float2 x = __bfloat1622float2(h[j]);
+          w[j] = pack_f16(x.x * up, x.y * up);
         }
-        s_q[(nq * KS + k) * 32 + lane] = make_uint4(hi[0], hi[1], lo[0], lo[1]);
+        s_q[(nq * KP + k) * 32 + lane] = make_uint4(w[0], w[1], w[2], w[3]);
       }
     }
     __syncthreads();
 
     float o[NQ][MD][4];
     float ref[NQ][2], sum[NQ][2], sc[NQ][2];         // of query rows nq * 8 + 2 c4 + {0, 1}
-    uint4 qf[NQ == 1 ? KS : 1];
+    uint4 qf[NQ == 1 ? KP : 1];
     if (NQ == 1) {
 #pragma unroll
-      for (int k = 0; k < KS; ++k) qf[NQ == 1 ? k : 0] = s_q[k * 32 + lane];
+      for (int k = 0; k < KP; ++k) qf[NQ == 1 ? k : 0] = s_q[k * 32 + lane];
     }
 #pragma unroll
     for (int nq = 0; nq < NQ; ++nq) {
@@ -359,7 +358,7 @@ __global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(S
 #pragma unroll
         for (int nq = 0; nq < NQ; ++nq) s[nq][0] = s[nq][1] = s[nq][2] = s[nq][3] = 0.f;
 #pragma unroll
-        for (int h = 0; h < KS / 2; ++h) {             // 16 bytes of both keys: two k steps
+        for (int h = 0; h < KP / 2; ++h) {             // 16 bytes of both keys: four k steps
           uint4 kr[2];
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
@@ -368,15 +367,19 @@ __global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(S
             const int line = DH == 128 ? key : key >> 1, chunk = DH == 128 ? 2 * c4 + h : 4 * (key & 1) + c4;
             kr[x] = lds128(kt + line * 128 + ((chunk ^ (line & 7)) << 4));
           }
+          unsigned a[4][4];              // [k step][key g: 2 dims, key g + 8, key g: next 2 dims, key g + 8]
+          kv8_decode4(kr[0].x, a[0][0], a[0][2]); kv8_decode4(kr[1].x, a[0][1], a[0][3]);
+          kv8_decode4(kr[0].y, a[1][0], a[1][2]); kv8_decode4(kr[1].y, a[1][1], a[1][3]);
+          kv8_decode4(kr[0].z, a[2][0], a[2][2]); kv8_decode4(kr[1].z, a[2][1], a[2][3]);
+          kv8_decode4(kr[0].w, a[3][0], a[3][2]); kv8_decode4(kr[1].w, a[3][1], a[3][3]);
 #pragma unroll
-          for (int nq = 0; nq < NQ; ++nq) {
-            const uint4 qa = NQ == 1 ? qf[NQ == 1 ? 2 * h : 0] : s_q[(nq * KS + 2 * h) * 32 + lane];
-            const uint4 qb = NQ == 1 ? qf[NQ == 1 ? 2 * h + 1 : 0] : s_q[(nq * KS + 2 * h + 1) * 32 + lane];
-            mma_e4m3(s[nq], kr[0].x, kr[1].x, kr[0].y, kr[1].y, qa.x, qa.y);
-            mma_e4m3(s[nq], kr[0].x, kr[1].x, kr[0].y, kr[1].y, qa.z, qa.w);
-            mma_e4m3(s[nq], kr[0].z, kr[1].z, kr[0].w, kr[1].w, qb.x, qb.y);
-            mma_e4m3(s[nq], kr[0].z, kr[1].z, kr[0].w, kr[1].w, qb.z, qb.w);
-          }
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int nq = 0; nq < NQ; ++nq) {
+              const uint4 qv = NQ == 1 ? qf[NQ == 1 ? 2 * h + i : 0] : s_q[(nq * KP + 2 * h + i) * 32 + lane];
+              mma_f16(s[nq], a[2 * i], qv.x, qv.y);
+              mma_f16(s[nq], a[2 * i + 1], qv.z, qv.w);
+            }
         }
         unsigned pr[NQ][2];
         bool grow = false;
@@ -508,74 +511,66 @@ __global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(S
 }
 
 // Items that more than one CTA held: out = sum_c 2^(m_c - m) o_c / sum_c 2^(m_c - m) l_c over the parts in order.
-// Rows that see nothing (vis = 0): zeros.  One CTA per (query tile slot, kv head), one warp per query row in turn.
+// One CTA per boundary between two shares; the boundaries inside an item share its output (query row, 32 dims) between
+// them, a warp each: four groups of eight lanes take every fourth part.
 template <int DH>
 __global__ void __launch_bounds__(256) k_attention_kv8_merge(StreamParams p, int R) {
-  constexpr int V = DH / 32;
   pdl_wait();
   pdl_trigger();
-  const int slot = (int)blockIdx.x, head = blockIdx.y;
-  const int row = warp_search(p.n_rows, slot, [&](int i) { return __ldg(p.cu_q + i) / p.tq + i; });
+  const long long total = p.prefix[p.n_rows], ctas = p.prefix[p.n_rows + 1];
+  const int cut = (int)blockIdx.x + 1;                // the boundary in front of share `cut`
+  if (cut >= ctas) return;
+  const long long u = share_start(cut, total, ctas);
+  // the last row whose prefix is <= u (a row without units shares its prefix with the next one)
+  const int row = warp_search(p.n_rows, u, [&](int i) { return p.prefix[i]; });
   RowInfo ri;
   row_info(p.cu_q, p.kv_base, p.vis, p.c.n_blocks, p.M, p.tq, row, ri);
-  const int tile = slot - (__ldg(p.cu_q + row) / p.tq + row);
-  if (tile < 0 || tile >= ri.tiles) return;
+  const long long local = u - p.prefix[row];
+  const int per = ri.item_units();
+  if (per == 0) return;
+  const int item = (int)(local / per);
+  // the item's blocks are units [first, first + nb) of the line
+  const long long first = u - local % per + kItemCost;
+  if (u <= first) return;                             // cut in front of its blocks: nothing is split here
+  const int c0 = share_of(first, total, ctas), c1 = share_of(first + ri.nb - 1, total, ctas);
+  const int head = item / ri.tiles, tile = item % ri.tiles;
   const int G = p.hq / p.hkv, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int t0 = ri.t0 + tile * p.tq, nrows = min(p.tq, ri.t0 + ri.n - t0) * G;
-  const long long total = p.prefix[p.n_rows], ctas = p.prefix[p.n_rows + 1];
-  // the item's blocks are units [first, first + nb) of the line
-  const long long first = p.prefix[row] + ((long long)head * ri.tiles + tile) * ri.item_units() + kItemCost;
-  int c0 = 0, c1 = -1;
-  if (ri.nb > 0) {
-    c0 = share_of(first, total, ctas);
-    c1 = share_of(first + ri.nb - 1, total, ctas);
-    if (c0 == c1) return;                  // held whole by one CTA, which wrote it
-  }
-  for (int f = warp; f < nrows; f += 8) {
-    float acc[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) acc[j] = 0.f;
+  // a CTA's first segment is in its even slot: this item, if the CTA's share begins at or inside it
+  auto slot_of = [&](int c) { return (size_t)2 * c + (first - kItemCost > share_start(c, total, ctas) ? 1 : 0); };
+  const int sub = lane >> 3;
+  for (int v = (cut - c0 - 1) * 8 + warp; v < nrows * (DH / 32); v += (c1 - c0) * 8) {
+    const int f = v / (DH / 32), d = v % (DH / 32) * 32 + (lane & 7) * 4;
     float m = -INFINITY, l = 0.f;
-    for (int c = c0; c <= c1; c += 4) {
-      float2 ml[4];
-      float v[4][V];
+    for (int c = c0 + lane; c <= c1; c += 32) m = fmaxf(m, p.part_ml[slot_of(c) * R + f].x);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int cc = min(c + k, c1);
-        // a CTA's first segment is in its even slot: the item this CTA began with, if it began inside the item's units
-        const size_t at = ((size_t)2 * cc + (first - kItemCost > share_start(cc, total, ctas) ? 1 : 0)) * R + f;
-        ml[k] = p.part_ml[at];
-        const float* src = p.part_o + at * DH + lane * V;
-        if (V == 4) {
-          const float4 w = *reinterpret_cast<const float4*>(src);
-          v[k][0] = w.x; v[k][1] = w.y; v[k][V - 2] = w.z; v[k][V - 1] = w.w;
-        } else {
-          const float2 w = *reinterpret_cast<const float2*>(src);
-          v[k][0] = w.x; v[k][1] = w.y;
-        }
-      }
-      float nm = m;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) nm = fmaxf(nm, ml[k].x);      // (a part listed twice changes nothing here)
-      const float f0 = m > -INFINITY ? exp2_fast(m - nm) : 1.f;
-      l *= f0;
-#pragma unroll
-      for (int j = 0; j < V; ++j) acc[j] *= f0;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        if (c + k > c1) continue;
-        const float w = ml[k].x > -INFINITY ? exp2_fast(ml[k].x - nm) : 1.f;   // (sums of NaN stay NaN)
-        l += w * ml[k].y;
-#pragma unroll
-        for (int j = 0; j < V; ++j) acc[j] += w * v[k][j];
-      }
-      m = nm;
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int c = c0 + sub; c <= c1; c += 4) {
+      const size_t at = slot_of(c) * R + f;
+      const float2 ml = p.part_ml[at];
+      const float4 x = *reinterpret_cast<const float4*>(p.part_o + at * DH + d);
+      const float w = ml.x > -INFINITY ? exp2_fast(ml.x - m) : 1.f;              // (parts of NaN stay NaN)
+      l += w * ml.y;
+      acc.x += w * x.x; acc.y += w * x.y; acc.z += w * x.z; acc.w += w * x.w;
     }
-    const float inv = ri.nb > 0 ? 1.0f / l : 0.f;
-    bf16* dst = p.out + (size_t)(t0 + f / G) * (p.hq * DH) + (head * G + f % G) * DH + lane * V;
 #pragma unroll
-    for (int j = 0; j < V; j += 2)
-      *reinterpret_cast<__nv_bfloat162*>(dst + j) = __floats2bfloat162_rn(acc[j] * inv, acc[j + 1] * inv);
+    for (int o = 8; o < 32; o <<= 1) {
+      l += __shfl_xor_sync(0xffffffffu, l, o);
+      acc.x += __shfl_xor_sync(0xffffffffu, acc.x, o);
+      acc.y += __shfl_xor_sync(0xffffffffu, acc.y, o);
+      acc.z += __shfl_xor_sync(0xffffffffu, acc.z, o);
+      acc.w += __shfl_xor_sync(0xffffffffu, acc.w, o);
+    }
+    if (sub == 0) {
+      const float inv = 1.0f / l;
+      uint2 w;
+      __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&w);
+      h[0] = __floats2bfloat162_rn(acc.x * inv, acc.y * inv);
+      h[1] = __floats2bfloat162_rn(acc.z * inv, acc.w * inv);
+      *reinterpret_cast<uint2*>(p.out + (size_t)(t0 + f / G) * (p.hq * DH) + (head * G + f % G) * DH + d) = w;
+    }
   }
 }
 
@@ -605,8 +600,7 @@ cudaError_t run_stream(StreamParams p, int index, cudaStream_t s) {
   }
   cudaError_t r = launch_pdl(kernel, dim3(d->wave[index]), dim3(kStreamThreads), (size_t)smem, s, p);
   if (r != cudaSuccess) return r;
-  const long long slots = (long long)p.M / p.tq + p.n_rows;
-  return launch_pdl(k_attention_kv8_merge<DH>, dim3((unsigned)slots, p.hkv), dim3(256), 0, s, p, 8 * NQ);
+  return launch_pdl(k_attention_kv8_merge<DH>, dim3(d->wave[index]), dim3(256), 0, s, p, 8 * NQ);
 }
 
 inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
@@ -637,7 +631,7 @@ cudaError_t launch_attention_kv8(const AttnKv8Args& a, cudaStream_t s) {
   p.part_ml = reinterpret_cast<float2*>(at);
   if (a.dh == 128)
     return nq == 1 ? run_stream<128, 1, 2, 3>(p, 0, s) : nq == 2 ? run_stream<128, 2, 2, 3>(p, 1, s) : run_stream<128, 4, 2, 2>(p, 2, s);
-  return nq == 1 ? run_stream<64, 1, 2, 3>(p, 3, s) : nq == 2 ? run_stream<64, 2, 2, 3>(p, 4, s) : run_stream<64, 4, 2, 3>(p, 5, s);
+  return nq == 1 ? run_stream<64, 1, 2, 3>(p, 3, s) : nq == 2 ? run_stream<64, 2, 2, 3>(p, 4, s) : run_stream<64, 4, 2, 2>(p, 5, s);
 }
 
 }  // namespace bs

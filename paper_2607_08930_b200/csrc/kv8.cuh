@@ -53,8 +53,8 @@ __device__ __forceinline__ void kv8_decode4(unsigned w, unsigned& a, unsigned& b
 
 // Largest r in [0, n) with key(r) <= item for a non-decreasing key with key(0) <= item: every lane of the calling warp
 // takes part and gets the result.  32 probes at a time: two round trips to memory up to 1024 rows.
-template <typename Key>
-__device__ __forceinline__ int warp_search(int n, int item, Key key) {
+template <typename Item, typename Key>
+__device__ __forceinline__ int warp_search(int n, Item item, Key key) {
   const int lane = threadIdx.x & 31;
   int lo = 0;
   for (int len = n; len > 1;) {
