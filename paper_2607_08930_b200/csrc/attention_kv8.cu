@@ -607,16 +607,21 @@ inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
 }  // namespace
 
+// Scratch: the streaming kernel's prefix, outputs and sums; the tensor-core kernel uses the same bytes for its chunks.
+constexpr size_t kPrefixBytes = (kAttnKv8MaxRows + 2) * sizeof(long long);
 size_t attention_kv8_scratch_bytes(int hq, int hkv, int dh) {
   (void)hq; (void)hkv;
   const size_t rows = (size_t)2 * kMaxStreamCtas * 32;
-  return up256((kAttnKv8MaxRows + 2) * sizeof(long long)) + up256(rows * dh * sizeof(float)) + up256(rows * sizeof(float2));
+  return up256(kPrefixBytes) + up256(rows * dh * sizeof(float)) + up256(rows * sizeof(float2));
 }
 
 cudaError_t launch_attention_kv8(const AttnKv8Args& a, cudaStream_t s) {
   if (a.M <= 0 || a.n_rows <= 0) return cudaSuccess;
   const int G = a.hq / a.hkv;
   const long long widest = (long long)(a.max_nq > 0 ? a.max_nq : a.M) * G;
+  // More than 32 query rows per kv head fill a good part of the 128-row tensor-core tiles.
+  if (a.dh == 128 && widest > 32)
+    return launch_attention_kv8_tc(a, static_cast<float*>(a.scratch), a.scratch_bytes / sizeof(float), s);
   const int nq = widest <= 8 ? 1 : widest <= 16 ? 2 : 4;
   StreamParams p;
   p.q = a.q; p.q_ld = a.q_ld; p.c = a.cache; p.out = a.out;
@@ -625,7 +630,7 @@ cudaError_t launch_attention_kv8(const AttnKv8Args& a, cudaStream_t s) {
   p.error_flag = a.error_flag;
   char* at = static_cast<char*>(a.scratch);
   p.prefix = reinterpret_cast<long long*>(at);
-  at += up256((kAttnKv8MaxRows + 2) * sizeof(long long));
+  at += up256(kPrefixBytes);
   p.part_o = reinterpret_cast<float*>(at);
   at += up256((size_t)2 * kMaxStreamCtas * 32 * a.dh * sizeof(float));
   p.part_ml = reinterpret_cast<float2*>(at);
