@@ -65,12 +65,14 @@ __device__ __forceinline__ uint2 lds64(unsigned at) {
 //
 // Few query rows per kv head (single tokens, block steps without grouped heads): bound by the bytes of the cache.
 // A work item is (row, kv head, tile of 8 NQ flattened (token, head-in-group) query rows).  All items' cache blocks
-// form one line - an item counts kItemCost blocks more than it has, about what starting and ending it costs - which the
-// CTAs of a single resident wave share evenly: CTA c takes units [c T / G, (c + 1) T / G), whatever the rows' lengths
-// are.  An item that a CTA holds whole is written out directly; a cut one leaves partial (output, reference, sum) parts,
-// at most two per CTA, that a second small kernel merges in order.
+// form one line - an item counts a few blocks more than it has, about what starting and ending it costs - which the
+// workers of a single resident wave share evenly: worker c takes units [c T / N, (c + 1) T / N), whatever the rows'
+// lengths are.  An item that a worker holds whole is written out directly; a cut one leaves partial (output, reference,
+// sum) parts, at most two per worker, that a second small kernel merges in order.
 //
-// Inside a CTA every warp takes whole cache blocks (32 keys) on its own, through a ring of shared-memory stages that
+// A worker is a CTA of four warps (W = 4: long items, few of them; the warps take the item's blocks in turn and add
+// their parts up in shared memory) or a single warp (W = 1: many items, whose beginnings and ends would leave four
+// warps waiting for one another).  Every warp moves its blocks (32 keys) through a ring of shared-memory stages that
 // no other warp touches (cp.async, no barrier): the next blocks are on their way while this one is computed.  Rows
 // behind the row's end arrive as zeros, whatever the cache holds there.
 //
@@ -86,7 +88,8 @@ __device__ __forceinline__ uint2 lds64(unsigned at) {
 constexpr int kStreamWarps = 4;
 constexpr int kStreamThreads = kStreamWarps * 32;
 constexpr int kMaxStreamCtas = 592;
-constexpr int kItemCost = 8;
+// Units an item counts beyond its blocks, in block times of one worker.
+__host__ __device__ constexpr int item_cost(int w) { return w == 1 ? 3 : 8; }
 // Weights are formed against a reference kBias below the running maximum (log2 units), which is moved only when the
 // maximum has grown kGrow above it: they stay below 2^kGrow in fp16 and keep full precision down to 2^-20 of the
 // largest one.
@@ -101,18 +104,22 @@ struct StreamParams {
   const int* kv_base;
   const int* vis;
   int n_rows, M, hq, hkv, tq;
-  long long* prefix;     // scratch: [n_rows + 1] units before each row, then the number of CTAs that share them
-  float* part_o;         // scratch: [2 CTAs][8 NQ][DH]
-  float2* part_ml;       // scratch: [2 CTAs][8 NQ]
+  struct Cut* cuts;      // scratch: [workers] the item that the boundary in front of a worker's share cuts
+  float* part_o;         // scratch: [2 workers][8 NQ][DH]
+  float2* part_ml;       // scratch: [2 workers][8 NQ]
   int* error_flag;
 };
+
+// A cut item: the workers that hold parts of it, its first query token, number of query rows (0: nothing is cut) and
+// kv head; whether worker c0 began with it (its part is then in the even slot, as everybody else's is).
+struct Cut { int c0, c1, t0, nrows, head, even, pad0, pad1; };
 
 struct RowInfo {
   int t0, n, vis, nb, tiles;
   long long base;
   // units of one item, and of the row
-  __device__ __forceinline__ int item_units() const { return nb > 0 ? nb + kItemCost : 0; }
-  __device__ __forceinline__ long long units(int hkv) const { return (long long)tiles * hkv * item_units(); }
+  __device__ __forceinline__ int item_units(int cost) const { return nb > 0 ? nb + cost : 0; }
+  __device__ __forceinline__ long long units(int hkv, int cost) const { return (long long)tiles * hkv * item_units(cost); }
 };
 
 __device__ __forceinline__ bool row_info(const int* cu_q, const int* kv_base, const int* vis, long long n_blocks, int M,
@@ -131,46 +138,49 @@ __device__ __forceinline__ bool row_info(const int* cu_q, const int* kv_base, co
   return ok;
 }
 
-// First unit of CTA c's share, and the CTA that holds unit u.
-__device__ __forceinline__ long long share_start(long long c, long long total, long long ctas) { return c * total / ctas; }
-__device__ __forceinline__ int share_of(long long u, long long total, long long ctas) { return (int)(((u + 1) * ctas - 1) / total); }
+// First unit of worker c's share, and the worker that holds unit u.
+__device__ __forceinline__ long long share_start(long long c, long long total, long long n) { return c * total / n; }
+__device__ __forceinline__ int share_of(long long u, long long total, long long n) { return (int)(((u + 1) * n - 1) / total); }
 
 template <int DH>
 constexpr int kTileBytes = kKv8Block * DH;           // one block of one head, K or V
-template <int DH, int NQ, int STAGES>
+template <int DH, int NQ, int STAGES, int W>
 struct StreamSmem {
-  static constexpr int R = 8 * NQ, LDO = DH + 4;
+  static constexpr int R = 8 * NQ, LDO = DH + 4, groups = kStreamWarps / W;
   static constexpr int ring = kStreamWarps * STAGES * 2 * kTileBytes<DH>;
-  static constexpr int merge = kStreamWarps * R * LDO * 4;         // the warps' outputs, over the ring when it is idle
+  static constexpr int merge = W == 1 ? 0 : W * R * LDO * 4;       // the warps' outputs, over the ring when it is idle
   static constexpr int front = ring > merge ? ring : merge;
   static constexpr int q = NQ * (DH / 32) * 32 * 16;               // query fragments, two k steps in 16 bytes
-  static constexpr int total = 128 + front + q + kStreamWarps * R * 8 + R * 4;
+  static constexpr int total = 128 + front + groups * (q + W * R * 8 + R * 4);
 };
 constexpr int kRowsPerThread = kAttnKv8MaxRows / kStreamThreads;
 
-template <int DH, int NQ, int STAGES, int MINB>
+template <int DH, int NQ, int STAGES, int W, int MINB>
 __global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(StreamParams p) {
-  using L = StreamSmem<DH, NQ, STAGES>;
+  using L = StreamSmem<DH, NQ, STAGES, W>;
   constexpr int KP = DH / 32;            // pairs of k steps of the scores
   constexpr int MD = DH / 16;            // m tiles of the output
   constexpr int kHalves = NQ == 1 ? 2 : 1;             // (unrolled, the wider instantiations do not fit their registers)
-  constexpr int R = L::R, LDO = L::LDO, TB = kTileBytes<DH>;
+  constexpr int R = L::R, LDO = L::LDO, TB = kTileBytes<DH>, kCost = item_cost(W);
   extern __shared__ unsigned char smem_raw[];
-  unsigned char* smem = smem_raw + ((128u - (tc::smem_u32(smem_raw) & 127u)) & 127u);
-  float* s_o = reinterpret_cast<float*>(smem);                               // [warps][R][LDO]
-  uint4* s_q = reinterpret_cast<uint4*>(smem + L::front);                    // [NQ][KS][32]
-  float2* s_ml = reinterpret_cast<float2*>(smem + L::front + L::q);          // [warps][R]
-  float* s_sc = reinterpret_cast<float*>(s_ml + kStreamWarps * R);           // [R]
   __shared__ long long s_warp[kStreamWarps];
-  __shared__ long long s_first;          // units before s_row
-  __shared__ int s_row;
+  __shared__ long long s_first[L::groups];   // units before s_row
+  __shared__ int s_row[L::groups];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int g = lane >> 2, c4 = lane & 3;
   const int G = p.hq / p.hkv;
+  // this thread's worker: its number in the CTA, and the warp's and the thread's number in the worker
+  const int wk = W == 1 ? warp : 0, member = W == 1 ? 0 : warp, wtid = W == 1 ? lane : tid;
+  auto sync_worker = [&]() { if (W == 1) __syncwarp(); else __syncthreads(); };
+  unsigned char* smem = smem_raw + ((128u - (tc::smem_u32(smem_raw) & 127u)) & 127u);
+  float* s_o = reinterpret_cast<float*>(smem);                               // [warps][R][LDO] (W = 4)
+  uint4* s_q = reinterpret_cast<uint4*>(smem + L::front + wk * (L::q + W * R * 8 + R * 4));    // [NQ][KP][32]
+  float2* s_ml = reinterpret_cast<float2*>(s_q + L::q / 16);                 // [W][R]
+  float* s_sc = reinterpret_cast<float*>(s_ml + W * R);                      // [R]
   pdl_wait();
   pdl_trigger();
 
-  // ---- units before every row (exclusive prefix); the row that holds this CTA's first unit ----
+  // ---- units before every row (exclusive prefix); the row that holds each worker's first unit ----
   long long before[kRowsPerThread], cost[kRowsPerThread];
   long long total = 0;
 #pragma unroll
@@ -182,7 +192,7 @@ __global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(S
       RowInfo ri;
       if (!row_info(p.cu_q, p.kv_base, p.vis, p.c.n_blocks, p.M, p.tq, r, ri) && blockIdx.x == 0 && p.error_flag)
         atomicMax(p.error_flag, 100 + SITE_ATTN_KV8);
-      w = ri.units(p.hkv);
+      w = ri.units(p.hkv, kCost);
     }
     long long inc = w;
 #pragma unroll
@@ -203,20 +213,19 @@ __global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(S
     __syncthreads();
   }
   // a share holds one block per warp at least
-  const long long ctas = max(1ll, min((long long)gridDim.x, total / (kItemCost + kStreamWarps)));
-  const long long u0 = share_start(blockIdx.x, total, ctas), u1 = share_start((long long)blockIdx.x + 1, total, ctas);
+  const long long workers = max(1ll, min((long long)gridDim.x * L::groups, total / (kCost + W)));
+  const long long me = (long long)blockIdx.x * L::groups + wk;
 #pragma unroll
-  for (int i = 0; i < kRowsPerThread; ++i) {
-    if (i * kStreamThreads >= p.n_rows) break;
-    const int r = i * kStreamThreads + tid;
-    if (r < p.n_rows) {
-      if (blockIdx.x == 0) p.prefix[r] = before[i];
-      if (before[i] <= u0 && u0 < before[i] + cost[i]) { s_row = r; s_first = before[i]; }   // one thread at most
+  for (int k = 0; k < L::groups; ++k) {
+    const long long u = share_start((long long)blockIdx.x * L::groups + k, total, workers);
+#pragma unroll
+    for (int i = 0; i < kRowsPerThread; ++i) {
+      if (i * kStreamThreads >= p.n_rows) break;
+      if (before[i] <= u && u < before[i] + cost[i]) {     // (rows behind the last one count nothing); one thread at most
+        s_row[k] = i * kStreamThreads + tid;
+        s_first[k] = before[i];
+      }
     }
-  }
-  if (blockIdx.x == 0 && tid == 0) {
-    p.prefix[p.n_rows] = total;
-    p.prefix[p.n_rows + 1] = ctas;
   }
   // rows that see nothing: zeros
   for (int r = blockIdx.x; r < p.n_rows; r += gridDim.x) {
@@ -227,12 +236,32 @@ __global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(S
       for (long long i = tid; i < (long long)z.n * (p.hq * DH / 8); i += kStreamThreads) dst[i] = make_uint4(0, 0, 0, 0);
     }
   }
-  if (total == 0 || (long long)blockIdx.x >= ctas) return;
   __syncthreads();
-  int row = s_row;
-  long long first = s_first;
+  if (total == 0 || me >= workers) {
+    if (wtid == 0) p.cuts[me].nrows = 0;
+    return;                                // (from here on only the worker's own threads wait for one another)
+  }
+  const long long u0 = share_start(me, total, workers), u1 = share_start(me + 1, total, workers);
+  int row = s_row[wk];
+  long long first = s_first[wk];
   RowInfo ri;
   row_info(p.cu_q, p.kv_base, p.vis, p.c.n_blocks, p.M, p.tq, row, ri);
+  {   // does this share begin inside an item's blocks?
+    const int per = ri.item_units(kCost), item = (int)((u0 - first) / per), at = (int)((u0 - first) % per);
+    if (wtid == 0) {
+      Cut c = {};
+      if (at > kCost) {
+        const long long begin = u0 - at;                     // the item's first unit; its blocks begin kCost later
+        c.c0 = share_of(begin + kCost, total, workers);
+        c.c1 = share_of(begin + per - 1, total, workers);
+        c.even = begin <= share_start(c.c0, total, workers);
+        c.head = item / ri.tiles;
+        c.t0 = ri.t0 + item % ri.tiles * p.tq;
+        c.nrows = min(p.tq, ri.t0 + ri.n - c.t0) * G;
+      }
+      p.cuts[me] = c;
+    }
+  }
 
   // this warp's ring, and this lane's part of a block's copy: 16 bytes i * 512 + lane * 16 of K and of V
   const unsigned ring = tc::smem_u32(smem) + (unsigned)warp * STAGES * 2 * TB;
@@ -252,35 +281,37 @@ __global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(S
   };
 
   for (long long u = u0; u < u1;) {
-    while (u - first >= ri.units(p.hkv)) {
-      first += ri.units(p.hkv);
+    for (long long w; u - first >= (w = ri.units(p.hkv, kCost));) {
+      first += w;
       ++row;
       row_info(p.cu_q, p.kv_base, p.vis, p.c.n_blocks, p.M, p.tq, row, ri);
     }
     const long long local = u - first;
-    const int per = ri.item_units(), item = (int)(local / per), at = (int)(local % per);
-    const int b0 = max(0, at - kItemCost);                        // an item's first kItemCost units hold no block
-    const int b1 = (int)min((long long)ri.nb, max(0ll, at + (u1 - u) - kItemCost));
+    const int per = ri.item_units(kCost);
+    const int item = local < 0x7fffffffll ? (int)local / per : (int)(local / per);
+    const int at = (int)(local - (long long)item * per);
+    const int b0 = max(0, at - kCost);                            // an item's first kCost units hold no block
+    const int b1 = (int)min((long long)ri.nb, max(0ll, at + (u1 - u) - kCost));
     const bool opens = u == u0;                                   // (the partial slot of this segment)
     u += per - at;
     if (b1 <= b0) continue;
-    const int head = item / ri.tiles, tile = item % ri.tiles;
+    const int head = item / ri.tiles, tile = item - head * ri.tiles;
     const int t0 = ri.t0 + tile * p.tq, nt = min(p.tq, ri.t0 + ri.n - t0), nrows = nt * G;
 
-    __syncthreads();                     // the previous segment's fragments, sums and outputs are no longer read
+    sync_worker();                       // the previous segment's fragments, sums and outputs are no longer read
 #pragma unroll
     for (int i = 0; i < STAGES - 1; ++i) {
-      if (b0 + warp + i * kStreamWarps < b1) fetch(i, b0 + warp + i * kStreamWarps, head);
+      if (b0 + member + i * W < b1) fetch(i, b0 + member + i * W, head);
       asm volatile("cp.async.commit_group;\n" ::: "memory");
     }
     float ks_next = 1.f, vs_next = 1.f;
-    if (b0 + warp < b1) {
-      const size_t sa = (size_t)(ri.base + b0 + warp) * p.hkv + head;
+    if (b0 + member < b1) {
+      const size_t sa = (size_t)(ri.base + b0 + member) * p.hkv + head;
       ks_next = __ldg(p.c.k_scale + sa);
       vs_next = __ldg(p.c.v_scale + sa);
     }
     // ---- queries: fp16 fragments in shared memory ----
-    for (int nq = warp; nq < NQ; nq += kStreamWarps) {
+    for (int nq = member; nq < NQ; nq += W) {
       const int f = nq * 8 + g;          // query row of this lane (n index of the scores)
       const bool valid = f < nrows;
       const bf16* src = p.q + (size_t)(t0 + (valid ? f / G : 0)) * p.q_ld + (head * G + (valid ? f % G : 0)) * DH + c4 * (DH / 4);
@@ -313,7 +344,7 @@ __global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(S
         s_q[(nq * KP + k) * 32 + lane] = make_uint4(w[0], w[1], w[2], w[3]);
       }
     }
-    __syncthreads();
+    sync_worker();
 
     float o[NQ][MD][4];
     float ref[NQ][2], sum[NQ][2], sc[NQ][2];         // of query rows nq * 8 + 2 c4 + {0, 1}
@@ -335,14 +366,14 @@ __global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(S
     }
 
     int stage = 0;
-    for (int b = b0 + warp; b < b1; b += kStreamWarps) {
+    for (int b = b0 + member; b < b1; b += W) {
       const float ks = kv8_clamp_scale(ks_next), vs = kv8_clamp_scale(vs_next);
       {
-        const int nb = b + (STAGES - 1) * kStreamWarps;
+        const int nb = b + (STAGES - 1) * W;
         if (nb < b1) fetch(stage == 0 ? STAGES - 1 : stage - 1, nb, head);
         asm volatile("cp.async.commit_group;\n" ::: "memory");
-        if (b + kStreamWarps < b1) {
-          const size_t sa = (size_t)(ri.base + b + kStreamWarps) * p.hkv + head;
+        if (b + W < b1) {
+          const size_t sa = (size_t)(ri.base + b + W) * p.hkv + head;
           ks_next = __ldg(p.c.k_scale + sa);
           vs_next = __ldg(p.c.v_scale + sa);
         }
@@ -451,18 +482,51 @@ __global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(S
       __syncwarp();                      // the stage may be filled again
     }
 
-    // ---- the warps' parts of this segment become one ----
+    const bool whole = b0 == 0 && b1 == ri.nb;
+    const size_t slot = 2 * (size_t)me + (opens ? 0 : 1);
 #pragma unroll
     for (int nq = 0; nq < NQ; ++nq)
 #pragma unroll
       for (int y = 0; y < 2; ++y) {
-        float l = sum[nq][y];
-        l += __shfl_xor_sync(0xffffffffu, l, 4);
-        l += __shfl_xor_sync(0xffffffffu, l, 8);
-        l += __shfl_xor_sync(0xffffffffu, l, 16);
-        if (g == 0) s_ml[warp * R + nq * 8 + 2 * c4 + y] = make_float2(ref[nq][y], l);
+        sum[nq][y] += __shfl_xor_sync(0xffffffffu, sum[nq][y], 4);
+        sum[nq][y] += __shfl_xor_sync(0xffffffffu, sum[nq][y], 8);
+        sum[nq][y] += __shfl_xor_sync(0xffffffffu, sum[nq][y], 16);
       }
-    __syncthreads();                     // (the ring is idle from here on)
+    if constexpr (W == 1) {
+      // straight from the registers: lane (g, c4) holds 16 (head_dim 64: 8) dims of query rows 2 c4 and 2 c4 + 1
+#pragma unroll
+      for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          const int f = nq * 8 + 2 * c4 + y;
+          if (f >= nrows) continue;
+          if (whole) {
+            const float inv = 1.0f / sum[nq][y];
+            bf16* dst = p.out + (size_t)(t0 + f / G) * (p.hq * DH) + (head * G + f % G) * DH + g * (DH / 8);
+#pragma unroll
+            for (int i = 0; i < MD; i += 4) {
+              uint4 w;
+              __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&w);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) h[j] = __floats2bfloat162_rn(o[nq][i + j][y] * inv, o[nq][i + j][2 + y] * inv);
+              *reinterpret_cast<uint4*>(dst + 2 * i) = w;
+            }
+          } else {
+            float* dst = p.part_o + (slot * R + f) * DH + g * (DH / 8);
+#pragma unroll
+            for (int i = 0; i < MD; i += 2)
+              *reinterpret_cast<float4*>(dst + 2 * i) = make_float4(o[nq][i][y], o[nq][i][2 + y], o[nq][i + 1][y], o[nq][i + 1][2 + y]);
+            if (g == 0) p.part_ml[slot * R + f] = make_float2(ref[nq][y], sum[nq][y]);
+          }
+        }
+    } else {
+    // ---- the warps' parts of this segment become one ----
+#pragma unroll
+    for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+      for (int y = 0; y < 2; ++y)
+        if (g == 0) s_ml[member * R + nq * 8 + 2 * c4 + y] = make_float2(ref[nq][y], sum[nq][y]);
+    sync_worker();                       // (the ring is idle from here on)
 #pragma unroll
     for (int nq = 0; nq < NQ; ++nq)
 #pragma unroll
@@ -470,26 +534,24 @@ __global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(S
         const int f = nq * 8 + 2 * c4 + y;
         float m = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < kStreamWarps; ++w) m = fmaxf(m, s_ml[w * R + f].x);
+        for (int w = 0; w < W; ++w) m = fmaxf(m, s_ml[w * R + f].x);
         // a warp without blocks has an output of zeros; one that met nothing but NaN has NaN, and keeps it
         const float turn = ref[nq][y] > -INFINITY ? exp2_fast(ref[nq][y] - m) : 1.f;
-        float* dst = s_o + (warp * R + f) * LDO + g * (DH / 8);
+        float* dst = s_o + (member * R + f) * LDO + g * (DH / 8);
 #pragma unroll
         for (int i = 0; i < MD; i += 2)
           *reinterpret_cast<float4*>(dst + 2 * i) = make_float4(o[nq][i][y] * turn, o[nq][i][2 + y] * turn,
                                                                 o[nq][i + 1][y] * turn, o[nq][i + 1][2 + y] * turn);
       }
-    __syncthreads();
-    const bool whole = b0 == 0 && b1 == ri.nb;
-    const size_t slot = 2 * (size_t)blockIdx.x + (opens ? 0 : 1);
-    for (int v = tid; v < nrows * (DH / 4); v += kStreamThreads) {
+    sync_worker();
+    for (int v = wtid; v < nrows * (DH / 4); v += W * 32) {
       const int f = v / (DH / 4), d = v % (DH / 4) * 4;
       float m = -INFINITY, l = 0.f;
 #pragma unroll
-      for (int w = 0; w < kStreamWarps; ++w) m = fmaxf(m, s_ml[w * R + f].x);
+      for (int w = 0; w < W; ++w) m = fmaxf(m, s_ml[w * R + f].x);
       float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int w = 0; w < kStreamWarps; ++w) {
+      for (int w = 0; w < W; ++w) {
         const float2 ml = s_ml[w * R + f];
         l += ml.x > -INFINITY ? ml.y * exp2_fast(ml.x - m) : ml.y;
         const float4 x = *reinterpret_cast<const float4*>(s_o + (w * R + f) * LDO + d);
@@ -507,82 +569,95 @@ __global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(S
         if (d == 0) p.part_ml[slot * R + f] = make_float2(m, l);
       }
     }
+    }
   }
 }
 
-// Items that more than one CTA held: out = sum_c 2^(m_c - m) o_c / sum_c 2^(m_c - m) l_c over the parts in order.
-// One CTA per boundary between two shares; the boundaries inside an item share its output (query row, 32 dims) between
-// them, a warp each: four groups of eight lanes take every fourth part.
+// Items that more than one worker held: out = sum_c 2^(m_c - m) o_c / sum_c 2^(m_c - m) l_c over the parts in order.
+// One CTA per boundary between two shares; the boundaries inside an item divide its output, in units of four dims of a
+// query row, between them.  The parts' weights are formed once per row; then a unit is one thread, or, where there are
+// fewer units than threads, up to 32 neighbouring lanes, each with every so-manieth part.
+constexpr int kMergeThreads = 256;
+// Weights of one CTA: parts x the rows it touches.  With b boundaries inside an item of at most 32 rows it is at most
+// (b + 1) (32 / b + 2) <= 2 b + 66, and b < 4 x 592.
+constexpr int kMergeWeights = 2 * kMaxStreamCtas * kStreamWarps + 66;
 template <int DH>
-__global__ void __launch_bounds__(256) k_attention_kv8_merge(StreamParams p, int R) {
+__global__ void __launch_bounds__(kMergeThreads) k_attention_kv8_merge(StreamParams p, int R) {
+  __shared__ float s_w[kMergeWeights];
   pdl_wait();
   pdl_trigger();
-  const long long total = p.prefix[p.n_rows], ctas = p.prefix[p.n_rows + 1];
-  const int cut = (int)blockIdx.x + 1;                // the boundary in front of share `cut`
-  if (cut >= ctas) return;
-  const long long u = share_start(cut, total, ctas);
-  // the last row whose prefix is <= u (a row without units shares its prefix with the next one)
-  const int row = warp_search(p.n_rows, u, [&](int i) { return p.prefix[i]; });
-  RowInfo ri;
-  row_info(p.cu_q, p.kv_base, p.vis, p.c.n_blocks, p.M, p.tq, row, ri);
-  const long long local = u - p.prefix[row];
-  const int per = ri.item_units();
-  if (per == 0) return;
-  const int item = (int)(local / per);
-  // the item's blocks are units [first, first + nb) of the line
-  const long long first = u - local % per + kItemCost;
-  if (u <= first) return;                             // cut in front of its blocks: nothing is split here
-  const int c0 = share_of(first, total, ctas), c1 = share_of(first + ri.nb - 1, total, ctas);
-  const int head = item / ri.tiles, tile = item % ri.tiles;
+  const Cut c = p.cuts[blockIdx.x];
+  if (c.nrows == 0) return;
+  const int parts = c.c1 - c.c0 + 1, cuts = parts - 1, nth = (int)blockIdx.x - c.c0 - 1;
+  const int units = c.nrows * (DH / 4);
+  const int v0 = (int)((long long)units * nth / cuts), v1 = (int)((long long)units * (nth + 1) / cuts);
+  if (v0 >= v1) return;
+  const int f0 = v0 / (DH / 4), f1 = (v1 - 1) / (DH / 4);
   const int G = p.hq / p.hkv, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int t0 = ri.t0 + tile * p.tq, nrows = min(p.tq, ri.t0 + ri.n - t0) * G;
-  // a CTA's first segment is in its even slot: this item, if the CTA's share begins at or inside it
-  auto slot_of = [&](int c) { return (size_t)2 * c + (first - kItemCost > share_start(c, total, ctas) ? 1 : 0); };
-  const int sub = lane >> 3;
-  for (int v = (cut - c0 - 1) * 8 + warp; v < nrows * (DH / 32); v += (c1 - c0) * 8) {
-    const int f = v / (DH / 32), d = v % (DH / 32) * 32 + (lane & 7) * 4;
+  // the first holder's part is in its odd slot unless it began with the item; everybody else began with it
+  auto slot_of = [&](int k) { return (size_t)2 * (c.c0 + k) + (k == 0 && !c.even ? 1 : 0); };
+  for (int f = f0 + warp; f <= f1; f += kMergeThreads / 32) {
     float m = -INFINITY, l = 0.f;
-    for (int c = c0 + lane; c <= c1; c += 32) m = fmaxf(m, p.part_ml[slot_of(c) * R + f].x);
+    for (int k = lane; k < parts; k += 32) m = fmaxf(m, p.part_ml[slot_of(k) * R + f].x);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int c = c0 + sub; c <= c1; c += 4) {
-      const size_t at = slot_of(c) * R + f;
-      const float2 ml = p.part_ml[at];
-      const float4 x = *reinterpret_cast<const float4*>(p.part_o + at * DH + d);
-      const float w = ml.x > -INFINITY ? exp2_fast(ml.x - m) : 1.f;              // (parts of NaN stay NaN)
-      l += w * ml.y;
-      acc.x += w * x.x; acc.y += w * x.y; acc.z += w * x.z; acc.w += w * x.w;
+    for (int k = lane; k < parts; k += 32) {
+      const float2 ml = p.part_ml[slot_of(k) * R + f];
+      l += (ml.x > -INFINITY ? exp2_fast(ml.x - m) : 1.f) * ml.y;     // (parts of NaN stay NaN)
     }
 #pragma unroll
-    for (int o = 8; o < 32; o <<= 1) {
-      l += __shfl_xor_sync(0xffffffffu, l, o);
+    for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+    const float inv = 1.0f / l;
+    for (int k = lane; k < parts; k += 32) {
+      const float ref = p.part_ml[slot_of(k) * R + f].x;
+      s_w[(f - f0) * parts + k] = (ref > -INFINITY ? exp2_fast(ref - m) : 1.f) * inv;
+    }
+  }
+  __syncthreads();
+  int lanes = 1;
+  while (lanes < 32 && 2 * lanes <= parts && 2 * lanes * (v1 - v0) <= kMergeThreads) lanes *= 2;
+  const int sub = threadIdx.x & (lanes - 1);
+  for (int base = v0; base < v1; base += kMergeThreads / lanes) {     // uniform: every lane takes part in the shuffles
+    const int v = base + (int)threadIdx.x / lanes;
+    const int f = min(v, v1 - 1) / (DH / 4), d = min(v, v1 - 1) % (DH / 4) * 4;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int k = sub; k < parts; k += lanes) {
+      const float4 x = *reinterpret_cast<const float4*>(p.part_o + (slot_of(k) * R + f) * DH + d);
+      const float w = s_w[(f - f0) * parts + k];
+      acc.x += w * x.x; acc.y += w * x.y; acc.z += w * x.z; acc.w += w * x.w;
+    }
+    for (int o = 1; o < lanes; o <<= 1) {
       acc.x += __shfl_xor_sync(0xffffffffu, acc.x, o);
       acc.y += __shfl_xor_sync(0xffffffffu, acc.y, o);
       acc.z += __shfl_xor_sync(0xffffffffu, acc.z, o);
       acc.w += __shfl_xor_sync(0xffffffffu, acc.w, o);
     }
-    if (sub == 0) {
-      const float inv = 1.0f / l;
+    if (sub == 0 && v < v1) {
       uint2 w;
       __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&w);
-      h[0] = __floats2bfloat162_rn(acc.x * inv, acc.y * inv);
-      h[1] = __floats2bfloat162_rn(acc.z * inv, acc.w * inv);
-      *reinterpret_cast<uint2*>(p.out + (size_t)(t0 + f / G) * (p.hq * DH) + (head * G + f % G) * DH + d) = w;
+      h[0] = __floats2bfloat162_rn(acc.x, acc.y);
+      h[1] = __floats2bfloat162_rn(acc.z, acc.w);
+      *reinterpret_cast<uint2*>(p.out + (size_t)(c.t0 + f / G) * (p.hq * DH) + (c.head * G + f % G) * DH + d) = w;
     }
   }
 }
 
+constexpr size_t kCutBytes = (size_t)kMaxStreamCtas * kStreamWarps * sizeof(Cut);
+// Query rows of all partial slots, two slots per worker: 296 CTAs of four single-warp workers with 32 rows, or 592
+// four-warp workers.  A launch takes no more CTAs than these hold.
+constexpr size_t kPartRows = 2 * (size_t)kStreamWarps * 296 * 32;
+
 // Per device: how many CTAs of each instantiation one wave holds (0: not asked yet).
-struct DeviceInfo { int wave[6]; };
+struct DeviceInfo { int wave[12]; };
 DeviceInfo g_dev[kMaxDevices];
 std::mutex g_mutex;
 
-template <int DH, int NQ, int STAGES, int MINB>
-cudaError_t run_stream(StreamParams p, int index, cudaStream_t s) {
-  constexpr auto kernel = k_attention_kv8_stream<DH, NQ, STAGES, MINB>;
-  constexpr int smem = StreamSmem<DH, NQ, STAGES>::total;
+template <int DH, int NQ, int STAGES, int W, int MINB>
+cudaError_t run_stream(StreamParams p, cudaStream_t s) {
+  constexpr int index = (DH == 128 ? 6 : 0) + (NQ == 4 ? 2 : NQ - 1) * 2 + (W == 1 ? 1 : 0);
+  constexpr auto kernel = k_attention_kv8_stream<DH, NQ, STAGES, W, MINB>;
+  constexpr int smem = StreamSmem<DH, NQ, STAGES, W>::total;
   DeviceInfo* d = device_slot(g_dev);
   if (!d) return cudaErrorInvalidDevice;
   {
@@ -595,30 +670,30 @@ cudaError_t run_stream(StreamParams p, int index, cudaStream_t s) {
       if (r == cudaSuccess) r = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, kernel, kStreamThreads, smem);
       if (r != cudaSuccess) return r;
       if (sms < 1 || per < 1) return cudaErrorInvalidDevice;
-      d->wave[index] = std::min(sms * per, kMaxStreamCtas);
+      d->wave[index] = std::min(std::min(sms * per, kMaxStreamCtas), (int)(kPartRows / (2 * 8 * NQ * (kStreamWarps / W))));
     }
   }
   cudaError_t r = launch_pdl(kernel, dim3(d->wave[index]), dim3(kStreamThreads), (size_t)smem, s, p);
   if (r != cudaSuccess) return r;
-  return launch_pdl(k_attention_kv8_merge<DH>, dim3(d->wave[index]), dim3(256), 0, s, p, 8 * NQ);
+  return launch_pdl(k_attention_kv8_merge<DH>, dim3(d->wave[index] * (kStreamWarps / W)), dim3(kMergeThreads), 0, s, p, 8 * NQ);
 }
 
 inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
+
 }  // namespace
 
-// Scratch: the streaming kernel's prefix, outputs and sums; the tensor-core kernel uses the same bytes for its chunks.
-constexpr size_t kPrefixBytes = (kAttnKv8MaxRows + 2) * sizeof(long long);
+// Scratch: the streaming kernel's cuts, partial outputs and sums; the tensor-core kernel uses the same bytes for its chunks.
 size_t attention_kv8_scratch_bytes(int hq, int hkv, int dh) {
   (void)hq; (void)hkv;
-  const size_t rows = (size_t)2 * kMaxStreamCtas * 32;
-  return up256(kPrefixBytes) + up256(rows * dh * sizeof(float)) + up256(rows * sizeof(float2));
+  return up256(kCutBytes) + up256(kPartRows * dh * sizeof(float)) + up256(kPartRows * sizeof(float2));
 }
 
 cudaError_t launch_attention_kv8(const AttnKv8Args& a, cudaStream_t s) {
   if (a.M <= 0 || a.n_rows <= 0) return cudaSuccess;
   const int G = a.hq / a.hkv;
-  const long long widest = (long long)(a.max_nq > 0 ? a.max_nq : a.M) * G;
+  const int max_nq = a.max_nq > 0 ? std::min(a.max_nq, a.M) : a.M;
+  const long long widest = (long long)max_nq * G;
   // More than 32 query rows per kv head fill a good part of the 128-row tensor-core tiles.
   if (a.dh == 128 && widest > 32)
     return launch_attention_kv8_tc(a, static_cast<float*>(a.scratch), a.scratch_bytes / sizeof(float), s);
@@ -629,14 +704,22 @@ cudaError_t launch_attention_kv8(const AttnKv8Args& a, cudaStream_t s) {
   p.n_rows = a.n_rows; p.M = a.M; p.hq = a.hq; p.hkv = a.hkv; p.tq = 8 * nq / G;
   p.error_flag = a.error_flag;
   char* at = static_cast<char*>(a.scratch);
-  p.prefix = reinterpret_cast<long long*>(at);
-  at += up256(kPrefixBytes);
+  p.cuts = reinterpret_cast<Cut*>(at);
+  at += up256(kCutBytes);
   p.part_o = reinterpret_cast<float*>(at);
-  at += up256((size_t)2 * kMaxStreamCtas * 32 * a.dh * sizeof(float));
+  at += up256(kPartRows * a.dh * sizeof(float));
   p.part_ml = reinterpret_cast<float2*>(at);
-  if (a.dh == 128)
-    return nq == 1 ? run_stream<128, 1, 2, 3>(p, 0, s) : nq == 2 ? run_stream<128, 2, 2, 3>(p, 1, s) : run_stream<128, 4, 2, 2>(p, 2, s);
-  return nq == 1 ? run_stream<64, 1, 2, 3>(p, 3, s) : nq == 2 ? run_stream<64, 2, 2, 3>(p, 4, s) : run_stream<64, 4, 2, 2>(p, 5, s);
+  // Single-warp workers once there are about as many items as half of them.
+  const long long items = (long long)a.n_rows * a.hkv * ((max_nq + p.tq - 1) / p.tq);
+  const bool many = items >= 592;
+  if (a.dh == 128) {
+    if (nq == 1) return many ? run_stream<128, 1, 2, 1, 3>(p, s) : run_stream<128, 1, 2, 4, 3>(p, s);
+    if (nq == 2) return many ? run_stream<128, 2, 2, 1, 2>(p, s) : run_stream<128, 2, 2, 4, 3>(p, s);
+    return many ? run_stream<128, 4, 2, 1, 2>(p, s) : run_stream<128, 4, 2, 4, 2>(p, s);
+  }
+  if (nq == 1) return many ? run_stream<64, 1, 2, 1, 3>(p, s) : run_stream<64, 1, 2, 4, 3>(p, s);
+  if (nq == 2) return many ? run_stream<64, 2, 2, 1, 3>(p, s) : run_stream<64, 2, 2, 4, 3>(p, s);
+  return many ? run_stream<64, 4, 2, 1, 2>(p, s) : run_stream<64, 4, 2, 4, 2>(p, s);
 }
 
 }  // namespace bs
