@@ -388,6 +388,7 @@ __global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(S
         float s[NQ][4];
 #pragma unroll
         for (int nq = 0; nq < NQ; ++nq) s[nq][0] = s[nq][1] = s[nq][2] = s[nq][3] = 0.f;
+        float s_odd[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int h = 0; h < KP / 2; ++h) {             // 16 bytes of both keys: four k steps
           uint4 kr[2];
@@ -403,14 +404,22 @@ __global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(S
           kv8_decode4(kr[0].y, a[1][0], a[1][2]); kv8_decode4(kr[1].y, a[1][1], a[1][3]);
           kv8_decode4(kr[0].z, a[2][0], a[2][2]); kv8_decode4(kr[1].z, a[2][1], a[2][3]);
           kv8_decode4(kr[0].w, a[3][0], a[3][2]); kv8_decode4(kr[1].w, a[3][1], a[3][3]);
+          // a product's latency is that of two to three others: the chains of the query tiles (one tile: of even and
+          // odd k steps) take turns
 #pragma unroll
-          for (int i = 0; i < 2; ++i)
+          for (int i = 0; i < 2; ++i) {
+            uint4 qv[NQ];
 #pragma unroll
-            for (int nq = 0; nq < NQ; ++nq) {
-              const uint4 qv = NQ == 1 ? qf[NQ == 1 ? 2 * h + i : 0] : s_q[(nq * KP + 2 * h + i) * 32 + lane];
-              mma_f16(s[nq], a[2 * i], qv.x, qv.y);
-              mma_f16(s[nq], a[2 * i + 1], qv.z, qv.w);
-            }
+            for (int nq = 0; nq < NQ; ++nq) qv[nq] = NQ == 1 ? qf[NQ == 1 ? 2 * h + i : 0] : s_q[(nq * KP + 2 * h + i) * 32 + lane];
+#pragma unroll
+            for (int nq = 0; nq < NQ; ++nq) mma_f16(s[nq], a[2 * i], qv[nq].x, qv[nq].y);
+#pragma unroll
+            for (int nq = 0; nq < NQ; ++nq) mma_f16(NQ == 1 ? s_odd : s[nq], a[2 * i + 1], qv[nq].z, qv[nq].w);
+          }
+        }
+        if (NQ == 1) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) s[0][j] += s_odd[j];
         }
         unsigned pr[NQ][2];
         bool grow = false;
@@ -598,49 +607,71 @@ __global__ void __launch_bounds__(kMergeThreads) k_attention_kv8_merge(StreamPar
   auto slot_of = [&](int k) { return (size_t)2 * (c.c0 + k) + (k == 0 && !c.even ? 1 : 0); };
   for (int f = f0 + warp; f <= f1; f += kMergeThreads / 32) {
     float m = -INFINITY, l = 0.f;
-    for (int k = lane; k < parts; k += 32) m = fmaxf(m, p.part_ml[slot_of(k) * R + f].x);
+    const float2 mine = lane < parts ? p.part_ml[slot_of(lane) * R + f] : make_float2(-INFINITY, 0.f);
+    m = mine.x;
+    for (int k = lane + 32; k < parts; k += 32) m = fmaxf(m, p.part_ml[slot_of(k) * R + f].x);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    for (int k = lane; k < parts; k += 32) {
+    auto weight = [&](float ref) { return ref > -INFINITY ? exp2_fast(ref - m) : 1.f; };     // (parts of NaN stay NaN)
+    l = weight(mine.x) * mine.y;
+    for (int k = lane + 32; k < parts; k += 32) {
       const float2 ml = p.part_ml[slot_of(k) * R + f];
-      l += (ml.x > -INFINITY ? exp2_fast(ml.x - m) : 1.f) * ml.y;     // (parts of NaN stay NaN)
+      l += weight(ml.x) * ml.y;
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
     const float inv = 1.0f / l;
-    for (int k = lane; k < parts; k += 32) {
-      const float ref = p.part_ml[slot_of(k) * R + f].x;
-      s_w[(f - f0) * parts + k] = (ref > -INFINITY ? exp2_fast(ref - m) : 1.f) * inv;
-    }
+    if (lane < parts) s_w[(f - f0) * parts + lane] = weight(mine.x) * inv;
+    for (int k = lane + 32; k < parts; k += 32) s_w[(f - f0) * parts + k] = weight(p.part_ml[slot_of(k) * R + f].x) * inv;
   }
   __syncthreads();
+  auto store = [&](int v, const float4& x) {
+    const int f = v / (DH / 4), d = v % (DH / 4) * 4;
+    uint2 w;
+    __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&w);
+    h[0] = __floats2bfloat162_rn(x.x, x.y);
+    h[1] = __floats2bfloat162_rn(x.z, x.w);
+    *reinterpret_cast<uint2*>(p.out + (size_t)(c.t0 + f / G) * (p.hq * DH) + (c.head * G + f % G) * DH + d) = w;
+  };
   int lanes = 1;
   while (lanes < 32 && 2 * lanes <= parts && 2 * lanes * (v1 - v0) <= kMergeThreads) lanes *= 2;
-  const int sub = threadIdx.x & (lanes - 1);
-  for (int base = v0; base < v1; base += kMergeThreads / lanes) {     // uniform: every lane takes part in the shuffles
-    const int v = base + (int)threadIdx.x / lanes;
-    const int f = min(v, v1 - 1) / (DH / 4), d = min(v, v1 - 1) % (DH / 4) * 4;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int k = sub; k < parts; k += lanes) {
-      const float4 x = *reinterpret_cast<const float4*>(p.part_o + (slot_of(k) * R + f) * DH + d);
-      const float w = s_w[(f - f0) * parts + k];
-      acc.x += w * x.x; acc.y += w * x.y; acc.z += w * x.z; acc.w += w * x.w;
+  if (lanes == 1) {                        // four units of a thread at a time: their loads are independent
+    for (int base = v0 + (int)threadIdx.x; base < v1; base += 4 * kMergeThreads) {
+      float4 acc[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+      for (int k = 0; k < parts; ++k) {
+        const float* from = p.part_o + slot_of(k) * R * DH;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int v = min(base + j * kMergeThreads, v1 - 1);
+          const float4 x = *reinterpret_cast<const float4*>(from + 4 * v);
+          const float w = s_w[(v / (DH / 4) - f0) * parts + k];
+          acc[j].x += w * x.x; acc[j].y += w * x.y; acc[j].z += w * x.z; acc[j].w += w * x.w;
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (base + j * kMergeThreads < v1) store(base + j * kMergeThreads, acc[j]);
     }
-    for (int o = 1; o < lanes; o <<= 1) {
-      acc.x += __shfl_xor_sync(0xffffffffu, acc.x, o);
-      acc.y += __shfl_xor_sync(0xffffffffu, acc.y, o);
-      acc.z += __shfl_xor_sync(0xffffffffu, acc.z, o);
-      acc.w += __shfl_xor_sync(0xffffffffu, acc.w, o);
-    }
-    if (sub == 0 && v < v1) {
-      uint2 w;
-      __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&w);
-      h[0] = __floats2bfloat162_rn(acc.x, acc.y);
-      h[1] = __floats2bfloat162_rn(acc.z, acc.w);
-      *reinterpret_cast<uint2*>(p.out + (size_t)(c.t0 + f / G) * (p.hq * DH) + (c.head * G + f % G) * DH + d) = w;
-    }
+    return;
   }
+  const int sub = threadIdx.x & (lanes - 1), v = v0 + (int)threadIdx.x / lanes, vc = min(v, v1 - 1);   // v1 - v0 <= 256 / lanes
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int k = sub; k < parts; k += lanes) {
+    const float4 x = *reinterpret_cast<const float4*>(p.part_o + slot_of(k) * R * DH + 4 * vc);
+    const float w = s_w[(vc / (DH / 4) - f0) * parts + k];
+    acc.x += w * x.x; acc.y += w * x.y; acc.z += w * x.z; acc.w += w * x.w;
+  }
+  for (int o = 1; o < lanes; o <<= 1) {
+    acc.x += __shfl_xor_sync(0xffffffffu, acc.x, o);
+    acc.y += __shfl_xor_sync(0xffffffffu, acc.y, o);
+    acc.z += __shfl_xor_sync(0xffffffffu, acc.z, o);
+    acc.w += __shfl_xor_sync(0xffffffffu, acc.w, o);
+  }
+  if (sub == 0 && v < v1) store(v, acc);
 }
 
 constexpr size_t kCutBytes = (size_t)kMaxStreamCtas * kStreamWarps * sizeof(Cut);
