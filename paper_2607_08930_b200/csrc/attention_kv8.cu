@@ -14,7 +14,7 @@
 #include <algorithm>
 #include <mutex>
 
-#include "kv8.cuh"
+#include "kv8_line.cuh"
 #include "tc_common.cuh"
 
 namespace bs {
@@ -35,16 +35,6 @@ __device__ __forceinline__ unsigned transpose8x8(unsigned x) {
 __device__ __forceinline__ unsigned pack_f16(float a, float b) {
   const __half2 h = __floats2half2_rn(a, b);
   return *reinterpret_cast<const unsigned*>(&h);
-}
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ float log2_fast(float x) {      // exact for powers of two
-  float y;
-  asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
 }
 // 16 bytes to shared memory, or zeros (`real` = false; the source is then not read)
 __device__ __forceinline__ void copy_async16(unsigned dst, const void* src, bool real) {
@@ -95,53 +85,6 @@ __host__ __device__ constexpr int item_cost(int w) { return w == 1 ? 3 : 8; }
 // largest one.
 constexpr float kBias = 6.f, kGrow = 14.f;
 
-struct StreamParams {
-  const bf16* q;
-  int q_ld;
-  Kv8Cache c;
-  bf16* out;
-  const int* cu_q;
-  const int* kv_base;
-  const int* vis;
-  int n_rows, M, hq, hkv, tq;
-  struct Cut* cuts;      // scratch: [workers] the item that the boundary in front of a worker's share cuts
-  float* part_o;         // scratch: [2 workers][8 NQ][DH]
-  float2* part_ml;       // scratch: [2 workers][8 NQ]
-  int* error_flag;
-};
-
-// A cut item: the workers that hold parts of it, its first query token, number of query rows (0: nothing is cut) and
-// kv head; whether worker c0 began with it (its part is then in the even slot, as everybody else's is).
-struct Cut { int c0, c1, t0, nrows, head, even, pad0, pad1; };
-
-struct RowInfo {
-  int t0, n, vis, nb, tiles;
-  long long base;
-  // units of one item, and of the row
-  __device__ __forceinline__ int item_units(int cost) const { return nb > 0 ? nb + cost : 0; }
-  __device__ __forceinline__ long long units(int hkv, int cost) const { return (long long)tiles * hkv * item_units(cost); }
-};
-
-__device__ __forceinline__ bool row_info(const int* cu_q, const int* kv_base, const int* vis, long long n_blocks, int M,
-                                         int tq, int r, RowInfo& w) {
-  w.t0 = __ldg(cu_q + r);
-  const int t1 = __ldg(cu_q + r + 1);
-  w.n = t1 - w.t0;
-  w.vis = __ldg(vis + r);
-  const int base = __ldg(kv_base + r);
-  w.base = (long long)base / kKv8Block;
-  const bool ok = w.t0 >= 0 && w.n >= 0 && t1 <= M && w.vis >= 0 && base >= 0 && base % kKv8Block == 0 &&
-                  (long long)base + w.vis <= n_blocks * kKv8Block;
-  if (!ok) w.n = w.vis = 0;
-  w.nb = (w.vis + kKv8Block - 1) / kKv8Block;
-  w.tiles = (w.n + tq - 1) / tq;
-  return ok;
-}
-
-// First unit of worker c's share, and the worker that holds unit u.
-__device__ __forceinline__ long long share_start(long long c, long long total, long long n) { return c * total / n; }
-__device__ __forceinline__ int share_of(long long u, long long total, long long n) { return (int)(((u + 1) * n - 1) / total); }
-
 template <int DH>
 constexpr int kTileBytes = kKv8Block * DH;           // one block of one head, K or V
 template <int DH, int NQ, int STAGES, int W>
@@ -153,19 +96,15 @@ struct StreamSmem {
   static constexpr int q = NQ * (DH / 32) * 32 * 16;               // query fragments, two k steps in 16 bytes
   static constexpr int total = 128 + front + groups * (q + W * R * 8 + R * 4);
 };
-constexpr int kRowsPerThread = kAttnKv8MaxRows / kStreamThreads;
-
 template <int DH, int NQ, int STAGES, int W, int MINB>
-__global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(StreamParams p) {
+__global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(const LineParams p) {
   using L = StreamSmem<DH, NQ, STAGES, W>;
   constexpr int KP = DH / 32;            // pairs of k steps of the scores
   constexpr int MD = DH / 16;            // m tiles of the output
   constexpr int kHalves = NQ == 1 ? 2 : 1;             // (unrolled, the wider instantiations do not fit their registers)
   constexpr int R = L::R, LDO = L::LDO, TB = kTileBytes<DH>, kCost = item_cost(W);
   extern __shared__ unsigned char smem_raw[];
-  __shared__ long long s_warp[kStreamWarps];
-  __shared__ long long s_first[L::groups];   // units before s_row
-  __shared__ int s_row[L::groups];
+  __shared__ LineShared<kStreamThreads, L::groups> s_line;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int g = lane >> 2, c4 = lane & 3;
   const int G = p.hq / p.hkv;
@@ -180,97 +119,25 @@ __global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(S
   pdl_wait();
   pdl_trigger();
 
-  // ---- units before every row (exclusive prefix); the row that holds each worker's first unit ----
-  long long before[kRowsPerThread], cost[kRowsPerThread];
-  long long total = 0;
-#pragma unroll
-  for (int i = 0; i < kRowsPerThread; ++i) {
-    if (i * kStreamThreads >= p.n_rows) break;
-    const int r = i * kStreamThreads + tid;
-    long long w = 0;
-    if (r < p.n_rows) {
-      RowInfo ri;
-      if (!row_info(p.cu_q, p.kv_base, p.vis, p.c.n_blocks, p.M, p.tq, r, ri) && blockIdx.x == 0 && p.error_flag)
-        atomicMax(p.error_flag, 100 + SITE_ATTN_KV8);
-      w = ri.units(p.hkv, kCost);
-    }
-    long long inc = w;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const long long v = __shfl_up_sync(0xffffffffu, inc, o);
-      if (lane >= o) inc += v;
-    }
-    if (lane == 31) s_warp[warp] = inc;
-    __syncthreads();
-    long long b = total;
-#pragma unroll
-    for (int k = 0; k < kStreamWarps; ++k) {
-      if (k < warp) b += s_warp[k];
-      total += s_warp[k];
-    }
-    before[i] = b + inc - w;
-    cost[i] = w;
-    __syncthreads();
-  }
-  // a share holds one block per warp at least
-  const long long workers = max(1ll, min((long long)gridDim.x * L::groups, total / (kCost + W)));
-  const long long me = (long long)blockIdx.x * L::groups + wk;
-#pragma unroll
-  for (int k = 0; k < L::groups; ++k) {
-    const long long u = share_start((long long)blockIdx.x * L::groups + k, total, workers);
-#pragma unroll
-    for (int i = 0; i < kRowsPerThread; ++i) {
-      if (i * kStreamThreads >= p.n_rows) break;
-      if (before[i] <= u && u < before[i] + cost[i]) {     // (rows behind the last one count nothing); one thread at most
-        s_row[k] = i * kStreamThreads + tid;
-        s_first[k] = before[i];
-      }
-    }
-  }
-  // rows that see nothing: zeros
-  for (int r = blockIdx.x; r < p.n_rows; r += gridDim.x) {
-    RowInfo z;
-    row_info(p.cu_q, p.kv_base, p.vis, p.c.n_blocks, p.M, p.tq, r, z);
-    if (z.nb == 0) {
-      uint4* dst = reinterpret_cast<uint4*>(p.out + (size_t)z.t0 * (p.hq * DH));
-      for (long long i = tid; i < (long long)z.n * (p.hq * DH / 8); i += kStreamThreads) dst[i] = make_uint4(0, 0, 0, 0);
-    }
-  }
-  __syncthreads();
-  if (total == 0 || me >= workers) {
+  LineShare share;
+  line_share<kStreamThreads, L::groups, kKv8Block, DH>(p, kCost, W, s_line, wk, share);
+  const size_t me = (size_t)blockIdx.x * L::groups + wk;
+  if (share.u0 == share.u1) {
     if (wtid == 0) p.cuts[me].nrows = 0;
     return;                                // (from here on only the worker's own threads wait for one another)
   }
-  const long long u0 = share_start(me, total, workers), u1 = share_start(me + 1, total, workers);
-  int row = s_row[wk];
-  long long first = s_first[wk];
-  RowInfo ri;
-  row_info(p.cu_q, p.kv_base, p.vis, p.c.n_blocks, p.M, p.tq, row, ri);
-  {   // does this share begin inside an item's blocks?
-    const int per = ri.item_units(kCost), item = (int)((u0 - first) / per), at = (int)((u0 - first) % per);
-    if (wtid == 0) {
-      Cut c = {};
-      if (at > kCost) {
-        const long long begin = u0 - at;                     // the item's first unit; its blocks begin kCost later
-        c.c0 = share_of(begin + kCost, total, workers);
-        c.c1 = share_of(begin + per - 1, total, workers);
-        c.even = begin <= share_start(c.c0, total, workers);
-        c.head = item / ri.tiles;
-        c.t0 = ri.t0 + item % ri.tiles * p.tq;
-        c.nrows = min(p.tq, ri.t0 + ri.n - c.t0) * G;
-      }
-      p.cuts[me] = c;
-    }
-  }
+  if (wtid == 0) line_cut<kKv8Block>(p, kCost, share, (int)me);
 
   // this warp's ring, and this lane's part of a block's copy: 16 bytes i * 512 + lane * 16 of K and of V
   const unsigned ring = tc::smem_u32(smem) + (unsigned)warp * STAGES * 2 * TB;
   const unsigned put0 = (unsigned)((lane >> 3) * 128 + (((lane & 7) ^ (lane >> 3)) << 4));
   const unsigned put1 = (unsigned)((lane >> 3) * 128 + (((lane & 7) ^ (4 + (lane >> 3))) << 4));
-  auto fetch = [&](int stage, int b, int head) {
-    const size_t at = ((size_t)(ri.base + b) * p.hkv + head) * TB + lane * 16;
+  LineItem it = {};
+  auto tile_of = [&](int b) { return ((size_t)it.block0 + b) * p.hkv + it.head; };
+  auto fetch = [&](int stage, int b) {
+    const size_t at = tile_of(b) * TB + lane * 16;
     const unsigned dst = ring + (unsigned)stage * 2 * TB;
-    const int rows = ri.vis - b * kKv8Block;
+    const int rows = it.vis - b * kKv8Block;
 #pragma unroll
     for (int i = 0; i < TB / 512; ++i) {
       const bool real = (i * 512 + lane * 16) / DH < rows;
@@ -280,35 +147,19 @@ __global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(S
     }
   };
 
-  for (long long u = u0; u < u1;) {
-    for (long long w; u - first >= (w = ri.units(p.hkv, kCost));) {
-      first += w;
-      ++row;
-      row_info(p.cu_q, p.kv_base, p.vis, p.c.n_blocks, p.M, p.tq, row, ri);
-    }
-    const long long local = u - first;
-    const int per = ri.item_units(kCost);
-    const int item = local < 0x7fffffffll ? (int)local / per : (int)(local / per);
-    const int at = (int)(local - (long long)item * per);
-    const int b0 = max(0, at - kCost);                            // an item's first kCost units hold no block
-    const int b1 = (int)min((long long)ri.nb, max(0ll, at + (u1 - u) - kCost));
-    const bool opens = u == u0;                                   // (the partial slot of this segment)
-    u += per - at;
-    if (b1 <= b0) continue;
-    const int head = item / ri.tiles, tile = item - head * ri.tiles;
-    const int t0 = ri.t0 + tile * p.tq, nt = min(p.tq, ri.t0 + ri.n - t0), nrows = nt * G;
-
+  for (LineWalk walk(share); walk.next<kKv8Block>(p, kCost, it);) {
+    const int b0 = it.b0, b1 = it.b1, head = it.head, t0 = it.t0, nrows = it.nrows;
     sync_worker();                       // the previous segment's fragments, sums and outputs are no longer read
 #pragma unroll
     for (int i = 0; i < STAGES - 1; ++i) {
-      if (b0 + member + i * W < b1) fetch(i, b0 + member + i * W, head);
+      if (b0 + member + i * W < b1) fetch(i, b0 + member + i * W);
       asm volatile("cp.async.commit_group;\n" ::: "memory");
     }
     float ks_next = 1.f, vs_next = 1.f;
     if (b0 + member < b1) {
-      const size_t sa = (size_t)(ri.base + b0 + member) * p.hkv + head;
-      ks_next = __ldg(p.c.k_scale + sa);
-      vs_next = __ldg(p.c.v_scale + sa);
+      const size_t sa = tile_of(b0 + member);
+      ks_next = __ldcg(p.c.k_scale + sa);
+      vs_next = __ldcg(p.c.v_scale + sa);
     }
     // ---- queries: fp16 fragments in shared memory ----
     for (int nq = member; nq < NQ; nq += W) {
@@ -370,16 +221,16 @@ __global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(S
       const float ks = kv8_clamp_scale(ks_next), vs = kv8_clamp_scale(vs_next);
       {
         const int nb = b + (STAGES - 1) * W;
-        if (nb < b1) fetch(stage == 0 ? STAGES - 1 : stage - 1, nb, head);
+        if (nb < b1) fetch(stage == 0 ? STAGES - 1 : stage - 1, nb);
         asm volatile("cp.async.commit_group;\n" ::: "memory");
         if (b + W < b1) {
-          const size_t sa = (size_t)(ri.base + b + W) * p.hkv + head;
-          ks_next = __ldg(p.c.k_scale + sa);
-          vs_next = __ldg(p.c.v_scale + sa);
+          const size_t sa = tile_of(b + W);
+          ks_next = __ldcg(p.c.k_scale + sa);
+          vs_next = __ldcg(p.c.v_scale + sa);
         }
       }
       const float lv = log2_fast(vs), inv_vs = 1.0f / vs;
-      const int left = ri.vis - b * kKv8Block;         // keys of this block that the row sees (> 0)
+      const int left = it.vis - b * kKv8Block;         // keys of this block that the row sees (> 0)
       asm volatile("cp.async.wait_group %0;\n" ::"n"(STAGES - 1) : "memory");
       __syncwarp();
       const unsigned kt = ring + (unsigned)stage * 2 * TB, vt = kt + TB;
@@ -491,8 +342,8 @@ __global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(S
       __syncwarp();                      // the stage may be filled again
     }
 
-    const bool whole = b0 == 0 && b1 == ri.nb;
-    const size_t slot = 2 * (size_t)me + (opens ? 0 : 1);
+    const bool whole = b0 == 0 && b1 == it.nb;
+    const size_t slot = 2 * me + (it.opens ? 0 : 1);
 #pragma unroll
     for (int nq = 0; nq < NQ; ++nq)
 #pragma unroll
@@ -587,11 +438,11 @@ __global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(S
 // query row, between them.  The parts' weights are formed once per row; then a unit is one thread, or, where there are
 // fewer units than threads, up to 32 neighbouring lanes, each with every so-manieth part.
 constexpr int kMergeThreads = 256;
-// Weights of one CTA: parts x the rows it touches.  With b boundaries inside an item of at most 32 rows it is at most
-// (b + 1) (32 / b + 2) <= 2 b + 66, and b < 4 x 592.
+// Weights of one CTA: parts x the rows it touches.  With b boundaries inside an item of at most R rows it is at most
+// (b + 1) (R / b + 2) <= 2 b + 2 R + 2; b < 4 x 592 with R = 32, fewer CTAs with R = 128.
 constexpr int kMergeWeights = 2 * kMaxStreamCtas * kStreamWarps + 66;
 template <int DH>
-__global__ void __launch_bounds__(kMergeThreads) k_attention_kv8_merge(StreamParams p, int R) {
+__global__ void __launch_bounds__(kMergeThreads) k_attention_kv8_merge(const LineParams p, int R) {
   __shared__ float s_w[kMergeWeights];
   pdl_wait();
   pdl_trigger();
@@ -685,7 +536,7 @@ DeviceInfo g_dev[kMaxDevices];
 std::mutex g_mutex;
 
 template <int DH, int NQ, int STAGES, int W, int MINB>
-cudaError_t run_stream(StreamParams p, cudaStream_t s) {
+cudaError_t run_stream(const LineParams& p, cudaStream_t s) {
   constexpr int index = (DH == 128 ? 6 : 0) + (NQ == 4 ? 2 : NQ - 1) * 2 + (W == 1 ? 1 : 0);
   constexpr auto kernel = k_attention_kv8_stream<DH, NQ, STAGES, W, MINB>;
   constexpr int smem = StreamSmem<DH, NQ, STAGES, W>::total;
@@ -714,7 +565,7 @@ inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
 }  // namespace
 
-// Scratch: the streaming kernel's cuts, partial outputs and sums; the tensor-core kernel uses the same bytes for its chunks.
+// Scratch: the streaming kernel's cuts, partial outputs and sums; the tensor-core kernel uses the same ones (two slots of 128 rows per CTA).
 size_t attention_kv8_scratch_bytes(int hq, int hkv, int dh) {
   (void)hq; (void)hkv;
   return up256(kCutBytes) + up256(kPartRows * dh * sizeof(float)) + up256(kPartRows * sizeof(float2));
@@ -725,14 +576,10 @@ cudaError_t launch_attention_kv8(const AttnKv8Args& a, cudaStream_t s) {
   const int G = a.hq / a.hkv;
   const int max_nq = a.max_nq > 0 ? std::min(a.max_nq, a.M) : a.M;
   const long long widest = (long long)max_nq * G;
-  // More than 32 query rows per kv head fill a good part of the 128-row tensor-core tiles.
-  if (a.dh == 128 && widest > 32)
-    return launch_attention_kv8_tc(a, static_cast<float*>(a.scratch), a.scratch_bytes / sizeof(float), s);
-  const int nq = widest <= 8 ? 1 : widest <= 16 ? 2 : 4;
-  StreamParams p;
+  LineParams p;
   p.q = a.q; p.q_ld = a.q_ld; p.c = a.cache; p.out = a.out;
   p.cu_q = a.cu_q; p.kv_base = a.kv_base; p.vis = a.vis;
-  p.n_rows = a.n_rows; p.M = a.M; p.hq = a.hq; p.hkv = a.hkv; p.tq = 8 * nq / G;
+  p.n_rows = a.n_rows; p.M = a.M; p.hq = a.hq; p.hkv = a.hkv;
   p.error_flag = a.error_flag;
   char* at = static_cast<char*>(a.scratch);
   p.cuts = reinterpret_cast<Cut*>(at);
@@ -740,6 +587,16 @@ cudaError_t launch_attention_kv8(const AttnKv8Args& a, cudaStream_t s) {
   p.part_o = reinterpret_cast<float*>(at);
   at += up256(kPartRows * a.dh * sizeof(float));
   p.part_ml = reinterpret_cast<float2*>(at);
+  // More than 32 query rows per kv head fill a good part of the 128-row tensor-core tiles.
+  if (widest > 32) {
+    p.tq = 128 / G;
+    int ctas = 0;
+    if (cudaError_t r = launch_attention_kv8_tc(p, a.dh, (int)(kPartRows / 256), &ctas, s)) return r;
+    return launch_pdl(a.dh == 128 ? k_attention_kv8_merge<128> : k_attention_kv8_merge<64>, dim3(ctas), dim3(kMergeThreads), 0,
+                      s, p, 128);
+  }
+  const int nq = widest <= 8 ? 1 : widest <= 16 ? 2 : 4;
+  p.tq = 8 * nq / G;
   // Single-warp workers once there are about as many items as half of them.
   const long long items = (long long)a.n_rows * a.hkv * ((max_nq + p.tq - 1) / p.tq);
   const bool many = items >= 592;

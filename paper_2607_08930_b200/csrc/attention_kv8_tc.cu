@@ -1,27 +1,34 @@
-// Ragged attention over the 8-bit KV cache on the 5th-generation tensor cores (head_dim 128), for work items with more
-// query rows than the streaming kernel takes: block steps with grouped heads, whole rows.  Formulas and the handling of
-// the scales as in attention_kv8.cu.
+// Ragged attention over the 8-bit KV cache on the 5th-generation tensor cores, for work items with more query rows than
+// the streaming kernel takes: block steps, whole rows.  Formulas and the handling of the scales as in attention_kv8.cu.
 //
-// Work item = (row, span of its query tokens, kv head): up to NT tiles of 128 flattened (token, head-in-group) query
-// rows, one row per thread of a softmax group and per tensor-memory lane.  One CTA per SM, warp-specialised:
-//   warp 0        producer: 128-key tiles of K and V codes by TMA, each through a ring of its own
+// Work item = (row, kv head, tile of 128 flattened (token, head-in-group) query rows); a query row is a tensor-memory
+// lane.  All items' key tiles (128 keys) form one line - an item counts a little more than its tiles - that the CTAs of
+// one resident wave, one per SM, share evenly; cut items leave parts for the merge kernel (attention_kv8.cu).  A CTA is
+// persistent and warp-specialised; the rings run on from one item to the next:
+//   warp 0        producer: tiles of K and V codes by TMA, each through a ring of its own
 //   warp 1        issues the products.  S = Q K^T takes K's codes as they arrive (kind::f8f6f4, e4m3 x e4m3): a query
 //                 element, after a power of two per query row has brought the row's largest into [128, 256), is the sum
 //                 of two e4m3 values - the nearest one and the rest (4 + 4 significant bits, bf16 has 8: exact above
 //                 2^-10 of the row's largest element, within 2^-17 of that element below) - so S is two products at
-//                 twice the rate of one in fp16, and K is neither converted nor stored a second time
-//   4 NT warps    softmax, four per query tile.  The weights w = 2^(t - M) go back to tensor memory as fp16, over the first
-//                 half of their scores, as the A operand of O += W V
-//   4 more warps  V's codes to fp16 (exact) in the layout of a B operand; rows behind the row's end become zeros
+//                 twice the rate of one in fp16, and K is neither converted nor stored a second time.  Q is an operand
+//                 from tensor memory (two buffers): read from shared memory it would take half of that memory's
+//                 bandwidth, which is what the products of a 128 x 128 tile are bound by.
+//   8 warps       softmax: two threads per query row, half of a tile's keys each; they hold their scores in registers
+//                 from the maximum to the weights.  The weights w = 2^(t - M) go back to tensor memory as fp16, over
+//                 the first half of their scores, as the A operand of O += W V.  Scores are double-buffered: the next
+//                 tile's are formed while this one's are worked on.
+//   4 more warps  V's codes to fp16 (exact) in the layout of a B operand, rows behind the row's end as zeros; and the
+//                 next item's queries to tensor memory.
 // Weights are formed against a running reference that lags the maximum (kTcBias, kTcGrow): the output is rescaled only
 // when a row's maximum has outgrown it.
-// Every wait is bounded; on a timeout the flag is raised, all roles drain, the copies in flight are waited for.
+// Every wait is bounded; on a timeout the flag is raised, all roles run through their loops without waiting, and the
+// copies in flight are waited for.
 #include <math.h>
 
 #include <algorithm>
 #include <mutex>
 
-#include "kv8.cuh"
+#include "kv8_line.cuh"
 #include "tc_common.cuh"
 
 namespace bs {
@@ -30,22 +37,20 @@ namespace {
 
 using namespace tc;
 
-constexpr int DH = 128;
 constexpr int KT = 128;                              // keys per tile: four cache blocks
-constexpr int kK8Bytes = KT * DH;                    // one tile of codes
-constexpr int kV16Half = KT * 128;                   // 64 dims of a tile in fp16
-constexpr int kQTileBytes = 2 * 128 * DH;            // nearest values, rests
-constexpr int kKStages = 3, kV8Stages = 2, kV16Stages = 2;
+constexpr int kTcThreads = 512;
+constexpr int kKStages = 4, kV8Stages = 3, kV16Stages = 2;
 constexpr float kTcBias = 6.f, kTcGrow = 14.f;       // weights reach 2^14 at most, 2^6 when the reference is set
+constexpr int kTcItemCost = 1;                       // tiles that an item counts beyond its own
+constexpr unsigned kOCol = 256, kQCol = 384;         // tensor memory: two scores buffers, output, two query buffers
 
-template <int NT>
+template <int DH>
 struct TcLayout {
-  static constexpr int threads = 128 + 128 * NT + 128;
-  static constexpr int q = 0, k = q + NT * kQTileBytes, v8 = k + kKStages * kK8Bytes, v16 = v8 + kV8Stages * kK8Bytes;
-  static constexpr int bytes = v16 + kV16Stages * 2 * kV16Half;
+  static constexpr int k8 = KT * DH;                 // one tile of codes
+  static constexpr int v16 = KT * DH * 2;            // one tile of V in fp16: DH / 64 parts of 64 dims
+  static constexpr int k = 0, v8 = k + kKStages * k8, v = v8 + kV8Stages * k8, bytes = v + kV16Stages * v16;
   static constexpr int smem = bytes + 1024;
-  static constexpr int s_bufs = NT == 2 ? 1 : 2;     // scores buffers per query tile (tensor memory: 128 columns each)
-  static constexpr unsigned o_col = 256;             // outputs behind the two scores buffers
+  static constexpr int q_cols = DH / 2;              // tensor-memory columns of one query buffer (nearest values, rests)
 };
 
 __device__ __forceinline__ void tma_load_4d(unsigned dst, const CUtensorMap* map, int c0, int c1, int c2, int c3, unsigned bar) {
@@ -53,26 +58,30 @@ __device__ __forceinline__ void tma_load_4d(unsigned dst, const CUtensorMap* map
       "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
       ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar) : "memory");
 }
-// S: e4m3 x e4m3 (both K-major), fp32 accumulator, 128 x 128 x 32
+// High word of a descriptor of an operand whose rows are row_bytes long (128 or 64, swizzled by as much), K-major.
+template <int ROW>
+__host__ __device__ constexpr unsigned desc_hi() { return (unsigned)(8 * ROW >> 4) | (1u << 14) | ((ROW == 128 ? 2u : 4u) << 29); }
+// S: e4m3 (A, tensor memory) x e4m3 (B, K-major), fp32 accumulator, 128 x 128 x 32
 constexpr unsigned kIdescS = (1u << 4) | ((unsigned)(KT >> 3) << 17) | ((128u >> 4) << 24);
-// O: fp16 x fp16, B MN-major, fp32 accumulator, 128 x 128 x 16
-constexpr unsigned kIdescO = (1u << 4) | (1u << 16) | ((unsigned)(DH >> 3) << 17) | ((128u >> 4) << 24);
-__device__ __forceinline__ void umma_e4m3(unsigned d_tmem, unsigned a_lo, unsigned b_lo, unsigned accumulate) {
+template <int DH>
+__device__ __forceinline__ void umma_qk(unsigned d_tmem, unsigned a_tmem, unsigned b_lo, unsigned accumulate) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
+      "{\n\t.reg .pred p;\n\t.reg .b64 db;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
-      "mov.b64 da, {%1, %5};\n\t"
       "mov.b64 db, {%2, %5};\n\t"
-      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], da, db, %3, p;\n\t}"
-      ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(kIdescS), "r"(accumulate), "r"(kDescHi) : "memory");
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], [%1], db, %3, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(kIdescS), "r"(accumulate), "r"(desc_hi<DH>()) : "memory");
 }
+// O: fp16 (A, tensor memory) x fp16 (B, MN-major), fp32 accumulator, 128 x DH x 16
+template <int DH>
 __device__ __forceinline__ void umma_pv(unsigned d_tmem, unsigned a_tmem, unsigned b_lo, unsigned accumulate) {
+  constexpr unsigned idesc = (1u << 4) | (1u << 16) | ((unsigned)(DH >> 3) << 17) | ((128u >> 4) << 24);
   asm volatile(
       "{\n\t.reg .pred p;\n\t.reg .b64 db;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
       "mov.b64 db, {%2, %5};\n\t"
       "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}"
-      ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(kIdescO), "r"(accumulate), "r"(kDescHi) : "memory");
+      ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kDescHi) : "memory");
 }
 __device__ __forceinline__ void tmem_st32(unsigned taddr, const unsigned* w) {
   asm volatile(
@@ -85,25 +94,11 @@ __device__ __forceinline__ void tmem_st32(unsigned taddr, const unsigned* w) {
         "r"(w[27]), "r"(w[28]), "r"(w[29]), "r"(w[30]), "r"(w[31])
       : "memory");
 }
-__device__ __forceinline__ void tmem_ld16_nowait(unsigned taddr, unsigned* r) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-      : "r"(taddr));
+__device__ __forceinline__ void tmem_st8(unsigned taddr, const unsigned* w) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"r"(taddr), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ float log2_fast(float x) {
-  float y;
-  asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 __device__ __forceinline__ uint4 lds128(unsigned at) {
   uint4 v;
   asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
@@ -112,81 +107,49 @@ __device__ __forceinline__ uint4 lds128(unsigned at) {
 __device__ __forceinline__ void sts128(unsigned at, unsigned a, unsigned b, unsigned c, unsigned d) {
   asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
-__device__ __forceinline__ void sts64(unsigned at, unsigned a, unsigned b) {
-  asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(at), "r"(a), "r"(b) : "memory");
-}
 // generic-proxy writes to shared memory before tensor-core reads of it
 __device__ __forceinline__ void fence_smem_for_mma() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-
-struct TcParams {
-  const bf16* q;
-  int q_ld;
-  const float* k_scale;
-  const float* v_scale;
-  long long n_blocks;
-  bf16* out;
-  const int* cu_q;
-  const int* kv_base;
-  const int* vis;
-  int n_rows, M, hq, hkv;
-  int tq;            // query tokens per query tile
-  int chunks;        // key chunks per row (grid z); > 1: partials instead of the output
-  float* part_o;     // [chunks][M][hq][DH]
-  float2* part_ml;   // [chunks][M][hq] (reference, sum); sum 0: a chunk without keys
-  int* error_flag;
-};
-
-// Whether row r's indices fit (a row whose do not is skipped).
-__device__ __forceinline__ bool row_fits(const TcParams& p, int cq0, int cq1, int vis, int base) {
-  return cq0 >= 0 && cq1 >= cq0 && cq1 <= p.M && vis >= 0 && base >= 0 && base % kKv8Block == 0 &&
-         (long long)base + vis <= p.n_blocks * kKv8Block;
+// the two warps of a query row quarter: do any of their threads say yes?  (also their barrier)
+__device__ __forceinline__ bool pair_any(int id, bool x) {
+  unsigned r;
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, %2, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+               : "=r"(r) : "r"((unsigned)x), "r"(id) : "memory");
+  return r != 0;
 }
+__device__ __forceinline__ void pair_sync(int id) { asm volatile("barrier.cta.sync %0, 64;" ::"r"(id) : "memory"); }
 
-template <int NT>
-__global__ void __launch_bounds__(TcLayout<NT>::threads, 1)
-k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const TcParams p) {
-  using L = TcLayout<NT>;
-  constexpr int SB = L::s_bufs;
+template <int DH>
+__global__ void __launch_bounds__(kTcThreads, 1)
+k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const LineParams p) {
+  using L = TcLayout<DH>;
   enum { B_KFULL = 0, B_KEMPTY = B_KFULL + kKStages, B_V8FULL = B_KEMPTY + kKStages, B_V8EMPTY = B_V8FULL + kV8Stages,
          B_VFULL = B_V8EMPTY + kV8Stages, B_VEMPTY = B_VFULL + kV16Stages, B_SFULL = B_VEMPTY + kV16Stages,
-         B_PFULL = B_SFULL + 2, B_OFULL = B_PFULL + 2, B_COUNT = B_OFULL + 2 };
+         B_PFULL = B_SFULL + 2, B_QFULL = B_PFULL + 2, B_QEMPTY = B_QFULL + 2, B_OFULL = B_QEMPTY + 2,
+         B_OEMPTY = B_OFULL + 1, B_COUNT = B_OEMPTY + 1 };
   extern __shared__ unsigned char smem_dyn[];
   __shared__ __align__(8) unsigned long long bars[B_COUNT];
   __shared__ unsigned tmem_base_slot;
   __shared__ int s_abort;
-  __shared__ float s_sc[NT * 128];
+  __shared__ float s_sc[2][128];                     // score scale of every query row, by item parity
+  __shared__ float s_pair[2][128];                   // exchange between the two threads of a query row
+  __shared__ LineShared<kTcThreads, 1> s_line;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const unsigned smem0 = (smem_u32(smem_dyn) + 1023u) & ~1023u;
-  const unsigned sQ = smem0 + L::q, sK = smem0 + L::k, sV8 = smem0 + L::v8, sV16 = smem0 + L::v16;
+  const unsigned sK = smem0 + L::k, sV8 = smem0 + L::v8, sV16 = smem0 + L::v;
   const unsigned bar0 = smem_u32(&bars[0]);
   auto bar = [&](int i) { return bar0 + 8u * (unsigned)i; };
-  pdl_wait();
-  pdl_trigger();
-
-  // ---- the work item ----
-  const int G = p.hq / p.hkv, kh = blockIdx.y, per_cta = NT * p.tq;
-  const int slot = (int)blockIdx.x;
-  const int row = warp_search(p.n_rows, slot, [&](int i) { return __ldg(p.cu_q + i) / per_cta + i; });
-  const int cq0 = __ldg(p.cu_q + row), cq1 = __ldg(p.cu_q + row + 1), vis = __ldg(p.vis + row), base = __ldg(p.kv_base + row);
-  if (!row_fits(p, cq0, cq1, vis, base)) {
-    if (threadIdx.x == 0 && p.error_flag) atomicMax(p.error_flag, 100 + SITE_ATTN_KV8);
-    return;
-  }
-  const int t0 = cq0 + (slot - (cq0 / per_cta + row)) * per_cta;
-  const int nt = min(per_cta, cq1 - t0);                    // query tokens of this CTA
-  if (t0 < cq0 || nt <= 0) return;                          // a slot that no tokens fall into
-  const int n_qt = NT == 1 || nt <= p.tq ? 1 : 2;
-  const int tiles_all = (vis + KT - 1) / KT;
-  const int per_chunk = (tiles_all + p.chunks - 1) / p.chunks;
-  const int kt0 = (int)blockIdx.z * per_chunk;
-  const int n_tiles = max(0, min(tiles_all, kt0 + per_chunk) - kt0);
-
   if (threadIdx.x == 0) {
     s_abort = 0;
     for (int i = 0; i < kKStages; ++i) { mbar_init(bar(B_KFULL + i), 1); mbar_init(bar(B_KEMPTY + i), 1); }
     for (int i = 0; i < kV8Stages; ++i) { mbar_init(bar(B_V8FULL + i), 1); mbar_init(bar(B_V8EMPTY + i), 4); }
     for (int i = 0; i < kV16Stages; ++i) { mbar_init(bar(B_VFULL + i), 4); mbar_init(bar(B_VEMPTY + i), 1); }
-    for (int i = 0; i < 2; ++i) { mbar_init(bar(B_SFULL + i), 1); mbar_init(bar(B_PFULL + i), 4); mbar_init(bar(B_OFULL + i), 1); }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(bar(B_SFULL + i), 1); mbar_init(bar(B_PFULL + i), 8);
+      mbar_init(bar(B_QFULL + i), 4);
+      mbar_init(bar(B_QEMPTY + i), 9);           // the last scores of an item, and the softmax warps once they know its scales
+    }
+    mbar_init(bar(B_OFULL), 1);
+    mbar_init(bar(B_OEMPTY), 8);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
@@ -196,343 +159,363 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
                  ::"r"(smem_u32(&tmem_base_slot)), "r"(512u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  // ---- queries: 16 lanes per row, 8 dims each ----
-  if (n_tiles > 0) {
-    const int p16 = lane & 15;
-    for (int r = (int)(threadIdx.x >> 4); r < n_qt * 128; r += L::threads / 16) {
-      const int x = r >> 7, f = r & 127;
-      const int tok = x * p.tq + f / G;
-      const bool valid = f < p.tq * G && tok < nt;
-      uint4 raw = make_uint4(0, 0, 0, 0);
-      if (valid) raw = *(reinterpret_cast<const uint4*>(p.q + (size_t)(t0 + tok) * p.q_ld + (kh * G + f % G) * DH) + p16);
-      float v[8];
-      const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&raw);
-      float top = 0.f;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float2 y = __bfloat1622float2(h[j]);
-        v[2 * j] = y.x;
-        v[2 * j + 1] = y.y;
-        top = fmaxf(top, fmaxf(fabsf(y.x), fabsf(y.y)));
-      }
-      const unsigned half_mask = 0xffffu << (lane & 16);
-#pragma unroll
-      for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(half_mask, top, o));
-      const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 100);
-      const float up = pow2i(7 - e);
-      if (p16 == 0) s_sc[r] = pow2i(e - 7) * (1.4426950408889634f * rsqrtf((float)DH));
-      unsigned hi[2] = {0u, 0u}, lo[2] = {0u, 0u};
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float a = v[2 * j] * up, b = v[2 * j + 1] * up;
-        const unsigned near = kv8_encode2(a, b), back = kv8_decode2((unsigned short)near);
-        const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&back));
-        hi[j >> 1] |= near << (16 * (j & 1));
-        lo[j >> 1] |= kv8_encode2(a - y.x, b - y.y) << (16 * (j & 1));
-      }
-      const unsigned at = sQ + x * kQTileBytes + f * 128 + (((p16 >> 1) ^ (f & 7)) << 4) + (p16 & 1) * 8;
-      sts64(at, hi[0], hi[1]);
-      sts64(at + 128 * DH, lo[0], lo[1]);
-    }
-    fence_smem_for_mma();
-  }
+  pdl_wait();
+  pdl_trigger();
+
+  // ---- this CTA's share of the line ----
+  LineShare share;
+  line_share<kTcThreads, 1, KT, DH>(p, kTcItemCost, 1, s_line, 0, share);
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const unsigned tmem_base = tmem_base_slot;
   volatile int* abort_flag = &s_abort;
-  const int blk0 = base / kKv8Block + kt0 * (KT / kKv8Block);      // cache block of the chunk's first key
+  const int G = p.hq / p.hkv;
+  const bool work = share.u0 < share.u1;
+  if (work && threadIdx.x == 0) line_cut<KT>(p, kTcItemCost, share, (int)blockIdx.x);
+  if (!work && threadIdx.x == 0) p.cuts[blockIdx.x].nrows = 0;
 
-  // Two query tiles: 4 x 128 registers a thread at launch become 56 + 2 x 192 + 72.
+  // 4 x 128 registers a thread at launch become 80 + 2 x 176 + 80.
   const int group = warp >> 2;
   if (group == 0) {
-    if (NT == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-  if (warp == 0) {
-    // ------------------------------------------------------------------ TMA producer
-    if (lane == 0 && n_tiles > 0) {
-      int issued = 0;
-      for (int t = 0; t < n_tiles; ++t) {
-        const int ks = t % kKStages, vs = t % kV8Stages;
-        if (!mbar_wait(bar(B_KEMPTY + ks), (unsigned)((t / kKStages) & 1) ^ 1u, abort_flag)) break;
-        if (!mbar_wait(bar(B_V8EMPTY + vs), (unsigned)((t / kV8Stages) & 1) ^ 1u, abort_flag)) break;
-        mbar_expect_tx(bar(B_KFULL + ks), (unsigned)kK8Bytes);
-        tma_load_4d(sK + ks * kK8Bytes, &map_k, 0, 0, kh, blk0 + 4 * t, bar(B_KFULL + ks));
-        mbar_expect_tx(bar(B_V8FULL + vs), (unsigned)kK8Bytes);
-        tma_load_4d(sV8 + vs * kK8Bytes, &map_v, 0, 0, kh, blk0 + 4 * t, bar(B_V8FULL + vs));
-        issued = t + 1;
-      }
-      if (*abort_flag) {            // copies in flight end before the CTA does
-        for (int t = max(0, issued - kKStages); t < issued; ++t) {
-          const long long begin = clock64();
-          while (!(mbar_try_wait(bar(B_KFULL + t % kKStages), (unsigned)(t / kKStages) & 1u) &&
-                   (t < issued - kV8Stages || mbar_try_wait(bar(B_V8FULL + t % kV8Stages), (unsigned)(t / kV8Stages) & 1u))) &&
-                 clock64() - begin < kWaitCycles / 64) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    if (warp == 0) {
+      // ------------------------------------------------------------------ TMA producer
+      if (lane == 0 && work) {
+        int n = 0;
+        LineItem it;
+        for (LineWalk w(share); w.next<KT>(p, kTcItemCost, it);) {
+          const int blk0 = it.block0 + it.b0 * (KT / kKv8Block);
+          for (int t = 0; t < it.b1 - it.b0; ++t, ++n) {
+            const int ks = n % kKStages, vs = n % kV8Stages;
+            if (!mbar_wait(bar(B_KEMPTY + ks), (unsigned)((n / kKStages) & 1) ^ 1u, abort_flag)) break;
+            if (!mbar_wait(bar(B_V8EMPTY + vs), (unsigned)((n / kV8Stages) & 1) ^ 1u, abort_flag)) break;
+            mbar_expect_tx(bar(B_KFULL + ks), (unsigned)L::k8);
+            tma_load_4d(sK + ks * L::k8, &map_k, 0, 0, it.head, blk0 + 4 * t, bar(B_KFULL + ks));
+            mbar_expect_tx(bar(B_V8FULL + vs), (unsigned)L::k8);
+            tma_load_4d(sV8 + vs * L::k8, &map_v, 0, 0, it.head, blk0 + 4 * t, bar(B_V8FULL + vs));
           }
+          if (*abort_flag) break;
         }
-      }
-    }
-  } else if (warp == 1) {
-    // ------------------------------------------------------------------ MMA issuer
-    if (lane == 0 && n_tiles > 0) {
-      bool ok = true;
-      auto wait_k = [&](int t) { return mbar_wait(bar(B_KFULL + t % kKStages), (unsigned)(t / kKStages) & 1u, abort_flag); };
-      auto wait_v = [&](int t) { return mbar_wait(bar(B_VFULL + t % kV16Stages), (unsigned)(t / kV16Stages) & 1u, abort_flag); };
-      // scores of key tile t and query tile x into scores buffer s.  The buffer is free: its weights were read by the
-      // last product issued against it, and the tensor pipe runs this thread's instructions in order.
-      auto scores = [&](int t, int x, int s) {
-        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const unsigned q_hi = desc_lo(sQ + x * kQTileBytes), q_lo = desc_lo(sQ + x * kQTileBytes + 128 * DH);
-        const unsigned k_lo = desc_lo(sK + (t % kKStages) * kK8Bytes), d = tmem_base + s * 128;
-#pragma unroll
-        for (int k = 0; k < DH / 32; ++k) {
-          umma_e4m3(d, q_hi + 2 * k, k_lo + 2 * k, k ? 1u : 0u);
-          umma_e4m3(d, q_lo + 2 * k, k_lo + 2 * k, 1u);
-        }
-        umma_commit(bar(B_SFULL + s));
-      };
-      auto pv = [&](int t, int x, int s) {
-        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const unsigned v_lo = desc_lo(sV16 + (t % kV16Stages) * 2 * kV16Half, kV16Half);
-        const unsigned d = tmem_base + L::o_col + x * 128, a = tmem_base + s * 128;
-#pragma unroll
-        for (int j = 0; j < KT / 16; ++j) umma_pv(d, a + j * 8, v_lo + j * (2048 >> 4), (t || j) ? 1u : 0u);
-        umma_commit(bar(B_OFULL + x));
-      };
-      auto wait_p = [&](int t, int x) { return mbar_wait(bar(B_PFULL + x), (unsigned)t & 1u, abort_flag); };
-      if (NT == 1) {
-        for (int t = 0; t < 2 && t < n_tiles && ok; ++t) {
-          ok = wait_k(t);
-          if (ok) { scores(t, 0, t); umma_commit(bar(B_KEMPTY + t % kKStages)); }
-        }
-        for (int t = 0; t < n_tiles && ok; ++t) {
-          if (!(ok = wait_p(t, 0) && wait_v(t))) break;
-          pv(t, 0, t & 1);
-          umma_commit(bar(B_VEMPTY + t % kV16Stages));
-          if (t + 2 < n_tiles) {
-            if (!(ok = wait_k(t + 2))) break;
-            scores(t + 2, 0, t & 1);
-            umma_commit(bar(B_KEMPTY + (t + 2) % kKStages));
-          }
-        }
-      } else {
-        ok = wait_k(0);
-        for (int x = 0; x < n_qt && ok; ++x) scores(0, x, x);
-        if (ok) umma_commit(bar(B_KEMPTY));
-        for (int t = 0; t < n_tiles && ok; ++t) {
-          for (int x = 0; x < n_qt && ok; ++x) {
-            if (!(ok = wait_p(t, x) && (x > 0 || wait_v(t)))) break;
-            pv(t, x, x);
-            if (x == n_qt - 1) umma_commit(bar(B_VEMPTY + t % kV16Stages));
-            if (t + 1 < n_tiles) {
-              if (x == 0 && !(ok = wait_k(t + 1))) break;
-              scores(t + 1, x, x);
-              if (x == n_qt - 1) umma_commit(bar(B_KEMPTY + (t + 1) % kKStages));
+        if (*abort_flag) {            // copies in flight end before the CTA does
+          for (int t = max(0, n - kKStages); t < n; ++t) {
+            const long long begin = clock64();
+            while (!(mbar_try_wait(bar(B_KFULL + t % kKStages), (unsigned)(t / kKStages) & 1u) &&
+                     (t < n - kV8Stages || mbar_try_wait(bar(B_V8FULL + t % kV8Stages), (unsigned)(t / kV8Stages) & 1u))) &&
+                   clock64() - begin < kWaitCycles / 64) {
             }
           }
         }
       }
-    }
-  }
-  } else if (group == 1 + NT) {
-    // ------------------------------------------------------------------ V: codes -> fp16 B operand
-    if (NT == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-    const int c = (int)threadIdx.x & 127;
-    const int j = c & 7;                                     // 16 dims 16 j of a key, 8 lanes per key
-    const unsigned first = (unsigned)((j >> 2) * kV16Half);
-    for (int t = 0; t < n_tiles; ++t) {
-      const int a = t % kV8Stages, b = t % kV16Stages;
-      if (!mbar_wait(bar(B_V8FULL + a), (unsigned)(t / kV8Stages) & 1u, abort_flag)) break;
-      if (!mbar_wait(bar(B_VEMPTY + b), (unsigned)((t / kV16Stages) & 1) ^ 1u, abort_flag)) break;
-      const int left = vis - (kt0 + t) * KT;
-      const unsigned src = sV8 + a * kK8Bytes + c * 16, dst = sV16 + b * 2 * kV16Half + first;
+    } else if (warp == 1) {
+      // ------------------------------------------------------------------ MMA issuer
+      if (lane == 0 && work) {
+        // Two walks over the same tiles: the scores run two tiles ahead of the products with V.  The scores buffer of
+        // tile n is that of tile n - 2, whose weights the product issued just before has read: the tensor pipe runs
+        // this thread's instructions in order.
+        LineWalk ws(share), wv(share);
+        LineItem is, iv;
+        int ns = 0, ts = 0, items_s = 0;         // next scores: tile number, tile within the item, item number
+        bool more = ws.next<KT>(p, kTcItemCost, is);
+        auto scores = [&]() {
+          if (!more) return;
+          bool ok = true;
+          const int qb = items_s & 1;
+          if (ts == 0) ok = mbar_wait(bar(B_QFULL + qb), (unsigned)(items_s >> 1) & 1u, abort_flag);
+          if (ok) ok = mbar_wait(bar(B_KFULL + ns % kKStages), (unsigned)(ns / kKStages) & 1u, abort_flag);
+          if (!ok) { more = false; return; }
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const unsigned k_lo = desc_lo(sK + (ns % kKStages) * L::k8), d = tmem_base + (ns & 1) * 128;
+          const unsigned q = tmem_base + kQCol + qb * 64;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int key = i * 16 + (c >> 3);
-        uint4 w = lds128(src + i * 2048);
-        if (key >= left) w = make_uint4(0, 0, 0, 0);
-        unsigned x[8];
-        kv8_decode4(w.x, x[0], x[1]);
-        kv8_decode4(w.y, x[2], x[3]);
-        kv8_decode4(w.z, x[4], x[5]);
-        kv8_decode4(w.w, x[6], x[7]);
-        // chunks 2 (j % 4) and + 1 of the key's 128-byte line; the upper half of the dims stores them the other way
-        // round, so that the eight lanes of a key hit eight different banks groups
-        const unsigned line = dst + key * 128, c0 = 2 * (j & 3), sw = key & 7;
-        if (j < 4) {
-          sts128(line + ((c0 ^ sw) << 4), x[0], x[1], x[2], x[3]);
-          sts128(line + (((c0 + 1) ^ sw) << 4), x[4], x[5], x[6], x[7]);
-        } else {
-          sts128(line + (((c0 + 1) ^ sw) << 4), x[4], x[5], x[6], x[7]);
-          sts128(line + ((c0 ^ sw) << 4), x[0], x[1], x[2], x[3]);
+          for (int k = 0; k < DH / 32; ++k) {
+            umma_qk<DH>(d, q + k * 8, k_lo + 2 * k, k ? 1u : 0u);
+            umma_qk<DH>(d, q + L::q_cols / 2 + k * 8, k_lo + 2 * k, 1u);
+          }
+          umma_commit(bar(B_SFULL + (ns & 1)));
+          umma_commit(bar(B_KEMPTY + ns % kKStages));
+          ++ns;
+          if (++ts == is.b1 - is.b0) {
+            umma_commit(bar(B_QEMPTY + qb));
+            ts = 0;
+            ++items_s;
+            more = ws.next<KT>(p, kTcItemCost, is);
+          }
+        };
+        scores();
+        scores();
+        int n = 0, items = 0;
+        while (!*abort_flag && wv.next<KT>(p, kTcItemCost, iv)) {
+          for (int t = 0; t < iv.b1 - iv.b0; ++t, ++n) {
+            const int vs = n % kV16Stages;
+            if (t == 0 && items > 0 && !mbar_wait(bar(B_OEMPTY), (unsigned)(items - 1) & 1u, abort_flag)) break;
+            if (!mbar_wait(bar(B_VFULL + vs), (unsigned)(n / kV16Stages) & 1u, abort_flag)) break;
+            if (!mbar_wait(bar(B_PFULL + (n & 1)), (unsigned)(n >> 1) & 1u, abort_flag)) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const unsigned v_lo = desc_lo(sV16 + vs * L::v16, KT * 128), a = tmem_base + (n & 1) * 128;
+#pragma unroll
+            for (int j = 0; j < KT / 16; ++j) umma_pv<DH>(tmem_base + kOCol, a + j * 8, v_lo + j * (2048 >> 4), (t || j) ? 1u : 0u);
+            umma_commit(bar(B_OFULL));
+            umma_commit(bar(B_VEMPTY + vs));
+            scores();
+          }
+          ++items;
         }
       }
-      fence_smem_for_mma();
-      __syncwarp();
-      if (lane == 0) {
-        mbar_arrive(bar(B_V8EMPTY + a));
-        mbar_arrive(bar(B_VFULL + b));
-      }
     }
+  } else if (group == 3) {
+    // ------------------------------------------------------------------ V: codes -> fp16 B operand; Q -> tensor memory
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    constexpr int LPK = DH / 16;                             // lanes per key, 16 dims each
+    const int c = (int)threadIdx.x & 127;
+    const int j = c % LPK;
+    int n = 0, items = 0;
+    LineItem it;
+    if (work)
+      for (LineWalk w(share); w.next<KT>(p, kTcItemCost, it); ++items) {
+        {   // query row c: 2 e4m3 values per element, four elements of a kind per column
+          const int qb = items & 1;
+          mbar_wait(bar(B_QEMPTY + qb), (unsigned)((items >> 1) & 1) ^ 1u, abort_flag);
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const bool valid = c < it.nrows;
+          const bf16* src = p.q + (size_t)(it.t0 + (valid ? c / G : 0)) * p.q_ld + (it.head * G + (valid ? c % G : 0)) * DH;
+          auto load = [&](int i) { return valid ? __ldcg(reinterpret_cast<const uint4*>(src) + i) : make_uint4(0, 0, 0, 0); };
+          float top = 0.f;                 // (two passes over the row: the second finds it in L2)
+#pragma unroll
+          for (int i = 0; i < DH / 8; ++i) {
+            const uint4 raw = load(i);
+            const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&raw);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const float2 y = __bfloat1622float2(h[k]);
+              top = fmaxf(top, fmaxf(fabsf(y.x), fabsf(y.y)));
+            }
+          }
+          const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 100);
+          const float up = pow2i(7 - e);
+          s_sc[qb][c] = pow2i(e - 7) * (1.4426950408889634f * rsqrtf((float)DH));
+          const unsigned dst = tmem_base + ((unsigned)(c & 96) << 16) + kQCol + qb * 64;
+#pragma unroll 1
+          for (int i = 0; i < DH / 32; ++i) {
+            uint4 raw[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) raw[k] = load(i * 4 + k);
+            unsigned hi[8], lo[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&raw[k >> 1]) + (k & 1) * 2;
+              hi[k] = lo[k] = 0u;
+#pragma unroll
+              for (int m = 0; m < 2; ++m) {
+                const float2 y = __bfloat1622float2(h[m]);
+                const float a = y.x * up, b = y.y * up;
+                const unsigned near = kv8_encode2(a, b), back = kv8_decode2((unsigned short)near);
+                const float2 z = __half22float2(*reinterpret_cast<const __half2*>(&back));
+                hi[k] |= near << (16 * m);
+                lo[k] |= kv8_encode2(a - z.x, b - z.y) << (16 * m);
+              }
+            }
+            tmem_st8(dst + i * 8, hi);
+            tmem_st8(dst + L::q_cols / 2 + i * 8, lo);
+          }
+          tmem_st_wait();
+          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(B_QFULL + qb));
+        }
+        for (int t = it.b0; t < it.b1; ++t, ++n) {
+          const int a = n % kV8Stages, b = n % kV16Stages;
+          mbar_wait(bar(B_V8FULL + a), (unsigned)(n / kV8Stages) & 1u, abort_flag);
+          mbar_wait(bar(B_VEMPTY + b), (unsigned)((n / kV16Stages) & 1) ^ 1u, abort_flag);
+          const int left = it.vis - t * KT;
+          const unsigned src = sV8 + a * L::k8 + c * 16, dst = sV16 + b * L::v16 + (j >> 2) * (KT * 128);
+#pragma unroll
+          for (int i = 0; i < DH / 16; ++i) {
+            const int key = i * (128 / LPK) + c / LPK;
+            uint4 x = lds128(src + i * 2048);
+            if (key >= left) x = make_uint4(0, 0, 0, 0);
+            unsigned y[8];
+            kv8_decode4(x.x, y[0], y[1]);
+            kv8_decode4(x.y, y[2], y[3]);
+            kv8_decode4(x.z, y[4], y[5]);
+            kv8_decode4(x.w, y[6], y[7]);
+            // chunks 2 (j % 4) and + 1 of the key's 128-byte line; with two lines per key, half of a store's eight lanes
+            // take them the other way round, so that the eight fall on different banks
+            const bool flip = DH == 128 && j >= 4;
+            const unsigned line = dst + key * 128, c0 = 2 * (j & 3) + (flip ? 1 : 0), sw = key & 7;
+            sts128(line + ((c0 ^ sw) << 4), y[flip ? 4 : 0], y[flip ? 5 : 1], y[flip ? 6 : 2], y[flip ? 7 : 3]);
+            sts128(line + (((c0 ^ 1) ^ sw) << 4), y[flip ? 0 : 4], y[flip ? 1 : 5], y[flip ? 2 : 6], y[flip ? 3 : 7]);
+          }
+          fence_smem_for_mma();
+          __syncwarp();
+          if (lane == 0) {
+            mbar_arrive(bar(B_V8EMPTY + a));
+            mbar_arrive(bar(B_VFULL + b));
+          }
+        }
+      }
   } else {
-    // ------------------------------------------------------------------ softmax: one query row per thread
-    if (NT == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
-    const int x = group - 1, quad = warp & 3, r = quad * 32 + lane;
-    const int nrows = x < n_qt ? min(p.tq, nt - x * p.tq) * G : 0;
-    const bool warp_has_rows = quad * 32 < nrows;
-    const int my_tiles = x < n_qt ? n_tiles : 0;
+    // ------------------------------------------------------------------ softmax: half of a query row's keys per thread
+    // (on a timeout nobody leaves the loops: the two warps of a pair meet at the same barriers to the end)
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
+    const int half = group - 1, quad = warp & 3, r = quad * 32 + lane, pair = quad + 1;
     const unsigned t_lane = tmem_base + ((unsigned)(quad * 32) << 16);
-    const unsigned t_out = t_lane + L::o_col + x * 128;
-    const float sc = n_tiles > 0 && x < n_qt ? s_sc[x * 128 + r] : 0.f;
-    float ref = -INFINITY, sum = 0.f;
+    const unsigned t_out = t_lane + kOCol + half * (DH / 2);
+    int n = 0, items = 0;
     bool ok = true;
-    float ksn[4], vsn[4];
-    auto load_scales = [&](int t) {
+    LineItem it;
+    if (work)
+      for (LineWalk w(share); w.next<KT>(p, kTcItemCost, it); ++items) {
+        const bool warp_has_rows = quad * 32 < it.nrows;
+        float ref = -INFINITY, sum = 0.f, sc = 0.f;
+        float ksn[2], vsn[2];
+        auto load_scales = [&](int t) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const long long blk = min((long long)blk0 + 4 * t + i, p.n_blocks - 1);   // (a tile may reach over the cache's end)
-        ksn[i] = __ldg(p.k_scale + blk * p.hkv + kh);
-        vsn[i] = __ldg(p.v_scale + blk * p.hkv + kh);
-      }
-    };
-    if (my_tiles > 0) load_scales(0);
-    for (int t = 0; t < my_tiles && ok; ++t) {
-      const int s = SB == 2 ? (t & 1) : x;
-      float f[4], lv[4], inv[4];
+          for (int i = 0; i < 2; ++i) {
+            const long long blk = min((long long)it.block0 + 4 * t + 2 * half + i, p.c.n_blocks - 1);   // (a tile may reach over the end)
+            ksn[i] = __ldcg(p.c.k_scale + blk * p.hkv + it.head);
+            vsn[i] = __ldcg(p.c.v_scale + blk * p.hkv + it.head);
+          }
+        };
+        load_scales(it.b0);
+        for (int t = it.b0; t < it.b1; ++t, ++n) {
+          const int s = n & 1;
+          float f[2], lv[2], inv[2];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float vs = kv8_clamp_scale(vsn[i]);
-        f[i] = sc * kv8_clamp_scale(ksn[i]);
-        lv[i] = log2_fast(vs);
-        inv[i] = 1.0f / vs;
-      }
-      if (t + 1 < my_tiles) load_scales(t + 1);
-      const int left = vis - (kt0 + t) * KT;
-      if (!mbar_wait(bar(B_SFULL + s), (unsigned)(SB == 2 ? t >> 1 : t) & 1u, abort_flag)) { ok = false; break; }
-      // The product of the tile before is done: the output may be rescaled, and no warp of the group - one without query
-      // rows has nothing to hold it up - publishes this tile before all four have published that one.
-      if (t > 0 && !mbar_wait(bar(B_OFULL + x), (unsigned)(t - 1) & 1u, abort_flag)) { ok = false; break; }
-      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      if (warp_has_rows) {
-        // the tile's maximum of t; the next 32 scores are loaded while these are worked on
-        float top = -INFINITY;
-        {
-          unsigned raw[2][32];
-          tmem_ld32_nowait(t_lane + s * 128, raw[0]);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
+          for (int i = 0; i < 2; ++i) {
+            const float vs = kv8_clamp_scale(vsn[i]);
+            f[i] = kv8_clamp_scale(ksn[i]);
+            lv[i] = log2_fast(vs);
+            inv[i] = 1.0f / vs;
+          }
+          if (t + 1 < it.b1) load_scales(t + 1);
+          const int left = it.vis - t * KT - half * 64;      // keys of this thread's half that the row sees
+          ok = mbar_wait(bar(B_SFULL + s), (unsigned)(n >> 1) & 1u, abort_flag) && ok;
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          if (t == it.b0) {
+            ok = mbar_wait(bar(B_QFULL + (items & 1)), (unsigned)(items >> 1) & 1u, abort_flag) && ok;
+            sc = s_sc[items & 1][r];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(B_QEMPTY + (items & 1)));
+          }
+          if (warp_has_rows) {
+            f[0] *= sc;
+            f[1] *= sc;
+            unsigned raw[64];
+            tmem_ld32_nowait(t_lane + s * 128 + half * 64, raw);
+            tmem_ld32_nowait(t_lane + s * 128 + half * 64 + 32, raw + 32);
             tmem_ld_wait();
-            if (i < 3) tmem_ld32_nowait(t_lane + s * 128 + (i + 1) * 32, raw[(i + 1) & 1]);
-            float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-            if (left >= (i + 1) * 32) {
+            if (left < 64) {
 #pragma unroll
-              for (int j = 0; j < 32; ++j) m4[j & 3] = fmaxf(m4[j & 3], __uint_as_float(raw[i & 1][j]));
+              for (int j = 0; j < 64; ++j) raw[j] = j < left ? raw[j] : 0xff800000u;      // -inf
+            }
+            float top = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+              for (int j = 0; j < 32; ++j) m4[j & 3] = fmaxf(m4[j & 3], __uint_as_float(raw[i * 32 + j]));
+              top = fmaxf(top, fmaf(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])), f[i], lv[i]));
+            }
+            // from here on the scores of both halves are in registers: the buffer may be overwritten
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            const bool grow = pair_any(pair, top > ref + kTcGrow);
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            if (grow) {
+              s_pair[half][r] = top;
+              pair_sync(pair);
+              top = fmaxf(top, s_pair[half ^ 1][r]);
+              pair_sync(pair);
+              float turn = 1.f;
+              if (top > ref + kTcGrow) {
+                turn = exp2_fast(ref - (top - kTcBias));     // 2^-inf = 0 on the first tile
+                ref = top - kTcBias;
+                sum *= turn;
+              }
+              if (t > it.b0) {
+                // the product of the tile before has to be done with the output
+                ok = mbar_wait(bar(B_OFULL), (unsigned)(n - 1) & 1u, abort_flag) && ok;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll 1
+                for (int c = 0; c < DH / 64; ++c) {
+                  unsigned o[32];
+                  tmem_ld32_nowait(t_out + c * 32, o);
+                  tmem_ld_wait();
+#pragma unroll
+                  for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * turn);
+                  tmem_st32(t_out + c * 32, o);
+                }
+                tmem_st_wait();
+              }
+            }
+            unsigned out[32];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const float shift = lv[i] - ref;
+              float a4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+              for (int j = 0; j < 32; j += 2) {
+                float e0 = exp2_fast(fmaf(__uint_as_float(raw[i * 32 + j]), f[i], shift));
+                float e1 = exp2_fast(fmaf(__uint_as_float(raw[i * 32 + j + 1]), f[i], shift));
+                a4[(j >> 1) & 3] += e0 + e1;
+                const __half2 h = __floats2half2_rn(e0, e1);
+                out[i * 16 + (j >> 1)] = *reinterpret_cast<const unsigned*>(&h);
+              }
+              sum = fmaf((a4[0] + a4[1]) + (a4[2] + a4[3]), inv[i], sum);
+            }
+            tmem_st32(t_lane + s * 128 + half * 32, out);
+            tmem_st_wait();
+          }
+          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(B_PFULL + s));
+        }
+        // ---- output: half of the dims per thread ----
+        // The item's last product; one tile at a time, for a parity cannot tell a phase from the one two before.  (Warps
+        // without query rows wait too: they would otherwise report the next item before the others have this one.)
+        if (n > 1) ok = mbar_wait(bar(B_OFULL), (unsigned)(n - 2) & 1u, abort_flag) && ok;
+        ok = mbar_wait(bar(B_OFULL), (unsigned)(n - 1) & 1u, abort_flag) && ok;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        if (warp_has_rows) {
+          s_pair[half][r] = sum;
+          pair_sync(pair);
+          const float total = sum + s_pair[half ^ 1][r];
+          pair_sync(pair);
+          const bool valid = r < it.nrows && ok;
+          const int rr = r < it.nrows ? r : 0;
+          const bool whole = it.b0 == 0 && it.b1 == it.nb;
+          const size_t slot = 2 * (size_t)blockIdx.x + (it.opens ? 0 : 1);
+          bf16* dst = p.out + ((size_t)(it.t0 + rr / G) * p.hq + it.head * G + rr % G) * DH + half * (DH / 2);
+          float* part = p.part_o + (slot * 128 + rr) * DH + half * (DH / 2);
+          const float inv = 1.0f / total;
+          if (!whole && valid && half == 0) p.part_ml[slot * 128 + rr] = make_float2(ref, total);
+#pragma unroll 1
+          for (int c = 0; c < DH / 64; ++c) {
+            unsigned o[32];
+            tmem_ld32_nowait(t_out + c * 32, o);
+            tmem_ld_wait();
+            if (!valid) continue;
+            if (!whole) {
+#pragma unroll
+              for (int g = 0; g < 8; ++g)
+                *reinterpret_cast<uint4*>(part + c * 32 + g * 4) = make_uint4(o[g * 4], o[g * 4 + 1], o[g * 4 + 2], o[g * 4 + 3]);
             } else {
 #pragma unroll
-              for (int j = 0; j < 32; ++j)
-                if (i * 32 + j < left) m4[j & 3] = fmaxf(m4[j & 3], __uint_as_float(raw[i & 1][j]));
-            }
-            top = fmaxf(top, fmaf(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])), f[i], lv[i]));
-          }
-        }
-        const bool grow = top > ref + kTcGrow;
-        if (__any_sync(0xffffffffu, grow)) {
-          float turn = 1.f;
-          if (grow) {
-            turn = exp2_fast(ref - (top - kTcBias));     // 2^-inf = 0 on the first tile
-            ref = top - kTcBias;
-            sum *= turn;
-          }
-          if (t > 0) {
-#pragma unroll 1
-            for (int c = 0; c < 4; ++c) {
-              unsigned o[32];
-              tmem_ld32_nowait(t_out + c * 32, o);
-              tmem_ld_wait();
+              for (int g = 0; g < 4; ++g) {
+                uint4 v;
+                __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&v);
 #pragma unroll
-              for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * turn);
-              tmem_st32(t_out + c * 32, o);
-              tmem_st_wait();
+                for (int j = 0; j < 4; ++j)
+                  h[j] = __floats2bfloat162_rn(__uint_as_float(o[g * 8 + 2 * j]) * inv, __uint_as_float(o[g * 8 + 2 * j + 1]) * inv);
+                *reinterpret_cast<uint4*>(dst + c * 32 + g * 8) = v;
+              }
             }
           }
         }
-        unsigned w[64];
-        {
-          unsigned raw[2][16];
-          tmem_ld16_nowait(t_lane + s * 128, raw[0]);
-          float part = 0.f;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            tmem_ld_wait();
-            if (i < 7) tmem_ld16_nowait(t_lane + s * 128 + (i + 1) * 16, raw[(i + 1) & 1]);
-            const float shift = lv[i >> 1] - ref;
-            float e[16];
-#pragma unroll
-            for (int j = 0; j < 16; ++j) e[j] = exp2_fast(fmaf(__uint_as_float(raw[i & 1][j]), f[i >> 1], shift));
-            if (left < (i + 1) * 16) {
-#pragma unroll
-              for (int j = 0; j < 16; ++j) e[j] = i * 16 + j < left ? e[j] : 0.f;
-            }
-            float a4[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int j = 0; j < 16; j += 2) {
-              a4[(j >> 1) & 3] += e[j] + e[j + 1];
-              const __half2 h = __floats2half2_rn(e[j], e[j + 1]);
-              w[i * 8 + (j >> 1)] = *reinterpret_cast<const unsigned*>(&h);
-            }
-            const float got = (a4[0] + a4[1]) + (a4[2] + a4[3]);
-            if (i & 1) sum = fmaf(part + got, inv[i >> 1], sum);
-            else part = got;
-          }
-        }
-        tmem_st32(t_lane + s * 128, w);
-        tmem_st32(t_lane + s * 128 + 32, w + 32);
-        tmem_st_wait();
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(B_OEMPTY));
       }
-      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(B_PFULL + x));
-    }
-    const bool have = ok && my_tiles > 0 && mbar_wait(bar(B_OFULL + x), (unsigned)(my_tiles - 1) & 1u, abort_flag);
-    if (warp_has_rows) {
-      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      const bool valid = r < nrows;
-      const int rr = valid ? r : 0;
-      const size_t tok = (size_t)(t0 + x * p.tq + rr / G);
-      const size_t at = (tok * p.hq + kh * G + rr % G) * DH;
-      const size_t ml_at = ((size_t)blockIdx.z * p.M + tok) * p.hq + kh * G + rr % G;
-      if (p.chunks > 1 && valid) p.part_ml[ml_at] = make_float2(have ? ref : -INFINITY, have ? sum : 0.f);
-      const float inv = have ? 1.0f / sum : 0.f;
-      float* pdst = p.part_o + (size_t)blockIdx.z * p.M * p.hq * DH + at;
-#pragma unroll 1
-      for (int c = 0; c < 4; ++c) {
-        unsigned o[32];
-        if (have) {
-          tmem_ld32_nowait(t_out + c * 32, o);
-          tmem_ld_wait();
-        } else {
-#pragma unroll
-          for (int j = 0; j < 32; ++j) o[j] = 0u;        // no keys: zeros
-        }
-        if (!valid) continue;
-        if (p.chunks > 1) {
-          if (have) {
-#pragma unroll
-            for (int g = 0; g < 8; ++g)
-              *reinterpret_cast<uint4*>(pdst + c * 32 + g * 4) = make_uint4(o[g * 4], o[g * 4 + 1], o[g * 4 + 2], o[g * 4 + 3]);
-          }
-        } else {
-#pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            uint4 v;
-            __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&v);
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              h[j] = __floats2bfloat162_rn(__uint_as_float(o[g * 8 + 2 * j]) * inv, __uint_as_float(o[g * 8 + 2 * j + 1]) * inv);
-            *reinterpret_cast<uint4*>(p.out + at + c * 32 + g * 8) = v;
-          }
-        }
-      }
-    }
   }
 
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -544,60 +527,17 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
   }
 }
 
-// Merges the key chunks of every (token, head): out = sum_c 2^(m_c - m) o_c / sum_c 2^(m_c - m) l_c.  A warp per head.
-constexpr int kMaxChunks = 4;
-__global__ void __launch_bounds__(256) k_attention_kv8_chunks(const TcParams p) {
-  pdl_wait();
-  pdl_trigger();
-  const float* part_o = p.part_o;
-  const float2* part_ml = p.part_ml;
-  const int chunks = p.chunks, M = p.M, hq = p.hq;
-  bf16* out = p.out;
-  const long long unit = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-  if (unit >= (long long)M * hq) return;
-  const int lane = threadIdx.x & 31, tok = (int)(unit / hq);
-  const int row = warp_search(p.n_rows, tok, [&](int i) { return __ldg(p.cu_q + i); });
-  const int cq0 = __ldg(p.cu_q + row), cq1 = __ldg(p.cu_q + row + 1);
-  if (tok < cq0 || tok >= cq1 || !row_fits(p, cq0, cq1, __ldg(p.vis + row), __ldg(p.kv_base + row))) return;
-  float2 ml[kMaxChunks];
-  float4 v[kMaxChunks];
-#pragma unroll
-  for (int c = 0; c < kMaxChunks; ++c) {
-    ml[c] = make_float2(-INFINITY, 0.f);
-    if (c < chunks) ml[c] = part_ml[(long long)c * M * hq + unit];
-    v[c] = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (c < chunks && ml[c].y != 0.f)
-      v[c] = *reinterpret_cast<const float4*>(part_o + ((long long)c * M * hq + unit) * DH + lane * 4);
-  }
-  float m = -INFINITY, l = 0.f;
-#pragma unroll
-  for (int c = 0; c < kMaxChunks; ++c) m = fmaxf(m, ml[c].x);
-  float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-  for (int c = 0; c < kMaxChunks; ++c) {
-    if (ml[c].y == 0.f) continue;
-    const float w = ml[c].x > -INFINITY ? exp2_fast(ml[c].x - m) : 1.f;
-    l += w * ml[c].y;
-    a.x += w * v[c].x; a.y += w * v[c].y; a.z += w * v[c].z; a.w += w * v[c].w;
-  }
-  const float inv = l != 0.f ? 1.0f / l : 0.f;
-  uint2 o;
-  __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&o);
-  h[0] = __floats2bfloat162_rn(a.x * inv, a.y * inv);
-  h[1] = __floats2bfloat162_rn(a.z * inv, a.w * inv);
-  *reinterpret_cast<uint2*>(out + unit * DH + lane * 4) = o;
-}
-
-// e4m3 codes [n_blocks][hkv][32][128] as bytes; box: four blocks of one head
-bool make_map(const unsigned char* ptr, int hkv, long long n_blocks, bool swizzle, CUtensorMap* out) {
+// e4m3 codes [n_blocks][hkv][32][dh] as bytes; box: four blocks of one head
+bool make_map(const unsigned char* ptr, int hkv, int dh, long long n_blocks, bool swizzle, CUtensorMap* out) {
   PFN_cuTensorMapEncodeTiled_v12000 encode = tensor_map_encoder();
   if (!encode) return false;
-  const cuuint64_t dims[4] = {(cuuint64_t)DH, (cuuint64_t)kKv8Block, (cuuint64_t)hkv, (cuuint64_t)n_blocks};
-  const cuuint64_t strides[3] = {(cuuint64_t)DH, (cuuint64_t)kKv8Block * DH, (cuuint64_t)hkv * kKv8Block * DH};
-  const cuuint32_t box[4] = {(cuuint32_t)DH, (cuuint32_t)kKv8Block, 1, KT / kKv8Block};
+  const cuuint64_t dims[4] = {(cuuint64_t)dh, (cuuint64_t)kKv8Block, (cuuint64_t)hkv, (cuuint64_t)n_blocks};
+  const cuuint64_t strides[3] = {(cuuint64_t)dh, (cuuint64_t)kKv8Block * dh, (cuuint64_t)hkv * kKv8Block * dh};
+  const cuuint32_t box[4] = {(cuuint32_t)dh, (cuuint32_t)kKv8Block, 1, KT / kKv8Block};
   const cuuint32_t estr[4] = {1, 1, 1, 1};
   return encode(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<unsigned char*>(ptr), dims, strides, box, estr,
-                CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
+                CU_TENSOR_MAP_INTERLEAVE_NONE,
+                !swizzle ? CU_TENSOR_MAP_SWIZZLE_NONE : dh == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
                 CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -606,7 +546,8 @@ std::mutex g_mutex;
 
 }  // namespace
 
-cudaError_t launch_attention_kv8_tc(const AttnKv8Args& a, float* part, size_t part_floats, cudaStream_t s) {
+// p: everything but the query tile; *ctas: how many partial-slot pairs the launch may use (two slots of 128 rows each).
+cudaError_t launch_attention_kv8_tc(LineParams p, int dh, int max_ctas, int* ctas, cudaStream_t s) {
   int* sms = device_slot(g_sms);
   if (!sms) return cudaErrorInvalidDevice;
   {
@@ -616,41 +557,19 @@ cudaError_t launch_attention_kv8_tc(const AttnKv8Args& a, float* part, size_t pa
       cudaError_t r = cudaGetDevice(&dev);
       if (r == cudaSuccess) r = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
       if (r == cudaSuccess)
-        r = cudaFuncSetAttribute(k_attention_kv8_tc<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, TcLayout<1>::smem);
+        r = cudaFuncSetAttribute(k_attention_kv8_tc<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, TcLayout<64>::smem);
       if (r == cudaSuccess)
-        r = cudaFuncSetAttribute(k_attention_kv8_tc<2>, cudaFuncAttributeMaxDynamicSharedMemorySize, TcLayout<2>::smem);
+        r = cudaFuncSetAttribute(k_attention_kv8_tc<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, TcLayout<128>::smem);
       if (r != cudaSuccess) return r;
       *sms = n;
     }
   }
   CUtensorMap mk, mv;
-  if (!make_map(a.cache.k, a.hkv, a.cache.n_blocks, true, &mk) || !make_map(a.cache.v, a.hkv, a.cache.n_blocks, false, &mv))
+  if (!make_map(p.c.k, p.hkv, dh, p.c.n_blocks, true, &mk) || !make_map(p.c.v, p.hkv, dh, p.c.n_blocks, false, &mv))
     return cudaErrorInvalidValue;
-  const int G = a.hq / a.hkv;
-  TcParams p;
-  p.q = a.q; p.q_ld = a.q_ld; p.k_scale = a.cache.k_scale; p.v_scale = a.cache.v_scale; p.n_blocks = a.cache.n_blocks;
-  p.out = a.out; p.cu_q = a.cu_q; p.kv_base = a.kv_base; p.vis = a.vis;
-  p.n_rows = a.n_rows; p.M = a.M; p.hq = a.hq; p.hkv = a.hkv; p.error_flag = a.error_flag;
-  p.tq = 128 / G;
-  // Two query tiles per CTA share every key tile it loads and converts; one per CTA fills the SMs when there are few.
-  const int nq = a.max_nq > 0 ? a.max_nq : a.M;
-  const long long singles = (long long)((nq + p.tq - 1) / p.tq) * a.n_rows * a.hkv;       // most query tiles there can be
-  const bool two = singles > 2ll * *sms && nq > p.tq;
-  const int key_tiles = a.max_vis > 0 ? (a.max_vis + KT - 1) / KT : 1;
-  int chunks = 1;
-  if (!two)
-    while (chunks < kMaxChunks && singles * (chunks + 1) <= *sms && key_tiles / (chunks + 1) >= 2 &&
-           (size_t)(chunks + 1) * a.M * a.hq * (DH + 2) <= part_floats)
-      ++chunks;
-  p.chunks = chunks;
-  p.part_o = part;
-  p.part_ml = reinterpret_cast<float2*>(part + (size_t)chunks * a.M * a.hq * DH);
-  const int per_cta = (two ? 2 : 1) * p.tq;
-  const dim3 grid((unsigned)((long long)a.M / per_cta + a.n_rows), a.hkv, chunks);
-  cudaError_t r = two ? launch_pdl(k_attention_kv8_tc<2>, grid, dim3(TcLayout<2>::threads), (size_t)TcLayout<2>::smem, s, mk, mv, p)
-                      : launch_pdl(k_attention_kv8_tc<1>, grid, dim3(TcLayout<1>::threads), (size_t)TcLayout<1>::smem, s, mk, mv, p);
-  if (r != cudaSuccess || chunks == 1) return r;
-  return launch_pdl(k_attention_kv8_chunks, dim3((unsigned)(((long long)a.M * a.hq + 7) / 8)), dim3(256), 0, s, p);
+  *ctas = std::min(*sms, max_ctas);
+  return dh == 128 ? launch_pdl(k_attention_kv8_tc<128>, dim3(*ctas), dim3(kTcThreads), (size_t)TcLayout<128>::smem, s, mk, mv, p)
+                   : launch_pdl(k_attention_kv8_tc<64>, dim3(*ctas), dim3(kTcThreads), (size_t)TcLayout<64>::smem, s, mk, mv, p);
 }
 
 }  // namespace bs

@@ -78,7 +78,7 @@ __device__ __forceinline__ void token_heads(const QkNormArgs& a, int t, int h0, 
                                             bf16* kc, bf16* vc) {
   constexpr int LPH = DH / 8, HPW = 32 / LPH;      // lanes per head, heads per warp pass
   const int lane = threadIdx.x & 31, p = lane % LPH;
-  const int pos = __ldg(a.tok_pos + t);
+  const int pos = __ldcg(a.tok_pos + t);
   if (pos < 0 || pos >= a.max_pos) {               // warp-uniform
     if (lane == 0) bad_index(a.error_flag, SITE_QK_NORM);
     return;
@@ -130,7 +130,7 @@ __global__ void __launch_bounds__(kWarps * 32) k_qk_norm_rope_kv(QkNormArgs a, c
   const long long unit = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5);
   const int t = (int)(unit / shares), part = (int)(unit % shares);
   if (t >= a.M) return;
-  const int row = __ldg(tok_kv + t);
+  const int row = __ldcg(tok_kv + t);
   if (row < 0) return;
   if (row >= kv_rows) {
     if ((threadIdx.x & 31) == 0) bad_index(a.error_flag, SITE_QK_NORM);
@@ -152,13 +152,13 @@ struct Slot {
 __device__ __forceinline__ bool find_slot(int slot, const int* __restrict__ cu, const int* __restrict__ kv_base,
                                           const int* __restrict__ kv_at, int n_rows, int M, long long n_blocks,
                                           int* flag, Slot& s) {
-  s.row = warp_search(n_rows, slot, [&](int i) { return __ldg(cu + i) / kKv8Block + 2 * i; });
+  s.row = warp_search(n_rows, slot, [&](int i) { return __ldcg(cu + i) / kKv8Block + 2 * i; });
   const int r = s.row;
-  s.t0 = __ldg(cu + r);
-  const int t1 = __ldg(cu + r + 1);
+  s.t0 = __ldcg(cu + r);
+  const int t1 = __ldcg(cu + r + 1);
   s.n = t1 - s.t0;
-  s.base = __ldg(kv_base + r);
-  s.at = __ldg(kv_at + r);
+  s.base = __ldcg(kv_base + r);
+  s.at = __ldcg(kv_at + r);
   if (s.n == 0) return false;
   const bool ok = s.t0 >= 0 && s.n > 0 && t1 <= M && s.base >= 0 && s.base % kKv8Block == 0 && s.at >= 0 &&
                   (long long)s.base + s.at + s.n <= n_blocks * kKv8Block;
@@ -205,7 +205,7 @@ __device__ void write_tile(const QkNormArgs& a, const Slot& s, int kv_len, const
     for (int j = 0; j < 8; ++j) cs[j] = make_float2(1.f, 0.f);
     if (at >= s.at && at < s.at + s.n) {
       const int t = s.t0 + at - s.at;
-      const int pos = __ldg(a.tok_pos + t);
+      const int pos = __ldcg(a.tok_pos + t);
       if (pos >= 0 && pos < a.max_pos) {
         state[i] = 2;
         const int h = a.hq + (is_k ? 0 : a.hkv) + head;
@@ -277,7 +277,7 @@ __global__ void __launch_bounds__(kTileThreads) k_qk_norm_rope_kv8(QkNormArgs a,
   if ((int)blockIdx.x < q_ctas) {
     const long long unit = (long long)blockIdx.x * (kTileThreads / 32) + (threadIdx.x >> 5);
     const int t = (int)(unit / shares), part = (int)(unit % shares);
-    if (t >= min(a.M, __ldg(cu_q + n_rows))) return;      // tokens behind the last row are left alone
+    if (t >= min(a.M, __ldcg(cu_q + n_rows))) return;      // tokens behind the last row are left alone
     token_heads<DH, false>(a, t, part * per_share, min(a.hq, (part + 1) * per_share), 0, nullptr, nullptr);
     return;
   }
@@ -285,7 +285,7 @@ __global__ void __launch_bounds__(kTileThreads) k_qk_norm_rope_kv8(QkNormArgs a,
   const int which = unit % (2 * a.hkv), slot = unit / (2 * a.hkv);
   Slot s;
   if (!find_slot(slot, cu_q, kv_base, kv_at, n_rows, a.M, c.n_blocks, a.error_flag, s)) return;
-  write_tile<DH>(a, s, __ldg(kv_len + s.row), c, which >> 1, (which & 1) == 0, s_max);
+  write_tile<DH>(a, s, __ldcg(kv_len + s.row), c, which >> 1, (which & 1) == 0, s_max);
 }
 
 // One CTA: one work slot (a cache block's share of a row), all kv heads, K and V.
@@ -306,7 +306,7 @@ __global__ void __launch_bounds__(256) k_kv8_read(Kv8Cache c, const int* __restr
     if (r < lo || r >= hi) continue;
     const size_t tile = (size_t)s.block * hkv + head;
     const unsigned char* codes = (hw & 1) ? c.v : c.k;
-    const float scale = kv8_clamp_scale(__ldg(((hw & 1) ? c.v_scale : c.k_scale) + tile));
+    const float scale = kv8_clamp_scale(__ldcg(((hw & 1) ? c.v_scale : c.k_scale) + tile));
     const uint2 w = *reinterpret_cast<const uint2*>(codes + (tile * kKv8Block + r) * DH + p * 8);
     unsigned h[4];
     kv8_decode4(w.x, h[0], h[1]);

@@ -6,6 +6,10 @@
 // 448.  e4m3 is a floating format, so a power of two loses no relative precision against amax / 448 (normal values
 // keep 4 significant bits either way); in exchange code * scale is exact in bf16 and fp32, and a tile whose scale
 // moves when rows are rewritten is re-encoded without a second rounding (except where values go subnormal).
+//
+// The kernels here may be on the device before the kernel in front of them has ended (programmatic dependent launch):
+// what that one may have written - queries, scales, indices - is read past the L1 cache (__ldcg, cp.async.cg, TMA) and
+// never through the read-only path, which is for weights and tables.
 #pragma once
 #include <cuda_fp16.h>
 
@@ -118,7 +122,5 @@ struct AttnKv8Args {
 constexpr int kAttnKv8MaxRows = 1024;
 size_t attention_kv8_scratch_bytes(int hq, int hkv, int dh);
 cudaError_t launch_attention_kv8(const AttnKv8Args& a, cudaStream_t s);
-// tensor-core kernel for many query rows per kv head (head_dim 128); part: scratch for partial results of key chunks
-cudaError_t launch_attention_kv8_tc(const AttnKv8Args& a, float* part, size_t part_floats, cudaStream_t s);
 
 }  // namespace bs
