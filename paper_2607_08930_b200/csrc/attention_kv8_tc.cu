@@ -5,7 +5,7 @@
 // lane.  All items' key tiles (128 keys) form one line - an item counts a little more than its tiles - that the CTAs of
 // one resident wave, one per SM, share evenly; cut items leave parts for the merge kernel (attention_kv8.cu).  A CTA is
 // persistent and warp-specialised; the rings run on from one item to the next:
-//   warp 0        producer: tiles of K and V codes by TMA, each through a ring of its own
+//   warp 0        producer: tiles of K and V codes by TMA, each through a ring of its own; the next item's query rows
 //   warp 1        issues the products.  S = Q K^T takes K's codes as they arrive (kind::f8f6f4, e4m3 x e4m3): a query
 //                 element, after a power of two per query row has brought the row's largest into [128, 256), is the sum
 //                 of two e4m3 values - the nearest one and the rest (4 + 4 significant bits, bf16 has 8: exact above
@@ -13,14 +13,14 @@
 //                 twice the rate of one in fp16, and K is neither converted nor stored a second time.  Q is an operand
 //                 from tensor memory (two buffers): read from shared memory it would take half of that memory's
 //                 bandwidth, which is what the products of a 128 x 128 tile are bound by.
-//   8 warps       softmax: two threads per query row, half of a tile's keys each; they hold their scores in registers
-//                 from the maximum to the weights.  The weights w = 2^(t - M) go back to tensor memory as fp16, over
-//                 the first half of their scores, as the A operand of O += W V.  Scores are double-buffered: the next
-//                 tile's are formed while this one's are worked on.
+//   2 x 4 warps   softmax, a query row per thread: one group takes the even tiles, the other the odd ones, each with a
+//                 scores buffer of its own, so that the exponentials of one run under the loads, maxima and stores of
+//                 the other.  The weights w = 2^(t - M) go back to tensor memory as fp16, over the first half of their
+//                 scores, as the A operand of O += W V.
 //   4 more warps  V's codes to fp16 (exact) in the layout of a B operand, rows behind the row's end as zeros; and the
 //                 next item's queries to tensor memory.
-// Weights are formed against a running reference that lags the maximum (kTcBias, kTcGrow): the output is rescaled only
-// when a row's maximum has outgrown it.
+// Weights are formed against a reference per row that lags the maximum (kTcBias, kTcGrow); the groups pass it to each
+// other from tile to tile.  The output is rescaled only when a row's maximum has outgrown it.
 // Every wait is bounded; on a timeout the flag is raised, all roles run through their loops without waiting, and the
 // copies in flight are waited for.
 #include <math.h>
@@ -40,6 +40,7 @@ using namespace tc;
 constexpr int KT = 128;                              // keys per tile: four cache blocks
 constexpr int kTcThreads = 512;
 constexpr int kKStages = 4, kV8Stages = 3, kV16Stages = 2;
+constexpr int kQPad = 16;                            // bytes between query rows in shared memory: every lane its own banks
 constexpr float kTcBias = 6.f, kTcGrow = 14.f;       // weights reach 2^14 at most, 2^6 when the reference is set
 constexpr int kTcItemCost = 1;                       // tiles that an item counts beyond its own
 constexpr unsigned kOCol = 256, kQCol = 384;         // tensor memory: two scores buffers, output, two query buffers
@@ -48,7 +49,9 @@ template <int DH>
 struct TcLayout {
   static constexpr int k8 = KT * DH;                 // one tile of codes
   static constexpr int v16 = KT * DH * 2;            // one tile of V in fp16: DH / 64 parts of 64 dims
-  static constexpr int k = 0, v8 = k + kKStages * k8, v = v8 + kV8Stages * k8, bytes = v + kV16Stages * v16;
+  static constexpr int q_row = DH * 2 + kQPad;
+  static constexpr int k = 0, v8 = k + kKStages * k8, v = v8 + kV8Stages * k8, q = v + kV16Stages * v16,
+                       bytes = q + 128 * q_row;
   static constexpr int smem = bytes + 1024;
   static constexpr int q_cols = DH / 2;              // tensor-memory columns of one query buffer (nearest values, rests)
 };
@@ -58,30 +61,43 @@ __device__ __forceinline__ void tma_load_4d(unsigned dst, const CUtensorMap* map
       "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
       ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar) : "memory");
 }
+__device__ __forceinline__ void bulk_load(unsigned dst, const void* src, unsigned bytes, unsigned bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
 // High word of a descriptor of an operand whose rows are row_bytes long (128 or 64, swizzled by as much), K-major.
 template <int ROW>
 __host__ __device__ constexpr unsigned desc_hi() { return (unsigned)(8 * ROW >> 4) | (1u << 14) | ((ROW == 128 ? 2u : 4u) << 29); }
 // S: e4m3 (A, tensor memory) x e4m3 (B, K-major), fp32 accumulator, 128 x 128 x 32
 constexpr unsigned kIdescS = (1u << 4) | ((unsigned)(KT >> 3) << 17) | ((128u >> 4) << 24);
+// The issuing warp runs as a whole and one lane's instructions take effect: descriptors and addresses then stay in
+// uniform registers, where the instruction wants them.
 template <int DH>
-__device__ __forceinline__ void umma_qk(unsigned d_tmem, unsigned a_tmem, unsigned b_lo, unsigned accumulate) {
+__device__ __forceinline__ void umma_qk(unsigned d_tmem, unsigned a_tmem, unsigned b_lo, unsigned accumulate, unsigned leader) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t.reg .b64 db;\n\t"
+      "{\n\t.reg .pred p, q;\n\t.reg .b64 db;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
+      "setp.ne.b32 q, %6, 0;\n\t"
       "mov.b64 db, {%2, %5};\n\t"
-      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], [%1], db, %3, p;\n\t}"
-      ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(kIdescS), "r"(accumulate), "r"(desc_hi<DH>()) : "memory");
+      "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], [%1], db, %3, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(kIdescS), "r"(accumulate), "r"(desc_hi<DH>()), "r"(leader) : "memory");
 }
 // O: fp16 (A, tensor memory) x fp16 (B, MN-major), fp32 accumulator, 128 x DH x 16
 template <int DH>
-__device__ __forceinline__ void umma_pv(unsigned d_tmem, unsigned a_tmem, unsigned b_lo, unsigned accumulate) {
+__device__ __forceinline__ void umma_pv(unsigned d_tmem, unsigned a_tmem, unsigned b_lo, unsigned accumulate, unsigned leader) {
   constexpr unsigned idesc = (1u << 4) | (1u << 16) | ((unsigned)(DH >> 3) << 17) | ((128u >> 4) << 24);
   asm volatile(
-      "{\n\t.reg .pred p;\n\t.reg .b64 db;\n\t"
+      "{\n\t.reg .pred p, q;\n\t.reg .b64 db;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
+      "setp.ne.b32 q, %6, 0;\n\t"
       "mov.b64 db, {%2, %5};\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}"
-      ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kDescHi) : "memory");
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kDescHi), "r"(leader) : "memory");
+}
+__device__ __forceinline__ void umma_commit_if(unsigned bar, unsigned leader) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar), "r"(leader) : "memory");
 }
 __device__ __forceinline__ void tmem_st32(unsigned taddr, const unsigned* w) {
   asm volatile(
@@ -98,6 +114,14 @@ __device__ __forceinline__ void tmem_st8(unsigned taddr, const unsigned* w) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
                ::"r"(taddr), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
 }
+__device__ __forceinline__ void tmem_st16(unsigned taddr, const unsigned* w) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+      ::"r"(taddr), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]), "r"(w[8]),
+        "r"(w[9]), "r"(w[10]), "r"(w[11]), "r"(w[12]), "r"(w[13]), "r"(w[14]), "r"(w[15])
+      : "memory");
+}
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ uint4 lds128(unsigned at) {
   uint4 v;
@@ -109,14 +133,9 @@ __device__ __forceinline__ void sts128(unsigned at, unsigned a, unsigned b, unsi
 }
 // generic-proxy writes to shared memory before tensor-core reads of it
 __device__ __forceinline__ void fence_smem_for_mma() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-// the two warps of a query row quarter: do any of their threads say yes?  (also their barrier)
-__device__ __forceinline__ bool pair_any(int id, bool x) {
-  unsigned r;
-  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, %2, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-               : "=r"(r) : "r"((unsigned)x), "r"(id) : "memory");
-  return r != 0;
-}
-__device__ __forceinline__ void pair_sync(int id) { asm volatile("barrier.cta.sync %0, 64;" ::"r"(id) : "memory"); }
+// hand-over between the two warps that own the same query rows: one waits, the other has gone ahead
+__device__ __forceinline__ void turn_wait(int id) { asm volatile("barrier.cta.sync %0, 64;" ::"r"(id) : "memory"); }
+__device__ __forceinline__ void turn_pass(int id) { asm volatile("barrier.cta.arrive %0, 64;" ::"r"(id) : "memory"); }
 
 template <int DH>
 __global__ void __launch_bounds__(kTcThreads, 1)
@@ -124,14 +143,16 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
   using L = TcLayout<DH>;
   enum { B_KFULL = 0, B_KEMPTY = B_KFULL + kKStages, B_V8FULL = B_KEMPTY + kKStages, B_V8EMPTY = B_V8FULL + kV8Stages,
          B_VFULL = B_V8EMPTY + kV8Stages, B_VEMPTY = B_VFULL + kV16Stages, B_SFULL = B_VEMPTY + kV16Stages,
-         B_PFULL = B_SFULL + 2, B_QFULL = B_PFULL + 2, B_QEMPTY = B_QFULL + 2, B_OFULL = B_QEMPTY + 2,
-         B_OEMPTY = B_OFULL + 1, B_COUNT = B_OEMPTY + 1 };
+         B_PFULL = B_SFULL + 2, B_QFULL = B_PFULL + 2, B_QEMPTY = B_QFULL + 2, B_CFULL = B_QEMPTY + 2,
+         B_LFULL = B_CFULL + 4, B_OFULL = B_LFULL + 2, B_OEMPTY = B_OFULL + 2, B_RFULL = B_OEMPTY + 1,
+         B_REMPTY = B_RFULL + 1, B_COUNT = B_REMPTY + 1 };
   extern __shared__ unsigned char smem_dyn[];
   __shared__ __align__(8) unsigned long long bars[B_COUNT];
   __shared__ unsigned tmem_base_slot;
   __shared__ int s_abort;
-  __shared__ float s_sc[2][128];                     // score scale of every query row, by item parity
-  __shared__ float s_pair[2][128];                   // exchange between the two threads of a query row
+  __shared__ float s_sc[4][128];                     // score scale of every query row, by item
+  __shared__ float s_ref[128];                       // reference of every query row
+  __shared__ float2 s_part[2][128];                  // (reference, sum) of the group that does not write the item, by item parity
   __shared__ LineShared<kTcThreads, 1> s_line;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const unsigned smem0 = (smem_u32(smem_dyn) + 1023u) & ~1023u;
@@ -144,12 +165,15 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
     for (int i = 0; i < kV8Stages; ++i) { mbar_init(bar(B_V8FULL + i), 1); mbar_init(bar(B_V8EMPTY + i), 4); }
     for (int i = 0; i < kV16Stages; ++i) { mbar_init(bar(B_VFULL + i), 4); mbar_init(bar(B_VEMPTY + i), 1); }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(bar(B_SFULL + i), 1); mbar_init(bar(B_PFULL + i), 8);
-      mbar_init(bar(B_QFULL + i), 4);
-      mbar_init(bar(B_QEMPTY + i), 9);           // the last scores of an item, and the softmax warps once they know its scales
+      mbar_init(bar(B_SFULL + i), 1); mbar_init(bar(B_PFULL + i), 4);
+      mbar_init(bar(B_QFULL + i), 4); mbar_init(bar(B_QEMPTY + i), 1);
+      mbar_init(bar(B_LFULL + i), 4);
+      mbar_init(bar(B_OFULL + i), 1);
     }
-    mbar_init(bar(B_OFULL), 1);
-    mbar_init(bar(B_OEMPTY), 8);
+    for (int i = 0; i < 4; ++i) mbar_init(bar(B_CFULL + i), 4);
+    mbar_init(bar(B_OEMPTY), 4);
+    mbar_init(bar(B_RFULL), 1);
+    mbar_init(bar(B_REMPTY), 4);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
@@ -168,48 +192,61 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-  const unsigned tmem_base = tmem_base_slot;
+  constexpr unsigned tmem_base = 0;                  // the only place an allocation of all 512 columns can have
   volatile int* abort_flag = &s_abort;
   const int G = p.hq / p.hkv;
   const bool work = share.u0 < share.u1;
+  if (threadIdx.x == 0 && tmem_base_slot != 0) s_abort = 1;
   if (work && threadIdx.x == 0) line_cut<KT>(p, kTcItemCost, share, (int)blockIdx.x);
   if (!work && threadIdx.x == 0) p.cuts[blockIdx.x].nrows = 0;
 
-  // 4 x 128 registers a thread at launch become 80 + 2 x 176 + 80.
+  // 4 x 128 registers a thread at launch become 104 + 2 x 152 + 104.
   const int group = warp >> 2;
   if (group == 0) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
     if (warp == 0) {
-      // ------------------------------------------------------------------ TMA producer
-      if (lane == 0 && work) {
-        int n = 0;
+      // ------------------------------------------------------------------ producer
+      if (work) {
+        int n = 0, items = 0;
         LineItem it;
-        for (LineWalk w(share); w.next<KT>(p, kTcItemCost, it);) {
-          const int blk0 = it.block0 + it.b0 * (KT / kKv8Block);
-          for (int t = 0; t < it.b1 - it.b0; ++t, ++n) {
-            const int ks = n % kKStages, vs = n % kV8Stages;
-            if (!mbar_wait(bar(B_KEMPTY + ks), (unsigned)((n / kKStages) & 1) ^ 1u, abort_flag)) break;
-            if (!mbar_wait(bar(B_V8EMPTY + vs), (unsigned)((n / kV8Stages) & 1) ^ 1u, abort_flag)) break;
-            mbar_expect_tx(bar(B_KFULL + ks), (unsigned)L::k8);
-            tma_load_4d(sK + ks * L::k8, &map_k, 0, 0, it.head, blk0 + 4 * t, bar(B_KFULL + ks));
-            mbar_expect_tx(bar(B_V8FULL + vs), (unsigned)L::k8);
-            tma_load_4d(sV8 + vs * L::k8, &map_v, 0, 0, it.head, blk0 + 4 * t, bar(B_V8FULL + vs));
-          }
-          if (*abort_flag) break;
-        }
-        if (*abort_flag) {            // copies in flight end before the CTA does
-          for (int t = max(0, n - kKStages); t < n; ++t) {
-            const long long begin = clock64();
-            while (!(mbar_try_wait(bar(B_KFULL + t % kKStages), (unsigned)(t / kKStages) & 1u) &&
-                     (t < n - kV8Stages || mbar_try_wait(bar(B_V8FULL + t % kV8Stages), (unsigned)(t / kV8Stages) & 1u))) &&
-                   clock64() - begin < kWaitCycles / 64) {
+        for (LineWalk w(share); w.next<KT>(p, kTcItemCost, it); ++items) {
+          // (one lane's word counts for the warp: it stays together)
+          if (!__shfl_sync(0xffffffffu, lane > 0 || mbar_wait(bar(B_REMPTY), (unsigned)(items & 1) ^ 1u, abort_flag), 0)) break;
+          if (lane == 0) mbar_expect_tx(bar(B_RFULL), (unsigned)(it.nrows * DH * 2));
+          __syncwarp();
+          for (int f = lane; f < it.nrows; f += 32)
+            bulk_load(smem0 + L::q + f * L::q_row, p.q + (size_t)(it.t0 + f / G) * p.q_ld + (it.head * G + f % G) * DH, DH * 2,
+                      bar(B_RFULL));
+          __syncwarp();
+          if (lane == 0) {
+            const int blk0 = it.block0 + it.b0 * (KT / kKv8Block);
+            for (int t = 0; t < it.b1 - it.b0; ++t, ++n) {
+              const int ks = n % kKStages, vs = n % kV8Stages;
+              if (!mbar_wait(bar(B_KEMPTY + ks), (unsigned)((n / kKStages) & 1) ^ 1u, abort_flag)) break;
+              if (!mbar_wait(bar(B_V8EMPTY + vs), (unsigned)((n / kV8Stages) & 1) ^ 1u, abort_flag)) break;
+              mbar_expect_tx(bar(B_KFULL + ks), (unsigned)L::k8);
+              tma_load_4d(sK + ks * L::k8, &map_k, 0, 0, it.head, blk0 + 4 * t, bar(B_KFULL + ks));
+              mbar_expect_tx(bar(B_V8FULL + vs), (unsigned)L::k8);
+              tma_load_4d(sV8 + vs * L::k8, &map_v, 0, 0, it.head, blk0 + 4 * t, bar(B_V8FULL + vs));
             }
           }
+          if (__shfl_sync(0xffffffffu, *abort_flag, 0)) break;
+        }
+        if (lane == 0 && *abort_flag) {   // copies in flight end before the CTA does
+          const long long begin = clock64();
+          auto ended = [&](int barrier, int phase) {
+            while (!mbar_try_wait(bar(barrier), (unsigned)phase & 1u) && clock64() - begin < kWaitCycles / 16) {
+            }
+          };
+          for (int t = max(0, n - kKStages); t < n; ++t) ended(B_KFULL + t % kKStages, t / kKStages);
+          for (int t = max(0, n - kV8Stages); t < n; ++t) ended(B_V8FULL + t % kV8Stages, t / kV8Stages);
+          ended(B_RFULL, items);          // (where this item's was not issued, the wait runs out)
         }
       }
     } else if (warp == 1) {
       // ------------------------------------------------------------------ MMA issuer
-      if (lane == 0 && work) {
+      if (work) {
+        const unsigned leader = lane == 0;
         // Two walks over the same tiles: the scores run two tiles ahead of the products with V.  The scores buffer of
         // tile n is that of tile n - 2, whose weights the product issued just before has read: the tensor pipe runs
         // this thread's instructions in order.
@@ -229,14 +266,14 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
           const unsigned q = tmem_base + kQCol + qb * 64;
 #pragma unroll
           for (int k = 0; k < DH / 32; ++k) {
-            umma_qk<DH>(d, q + k * 8, k_lo + 2 * k, k ? 1u : 0u);
-            umma_qk<DH>(d, q + L::q_cols / 2 + k * 8, k_lo + 2 * k, 1u);
+            umma_qk<DH>(d, q + k * 8, k_lo + 2 * k, k ? 1u : 0u, leader);
+            umma_qk<DH>(d, q + L::q_cols / 2 + k * 8, k_lo + 2 * k, 1u, leader);
           }
-          umma_commit(bar(B_SFULL + (ns & 1)));
-          umma_commit(bar(B_KEMPTY + ns % kKStages));
+          umma_commit_if(bar(B_SFULL + (ns & 1)), leader);
+          umma_commit_if(bar(B_KEMPTY + ns % kKStages), leader);
           ++ns;
           if (++ts == is.b1 - is.b0) {
-            umma_commit(bar(B_QEMPTY + qb));
+            umma_commit_if(bar(B_QEMPTY + qb), leader);
             ts = 0;
             ++items_s;
             more = ws.next<KT>(p, kTcItemCost, is);
@@ -254,9 +291,9 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const unsigned v_lo = desc_lo(sV16 + vs * L::v16, KT * 128), a = tmem_base + (n & 1) * 128;
 #pragma unroll
-            for (int j = 0; j < KT / 16; ++j) umma_pv<DH>(tmem_base + kOCol, a + j * 8, v_lo + j * (2048 >> 4), (t || j) ? 1u : 0u);
-            umma_commit(bar(B_OFULL));
-            umma_commit(bar(B_VEMPTY + vs));
+            for (int j = 0; j < KT / 16; ++j) umma_pv<DH>(tmem_base + kOCol, a + j * 8, v_lo + j * (2048 >> 4), (t || j) ? 1u : 0u, leader);
+            umma_commit_if(bar(B_OFULL + (n & 1)), leader);
+            umma_commit_if(bar(B_VEMPTY + vs), leader);
             scores();
           }
           ++items;
@@ -265,7 +302,7 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
     }
   } else if (group == 3) {
     // ------------------------------------------------------------------ V: codes -> fp16 B operand; Q -> tensor memory
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
     constexpr int LPK = DH / 16;                             // lanes per key, 16 dims each
     const int c = (int)threadIdx.x & 127;
     const int j = c % LPK;
@@ -275,15 +312,15 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
       for (LineWalk w(share); w.next<KT>(p, kTcItemCost, it); ++items) {
         {   // query row c: 2 e4m3 values per element, four elements of a kind per column
           const int qb = items & 1;
+          mbar_wait(bar(B_RFULL), (unsigned)items & 1u, abort_flag);
           mbar_wait(bar(B_QEMPTY + qb), (unsigned)((items >> 1) & 1) ^ 1u, abort_flag);
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           const bool valid = c < it.nrows;
-          const bf16* src = p.q + (size_t)(it.t0 + (valid ? c / G : 0)) * p.q_ld + (it.head * G + (valid ? c % G : 0)) * DH;
-          auto load = [&](int i) { return valid ? __ldcg(reinterpret_cast<const uint4*>(src) + i) : make_uint4(0, 0, 0, 0); };
-          float top = 0.f;                 // (two passes over the row: the second finds it in L2)
+          const unsigned src = smem0 + L::q + c * L::q_row;
+          float top = 0.f;
 #pragma unroll
           for (int i = 0; i < DH / 8; ++i) {
-            const uint4 raw = load(i);
+            const uint4 raw = lds128(src + i * 16);
             const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&raw);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
@@ -291,28 +328,31 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
               top = fmaxf(top, fmaxf(fabsf(y.x), fabsf(y.y)));
             }
           }
+          if (!valid) top = 0.f;
           const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 100);
-          const float up = pow2i(7 - e);
-          s_sc[qb][c] = pow2i(e - 7) * (1.4426950408889634f * rsqrtf((float)DH));
+          const float up = valid ? pow2i(7 - e) : 0.f;
+          s_sc[items & 3][c] = pow2i(e - 7) * (1.4426950408889634f * rsqrtf((float)DH));
           const unsigned dst = tmem_base + ((unsigned)(c & 96) << 16) + kQCol + qb * 64;
 #pragma unroll 1
           for (int i = 0; i < DH / 32; ++i) {
-            uint4 raw[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) raw[k] = load(i * 4 + k);
             unsigned hi[8], lo[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-              const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&raw[k >> 1]) + (k & 1) * 2;
               hi[k] = lo[k] = 0u;
+            }
 #pragma unroll
-              for (int m = 0; m < 2; ++m) {
+            for (int k = 0; k < 4; ++k) {
+              uint4 raw = lds128(src + (i * 4 + k) * 16);
+              if (!valid) raw = make_uint4(0, 0, 0, 0);      // (what was there before may be anything)
+              const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&raw);
+#pragma unroll
+              for (int m = 0; m < 4; ++m) {
                 const float2 y = __bfloat1622float2(h[m]);
                 const float a = y.x * up, b = y.y * up;
                 const unsigned near = kv8_encode2(a, b), back = kv8_decode2((unsigned short)near);
                 const float2 z = __half22float2(*reinterpret_cast<const __half2*>(&back));
-                hi[k] |= near << (16 * m);
-                lo[k] |= kv8_encode2(a - z.x, b - z.y) << (16 * m);
+                hi[2 * k + (m >> 1)] |= near << (16 * (m & 1));
+                lo[2 * k + (m >> 1)] |= kv8_encode2(a - z.x, b - z.y) << (16 * (m & 1));
               }
             }
             tmem_st8(dst + i * 8, hi);
@@ -321,7 +361,11 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
           tmem_st_wait();
           asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
           __syncwarp();
-          if (lane == 0) mbar_arrive(bar(B_QFULL + qb));
+          if (lane == 0) {
+            mbar_arrive(bar(B_REMPTY));
+            mbar_arrive(bar(B_QFULL + qb));
+            mbar_arrive(bar(B_CFULL + (items & 3)));
+          }
         }
         for (int t = it.b0; t < it.b1; ++t, ++n) {
           const int a = n % kV8Stages, b = n % kV16Stages;
@@ -329,7 +373,7 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
           mbar_wait(bar(B_VEMPTY + b), (unsigned)((n / kV16Stages) & 1) ^ 1u, abort_flag);
           const int left = it.vis - t * KT;
           const unsigned src = sV8 + a * L::k8 + c * 16, dst = sV16 + b * L::v16 + (j >> 2) * (KT * 128);
-#pragma unroll
+#pragma unroll 4
           for (int i = 0; i < DH / 16; ++i) {
             const int key = i * (128 / LPK) + c / LPK;
             uint4 x = lds128(src + i * 2048);
@@ -355,89 +399,87 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
         }
       }
   } else {
-    // ------------------------------------------------------------------ softmax: half of a query row's keys per thread
-    // (on a timeout nobody leaves the loops: the two warps of a pair meet at the same barriers to the end)
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
-    const int half = group - 1, quad = warp & 3, r = quad * 32 + lane, pair = quad + 1;
-    const unsigned t_lane = tmem_base + ((unsigned)(quad * 32) << 16);
-    const unsigned t_out = t_lane + kOCol + half * (DH / 2);
-    int n = 0, items = 0;
-    bool ok = true;
+    // ------------------------------------------------------------------ softmax: one query row per thread
+    // (On a timeout nobody leaves the loops: the two warps of the same rows meet at the same barriers to the end.)
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 152;");
+    const int me = group - 1, quad = warp & 3, r = quad * 32 + lane;
+    const int my_turn = 1 + 2 * quad + me, your_turn = 1 + 2 * quad + (me ^ 1);
+    const unsigned t_lane = tmem_base + ((unsigned)(quad * 32) << 16), t_s = t_lane + me * 128, t_out = t_lane + kOCol;
+    int n = 0, items = 0;                  // n: number of the item's first tile; group `me` takes the tiles of its parity
+    unsigned lphase = 0;                   // phases of B_LFULL, which only items of two tiles and more use
     LineItem it;
-    if (work)
+    if (work) {
+      if (me == 1) turn_pass(your_turn);
       for (LineWalk w(share); w.next<KT>(p, kTcItemCost, it); ++items) {
         const bool warp_has_rows = quad * 32 < it.nrows;
+        const int end = n + it.b1 - it.b0;
+        const int start = n + ((n ^ me) & 1);
+        const size_t scale0 = ((size_t)it.block0 + 4 * it.b0) * p.hkv + it.head;
+        const int scales_left = (int)min(p.c.n_blocks - it.block0 - 4ll * it.b0, 0x7fffffffll);   // (a tile may reach over the end)
         float ref = -INFINITY, sum = 0.f, sc = 0.f;
-        float ksn[2], vsn[2];
+        // The tile's four pairs of scales: lane l looks after block l % 4, one tile ahead.
+        float ksn = 1.f, vsn = 1.f;
         auto load_scales = [&](int t) {
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const long long blk = min((long long)it.block0 + 4 * t + 2 * half + i, p.c.n_blocks - 1);   // (a tile may reach over the end)
-            ksn[i] = __ldcg(p.c.k_scale + blk * p.hkv + it.head);
-            vsn[i] = __ldcg(p.c.v_scale + blk * p.hkv + it.head);
-          }
+          const size_t at = scale0 + (size_t)min(4 * t + (lane & 3), scales_left - 1) * p.hkv;
+          ksn = __ldcg(p.c.k_scale + at);
+          vsn = __ldcg(p.c.v_scale + at);
         };
-        load_scales(it.b0);
-        for (int t = it.b0; t < it.b1; ++t, ++n) {
-          const int s = n & 1;
-          float f[2], lv[2], inv[2];
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const float vs = kv8_clamp_scale(vsn[i]);
-            f[i] = kv8_clamp_scale(ksn[i]);
-            lv[i] = log2_fast(vs);
-            inv[i] = 1.0f / vs;
+        if (start < end) load_scales(start - n);
+        for (int t = start; t < end; t += 2) {
+          const float f = kv8_clamp_scale(ksn), lv = log2_fast(kv8_clamp_scale(vsn));
+          if (t + 2 < end) load_scales(t + 2 - n);
+          const int left = it.vis - (it.b0 + t - n) * KT;     // keys of this tile that the row sees
+          if (t == start) {
+            mbar_wait(bar(B_CFULL + (items & 3)), (unsigned)(items >> 2) & 1u, abort_flag);
+            sc = s_sc[items & 3][r];
           }
-          if (t + 1 < it.b1) load_scales(t + 1);
-          const int left = it.vis - t * KT - half * 64;      // keys of this thread's half that the row sees
-          ok = mbar_wait(bar(B_SFULL + s), (unsigned)(n >> 1) & 1u, abort_flag) && ok;
+          mbar_wait(bar(B_SFULL + me), (unsigned)(t >> 1) & 1u, abort_flag);
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          if (t == it.b0) {
-            ok = mbar_wait(bar(B_QFULL + (items & 1)), (unsigned)(items >> 1) & 1u, abort_flag) && ok;
-            sc = s_sc[items & 1][r];
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(B_QEMPTY + (items & 1)));
-          }
-          if (warp_has_rows) {
-            f[0] *= sc;
-            f[1] *= sc;
-            unsigned raw[64];
-            tmem_ld32_nowait(t_lane + s * 128 + half * 64, raw);
-            tmem_ld32_nowait(t_lane + s * 128 + half * 64 + 32, raw + 32);
-            tmem_ld_wait();
-            if (left < 64) {
+          // (The loops over 32 scores are kept rolled: unrolled, four roles' straight-line code does not fit the
+          // instruction caches.  The next 32 are loaded while these are worked on.)
+          auto mask = [&](unsigned* x, int first) {
+            if (left < first + 32) {
 #pragma unroll
-              for (int j = 0; j < 64; ++j) raw[j] = j < left ? raw[j] : 0xff800000u;      // -inf
+              for (int j = 0; j < 32; ++j) x[j] = first + j < left ? x[j] : 0xff800000u;      // -inf
             }
-            float top = -INFINITY;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
+          };
+          float top = -INFINITY;
+          if (warp_has_rows) {
+            unsigned ra[32], rb[32];
+            auto largest = [&](unsigned* x, int i) {
+              mask(x, i * 32);
               float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-              for (int j = 0; j < 32; ++j) m4[j & 3] = fmaxf(m4[j & 3], __uint_as_float(raw[i * 32 + j]));
-              top = fmaxf(top, fmaf(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])), f[i], lv[i]));
-            }
-            // from here on the scores of both halves are in registers: the buffer may be overwritten
-            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-            const bool grow = pair_any(pair, top > ref + kTcGrow);
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            if (grow) {
-              s_pair[half][r] = top;
-              pair_sync(pair);
-              top = fmaxf(top, s_pair[half ^ 1][r]);
-              pair_sync(pair);
-              float turn = 1.f;
-              if (top > ref + kTcGrow) {
-                turn = exp2_fast(ref - (top - kTcBias));     // 2^-inf = 0 on the first tile
-                ref = top - kTcBias;
-                sum *= turn;
-              }
-              if (t > it.b0) {
-                // the product of the tile before has to be done with the output
-                ok = mbar_wait(bar(B_OFULL), (unsigned)(n - 1) & 1u, abort_flag) && ok;
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+              for (int j = 0; j < 32; ++j) m4[j & 3] = fmaxf(m4[j & 3], __uint_as_float(x[j]));
+              const float fi = __shfl_sync(0xffffffffu, f, i) * sc, li = __shfl_sync(0xffffffffu, lv, i);
+              top = fmaxf(top, fmaf(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])), fi, li));
+            };
+            tmem_ld32_nowait(t_s, ra);
 #pragma unroll 1
-                for (int c = 0; c < DH / 64; ++c) {
+            for (int i = 0; i < 4; i += 2) {
+              tmem_ld_wait();
+              tmem_ld32_nowait(t_s + i * 32 + 32, rb);
+              largest(ra, i);
+              tmem_ld_wait();
+              if (i == 0) tmem_ld32_nowait(t_s + 64, ra);
+              largest(rb, i + 1);
+            }
+          }
+          // ---- the reference, after the tile before has settled it ----
+          turn_wait(my_turn);
+          if (warp_has_rows) {
+            const float old = t == n ? -INFINITY : s_ref[r];
+            const bool grow = top > old + kTcGrow;
+            const float now = grow ? top - kTcBias : old;
+            if (__any_sync(0xffffffffu, grow)) {
+              s_ref[r] = now;
+              if (t > n) {
+                // the product of the tile before has to be done with the output
+                mbar_wait(bar(B_OFULL + ((t - 1) & 1)), (unsigned)((t - 1) >> 1) & 1u, abort_flag);
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const float turn = grow ? exp2_fast(old - now) : 1.f;
+#pragma unroll 1
+                for (int c = 0; c < DH / 32; ++c) {
                   unsigned o[32];
                   tmem_ld32_nowait(t_out + c * 32, o);
                   tmem_ld_wait();
@@ -446,76 +488,113 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
                   tmem_st32(t_out + c * 32, o);
                 }
                 tmem_st_wait();
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
               }
+            } else if (t == n) {
+              s_ref[r] = now;
             }
-            unsigned out[32];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const float shift = lv[i] - ref;
+            if (now != ref) {
+              sum = ref > -INFINITY ? sum * exp2_fast(ref - now) : sum;      // (a row of NaN keeps its NaN)
+              ref = now;
+            }
+          }
+          __syncwarp();
+          turn_pass(your_turn);
+          if (warp_has_rows) {
+            unsigned ra[32], rb[32];
+            // 32 weights; they go over columns that were read before
+            auto weights = [&](unsigned* x, int i) {
+              mask(x, i * 32);
+              const float fi = __shfl_sync(0xffffffffu, f, i) * sc, li = __shfl_sync(0xffffffffu, lv, i), shift = li - ref;
+              unsigned out[16];
               float a4[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
               for (int j = 0; j < 32; j += 2) {
-                float e0 = exp2_fast(fmaf(__uint_as_float(raw[i * 32 + j]), f[i], shift));
-                float e1 = exp2_fast(fmaf(__uint_as_float(raw[i * 32 + j + 1]), f[i], shift));
+                const float e0 = exp2_fast(fmaf(__uint_as_float(x[j]), fi, shift));
+                const float e1 = exp2_fast(fmaf(__uint_as_float(x[j + 1]), fi, shift));
                 a4[(j >> 1) & 3] += e0 + e1;
                 const __half2 h = __floats2half2_rn(e0, e1);
-                out[i * 16 + (j >> 1)] = *reinterpret_cast<const unsigned*>(&h);
+                out[j >> 1] = *reinterpret_cast<const unsigned*>(&h);
               }
-              sum = fmaf((a4[0] + a4[1]) + (a4[2] + a4[3]), inv[i], sum);
+              sum = fmaf((a4[0] + a4[1]) + (a4[2] + a4[3]), exp2_fast(-li), sum);      // 2^-lv: the inverse of the V scale
+              tmem_st16(t_s + i * 16, out);
+            };
+            tmem_ld32_nowait(t_s, ra);
+#pragma unroll 1
+            for (int i = 0; i < 4; i += 2) {
+              tmem_ld_wait();
+              tmem_ld32_nowait(t_s + i * 32 + 32, rb);
+              weights(ra, i);
+              tmem_ld_wait();
+              if (i == 0) tmem_ld32_nowait(t_s + 64, ra);
+              weights(rb, i + 1);
             }
-            tmem_st32(t_lane + s * 128 + half * 32, out);
             tmem_st_wait();
           }
           asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+          if (t == end - 2) s_part[items & 1][r] = make_float2(ref, sum);      // the other group writes the item
           __syncwarp();
-          if (lane == 0) mbar_arrive(bar(B_PFULL + s));
+          if (lane == 0) {
+            mbar_arrive(bar(B_PFULL + me));
+            if (t == end - 2) mbar_arrive(bar(B_LFULL + (items & 1)));
+          }
         }
-        // ---- output: half of the dims per thread ----
-        // The item's last product; one tile at a time, for a parity cannot tell a phase from the one two before.  (Warps
-        // without query rows wait too: they would otherwise report the next item before the others have this one.)
-        if (n > 1) ok = mbar_wait(bar(B_OFULL), (unsigned)(n - 2) & 1u, abort_flag) && ok;
-        ok = mbar_wait(bar(B_OFULL), (unsigned)(n - 1) & 1u, abort_flag) && ok;
-        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        if (warp_has_rows) {
-          s_pair[half][r] = sum;
-          pair_sync(pair);
-          const float total = sum + s_pair[half ^ 1][r];
-          pair_sync(pair);
-          const bool valid = r < it.nrows && ok;
-          const int rr = r < it.nrows ? r : 0;
-          const bool whole = it.b0 == 0 && it.b1 == it.nb;
-          const size_t slot = 2 * (size_t)blockIdx.x + (it.opens ? 0 : 1);
-          bf16* dst = p.out + ((size_t)(it.t0 + rr / G) * p.hq + it.head * G + rr % G) * DH + half * (DH / 2);
-          float* part = p.part_o + (slot * 128 + rr) * DH + half * (DH / 2);
-          const float inv = 1.0f / total;
-          if (!whole && valid && half == 0) p.part_ml[slot * 128 + rr] = make_float2(ref, total);
+        // ---- output, by the group that took the last tile ----
+        if (((end - 1) & 1) == me) {
+          // (Warps without query rows wait for the item's last product too: they would otherwise report the next item
+          // before the others have this one.)
+          const bool ok = mbar_wait(bar(B_OFULL + ((end - 1) & 1)), (unsigned)((end - 1) >> 1) & 1u, abort_flag);
+          if (end - n > 1) {
+            mbar_wait(bar(B_LFULL + (items & 1)), (unsigned)(lphase >> (items & 1)) & 1u, abort_flag);
+            lphase ^= 1u << (items & 1);
+          }
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          if (warp_has_rows) {
+            float total = sum;
+            if (end - n > 1) {
+              const float2 o = s_part[items & 1][r];
+              total += o.x > -INFINITY ? o.y * exp2_fast(o.x - ref) : o.y;
+            }
+            const bool valid = r < it.nrows && ok;
+            const int rr = r < it.nrows ? r : 0;
+            const bool whole = it.b0 == 0 && it.b1 == it.nb;
+            const size_t slot = 2 * (size_t)blockIdx.x + (it.opens ? 0 : 1);
+            bf16* dst = p.out + ((size_t)(it.t0 + rr / G) * p.hq + it.head * G + rr % G) * DH;
+            float* part = p.part_o + (slot * 128 + rr) * DH;
+            const float inv = 1.0f / total;
+            if (!whole && valid) p.part_ml[slot * 128 + rr] = make_float2(ref, total);
 #pragma unroll 1
-          for (int c = 0; c < DH / 64; ++c) {
-            unsigned o[32];
-            tmem_ld32_nowait(t_out + c * 32, o);
-            tmem_ld_wait();
-            if (!valid) continue;
-            if (!whole) {
+            for (int c = 0; c < DH / 32; ++c) {
+              unsigned o[32];
+              tmem_ld32_nowait(t_out + c * 32, o);
+              tmem_ld_wait();
+              if (!valid) continue;
+              if (!whole) {
 #pragma unroll
-              for (int g = 0; g < 8; ++g)
-                *reinterpret_cast<uint4*>(part + c * 32 + g * 4) = make_uint4(o[g * 4], o[g * 4 + 1], o[g * 4 + 2], o[g * 4 + 3]);
-            } else {
+                for (int g = 0; g < 8; ++g)
+                  *reinterpret_cast<uint4*>(part + c * 32 + g * 4) = make_uint4(o[g * 4], o[g * 4 + 1], o[g * 4 + 2], o[g * 4 + 3]);
+              } else {
 #pragma unroll
-              for (int g = 0; g < 4; ++g) {
-                uint4 v;
-                __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&v);
+                for (int g = 0; g < 4; ++g) {
+                  uint4 v;
+                  __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&v);
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                  h[j] = __floats2bfloat162_rn(__uint_as_float(o[g * 8 + 2 * j]) * inv, __uint_as_float(o[g * 8 + 2 * j + 1]) * inv);
-                *reinterpret_cast<uint4*>(dst + c * 32 + g * 8) = v;
+                  for (int j = 0; j < 4; ++j)
+                    h[j] = __floats2bfloat162_rn(__uint_as_float(o[g * 8 + 2 * j]) * inv, __uint_as_float(o[g * 8 + 2 * j + 1]) * inv);
+                  *reinterpret_cast<uint4*>(dst + c * 32 + g * 8) = v;
+                }
               }
             }
           }
+          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(B_OEMPTY));
+        } else if (end - n > 1) {
+          lphase ^= 1u << (items & 1);
         }
-        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(B_OEMPTY));
+        n = end;
       }
+    }
   }
 
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -523,7 +602,7 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
   if (s_abort && threadIdx.x == 0 && p.error_flag) atomicMax(p.error_flag, 1);
   if (warp == 1) {
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512u) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base_slot), "r"(512u) : "memory");
   }
 }
 
