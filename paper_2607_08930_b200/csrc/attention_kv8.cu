@@ -119,14 +119,9 @@ __global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(c
   pdl_wait();
   pdl_trigger();
 
-  LineShare share;
-  line_share<kStreamThreads, L::groups, kKv8Block, DH>(p, kCost, W, s_line, wk, share);
+  line_share<kStreamThreads, L::groups, kKv8Block, DH>(p, kCost, W, s_line);
   const size_t me = (size_t)blockIdx.x * L::groups + wk;
-  if (share.u0 == share.u1) {
-    if (wtid == 0) p.cuts[me].nrows = 0;
-    return;                                // (from here on only the worker's own threads wait for one another)
-  }
-  if (wtid == 0) line_cut<kKv8Block>(p, kCost, share, (int)me);
+  if (s_line.share[wk].units == 0) return;   // (from here on only the worker's own threads wait for one another)
 
   // this warp's ring, and this lane's part of a block's copy: 16 bytes i * 512 + lane * 16 of K and of V
   const unsigned ring = tc::smem_u32(smem) + (unsigned)warp * STAGES * 2 * TB;
@@ -147,7 +142,9 @@ __global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(c
     }
   };
 
-  for (LineWalk walk(share); walk.next<kKv8Block>(p, kCost, it);) {
+  LineWalk walk;
+  walk.begin<kKv8Block>(p, s_line.share[wk]);
+  while (walk.next<kKv8Block>(p, kCost, it)) {
     const int b0 = it.b0, b1 = it.b1, head = it.head, t0 = it.t0, nrows = it.nrows;
     sync_worker();                       // the previous segment's fragments, sums and outputs are no longer read
 #pragma unroll

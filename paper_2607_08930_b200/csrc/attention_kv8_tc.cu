@@ -11,8 +11,7 @@
 //                 of two e4m3 values - the nearest one and the rest (4 + 4 significant bits, bf16 has 8: exact above
 //                 2^-10 of the row's largest element, within 2^-17 of that element below) - so S is two products at
 //                 twice the rate of one in fp16, and K is neither converted nor stored a second time.  Q is an operand
-//                 from tensor memory (two buffers): read from shared memory it would take half of that memory's
-//                 bandwidth, which is what the products of a 128 x 128 tile are bound by.
+//                 from tensor memory: read from shared memory it would take half of that memory's bandwidth.
 //   2 x 4 warps   softmax, a query row per thread: one group takes the even tiles, the other the odd ones, each with a
 //                 scores buffer of its own, so that the exponentials of one run under the loads, maxima and stores of
 //                 the other.  The weights w = 2^(t - M) go back to tensor memory as fp16, over the first half of their
@@ -40,8 +39,9 @@ using namespace tc;
 constexpr int KT = 128;                              // keys per tile: four cache blocks
 constexpr int kTcThreads = 512;
 constexpr int kKStages = 4, kV8Stages = 3, kV16Stages = 2;
+constexpr int kScaleStages = 8;                      // tiles whose scales are held; no ring runs that far ahead
 constexpr int kQPad = 16;                            // bytes between query rows in shared memory: every lane its own banks
-constexpr float kTcBias = 6.f, kTcGrow = 14.f;       // weights reach 2^14 at most, 2^6 when the reference is set
+constexpr float kTcBias = 2.f, kTcGrow = 15.f;       // weights reach 2^15 at most, 2^2 when the reference is set
 constexpr int kTcItemCost = 1;                       // tiles that an item counts beyond its own
 constexpr unsigned kOCol = 256, kQCol = 384;         // tensor memory: two scores buffers, output, two query buffers
 
@@ -114,13 +114,13 @@ __device__ __forceinline__ void tmem_st8(unsigned taddr, const unsigned* w) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
                ::"r"(taddr), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
 }
-__device__ __forceinline__ void tmem_st16(unsigned taddr, const unsigned* w) {
+__device__ __forceinline__ void tmem_ld16_nowait(unsigned taddr, unsigned* r) {
   asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
-      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
-      ::"r"(taddr), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]), "r"(w[8]),
-        "r"(w[9]), "r"(w[10]), "r"(w[11]), "r"(w[12]), "r"(w[13]), "r"(w[14]), "r"(w[15])
-      : "memory");
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr));
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ uint4 lds128(unsigned at) {
@@ -143,13 +143,14 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
   using L = TcLayout<DH>;
   enum { B_KFULL = 0, B_KEMPTY = B_KFULL + kKStages, B_V8FULL = B_KEMPTY + kKStages, B_V8EMPTY = B_V8FULL + kV8Stages,
          B_VFULL = B_V8EMPTY + kV8Stages, B_VEMPTY = B_VFULL + kV16Stages, B_SFULL = B_VEMPTY + kV16Stages,
-         B_PFULL = B_SFULL + 2, B_QFULL = B_PFULL + 2, B_QEMPTY = B_QFULL + 2, B_CFULL = B_QEMPTY + 2,
-         B_LFULL = B_CFULL + 4, B_OFULL = B_LFULL + 2, B_OEMPTY = B_OFULL + 2, B_RFULL = B_OEMPTY + 1,
+         B_PFULL = B_SFULL + 2, B_OFULL = B_PFULL + 2, B_LFULL = B_OFULL + 2, B_CFULL = B_LFULL + 2, B_TFULL = B_CFULL + 4,
+         B_QFULL = B_TFULL + kScaleStages, B_QEMPTY = B_QFULL + 2, B_OEMPTY = B_QEMPTY + 2, B_RFULL = B_OEMPTY + 1,
          B_REMPTY = B_RFULL + 1, B_COUNT = B_REMPTY + 1 };
   extern __shared__ unsigned char smem_dyn[];
   __shared__ __align__(8) unsigned long long bars[B_COUNT];
   __shared__ unsigned tmem_base_slot;
   __shared__ int s_abort;
+  __shared__ float2 s_scale[kScaleStages][4];        // (K scale, log2 of the V scale) of a tile's blocks
   __shared__ float s_sc[4][128];                     // score scale of every query row, by item
   __shared__ float s_ref[128];                       // reference of every query row
   __shared__ float2 s_part[2][128];                  // (reference, sum) of the group that does not write the item, by item parity
@@ -165,12 +166,15 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
     for (int i = 0; i < kV8Stages; ++i) { mbar_init(bar(B_V8FULL + i), 1); mbar_init(bar(B_V8EMPTY + i), 4); }
     for (int i = 0; i < kV16Stages; ++i) { mbar_init(bar(B_VFULL + i), 4); mbar_init(bar(B_VEMPTY + i), 1); }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(bar(B_SFULL + i), 1); mbar_init(bar(B_PFULL + i), 4);
-      mbar_init(bar(B_QFULL + i), 4); mbar_init(bar(B_QEMPTY + i), 1);
-      mbar_init(bar(B_LFULL + i), 4);
+      mbar_init(bar(B_SFULL + i), 1);
+      mbar_init(bar(B_PFULL + i), 4);
       mbar_init(bar(B_OFULL + i), 1);
+      mbar_init(bar(B_LFULL + i), 4);
+      mbar_init(bar(B_QFULL + i), 4);
+      mbar_init(bar(B_QEMPTY + i), 1);
     }
     for (int i = 0; i < 4; ++i) mbar_init(bar(B_CFULL + i), 4);
+    for (int i = 0; i < kScaleStages; ++i) mbar_init(bar(B_TFULL + i), 1);
     mbar_init(bar(B_OEMPTY), 4);
     mbar_init(bar(B_RFULL), 1);
     mbar_init(bar(B_REMPTY), 4);
@@ -187,18 +191,16 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
   pdl_trigger();
 
   // ---- this CTA's share of the line ----
-  LineShare share;
-  line_share<kTcThreads, 1, KT, DH>(p, kTcItemCost, 1, s_line, 0, share);
+  line_share<kTcThreads, 1, KT, DH>(p, kTcItemCost, 1, s_line);
+  const LineShare share = s_line.share[0];
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   constexpr unsigned tmem_base = 0;                  // the only place an allocation of all 512 columns can have
   volatile int* abort_flag = &s_abort;
   const int G = p.hq / p.hkv;
-  const bool work = share.u0 < share.u1;
+  const bool work = share.units > 0;
   if (threadIdx.x == 0 && tmem_base_slot != 0) s_abort = 1;
-  if (work && threadIdx.x == 0) line_cut<KT>(p, kTcItemCost, share, (int)blockIdx.x);
-  if (!work && threadIdx.x == 0) p.cuts[blockIdx.x].nrows = 0;
 
   // 4 x 128 registers a thread at launch become 104 + 2 x 152 + 104.
   const int group = warp >> 2;
@@ -209,7 +211,9 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
       if (work) {
         int n = 0, items = 0;
         LineItem it;
-        for (LineWalk w(share); w.next<KT>(p, kTcItemCost, it); ++items) {
+        LineWalk w;
+        w.begin<KT>(p, share);
+        for (; w.next<KT>(p, kTcItemCost, it); ++items) {
           // (one lane's word counts for the warp: it stays together)
           if (!__shfl_sync(0xffffffffu, lane > 0 || mbar_wait(bar(B_REMPTY), (unsigned)(items & 1) ^ 1u, abort_flag), 0)) break;
           if (lane == 0) mbar_expect_tx(bar(B_RFULL), (unsigned)(it.nrows * DH * 2));
@@ -218,17 +222,28 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
             bulk_load(smem0 + L::q + f * L::q_row, p.q + (size_t)(it.t0 + f / G) * p.q_ld + (it.head * G + f % G) * DH, DH * 2,
                       bar(B_RFULL));
           __syncwarp();
-          if (lane == 0) {
-            const int blk0 = it.block0 + it.b0 * (KT / kKv8Block);
-            for (int t = 0; t < it.b1 - it.b0; ++t, ++n) {
+          const int blk0 = it.block0 + it.b0 * (KT / kKv8Block);
+          for (int t = 0; t < it.b1 - it.b0; ++t, ++n) {
+            // lanes 0 .. 3: the scales of the tile's blocks (which may reach over the cache's end)
+            const size_t at = (size_t)min((long long)blk0 + 4 * t + (lane & 3), p.c.n_blocks - 1) * p.hkv + it.head;
+            const float ks8 = __ldcg(p.c.k_scale + at), vs8 = __ldcg(p.c.v_scale + at);
+            bool ok = true;
+            if (lane == 0) {
               const int ks = n % kKStages, vs = n % kV8Stages;
-              if (!mbar_wait(bar(B_KEMPTY + ks), (unsigned)((n / kKStages) & 1) ^ 1u, abort_flag)) break;
-              if (!mbar_wait(bar(B_V8EMPTY + vs), (unsigned)((n / kV8Stages) & 1) ^ 1u, abort_flag)) break;
-              mbar_expect_tx(bar(B_KFULL + ks), (unsigned)L::k8);
-              tma_load_4d(sK + ks * L::k8, &map_k, 0, 0, it.head, blk0 + 4 * t, bar(B_KFULL + ks));
-              mbar_expect_tx(bar(B_V8FULL + vs), (unsigned)L::k8);
-              tma_load_4d(sV8 + vs * L::k8, &map_v, 0, 0, it.head, blk0 + 4 * t, bar(B_V8FULL + vs));
+              ok = mbar_wait(bar(B_KEMPTY + ks), (unsigned)((n / kKStages) & 1) ^ 1u, abort_flag) &&
+                   mbar_wait(bar(B_V8EMPTY + vs), (unsigned)((n / kV8Stages) & 1) ^ 1u, abort_flag);
+              if (ok) {
+                mbar_expect_tx(bar(B_KFULL + ks), (unsigned)L::k8);
+                tma_load_4d(sK + ks * L::k8, &map_k, 0, 0, it.head, blk0 + 4 * t, bar(B_KFULL + ks));
+                mbar_expect_tx(bar(B_V8FULL + vs), (unsigned)L::k8);
+                tma_load_4d(sV8 + vs * L::k8, &map_v, 0, 0, it.head, blk0 + 4 * t, bar(B_V8FULL + vs));
+              }
             }
+            if (!__shfl_sync(0xffffffffu, ok, 0)) break;
+            // (the entry's tile before, eight back, is long done with: K's ring lets this one pass only behind its scores)
+            if (lane < 4) s_scale[n % kScaleStages][lane] = make_float2(kv8_clamp_scale(ks8), log2_fast(kv8_clamp_scale(vs8)));
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(B_TFULL + n % kScaleStages));
           }
           if (__shfl_sync(0xffffffffu, *abort_flag, 0)) break;
         }
@@ -250,15 +265,16 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
         // Two walks over the same tiles: the scores run two tiles ahead of the products with V.  The scores buffer of
         // tile n is that of tile n - 2, whose weights the product issued just before has read: the tensor pipe runs
         // this thread's instructions in order.
-        LineWalk ws(share), wv(share);
+        LineWalk ws, wv;
+        ws.begin<KT>(p, share);
+        wv = ws;
         LineItem is, iv;
         int ns = 0, ts = 0, items_s = 0;         // next scores: tile number, tile within the item, item number
         bool more = ws.next<KT>(p, kTcItemCost, is);
         auto scores = [&]() {
           if (!more) return;
-          bool ok = true;
           const int qb = items_s & 1;
-          if (ts == 0) ok = mbar_wait(bar(B_QFULL + qb), (unsigned)(items_s >> 1) & 1u, abort_flag);
+          bool ok = ts > 0 || mbar_wait(bar(B_QFULL + qb), (unsigned)(items_s >> 1) & 1u, abort_flag);
           if (ok) ok = mbar_wait(bar(B_KFULL + ns % kKStages), (unsigned)(ns / kKStages) & 1u, abort_flag);
           if (!ok) { more = false; return; }
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -308,11 +324,13 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
     const int j = c % LPK;
     int n = 0, items = 0;
     LineItem it;
-    if (work)
-      for (LineWalk w(share); w.next<KT>(p, kTcItemCost, it); ++items) {
+    if (work) {
+      LineWalk w;
+      w.begin<KT>(p, share);
+      for (; w.next<KT>(p, kTcItemCost, it); ++items) {
         {   // query row c: 2 e4m3 values per element, four elements of a kind per column
-          const int qb = items & 1;
           mbar_wait(bar(B_RFULL), (unsigned)items & 1u, abort_flag);
+          const int qb = items & 1;
           mbar_wait(bar(B_QEMPTY + qb), (unsigned)((items >> 1) & 1) ^ 1u, abort_flag);
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           const bool valid = c < it.nrows;
@@ -373,22 +391,27 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
           mbar_wait(bar(B_VEMPTY + b), (unsigned)((n / kV16Stages) & 1) ^ 1u, abort_flag);
           const int left = it.vis - t * KT;
           const unsigned src = sV8 + a * L::k8 + c * 16, dst = sV16 + b * L::v16 + (j >> 2) * (KT * 128);
-#pragma unroll 4
-          for (int i = 0; i < DH / 16; ++i) {
-            const int key = i * (128 / LPK) + c / LPK;
-            uint4 x = lds128(src + i * 2048);
-            if (key >= left) x = make_uint4(0, 0, 0, 0);
-            unsigned y[8];
-            kv8_decode4(x.x, y[0], y[1]);
-            kv8_decode4(x.y, y[2], y[3]);
-            kv8_decode4(x.z, y[4], y[5]);
-            kv8_decode4(x.w, y[6], y[7]);
-            // chunks 2 (j % 4) and + 1 of the key's 128-byte line; with two lines per key, half of a store's eight lanes
-            // take them the other way round, so that the eight fall on different banks
-            const bool flip = DH == 128 && j >= 4;
-            const unsigned line = dst + key * 128, c0 = 2 * (j & 3) + (flip ? 1 : 0), sw = key & 7;
-            sts128(line + ((c0 ^ sw) << 4), y[flip ? 4 : 0], y[flip ? 5 : 1], y[flip ? 6 : 2], y[flip ? 7 : 3]);
-            sts128(line + (((c0 ^ 1) ^ sw) << 4), y[flip ? 0 : 4], y[flip ? 1 : 5], y[flip ? 2 : 6], y[flip ? 3 : 7]);
+#pragma unroll 1
+          for (int i0 = 0; i0 < DH / 16; i0 += 4) {
+            uint4 w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = lds128(src + (i0 + i) * 2048);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int key = (i0 + i) * (128 / LPK) + c / LPK;
+              if (key >= left) w[i] = make_uint4(0, 0, 0, 0);
+              unsigned y[8];
+              kv8_decode4(w[i].x, y[0], y[1]);
+              kv8_decode4(w[i].y, y[2], y[3]);
+              kv8_decode4(w[i].z, y[4], y[5]);
+              kv8_decode4(w[i].w, y[6], y[7]);
+              // chunks 2 (j % 4) and + 1 of the key's 128-byte line; with two lines per key, half of a store's eight lanes
+              // take them the other way round, so that the eight fall on different banks
+              const bool flip = DH == 128 && j >= 4;
+              const unsigned line = dst + key * 128, c0 = 2 * (j & 3) + (flip ? 1 : 0), sw = key & 7;
+              sts128(line + ((c0 ^ sw) << 4), y[flip ? 4 : 0], y[flip ? 5 : 1], y[flip ? 6 : 2], y[flip ? 7 : 3]);
+              sts128(line + (((c0 ^ 1) ^ sw) << 4), y[flip ? 0 : 4], y[flip ? 1 : 5], y[flip ? 2 : 6], y[flip ? 3 : 7]);
+            }
           }
           fence_smem_for_mma();
           __syncwarp();
@@ -398,6 +421,7 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
           }
         }
       }
+    }
   } else {
     // ------------------------------------------------------------------ softmax: one query row per thread
     // (On a timeout nobody leaves the loops: the two warps of the same rows meet at the same barriers to the end.)
@@ -410,59 +434,53 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
     LineItem it;
     if (work) {
       if (me == 1) turn_pass(your_turn);
-      for (LineWalk w(share); w.next<KT>(p, kTcItemCost, it); ++items) {
+      LineWalk w;
+        w.begin<KT>(p, share);
+        for (; w.next<KT>(p, kTcItemCost, it); ++items) {
         const bool warp_has_rows = quad * 32 < it.nrows;
         const int end = n + it.b1 - it.b0;
         const int start = n + ((n ^ me) & 1);
-        const size_t scale0 = ((size_t)it.block0 + 4 * it.b0) * p.hkv + it.head;
-        const int scales_left = (int)min(p.c.n_blocks - it.block0 - 4ll * it.b0, 0x7fffffffll);   // (a tile may reach over the end)
         float ref = -INFINITY, sum = 0.f, sc = 0.f;
-        // The tile's four pairs of scales: lane l looks after block l % 4, one tile ahead.
-        float ksn = 1.f, vsn = 1.f;
-        auto load_scales = [&](int t) {
-          const size_t at = scale0 + (size_t)min(4 * t + (lane & 3), scales_left - 1) * p.hkv;
-          ksn = __ldcg(p.c.k_scale + at);
-          vsn = __ldcg(p.c.v_scale + at);
-        };
-        if (start < end) load_scales(start - n);
         for (int t = start; t < end; t += 2) {
-          const float f = kv8_clamp_scale(ksn), lv = log2_fast(kv8_clamp_scale(vsn));
-          if (t + 2 < end) load_scales(t + 2 - n);
           const int left = it.vis - (it.b0 + t - n) * KT;     // keys of this tile that the row sees
+          const float2* scale = s_scale[t % kScaleStages];
           if (t == start) {
             mbar_wait(bar(B_CFULL + (items & 3)), (unsigned)(items >> 2) & 1u, abort_flag);
             sc = s_sc[items & 3][r];
           }
+          mbar_wait(bar(B_TFULL + t % kScaleStages), (unsigned)(t / kScaleStages) & 1u, abort_flag);
           mbar_wait(bar(B_SFULL + me), (unsigned)(t >> 1) & 1u, abort_flag);
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          // (The loops over 32 scores are kept rolled: unrolled, four roles' straight-line code does not fit the
-          // instruction caches.  The next 32 are loaded while these are worked on.)
+          // (The loops over 16 scores are kept rolled: unrolled, four roles' straight-line code does not fit the
+          // instruction caches - 128 scores unrolled measured 1.5 times the whole kernel's time.  The next 16 are loaded
+          // while these are worked on.)
           auto mask = [&](unsigned* x, int first) {
-            if (left < first + 32) {
+            if (left < first + 16) {
 #pragma unroll
-              for (int j = 0; j < 32; ++j) x[j] = first + j < left ? x[j] : 0xff800000u;      // -inf
+              for (int j = 0; j < 16; ++j) x[j] = first + j < left ? x[j] : 0xff800000u;      // -inf
             }
           };
           float top = -INFINITY;
           if (warp_has_rows) {
-            unsigned ra[32], rb[32];
-            auto largest = [&](unsigned* x, int i) {
-              mask(x, i * 32);
+            unsigned ra[16], rb[16];
+            auto largest = [&](unsigned* x, int first) {
+              mask(x, first);
               float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-              for (int j = 0; j < 32; ++j) m4[j & 3] = fmaxf(m4[j & 3], __uint_as_float(x[j]));
-              const float fi = __shfl_sync(0xffffffffu, f, i) * sc, li = __shfl_sync(0xffffffffu, lv, i);
-              top = fmaxf(top, fmaf(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])), fi, li));
+              for (int j = 0; j < 16; ++j) m4[j & 3] = fmaxf(m4[j & 3], __uint_as_float(x[j]));
+              return fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
             };
-            tmem_ld32_nowait(t_s, ra);
+            tmem_ld16_nowait(t_s, ra);
 #pragma unroll 1
-            for (int i = 0; i < 4; i += 2) {
+            for (int i = 0; i < 4; ++i) {
               tmem_ld_wait();
-              tmem_ld32_nowait(t_s + i * 32 + 32, rb);
-              largest(ra, i);
+              tmem_ld16_nowait(t_s + i * 32 + 16, rb);
+              const float fi = scale[i].x * sc, li = scale[i].y;
+              float m = largest(ra, i * 32);
               tmem_ld_wait();
-              if (i == 0) tmem_ld32_nowait(t_s + 64, ra);
-              largest(rb, i + 1);
+              if (i < 3) tmem_ld16_nowait(t_s + (i + 1) * 32, ra);
+              m = fmaxf(m, largest(rb, i * 32 + 16));
+              top = fmaxf(top, fmaf(m, fi, li));
             }
           }
           // ---- the reference, after the tile before has settled it ----
@@ -500,34 +518,37 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
           }
           __syncwarp();
           turn_pass(your_turn);
+          // ---- weights ----
           if (warp_has_rows) {
-            unsigned ra[32], rb[32];
-            // 32 weights; they go over columns that were read before
-            auto weights = [&](unsigned* x, int i) {
-              mask(x, i * 32);
-              const float fi = __shfl_sync(0xffffffffu, f, i) * sc, li = __shfl_sync(0xffffffffu, lv, i), shift = li - ref;
-              unsigned out[16];
-              float a4[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-              for (int j = 0; j < 32; j += 2) {
-                const float e0 = exp2_fast(fmaf(__uint_as_float(x[j]), fi, shift));
-                const float e1 = exp2_fast(fmaf(__uint_as_float(x[j + 1]), fi, shift));
-                a4[(j >> 1) & 3] += e0 + e1;
-                const __half2 h = __floats2half2_rn(e0, e1);
-                out[j >> 1] = *reinterpret_cast<const unsigned*>(&h);
-              }
-              sum = fmaf((a4[0] + a4[1]) + (a4[2] + a4[3]), exp2_fast(-li), sum);      // 2^-lv: the inverse of the V scale
-              tmem_st16(t_s + i * 16, out);
-            };
-            tmem_ld32_nowait(t_s, ra);
 #pragma unroll 1
-            for (int i = 0; i < 4; i += 2) {
+            for (int h = 0; h < 2; ++h) {                      // 64 scores
+              unsigned out[32];
+              unsigned ra[32], rb[32];
+              tmem_ld32_nowait(t_s + h * 64, ra);
               tmem_ld_wait();
-              tmem_ld32_nowait(t_s + i * 32 + 32, rb);
-              weights(ra, i);
+              tmem_ld32_nowait(t_s + h * 64 + 32, rb);
+              auto weights = [&](unsigned* x, int i, unsigned* w) {
+                const int first = h * 64 + i * 32;
+                const float fi = scale[2 * h + i].x * sc, li = scale[2 * h + i].y, shift = li - ref;
+                if (left < first + 32) {
+#pragma unroll
+                  for (int j = 0; j < 32; ++j) x[j] = first + j < left ? x[j] : 0xff800000u;      // -inf
+                }
+                float a4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int j = 0; j < 32; j += 2) {
+                  const float e0 = exp2_fast(fmaf(__uint_as_float(x[j]), fi, shift));
+                  const float e1 = exp2_fast(fmaf(__uint_as_float(x[j + 1]), fi, shift));
+                  a4[(j >> 1) & 3] += e0 + e1;
+                  const __half2 v = __floats2half2_rn(e0, e1);
+                  w[j >> 1] = *reinterpret_cast<const unsigned*>(&v);
+                }
+                sum = fmaf((a4[0] + a4[1]) + (a4[2] + a4[3]), exp2_fast(-li), sum);      // 2^-lv: the inverse of the V scale
+              };
+              weights(ra, 0, out);
               tmem_ld_wait();
-              if (i == 0) tmem_ld32_nowait(t_s + 64, ra);
-              weights(rb, i + 1);
+              weights(rb, 1, out + 16);
+              tmem_st32(t_s + h * 32, out);                    // (over columns that were read before)
             }
             tmem_st_wait();
           }

@@ -64,90 +64,95 @@ __device__ __forceinline__ bool row_info(const LineParams& p, int r, RowInfo& w)
 __device__ __forceinline__ long long share_start(long long c, long long total, long long n) { return c * total / n; }
 __device__ __forceinline__ int share_of(long long u, long long total, long long n) { return (int)(((u + 1) * n - 1) / total); }
 
+// A worker's share: `units` of the line from unit `at` of the item (row, head, tile) on; 0 units: an idle worker.
+struct LineShare {
+  long long units;
+  int row, head, tile, at;
+};
 template <int THREADS, int GROUPS>
 struct LineShared {
   long long warp[THREADS / 32];
-  long long first[GROUPS];       // units before row[]
-  int row[GROUPS];
-};
-struct LineShare {
-  long long u0, u1;              // this worker's units; empty for idle workers
-  long long first;               // units before `row`
-  long long total, workers;
-  int row;
+  LineShare share[GROUPS];
 };
 
-// The share of worker blockIdx.x * GROUPS + wk, by all THREADS threads of the CTA (GROUPS workers per CTA, at least
-// `least` units beyond the cost per share); also flags rows that do not fit and writes zeros for rows that see nothing.
+// Forms the shares of the CTA's GROUPS workers (by all THREADS threads; at least `least` units beyond the cost each) and
+// writes their cuts down; also flags rows that do not fit and writes zeros for rows that see nothing.  The divisions are
+// all here, in one place: the walk below has none.
 template <int THREADS, int GROUPS, int KEYS, int DH>
-__device__ __forceinline__ void line_share(const LineParams& p, int item_cost, int least, LineShared<THREADS, GROUPS>& s, int wk,
-                                           LineShare& out) {
-  constexpr int kPer = kAttnKv8MaxRows / THREADS;
+__device__ __forceinline__ void line_share(const LineParams& p, int item_cost, int least, LineShared<THREADS, GROUPS>& s) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  long long before[kPer], cost[kPer];
-  long long total = 0;
+  const int per_thread = (p.n_rows + THREADS - 1) / THREADS;       // consecutive rows
+  const int r0 = min(tid * per_thread, p.n_rows), r1 = min(r0 + per_thread, p.n_rows);
+  long long mine = 0;
+#pragma unroll 1
+  for (int r = r0; r < r1; ++r) {
+    RowInfo ri;
+    if (!row_info<KEYS>(p, r, ri) && blockIdx.x == 0 && p.error_flag) atomicMax(p.error_flag, 100 + SITE_ATTN_KV8);
+    mine += ri.units(p.hkv, item_cost);
+  }
+  long long inc = mine;
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    if (i * THREADS >= p.n_rows) break;
-    const int r = i * THREADS + tid;
-    long long w = 0;
-    if (r < p.n_rows) {
-      RowInfo ri;
-      if (!row_info<KEYS>(p, r, ri) && blockIdx.x == 0 && p.error_flag) atomicMax(p.error_flag, 100 + SITE_ATTN_KV8);
-      w = ri.units(p.hkv, item_cost);
-    }
-    long long inc = w;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const long long v = __shfl_up_sync(0xffffffffu, inc, o);
-      if (lane >= o) inc += v;
-    }
-    if (lane == 31) s.warp[warp] = inc;
-    __syncthreads();
-    long long b = total;
-#pragma unroll
-    for (int k = 0; k < THREADS / 32; ++k) {
-      if (k < warp) b += s.warp[k];
-      total += s.warp[k];
-    }
-    before[i] = b + inc - w;
-    cost[i] = w;
-    __syncthreads();
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long v = __shfl_up_sync(0xffffffffu, inc, o);
+    if (lane >= o) inc += v;
+  }
+  if (lane == 31) s.warp[warp] = inc;
+  if (tid < GROUPS) s.share[tid].units = 0;
+  __syncthreads();
+  long long total = 0, before = inc - mine;
+#pragma unroll 4
+  for (int k = 0; k < THREADS / 32; ++k) {
+    if (k < warp) before += s.warp[k];
+    total += s.warp[k];
   }
   const long long workers = max(1ll, min((long long)gridDim.x * GROUPS, total / (item_cost + least)));
-#pragma unroll
+#pragma unroll 1
   for (int k = 0; k < GROUPS; ++k) {
-    const long long u = share_start((long long)blockIdx.x * GROUPS + k, total, workers);
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      if (i * THREADS >= p.n_rows) break;
-      if (before[i] <= u && u < before[i] + cost[i]) {     // (rows behind the last one count nothing); one thread at most
-        s.row[k] = i * THREADS + tid;
-        s.first[k] = before[i];
-      }
+    const long long me = (long long)blockIdx.x * GROUPS + k;
+    const bool idle = total == 0 || me >= workers;
+    if (idle && tid == 0) p.cuts[me].nrows = 0;
+    if (idle) continue;
+    const long long u = share_start(me, total, workers);
+    if (u < before || u >= before + mine) continue;                // one thread of the CTA goes on
+    long long first = before;                                      // units before row r
+    RowInfo ri;
+    int r = r0;
+    for (;; ++r) {
+      row_info<KEYS>(p, r, ri);
+      if (u - first < ri.units(p.hkv, item_cost)) break;
+      first += ri.units(p.hkv, item_cost);
     }
+    const int per = ri.item_units(item_cost), item = (int)((u - first) / per), at = (int)((u - first) - (long long)item * per);
+    LineShare sh;
+    sh.units = share_start(me + 1, total, workers) - u;
+    sh.row = r;
+    sh.head = item / ri.tiles;
+    sh.tile = item - sh.head * ri.tiles;
+    sh.at = at;
+    s.share[k] = sh;
+    Cut c = {};
+    if (at > item_cost) {                                          // inside the item's key tiles
+      const long long begin = u - at;                              // its first unit; its key tiles begin item_cost later
+      c.c0 = share_of(begin + item_cost, total, workers);
+      c.c1 = share_of(begin + per - 1, total, workers);
+      c.even = begin <= share_start(c.c0, total, workers);
+      c.head = sh.head;
+      c.t0 = ri.t0 + sh.tile * p.tq;
+      c.nrows = min(p.tq, ri.t0 + ri.n - c.t0) * (p.hq / p.hkv);
+    }
+    p.cuts[me] = c;
   }
+#pragma unroll 1
   for (int r = blockIdx.x; r < p.n_rows; r += gridDim.x) {
     RowInfo z;
     row_info<KEYS>(p, r, z);
     if (z.nb == 0) {
       uint4* dst = reinterpret_cast<uint4*>(p.out + (size_t)z.t0 * (p.hq * DH));
+#pragma unroll 1
       for (long long i = tid; i < (long long)z.n * (p.hq * DH / 8); i += THREADS) dst[i] = make_uint4(0, 0, 0, 0);
     }
   }
   __syncthreads();
-  const long long me = (long long)blockIdx.x * GROUPS + wk;
-  out.total = total;
-  out.workers = workers;
-  out.u0 = out.u1 = 0;
-  out.first = 0;
-  out.row = 0;
-  if (total > 0 && me < workers) {
-    out.u0 = share_start(me, total, workers);
-    out.u1 = share_start(me + 1, total, workers);
-    out.row = s.row[wk];
-    out.first = s.first[wk];
-  }
 }
 
 // One stretch of an item that a worker holds: key tiles [b0, b1) of nb.
@@ -156,62 +161,46 @@ struct LineItem {
   bool opens;                    // the worker's first stretch (its partial slot is the even one)
 };
 struct LineWalk {
-  long long u, u0, u1, first;
-  int row;
+  long long left;                // units still to go
+  int row, head, tile, at;       // the next item; units of it that belong to the worker before
+  bool opens;
   RowInfo ri;
-  bool fresh;
-  __device__ __forceinline__ explicit LineWalk(const LineShare& s) : u(s.u0), u0(s.u0), u1(s.u1), first(s.first), row(s.row), fresh(true) {}
+  template <int KEYS>
+  __device__ __forceinline__ void begin(const LineParams& p, const LineShare& s) {
+    left = s.units;
+    row = s.row; head = s.head; tile = s.tile; at = s.at;
+    opens = true;
+    if (left > 0) row_info<KEYS>(p, row, ri);
+  }
   template <int KEYS>
   __device__ __forceinline__ bool next(const LineParams& p, int cost, LineItem& it) {
-    const int G = p.hq / p.hkv;
-    while (u < u1) {
-      if (fresh) row_info<KEYS>(p, row, ri);
-      fresh = false;
-      for (long long w; u - first >= (w = ri.units(p.hkv, cost));) {
-        first += w;
-        ++row;
-        row_info<KEYS>(p, row, ri);
+    while (left > 0) {
+      while (tile == ri.tiles || ri.nb == 0) {     // on to the next head, or the next row that has anything
+        tile = 0;
+        if (ri.tiles == 0 || ri.nb == 0 || ++head == p.hkv) {
+          head = 0;
+          row_info<KEYS>(p, ++row, ri);
+        }
       }
-      const long long local = u - first;
-      const int per = ri.item_units(cost);
-      const int item = local < 0x7fffffffll ? (int)local / per : (int)(local / per);
-      const int at = (int)(local - (long long)item * per);
-      it.b0 = max(0, at - cost);                                  // an item's first `cost` units hold no key tile
-      it.b1 = (int)min((long long)ri.nb, max(0ll, at + (u1 - u) - cost));
-      it.opens = u == u0;
-      u += per - at;
-      if (it.b1 <= it.b0) continue;
-      it.head = item / ri.tiles;
-      const int tile = item - it.head * ri.tiles;
+      const int per = ri.nb + cost;
+      it.b0 = max(0, at - cost);                   // an item's first `cost` units hold no key tile
+      it.b1 = left < per - at ? max(0, at + (int)left - cost) : ri.nb;
+      it.opens = opens;
+      it.head = head;
       it.t0 = ri.t0 + tile * p.tq;
-      it.nrows = min(p.tq, ri.t0 + ri.n - it.t0) * G;
+      it.nrows = min(p.tq, ri.t0 + ri.n - it.t0) * (p.hq / p.hkv);
       it.vis = ri.vis;
       it.nb = ri.nb;
       it.block0 = ri.block0;
-      return true;
+      left -= per - at;
+      at = 0;
+      ++tile;
+      opens = false;
+      if (it.b1 > it.b0) return true;
     }
     return false;
   }
 };
-
-// Writes down whether the share begins inside an item's key tiles (one thread of a worker that has one).
-template <int KEYS>
-__device__ __forceinline__ void line_cut(const LineParams& p, int cost, const LineShare& s, int worker) {
-  RowInfo ri;
-  row_info<KEYS>(p, s.row, ri);
-  const int per = ri.item_units(cost), item = (int)((s.u0 - s.first) / per), at = (int)((s.u0 - s.first) % per);
-  Cut c = {};
-  if (at > cost) {
-    const long long begin = s.u0 - at;                     // the item's first unit; its key tiles begin `cost` later
-    c.c0 = share_of(begin + cost, s.total, s.workers);
-    c.c1 = share_of(begin + per - 1, s.total, s.workers);
-    c.even = begin <= share_start(c.c0, s.total, s.workers);
-    c.head = item / ri.tiles;
-    c.t0 = ri.t0 + item % ri.tiles * p.tq;
-    c.nrows = min(p.tq, ri.t0 + ri.n - c.t0) * (p.hq / p.hkv);
-  }
-  p.cuts[worker] = c;
-}
 
 cudaError_t launch_attention_kv8_tc(LineParams p, int dh, int max_ctas, int* ctas, cudaStream_t s);
 

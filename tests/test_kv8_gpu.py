@@ -337,11 +337,11 @@ def attn_bound(out, mag, dot, flat, vmax, n_keys, dh):
     """How far a correct kernel may be: the output's rounding to bf16; a query element held to 2^-17 of its row's largest
     element at worst (as two e4m3 values: the largest lies in [2^7, 2^8), half the second value's least step is 2^-10);
     scores in fp32 (dh products, a relative 2^-23 per accumulation, the scale and the base-2 exponent's argument 4 more),
-    their error e^d - 1 on every weight; weights rounded to fp16 (2^-11, or 2^-30 of the largest weight where they are
-    subnormal), exponentials 2^-21; fp32 sums over the keys in chunks of 16."""
+    their error e^d - 1 on every weight; weights rounded to fp16 (2^-11, or half the subnormal step, 2^-25, where the
+    largest weight is 2^2 at least), exponentials 2^-21; fp32 sums over the keys in chunks of 16."""
     d = dot * (dh + 4) * 2.0 ** -23 + flat * 2.0 ** -17
     w = np.expm1(2 * d) + 2.0 ** -11 + 2.0 ** -20 + (n_keys / 16 + 16) * 2.0 ** -23
-    return (np.abs(out) * HALF_BF16 + mag * w + n_keys * 2.0 ** -30 * vmax) * (1 + 2.0 ** -7) + 1e-37
+    return (np.abs(out) * HALF_BF16 + mag * w + n_keys * 2.0 ** -27 * vmax) * (1 + 2.0 ** -7) + 1e-37
 
 
 def check_attention(got, q, hq, dh, n, vis, base, kc, vc):
