@@ -562,7 +562,7 @@ inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
 }  // namespace
 
-// Scratch: the streaming kernel's cuts, partial outputs and sums; the tensor-core kernel uses the same ones (two slots of 128 rows per CTA).
+// Scratch: the streaming kernel's cuts, partial outputs and sums; the tensor-core kernel uses the same bytes for its chunks.
 size_t attention_kv8_scratch_bytes(int hq, int hkv, int dh) {
   (void)hq; (void)hkv;
   return up256(kCutBytes) + up256(kPartRows * dh * sizeof(float)) + up256(kPartRows * sizeof(float2));
@@ -585,13 +585,7 @@ cudaError_t launch_attention_kv8(const AttnKv8Args& a, cudaStream_t s) {
   at += up256(kPartRows * a.dh * sizeof(float));
   p.part_ml = reinterpret_cast<float2*>(at);
   // More than 32 query rows per kv head fill a good part of the 128-row tensor-core tiles.
-  if (widest > 32) {
-    p.tq = 128 / G;
-    int ctas = 0;
-    if (cudaError_t r = launch_attention_kv8_tc(p, a.dh, (int)(kPartRows / 256), &ctas, s)) return r;
-    return launch_pdl(a.dh == 128 ? k_attention_kv8_merge<128> : k_attention_kv8_merge<64>, dim3(ctas), dim3(kMergeThreads), 0,
-                      s, p, 128);
-  }
+  if (widest > 32) return launch_attention_kv8_tc(a, static_cast<float*>(a.scratch), a.scratch_bytes / sizeof(float), s);
   const int nq = widest <= 8 ? 1 : widest <= 16 ? 2 : 4;
   p.tq = 8 * nq / G;
   // Single-warp workers once there are about as many items as half of them.

@@ -122,5 +122,7 @@ struct AttnKv8Args {
 constexpr int kAttnKv8MaxRows = 1024;
 size_t attention_kv8_scratch_bytes(int hq, int hkv, int dh);
 cudaError_t launch_attention_kv8(const AttnKv8Args& a, cudaStream_t s);
+// tensor-core kernel for many query rows per kv head; part: scratch for partial results of key chunks
+cudaError_t launch_attention_kv8_tc(const AttnKv8Args& a, float* part, size_t part_floats, cudaStream_t s);
 
 }  // namespace bs

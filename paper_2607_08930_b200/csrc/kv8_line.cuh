@@ -202,6 +202,4 @@ struct LineWalk {
   }
 };
 
-cudaError_t launch_attention_kv8_tc(LineParams p, int dh, int max_ctas, int* ctas, cudaStream_t s);
-
 }  // namespace bs
