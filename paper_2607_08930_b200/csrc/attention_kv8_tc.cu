@@ -33,7 +33,7 @@ using namespace tc;
 constexpr int KT = 128;                              // keys per tile: four cache blocks
 constexpr int kKStages = 3, kV8Stages = 2, kV16Stages = 2;
 constexpr float kTcBias = 2.f, kTcGrow = 15.f;       // weights reach 2^15 at most, 2^2 when the reference is set
-constexpr unsigned kOCol = 256;                      // tensor memory: outputs behind two scores buffers, 128 columns each
+constexpr unsigned kOCol = 256;                      // tensor memory: outputs behind the scores, 128 columns per query tile
 
 template <int DH, int NT>
 struct TcLayout {
@@ -44,7 +44,6 @@ struct TcLayout {
   static constexpr int q = 0, k = q + NT * 2 * q_part, v8 = k + kKStages * k8, v = v8 + kV8Stages * k8;
   static constexpr int bytes = v + kV16Stages * v16;
   static constexpr int smem = bytes + 1024;
-  static constexpr int s_bufs = NT == 2 ? 1 : 2;     // scores buffers per query tile
 };
 
 __device__ __forceinline__ void tma_load_4d(unsigned dst, const CUtensorMap* map, int c0, int c1, int c2, int c3, unsigned bar) {
@@ -55,36 +54,35 @@ __device__ __forceinline__ void tma_load_4d(unsigned dst, const CUtensorMap* map
 // High word of a descriptor of a K-major operand whose rows are row_bytes long (128 or 64, swizzled by as much).
 template <int ROW>
 __host__ __device__ constexpr unsigned desc_hi() { return (unsigned)(8 * ROW >> 4) | (1u << 14) | ((ROW == 128 ? 2u : 4u) << 29); }
-// S: e4m3 x e4m3 (both K-major), fp32 accumulator, 128 x 128 x 32.  The issuing warp runs as a whole and one lane's
-// instructions take effect: descriptors and addresses then stay in uniform registers, where the instruction wants them.
-constexpr unsigned kIdescS = (1u << 4) | ((unsigned)(KT >> 3) << 17) | ((128u >> 4) << 24);
+// One lane of a converged warp, in the form that tells the compiler so: the products it issues then cost 15 to 20 cycles
+// each (39 with both operands' descriptors), where a branch on the lane number costs 52, and 63 beside busy warps.
+__device__ __forceinline__ bool elect_one() {
+  unsigned r;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+  return r != 0;
+}
+// S: e4m3 x e4m3 (both K-major), fp32 accumulator, 128 x 64 x 32.
+constexpr unsigned kIdescS = (1u << 4) | ((unsigned)(KT / 2 >> 3) << 17) | ((128u >> 4) << 24);
 template <int DH>
-__device__ __forceinline__ void umma_qk(unsigned d_tmem, unsigned a_lo, unsigned b_lo, unsigned accumulate, unsigned leader) {
+__device__ __forceinline__ void umma_qk(unsigned d_tmem, unsigned a_lo, unsigned b_lo, unsigned accumulate) {
   asm volatile(
-      "{\n\t.reg .pred p, q;\n\t.reg .b64 da, db;\n\t"
+      "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
-      "setp.ne.b32 q, %6, 0;\n\t"
       "mov.b64 da, {%1, %5};\n\t"
       "mov.b64 db, {%2, %5};\n\t"
-      "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], da, db, %3, p;\n\t}"
-      ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(kIdescS), "r"(accumulate), "r"(desc_hi<DH>()), "r"(leader) : "memory");
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], da, db, %3, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(kIdescS), "r"(accumulate), "r"(desc_hi<DH>()) : "memory");
 }
 // O: fp16 (A, tensor memory) x fp16 (B, MN-major), fp32 accumulator, 128 x DH x 16
 template <int DH>
-__device__ __forceinline__ void umma_pv(unsigned d_tmem, unsigned a_tmem, unsigned b_lo, unsigned accumulate, unsigned leader) {
+__device__ __forceinline__ void umma_pv(unsigned d_tmem, unsigned a_tmem, unsigned b_lo, unsigned accumulate) {
   constexpr unsigned idesc = (1u << 4) | (1u << 16) | ((unsigned)(DH >> 3) << 17) | ((128u >> 4) << 24);
   asm volatile(
-      "{\n\t.reg .pred p, q;\n\t.reg .b64 db;\n\t"
+      "{\n\t.reg .pred p;\n\t.reg .b64 db;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
-      "setp.ne.b32 q, %6, 0;\n\t"
       "mov.b64 db, {%2, %5};\n\t"
-      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}"
-      ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kDescHi), "r"(leader) : "memory");
-}
-__device__ __forceinline__ void umma_commit_if(unsigned bar, unsigned leader) {
-  asm volatile(
-      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
-      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar), "r"(leader) : "memory");
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kDescHi) : "memory");
 }
 // two fp32 at a time
 typedef unsigned long long f32x2;
@@ -167,10 +165,9 @@ template <int DH, int NT>
 __global__ void __launch_bounds__(TcLayout<DH, NT>::threads, 1)
 k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const TcParams p) {
   using L = TcLayout<DH, NT>;
-  constexpr int SB = L::s_bufs;
   enum { B_KFULL = 0, B_KEMPTY = B_KFULL + kKStages, B_V8FULL = B_KEMPTY + kKStages, B_V8EMPTY = B_V8FULL + kV8Stages,
-         B_VFULL = B_V8EMPTY + kV8Stages, B_VEMPTY = B_VFULL + kV16Stages, B_SFULL = B_VEMPTY + kV16Stages,
-         B_PFULL = B_SFULL + 2, B_OFULL = B_PFULL + 2, B_COUNT = B_OFULL + 2 };
+         B_VFULL = B_V8EMPTY + kV8Stages, B_VEMPTY = B_VFULL + kV16Stages, B_QFULL = B_VEMPTY + kV16Stages,
+         B_SFULL = B_QFULL + 1, B_PFULL = B_SFULL + 2 * NT, B_OFULL = B_PFULL + 2 * NT, B_COUNT = B_OFULL + 2 * NT };
   extern __shared__ unsigned char smem_dyn[];
   __shared__ __align__(8) unsigned long long bars[B_COUNT];
   __shared__ unsigned tmem_base_slot;
@@ -207,7 +204,12 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
     for (int i = 0; i < kKStages; ++i) { mbar_init(bar(B_KFULL + i), 1); mbar_init(bar(B_KEMPTY + i), 1); }
     for (int i = 0; i < kV8Stages; ++i) { mbar_init(bar(B_V8FULL + i), 1); mbar_init(bar(B_V8EMPTY + i), 4); }
     for (int i = 0; i < kV16Stages; ++i) { mbar_init(bar(B_VFULL + i), 4); mbar_init(bar(B_VEMPTY + i), 1); }
-    for (int i = 0; i < 2; ++i) { mbar_init(bar(B_SFULL + i), 1); mbar_init(bar(B_PFULL + i), 4); mbar_init(bar(B_OFULL + i), 1); }
+    mbar_init(bar(B_QFULL), 4 * NT);
+    for (int i = 0; i < 2 * NT; ++i) {                       // [query tile][half of the key tile]
+      mbar_init(bar(B_SFULL + i), 1);
+      mbar_init(bar(B_PFULL + i), 4);
+      mbar_init(bar(B_OFULL + i), 1);
+    }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
@@ -216,49 +218,6 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
                  ::"r"(smem_u32(&tmem_base_slot)), "r"(512u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-  }
-  // ---- queries: 8 dims per lane ----
-  if (n_tiles > 0) {
-    constexpr int LPR = DH / 8;                              // lanes per row
-    const int pl = lane % LPR;
-#pragma unroll 1
-    for (int r = (int)threadIdx.x / LPR; r < n_qt * 128; r += L::threads / LPR) {
-      const int x = r >> 7, f = r & 127;
-      const int tok = x * p.tq + f / G;
-      const bool valid = f < p.tq * G && tok < nt;
-      uint4 raw = make_uint4(0, 0, 0, 0);
-      if (valid) raw = __ldcg(reinterpret_cast<const uint4*>(p.q + (size_t)(t0 + tok) * p.q_ld + (kh * G + f % G) * DH) + pl);
-      float v[8];
-      const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&raw);
-      float top = 0.f;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float2 y = __bfloat1622float2(h[j]);
-        v[2 * j] = y.x;
-        v[2 * j + 1] = y.y;
-        top = fmaxf(top, fmaxf(fabsf(y.x), fabsf(y.y)));
-      }
-      const unsigned row_mask = (unsigned)((1ull << LPR) - 1) << (lane - pl);
-#pragma unroll
-      for (int o = LPR / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(row_mask, top, o));
-      const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 100);
-      const float up = pow2i(7 - e);
-      if (pl == 0) s_sc[r] = pow2i(e - 7) * (1.4426950408889634f * rsqrtf((float)DH));
-      unsigned hi[2] = {0u, 0u}, lo[2] = {0u, 0u};
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float a = v[2 * j] * up, b = v[2 * j + 1] * up;
-        const unsigned near = kv8_encode2(a, b), back = kv8_decode2((unsigned short)near);
-        const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&back));
-        hi[j >> 1] |= near << (16 * (j & 1));
-        lo[j >> 1] |= kv8_encode2(a - y.x, b - y.y) << (16 * (j & 1));
-      }
-      const int turn = DH == 128 ? f & 7 : (f >> 1) & 3;     // the swizzle of 128- and of 64-byte rows
-      const unsigned at = sQ + x * 2 * L::q_part + f * DH + (((pl >> 1) ^ turn) << 4) + (pl & 1) * 8;
-      sts64(at, hi[0], hi[1]);
-      sts64(at + L::q_part, lo[0], lo[1]);
-    }
-    fence_smem_for_mma();
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
@@ -298,45 +257,43 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
     }
   } else if (warp == 1) {
     // ------------------------------------------------------------------ MMA issuer
-    if (n_tiles > 0) {
-      const unsigned leader = lane == 0;
+    if (n_tiles > 0 && elect_one()) {
       bool ok = true;
-      // scores of key tile t and query tile x into scores buffer b.  The buffer is free: its weights were read by the
-      // last product issued against it, and the tensor pipe runs one thread's instructions in order.
-      auto scores = [&](int t, int x, int b, bool last) {
-        if (!mbar_wait(bar(B_KFULL + t % kKStages), (unsigned)(t / kKStages) & 1u, abort_flag)) return false;
+      // Scores of half h of key tile t for query tile x.  The place is free: the weights in it were read by the last
+      // product issued before, and the tensor pipe runs one thread's instructions in order.
+      auto scores = [&](int t, int x, int h) {
+        if (x == 0 && h == 0 && !mbar_wait(bar(B_KFULL + t % kKStages), (unsigned)(t / kKStages) & 1u, abort_flag)) return false;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const unsigned q_hi = desc_lo(sQ + x * 2 * L::q_part), q_lo = desc_lo(sQ + x * 2 * L::q_part + L::q_part);
-        const unsigned k_lo = desc_lo(sK + (t % kKStages) * L::k8), d = tmem_base + b * 128;
+        const unsigned k_lo = desc_lo(sK + (t % kKStages) * L::k8 + h * (L::k8 / 2)), d = tmem_base + x * 128 + h * 64;
 #pragma unroll
         for (int k = 0; k < DH / 32; ++k) {
-          umma_qk<DH>(d, q_hi + 2 * k, k_lo + 2 * k, k ? 1u : 0u, leader);
-          umma_qk<DH>(d, q_lo + 2 * k, k_lo + 2 * k, 1u, leader);
+          umma_qk<DH>(d, q_hi + 2 * k, k_lo + 2 * k, k ? 1u : 0u);
+          umma_qk<DH>(d, q_lo + 2 * k, k_lo + 2 * k, 1u);
         }
-        umma_commit_if(bar(B_SFULL + b), leader);
-        if (last) umma_commit_if(bar(B_KEMPTY + t % kKStages), leader);
+        umma_commit(bar(B_SFULL + 2 * x + h));
+        if (h == 1 && x == n_qt - 1) umma_commit(bar(B_KEMPTY + t % kKStages));
         return true;
       };
-      for (int i = 0; i < 2 && ok; ++i) {                    // the first tile of both query tiles, or the first two of one
-        const int t = NT == 1 ? i : 0, x = NT == 1 ? 0 : i;
-        if (t < n_tiles && x < n_qt) ok = scores(t, x, i, NT == 1 || x == n_qt - 1);
-      }
-      for (int t = 0; t < n_tiles && ok; ++t)
-        for (int x = 0; x < n_qt && ok; ++x) {
-          const int b = NT == 1 ? t & 1 : x;
-          ok = (x > 0 || mbar_wait(bar(B_VFULL + t % kV16Stages), (unsigned)(t / kV16Stages) & 1u, abort_flag)) &&
-               mbar_wait(bar(B_PFULL + x), (unsigned)t & 1u, abort_flag);
+      ok = mbar_wait(bar(B_QFULL), 0, abort_flag);
+      for (int i = 0; i < 2 * n_qt && ok; ++i) ok = scores(0, NT == 1 ? 0 : i % n_qt, NT == 1 ? i : i / n_qt);
+      for (int t = 0; t < n_tiles && ok; ++t) {
+        ok = mbar_wait(bar(B_VFULL + t % kV16Stages), (unsigned)(t / kV16Stages) & 1u, abort_flag);
+        const unsigned v_lo = desc_lo(sV16 + (t % kV16Stages) * L::v16, KT * 128);
+#pragma unroll 1
+        for (int i = 0; i < 2 * n_qt && ok; ++i) {           // first halves of all query tiles, then the second ones
+          const int x = NT == 1 || n_qt == 1 ? 0 : i & 1, h = NT == 1 || n_qt == 1 ? i : i >> 1;
+          ok = mbar_wait(bar(B_PFULL + 2 * x + h), (unsigned)t & 1u, abort_flag);
           if (!ok) break;
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          const unsigned v_lo = desc_lo(sV16 + (t % kV16Stages) * L::v16, KT * 128);
-          const unsigned d = tmem_base + kOCol + x * 128, a = tmem_base + b * 128;
+          const unsigned d = tmem_base + kOCol + x * 128, a = tmem_base + x * 128 + h * 64, v = v_lo + h * (KT / 32) * (2048 >> 4);
 #pragma unroll
-          for (int j = 0; j < KT / 16; ++j) umma_pv<DH>(d, a + j * 8, v_lo + j * (2048 >> 4), (t || j) ? 1u : 0u, leader);
-          umma_commit_if(bar(B_OFULL + x), leader);
-          if (x == n_qt - 1) umma_commit_if(bar(B_VEMPTY + t % kV16Stages), leader);
-          const int next = t + (NT == 1 ? 2 : 1);
-          if (next < n_tiles) ok = scores(next, x, b, x == n_qt - 1);
+          for (int j = 0; j < KT / 32; ++j) umma_pv<DH>(d, a + j * 8, v + j * (2048 >> 4), (t || h || j) ? 1u : 0u);
+          umma_commit(bar(B_OFULL + 2 * x + h));
+          if (h == 1 && x == n_qt - 1) umma_commit(bar(B_VEMPTY + t % kV16Stages));
+          if (t + 1 < n_tiles) ok = scores(t + 1, x, h);
         }
+      }
     }
   }
   } else if (group == 1 + NT) {
@@ -395,11 +352,64 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
     const int nrows = x < n_qt ? min(p.tq, nt - x * p.tq) * G : 0;
     const bool warp_has_rows = quad * 32 < nrows;
     const int my_tiles = x < n_qt ? n_tiles : 0;
-    const unsigned t_lane = tmem_base + ((unsigned)(quad * 32) << 16);
-    const unsigned t_out = t_lane + kOCol + x * 128;
-    const float sc = n_tiles > 0 && x < n_qt ? s_sc[x * 128 + r] : 0.f;
+    const unsigned t_lane = tmem_base + ((unsigned)(quad * 32) << 16) + x * 128;
+    const unsigned t_out = t_lane + kOCol;
+    // ---- the warp's 32 queries, 8 dims per lane, several rows in flight ----
+    if (my_tiles > 0) {
+      constexpr int LPR = DH / 8, RPI = 32 / LPR, FLY = 8;   // lanes per row, rows per step, steps in flight
+      const int pl = lane % LPR;
+#pragma unroll 1
+      for (int i0 = 0; i0 < 32; i0 += RPI * FLY) {
+        uint4 raw[FLY];
+#pragma unroll
+        for (int i = 0; i < FLY; ++i) {
+          const int f = quad * 32 + i0 + i * RPI + lane / LPR;
+          const int tok = t0 + x * p.tq + f / G;
+          raw[i] = make_uint4(0, 0, 0, 0);
+          if (f < nrows) raw[i] = __ldcg(reinterpret_cast<const uint4*>(p.q + (size_t)tok * p.q_ld + (kh * G + f % G) * DH) + pl);
+        }
+#pragma unroll
+        for (int i = 0; i < FLY; ++i) {
+          const int f = quad * 32 + i0 + i * RPI + lane / LPR;
+          float v[8];
+          const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&raw[i]);
+          float top = 0.f;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float2 y = __bfloat1622float2(h[j]);
+            v[2 * j] = y.x;
+            v[2 * j + 1] = y.y;
+            top = fmaxf(top, fmaxf(fabsf(y.x), fabsf(y.y)));
+          }
+#pragma unroll
+          for (int o = LPR / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+          const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 100);
+          const float up = pow2i(7 - e);
+          if (pl == 0) s_sc[x * 128 + f] = pow2i(e - 7) * (1.4426950408889634f * rsqrtf((float)DH));
+          unsigned hi[2] = {0u, 0u}, lo[2] = {0u, 0u};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float a = v[2 * j] * up, b = v[2 * j + 1] * up;
+            const unsigned near = kv8_encode2(a, b), back = kv8_decode2((unsigned short)near);
+            const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&back));
+            hi[j >> 1] |= near << (16 * (j & 1));
+            lo[j >> 1] |= kv8_encode2(a - y.x, b - y.y) << (16 * (j & 1));
+          }
+          const int turn = DH == 128 ? f & 7 : (f >> 1) & 3;     // the swizzle of 128- and of 64-byte rows
+          const unsigned at = sQ + x * 2 * L::q_part + f * DH + (((pl >> 1) ^ turn) << 4) + (pl & 1) * 8;
+          sts64(at, hi[0], hi[1]);
+          sts64(at + L::q_part, lo[0], lo[1]);
+        }
+      }
+      fence_smem_for_mma();
+    }
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar(B_QFULL));
+    const float sc = my_tiles > 0 ? s_sc[x * 128 + r] : 0.f;
     float ref = -INFINITY, sum = 0.f;
     bool ok = true;
+    // whole warps go on or give up: the tensor-memory instructions want all lanes
+    auto wait = [&](int i, int phase) { return __all_sync(0xffffffffu, mbar_wait(bar(i), (unsigned)phase & 1u, abort_flag)) != 0; };
     // The tile's four pairs of scales: lane l looks after block l % 4, one tile ahead.
     float ksn = 1.f, vsn = 1.f;
     auto load_scales = [&](int t) {
@@ -409,98 +419,83 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
     };
     if (my_tiles > 0) load_scales(0);
     for (int t = 0; t < my_tiles && ok; ++t) {
-      const int s = SB == 2 ? (t & 1) : x;
       const float f = kv8_clamp_scale(ksn), lv = log2_fast(kv8_clamp_scale(vsn));
       if (t + 1 < my_tiles) load_scales(t + 1);
       const int left = vis - (kt0 + t) * KT;
-      if (!mbar_wait(bar(B_SFULL + s), (unsigned)(SB == 2 ? t >> 1 : t) & 1u, abort_flag)) { ok = false; break; }
-      // The product of the tile before is done: the output may be rescaled, and no warp of the group - one without query
-      // rows has nothing to hold it up - publishes this tile before all four have published that one.
-      if (t > 0 && !mbar_wait(bar(B_OFULL + x), (unsigned)(t - 1) & 1u, abort_flag)) { ok = false; break; }
-      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      if (warp_has_rows) {
-        // (The loops are kept rolled to 64 scores: with all 128 of both passes unrolled, the roles' code does not fit the
-        // instruction caches.)
-        auto mask = [&](unsigned* y, int first) {
-          if (left < first + 32) {
-#pragma unroll
-            for (int j = 0; j < 32; ++j) y[j] = first + j < left ? y[j] : 0xff800000u;       // -inf
-          }
-        };
-        float top = -INFINITY;
-        auto largest = [&](unsigned* y, int i) {
-          mask(y, i * 32);
-          float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-          for (int j = 0; j < 32; j += 2) m4[(j >> 1) & 3] = max3(m4[(j >> 1) & 3], __uint_as_float(y[j]), __uint_as_float(y[j + 1]));
-          const float fi = __shfl_sync(0xffffffffu, f, i) * sc, li = __shfl_sync(0xffffffffu, lv, i);
-          top = fmaxf(top, fmaf(max3(fmaxf(m4[0], m4[1]), m4[2], m4[3]), fi, li));
-        };
 #pragma unroll 1
-        for (int i = 0; i < 4; i += 2) {
-          unsigned ya[32], yb[32];
-          tmem_ld32_nowait(t_lane + s * 128 + i * 32, ya);
+      for (int h = 0; h < 2; ++h) {                          // 64 keys at a time: their scores fit the registers, read once
+        // (These scores were issued after the weights that stood in their place were used, so no warp of the group - one
+        // without query rows has nothing to hold it up - publishes here before all four have published there.)
+        if (!wait(B_SFULL + 2 * x + h, t)) { ok = false; break; }
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        if (warp_has_rows) {
+          unsigned y[64];
+          tmem_ld32_nowait(t_lane + h * 64, y);
+          tmem_ld32_nowait(t_lane + h * 64 + 32, y + 32);
           tmem_ld_wait();
-          tmem_ld32_nowait(t_lane + s * 128 + i * 32 + 32, yb);
-          largest(ya, i);
-          tmem_ld_wait();
-          largest(yb, i + 1);
-        }
-        const bool grow = top > ref + kTcGrow;
-        if (__any_sync(0xffffffffu, grow)) {
-          float turn = 1.f;
-          if (grow) {
-            turn = exp2_fast(ref - (top - kTcBias));     // 2^-inf = 0 on the first tile
-            ref = top - kTcBias;
-            sum *= turn;
-          }
-          if (t > 0) {
-#pragma unroll 1
-            for (int c = 0; c < DH / 32; ++c) {
-              unsigned o[32];
-              tmem_ld32_nowait(t_out + c * 32, o);
-              tmem_ld_wait();
+          if (left < h * 64 + 64) {
 #pragma unroll
-              for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * turn);
-              tmem_st32(t_out + c * 32, o);
-              tmem_st_wait();
+            for (int j = 0; j < 64; ++j) y[j] = h * 64 + j < left ? y[j] : 0xff800000u;       // -inf
+          }
+          float fi[2], li[2], top = -INFINITY;
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            fi[i] = __shfl_sync(0xffffffffu, f, 2 * h + i) * sc;
+            li[i] = __shfl_sync(0xffffffffu, lv, 2 * h + i);
+            float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+            for (int j = 0; j < 32; j += 2)
+              m4[(j >> 1) & 3] = max3(m4[(j >> 1) & 3], __uint_as_float(y[i * 32 + j]), __uint_as_float(y[i * 32 + j + 1]));
+            top = fmaxf(top, fmaf(max3(fmaxf(m4[0], m4[1]), m4[2], m4[3]), fi[i], li[i]));
+          }
+          const bool grow = top > ref + kTcGrow;
+          if (__any_sync(0xffffffffu, grow)) {
+            float turn = 1.f;
+            if (grow) {
+              turn = exp2_fast(ref - (top - kTcBias));       // 2^-inf = 0 on the first tile
+              ref = top - kTcBias;
+              sum *= turn;
+            }
+            if (t > 0 || h > 0) {
+              // the output stands still once the product issued last is in it
+              if (!wait(B_OFULL + 2 * x + (h ^ 1), t - 1 + h)) { ok = false; break; }
+              asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll 1
+              for (int c = 0; c < DH / 32; ++c) {
+                unsigned o[32];
+                tmem_ld32_nowait(t_out + c * 32, o);
+                tmem_ld_wait();
+#pragma unroll
+                for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * turn);
+                tmem_st32(t_out + c * 32, o);
+              }
             }
           }
-        }
-        auto weights = [&](unsigned* y, int i, unsigned* w) {
-          mask(y, i * 32);
-          const float fi = __shfl_sync(0xffffffffu, f, i) * sc, li = __shfl_sync(0xffffffffu, lv, i);
-          const f32x2 f2 = pack2(fi, fi), shift2 = pack2(li - ref, li - ref);
-          f32x2 a4[4] = {0ull, 0ull, 0ull, 0ull};
+          unsigned w[32];
 #pragma unroll
-          for (int j = 0; j < 32; j += 2) {
-            const float2 z = unpack2(fma2(pack2(__uint_as_float(y[j]), __uint_as_float(y[j + 1])), f2, shift2));
-            const float e0 = exp2_fast(z.x), e1 = exp2_fast(z.y);
-            a4[(j >> 1) & 3] = add2(a4[(j >> 1) & 3], pack2(e0, e1));
-            const __half2 h = __floats2half2_rn(e0, e1);
-            w[j >> 1] = *reinterpret_cast<const unsigned*>(&h);
+          for (int i = 0; i < 2; ++i) {
+            const f32x2 f2 = pack2(fi[i], fi[i]), shift2 = pack2(li[i] - ref, li[i] - ref);
+            f32x2 a4[4] = {0ull, 0ull, 0ull, 0ull};
+#pragma unroll
+            for (int j = 0; j < 32; j += 2) {
+              const float2 z = unpack2(fma2(pack2(__uint_as_float(y[i * 32 + j]), __uint_as_float(y[i * 32 + j + 1])), f2, shift2));
+              const float e0 = exp2_fast(z.x), e1 = exp2_fast(z.y);
+              a4[(j >> 1) & 3] = add2(a4[(j >> 1) & 3], pack2(e0, e1));
+              const __half2 hw = __floats2half2_rn(e0, e1);
+              w[i * 16 + (j >> 1)] = *reinterpret_cast<const unsigned*>(&hw);
+            }
+            const float2 got = unpack2(add2(add2(a4[0], a4[1]), add2(a4[2], a4[3])));
+            sum = fmaf(got.x + got.y, exp2_fast(-li[i]), sum);   // 2^-lv: the inverse of the V scale
           }
-          const float2 got = unpack2(add2(add2(a4[0], a4[1]), add2(a4[2], a4[3])));
-          sum = fmaf(got.x + got.y, exp2_fast(-li), sum);       // 2^-lv: the inverse of the V scale
-        };
-#pragma unroll 1
-        for (int i = 0; i < 4; i += 2) {
-          unsigned ya[32], yb[32], w[32];
-          tmem_ld32_nowait(t_lane + s * 128 + i * 32, ya);
-          tmem_ld_wait();
-          tmem_ld32_nowait(t_lane + s * 128 + i * 32 + 32, yb);
-          weights(ya, i, w);
-          tmem_ld_wait();
-          weights(yb, i + 1, w + 16);
-          tmem_st32(t_lane + s * 128 + i * 16, w);              // over columns that were read before
+          tmem_st32(t_lane + h * 64, w);                     // over scores that were read before
+          tmem_st_wait();
         }
-        tmem_st_wait();
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(B_PFULL + 2 * x + h));
       }
-      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(B_PFULL + x));
     }
-    const bool have = ok && my_tiles > 0 && mbar_wait(bar(B_OFULL + x), (unsigned)(my_tiles - 1) & 1u, abort_flag);
+    const bool have = ok && my_tiles > 0 && wait(B_OFULL + 2 * x + 1, my_tiles - 1);
     if (warp_has_rows) {
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       const bool valid = r < nrows;
