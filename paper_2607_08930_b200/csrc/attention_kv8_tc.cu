@@ -354,52 +354,53 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
     const int my_tiles = x < n_qt ? n_tiles : 0;
     const unsigned t_lane = tmem_base + ((unsigned)(quad * 32) << 16) + x * 128;
     const unsigned t_out = t_lane + kOCol;
-    // ---- the warp's 32 queries, 8 dims per lane, several rows in flight ----
+    // ---- the warp's 32 queries, 8 dims per lane, to two e4m3 terms in place: a step's rows stand, as bf16, in the very
+    // bytes that their nearest values (lower half of the lanes) and their rests (upper half) will take ----
     if (my_tiles > 0) {
-      constexpr int LPR = DH / 8, RPI = 32 / LPR, FLY = 8;   // lanes per row, rows per step, steps in flight
-      const int pl = lane % LPR;
+      constexpr int LPR = DH / 8, RPI = 32 / LPR;            // lanes per row, rows per step
+      const int pl = lane % LPR, f0 = quad * 32 + lane / LPR;
+      const unsigned place = sQ + x * 2 * L::q_part + quad * 32 * DH;
+      const unsigned mine = place + (lane >> 4) * L::q_part + (lane & 15) * 16;
+      int head = f0 % G, tok = f0 / G;
 #pragma unroll 1
-      for (int i0 = 0; i0 < 32; i0 += RPI * FLY) {
-        uint4 raw[FLY];
-#pragma unroll
-        for (int i = 0; i < FLY; ++i) {
-          const int f = quad * 32 + i0 + i * RPI + lane / LPR;
-          const int tok = t0 + x * p.tq + f / G;
-          raw[i] = make_uint4(0, 0, 0, 0);
-          if (f < nrows) raw[i] = __ldcg(reinterpret_cast<const uint4*>(p.q + (size_t)tok * p.q_ld + (kh * G + f % G) * DH) + pl);
+      for (int i = 0; i < LPR; ++i) {
+        const bool valid = f0 + i * RPI < nrows;
+        const bf16* src = p.q + (size_t)(t0 + x * p.tq + (valid ? tok : 0)) * p.q_ld + (kh * G + head) * DH + pl * 8;
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(mine + i * 256), "l"(src), "r"(valid ? 16 : 0) : "memory");
+        head += RPI;
+        while (head >= G) {
+          head -= G;
+          ++tok;
         }
+      }
+      asm volatile("cp.async.wait_all;" ::: "memory");
+#pragma unroll 2
+      for (int i = 0; i < LPR; ++i) {
+        const uint4 raw = lds128(mine + i * 256);
+        __syncwarp();
+        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&raw);
+        __nv_bfloat162 top2 = __hmax2(__hmax2(__habs2(h[0]), __habs2(h[1])), __hmax2(__habs2(h[2]), __habs2(h[3])));
 #pragma unroll
-        for (int i = 0; i < FLY; ++i) {
-          const int f = quad * 32 + i0 + i * RPI + lane / LPR;
-          float v[8];
-          const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&raw[i]);
-          float top = 0.f;
+        for (int o = LPR / 2; o > 0; o >>= 1) top2 = __hmax2(top2, __shfl_xor_sync(0xffffffffu, top2, o));
+        const float top = fmaxf(__low2float(top2), __high2float(top2));
+        const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 100);
+        const float up = pow2i(7 - e);
+        const int f = f0 + i * RPI;
+        if (pl == 0) s_sc[x * 128 + f] = pow2i(e - 7) * (1.4426950408889634f * rsqrtf((float)DH));
+        unsigned hi[2] = {0u, 0u}, lo[2] = {0u, 0u};
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float2 y = __bfloat1622float2(h[j]);
-            v[2 * j] = y.x;
-            v[2 * j + 1] = y.y;
-            top = fmaxf(top, fmaxf(fabsf(y.x), fabsf(y.y)));
-          }
-#pragma unroll
-          for (int o = LPR / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-          const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 100);
-          const float up = pow2i(7 - e);
-          if (pl == 0) s_sc[x * 128 + f] = pow2i(e - 7) * (1.4426950408889634f * rsqrtf((float)DH));
-          unsigned hi[2] = {0u, 0u}, lo[2] = {0u, 0u};
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float a = v[2 * j] * up, b = v[2 * j + 1] * up;
-            const unsigned near = kv8_encode2(a, b), back = kv8_decode2((unsigned short)near);
-            const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&back));
-            hi[j >> 1] |= near << (16 * (j & 1));
-            lo[j >> 1] |= kv8_encode2(a - y.x, b - y.y) << (16 * (j & 1));
-          }
-          const int turn = DH == 128 ? f & 7 : (f >> 1) & 3;     // the swizzle of 128- and of 64-byte rows
-          const unsigned at = sQ + x * 2 * L::q_part + f * DH + (((pl >> 1) ^ turn) << 4) + (pl & 1) * 8;
-          sts64(at, hi[0], hi[1]);
-          sts64(at + L::q_part, lo[0], lo[1]);
+        for (int j = 0; j < 4; ++j) {
+          const float2 v = __bfloat1622float2(h[j]);
+          const float a = v.x * up, b = v.y * up;
+          const unsigned near = kv8_encode2(a, b), back = kv8_decode2((unsigned short)near);
+          const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&back));
+          hi[j >> 1] |= near << (16 * (j & 1));
+          lo[j >> 1] |= kv8_encode2(a - y.x, b - y.y) << (16 * (j & 1));
         }
+        const int turn = DH == 128 ? f & 7 : (f >> 1) & 3;     // the swizzle of 128- and of 64-byte rows
+        const unsigned at = sQ + x * 2 * L::q_part + f * DH + (((pl >> 1) ^ turn) << 4) + (pl & 1) * 8;
+        sts64(at, hi[0], hi[1]);
+        sts64(at + L::q_part, lo[0], lo[1]);
       }
       fence_smem_for_mma();
     }
