@@ -410,7 +410,10 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
     float ref = -INFINITY, sum = 0.f;
     bool ok = true;
     // whole warps go on or give up: the tensor-memory instructions want all lanes
-    auto wait = [&](int i, int phase) { return __all_sync(0xffffffffu, mbar_wait(bar(i), (unsigned)phase & 1u, abort_flag)) != 0; };
+    auto wait = [&](int i, int phase) {
+      if (__all_sync(0xffffffffu, mbar_try_wait(bar(i), (unsigned)phase & 1u))) return true;
+      return __all_sync(0xffffffffu, mbar_wait(bar(i), (unsigned)phase & 1u, abort_flag)) != 0;
+    };
     // The tile's four pairs of scales: lane l looks after block l % 4, one tile ahead.
     float ksn = 1.f, vsn = 1.f;
     auto load_scales = [&](int t) {
@@ -423,7 +426,7 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
       const float f = kv8_clamp_scale(ksn), lv = log2_fast(kv8_clamp_scale(vsn));
       if (t + 1 < my_tiles) load_scales(t + 1);
       const int left = vis - (kt0 + t) * KT;
-#pragma unroll 1
+#pragma unroll
       for (int h = 0; h < 2; ++h) {                          // 64 keys at a time: their scores fit the registers, read once
         // (These scores were issued after the weights that stood in their place were used, so no warp of the group - one
         // without query rows has nothing to hold it up - publishes here before all four have published there.)
@@ -476,11 +479,23 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             const f32x2 f2 = pack2(fi[i], fi[i]), shift2 = pack2(li[i] - ref, li[i] - ref);
+            unsigned* z = y + i * 32;
+#pragma unroll
+            for (int j = 0; j < 32; j += 2) {
+              const float2 a = unpack2(fma2(pack2(__uint_as_float(z[j]), __uint_as_float(z[j + 1])), f2, shift2));
+              z[j] = __float_as_uint(a.x);
+              z[j + 1] = __float_as_uint(a.y);
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < 64; ++j) asm volatile("ex2.approx.ftz.f32 %0, %0;" : "+r"(y[j]));
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const unsigned* z = y + i * 32;
             f32x2 a4[4] = {0ull, 0ull, 0ull, 0ull};
 #pragma unroll
             for (int j = 0; j < 32; j += 2) {
-              const float2 z = unpack2(fma2(pack2(__uint_as_float(y[i * 32 + j]), __uint_as_float(y[i * 32 + j + 1])), f2, shift2));
-              const float e0 = exp2_fast(z.x), e1 = exp2_fast(z.y);
+              const float e0 = __uint_as_float(z[j]), e1 = __uint_as_float(z[j + 1]);
               a4[(j >> 1) & 3] = add2(a4[(j >> 1) & 3], pack2(e0, e1));
               const __half2 hw = __floats2half2_rn(e0, e1);
               w[i * 16 + (j >> 1)] = *reinterpret_cast<const unsigned*>(&hw);
