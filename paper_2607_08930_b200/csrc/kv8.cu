@@ -3,10 +3,12 @@
 //
 //   y = gain * x / sqrt(mean(x^2) + eps) over a head's dims; (y_j, y_{j + dh/2}) turned by the token's angle
 //
-// All three are bound by memory: every element of qkv is read once and its result written once.  dh / 8 lanes own one
-// head of one token (16 bytes each); the norm's sum and the rotation's partner half move by shuffles inside those
-// lanes, everything between the load and the one rounding at the end stays fp32.
+// All three are bound by memory: every element of qkv is read once and its result written once.  dh / 16 lanes own one
+// head of one token, 8 dims of its first half and the 8 they are turned with: the rotation stays inside a lane, the
+// norm's sum moves by shuffles inside those lanes, everything between the load and the one rounding at the end is fp32.
 #include <math.h>
+
+#include <algorithm>
 
 #include "kv8.cuh"
 
@@ -31,32 +33,64 @@ __device__ __forceinline__ uint4 pack8(const float* x) {
   return v;
 }
 
-// x: dims [8 p, 8 p + 8) of one head, p = this lane's place among the head's dh / 8 lanes.  All lanes of the warp call.
+// A lane's part of one head: x[0..8) = dims [8 p, 8 p + 8), x[8..16) = dims dh / 2 + [8 p, 8 p + 8), p = the lane's place
+// among the head's dh / 16 lanes.
+struct HeadLoad { uint4 lo, hi; };
 template <int DH>
-__device__ __forceinline__ void head_norm(float* x, const uint4& gain, float eps) {
+__device__ __forceinline__ HeadLoad load_head(const bf16* head, int p) {
+  const uint4* src = reinterpret_cast<const uint4*>(head) + p;
+  HeadLoad v;
+  v.lo = __ldcg(src);
+  v.hi = __ldcg(src + DH / 16);
+  return v;
+}
+template <int DH>
+__device__ __forceinline__ void store_head(bf16* head, int p, const HeadLoad& v) {
+  uint4* dst = reinterpret_cast<uint4*>(head) + p;
+  dst[0] = v.lo;
+  dst[DH / 16] = v.hi;
+}
+__device__ __forceinline__ void unpack16(const HeadLoad& v, float* x) {
+  unpack8(v.lo, x);
+  unpack8(v.hi, x + 8);
+}
+__device__ __forceinline__ HeadLoad no_head() {
+  HeadLoad v;
+  v.lo = v.hi = make_uint4(0, 0, 0, 0);
+  return v;
+}
+// 1 / root mean square of the head.  All lanes of the warp call.
+template <int DH>
+__device__ __forceinline__ float head_rms(const float* x, float eps) {
   float ss = 0.f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) ss += x[i] * x[i];
+  for (int i = 0; i < 16; ++i) ss += x[i] * x[i];
 #pragma unroll
-  for (int o = DH / 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-  const float r = rsqrtf(ss * (1.0f / DH) + eps);
-  float g[8];
-  unpack8(gain, g);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = x[i] * r * g[i];
+  for (int o = DH / 32; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+  return rsqrtf(ss * (1.0f / DH) + eps);
 }
-// cs: (cos, sin) of the pairs this lane's dims belong to; sign = -1 in the first half of the dims, +1 in the second
 template <int DH>
-__device__ __forceinline__ void head_rotate(float* x, const float2* cs, float sign) {
+__device__ __forceinline__ void head_gain(float* x, float r, const bf16* gain, int p) {
+  HeadLoad v;
+  v.lo = __ldg(reinterpret_cast<const uint4*>(gain) + p);
+  v.hi = __ldg(reinterpret_cast<const uint4*>(gain) + p + DH / 16);
+  float g[16];
+  unpack16(v, g);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) x[i] = x[i] * r * g[i];
+}
+// cs: (cos, sin) of the lane's 8 pairs
+__device__ __forceinline__ void head_rotate(float* x, const float2* cs) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float y = __shfl_xor_sync(0xffffffffu, x[i], DH / 16);
-    x[i] = x[i] * cs[i].x + sign * y * cs[i].y;
+    const float u = x[i], v = x[i + 8];
+    x[i] = u * cs[i].x - v * cs[i].y;
+    x[i + 8] = v * cs[i].x + u * cs[i].y;
   }
 }
 template <int DH>
 __device__ __forceinline__ void load_turn(const float* table, int pos, int p, float2* cs) {
-  const float4* src = reinterpret_cast<const float4*>(table + (size_t)pos * DH + (p % (DH / 16)) * 16);
+  const float4* src = reinterpret_cast<const float4*>(table + (size_t)pos * DH + p * 16);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const float4 v = __ldg(src + i);
@@ -69,53 +103,51 @@ __device__ __forceinline__ void bad_index(int* flag, int site) {
   if (flag) atomicMax(flag, 100 + site);
 }
 
-constexpr int kWarps = 8;
-constexpr int kUnroll = 4;      // heads in flight per lane
+constexpr int kWarps = 4;
+constexpr int kUnroll = 3;      // heads in flight per lane
 
 // One warp: heads [h0, h1) of token t.  BF16KV: k and v heads go to cache row `kv_row` of kc / vc; else h1 <= hq.
 template <int DH, bool BF16KV>
 __device__ __forceinline__ void token_heads(const QkNormArgs& a, int t, int h0, int h1, size_t kv_row,
                                             bf16* kc, bf16* vc) {
-  constexpr int LPH = DH / 8, HPW = 32 / LPH;      // lanes per head, heads per warp pass
-  const int lane = threadIdx.x & 31, p = lane % LPH;
+  constexpr int LPH = DH / 16, HPW = 32 / LPH;     // lanes per head, heads per warp pass
+  const int lane = threadIdx.x & 31, p = lane % LPH, mine = lane / LPH;
+  const int heads = a.hq + 2 * a.hkv;
+  const bf16* src = a.qkv + (size_t)t * heads * DH;
   const int pos = __ldcg(a.tok_pos + t);
+  HeadLoad raw[kUnroll];
+  auto fetch = [&](int h) {
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) raw[u] = h + u * HPW < h1 ? load_head<DH>(src + (size_t)(h + u * HPW) * DH, p) : no_head();
+  };
+  fetch(h0 + mine);                                // on its way beside the position and the angles
   if (pos < 0 || pos >= a.max_pos) {               // warp-uniform
     if (lane == 0) bad_index(a.error_flag, SITE_QK_NORM);
     return;
   }
   const bool norm = a.q_gain != nullptr;
-  uint4 gq = make_uint4(0, 0, 0, 0), gk = gq;
-  if (norm) {
-    gq = __ldg(reinterpret_cast<const uint4*>(a.q_gain) + p);
-    gk = __ldg(reinterpret_cast<const uint4*>(a.k_gain) + p);
-  }
-  const int heads = a.hq + 2 * a.hkv;
-  const uint4* src = reinterpret_cast<const uint4*>(a.qkv + (size_t)t * heads * DH) + p;
   float2 cs[8];
   load_turn<DH>(a.table, pos, p, cs);
-  const float sign = p < LPH / 2 ? -1.f : 1.f;
-  for (int hb = h0 + lane / LPH; hb - lane / LPH < h1; hb += kUnroll * HPW) {
-    uint4 raw[kUnroll];
+  for (int hb = h0 + mine; hb - mine < h1; hb += kUnroll * HPW) {
+    if (hb != h0 + mine) fetch(hb);
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       const int h = hb + u * HPW;
-      raw[u] = h < h1 ? src[(size_t)h * LPH] : make_uint4(0, 0, 0, 0);
-    }
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      const int h = hb + u * HPW;
-      float x[8];
-      unpack8(raw[u], x);
-      if (norm) head_norm<DH>(x, h < a.hq ? gq : gk, a.eps);
-      head_rotate<DH>(x, cs, sign);
+      float x[16];
+      unpack16(raw[u], x);
+      if (norm) head_gain<DH>(x, head_rms<DH>(x, a.eps), h < a.hq ? a.q_gain : a.k_gain, p);
+      head_rotate(x, cs);
       if (h >= h1) continue;
+      HeadLoad y;
+      y.lo = pack8(x);
+      y.hi = pack8(x + 8);
       if (h < a.hq) {
-        *reinterpret_cast<uint4*>(a.q_out + (size_t)t * a.q_ld + h * DH + p * 8) = pack8(x);
+        store_head<DH>(a.q_out + (size_t)t * a.q_ld + h * DH, p, y);
       } else if (BF16KV) {
         if (h < a.hq + a.hkv)
-          *(reinterpret_cast<uint4*>(kc + (kv_row * a.hkv + (h - a.hq)) * DH) + p) = pack8(x);
+          store_head<DH>(kc + (kv_row * a.hkv + (h - a.hq)) * DH, p, y);
         else
-          *(reinterpret_cast<uint4*>(vc + (kv_row * a.hkv + (h - a.hq - a.hkv)) * DH) + p) = raw[u];
+          store_head<DH>(vc + (kv_row * a.hkv + (h - a.hq - a.hkv)) * DH, p, raw[u]);
       }
     }
   }
@@ -123,7 +155,7 @@ __device__ __forceinline__ void token_heads(const QkNormArgs& a, int t, int h0, 
 
 // bf16 cache: warps of (token, share of the heads); tok_kv[t] < 0 marks a token that belongs to no row.
 template <int DH>
-__global__ void __launch_bounds__(kWarps * 32) k_qk_norm_rope_kv(QkNormArgs a, const int* __restrict__ tok_kv, bf16* kc,
+__global__ void __launch_bounds__(kWarps * 32, 5) k_qk_norm_rope_kv(QkNormArgs a, const int* __restrict__ tok_kv, bf16* kc,
                                                                  bf16* vc, long long kv_rows, int shares, int per_share) {
   pdl_wait();
   pdl_trigger();
@@ -144,14 +176,14 @@ __global__ void __launch_bounds__(kWarps * 32) k_qk_norm_rope_kv(QkNormArgs a, c
 
 // The rows of a span of cache rows, cut at cache blocks: which row and which of its blocks a work slot stands for.
 struct Slot {
-  int row, t0, n, at, base;
+  int row, t0, n, at, base, len;     // len: kv_len of the row (0 where the caller has none)
   long long block;     // cache block
   int first;           // cache position (offset from the row's base) of the block's row 0
 };
 // false: the slot holds nothing (or indices that do not fit: flagged).  Every lane of the warp gets the same answer.
 __device__ __forceinline__ bool find_slot(int slot, const int* __restrict__ cu, const int* __restrict__ kv_base,
-                                          const int* __restrict__ kv_at, int n_rows, int M, long long n_blocks,
-                                          int* flag, Slot& s) {
+                                          const int* __restrict__ kv_at, const int* __restrict__ kv_len, int n_rows,
+                                          int M, long long n_blocks, int* flag, Slot& s) {
   s.row = warp_search(n_rows, slot, [&](int i) { return __ldcg(cu + i) / kKv8Block + 2 * i; });
   const int r = s.row;
   s.t0 = __ldcg(cu + r);
@@ -159,6 +191,7 @@ __device__ __forceinline__ bool find_slot(int slot, const int* __restrict__ cu, 
   s.n = t1 - s.t0;
   s.base = __ldcg(kv_base + r);
   s.at = __ldcg(kv_at + r);
+  s.len = kv_len ? __ldcg(kv_len + r) : 0;
   if (s.n == 0) return false;
   const bool ok = s.t0 >= 0 && s.n > 0 && t1 <= M && s.base >= 0 && s.base % kKv8Block == 0 && s.at >= 0 &&
                   (long long)s.base + s.at + s.n <= n_blocks * kKv8Block;
@@ -174,165 +207,240 @@ __device__ __forceinline__ bool find_slot(int slot, const int* __restrict__ cu, 
   return true;
 }
 
-constexpr int kTileThreads = 128;
-
-// One CTA: one (cache block, kv head) tile of K or of V.  The tile's new rows are formed in registers, its kept rows
-// decoded beside them, the largest magnitude of both gives the scale, and all of them are encoded against it.
 template <int DH>
-__device__ void write_tile(const QkNormArgs& a, const Slot& s, int kv_len, const Kv8Cache& c, int head, bool is_k,
-                           float* s_max) {
-  constexpr int LPH = DH / 8, TPP = kTileThreads / LPH, PASSES = kKv8Block / TPP;   // lanes / token, tokens / pass
-  const int tid = threadIdx.x, p = tid % LPH, sub = tid / LPH;
-  const size_t tile = (size_t)s.block * a.hkv + head;
-  unsigned char* codes = (is_k ? c.k : c.v) + tile * kKv8Block * DH + p * 8;
-  float* scale_at = (is_k ? c.k_scale : c.v_scale) + tile;
-  const float old = kv8_clamp_scale(*scale_at);
-  const bool norm = is_k && a.k_gain != nullptr;
-  const uint4 gain = norm ? __ldg(reinterpret_cast<const uint4*>(a.k_gain) + p) : make_uint4(0, 0, 0, 0);
-  const float sign = p < LPH / 2 ? -1.f : 1.f;
-  const int heads = a.hq + 2 * a.hkv;
-  float x[PASSES][8];
-  int state[PASSES];                       // 0: not a valid row, 1: kept, 2: new
-  float top = 0.f;
+constexpr int kTileThreads = kKv8Block * (DH / 16);      // a thread per (row of a tile, lane of its head)
+
+// 16 fp32 values -> their codes at two places
+template <int DH>
+__device__ __forceinline__ void store_codes(unsigned char* row, int p, const float* x, float inv) {
+  uint2 w[2];
 #pragma unroll
-  for (int i = 0; i < PASSES; ++i) {
-    const int r = i * TPP + sub, at = s.first + r;
-    state[i] = 0;
+  for (int i = 0; i < 2; ++i) {
+    const float* y = x + 8 * i;
+    w[i].x = kv8_encode2(y[0] * inv, y[1] * inv) | (kv8_encode2(y[2] * inv, y[3] * inv) << 16);
+    w[i].y = kv8_encode2(y[4] * inv, y[5] * inv) | (kv8_encode2(y[6] * inv, y[7] * inv) << 16);
+    *reinterpret_cast<uint2*>(row + i * (DH / 2) + p * 8) = w[i];
+  }
+}
+// The codes of a lane's 16 dims, in a HeadLoad's first half.
+template <int DH>
+__device__ __forceinline__ HeadLoad load_codes(const unsigned char* row, int p) {
+  const uint2 a = __ldcg(reinterpret_cast<const uint2*>(row + p * 8));
+  const uint2 b = __ldcg(reinterpret_cast<const uint2*>(row + DH / 2 + p * 8));
+  HeadLoad v = no_head();
+  v.lo = make_uint4(a.x, a.y, b.x, b.y);
+  return v;
+}
+__device__ __forceinline__ void decode16(const HeadLoad& v, float scale, float* x) {
+  const unsigned w[4] = {v.lo.x, v.lo.y, v.lo.z, v.lo.w};
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[i][j] = 0.f;
-    float2 cs[8];
+  for (int i = 0; i < 4; ++i) {
+    unsigned h[2];
+    kv8_decode4(w[i], h[0], h[1]);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) cs[j] = make_float2(1.f, 0.f);
-    if (at >= s.at && at < s.at + s.n) {
-      const int t = s.t0 + at - s.at;
-      const int pos = __ldcg(a.tok_pos + t);
-      if (pos >= 0 && pos < a.max_pos) {
-        state[i] = 2;
-        const int h = a.hq + (is_k ? 0 : a.hkv) + head;
-        unpack8(*(reinterpret_cast<const uint4*>(a.qkv + ((size_t)t * heads + h) * DH) + p), x[i]);
-        if (is_k) load_turn<DH>(a.table, pos, p, cs);
-      } else if (p == 0) {
-        bad_index(a.error_flag, SITE_KV8);
-      }
-    } else if (at < kv_len) {
-      state[i] = 1;
-      const uint2 w = *reinterpret_cast<const uint2*>(codes + r * DH);
-      unsigned h[4];
-      kv8_decode4(w.x, h[0], h[1]);
-      kv8_decode4(w.y, h[2], h[3]);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float2 f = __half22float2(*reinterpret_cast<__half2*>(&h[j]));
-        x[i][2 * j] = f.x * old;
-        x[i][2 * j + 1] = f.y * old;
-      }
-    }
-    if (is_k) {                            // shuffles stay inside a token's lanes, whose state is the same
-      float y[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) y[j] = x[i][j];
-      if (norm) head_norm<DH>(y, gain, a.eps);
-      head_rotate<DH>(y, cs, sign);
-      if (state[i] == 2) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[i][j] = y[j];
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float m = fabsf(x[i][j]);
-      if (m <= 3.402823466e38f) top = fmaxf(top, m);      // finite values only
+    for (int j = 0; j < 2; ++j) {
+      const float2 f = __half22float2(*reinterpret_cast<__half2*>(&h[j]));
+      x[4 * i + 2 * j] = f.x * scale;
+      x[4 * i + 2 * j + 1] = f.y * scale;
     }
   }
+}
+// Largest finite magnitude, as its bits (they order like the magnitudes; infinities and NaN count nothing).
+__device__ __forceinline__ unsigned largest_finite(const float* x, bool counts) {
+  unsigned top = 0;
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  if ((tid & 31) == 0) s_max[tid >> 5] = top;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kTileThreads / 32; ++w) top = fmaxf(top, s_max[w]);
-  const int k = kv8_scale_exp(top);
-  const float scale = pow2i(k), inv = pow2i(-k);
-#pragma unroll
-  for (int i = 0; i < PASSES; ++i) {
-    if (state[i] == 0 || (state[i] == 1 && scale == old)) continue;
-    uint2 w;
-    w.x = kv8_encode2(x[i][0] * inv, x[i][1] * inv) | (kv8_encode2(x[i][2] * inv, x[i][3] * inv) << 16);
-    w.y = kv8_encode2(x[i][4] * inv, x[i][5] * inv) | (kv8_encode2(x[i][6] * inv, x[i][7] * inv) << 16);
-    *reinterpret_cast<uint2*>(codes + (i * TPP + sub) * DH) = w;
+  for (int j = 0; j < 16; ++j) {
+    const unsigned b = __float_as_uint(x[j]) & 0x7fffffffu;
+    top = max(top, b < 0x7f800000u ? b : 0u);
   }
-  if (tid == 0) *scale_at = scale;
+  return __reduce_max_sync(0xffffffffu, counts ? top : 0u);
 }
 
-// CTAs [0, q_ctas): query heads, a warp for (token, share of the heads).  CTAs beyond: the K and V tiles of the work
-// slots, one (slot, kv head, K or V) each.
+// One CTA: the K and V tiles of kv heads [g0, g1) of one cache block.  A thread owns one row of the block and keeps its
+// angles in registers from head to head; the next head's rows are fetched while this one's are turned.  New rows are
+// formed in registers, kept rows decoded beside them, the largest magnitude of both gives the scale, and all are encoded
+// against it.
+// MIXED: the block also has rows that are not written - a span's first or last one.
+template <int DH, bool MIXED>
+__device__ __forceinline__ void write_tiles(const QkNormArgs& a, const Slot& s, const Kv8Cache& c, int g0, int g1,
+                            unsigned (*s_max)[2][kTileThreads<DH> / 32]) {
+  constexpr int LPH = DH / 16, W = kTileThreads<DH> / 32;
+  const int p = threadIdx.x % LPH, r = threadIdx.x / LPH, at = s.first + r;
+  const int heads = a.hq + 2 * a.hkv;
+  const bool fresh = !MIXED || (at >= s.at && at < s.at + s.n);
+  int state = MIXED && !fresh && at < s.len ? 1 : 0;                // 0: not a valid row, 1: kept, 2: new
+  const int t = fresh ? s.t0 + at - s.at : 0;
+  const bf16* src = a.qkv + ((size_t)t * heads + a.hq) * DH;
+  const size_t tile0 = (size_t)s.block * a.hkv;
+  HeadLoad k = no_head(), v = no_head();
+  float next_k = 0.f, next_v = 0.f;                        // scales of kept rows
+  auto fetch = [&](int head) {
+    if (fresh) {
+      k = load_head<DH>(src + head * DH, p);
+      v = load_head<DH>(src + (a.hkv + head) * DH, p);
+    } else if (MIXED && state == 1) {
+      const size_t at_row = ((tile0 + head) * kKv8Block + r) * DH;
+      k = load_codes<DH>(c.k + at_row, p);
+      v = load_codes<DH>(c.v + at_row, p);
+    }
+    if (MIXED) {
+      next_k = __ldcg(c.k_scale + tile0 + head);
+      next_v = __ldcg(c.v_scale + tile0 + head);
+    }
+  };
+  fetch(g0);
+  float2 cs[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) cs[j] = make_float2(1.f, 0.f);
+  if (fresh) {
+    const int pos = __ldcg(a.tok_pos + t);
+    if (pos >= 0 && pos < a.max_pos) {
+      state = 2;
+      load_turn<DH>(a.table, pos, p, cs);
+    } else if (p == 0) {
+      bad_index(a.error_flag, SITE_KV8);
+    }
+  }
+  for (int head = g0; head < g1; ++head) {
+    const size_t tile = tile0 + head;
+    unsigned char* row_k = c.k + (tile * kKv8Block + r) * DH;
+    unsigned char* row_v = c.v + (tile * kKv8Block + r) * DH;
+    const HeadLoad vc = v;                                 // V waits for its scale as it came
+    const float old_k = kv8_clamp_scale(next_k), old_v = kv8_clamp_scale(next_v);
+    float x[16];
+    auto v_row = [&] {
+      if (MIXED && state == 1) decode16(vc, old_v, x); else unpack16(vc, x);
+    };
+    v_row();
+    unsigned top_v = largest_finite(x, state != 0);
+    if (MIXED && state == 1) decode16(k, old_k, x); else unpack16(k, x);
+    if (head + 1 < g1) fetch(head + 1);
+    const float rms = a.k_gain ? head_rms<DH>(x, a.eps) : 0.f;
+    if (state == 2) {
+      if (a.k_gain) head_gain<DH>(x, rms, a.k_gain, p);
+      head_rotate(x, cs);
+    }
+    unsigned top_k = largest_finite(x, state != 0);
+    unsigned (*place)[W] = s_max[(head - g0) & 1];         // the head before the last is done with it: one barrier a head
+    if ((threadIdx.x & 31) == 0) {
+      place[0][threadIdx.x >> 5] = top_k;
+      place[1][threadIdx.x >> 5] = top_v;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      top_k = max(top_k, place[0][w]);
+      top_v = max(top_v, place[1][w]);
+    }
+    const int ek = kv8_scale_exp(__uint_as_float(top_k)), ev = kv8_scale_exp(__uint_as_float(top_v));
+    if (state == 2 || (MIXED && state == 1 && pow2i(ek) != old_k)) store_codes<DH>(row_k, p, x, pow2i(-ek));
+    if (state == 2 || (MIXED && state == 1 && pow2i(ev) != old_v)) {
+      v_row();
+      store_codes<DH>(row_v, p, x, pow2i(-ev));
+    }
+    if (threadIdx.x == 0) {
+      c.k_scale[tile] = pow2i(ek);
+      c.v_scale[tile] = pow2i(ev);
+    }
+  }
+}
+
+// CTAs [0, q_ctas): query heads, a warp for (token, share of the heads).  CTAs beyond: the tiles of the work slots, one
+// CTA for (slot, `per_cta` kv heads).
 template <int DH>
-__global__ void __launch_bounds__(kTileThreads) k_qk_norm_rope_kv8(QkNormArgs a, const int* __restrict__ cu_q,
-                                                                   const int* __restrict__ kv_base,
-                                                                   const int* __restrict__ kv_at,
-                                                                   const int* __restrict__ kv_len, int n_rows,
-                                                                   Kv8Cache c, int q_ctas, int shares, int per_share) {
-  __shared__ float s_max[kTileThreads / 32];
+__global__ void __launch_bounds__(kTileThreads<DH>, 768 / kTileThreads<DH>) k_qk_norm_rope_kv8(QkNormArgs a, const int* __restrict__ cu_q,
+                                                                       const int* __restrict__ kv_base,
+                                                                       const int* __restrict__ kv_at,
+                                                                       const int* __restrict__ kv_len, int n_rows,
+                                                                       Kv8Cache c, int q_ctas, int shares, int per_share,
+                                                                       int per_cta) {
+  __shared__ unsigned s_max[2][2][kTileThreads<DH> / 32];
   pdl_wait();
   pdl_trigger();
   if ((int)blockIdx.x < q_ctas) {
-    const long long unit = (long long)blockIdx.x * (kTileThreads / 32) + (threadIdx.x >> 5);
+    const long long unit = (long long)blockIdx.x * (kTileThreads<DH> / 32) + (threadIdx.x >> 5);
     const int t = (int)(unit / shares), part = (int)(unit % shares);
     if (t >= min(a.M, __ldcg(cu_q + n_rows))) return;      // tokens behind the last row are left alone
     token_heads<DH, false>(a, t, part * per_share, min(a.hq, (part + 1) * per_share), 0, nullptr, nullptr);
     return;
   }
   const int unit = (int)blockIdx.x - q_ctas;
-  const int which = unit % (2 * a.hkv), slot = unit / (2 * a.hkv);
+  const int groups = (a.hkv + per_cta - 1) / per_cta, slot = unit / groups, g0 = (unit - slot * groups) * per_cta;
   Slot s;
-  if (!find_slot(slot, cu_q, kv_base, kv_at, n_rows, a.M, c.n_blocks, a.error_flag, s)) return;
-  write_tile<DH>(a, s, __ldcg(kv_len + s.row), c, which >> 1, (which & 1) == 0, s_max);
+  if (!find_slot(slot, cu_q, kv_base, kv_at, kv_len, n_rows, a.M, c.n_blocks, a.error_flag, s)) return;
+  const int g1 = min(a.hkv, g0 + per_cta);
+  if (s.first < s.at || s.first + kKv8Block > s.at + s.n)
+    write_tiles<DH, true>(a, s, c, g0, g1, s_max);
+  else
+    write_tiles<DH, false>(a, s, c, g0, g1, s_max);
 }
 
-// One CTA: one work slot (a cache block's share of a row), all kv heads, K and V.
+// One warp: one (head, K or V) tile of a work slot at a time, all of it in flight at once; a CTA takes `per_cta` tiles of
+// its slot.
 template <int DH>
-__global__ void __launch_bounds__(256) k_kv8_read(Kv8Cache c, const int* __restrict__ cu, const int* __restrict__ kv_base,
+__global__ void __launch_bounds__(256, 2) k_kv8_read(Kv8Cache c, const int* __restrict__ cu, const int* __restrict__ kv_base,
                                                   const int* __restrict__ kv_at, int n_rows, int total, int hkv,
-                                                  bf16* __restrict__ k_out, bf16* __restrict__ v_out, int* error_flag) {
+                                                  bf16* __restrict__ k_out, bf16* __restrict__ v_out, int* error_flag,
+                                                  int per_cta) {
   pdl_wait();
   pdl_trigger();
+  const int tiles = 2 * hkv, groups = (tiles + per_cta - 1) / per_cta;
+  const int slot = (int)blockIdx.x / groups, w0 = ((int)blockIdx.x - slot * groups) * per_cta;
   Slot s;
-  if (!find_slot(blockIdx.x, cu, kv_base, kv_at, n_rows, total, c.n_blocks, error_flag, s)) return;
-  constexpr int LPH = DH / 8;
+  if (!find_slot(slot, cu, kv_base, kv_at, nullptr, n_rows, total, c.n_blocks, error_flag, s)) return;
+  constexpr int LPR = DH / 8, RPP = 32 / LPR, PASSES = kKv8Block / RPP;      // lanes per row, rows per pass
+  const int lane = threadIdx.x & 31, p = lane % LPR, sub = lane / LPR;
   const int lo = max(s.first, s.at) - s.first, hi = min(s.first + kKv8Block, s.at + s.n) - s.first;
-  const int units = 2 * hkv * kKv8Block * LPH;
-  for (int u = threadIdx.x; u < units; u += 256) {
-    const int p = u % LPH, r = u / LPH % kKv8Block, hw = u / LPH / kKv8Block;
-    const int head = hw >> 1;
-    if (r < lo || r >= hi) continue;
+  const long long t0 = (long long)s.t0 + s.first - s.at;                     // token of the block's row 0
+  for (int w = w0 + (threadIdx.x >> 5); w < min(tiles, w0 + per_cta); w += 8) {
+    const int head = w >> 1;
     const size_t tile = (size_t)s.block * hkv + head;
-    const unsigned char* codes = (hw & 1) ? c.v : c.k;
-    const float scale = kv8_clamp_scale(__ldcg(((hw & 1) ? c.v_scale : c.k_scale) + tile));
-    const uint2 w = *reinterpret_cast<const uint2*>(codes + (tile * kKv8Block + r) * DH + p * 8);
-    unsigned h[4];
-    kv8_decode4(w.x, h[0], h[1]);
-    kv8_decode4(w.y, h[2], h[3]);
-    float x[8];
+    const unsigned char* codes = ((w & 1) ? c.v : c.k) + tile * kKv8Block * DH;
+    bf16* out = (w & 1) ? v_out : k_out;
+    const float scale = kv8_clamp_scale(__ldcg(((w & 1) ? c.v_scale : c.k_scale) + tile));
+    uint2 raw[PASSES];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float2 f = __half22float2(*reinterpret_cast<__half2*>(&h[j]));
-      x[2 * j] = f.x * scale;
-      x[2 * j + 1] = f.y * scale;
+    for (int i = 0; i < PASSES; ++i) {
+      const int r = i * RPP + sub;
+      raw[i] = make_uint2(0, 0);
+      if (r >= lo && r < hi) raw[i] = __ldcg(reinterpret_cast<const uint2*>(codes + r * DH) + p);
     }
-    const size_t t = (size_t)(s.t0 + s.first + r - s.at);
-    *(reinterpret_cast<uint4*>(((hw & 1) ? v_out : k_out) + (t * hkv + head) * DH) + p) = pack8(x);
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) {
+      const int r = i * RPP + sub;
+      if (r < lo || r >= hi) continue;
+      unsigned h[4];
+      kv8_decode4(raw[i].x, h[0], h[1]);
+      kv8_decode4(raw[i].y, h[2], h[3]);
+      float x[8];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float2 f = __half22float2(*reinterpret_cast<__half2*>(&h[j]));
+        x[2 * j] = f.x * scale;
+        x[2 * j + 1] = f.y * scale;
+      }
+      __stcs(reinterpret_cast<uint4*>(out + ((t0 + r) * hkv + head) * DH) + p, pack8(x));
+    }
   }
 }
 
 // Heads per warp: all of a token's heads when the tokens fill the machine (the rotation's cos / sin are then loaded
 // once per token), otherwise a share of them.
-void head_shares(int M, int heads, int dh, int* shares, int* per_share) {
-  const int per_pass = 32 / (dh / 8) * kUnroll;
+void head_shares(int M, int heads, int dh, int warps, int* shares, int* per_share) {
+  const int per_pass = 32 / (dh / 16) * kUnroll;
   const int passes = (heads + per_pass - 1) / per_pass;
   int n = 1;
-  while (n < passes && (long long)M * n < 148 * 32) ++n;
+  while (n < passes && (long long)M * n < 148 * warps) ++n;
   const int each = (passes + n - 1) / n;
   *per_share = each * per_pass;
   *shares = (passes + each - 1) / each;
+}
+// Of `n` items of each of `slots` work slots: how many one CTA takes, so that a slot's indices and angles are fetched for
+// as many as leave eight CTAs per SM.
+int items_per_cta(long long slots, int n, int least) {
+  int per = n;
+  while (per > least && slots * ((n + per - 1) / per) < 148 * 8) per = (per + 1) / 2;
+  return std::max(per, least);
 }
 
 }  // namespace
@@ -341,7 +449,7 @@ cudaError_t launch_qk_norm_rope_kv(const QkNormArgs& a, const int* tok_kv, bf16*
                                    cudaStream_t s) {
   if (a.M <= 0) return cudaSuccess;
   int shares, per_share;
-  head_shares(a.M, a.hq + 2 * a.hkv, a.dh, &shares, &per_share);
+  head_shares(a.M, a.hq + 2 * a.hkv, a.dh, 20, &shares, &per_share);
   const dim3 grid((unsigned)(((long long)a.M * shares + kWarps - 1) / kWarps));
   return launch_pdl(a.dh == 128 ? k_qk_norm_rope_kv<128> : k_qk_norm_rope_kv<64>, grid, dim3(kWarps * 32), 0, s, a, tok_kv,
                     kc, vc, kv_rows, shares, per_share);
@@ -351,20 +459,26 @@ cudaError_t launch_qk_norm_rope_kv8(const QkNormArgs& a, const int* cu_q, const 
                                     const int* kv_len, int n_rows, const Kv8Cache& c, cudaStream_t s) {
   if (a.M <= 0 || n_rows <= 0) return cudaSuccess;
   int shares, per_share;
-  head_shares(a.M, a.hq, a.dh, &shares, &per_share);
-  const long long q_ctas = ((long long)a.M * shares + kTileThreads / 32 - 1) / (kTileThreads / 32);
-  const long long ctas = q_ctas + kv8_span_slots(a.M, n_rows) * 2 * a.hkv;
+  head_shares(a.M, a.hq, a.dh, 6, &shares, &per_share);
+  const int threads = a.dh == 128 ? kTileThreads<128> : kTileThreads<64>;
+  const long long q_ctas = ((long long)a.M * shares + threads / 32 - 1) / (threads / 32);
+  const long long slots = kv8_span_slots(a.M, n_rows);
+  const int per_cta = items_per_cta(slots, a.hkv, 1);
+  const long long ctas = q_ctas + slots * ((a.hkv + per_cta - 1) / per_cta);
   if (ctas > 0x7fffffffll) return cudaErrorInvalidValue;
   return launch_pdl(a.dh == 128 ? k_qk_norm_rope_kv8<128> : k_qk_norm_rope_kv8<64>, dim3((unsigned)ctas),
-                    dim3(kTileThreads), 0, s, a, cu_q, kv_base, kv_at, kv_len, n_rows, c, (int)q_ctas, shares, per_share);
+                    dim3(threads), 0, s, a, cu_q, kv_base, kv_at, kv_len, n_rows, c, (int)q_ctas, shares, per_share, per_cta);
 }
 
 cudaError_t launch_kv8_read(const Kv8Cache& c, const int* cu, const int* kv_base, const int* kv_at, int n_rows, int total,
                             int hkv, int dh, bf16* k_out, bf16* v_out, int* error_flag, cudaStream_t s) {
   if (total <= 0 || n_rows <= 0) return cudaSuccess;
-  const dim3 grid((unsigned)kv8_span_slots(total, n_rows));
-  return launch_pdl(dh == 128 ? k_kv8_read<128> : k_kv8_read<64>, grid, dim3(256), 0, s, c, cu, kv_base, kv_at, n_rows,
-                    total, hkv, k_out, v_out, error_flag);
+  const long long slots = kv8_span_slots(total, n_rows);
+  const int per_cta = items_per_cta(slots, 2 * hkv, 8);
+  const long long ctas = slots * ((2 * hkv + per_cta - 1) / per_cta);
+  if (ctas > 0x7fffffffll) return cudaErrorInvalidValue;
+  return launch_pdl(dh == 128 ? k_kv8_read<128> : k_kv8_read<64>, dim3((unsigned)ctas), dim3(256), 0, s, c, cu, kv_base,
+                    kv_at, n_rows, total, hkv, k_out, v_out, error_flag, per_cta);
 }
 
 }  // namespace bs
