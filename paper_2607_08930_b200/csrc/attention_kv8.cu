@@ -58,7 +58,8 @@ __device__ __forceinline__ uint2 lds64(unsigned at) {
 // form one line - an item counts a few blocks more than it has, about what starting and ending it costs - which the
 // workers of a single resident wave share evenly: worker c takes units [c T / N, (c + 1) T / N), whatever the rows'
 // lengths are.  An item that a worker holds whole is written out directly; a cut one leaves partial (output, reference,
-// sum) parts, at most two per worker, that a second small kernel merges in order.
+// sum) parts, at most two per worker, that a second small kernel merges in order.  Where no row is long (DIRECT) every
+// item has a worker of its own instead, and there is neither a line to lay out nor a second kernel.
 //
 // A worker is a CTA of four warps (W = 4: long items, few of them; the warps take the item's blocks in turn and add
 // their parts up in shared memory) or a single warp (W = 1: many items, whose beginnings and ends would leave four
@@ -96,7 +97,7 @@ struct StreamSmem {
   static constexpr int q = NQ * (DH / 32) * 32 * 16;               // query fragments, two k steps in 16 bytes
   static constexpr int total = 128 + front + groups * (q + W * R * 8 + R * 4);
 };
-template <int DH, int NQ, int STAGES, int W, int MINB>
+template <int DH, int NQ, int STAGES, int W, int MINB, bool DIRECT>
 __global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(const LineParams p) {
   using L = StreamSmem<DH, NQ, STAGES, W>;
   constexpr int KP = DH / 32;            // pairs of k steps of the scores
@@ -119,15 +120,37 @@ __global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(c
   pdl_wait();
   pdl_trigger();
 
-  line_share<kStreamThreads, L::groups, kKv8Block, DH>(p, kCost, W, s_line);
   const size_t me = (size_t)blockIdx.x * L::groups + wk;
-  if (s_line.share[wk].units == 0) return;   // (from here on only the worker's own threads wait for one another)
+  LineItem it = {};
+  LineWalk walk;
+  int tile = 0;
+  if constexpr (DIRECT) {
+    if (!direct_item<kKv8Block>(p, (long long)me, wtid, it, walk.ri, tile)) return;
+  } else {
+    line_share<kStreamThreads, L::groups, kKv8Block, DH>(p, kCost, W, s_line);
+    if (s_line.share[wk].units == 0) return;   // (from here on only the worker's own threads wait for one another)
+    walk.begin<kKv8Block>(p, s_line.share[wk]);
+  }
+  auto next = [&]() {
+    if constexpr (!DIRECT) return walk.next<kKv8Block>(p, kCost, it);
+    for (; tile < walk.ri.tiles; tile += p.direct) {
+      it.t0 = walk.ri.t0 + tile * p.tq;
+      it.nrows = min(p.tq, walk.ri.t0 + walk.ri.n - it.t0) * G;
+      if (it.nb > 0) {
+        tile += p.direct;
+        return true;
+      }
+      for (int i = wtid; i < it.nrows * (DH / 8); i += W * 32)       // a row that sees nothing
+        reinterpret_cast<uint4*>(p.out + (size_t)(it.t0 + i / (DH / 8) / G) * (p.hq * DH) +
+                                 (it.head * G + i / (DH / 8) % G) * DH)[i % (DH / 8)] = make_uint4(0, 0, 0, 0);
+    }
+    return false;
+  };
 
   // this warp's ring, and this lane's part of a block's copy: 16 bytes i * 512 + lane * 16 of K and of V
   const unsigned ring = tc::smem_u32(smem) + (unsigned)warp * STAGES * 2 * TB;
   const unsigned put0 = (unsigned)((lane >> 3) * 128 + (((lane & 7) ^ (lane >> 3)) << 4));
   const unsigned put1 = (unsigned)((lane >> 3) * 128 + (((lane & 7) ^ (4 + (lane >> 3))) << 4));
-  LineItem it = {};
   auto tile_of = [&](int b) { return ((size_t)it.block0 + b) * p.hkv + it.head; };
   auto fetch = [&](int stage, int b) {
     const size_t at = tile_of(b) * TB + lane * 16;
@@ -142,9 +165,7 @@ __global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(c
     }
   };
 
-  LineWalk walk;
-  walk.begin<kKv8Block>(p, s_line.share[wk]);
-  while (walk.next<kKv8Block>(p, kCost, it)) {
+  while (next()) {
     const int b0 = it.b0, b1 = it.b1, head = it.head, t0 = it.t0, nrows = it.nrows;
     sync_worker();                       // the previous segment's fragments, sums and outputs are no longer read
 #pragma unroll
@@ -167,7 +188,7 @@ __global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(c
       float top = 0.f;
 #pragma unroll
       for (int k = 0; k < KP; ++k) {     // k step i of lane c4 stands for dims c4 DH / 4 + 4 i .. + 3
-        raw[k] = valid ? *reinterpret_cast<const uint4*>(src + k * 8) : make_uint4(0, 0, 0, 0);
+        raw[k] = valid ? __ldcg(reinterpret_cast<const uint4*>(src + k * 8)) : make_uint4(0, 0, 0, 0);
         const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&raw[k]);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -339,7 +360,7 @@ __global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(c
       __syncwarp();                      // the stage may be filled again
     }
 
-    const bool whole = b0 == 0 && b1 == it.nb;
+    const bool whole = DIRECT || (b0 == 0 && b1 == it.nb);
     const size_t slot = 2 * me + (it.opens ? 0 : 1);
 #pragma unroll
     for (int nq = 0; nq < NQ; ++nq)
@@ -443,7 +464,9 @@ __global__ void __launch_bounds__(kMergeThreads) k_attention_kv8_merge(const Lin
   __shared__ float s_w[kMergeWeights];
   pdl_wait();
   pdl_trigger();
-  const Cut c = p.cuts[blockIdx.x];
+  Cut c;
+  reinterpret_cast<int4*>(&c)[0] = __ldcg(reinterpret_cast<const int4*>(p.cuts + blockIdx.x));
+  reinterpret_cast<int4*>(&c)[1] = __ldcg(reinterpret_cast<const int4*>(p.cuts + blockIdx.x) + 1);
   if (c.nrows == 0) return;
   const int parts = c.c1 - c.c0 + 1, cuts = parts - 1, nth = (int)blockIdx.x - c.c0 - 1;
   const int units = c.nrows * (DH / 4);
@@ -455,22 +478,22 @@ __global__ void __launch_bounds__(kMergeThreads) k_attention_kv8_merge(const Lin
   auto slot_of = [&](int k) { return (size_t)2 * (c.c0 + k) + (k == 0 && !c.even ? 1 : 0); };
   for (int f = f0 + warp; f <= f1; f += kMergeThreads / 32) {
     float m = -INFINITY, l = 0.f;
-    const float2 mine = lane < parts ? p.part_ml[slot_of(lane) * R + f] : make_float2(-INFINITY, 0.f);
+    const float2 mine = lane < parts ? __ldcg(p.part_ml + slot_of(lane) * R + f) : make_float2(-INFINITY, 0.f);
     m = mine.x;
-    for (int k = lane + 32; k < parts; k += 32) m = fmaxf(m, p.part_ml[slot_of(k) * R + f].x);
+    for (int k = lane + 32; k < parts; k += 32) m = fmaxf(m, __ldcg(p.part_ml + slot_of(k) * R + f).x);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
     auto weight = [&](float ref) { return ref > -INFINITY ? exp2_fast(ref - m) : 1.f; };     // (parts of NaN stay NaN)
     l = weight(mine.x) * mine.y;
     for (int k = lane + 32; k < parts; k += 32) {
-      const float2 ml = p.part_ml[slot_of(k) * R + f];
+      const float2 ml = __ldcg(p.part_ml + slot_of(k) * R + f);
       l += weight(ml.x) * ml.y;
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
     const float inv = 1.0f / l;
     if (lane < parts) s_w[(f - f0) * parts + lane] = weight(mine.x) * inv;
-    for (int k = lane + 32; k < parts; k += 32) s_w[(f - f0) * parts + k] = weight(p.part_ml[slot_of(k) * R + f].x) * inv;
+    for (int k = lane + 32; k < parts; k += 32) s_w[(f - f0) * parts + k] = weight(__ldcg(p.part_ml + slot_of(k) * R + f).x) * inv;
   }
   __syncthreads();
   auto store = [&](int v, const float4& x) {
@@ -494,7 +517,7 @@ __global__ void __launch_bounds__(kMergeThreads) k_attention_kv8_merge(const Lin
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const int v = min(base + j * kMergeThreads, v1 - 1);
-          const float4 x = *reinterpret_cast<const float4*>(from + 4 * v);
+          const float4 x = __ldcg(reinterpret_cast<const float4*>(from + 4 * v));
           const float w = s_w[(v / (DH / 4) - f0) * parts + k];
           acc[j].x += w * x.x; acc[j].y += w * x.y; acc[j].z += w * x.z; acc[j].w += w * x.w;
         }
@@ -509,7 +532,7 @@ __global__ void __launch_bounds__(kMergeThreads) k_attention_kv8_merge(const Lin
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
   for (int k = sub; k < parts; k += lanes) {
-    const float4 x = *reinterpret_cast<const float4*>(p.part_o + slot_of(k) * R * DH + 4 * vc);
+    const float4 x = __ldcg(reinterpret_cast<const float4*>(p.part_o + slot_of(k) * R * DH + 4 * vc));
     const float w = s_w[(vc / (DH / 4) - f0) * parts + k];
     acc.x += w * x.x; acc.y += w * x.y; acc.z += w * x.z; acc.w += w * x.w;
   }
@@ -528,14 +551,14 @@ constexpr size_t kCutBytes = (size_t)kMaxStreamCtas * kStreamWarps * sizeof(Cut)
 constexpr size_t kPartRows = 2 * (size_t)kStreamWarps * 296 * 32;
 
 // Per device: how many CTAs of each instantiation one wave holds (0: not asked yet).
-struct DeviceInfo { int wave[12]; };
+struct DeviceInfo { int wave[24]; };
 DeviceInfo g_dev[kMaxDevices];
 std::mutex g_mutex;
 
-template <int DH, int NQ, int STAGES, int W, int MINB>
-cudaError_t run_stream(const LineParams& p, cudaStream_t s) {
-  constexpr int index = (DH == 128 ? 6 : 0) + (NQ == 4 ? 2 : NQ - 1) * 2 + (W == 1 ? 1 : 0);
-  constexpr auto kernel = k_attention_kv8_stream<DH, NQ, STAGES, W, MINB>;
+template <int DH, int NQ, int STAGES, int W, int MINB, bool DIRECT>
+cudaError_t run_as(const LineParams& p, cudaStream_t s) {
+  constexpr int index = (DH == 128 ? 6 : 0) + (NQ == 4 ? 2 : NQ - 1) * 2 + (W == 1 ? 1 : 0) + (DIRECT ? 12 : 0);
+  constexpr auto kernel = k_attention_kv8_stream<DH, NQ, STAGES, W, MINB, DIRECT>;
   constexpr int smem = StreamSmem<DH, NQ, STAGES, W>::total;
   DeviceInfo* d = device_slot(g_dev);
   if (!d) return cudaErrorInvalidDevice;
@@ -552,9 +575,19 @@ cudaError_t run_stream(const LineParams& p, cudaStream_t s) {
       d->wave[index] = std::min(std::min(sms * per, kMaxStreamCtas), (int)(kPartRows / (2 * 8 * NQ * (kStreamWarps / W))));
     }
   }
+  if constexpr (DIRECT) {
+    const long long ctas = ((long long)p.n_rows * p.hkv * p.direct + kStreamWarps / W - 1) / (kStreamWarps / W);
+    if (ctas > 0x7fffffffll) return cudaErrorInvalidValue;
+    return launch_pdl(kernel, dim3((unsigned)ctas), dim3(kStreamThreads), (size_t)smem, s, p);
+  }
   cudaError_t r = launch_pdl(kernel, dim3(d->wave[index]), dim3(kStreamThreads), (size_t)smem, s, p);
   if (r != cudaSuccess) return r;
   return launch_pdl(k_attention_kv8_merge<DH>, dim3(d->wave[index] * (kStreamWarps / W)), dim3(kMergeThreads), 0, s, p, 8 * NQ);
+}
+
+template <int DH, int NQ, int STAGES, int W, int MINB>
+cudaError_t run_stream(const LineParams& p, cudaStream_t s) {
+  return p.direct ? run_as<DH, NQ, STAGES, W, MINB, true>(p, s) : run_as<DH, NQ, STAGES, W, MINB, false>(p, s);
 }
 
 inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
@@ -588,9 +621,14 @@ cudaError_t launch_attention_kv8(const AttnKv8Args& a, cudaStream_t s) {
   if (widest > 32) return launch_attention_kv8_tc(a, static_cast<float*>(a.scratch), a.scratch_bytes / sizeof(float), s);
   const int nq = widest <= 8 ? 1 : widest <= 16 ? 2 : 4;
   p.tq = 8 * nq / G;
-  // Single-warp workers once there are about as many items as half of them.
+  // Single-warp workers once there are about as many items as half of them (64 rows x 32 tokens, 2048 items: 121 us; 140
+  // with four-warp workers).
   const long long items = (long long)a.n_rows * a.hkv * ((max_nq + p.tq - 1) / p.tq);
   const bool many = items >= 592;
+  // Short rows have a worker per item and nothing to merge.  Four-warp workers, 2 rows of up to 1524 keys: 10.1 us, 15.5
+  // by the line; 2 rows of up to 15,778: 60 and 13.  Single-warp workers, 56 rows x 32 tokens, 32 heads, up to 64 keys:
+  // 31 us, 41 by the line; 64 rows of up to 1024: 126 and 121.
+  p.direct = a.max_vis > 0 && a.max_vis <= (many ? 512 : 2048) ? (max_nq + p.tq - 1) / p.tq : 0;
   if (a.dh == 128) {
     if (nq == 1) return many ? run_stream<128, 1, 2, 1, 3>(p, s) : run_stream<128, 1, 2, 4, 3>(p, s);
     if (nq == 2) return many ? run_stream<128, 2, 2, 1, 2>(p, s) : run_stream<128, 2, 2, 4, 3>(p, s);

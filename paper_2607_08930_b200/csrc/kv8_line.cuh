@@ -19,7 +19,7 @@ __device__ __forceinline__ float log2_fast(float x) {      // exact for powers o
 
 // A cut item: the workers that hold parts of it, its first query token, number of query rows (0: nothing is cut) and
 // kv head; whether worker c0 began with it (its part is then in the even slot, as everybody else's is).
-struct Cut { int c0, c1, t0, nrows, head, even, pad0, pad1; };
+struct alignas(16) Cut { int c0, c1, t0, nrows, head, even, pad0, pad1; };
 
 struct LineParams {
   const bf16* q;
@@ -31,6 +31,7 @@ struct LineParams {
   const int* vis;
   int n_rows, M, hq, hkv;
   int tq;                // query tokens per tile
+  int direct;            // 0: the line of work.  > 0: workers of whole items, this many for the tiles of a (row, kv head)
   Cut* cuts;             // scratch: [workers] the item that the boundary in front of a worker's share cuts
   float* part_o;         // scratch: [2 workers][rows of a tile][DH]
   float2* part_ml;       // scratch: [2 workers][rows of a tile] (reference, sum)
@@ -160,6 +161,23 @@ struct LineItem {
   int head, t0, nrows, vis, nb, b0, b1, block0;
   bool opens;                    // the worker's first stretch (its partial slot is the even one)
 };
+// The worker's item when every item has a worker of its own; false: none.  Flags rows that do not fit.
+template <int KEYS>
+__device__ __forceinline__ bool direct_item(const LineParams& p, long long worker, int lane, LineItem& it, RowInfo& ri, int& tile) {
+  const long long unit = worker / p.direct;                // (row, kv head)
+  const int r = (int)(unit / p.hkv);
+  tile = (int)(worker - unit * p.direct);
+  if (r >= p.n_rows) return false;
+  it.head = (int)(unit - (long long)r * p.hkv);
+  if (!row_info<KEYS>(p, r, ri) && lane == 0 && p.error_flag) atomicMax(p.error_flag, 100 + SITE_ATTN_KV8);
+  it.vis = ri.vis;
+  it.nb = it.b1 = ri.nb;
+  it.b0 = 0;
+  it.block0 = ri.block0;
+  it.opens = true;
+  return tile < ri.tiles;
+}
+
 struct LineWalk {
   long long left;                // units still to go
   int row, head, tile, at;       // the next item; units of it that belong to the worker before
