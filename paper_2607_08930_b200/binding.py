@@ -459,10 +459,11 @@ def _refuse(name: str, why: str) -> None:
 
 def _need(name: str, dev: int, dtype: torch.dtype, least: int, args: str, *tensors) -> None:
     """Every tensor (named by the words of `args`): contiguous, on device `dev`, `dtype`, at least `least` elements."""
-    for i, t in enumerate(tensors):
+    for t in tensors:
         if t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous() or t.numel() < least:
-            _refuse(name, f"{args.split()[i]} must be a contiguous {dtype} tensor of at least {least} elements on the "
-                          f"operator's device, got {tuple(t.shape)} {t.dtype} on {t.device}")
+            arg = args.split()[next(i for i, u in enumerate(tensors) if u is t)]
+            _refuse(name, f"{arg} must be a contiguous {dtype} tensor of at least {least} elements on the operator's "
+                          f"device, got {tuple(t.shape)} {t.dtype} on {t.device}")
 
 
 def _call(name: str, dev: int, fn, *args) -> None:
@@ -498,21 +499,22 @@ def kv8_cache(kv_rows: int, hkv: int, dh: int, device="cuda"):
 def _kv8_shape(name: str, dev: int, k8, v8, k_scale, v_scale):
     """(kv_rows, kv heads, head_dim) of an 8-bit cache."""
     shape = k8.shape
-    if len(shape) != 4 or shape[2] != KV8_BLOCK or v8.shape != shape or k_scale.shape != shape[:2] or \
-            v_scale.shape != shape[:2]:
+    blocks, hkv, rows, dh = shape if len(shape) == 4 else (0, 0, 0, 0)
+    if rows != KV8_BLOCK or v8.shape != shape or k_scale.shape != (blocks, hkv) or v_scale.shape != (blocks, hkv):
         _refuse(name, "an 8-bit cache is codes [blocks, kv heads, 32, head_dim] and scales [blocks, kv heads]")
     _need(name, dev, _E4M3, 1, "k8 v8", k8, v8)
     _need(name, dev, _F32, 1, "k_scale v_scale", k_scale, v_scale)
-    return shape[0] * KV8_BLOCK, shape[1], shape[3]
+    return blocks * KV8_BLOCK, hkv, dh
 
 
 def _row_stride(name: str, dev: int, arg: str, t: torch.Tensor, rows: int, width: int) -> int:
     """Row stride of a bf16 matrix of at least `rows` rows of `width` adjacent elements."""
-    if t.dim() != 2 or t.dtype is not _BF16 or t.get_device() != dev or t.shape[0] < rows or t.shape[1] < width or \
+    shape = t.shape
+    if len(shape) != 2 or t.dtype is not _BF16 or t.get_device() != dev or shape[0] < rows or shape[1] < width or \
             (t.stride(1) != 1 and t.numel() > 0):
         _refuse(name, f"{arg} must be a bfloat16 matrix of at least {rows} rows of {width} adjacent elements on the "
                       f"operator's device, got {tuple(t.shape)} {t.dtype} on {t.device}")
-    return t.stride(0) if rows > 1 else max(t.stride(0), t.shape[1])
+    return t.stride(0) if rows > 1 else max(t.stride(0), shape[1])
 
 
 def _norm_inputs(name: str, dev: int, qkv, q_gain, k_gain, tok_pos, hq, hkv, dh, rope, q_out, error_flag):
@@ -529,7 +531,7 @@ def _norm_inputs(name: str, dev: int, qkv, q_gain, k_gain, tok_pos, hq, hkv, dh,
     if error_flag is not None:
         _need(name, dev, _I32, 1, "error_flag", error_flag)
     if q_out is None:
-        q_out = torch.empty(M, hq * dh, dtype=_BF16, device=qkv.device)
+        return M, torch.empty(M, hq * dh, dtype=_BF16, device=qkv.device), hq * dh
     return M, q_out, _row_stride(name, dev, "q_out", q_out, M, hq * dh)
 
 
@@ -584,9 +586,12 @@ def op_kv8_read(k8, v8, k_scale, v_scale, cu, kv_base, kv_at, total: int, k_out:
         _refuse(name, "total must not be negative")
     if k_out is None:
         k_out = torch.empty(total, hkv, dh, dtype=_BF16, device=k8.device)
+    else:
+        _need(name, dev, _BF16, total * hkv * dh, "k_out", k_out)
     if v_out is None:
-        v_out = torch.empty(total, hkv, dh, dtype=_BF16, device=k8.device)
-    _need(name, dev, _BF16, total * hkv * dh, "k_out v_out", k_out, v_out)
+        v_out = torch.empty_like(k_out) if k_out.shape == (total, hkv, dh) else k_out.new_empty(total, hkv, dh)
+    else:
+        _need(name, dev, _BF16, total * hkv * dh, "v_out", v_out)
     if error_flag is not None:
         _need(name, dev, _I32, 1, "error_flag", error_flag)
     _call(name, dev, (_lib or lib()).bs_op_kv8_read, k8.data_ptr(), v8.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
