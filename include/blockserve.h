@@ -358,7 +358,8 @@ int bs_op_qk_norm_rope_kv(const void* qkv, const void* q_gain, const void* k_gai
 /* The same pass with the 8-bit cache.  The tokens of row i are written to its cache positions kv_at[i],
  * kv_at[i] + 1, ... (offsets from kv_base[i]); positions [0, kv_len[i]) held valid rows before the call.  Blocks that
  * the span touches get the scale of everything that is valid in them afterwards - the new rows and the ones that stay -
- * and rows that stay are re-encoded if their scale moved; codes at other positions are left as they were.
+ * and rows that stay are re-encoded if their scale moved; codes at other positions are left as they were.  A token whose
+ * position id is out of range is skipped; the cache row it was to take holds nothing valid afterwards.
  * (Block step: kv_len = the row's visible length.  Append: kv_at = kv_len.  Whole-row refresh: kv_at = kv_len = 0.) */
 int bs_op_qk_norm_rope_kv8(const void* qkv, const void* q_gain, const void* k_gain, float eps, const int* tok_pos,
                            const int* cu_q, const int* kv_base, const int* kv_at, const int* kv_len, int n_rows,

@@ -585,12 +585,12 @@ __global__ void __launch_bounds__(256) k_attention_kv8_chunks(const TcParams p) 
 #pragma unroll
   for (int c = 0; c < kMaxChunks; ++c) {
     ml[c] = make_float2(-INFINITY, 0.f);
-    if (c < chunks) ml[c] = part_ml[(long long)c * M * hq + unit];
+    if (c < chunks) ml[c] = __ldcg(part_ml + (long long)c * M * hq + unit);
     const float* src = part_o + ((long long)c * M * hq + unit) * DH + lane * V;
 #pragma unroll
     for (int j = 0; j < V; j += 2) {
       float2 y = make_float2(0.f, 0.f);
-      if (c < chunks && ml[c].y != 0.f) y = *reinterpret_cast<const float2*>(src + j);
+      if (c < chunks && ml[c].y != 0.f) y = __ldcg(reinterpret_cast<const float2*>(src + j));
       v[c][j] = y.x;
       v[c][j + 1] = y.y;
     }

@@ -55,8 +55,9 @@ def to_gpu(codes, scales):
             torch.from_numpy(np.ascontiguousarray(scales.astype(np.float32))).cuda())
 
 
-# fp32 chain of the norm and the rotation: the mean of dh squares (relative error under (dh / 8 + 8) 2^-24: eight
-# serial sums per lane, then a tree), rsqrtf (2^-22), three products and a sum of two, the table's own 2^-24
+# fp32 chain of the norm and the rotation: the mean of dh squares (sixteen serial sums per lane, then a tree: a relative
+# error under 19 2^-24, half of it after the root - (dh / 8 + 8) 2^-24 and more is allowed), rsqrtf (2^-22), three products
+# and a sum of two, the table's own 2^-24
 def chain_tol(x, dh):
     half = dh // 2
     pair = np.abs(x[..., :half]) + np.abs(x[..., half:])
@@ -591,3 +592,87 @@ def test_two_streams_at_once(B):
     for i in range(2):
         for o in outs[i]:
             assert torch.equal(o, want[i])
+
+
+HINT_CASES = [  # hq, hkv, dh, rows of (queries, vis): one token a row, block steps, long and short rows mixed, whole rows
+    (28, 4, 128, [(1, 40), (1, 2500), (1, 0), (1, 129)]),
+    (8, 8, 64, [(32, 96), (5, 700), (0, 9), (32, 0), (1, 33)]),
+    (32, 32, 128, [(32, 64)] * 20 + [(32, 600), (2, 1)]),
+    (14, 2, 128, [(70, 300), (3, 31), (129, 1200)])]
+
+
+@pytest.mark.parametrize("max_nq,max_vis", [(0, 0), (1, 1), (0, 1), (1, 0), (3, 128), (1 << 20, 1 << 20)])
+@pytest.mark.parametrize("hq,hkv,dh,rows", HINT_CASES)
+def test_hints_choose_the_kernel_and_nothing_else(B, hq, hkv, dh, rows, max_nq, max_vis):
+    """Too small, too large and absent: rows of any length come out right, and a row that does not fit is skipped alone."""
+    rng = np.random.default_rng(len(rows) + dh)
+    n, vis, base, kc, vc, q = attn_inputs(rng, hq, hkv, dh, rows)
+    (k8, ks), (v8, vs) = to_gpu(*kc), to_gpu(*vc)
+    flag = torch.zeros(1, dtype=torch.int32, device="cuda")
+    out = torch.full((len(q), hq * dh), 6.0, dtype=torch.bfloat16, device="cuda")
+    call = lambda v: B.op_attention_kv8(q.cuda(), k8, v8, ks, vs, ints(prefix(n)), ints(base), ints(v), hq, max_nq=max_nq,   # noqa: E731
+                                        max_vis=max_vis, out=out, error_flag=flag)
+    call(vis)
+    assert int(flag.item()) == 0
+    check_attention(host(out), q, hq, dh, n, vis, base, kc, vc)
+    out.fill_(6.0)
+    wrong = vis.copy()
+    wrong[1] = k8.shape[0] * 32 + 1 - base[1]
+    call(wrong)
+    lo, hi = prefix(n)[1:3]
+    assert int(flag.item()) >= 100
+    assert (out[lo:hi] == 6.0).all()
+    # (not the bits of before: where the rows' keys are split depends on all of them)
+    rest = np.arange(len(n)) != 1
+    left = np.concatenate([host(out)[:lo], host(out)[hi:]])
+    check_attention(left, torch.cat([q[:lo], q[hi:]]), hq, dh, n[rest], vis[rest], base[rest], kc, vc)
+
+
+@pytest.mark.parametrize("hq,hkv,dh", [(8, 8, 64), (9, 3, 128)])
+def test_write_with_several_heads_to_a_block_of_threads(B, hq, hkv, dh):
+    """Enough cache blocks that one CTA walks over the kv heads: codes and scales of V bit for bit, K by its scale."""
+    rng = np.random.default_rng(dh)
+    n = np.full(40, 300) + rng.integers(-40, 40, 40)
+    at = rng.integers(0, 64, 40)
+    base, blocks = slabs(rng, at + n)
+    M, cu = int(n.sum()), prefix(n)
+    qkv = bf16(rng.normal(size=(M, (hq + 2 * hkv) * dh)))
+    g = bf16(np.ones(dh))
+    row = np.repeat(np.arange(len(n)), n)
+    pos = at[row] + np.arange(M) - cu[row]
+    ck, sk = random_cache(rng, blocks, hkv, dh)
+    cv, sv = random_cache(rng, blocks, hkv, dh)
+    (k8, ks), (v8, vs) = to_gpu(ck, sk), to_gpu(cv, sv)
+    B.op_qk_norm_rope_kv8(qkv.cuda(), g.cuda(), g.cuda(), EPS, ints(pos), ints(cu), ints(base), ints(at), ints(at), k8, v8,
+                          ks, vs, hq, hkv, dh, B.rope_table(1000, dh, THETA))
+    x = host(qkv).reshape(M, hq + 2 * hkv, dh)
+    plan = list(zip(cu[:-1], n, base, at, at))
+    rv, rsv = K.write(cv, sv, plan, x[:, hq + hkv:])
+    assert (vs.cpu().numpy() == rsv).all() and (v8.view(torch.uint8).cpu().numpy() == rv).all()
+    k = K.norm_rope(x[:, hq:hq + hkv], np.ones(dh), EPS, pos, THETA)
+    gk8, gks = k8.view(torch.uint8).cpu().numpy(), ks.cpu().numpy().astype(np.float64)
+    at_row = base[row] + pos
+    vals = K.decode(gk8[at_row // 32, :, at_row % 32]) * gks[at_row // 32][..., None]
+    assert (np.abs(vals - k) <= np.maximum(np.abs(k) * 2.0 ** -4, gks[at_row // 32][..., None] * 2.0 ** -10) + 2 * chain_tol(k, dh)).all()
+
+
+def test_rows_that_stay_keep_their_nan_to_themselves(B):
+    """A kept row's NaN codes meet neither the rotation nor the norm of the new rows beside it; its finite codes follow the
+    scale."""
+    hq, hkv, dh = 2, 2, 64
+    rng = np.random.default_rng(11)
+    ck, sk = random_cache(rng, 2, hkv, dh)
+    ck[1, 0, 3, 7], ck[1, 1, 4, 40] = 127, 255
+    (k8, ks), (v8, vs) = to_gpu(ck, sk), to_gpu(ck, sk)
+    qkv = bf16(rng.normal(size=(4, 6 * dh)) * 8)
+    g = bf16(np.ones(dh)).cuda()
+    B.op_qk_norm_rope_kv8(qkv.cuda(), g, g, EPS, ints([5, 6, 7, 8]), ints([0, 4]), ints([32]), ints([5]), ints([5]), k8, v8, ks,
+                          vs, hq, hkv, dh, B.rope_table(50, dh, THETA))
+    for codes, scales in ((k8, ks), (v8, vs)):
+        c, s = codes.view(torch.uint8).cpu().numpy(), scales.cpu().numpy().astype(np.float64)
+        was = K.decode(ck[1, :, :5]) * sk[1][:, None, None]
+        now = K.decode(c[1, :, :5]) * s[1][:, None, None]
+        assert np.array_equal(np.isnan(now), np.isnan(was)) and np.isnan(now).sum() == 2
+        half_step = np.maximum(np.abs(was) * 2.0 ** -4, s[1][:, None, None] * 2.0 ** -10)
+        assert (np.abs(now - was)[~np.isnan(was)] <= half_step[~np.isnan(was)]).all()
+        assert not np.isnan(K.decode(c[1, :, 5:9])).any()
