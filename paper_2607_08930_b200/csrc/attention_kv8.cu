@@ -477,23 +477,35 @@ __global__ void __launch_bounds__(kMergeThreads) k_attention_kv8_merge(const Lin
   // the first holder's part is in its odd slot unless it began with the item; everybody else began with it
   auto slot_of = [&](int k) { return (size_t)2 * (c.c0 + k) + (k == 0 && !c.even ? 1 : 0); };
   for (int f = f0 + warp; f <= f1; f += kMergeThreads / 32) {
+    // the first 128 parts' references and sums in registers, all on their way at once
+    constexpr int KEEP = 4;
+    float2 ml[KEEP];
     float m = -INFINITY, l = 0.f;
-    const float2 mine = lane < parts ? __ldcg(p.part_ml + slot_of(lane) * R + f) : make_float2(-INFINITY, 0.f);
-    m = mine.x;
-    for (int k = lane + 32; k < parts; k += 32) m = fmaxf(m, __ldcg(p.part_ml + slot_of(k) * R + f).x);
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i) {
+      const int k = lane + 32 * i;
+      ml[i] = k < parts ? __ldcg(p.part_ml + slot_of(k) * R + f) : make_float2(-INFINITY, 0.f);
+    }
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i) m = fmaxf(m, ml[i].x);
+    for (int k = lane + 32 * KEEP; k < parts; k += 32) m = fmaxf(m, __ldcg(p.part_ml + slot_of(k) * R + f).x);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
     auto weight = [&](float ref) { return ref > -INFINITY ? exp2_fast(ref - m) : 1.f; };     // (parts of NaN stay NaN)
-    l = weight(mine.x) * mine.y;
-    for (int k = lane + 32; k < parts; k += 32) {
-      const float2 ml = __ldcg(p.part_ml + slot_of(k) * R + f);
-      l += weight(ml.x) * ml.y;
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i) l += weight(ml[i].x) * ml[i].y;
+    for (int k = lane + 32 * KEEP; k < parts; k += 32) {
+      const float2 x = __ldcg(p.part_ml + slot_of(k) * R + f);
+      l += weight(x.x) * x.y;
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
     const float inv = 1.0f / l;
-    if (lane < parts) s_w[(f - f0) * parts + lane] = weight(mine.x) * inv;
-    for (int k = lane + 32; k < parts; k += 32) s_w[(f - f0) * parts + k] = weight(__ldcg(p.part_ml + slot_of(k) * R + f).x) * inv;
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i)
+      if (lane + 32 * i < parts) s_w[(f - f0) * parts + lane + 32 * i] = weight(ml[i].x) * inv;
+    for (int k = lane + 32 * KEEP; k < parts; k += 32)
+      s_w[(f - f0) * parts + k] = weight(__ldcg(p.part_ml + slot_of(k) * R + f).x) * inv;
   }
   __syncthreads();
   auto store = [&](int v, const float4& x) {
