@@ -629,24 +629,29 @@ cudaError_t launch_attention_kv8(const AttnKv8Args& a, cudaStream_t s) {
   p.part_o = reinterpret_cast<float*>(at);
   at += up256(kPartRows * a.dh * sizeof(float));
   p.part_ml = reinterpret_cast<float2*>(at);
-  // More than 32 query rows per kv head fill a good part of the 128-row tensor-core tiles.
+  // More than 32 query rows per kv head fill a good part of the 128-row tensor-core tiles (16 rows of 320 to 800 keys: 35
+  // query rows 18.2 us, 20.2 by the streaming kernel, 224 19.9 and 38.6; 32 heads, 40 query rows 62 and 68).
   if (widest > 32) return launch_attention_kv8_tc(a, static_cast<float*>(a.scratch), a.scratch_bytes / sizeof(float), s);
   const int nq = widest <= 8 ? 1 : widest <= 16 ? 2 : 4;
   p.tq = 8 * nq / G;
-  // Single-warp workers once there are about as many items as half of them (64 rows x 32 tokens, 2048 items: 121 us; 140
-  // with four-warp workers).
+  // Single-warp workers where there are more items than warps to hold them (6 CTAs of work for every SM), and each is
+  // work for a warp: from two query tiles on.  100 to 500 keys: 300 rows x 2 tokens, 7 heads a group, 1200 items 34.3 us
+  // (35.5 with four-warp workers), 120 x 32 tokens, head_dim 64, 1920 items 59 us (73); 800 items 29.2 us (26.4); one query
+  // tile, 800 items 20.9 us (19.3).
   const long long items = (long long)a.n_rows * a.hkv * ((max_nq + p.tq - 1) / p.tq);
-  const bool many = items >= 592;
-  // Short rows have a worker per item and nothing to merge.  Four-warp workers, 2 rows of up to 1524 keys: 10.1 us, 15.5
-  // by the line; 2 rows of up to 15,778: 60 and 13.  Single-warp workers, 56 rows x 32 tokens, 32 heads, up to 64 keys:
-  // 31 us, 41 by the line; 64 rows of up to 1024: 126 and 121.
-  p.direct = a.max_vis > 0 && a.max_vis <= (many ? 512 : 2048) ? (max_nq + p.tq - 1) / p.tq : 0;
+  const bool many = nq > 1 && items >= 6 * 148;
+  // Short rows have a worker per item and nothing to merge; so do rows of some length where there are about as many items
+  // as workers fit the machine.  Four-warp workers: 2 rows of up to 1524 keys 10.1 us, 15.5 by the line; 2 rows of up to
+  // 15,778 60 and 13; 480 items of up to 3000 59 and 66; 256 items of up to 4000 41 and 38.  Single-warp workers: 1280
+  // items of up to 300 keys 48 us, 59 by the line; 2048 items of up to 1024 126 and 121.
+  const int reach = many ? 512 : items >= 400 ? 4096 : 2048;
+  p.direct = a.max_vis > 0 && a.max_vis <= reach ? (max_nq + p.tq - 1) / p.tq : 0;
   if (a.dh == 128) {
-    if (nq == 1) return many ? run_stream<128, 1, 2, 1, 3>(p, s) : run_stream<128, 1, 2, 4, 3>(p, s);
+    if (nq == 1) return run_stream<128, 1, 2, 4, 3>(p, s);
     if (nq == 2) return many ? run_stream<128, 2, 2, 1, 2>(p, s) : run_stream<128, 2, 2, 4, 3>(p, s);
     return many ? run_stream<128, 4, 2, 1, 2>(p, s) : run_stream<128, 4, 2, 4, 2>(p, s);
   }
-  if (nq == 1) return many ? run_stream<64, 1, 2, 1, 3>(p, s) : run_stream<64, 1, 2, 4, 3>(p, s);
+  if (nq == 1) return run_stream<64, 1, 2, 4, 3>(p, s);
   if (nq == 2) return many ? run_stream<64, 2, 2, 1, 3>(p, s) : run_stream<64, 2, 2, 4, 3>(p, s);
   return many ? run_stream<64, 4, 2, 1, 2>(p, s) : run_stream<64, 4, 2, 4, 2>(p, s);
 }

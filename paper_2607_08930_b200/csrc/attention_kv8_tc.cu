@@ -149,7 +149,8 @@ struct TcParams {
   const int* vis;
   int n_rows, M, hq, hkv;
   int tq;            // query tokens per query tile
-  int chunks;        // key chunks per row (grid z); > 1: partials instead of the output
+  int per_row;       // spans of a row that have a CTA of their own
+  int chunks;        // key chunks per row; > 1: partials instead of the output
   float* part_o;     // [chunks][M][hq][DH]
   float2* part_ml;   // [chunks][M][hq] (reference, sum); sum 0: a chunk without keys
   int* error_flag;
@@ -182,21 +183,26 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
   pdl_trigger();
 
   // ---- the work item ----
-  const int G = p.hq / p.hkv, kh = blockIdx.y, per_cta = NT * p.tq;
-  const int slot = (int)blockIdx.x;
-  const int row = warp_search(p.n_rows, slot, [&](int i) { return __ldcg(p.cu_q + i) / per_cta + i; });
+  const int G = p.hq / p.hkv, per_cta = NT * p.tq;
+  // A CTA is (span, key chunk, kv head), heads next to each other.  Spans [0, n_rows per_row): the first per_row of every
+  // row.  Behind them: the rest, if a row has any, by slots that need no prefix (row i's begin at cu[i] / per_cta + i).
+  const int unit = (int)blockIdx.x / p.hkv, kh = (int)blockIdx.x - unit * p.hkv, at = unit / p.chunks, chunk = unit - at * p.chunks;
+  const int slot = at - p.n_rows * p.per_row;
+  const int row = slot < 0 ? at / p.per_row
+                           : warp_search(p.n_rows, slot, [&](int i) { return __ldcg(p.cu_q + i) / per_cta + i; });
   const int cq0 = __ldcg(p.cu_q + row), cq1 = __ldcg(p.cu_q + row + 1), vis = __ldcg(p.vis + row), base = __ldcg(p.kv_base + row);
   if (!row_fits(p, cq0, cq1, vis, base)) {
     if (threadIdx.x == 0 && p.error_flag) atomicMax(p.error_flag, 100 + SITE_ATTN_KV8);
     return;
   }
-  const int t0 = cq0 + (slot - (cq0 / per_cta + row)) * per_cta;
+  const int span = slot < 0 ? at - row * p.per_row : slot - (cq0 / per_cta + row);
+  const int t0 = cq0 + span * per_cta;
   const int nt = min(per_cta, cq1 - t0);                    // query tokens of this CTA
-  if (t0 < cq0 || nt <= 0) return;                          // a slot that no tokens fall into
+  if (nt <= 0 || span < (slot < 0 ? 0 : p.per_row)) return; // no tokens, or somebody else's
   const int n_qt = NT == 1 || nt <= p.tq ? 1 : 2;
   const int tiles_all = (vis + KT - 1) / KT;
   const int per_chunk = (tiles_all + p.chunks - 1) / p.chunks;
-  const int kt0 = (int)blockIdx.z * per_chunk;
+  const int kt0 = chunk * per_chunk;
   const int n_tiles = max(0, min(tiles_all, kt0 + per_chunk) - kt0);
 
   if (threadIdx.x == 0) {
@@ -518,10 +524,10 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
       const int rr = valid ? r : 0;
       const size_t tok = (size_t)(t0 + x * p.tq + rr / G);
       const size_t at = (tok * p.hq + kh * G + rr % G) * DH;
-      const size_t ml_at = ((size_t)blockIdx.z * p.M + tok) * p.hq + kh * G + rr % G;
+      const size_t ml_at = ((size_t)chunk * p.M + tok) * p.hq + kh * G + rr % G;
       if (p.chunks > 1 && valid) p.part_ml[ml_at] = make_float2(have ? ref : -INFINITY, have ? sum : 0.f);
       const float inv = have ? 1.0f / sum : 0.f;
-      float* pdst = p.part_o + (size_t)blockIdx.z * p.M * p.hq * DH + at;
+      float* pdst = p.part_o + (size_t)chunk * p.M * p.hq * DH + at;
 #pragma unroll 1
       for (int c = 0; c < DH / 32; ++c) {
         unsigned o[32];
@@ -564,7 +570,7 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
 }
 
 // Merges the key chunks of every (token, head): out = sum_c 2^(m_c - m) o_c / sum_c 2^(m_c - m) l_c.  A warp per head.
-constexpr int kMaxChunks = 4;
+constexpr int kMaxChunks = 16;
 template <int DH>
 __global__ void __launch_bounds__(256) k_attention_kv8_chunks(const TcParams p) {
   constexpr int V = DH / 32;                                 // dims per lane
@@ -654,21 +660,31 @@ cudaError_t run_tc(const AttnKv8Args& a, float* part, size_t part_floats, int sm
   p.out = a.out; p.cu_q = a.cu_q; p.kv_base = a.kv_base; p.vis = a.vis;
   p.n_rows = a.n_rows; p.M = a.M; p.hq = a.hq; p.hkv = a.hkv; p.error_flag = a.error_flag;
   p.tq = 128 / G;
-  // Two query tiles per CTA share every key tile it loads and converts; one per CTA fills the SMs when there are few.
+  // Two query tiles per CTA share every key tile it loads and converts (6 rows of 1200 to 2304 tokens, 7 heads a group: 379
+  // us, 552 with one; 3 rows of 600 to 700 49 and 72); one per CTA fills the SMs when there are few.
   const int nq = a.max_nq > 0 ? std::min(a.max_nq, a.M) : a.M;
   const long long singles = (long long)((nq + p.tq - 1) / p.tq) * a.n_rows * a.hkv;       // most query tiles there can be
   const bool two = singles > 2ll * sms && nq > p.tq;
   const int key_tiles = a.max_vis > 0 ? (a.max_vis + KT - 1) / KT : 1;
+  // Few CTAs: the keys are cut, too, as long as a chunk keeps four key tiles (32 tokens, 4 kv heads: a row of 30,000 to 40,000
+  // keys 45 us, 369 uncut, 4 rows of 1000 to 2000 26 and 34; 9 rows of 500 to 800 25 us in two chunks, 20 uncut).
   int chunks = 1;
   if (!two)
-    while (chunks < kMaxChunks && singles * (chunks + 1) <= sms && key_tiles / (chunks + 1) >= 2 &&
+    while (chunks < kMaxChunks && singles * (chunks + 1) <= sms && key_tiles / (chunks + 1) >= 4 &&
            (size_t)(chunks + 1) * a.M * a.hq * (DH + 2) <= part_floats)
       ++chunks;
   p.chunks = chunks;
   p.part_o = part;
   p.part_ml = reinterpret_cast<float2*>(part + (size_t)chunks * a.M * a.hq * DH);
   const int per_cta = (two ? 2 : 1) * p.tq;
-  const dim3 grid((unsigned)((long long)a.M / per_cta + a.n_rows), a.hkv, chunks);
+  // CTAs by slots are as many as there could be spans, up to half of them empty; where the caller's largest row says where
+  // the spans are, the CTAs that have work come first and the slots, for rows longer than that, last.
+  const long long slots = (long long)a.M / per_cta + a.n_rows;
+  const long long spans = a.max_nq > 0 ? (nq + per_cta - 1) / per_cta : 0;
+  p.per_row = (int)(spans * a.n_rows <= slots ? spans : 0);
+  const long long ctas = (slots + (long long)a.n_rows * p.per_row) * a.hkv * chunks;
+  if (ctas > 0x7fffffffll) return cudaErrorInvalidValue;
+  const dim3 grid((unsigned)ctas);
   cudaError_t r = two ? launch_pdl(k_attention_kv8_tc<DH, 2>, grid, dim3(TcLayout<DH, 2>::threads), (size_t)TcLayout<DH, 2>::smem, s, mk, mv, p)
                       : launch_pdl(k_attention_kv8_tc<DH, 1>, grid, dim3(TcLayout<DH, 1>::threads), (size_t)TcLayout<DH, 1>::smem, s, mk, mv, p);
   if (r != cudaSuccess || chunks == 1) return r;

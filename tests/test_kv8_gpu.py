@@ -676,3 +676,14 @@ def test_rows_that_stay_keep_their_nan_to_themselves(B):
         half_step = np.maximum(np.abs(was) * 2.0 ** -4, s[1][:, None, None] * 2.0 ** -10)
         assert (np.abs(now - was)[~np.isnan(was)] <= half_step[~np.isnan(was)]).all()
         assert not np.isnan(K.decode(c[1, :, 5:9])).any()
+
+
+@pytest.mark.parametrize("hq,hkv,dh,rows", [(28, 4, 128, [(32, 9000)]), (8, 2, 64, [(40, 4200), (9, 700), (33, 0)])])
+def test_a_few_long_rows_in_many_chunks(B, hq, hkv, dh, rows):
+    """Few query tiles over long rows: the keys are cut into as many chunks as the rows' lengths allow, some of them empty."""
+    rng = np.random.default_rng(dh)
+    n, vis, base, kc, vc, q = attn_inputs(rng, hq, hkv, dh, rows, qscale=0.2)
+    (k8, ks), (v8, vs) = to_gpu(*kc), to_gpu(*vc)
+    out = B.op_attention_kv8(q.cuda(), k8, v8, ks, vs, ints(prefix(n)), ints(base), ints(vis), hq, max_nq=int(n.max()),
+                             max_vis=int(vis.max()))
+    check_attention(host(out), q, hq, dh, n, vis, base, kc, vc)
