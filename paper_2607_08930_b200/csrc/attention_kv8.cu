@@ -67,6 +67,12 @@ __device__ __forceinline__ uint2 lds64(unsigned at) {
 // no other warp touches (cp.async, no barrier): the next blocks are on their way while this one is computed.  Rows
 // behind the row's end arrive as zeros, whatever the cache holds there.
 //
+// What it reaches: 64 single-token rows of 1024 to 4096 keys (28 / 4 heads, 175 MB) 32 us of streaming, 5.5 TB/s of the
+// 6.5 measured for a copy, and 5 us of merge; two rows of 50,001 and 65,536 keys 23 us and 6.  64 rows x 32 tokens over
+// up to 1024 keys of 32 heads, 121 us, are bound by the instructions around the products instead - a block of 32 keys
+// takes a warp about 3600 clk, 1040 of them in its 128 products, with two warps per scheduler to overlap (255 registers,
+// most of them outputs).
+//
 // Keys are the rows (M) of both products and the queries their columns (N), so that 8 query rows - a group of heads of
 // one token - fill an instruction.  Codes go to the tensor cores as fp16, which holds every e4m3 value (the warp-level
 // e4m3 product is no way around that: measured on B200, it runs as conversions and two fp16 products, 25 clk against 8).
@@ -646,14 +652,18 @@ cudaError_t launch_attention_kv8(const AttnKv8Args& a, cudaStream_t s) {
   // items of up to 300 keys 48 us, 59 by the line; 2048 items of up to 1024 126 and 121.
   const int reach = many ? 512 : items >= 400 ? 4096 : 2048;
   p.direct = a.max_vis > 0 && a.max_vis <= reach ? (max_nq + p.tq - 1) / p.tq : 0;
+  // Stages and CTAs per SM.  One query tile, head_dim 128: three stages on two CTAs, 64 rows of 1024 to 4096 keys 37.0 us
+  // (two on three 38.7).  Two: two on three, 200 rows x 2 tokens 26.4 us (three on two 33.3).  Four, single-warp: two on
+  // two, 64 rows x 32 tokens 121 us (three on two 166: spills); head_dim 64 two on three, 120 rows x 32 tokens 55.9 us (on
+  // two 59.3).  One, head_dim 64: two on three, 60 rows of 1000 to 8000 keys 30.6 us (three on three 34.7).
   if (a.dh == 128) {
-    if (nq == 1) return run_stream<128, 1, 2, 4, 3>(p, s);
+    if (nq == 1) return run_stream<128, 1, 3, 4, 2>(p, s);
     if (nq == 2) return many ? run_stream<128, 2, 2, 1, 2>(p, s) : run_stream<128, 2, 2, 4, 3>(p, s);
     return many ? run_stream<128, 4, 2, 1, 2>(p, s) : run_stream<128, 4, 2, 4, 2>(p, s);
   }
   if (nq == 1) return run_stream<64, 1, 2, 4, 3>(p, s);
   if (nq == 2) return many ? run_stream<64, 2, 2, 1, 3>(p, s) : run_stream<64, 2, 2, 4, 3>(p, s);
-  return many ? run_stream<64, 4, 2, 1, 2>(p, s) : run_stream<64, 4, 2, 4, 2>(p, s);
+  return many ? run_stream<64, 4, 2, 1, 3>(p, s) : run_stream<64, 4, 2, 4, 2>(p, s);
 }
 
 }  // namespace bs
