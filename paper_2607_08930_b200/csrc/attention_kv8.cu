@@ -69,9 +69,8 @@ __device__ __forceinline__ uint2 lds64(unsigned at) {
 //
 // What it reaches: 64 single-token rows of 1024 to 4096 keys (28 / 4 heads, 175 MB) 32 us of streaming, 5.5 TB/s of the
 // 6.5 measured for a copy, and 5 us of merge; two rows of 50,001 and 65,536 keys 23 us and 6.  64 rows x 32 tokens over
-// up to 1024 keys of 32 heads, 121 us, are bound by the instructions around the products instead - a block of 32 keys
-// takes a warp about 3600 clk, 1040 of them in its 128 products, with two warps per scheduler to overlap (255 registers,
-// most of them outputs).
+// up to 1024 keys of 32 heads, 122 us, are bound by the instructions around the products instead: a block of 32 keys is
+// decoded (about 500 clk) for only 16 query rows' 64 products (520 clk), with two warps per scheduler to overlap.
 //
 // Keys are the rows (M) of both products and the queries their columns (N), so that 8 query rows - a group of heads of
 // one token - fill an instruction.  Codes go to the tensor cores as fp16, which holds every e4m3 value (the warp-level
@@ -108,7 +107,7 @@ __global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(c
   using L = StreamSmem<DH, NQ, STAGES, W>;
   constexpr int KP = DH / 32;            // pairs of k steps of the scores
   constexpr int MD = DH / 16;            // m tiles of the output
-  constexpr int kHalves = NQ == 1 ? 2 : 1;             // (unrolled, the wider instantiations do not fit their registers)
+  constexpr int kHalves = NQ == 1 ? 2 : 1;             // (unrolled, two query tiles do not fit their registers)
   constexpr int R = L::R, LDO = L::LDO, TB = kTileBytes<DH>, kCost = item_cost(W);
   extern __shared__ unsigned char smem_raw[];
   __shared__ LineShared<kStreamThreads, L::groups> s_line;
@@ -463,8 +462,8 @@ __global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(c
 // fewer units than threads, up to 32 neighbouring lanes, each with every so-manieth part.
 constexpr int kMergeThreads = 256;
 // Weights of one CTA: parts x the rows it touches.  With b boundaries inside an item of at most R rows it is at most
-// (b + 1) (R / b + 2) <= 2 b + 2 R + 2; b < 4 x 592 with R = 32, fewer CTAs with R = 128.
-constexpr int kMergeWeights = 2 * kMaxStreamCtas * kStreamWarps + 66;
+// (b + 1) (R / b + 2) <= 2 b + 2 R + 2, with b < 4 x 592 and R <= 16.
+constexpr int kMergeWeights = 2 * kMaxStreamCtas * kStreamWarps + 34;
 template <int DH>
 __global__ void __launch_bounds__(kMergeThreads) k_attention_kv8_merge(const LineParams p, int R) {
   __shared__ float s_w[kMergeWeights];
@@ -564,18 +563,18 @@ __global__ void __launch_bounds__(kMergeThreads) k_attention_kv8_merge(const Lin
 }
 
 constexpr size_t kCutBytes = (size_t)kMaxStreamCtas * kStreamWarps * sizeof(Cut);
-// Query rows of all partial slots, two slots per worker: 296 CTAs of four single-warp workers with 32 rows, or 592
-// four-warp workers.  A launch takes no more CTAs than these hold.
-constexpr size_t kPartRows = 2 * (size_t)kStreamWarps * 296 * 32;
+// Query rows of all partial slots, two slots per worker: 592 CTAs of four single-warp workers with 16 rows.  A launch takes
+// no more CTAs than these hold.
+constexpr size_t kPartRows = 2 * (size_t)kStreamWarps * kMaxStreamCtas * 16;
 
 // Per device: how many CTAs of each instantiation one wave holds (0: not asked yet).
-struct DeviceInfo { int wave[24]; };
+struct DeviceInfo { int wave[16]; };
 DeviceInfo g_dev[kMaxDevices];
 std::mutex g_mutex;
 
 template <int DH, int NQ, int STAGES, int W, int MINB, bool DIRECT>
 cudaError_t run_as(const LineParams& p, cudaStream_t s) {
-  constexpr int index = (DH == 128 ? 6 : 0) + (NQ == 4 ? 2 : NQ - 1) * 2 + (W == 1 ? 1 : 0) + (DIRECT ? 12 : 0);
+  constexpr int index = (DH == 128 ? 4 : 0) + (NQ - 1) * 2 + (W == 1 ? 1 : 0) + (DIRECT ? 8 : 0);
   constexpr auto kernel = k_attention_kv8_stream<DH, NQ, STAGES, W, MINB, DIRECT>;
   constexpr int smem = StreamSmem<DH, NQ, STAGES, W>::total;
   DeviceInfo* d = device_slot(g_dev);
@@ -635,35 +634,36 @@ cudaError_t launch_attention_kv8(const AttnKv8Args& a, cudaStream_t s) {
   p.part_o = reinterpret_cast<float*>(at);
   at += up256(kPartRows * a.dh * sizeof(float));
   p.part_ml = reinterpret_cast<float2*>(at);
-  // More than 32 query rows per kv head fill a good part of the 128-row tensor-core tiles (16 rows of 320 to 800 keys: 35
-  // query rows 18.2 us, 20.2 by the streaming kernel, 224 19.9 and 38.6; 32 heads, 40 query rows 62 and 68).
-  if (widest > 32) return launch_attention_kv8_tc(a, static_cast<float*>(a.scratch), a.scratch_bytes / sizeof(float), s);
-  const int nq = widest <= 8 ? 1 : widest <= 16 ? 2 : 4;
+  // From 48 (head_dim 64: 96) query rows per kv head on the 128-row tensor-core tiles pay (16 rows of 320 to 800 keys, 7
+  // heads a group: 35 query rows 18.1 us, 15.4 by the streaming kernel, 112 19.4 and 24.7; 32 heads: 40 query rows 62 and
+  // 58, 64 63 and 71; head_dim 64, 96 query rows 14.6 and 12.0).  The streaming kernel's tiles hold a token's group of up to
+  // 16 heads.
+  if (G > 16 || widest > (a.dh == 128 ? 48 : 96)) return launch_attention_kv8_tc(a, static_cast<float*>(a.scratch), a.scratch_bytes / sizeof(float), s);
+  // 8 or 16 query rows per item.  (32, which reads a block once for all of a 32-token step, leaves two warps per scheduler
+  // with 255 registers: 20 rows x 32 tokens, 32 heads 38.2 us against 32.0 with 16, 64 rows 121 and 122.)
+  const int nq = widest <= 8 ? 1 : 2;
   p.tq = 8 * nq / G;
-  // Single-warp workers where there are more items than warps to hold them (6 CTAs of work for every SM), and each is
-  // work for a warp: from two query tiles on.  100 to 500 keys: 300 rows x 2 tokens, 7 heads a group, 1200 items 34.3 us
-  // (35.5 with four-warp workers), 120 x 32 tokens, head_dim 64, 1920 items 59 us (73); 800 items 29.2 us (26.4); one query
-  // tile, 800 items 20.9 us (19.3).
+  // Single-warp workers where there are many items and two query tiles make each of them work for a warp.  64 rows x 32
+  // tokens, 32 heads, 4096 items: 200 to 512 keys 89 us (107 with four-warp workers), 96 to 1024 122 us (131); 1280 items:
+  // 96 to 500 keys 31.9 us (34.4), but 500 to 3000 114 us (106); 800 items 29.4 us (26.2).
   const long long items = (long long)a.n_rows * a.hkv * ((max_nq + p.tq - 1) / p.tq);
-  const bool many = nq > 1 && items >= 6 * 148;
+  const bool many = nq > 1 && items >= (a.max_vis > 0 && a.max_vis <= 512 ? 6 : 16) * 148;
   // Short rows have a worker per item and nothing to merge; so do rows of some length where there are about as many items
   // as workers fit the machine.  Four-warp workers: 2 rows of up to 1524 keys 10.1 us, 15.5 by the line; 2 rows of up to
-  // 15,778 60 and 13; 480 items of up to 3000 59 and 66; 256 items of up to 4000 41 and 38.  Single-warp workers: 1280
-  // items of up to 300 keys 48 us, 59 by the line; 2048 items of up to 1024 126 and 121.
+  // 15,778 60 and 13; 480 items of up to 3000 59 and 66; 256 items of up to 4000 41 and 38.  Single-warp workers: 4096
+  // items of up to 512 keys 89 us, 95 by the line; of up to 1024 130 and 122.
   const int reach = many ? 512 : items >= 400 ? 4096 : 2048;
   p.direct = a.max_vis > 0 && a.max_vis <= reach ? (max_nq + p.tq - 1) / p.tq : 0;
   // Stages and CTAs per SM.  One query tile, head_dim 128: three stages on two CTAs, 64 rows of 1024 to 4096 keys 37.0 us
-  // (two on three 38.7).  Two: two on three, 200 rows x 2 tokens 26.4 us (three on two 33.3).  Four, single-warp: two on
-  // two, 64 rows x 32 tokens 121 us (three on two 166: spills); head_dim 64 two on three, 120 rows x 32 tokens 55.9 us (on
-  // two 59.3).  One, head_dim 64: two on three, 60 rows of 1000 to 8000 keys 30.6 us (three on three 34.7).
+  // (two on three 38.7); head_dim 64: two on three, 60 rows of 1000 to 8000 keys 30.6 us (three on three 34.7).  Two query
+  // tiles, head_dim 128, four-warp: two on three, 200 rows x 2 tokens 26.4 us (three on two 33.3); single-warp: two on two,
+  // 64 rows x 32 tokens 122 us (two on three, which spills, 125).
   if (a.dh == 128) {
     if (nq == 1) return run_stream<128, 1, 3, 4, 2>(p, s);
-    if (nq == 2) return many ? run_stream<128, 2, 2, 1, 2>(p, s) : run_stream<128, 2, 2, 4, 3>(p, s);
-    return many ? run_stream<128, 4, 2, 1, 2>(p, s) : run_stream<128, 4, 2, 4, 2>(p, s);
+    return many ? run_stream<128, 2, 2, 1, 2>(p, s) : run_stream<128, 2, 2, 4, 3>(p, s);
   }
   if (nq == 1) return run_stream<64, 1, 2, 4, 3>(p, s);
-  if (nq == 2) return many ? run_stream<64, 2, 2, 1, 3>(p, s) : run_stream<64, 2, 2, 4, 3>(p, s);
-  return many ? run_stream<64, 4, 2, 1, 3>(p, s) : run_stream<64, 4, 2, 4, 2>(p, s);
+  return many ? run_stream<64, 2, 2, 1, 3>(p, s) : run_stream<64, 2, 2, 4, 3>(p, s);
 }
 
 }  // namespace bs
