@@ -638,7 +638,10 @@ cudaError_t launch_attention_kv8(const AttnKv8Args& a, cudaStream_t s) {
   // heads a group: 35 query rows 18.1 us, 15.4 by the streaming kernel, 112 19.4 and 24.7; 32 heads: 40 query rows 62 and
   // 58, 64 63 and 71; head_dim 64, 96 query rows 14.6 and 12.0).  The streaming kernel's tiles hold a token's group of up to
   // 16 heads.
-  if (G > 16 || widest > (a.dh == 128 ? 48 : 96)) return launch_attention_kv8_tc(a, static_cast<float*>(a.scratch), a.scratch_bytes / sizeof(float), s);
+  // Rows of up to 96 keys do not fill a key tile and are streamed whatever the width (16 rows x 32 tokens, 7 heads a group: 43
+  // keys 8.6 us, tcgen05 11.5, 100 keys 10.6 and 11.8; 200 rows: 64 keys 82 and 105, 128 keys 108 and 106).
+  const bool brief = a.max_vis > 0 && a.max_vis <= 96;
+  if (G > 16 || (!brief && widest > (a.dh == 128 ? 48 : 96))) return launch_attention_kv8_tc(a, static_cast<float*>(a.scratch), a.scratch_bytes / sizeof(float), s);
   // 8 or 16 query rows per item.  (32, which reads a block once for all of a 32-token step, leaves two warps per scheduler
   // with 255 registers: 20 rows x 32 tokens, 32 heads 38.2 us against 32.0 with 16, 64 rows 121 and 122.)
   const int nq = widest <= 8 ? 1 : 2;
