@@ -158,7 +158,7 @@ struct TcParams {
   const int* cu_q;
   const int* kv_base;
   const int* vis;
-  int n_rows, M, hq, hkv;
+  int n_rows, M, hq, hkv, G;   // G = hq / hkv
   int tq;            // query tokens per query tile
   int per_row;       // spans of a row that have a CTA of their own
   int chunks;        // key chunks per row; > 1: partials instead of the output
@@ -194,10 +194,11 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
   pdl_trigger();
 
   // ---- the work item ----
-  const int G = p.hq / p.hkv, per_cta = NT * p.tq;
+  const int G = p.G, per_cta = NT * p.tq;
   // A CTA is (span, key chunk, kv head), heads next to each other.  Spans [0, n_rows per_row): the first per_row of every
   // row.  Behind them: the rest, if a row has any, by slots that need no prefix (row i's begin at cu[i] / per_cta + i).
-  const int unit = (int)blockIdx.x / p.hkv, kh = (int)blockIdx.x - unit * p.hkv, at = unit / p.chunks, chunk = unit - at * p.chunks;
+  const int unit = (int)(blockIdx.x / (unsigned)p.hkv), kh = (int)blockIdx.x - unit * p.hkv;
+  const int at = p.chunks == 1 ? unit : unit / p.chunks, chunk = unit - at * p.chunks;
   const int slot = at - p.n_rows * p.per_row;
   const int row = slot < 0 ? at / p.per_row
                            : warp_search(p.n_rows, slot, [&](int i) { return __ldcg(p.cu_q + i) / per_cta + i; });
@@ -378,46 +379,56 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
       const int pl = lane % LPR, f0 = quad * 32 + lane / LPR;
       const unsigned place = sQ + x * 2 * L::q_part + quad * 32 * DH;
       const unsigned mine = place + (lane >> 4) * L::q_part + (lane & 15) * 16;
-      int head = f0 % G, tok = f0 / G;
-#pragma unroll 1
+      const unsigned by_G = (65536u + G - 1) / G;            // f / G = f by_G >> 16 for f < 128
+#pragma unroll 4
       for (int i = 0; i < LPR; ++i) {
-        const bool valid = f0 + i * RPI < nrows;
-        const bf16* src = p.q + (size_t)(t0 + x * p.tq + (valid ? tok : 0)) * p.q_ld + (kh * G + head) * DH + pl * 8;
+        const int f = f0 + i * RPI;
+        const bool valid = f < nrows;
+        const int tok = valid ? (int)(f * by_G >> 16) : 0, head = valid ? f - tok * G : 0;
+        const bf16* src = p.q + (size_t)(t0 + x * p.tq + tok) * p.q_ld + (kh * G + head) * DH + pl * 8;
         asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(mine + i * 256), "l"(src), "r"(valid ? 16 : 0) : "memory");
-        head += RPI;
-        while (head >= G) {
-          head -= G;
-          ++tok;
-        }
       }
       asm volatile("cp.async.wait_all;" ::: "memory");
-#pragma unroll 2
-      for (int i = 0; i < LPR; ++i) {
-        const uint4 raw = lds128(mine + i * 256);
+      constexpr int FLY = 4;                                 // steps whose chains of shuffles and conversions overlap
+#pragma unroll 1
+      for (int i0 = 0; i0 < LPR; i0 += FLY) {
+        uint4 raw[FLY];
+        __nv_bfloat162 top2[FLY];
+#pragma unroll
+        for (int u = 0; u < FLY; ++u) raw[u] = lds128(mine + (i0 + u) * 256);
         __syncwarp();
-        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&raw);
-        __nv_bfloat162 top2 = __hmax2(__hmax2(__habs2(h[0]), __habs2(h[1])), __hmax2(__habs2(h[2]), __habs2(h[3])));
 #pragma unroll
-        for (int o = LPR / 2; o > 0; o >>= 1) top2 = __hmax2(top2, __shfl_xor_sync(0xffffffffu, top2, o));
-        const float top = fmaxf(__low2float(top2), __high2float(top2));
-        const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 100);
-        const float up = pow2i(7 - e);
-        const int f = f0 + i * RPI;
-        if (pl == 0) s_sc[x * 128 + f] = pow2i(e - 7) * (1.4426950408889634f * rsqrtf((float)DH));
-        unsigned hi[2] = {0u, 0u}, lo[2] = {0u, 0u};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float2 v = __bfloat1622float2(h[j]);
-          const float a = v.x * up, b = v.y * up;
-          const unsigned near = kv8_encode2(a, b), back = kv8_decode2((unsigned short)near);
-          const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&back));
-          hi[j >> 1] |= near << (16 * (j & 1));
-          lo[j >> 1] |= kv8_encode2(a - y.x, b - y.y) << (16 * (j & 1));
+        for (int u = 0; u < FLY; ++u) {
+          const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&raw[u]);
+          top2[u] = __hmax2(__hmax2(__habs2(h[0]), __habs2(h[1])), __hmax2(__habs2(h[2]), __habs2(h[3])));
         }
-        const int turn = DH == 128 ? f & 7 : (f >> 1) & 3;     // the swizzle of 128- and of 64-byte rows
-        const unsigned at = sQ + x * 2 * L::q_part + f * DH + (((pl >> 1) ^ turn) << 4) + (pl & 1) * 8;
-        sts64(at, hi[0], hi[1]);
-        sts64(at + L::q_part, lo[0], lo[1]);
+#pragma unroll
+        for (int o = LPR / 2; o > 0; o >>= 1)
+#pragma unroll
+          for (int u = 0; u < FLY; ++u) top2[u] = __hmax2(top2[u], __shfl_xor_sync(0xffffffffu, top2[u], o));
+#pragma unroll
+        for (int u = 0; u < FLY; ++u) {
+          const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&raw[u]);
+          const float top = fmaxf(__low2float(top2[u]), __high2float(top2[u]));
+          const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 100);
+          const float up = pow2i(7 - e);
+          const int f = f0 + (i0 + u) * RPI;
+          if (pl == 0) s_sc[x * 128 + f] = pow2i(e - 7) * (1.4426950408889634f * rsqrtf((float)DH));
+          unsigned hi[2] = {0u, 0u}, lo[2] = {0u, 0u};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float2 v = __bfloat1622float2(h[j]);
+            const float a = v.x * up, b = v.y * up;
+            const unsigned near = kv8_encode2(a, b), back = kv8_decode2((unsigned short)near);
+            const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&back));
+            hi[j >> 1] |= near << (16 * (j & 1));
+            lo[j >> 1] |= kv8_encode2(a - y.x, b - y.y) << (16 * (j & 1));
+          }
+          const int turn = DH == 128 ? f & 7 : (f >> 1) & 3;   // the swizzle of 128- and of 64-byte rows
+          const unsigned at = sQ + x * 2 * L::q_part + f * DH + (((pl >> 1) ^ turn) << 4) + (pl & 1) * 8;
+          sts64(at, hi[0], hi[1]);
+          sts64(at + L::q_part, lo[0], lo[1]);
+        }
       }
       fence_smem_for_mma();
     }
@@ -669,7 +680,7 @@ cudaError_t run_tc(const AttnKv8Args& a, float* part, size_t part_floats, int sm
   TcParams p;
   p.q = a.q; p.q_ld = a.q_ld; p.k_scale = a.cache.k_scale; p.v_scale = a.cache.v_scale; p.n_blocks = a.cache.n_blocks;
   p.out = a.out; p.cu_q = a.cu_q; p.kv_base = a.kv_base; p.vis = a.vis;
-  p.n_rows = a.n_rows; p.M = a.M; p.hq = a.hq; p.hkv = a.hkv; p.error_flag = a.error_flag;
+  p.n_rows = a.n_rows; p.M = a.M; p.hq = a.hq; p.hkv = a.hkv; p.G = G; p.error_flag = a.error_flag;
   p.tq = 128 / G;
   // Two query tiles per CTA share every key tile it loads and converts (6 rows of 1200 to 2304 tokens, 7 heads a group: 379
   // us, 552 with one; 3 rows of 600 to 700 49 and 72); one per CTA fills the SMs when there are few.
