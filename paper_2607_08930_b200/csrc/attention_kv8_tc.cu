@@ -134,6 +134,12 @@ __device__ __forceinline__ void tmem_st32(unsigned taddr, const unsigned* w) {
       : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// two fp16 values -> two e4m3 codes, to nearest even
+__device__ __forceinline__ unsigned encode_half2(__half2 x) {
+  unsigned short r;
+  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(*reinterpret_cast<const unsigned*>(&x)));
+  return r;
+}
 __device__ __forceinline__ uint4 lds128(unsigned at) {
   uint4 v;
   asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
@@ -413,16 +419,18 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
           const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 100);
           const float up = pow2i(7 - e);
           const int f = f0 + (i0 + u) * RPI;
-          if (pl == 0) s_sc[x * 128 + f] = pow2i(e - 7) * (1.4426950408889634f * rsqrtf((float)DH));
+          // (an infinite element would saturate: its row becomes NaN here, as its softmax is)
+          const float sc = pow2i(e - 7) * (1.4426950408889634f * rsqrtf((float)DH));
+          if (pl == 0) s_sc[x * 128 + f] = top < INFINITY ? sc : __int_as_float(0x7fffffff);
           unsigned hi[2] = {0u, 0u}, lo[2] = {0u, 0u};
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
+            // (fp16 holds the scaled element but for what lies 2^-32 under the row's largest)
             const float2 v = __bfloat1622float2(h[j]);
-            const float a = v.x * up, b = v.y * up;
-            const unsigned near = kv8_encode2(a, b), back = kv8_decode2((unsigned short)near);
-            const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&back));
+            const __half2 y = __floats2half2_rn(v.x * up, v.y * up);
+            const unsigned near = encode_half2(y), back = kv8_decode2((unsigned short)near);
             hi[j >> 1] |= near << (16 * (j & 1));
-            lo[j >> 1] |= kv8_encode2(a - y.x, b - y.y) << (16 * (j & 1));
+            lo[j >> 1] |= encode_half2(__hsub2(y, *reinterpret_cast<const __half2*>(&back))) << (16 * (j & 1));
           }
           const int turn = DH == 128 ? f & 7 : (f >> 1) & 3;   // the swizzle of 128- and of 64-byte rows
           const unsigned at = sQ + x * 2 * L::q_part + f * DH + (((pl >> 1) ^ turn) << 4) + (pl & 1) * 8;

@@ -687,3 +687,18 @@ def test_a_few_long_rows_in_many_chunks(B, hq, hkv, dh, rows):
     out = B.op_attention_kv8(q.cuda(), k8, v8, ks, vs, ints(prefix(n)), ints(base), ints(vis), hq, max_nq=int(n.max()),
                              max_vis=int(vis.max()))
     check_attention(host(out), q, hq, dh, n, vis, base, kc, vc)
+
+
+@pytest.mark.parametrize("hq,hkv,dh,nq,vis", [(14, 2, 128, 1, 200), (14, 2, 128, 40, 90), (14, 2, 128, 40, 200), (8, 2, 64, 64, 333),
+                                              (28, 4, 128, 600, 700)])
+@pytest.mark.parametrize("what", [float("inf"), float("-inf"), float("nan")])
+def test_what_is_not_finite_stays_in_its_query_row(B, hq, hkv, dh, nq, vis, what):
+    rng = np.random.default_rng(nq)
+    n, vis, base, kc, vc, q = attn_inputs(rng, hq, hkv, dh, [(nq, vis)])
+    q[0, dh + 5] = what
+    (k8, ks), (v8, vs) = to_gpu(*kc), to_gpu(*vc)
+    out = host(B.op_attention_kv8(q.cuda(), k8, v8, ks, vs, ints([0, nq]), ints(base), ints(vis), hq, max_nq=nq, max_vis=int(vis[0])))
+    out = out.reshape(nq, hq, dh)
+    assert np.isnan(out[0, 1]).all()
+    out[0, 1] = 0
+    assert np.isfinite(out).all()
