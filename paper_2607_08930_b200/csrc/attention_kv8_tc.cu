@@ -19,13 +19,14 @@
 // Weights are formed against a running reference that lags the maximum (kTcBias, kTcGrow): the output is rescaled only
 // when a row's maximum has outgrown it.
 //
-// What bounds it: 6 rows of 1200 to 2304 tokens (28 / 4 heads, head_dim 128) 378 us, 758 TFLOP/s counted as a 16-bit
-// attention, 45 % of the measured matrix rate.  Of a 128-key step of two query tiles, about 4000 clk, the tensor pipe
+// What bounds it: 6 rows of 1200 to 2304 tokens (28 / 4 heads, head_dim 128) 361 us, 793 TFLOP/s counted as a 16-bit
+// attention, 47 % of the measured matrix rate.  Of a 128-key step of two query tiles, about 3900 clk, the tensor pipe
 // works for 2600 (1024 per tile at the full rate; the halves of the scores, 128 x 64 x 32 from shared memory, take 49 clk
 // instead of 32) and each scheduler's exponentials take 2048; the two softmax warps of a scheduler overlap them with their
-// other work only in part.  Scores of 128 keys at once (two passes over them, no spare half) measured 480 us.
-// A CTA's beginning - indices, barriers, queries to two terms - is about 4 us of 45; 16 block steps of 32 tokens over 320 to
-// 800 keys, one query tile per CTA, are bound by it and by the chain of seven tiles: 19.4 us.
+// other work only in part.  Scores of 128 keys at once (two passes over them, no spare half) took 480 us where halves with
+// the same way of issuing took 529, and 398 with products issued by an elected lane.  16 block steps of 32 tokens over 320
+// to 800 keys, one query tile per CTA, 17.9 us, are bound by a CTA's beginning - indices, barriers, queries to two terms:
+// 4 us - and by its chain of three to seven tiles.
 // Every wait is bounded; on a timeout the flag is raised, all roles drain, the copies in flight are waited for.
 #include <math.h>
 

@@ -9,8 +9,8 @@
 //
 // Measured against a copy's 6.5 TB/s: norms and rotation into the bf16 cache, 16 rows of 320 to 1024 tokens (28 / 4 heads,
 // head_dim 128, 191 MB) 35.4 us, 5.4 TB/s (three heads in flight per lane and CTAs of four warps; four heads 39 us, eight
-// warps 40 us); the same pass into the 8-bit cache, 32 heads, 308 MB, 66 us, 4.7 TB/s (the tiles' rows are 256 bytes every
-// 24 KB, and a tile waits for its scale); reading back, 617 MB, 102 us, 6.0 TB/s (a whole tile in flight per warp; half of
+// warps 40 us); the same pass into the 8-bit cache, 32 heads, 308 MB, 63 us, 4.9 TB/s (a tile waits for its scale, and the
+// instructions of norm, rotation, maximum and encoding take two thirds of the issue slots); reading back, 617 MB, 102 us, 6.0 TB/s (a whole tile in flight per warp; half of
 // one 108 us).  A single-token batch is latency: 64 tokens 2.7 us, three trips to memory.
 #include <math.h>
 
@@ -251,18 +251,33 @@ __device__ __forceinline__ void decode16(const HeadLoad& v, float scale, float* 
     }
   }
 }
-// Largest finite magnitude, as its bits (they order like the magnitudes; infinities and NaN count nothing).
-__device__ __forceinline__ unsigned largest_finite(const float* x, bool counts) {
-  unsigned top = 0;
+// Largest finite magnitude over the warp, as its bits (they order like the magnitudes; infinities and NaN count nothing).
+// The maximum passes NaN by; where it is infinite, which is rare, every element is looked at.
+__device__ __forceinline__ unsigned largest_finite(const float* x, float top, bool counts) {
+  if (counts && top == INFINITY) {
+    top = 0.f;
 #pragma unroll
-  for (int j = 0; j < 16; ++j) {
-    const unsigned b = __float_as_uint(x[j]) & 0x7fffffffu;
-    top = max(top, b < 0x7f800000u ? b : 0u);
+    for (int j = 0; j < 16; ++j)
+      if (fabsf(x[j]) < INFINITY) top = fmaxf(top, fabsf(x[j]));
   }
-  return __reduce_max_sync(0xffffffffu, counts ? top : 0u);
+  return __reduce_max_sync(0xffffffffu, counts ? __float_as_uint(top) : 0u);
+}
+__device__ __forceinline__ float largest16(const float* x) {
+  float top = 0.f;
+#pragma unroll
+  for (int j = 0; j < 16; j += 2) asm("max.f32 %0, %0, %1, %2;" : "+f"(top) : "f"(fabsf(x[j])), "f"(fabsf(x[j + 1])));
+  return top;
+}
+__device__ __forceinline__ float largest16(const HeadLoad& v) {
+  const __nv_bfloat162* a = reinterpret_cast<const __nv_bfloat162*>(&v.lo);
+  const __nv_bfloat162* b = reinterpret_cast<const __nv_bfloat162*>(&v.hi);
+  __nv_bfloat162 top = __floats2bfloat162_rn(0.f, 0.f);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) top = __hmax2(top, __hmax2(__habs2(a[j]), __habs2(b[j])));
+  return fmaxf(__low2float(top), __high2float(top));
 }
 
-// Three CTAs of 256 threads per SM (80 registers; two of 110 measured 76 us against 66 on 16 whole rows of 32 heads).
+// Three CTAs of 256 threads per SM (80 registers; two of 110 measured 76 us where three took 66, 16 whole rows of 32 heads).
 // One CTA: the K and V tiles of kv heads [g0, g1) of one cache block.  A thread owns one row of the block and keeps its
 // angles in registers from head to head; the next head's rows are fetched while this one's are turned.  New rows are
 // formed in registers, kept rows decoded beside them, the largest magnitude of both gives the scale, and all are encoded
@@ -270,7 +285,7 @@ __device__ __forceinline__ unsigned largest_finite(const float* x, bool counts) 
 // MIXED: the block also has rows that are not written - a span's first or last one.
 template <int DH, bool MIXED>
 __device__ __forceinline__ void write_tiles(const QkNormArgs& a, const Slot& s, const Kv8Cache& c, int g0, int g1,
-                            unsigned (*s_max)[2][kTileThreads<DH> / 32]) {
+                            unsigned (*s_max)[2][kTileThreads<DH> / 32], float4* s_gain) {
   constexpr int LPH = DH / 16, W = kTileThreads<DH> / 32;
   const int p = threadIdx.x % LPH, r = threadIdx.x / LPH, at = s.first + r;
   const int heads = a.hq + 2 * a.hkv;
@@ -296,6 +311,11 @@ __device__ __forceinline__ void write_tiles(const QkNormArgs& a, const Slot& s, 
     }
   };
   fetch(g0);
+  if (a.k_gain && threadIdx.x < DH) {
+    const int d = threadIdx.x, lane_of = d % (DH / 2) / 8, q = d / (DH / 2) * 2 + d % 8 / 4;
+    reinterpret_cast<float*>(s_gain)[(q * LPH + lane_of) * 4 + d % 4] = __bfloat162float(a.k_gain[d]);
+  }
+  __syncthreads();
   float2 cs[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) cs[j] = make_float2(1.f, 0.f);
@@ -318,16 +338,25 @@ __device__ __forceinline__ void write_tiles(const QkNormArgs& a, const Slot& s, 
     auto v_row = [&] {
       if (MIXED && state == 1) decode16(vc, old_v, x); else unpack16(vc, x);
     };
-    v_row();
-    unsigned top_v = largest_finite(x, state != 0);
+    float top = MIXED || !(largest16(vc) < INFINITY) ? (v_row(), largest16(x)) : largest16(vc);
+    unsigned top_v = largest_finite(x, top, state != 0);
     if (MIXED && state == 1) decode16(k, old_k, x); else unpack16(k, x);
     if (head + 1 < g1) fetch(head + 1);
     const float rms = a.k_gain ? head_rms<DH>(x, a.eps) : 0.f;
     if (state == 2) {
-      if (a.k_gain) head_gain<DH>(x, rms, a.k_gain, p);
+      if (a.k_gain) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float4 g = s_gain[i * LPH + p];
+          x[4 * i] *= rms * g.x;
+          x[4 * i + 1] *= rms * g.y;
+          x[4 * i + 2] *= rms * g.z;
+          x[4 * i + 3] *= rms * g.w;
+        }
+      }
       head_rotate(x, cs);
     }
-    unsigned top_k = largest_finite(x, state != 0);
+    unsigned top_k = largest_finite(x, largest16(x), state != 0);
     unsigned (*place)[W] = s_max[(head - g0) & 1];         // the head before the last is done with it: one barrier a head
     if ((threadIdx.x & 31) == 0) {
       place[0][threadIdx.x >> 5] = top_k;
@@ -362,6 +391,7 @@ __global__ void __launch_bounds__(kTileThreads<DH>, 768 / kTileThreads<DH>) k_qk
                                                                        Kv8Cache c, int q_ctas, int shares, int per_share,
                                                                        int per_cta) {
   __shared__ unsigned s_max[2][2][kTileThreads<DH> / 32];
+  __shared__ float4 s_gain[DH / 4];      // k_gain as floats, by the lanes' order: [four dims of a lane][lane]
   pdl_wait();
   pdl_trigger();
   if ((int)blockIdx.x < q_ctas) {
@@ -377,9 +407,9 @@ __global__ void __launch_bounds__(kTileThreads<DH>, 768 / kTileThreads<DH>) k_qk
   if (!find_slot(slot, cu_q, kv_base, kv_at, kv_len, n_rows, a.M, c.n_blocks, a.error_flag, s)) return;
   const int g1 = min(a.hkv, g0 + per_cta);
   if (s.first < s.at || s.first + kKv8Block > s.at + s.n)
-    write_tiles<DH, true>(a, s, c, g0, g1, s_max);
+    write_tiles<DH, true>(a, s, c, g0, g1, s_max, s_gain);
   else
-    write_tiles<DH, false>(a, s, c, g0, g1, s_max);
+    write_tiles<DH, false>(a, s, c, g0, g1, s_max, s_gain);
 }
 
 // One warp: one (head, K or V) tile of a work slot at a time, all of it in flight at once; a CTA takes `per_cta` tiles of
@@ -443,7 +473,7 @@ void head_shares(int M, int heads, int dh, int warps, int* shares, int* per_shar
   *shares = (passes + each - 1) / each;
 }
 // Of `n` items of each of `slots` work slots: how many one CTA takes, so that a slot's indices and angles are fetched for
-// as many as leave eight CTAs per SM (three: 16 whole rows written in 69.5 us instead of 66, read in 107 instead of 102).
+// as many as leave eight CTAs per SM (three: 16 whole rows written in 69.5 us where eight took 66, read in 107 and 102).
 int items_per_cta(long long slots, int n, int least) {
   int per = n;
   while (per > least && slots * ((n + per - 1) / per) < 148 * 8) per = (per + 1) / 2;
