@@ -1030,8 +1030,9 @@ int bs_op_kv8_read(const void* k8, const void* v8, const float* k_scale, const f
   if (total < 0 || n_rows < 1 || !kv8_shape_ok(n_kv_heads, n_kv_heads, head_dim) || !aligned16({k_out, v_out}) || !cu ||
       !kv_base || !kv_at || !kv8_cache_of(k8, v8, k_scale, v_scale, kv_rows, &c))
     return BS_E_ARG;
-  return launch_kv8_read(c, cu, kv_base, kv_at, n_rows, total, n_kv_heads, head_dim, (bf16*)k_out, (bf16*)v_out, error_flag,
-                         (cudaStream_t)stream) == cudaSuccess ? BS_OK : BS_E_CUDA;
+  const cudaError_t r = launch_kv8_read(c, cu, kv_base, kv_at, n_rows, total, n_kv_heads, head_dim, (bf16*)k_out,
+                                        (bf16*)v_out, error_flag, (cudaStream_t)stream);
+  return r == cudaSuccess ? BS_OK : (r == cudaErrorInvalidValue ? BS_E_ARG : BS_E_CUDA);
 }
 
 size_t bs_op_attention_kv8_scratch_bytes(int n_q_heads, int n_kv_heads, int head_dim) {
