@@ -69,7 +69,7 @@ __device__ __forceinline__ uint2 lds64(unsigned at) {
 //
 // What it reaches: 64 single-token rows of 1024 to 4096 keys (28 / 4 heads, 175 MB) 32 us of streaming, 5.5 TB/s of the
 // 6.5 measured for a copy, and 5 us of merge; two rows of 50,001 and 65,536 keys 23 us and 6.  64 rows x 32 tokens over
-// up to 1024 keys of 32 heads, 122 us, are bound by the instructions around the products instead: a block of 32 keys is
+// up to 1024 keys of 32 heads, 117 us, are bound by the instructions around the products instead: a block of 32 keys is
 // decoded (about 500 clk) for only 16 query rows' 64 products (520 clk), with two warps per scheduler to overlap.
 //
 // Keys are the rows (M) of both products and the queries their columns (N), so that 8 query rows - a group of heads of
@@ -107,7 +107,6 @@ __global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(c
   using L = StreamSmem<DH, NQ, STAGES, W>;
   constexpr int KP = DH / 32;            // pairs of k steps of the scores
   constexpr int MD = DH / 16;            // m tiles of the output
-  constexpr int kHalves = NQ == 1 ? 2 : 1;             // (unrolled, two query tiles do not fit their registers)
   constexpr int R = L::R, LDO = L::LDO, TB = kTileBytes<DH>, kCost = item_cost(W);
   extern __shared__ unsigned char smem_raw[];
   __shared__ LineShared<kStreamThreads, L::groups> s_line;
@@ -257,7 +256,7 @@ __global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(c
       asm volatile("cp.async.wait_group %0;\n" ::"n"(STAGES - 1) : "memory");
       __syncwarp();
       const unsigned kt = ring + (unsigned)stage * 2 * TB, vt = kt + TB;
-#pragma unroll kHalves
+#pragma unroll
       for (int m = 0; m < 2; ++m) {                    // 16 keys: rows 16 m + g and 16 m + g + 8 of this lane
         float s[NQ][4];
 #pragma unroll
