@@ -378,8 +378,10 @@ int bs_op_kv8_read(const void* k8, const void* v8, const float* k_scale, const f
  * be anything, NaN included.  q bf16, row stride q_ld elements (a multiple of 8): q_out of the operators above, or
  * the query part of a qkv buffer.  max_nq (0: unknown) and max_vis (0: unknown) are the largest query count and vis of
  * a row; they choose the kernel, not the result's meaning.  At most BS_KV8_MAX_ROWS rows and 32 query heads per kv
- * head.  scratch: bs_op_attention_kv8_scratch_bytes bytes of device memory, overwritten. */
+ * head.  scratch: bs_op_attention_kv8_scratch_bytes bytes of device memory, overwritten; may be NULL for sizes of which
+ * bs_op_attention_kv8_uses_scratch says 0 (whole items by workers of their own, keys that are not cut). */
 size_t bs_op_attention_kv8_scratch_bytes(int n_q_heads, int n_kv_heads, int head_dim);
+int bs_op_attention_kv8_uses_scratch(int n_rows, int M, int max_nq, int max_vis, int n_q_heads, int n_kv_heads, int head_dim);
 int bs_op_attention_kv8(const void* q, int q_ld, const void* k8, const void* v8, const float* k_scale,
                         const float* v_scale, long long kv_rows, void* out, const int* cu_q, const int* kv_base,
                         const int* vis, int n_rows, int M, int max_nq, int max_vis, int n_q_heads, int n_kv_heads,

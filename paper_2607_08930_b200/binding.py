@@ -68,7 +68,8 @@ EXPORTS = ["bs_query_sizes", "bs_init_model", "bs_admit", "bs_evict_refill", "bs
            "bs_debug_force_commit", "bs_debug_snapshot", "bs_debug_restore", "bs_op_gemm", "bs_op_gemm_cluster_splits",
            "bs_op_rmsnorm", "bs_op_rope_kv", "bs_op_rope_kv_static", "bs_op_attention_q_tile", "bs_op_attention", "bs_op_confidence",
            "bs_op_lm_head_confidence", "bs_op_lm_head_confidence_scratch_bytes", "bs_rope_table", "bs_op_qk_norm_rope_kv",
-           "bs_op_qk_norm_rope_kv8", "bs_op_kv8_read", "bs_op_attention_kv8", "bs_op_attention_kv8_scratch_bytes"]
+           "bs_op_qk_norm_rope_kv8", "bs_op_kv8_read", "bs_op_attention_kv8", "bs_op_attention_kv8_scratch_bytes",
+           "bs_op_attention_kv8_uses_scratch"]
 
 _lib = None
 
@@ -121,6 +122,7 @@ def lib() -> C.CDLL:
         L.bs_op_kv8_read.argtypes = [vp, vp, vp, vp, ll, vp, vp, vp, i, i, i, i, vp, vp, vp, vp]
         L.bs_op_attention_kv8_scratch_bytes.argtypes = [i, i, i]
         L.bs_op_attention_kv8_scratch_bytes.restype = C.c_size_t
+        L.bs_op_attention_kv8_uses_scratch.argtypes = [i] * 7
         L.bs_op_attention_kv8.argtypes = [vp, i, vp, vp, vp, vp, ll, vp, vp, vp, vp, i, i, i, i, i, i, i, vp, C.c_size_t,
                                           vp, vp]
         _lib = L
@@ -451,6 +453,7 @@ KV8_BLOCK, KV8_MAX_ROWS = 32, 1024
 _BF16, _F32, _I32, _E4M3, _U8 = torch.bfloat16, torch.float32, torch.int32, torch.float8_e4m3fn, torch.uint8
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda dev: torch.cuda.current_stream(dev).cuda_stream)      # the handle alone: a fiftieth of the Stream object's cost
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _refuse(name: str, why: str) -> None:
@@ -470,7 +473,7 @@ def _call(name: str, dev: int, fn, *args) -> None:
     """The library's kernels go to the current stream of the tensors' device, whatever device is current."""
     if dev < 0:
         _refuse(name, "the operators run on CUDA tensors only")
-    if torch.cuda.current_device() == dev:
+    if _current_device() == dev:
         rc = fn(*args, _raw_stream(dev))
     else:
         with torch.cuda.device(dev):
@@ -500,11 +503,27 @@ def _kv8_shape(name: str, dev: int, k8, v8, k_scale, v_scale):
     """(kv_rows, kv heads, head_dim) of an 8-bit cache."""
     shape = k8.shape
     blocks, hkv, rows, dh = shape if len(shape) == 4 else (0, 0, 0, 0)
-    if rows != KV8_BLOCK or v8.shape != shape or k_scale.shape != (blocks, hkv) or v_scale.shape != (blocks, hkv):
+    scales = (blocks, hkv)
+    if rows != KV8_BLOCK or v8.shape != shape or k_scale.shape != scales or v_scale.shape != scales:
         _refuse(name, "an 8-bit cache is codes [blocks, kv heads, 32, head_dim] and scales [blocks, kv heads]")
-    _need(name, dev, _E4M3, 1, "k8 v8", k8, v8)
-    _need(name, dev, _F32, 1, "k_scale v_scale", k_scale, v_scale)
+    # (all in one expression: a call of a small batch costs the host more than the device; what is wrong is found below)
+    if not (k8.dtype is v8.dtype is _E4M3 and k_scale.dtype is v_scale.dtype is _F32 and blocks and hkv and dh and
+            k8.get_device() == v8.get_device() == k_scale.get_device() == v_scale.get_device() == dev and
+            k8.is_contiguous() and v8.is_contiguous() and k_scale.is_contiguous() and v_scale.is_contiguous()):
+        _need(name, dev, _E4M3, 1, "k8 v8", k8, v8)
+        _need(name, dev, _F32, 1, "k_scale v_scale", k_scale, v_scale)
     return blocks * KV8_BLOCK, hkv, dh
+
+
+def _rows_of(name: str, dev: int, args: str, cu, *tensors) -> int:
+    """Number of rows of an index set: cu [n + 1] and tensors of at least n elements."""
+    n = cu.numel() - 1
+    if cu.dtype is not _I32 or n < 0 or cu.get_device() != dev or not cu.is_contiguous():
+        _need(name, dev, _I32, 1, args, cu)
+    for t in tensors:
+        if t.dtype is not _I32 or t.numel() < n or t.get_device() != dev or not t.is_contiguous():
+            _need(name, dev, _I32, n, args.partition(" ")[2], *tensors)
+    return n
 
 
 def _row_stride(name: str, dev: int, arg: str, t: torch.Tensor, rows: int, width: int) -> int:
@@ -518,12 +537,16 @@ def _row_stride(name: str, dev: int, arg: str, t: torch.Tensor, rows: int, width
 
 
 def _norm_inputs(name: str, dev: int, qkv, q_gain, k_gain, tok_pos, hq, hkv, dh, rope, q_out, error_flag):
-    M, width = qkv.shape[0], (hq + 2 * hkv) * dh
-    if qkv.dim() != 2 or qkv.shape[1] != width or rope.dim() != 3 or rope.shape[1:] != (dh // 2, 2):
+    shape, width = qkv.shape, (hq + 2 * hkv) * dh
+    if len(shape) != 2 or shape[1] != width or rope.dim() != 3 or rope.shape[1:] != (dh // 2, 2):
         _refuse(name, f"qkv must be [M, {width}] and rope_table [max_pos, {dh // 2}, 2]")
-    _need(name, dev, _BF16, 0, "qkv", qkv)
-    _need(name, dev, _I32, M, "tok_pos", tok_pos)
-    _need(name, dev, _F32, dh, "rope_table", rope)
+    M = shape[0]
+    if not (qkv.dtype is _BF16 and tok_pos.dtype is _I32 and rope.dtype is _F32 and tok_pos.numel() >= M and
+            qkv.get_device() == tok_pos.get_device() == rope.get_device() == dev and qkv.is_contiguous() and
+            tok_pos.is_contiguous() and rope.is_contiguous() and rope.numel() >= dh):
+        _need(name, dev, _BF16, 0, "qkv", qkv)
+        _need(name, dev, _I32, M, "tok_pos", tok_pos)
+        _need(name, dev, _F32, dh, "rope_table", rope)
     if (q_gain is None) != (k_gain is None):
         _refuse(name, "q_gain and k_gain are given together or not at all")
     if q_gain is not None:
@@ -564,9 +587,7 @@ def op_qk_norm_rope_kv8(qkv, q_gain, k_gain, eps: float, tok_pos, cu_q, kv_base,
     rows, heads, width = _kv8_shape(name, dev, k8, v8, k_scale, v_scale)
     if heads != hkv or width != dh:
         _refuse(name, f"the cache holds {heads} heads of {width}, not {hkv} of {dh}")
-    n = cu_q.numel() - 1
-    _need(name, dev, _I32, 1, "cu_q", cu_q)
-    _need(name, dev, _I32, n, "kv_base kv_at kv_len", kv_base, kv_at, kv_len)
+    n = _rows_of(name, dev, "cu_q kv_base kv_at kv_len", cu_q, kv_base, kv_at, kv_len)
     _call(name, dev, (_lib or lib()).bs_op_qk_norm_rope_kv8, qkv.data_ptr(), _ptr(q_gain), _ptr(k_gain), eps,
           tok_pos.data_ptr(), cu_q.data_ptr(), kv_base.data_ptr(), kv_at.data_ptr(), kv_len.data_ptr(), n,
           q_out.data_ptr(), ld, k8.data_ptr(), v8.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), rows, M, hq, hkv, dh,
@@ -579,9 +600,7 @@ def op_kv8_read(k8, v8, k_scale, v_scale, cu, kv_base, kv_at, total: int, k_out:
     """Cache positions [kv_at[i], kv_at[i] + cu[i+1] - cu[i]) of every row, packed: bf16 (K, V) [total, hkv, dh]."""
     name, dev = "bs_op_kv8_read", k8.get_device()
     rows, hkv, dh = _kv8_shape(name, dev, k8, v8, k_scale, v_scale)
-    n = cu.numel() - 1
-    _need(name, dev, _I32, 1, "cu", cu)
-    _need(name, dev, _I32, n, "kv_base kv_at", kv_base, kv_at)
+    n = _rows_of(name, dev, "cu kv_base kv_at", cu, kv_base, kv_at)
     if total < 0:
         _refuse(name, "total must not be negative")
     if k_out is None:
@@ -605,6 +624,11 @@ def attention_kv8_scratch_bytes(hq: int, hkv: int, dh: int) -> int:
     return max(256, lib().bs_op_attention_kv8_scratch_bytes(hq, hkv, dh))
 
 
+@functools.lru_cache(maxsize=4096)
+def _kv8_uses_scratch(n: int, M: int, max_nq: int, max_vis: int, hq: int, hkv: int, dh: int) -> bool:
+    return lib().bs_op_attention_kv8_uses_scratch(n, M, max_nq, max_vis, hq, hkv, dh) != 0
+
+
 def attention_kv8_scratch(hq: int, hkv: int, dh: int, device="cuda") -> torch.Tensor:
     """Scratch of op_attention_kv8, for callers that keep it (calls that share it must be ordered)."""
     return torch.empty(attention_kv8_scratch_bytes(hq, hkv, dh), dtype=_U8, device=device)
@@ -618,21 +642,21 @@ def op_attention_kv8(q, k8, v8, k_scale, v_scale, cu_q, kv_base, vis, hq: int, m
     largest number of query tokens and of visible positions of a row.  Without `scratch` it comes from torch's allocator."""
     name, dev = "bs_op_attention_kv8", q.get_device()
     rows, hkv, dh = _kv8_shape(name, dev, k8, v8, k_scale, v_scale)
-    n, M = cu_q.numel() - 1, q.shape[0]
+    M = q.shape[0]
     ld = _row_stride(name, dev, "q", q, M, hq * dh)
-    _need(name, dev, _I32, 1, "cu_q", cu_q)
-    _need(name, dev, _I32, n, "kv_base vis", kv_base, vis)
+    n = _rows_of(name, dev, "cu_q kv_base vis", cu_q, kv_base, vis)
     if out is None:
         out = torch.empty(M, hq * dh, dtype=_BF16, device=q.device)
     else:
         _need(name, dev, _BF16, M * hq * dh, "out", out)
-    if scratch is None:
-        scratch = torch.empty(attention_kv8_scratch_bytes(hq, hkv, dh), dtype=_U8, device=q.device)
-    else:
+    if scratch is not None:
         _need(name, dev, _U8, 0, "scratch", scratch)
+    elif _kv8_uses_scratch(n, M, max_nq, max_vis, hq, hkv, dh):
+        scratch = torch.empty(attention_kv8_scratch_bytes(hq, hkv, dh), dtype=_U8, device=q.device)
     if error_flag is not None:
         _need(name, dev, _I32, 1, "error_flag", error_flag)
     _call(name, dev, (_lib or lib()).bs_op_attention_kv8, q.data_ptr(), ld, k8.data_ptr(), v8.data_ptr(),
           k_scale.data_ptr(), v_scale.data_ptr(), rows, out.data_ptr(), cu_q.data_ptr(), kv_base.data_ptr(), vis.data_ptr(),
-          n, M, max_nq, max_vis, hq, hkv, dh, scratch.data_ptr(), scratch.numel(), _ptr(error_flag))
+          n, M, max_nq, max_vis, hq, hkv, dh, _ptr(scratch),
+          0 if scratch is None else scratch.numel(), _ptr(error_flag))
     return out

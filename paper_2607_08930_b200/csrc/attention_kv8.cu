@@ -617,45 +617,76 @@ size_t attention_kv8_scratch_bytes(int hq, int hkv, int dh) {
   return up256(kCutBytes) + up256(kPartRows * dh * sizeof(float)) + up256(kPartRows * sizeof(float2));
 }
 
-cudaError_t launch_attention_kv8(const AttnKv8Args& a, cudaStream_t s) {
-  if (a.M <= 0 || a.n_rows <= 0) return cudaSuccess;
-  const int G = a.hq / a.hkv;
-  const int max_nq = a.max_nq > 0 ? std::min(a.max_nq, a.M) : a.M;
+namespace {
+
+// The way of a call, from the sizes that the host knows.
+struct Route {
+  bool tensor, many;     // the tensor-core kernel; single-warp workers
+  int nq, tq, direct;    // query tiles of 8 rows and query tokens per item; as in LineParams
+};
+Route route_of(int n_rows, int M, int hint_nq, int max_vis, int hq, int hkv, int dh) {
+  Route w = {};
+  const int G = hq / hkv;
+  const int max_nq = hint_nq > 0 ? std::min(hint_nq, M) : M;
   const long long widest = (long long)max_nq * G;
-  LineParams p;
-  p.q = a.q; p.q_ld = a.q_ld; p.c = a.cache; p.out = a.out;
-  p.cu_q = a.cu_q; p.kv_base = a.kv_base; p.vis = a.vis;
-  p.n_rows = a.n_rows; p.M = a.M; p.hq = a.hq; p.hkv = a.hkv;
-  p.error_flag = a.error_flag;
-  char* at = static_cast<char*>(a.scratch);
-  p.cuts = reinterpret_cast<Cut*>(at);
-  at += up256(kCutBytes);
-  p.part_o = reinterpret_cast<float*>(at);
-  at += up256(kPartRows * a.dh * sizeof(float));
-  p.part_ml = reinterpret_cast<float2*>(at);
   // From 48 (head_dim 64: 96) query rows per kv head on the 128-row tensor-core tiles pay (16 rows of 320 to 800 keys, 7
   // heads a group: 35 query rows 18.1 us, 15.4 by the streaming kernel, 112 19.4 and 24.7; 32 heads: 40 query rows 62 and
   // 58, 64 63 and 71; head_dim 64, 96 query rows 14.6 and 12.0).  The streaming kernel's tiles hold a token's group of up to
   // 16 heads.
   // Rows of up to 96 keys do not fill a key tile and are streamed whatever the width (16 rows x 32 tokens, 7 heads a group: 43
   // keys 8.6 us, tcgen05 11.5, 100 keys 10.6 and 11.8; 200 rows: 64 keys 82 and 105, 128 keys 108 and 106).
-  const bool brief = a.max_vis > 0 && a.max_vis <= 96;
-  if (G > 16 || (!brief && widest > (a.dh == 128 ? 48 : 96))) return launch_attention_kv8_tc(a, static_cast<float*>(a.scratch), a.scratch_bytes / sizeof(float), s);
+  const bool brief = max_vis > 0 && max_vis <= 96;
+  w.tensor = G > 16 || (!brief && widest > (dh == 128 ? 48 : 96));
+  if (w.tensor) return w;
   // 8 or 16 query rows per item.  (32, which reads a block once for all of a 32-token step, leaves two warps per scheduler
   // with 255 registers: 20 rows x 32 tokens, 32 heads 38.2 us against 32.0 with 16, 64 rows 121 and 122.)
-  const int nq = widest <= 8 ? 1 : 2;
-  p.tq = 8 * nq / G;
+  w.nq = widest <= 8 ? 1 : 2;
+  w.tq = 8 * w.nq / G;
   // Single-warp workers where there are many items and two query tiles make each of them work for a warp.  64 rows x 32
   // tokens, 32 heads, 4096 items: 200 to 512 keys 89 us (107 with four-warp workers), 96 to 1024 122 us (131); 1280 items:
   // 96 to 500 keys 31.9 us (34.4), but 500 to 3000 114 us (106); 800 items 29.4 us (26.2).
-  const long long items = (long long)a.n_rows * a.hkv * ((max_nq + p.tq - 1) / p.tq);
-  const bool many = nq > 1 && items >= (a.max_vis > 0 && a.max_vis <= 512 ? 6 : 16) * 148;
+  const int tiles = (max_nq + w.tq - 1) / w.tq;
+  const long long items = (long long)n_rows * hkv * tiles;
+  w.many = w.nq > 1 && items >= (max_vis > 0 && max_vis <= 512 ? 6 : 16) * 148;
   // Short rows have a worker per item and nothing to merge; so do rows of some length where there are about as many items
   // as workers fit the machine.  Four-warp workers: 2 rows of up to 1524 keys 10.1 us, 15.5 by the line; 2 rows of up to
   // 15,778 60 and 13; 480 items of up to 3000 59 and 66; 256 items of up to 4000 41 and 38.  Single-warp workers: 4096
   // items of up to 512 keys 89 us, 95 by the line; of up to 1024 130 and 122.
-  const int reach = many ? 512 : items >= 400 ? 4096 : 2048;
-  p.direct = a.max_vis > 0 && a.max_vis <= reach ? (max_nq + p.tq - 1) / p.tq : 0;
+  const int reach = w.many ? 512 : items >= 400 ? 4096 : 2048;
+  w.direct = max_vis > 0 && max_vis <= reach ? tiles : 0;
+  return w;
+}
+
+}  // namespace
+
+bool attention_kv8_uses_scratch(int n_rows, int M, int max_nq, int max_vis, int hq, int hkv, int dh) {
+  const Route w = route_of(n_rows, M, max_nq, max_vis, hq, hkv, dh);
+  return w.tensor ? max_vis > (kAttnKv8CutTiles - 1) * 128 : w.direct == 0;
+}
+
+cudaError_t launch_attention_kv8(const AttnKv8Args& a, cudaStream_t s) {
+  if (a.M <= 0 || a.n_rows <= 0) return cudaSuccess;
+  const Route w = route_of(a.n_rows, a.M, a.max_nq, a.max_vis, a.hq, a.hkv, a.dh);
+  if (w.tensor) return launch_attention_kv8_tc(a, static_cast<float*>(a.scratch), a.scratch_bytes / sizeof(float), s);
+  LineParams p;
+  p.q = a.q; p.q_ld = a.q_ld; p.c = a.cache; p.out = a.out;
+  p.cu_q = a.cu_q; p.kv_base = a.kv_base; p.vis = a.vis;
+  p.n_rows = a.n_rows; p.M = a.M; p.hq = a.hq; p.hkv = a.hkv;
+  p.tq = w.tq;
+  p.direct = w.direct;
+  p.error_flag = a.error_flag;
+  char* at = static_cast<char*>(a.scratch);              // (a worker per item uses none)
+  p.cuts = reinterpret_cast<Cut*>(at);
+  p.part_o = nullptr;
+  p.part_ml = nullptr;
+  if (at) {
+    at += up256(kCutBytes);
+    p.part_o = reinterpret_cast<float*>(at);
+    at += up256(kPartRows * a.dh * sizeof(float));
+    p.part_ml = reinterpret_cast<float2*>(at);
+  }
+  const int nq = w.nq;
+  const bool many = w.many;
   // Stages and CTAs per SM.  One query tile, head_dim 128: three stages on two CTAs, 64 rows of 1024 to 4096 keys 37.0 us
   // (two on three 38.7); head_dim 64: two on three, 60 rows of 1000 to 8000 keys 30.6 us (three on three 34.7).  Two query
   // tiles, head_dim 128, four-warp: two on three, 200 rows x 2 tokens 26.4 us (three on two 33.3); single-warp: two on two,

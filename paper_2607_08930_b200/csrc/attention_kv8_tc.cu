@@ -701,7 +701,7 @@ cudaError_t run_tc(const AttnKv8Args& a, float* part, size_t part_floats, int sm
   // keys 45 us, 369 uncut, 4 rows of 1000 to 2000 26 and 34; 9 rows of 500 to 800 25 us in two chunks, 20 uncut).
   int chunks = 1;
   if (!two)
-    while (chunks < kMaxChunks && singles * (chunks + 1) <= sms && key_tiles / (chunks + 1) >= 4 &&
+    while (chunks < kMaxChunks && singles * (chunks + 1) <= sms && key_tiles / (chunks + 1) >= kAttnKv8CutTiles / 2 &&
            (size_t)(chunks + 1) * a.M * a.hq * (DH + 2) <= part_floats)
       ++chunks;
   p.chunks = chunks;

@@ -1040,6 +1040,11 @@ size_t bs_op_attention_kv8_scratch_bytes(int n_q_heads, int n_kv_heads, int head
   return attention_kv8_scratch_bytes(n_q_heads, n_kv_heads, head_dim);
 }
 
+int bs_op_attention_kv8_uses_scratch(int n_rows, int M, int max_nq, int max_vis, int n_q_heads, int n_kv_heads, int head_dim) {
+  return n_rows >= 1 && M >= 1 && kv8_shape_ok(n_q_heads, n_kv_heads, head_dim) &&
+         attention_kv8_uses_scratch(n_rows, M, max_nq, max_vis, n_q_heads, n_kv_heads, head_dim);
+}
+
 int bs_op_attention_kv8(const void* q, int q_ld, const void* k8, const void* v8, const float* k_scale,
                         const float* v_scale, long long kv_rows, void* out, const int* cu_q, const int* kv_base,
                         const int* vis, int n_rows, int M, int max_nq, int max_vis, int n_q_heads, int n_kv_heads,
@@ -1048,15 +1053,16 @@ int bs_op_attention_kv8(const void* q, int q_ld, const void* k8, const void* v8,
   AttnKv8Args a;
   if (M < 0 || n_rows < 1 || n_rows > kAttnKv8MaxRows || max_nq < 0 || max_vis < 0 ||
       !kv8_shape_ok(n_q_heads, n_kv_heads, head_dim) || q_ld < n_q_heads * head_dim || q_ld % 8 ||
-      !aligned16({q, out, scratch}) || ((uintptr_t)scratch & 255) || !cu_q || !kv_base || !vis ||
-      scratch_bytes < attention_kv8_scratch_bytes(n_q_heads, n_kv_heads, head_dim) ||
+      !aligned16({q, out}) || ((uintptr_t)scratch & 255) || !cu_q || !kv_base || !vis ||
+      ((!scratch || scratch_bytes < attention_kv8_scratch_bytes(n_q_heads, n_kv_heads, head_dim)) &&
+       attention_kv8_uses_scratch(n_rows, M, max_nq, max_vis, n_q_heads, n_kv_heads, head_dim)) ||
       !kv8_cache_of(k8, v8, k_scale, v_scale, kv_rows, &a.cache))
     return BS_E_ARG;
   a.q = (const bf16*)q; a.q_ld = q_ld; a.out = (bf16*)out;
   a.cu_q = cu_q; a.kv_base = kv_base; a.vis = vis;
   a.n_rows = n_rows; a.M = M; a.max_nq = max_nq; a.max_vis = max_vis;
   a.hq = n_q_heads; a.hkv = n_kv_heads; a.dh = head_dim;
-  a.scratch = scratch; a.scratch_bytes = scratch_bytes; a.error_flag = error_flag;
+  a.scratch = scratch; a.scratch_bytes = scratch ? scratch_bytes : 0; a.error_flag = error_flag;
   return launch_attention_kv8(a, (cudaStream_t)stream) == cudaSuccess ? BS_OK : BS_E_CUDA;
 }
 

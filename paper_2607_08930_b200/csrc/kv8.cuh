@@ -121,6 +121,9 @@ struct AttnKv8Args {
 };
 constexpr int kAttnKv8MaxRows = 1024;
 size_t attention_kv8_scratch_bytes(int hq, int hkv, int dh);
+// Whether a call of these sizes puts anything there.
+bool attention_kv8_uses_scratch(int n_rows, int M, int max_nq, int max_vis, int hq, int hkv, int dh);
+constexpr int kAttnKv8CutTiles = 8;      // key tiles (of 128) from which the tensor-core kernel may cut a row's keys
 cudaError_t launch_attention_kv8(const AttnKv8Args& a, cudaStream_t s);
 // tensor-core kernel for many query rows per kv head; part: scratch for partial results of key chunks
 cudaError_t launch_attention_kv8_tc(const AttnKv8Args& a, float* part, size_t part_floats, cudaStream_t s);

@@ -68,7 +68,8 @@ def _attn(B, **over):
                                   dict(kv_rows=63), dict(kv_rows=0), dict(kv_rows=1 << 31), dict(out=None), dict(cu=None),
                                   dict(base=None), dict(vis=None), dict(n_rows=-1), dict(n_rows=1025), dict(M=-1),
                                   dict(max_nq=-1), dict(max_vis=-1), dict(hq=27), dict(hkv=0), dict(hq=66, hkv=2, q_ld=66 * 128),
-                                  dict(dh=96), dict(dh=0), dict(scratch=None), dict(scratch=P + 16), dict(nbytes=1024)])
+                                  dict(dh=96), dict(dh=0), dict(scratch=None, max_vis=0), dict(scratch=P + 16),
+                                  dict(nbytes=1024, max_vis=0)])
 def test_attention_refuses(B, over):
     assert _attn(B, **over) == B.BS_E_ARG
 
@@ -77,6 +78,9 @@ def test_empty_calls_are_accepted(B):
     assert _attn(B, M=0) == B.BS_OK and _attn(B, n_rows=0) == B.BS_OK
     L = B.lib()
     assert L.bs_op_kv8_read(None, None, None, None, 0, None, None, None, 1, 0, 4, 128, None, None, None, None) == B.BS_OK
+    uses = L.bs_op_attention_kv8_uses_scratch
+    assert uses(2, 2, 1, 0, 28, 4, 128) == 1 and uses(2, 2, 1, 10, 28, 4, 128) == 0 and uses(2, 64, 32, 300, 28, 4, 128) == 0
+    assert uses(2, 64, 32, 40000, 28, 4, 128) == 1 and uses(2, 2, 1, 40000, 28, 4, 128) == 1 and uses(2, 2, 1, 0, 28, 5, 128) == 0
     assert L.bs_op_attention_kv8_scratch_bytes(28, 4, 128) > 0 and L.bs_op_attention_kv8_scratch_bytes(28, 5, 128) == 0
 
 
