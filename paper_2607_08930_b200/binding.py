@@ -550,7 +550,9 @@ def _norm_inputs(name: str, dev: int, qkv, q_gain, k_gain, tok_pos, hq, hkv, dh,
     if (q_gain is None) != (k_gain is None):
         _refuse(name, "q_gain and k_gain are given together or not at all")
     if q_gain is not None:
-        _need(name, dev, _BF16, dh, "q_gain k_gain", q_gain, k_gain)
+        if not (q_gain.dtype is k_gain.dtype is _BF16 and q_gain.get_device() == k_gain.get_device() == dev and
+                q_gain.is_contiguous() and k_gain.is_contiguous() and q_gain.numel() >= dh and k_gain.numel() >= dh):
+            _need(name, dev, _BF16, dh, "q_gain k_gain", q_gain, k_gain)
     if error_flag is not None:
         _need(name, dev, _I32, 1, "error_flag", error_flag)
     if q_out is None:
@@ -566,13 +568,18 @@ def op_qk_norm_rope_kv(qkv, q_gain, k_gain, eps: float, tok_pos, tok_kv, kcache,
     [M, hq * dh]; q_out = qkv rotates in place.  error_flag (int32 [1]) gets >= 100 where an index was out of range."""
     name, dev = "bs_op_qk_norm_rope_kv", qkv.get_device()
     M, q_out, ld = _norm_inputs(name, dev, qkv, q_gain, k_gain, tok_pos, hq, hkv, dh, rope_table, q_out, error_flag)
-    if kcache.dim() != 3 or kcache.shape[1:] != (hkv, dh) or vcache.shape != kcache.shape:
+    shape = kcache.shape
+    rows = shape[0] if len(shape) == 3 else 0
+    if shape != (rows, hkv, dh) or vcache.shape != shape:
         _refuse(name, f"the caches must be [kv_rows, {hkv}, {dh}]")
-    _need(name, dev, _BF16, 1, "kcache vcache", kcache, vcache)
-    _need(name, dev, _I32, M, "tok_kv", tok_kv)
+    if not (kcache.dtype is vcache.dtype is _BF16 and tok_kv.dtype is _I32 and rows and tok_kv.numel() >= M and
+            kcache.get_device() == vcache.get_device() == tok_kv.get_device() == dev and
+            kcache.is_contiguous() and vcache.is_contiguous() and tok_kv.is_contiguous()):
+        _need(name, dev, _BF16, 1, "kcache vcache", kcache, vcache)
+        _need(name, dev, _I32, M, "tok_kv", tok_kv)
     _call(name, dev, (_lib or lib()).bs_op_qk_norm_rope_kv, qkv.data_ptr(), _ptr(q_gain), _ptr(k_gain), eps,
           tok_pos.data_ptr(), tok_kv.data_ptr(), q_out.data_ptr(), ld, kcache.data_ptr(), vcache.data_ptr(),
-          kcache.shape[0], M, hq, hkv, dh, rope_table.data_ptr(), rope_table.shape[0], _ptr(error_flag))
+          rows, M, hq, hkv, dh, rope_table.data_ptr(), rope_table.shape[0], _ptr(error_flag))
     return q_out
 
 
