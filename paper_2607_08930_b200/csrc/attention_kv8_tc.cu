@@ -198,7 +198,6 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
   const unsigned bar0 = smem_u32(&bars[0]);
   auto bar = [&](int i) { return bar0 + 8u * (unsigned)i; };
   pdl_wait();
-  pdl_trigger();
 
   // ---- the work item ----
   const int G = p.G, per_cta = NT * p.tq;
@@ -247,6 +246,7 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  pdl_trigger();      // not before the tensor memory is here: the kernel behind may take its own before it waits for this grid
   constexpr unsigned tmem_base = 0;                         // the only place an allocation of all 512 columns can have
   volatile int* abort_flag = &s_abort;
   if (threadIdx.x == 0 && tmem_base_slot != 0) s_abort = 1;
