@@ -440,7 +440,7 @@ def test_attention_of_queries_that_are_not_finite(B):
         assert (np.abs(got[0, 1] - mean) <= np.abs(mean) * HALF_BF16 + np.abs(K.span(*vc, base[0], 0, 90)).max() * 2.0 ** -11).all()
 
 
-@pytest.mark.parametrize("nq", [1, 32])
+@pytest.mark.parametrize("nq", [1, 32, 64])
 def test_offsets_beyond_32_bits(B, nq):
     """A cache of more than 4 GiB of codes: rows near its end, written, attended to and read back."""
     hq, hkv, dh = 32, 32, 128
@@ -702,3 +702,41 @@ def test_what_is_not_finite_stays_in_its_query_row(B, hq, hkv, dh, nq, vis, what
     assert np.isnan(out[0, 1]).all()
     out[0, 1] = 0
     assert np.isfinite(out).all()
+
+
+def some_rows(count, nq, lo, hi, longest):
+    """`count` rows of nq queries (a few of fewer, one of none) over lo..hi keys, one over `longest`, one over nothing."""
+    rng = np.random.default_rng(count)
+    rows = [(nq if i % 7 else max(1, nq - 3), int(v)) for i, v in enumerate(rng.integers(lo, hi + 1, count))]
+    rows[1], rows[2], rows[count // 2] = (nq, 0), (0, hi), (nq, longest)
+    return rows
+
+
+WAYS = [  # hq, hkv, dh, rows, whether the largest number of keys is told, scratch expected
+    (32, 32, 128, some_rows(32, 9, 1, 200, 300), True, 0),        # single-warp workers, one per item
+    (32, 32, 128, some_rows(80, 9, 1, 70, 700), True, 1),         # single-warp workers on the shared line
+    (16, 16, 64, some_rows(60, 12, 1, 200, 500), True, 0),
+    (16, 16, 64, some_rows(160, 10, 1, 60, 800), True, 1),
+    (6, 2, 128, some_rows(6, 4, 1, 900, 2800), False, 1),         # four-warp workers, two query tiles: line, one per item
+    (6, 2, 128, some_rows(6, 4, 1, 900, 1800), True, 0),
+    (8, 2, 64, some_rows(6, 4, 1, 900, 2800), False, 1),
+    (8, 2, 64, some_rows(6, 24, 1, 900, 1800), True, 0),
+    (28, 4, 128, some_rows(9, 1, 1, 900, 2800), False, 1),        # one query tile
+    (4, 4, 64, some_rows(120, 1, 1, 300, 4000), True, 0),
+    (28, 4, 128, some_rows(12, 32, 1, 80, 96), True, 0),          # wide, but brief
+    (28, 4, 128, some_rows(5, 40, 100, 400, 1300), True, 1)]      # tensor-core tiles, keys cut
+
+
+@pytest.mark.parametrize("hq,hkv,dh,rows,told,scratch", WAYS)
+def test_every_way_through_the_attention(B, hq, hkv, dh, rows, told, scratch):
+    rng = np.random.default_rng(len(rows) + hq)
+    n, vis, base, kc, vc, q = attn_inputs(rng, hq, hkv, dh, rows, qscale=0.5)
+    (k8, ks), (v8, vs) = to_gpu(*kc), to_gpu(*vc)
+    hints = dict(max_nq=int(n.max()), max_vis=int(vis.max()) if told else 0)
+    assert B.lib().bs_op_attention_kv8_uses_scratch(len(n), len(q), hints["max_nq"], hints["max_vis"], hq, hkv, dh) == scratch
+    flag = torch.zeros(1, dtype=torch.int32, device="cuda")
+    run = lambda: B.op_attention_kv8(q.cuda(), k8, v8, ks, vs, ints(prefix(n)), ints(base), ints(vis), hq, error_flag=flag, **hints)   # noqa: E731
+    out = run()
+    assert int(flag.item()) == 0
+    check_attention(host(out), q, hq, dh, n, vis, base, kc, vc)
+    assert torch.equal(out, run())
