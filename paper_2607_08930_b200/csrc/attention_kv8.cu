@@ -36,6 +36,13 @@ __device__ __forceinline__ unsigned pack_f16(float a, float b) {
   const __half2 h = __floats2half2_rn(a, b);
   return *reinterpret_cast<const unsigned*>(&h);
 }
+// Weights, up to 2^kGrow: beyond 2^23 the sum ref + kGrow that they are compared with is rounded itself, and one may reach
+// 2^16, just over fp16's range (held to 65504, a relative 2^-11).
+__device__ __forceinline__ unsigned pack_weights(float a, float b) {
+  unsigned r;
+  asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+  return r;
+}
 // 16 bytes to shared memory, or zeros (`real` = false; the source is then not read)
 __device__ __forceinline__ void copy_async16(unsigned dst, const void* src, bool real) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
@@ -331,8 +338,8 @@ __global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(c
           const float e2 = exp2_fast(s[nq][2] - ref[nq][0]), e3 = exp2_fast(s[nq][3] - ref[nq][1]);
           sum[nq][0] = fmaf(e0 + e2, inv_vs, sum[nq][0]);
           sum[nq][1] = fmaf(e1 + e3, inv_vs, sum[nq][1]);
-          pr[nq][0] = transpose8x8(pack_f16(e0, e1));
-          pr[nq][1] = transpose8x8(pack_f16(e2, e3));
+          pr[nq][0] = transpose8x8(pack_weights(e0, e1));
+          pr[nq][1] = transpose8x8(pack_weights(e2, e3));
         }
         // ---- output: dims g DH / 8 + 2 i (row g of m tile i) and + 1 (row g + 8) ----
         unsigned vr[4][DH / 32];         // keys 16 m + 2 c4, + 1, + 8, + 9

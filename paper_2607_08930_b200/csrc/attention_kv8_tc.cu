@@ -32,6 +32,7 @@
 
 #include <algorithm>
 #include <mutex>
+#include <type_traits>
 
 #include "kv8_line.cuh"
 #include "tc_common.cuh"
@@ -459,15 +460,19 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
       vsn = __ldcg(p.v_scale + at);
     };
     if (my_tiles > 0) load_scales(0);
-    for (int t = 0; t < my_tiles && ok; ++t) {
-      const float f = kv8_clamp_scale(ksn), lv = log2_fast(kv8_clamp_scale(vsn));
-      if (t + 1 < my_tiles) load_scales(t + 1);
-      const int left = vis - (kt0 + t) * KT;
-#pragma unroll
+    // A key tile; false: a wait ran out.  A weight's exponent s f + (lv - ref) is rounded once, so what the reference, itself a
+    // rounded sum, was rounded by stays in it: more than a weight's whole range once scores pass 2^23.  FAR (such scores are
+    // possible: a score is at most 256 x 448 x 128 f, none of 2^23 where f is below 1/2 for all rows of the warp): s f + lv is
+    // rounded first, for every use alike.  Rolled, as next to no call comes here (the other way: 6 whole rows 366 us, 364
+    // without a choice, 369 with a vote on every row's own f).
+    const float sc_top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(sc)));
+    auto tile = [&](auto far, int t, float f, float lv, int left) {
+      constexpr bool FAR = decltype(far)::value;
+#pragma unroll (FAR ? 1 : 2)
       for (int h = 0; h < 2; ++h) {                          // 64 keys at a time: their scores fit the registers, read once
         // (These scores were issued after the weights that stood in their place were used, so no warp of the group - one
         // without query rows has nothing to hold it up - publishes here before all four have published there.)
-        if (!wait(B_SFULL + 2 * x + h, t)) { ok = false; break; }
+        if (!wait(B_SFULL + 2 * x + h, t)) return false;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         if (warp_has_rows) {
           unsigned y[64];
@@ -478,18 +483,24 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
 #pragma unroll
             for (int j = 0; j < 64; ++j) y[j] = h * 64 + j < left ? y[j] : 0xff800000u;       // -inf
           }
-          float fi[2], li[2], top = -INFINITY;
+          float fi[2], li[2], add[2], top = -INFINITY;
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             fi[i] = __shfl_sync(0xffffffffu, f, 2 * h + i) * sc;
-            li[i] = __shfl_sync(0xffffffffu, lv, 2 * h + i);
+            li[i] = add[i] = __shfl_sync(0xffffffffu, lv, 2 * h + i);
+            if (FAR) {
+#pragma unroll
+              for (int j = 0; j < 32; ++j) y[i * 32 + j] = __float_as_uint(fmaf(__uint_as_float(y[i * 32 + j]), fi[i], li[i]));
+              fi[i] = 1.f;
+              add[i] = 0.f;
+            }
             float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
             for (int j = 0; j < 32; j += 2)
               m4[(j >> 1) & 3] = max3(m4[(j >> 1) & 3], __uint_as_float(y[i * 32 + j]), __uint_as_float(y[i * 32 + j + 1]));
-            top = fmaxf(top, fmaf(max3(fmaxf(m4[0], m4[1]), m4[2], m4[3]), fi[i], li[i]));
+            top = fmaxf(top, fmaf(max3(fmaxf(m4[0], m4[1]), m4[2], m4[3]), fi[i], add[i]));
           }
-          const bool grow = top > ref + kTcGrow;
+          const bool grow = top - ref > kTcGrow;             // (ref + kTcGrow may be rounded up to top)
           if (__any_sync(0xffffffffu, grow)) {
             float turn = 1.f;
             if (grow) {
@@ -499,7 +510,7 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
             }
             if (t > 0 || h > 0) {
               // the output stands still once the product issued last is in it
-              if (!wait(B_OFULL + 2 * x + (h ^ 1), t - 1 + h)) { ok = false; break; }
+              if (!wait(B_OFULL + 2 * x + (h ^ 1), t - 1 + h)) return false;
               asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll 1
               for (int c = 0; c < DH / 32; ++c) {
@@ -515,7 +526,7 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
           unsigned w[32];
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            const f32x2 f2 = pack2(fi[i], fi[i]), shift2 = pack2(li[i] - ref, li[i] - ref);
+            const f32x2 f2 = pack2(fi[i], fi[i]), shift2 = pack2(add[i] - ref, add[i] - ref);
             unsigned* z = y + i * 32;
 #pragma unroll
             for (int j = 0; j < 32; j += 2) {
@@ -547,6 +558,13 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(B_PFULL + 2 * x + h));
       }
+      return true;
+    };
+    for (int t = 0; t < my_tiles && ok; ++t) {
+      const float f = kv8_clamp_scale(ksn), lv = log2_fast(kv8_clamp_scale(vsn));
+      if (t + 1 < my_tiles) load_scales(t + 1);
+      const int left = vis - (kt0 + t) * KT;
+      ok = __any_sync(0xffffffffu, !(f * sc_top < 0.5f)) ? tile(std::true_type(), t, f, lv, left) : tile(std::false_type(), t, f, lv, left);
     }
     const bool have = ok && my_tiles > 0 && wait(B_OFULL + 2 * x + 1, my_tiles - 1);
     if (warp_has_rows) {

@@ -1,0 +1,76 @@
+"""Calls at the borders of what the 8-bit cache operators take, against the 64-bit oracle (needs a B200)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import kv8_oracle as K
+from test_kv8_gpu import B, HALF_BF16, attn_bound, attn_inputs, bf16, host, ints, prefix, to_gpu  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- queries far from one ------------------------------------------------------------------------------------
+
+def check_winners(got, q, hq, dh, k, v):
+    """Scores so far apart that the softmax is its largest key's alone: the output is that key's V (which bf16 holds
+    exactly), off by the weight's fp16 rounding in the product (2^-11) and half a bf16 step.  Query rows whose two largest
+    scores lie within twice the scores' error (sums of dh products in fp32, a query element held to 2^-17 of its row's
+    largest) plus 40 are left out: they are few."""
+    n, g, seen = len(q), hq // k.shape[1], 0
+    for h in range(hq):
+        z = q[:, h] @ k[:, h // g].T / np.sqrt(dh)
+        err = (np.abs(q[:, h]) @ np.abs(k[:, h // g]).T).max(1) / np.sqrt(dh) * (dh + 4) * 2.0 ** -23 + \
+            np.abs(q[:, h]).max(1) * np.abs(k[:, h // g]).sum(1).max() / np.sqrt(dh) * 2.0 ** -17
+        top = np.sort(z, 1)
+        clear = top[:, -1] - top[:, -2] > 2 * err + 40
+        want = v[z.argmax(1), h // g]
+        tol = np.abs(want) * (HALF_BF16 + 2.0 ** -11 + 2.0 ** -20) + np.abs(v).max() * 2.0 ** -40
+        assert (np.abs(got[:, h] - want)[clear] <= tol[clear]).all(), h
+        seen += int(clear.sum())
+    assert seen >= 0.8 * n * hq
+
+
+@pytest.mark.parametrize("power", [24, 30, 33, 36, 45, 60])
+@pytest.mark.parametrize("hq,hkv,dh,rows", [(28, 4, 128, [(1, 300)]), (32, 32, 128, [(32, 129)] * 3), (8, 2, 64, [(12, 200)]),
+                                            (14, 2, 128, [(40, 200), (40, 1100)]), (8, 2, 64, [(64, 333)]),
+                                            (28, 4, 128, [(300, 500)] * 6)])
+def test_queries_of_any_finite_size(B, hq, hkv, dh, rows, power):
+    """Every other token's queries are 2^power as large, up to the type's last binade; the others keep their results."""
+    rng = np.random.default_rng(power)
+    n, vis, base, kc, vc, q = attn_inputs(rng, hq, hkv, dh, rows)
+    kc[1][np.isfinite(kc[1])] = 2.0 ** -20
+    q = bf16(np.clip(host(q), -7.9, 7.9))                  # 7.9 x 2^125 is below the largest bf16
+    q[::2] = (q[::2].double() * 2.0 ** power).to(torch.bfloat16)
+    assert torch.isfinite(q).all()
+    (k8, ks), (v8, vs) = to_gpu(*kc), to_gpu(*vc)
+    out = host(B.op_attention_kv8(q.cuda(), k8, v8, ks, vs, ints(prefix(n)), ints(base), ints(vis), hq, max_nq=int(n.max()),
+                                  max_vis=int(vis.max())))
+    cu = prefix(n)
+    for i in range(len(n)):
+        k, v = K.span(*kc, base[i], 0, vis[i]), K.span(*vc, base[i], 0, vis[i])
+        t = np.arange(cu[i], cu[i + 1])
+        large, small = t[t % 2 == 0], t[t % 2 == 1]
+        check_winners(out[large].reshape(-1, hq, dh), host(q[large]).reshape(-1, hq, dh), hq, dh, k, v)
+        if len(small):
+            ref, mag, dot, flat = K.attention(host(q[small]).reshape(-1, hq, dh), k, v)
+            assert (np.abs(out[small].reshape(-1, hq, dh) - ref) <= attn_bound(ref, mag, dot, flat, np.abs(v).max(), vis[i], dh)).all()
+
+
+@pytest.mark.parametrize("hq,hkv,dh,nq", [(28, 4, 128, 1), (32, 32, 128, 32), (8, 2, 64, 12), (14, 2, 128, 64), (8, 2, 64, 64)])
+def test_scores_a_few_of_their_own_steps_apart(B, hq, hkv, dh, nq):
+    """Keys whose scores, 2^23 to 2^30 in log2 units, differ by a few of fp32's steps there: which of them win is a matter of
+    rounding, but every output is a mean of the values, between 1 and 2."""
+    rng = np.random.default_rng(nq + hq)
+    vis, blocks = 400, 13
+    codes = np.zeros((blocks, hkv, 32, dh), np.uint8)
+    codes[..., 1:17] = rng.integers(0, 16, codes[..., 1:17].shape)
+    codes[..., 0] = 126                                    # 448
+    values = rng.integers(56, 65, codes.shape).astype(np.uint8)      # 1 to 2
+    q = np.zeros((nq, hq, dh))
+    q[..., 0] = 2.0 ** rng.integers(18, 25, (nq, hq))
+    q[..., 1:17] = rng.normal(size=(nq, hq, 16)) * q[..., :1] * 2.0 ** rng.integers(-10, -4, (nq, hq, 1))
+    q = bf16(q.reshape(nq, hq * dh))
+    (k8, ks), (v8, vs) = to_gpu(codes, np.ones((blocks, hkv))), to_gpu(values, np.ones((blocks, hkv)))
+    for max_vis in (vis, 0):
+        out = host(B.op_attention_kv8(q.cuda(), k8, v8, ks, vs, ints([0, nq]), ints([0]), ints([vis]), hq, max_nq=nq, max_vis=max_vis))
+        assert np.isfinite(out).all() and out.min() >= 1 - 2.0 ** -8 and out.max() <= 2 * (1 + 2.0 ** -8)
