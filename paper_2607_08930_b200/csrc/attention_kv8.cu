@@ -9,6 +9,7 @@
 //   w_j = vs_b e^(s_j - m) = 2^(t_j - M),   t_j = log2(e) s_j + log2(vs_b),   M: running maximum of t
 //
 // so that weights are largest where the summands w_j c'_j are; the denominator takes w_j / vs_b.
+#include <float.h>
 #include <math.h>
 
 #include <algorithm>
@@ -82,8 +83,9 @@ __device__ __forceinline__ uint2 lds64(unsigned at) {
 // Keys are the rows (M) of both products and the queries their columns (N), so that 8 query rows - a group of heads of
 // one token - fill an instruction.  Codes go to the tensor cores as fp16, which holds every e4m3 value (the warp-level
 // e4m3 product is no way around that: measured on B200, it runs as conversions and two fp16 products, 25 clk against 8).
-// Queries become fp16 after a power of two per query row has brought their largest element into [1, 2): bf16's 8 bits
-// fit fp16's 11, and what drops below 2^-24 of the row's largest element is below the fp32 sum's own rounding.  Weights
+// Queries become fp16 after a power of two per query row has brought their largest element into [1, 2), or [2, 4) in the
+// type's last binade: bf16's 8 bits fit fp16's 11, and what drops below 2^-24 of the row's largest element is below the
+// fp32 sum's own rounding.  Weights
 // are fp16, transposed in registers (movmatrix).  The order of the dims in the scores' k index and of the dims in the
 // output's m index is free, and is chosen so that a lane's 16-byte shared-memory loads hold its operand registers; a
 // 16-byte chunk's place in its 128-byte line is turned by the line's number, which keeps those loads free of bank
@@ -209,9 +211,9 @@ __global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(c
       }
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-      const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 100);
+      const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 126);     // 2^-126 is fp32's least normal power
       const float up = pow2i(-e);
-      if (c4 == 0) s_sc[f] = pow2i(e) * (1.4426950408889634f * rsqrtf((float)DH));
+      if (c4 == 0) s_sc[f] = fminf(pow2i(e) * (1.4426950408889634f * rsqrtf((float)DH)), kMaxFactor);
 #pragma unroll
       for (int k = 0; k < KP; ++k) {
         const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&raw[k]);
@@ -239,7 +241,7 @@ __global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(c
       for (int i = 0; i < MD; ++i) o[nq][i][0] = o[nq][i][1] = o[nq][i][2] = o[nq][i][3] = 0.f;
 #pragma unroll
       for (int y = 0; y < 2; ++y) {
-        ref[nq][y] = -INFINITY;
+        ref[nq][y] = -FLT_MAX;           // (under any score but -inf, whose weight it makes 0)
         sum[nq][y] = 0.f;
         sc[nq][y] = s_sc[nq * 8 + 2 * c4 + y];
       }
@@ -424,8 +426,7 @@ __global__ void __launch_bounds__(kStreamThreads, MINB) k_attention_kv8_stream(c
         float m = -INFINITY;
 #pragma unroll
         for (int w = 0; w < W; ++w) m = fmaxf(m, s_ml[w * R + f].x);
-        // a warp without blocks has an output of zeros; one that met nothing but NaN has NaN, and keeps it
-        const float turn = ref[nq][y] > -INFINITY ? exp2_fast(ref[nq][y] - m) : 1.f;
+        const float turn = exp2_fast(ref[nq][y] - m);        // (a warp without blocks: zeros; NaN stays NaN)
         float* dst = s_o + (member * R + f) * LDO + g * (DH / 8);
 #pragma unroll
         for (int i = 0; i < MD; i += 2)
@@ -502,7 +503,7 @@ __global__ void __launch_bounds__(kMergeThreads) k_attention_kv8_merge(const Lin
     for (int k = lane + 32 * KEEP; k < parts; k += 32) m = fmaxf(m, __ldcg(p.part_ml + slot_of(k) * R + f).x);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    auto weight = [&](float ref) { return ref > -INFINITY ? exp2_fast(ref - m) : 1.f; };     // (parts of NaN stay NaN)
+    auto weight = [&](float ref) { return ref > -INFINITY ? exp2_fast(ref - m) : 1.f; };     // (no part: its sum is 0)
 #pragma unroll
     for (int i = 0; i < KEEP; ++i) l += weight(ml[i].x) * ml[i].y;
     for (int k = lane + 32 * KEEP; k < parts; k += 32) {

@@ -28,6 +28,7 @@
 // to 800 keys, one query tile per CTA, 17.9 us, are bound by a CTA's beginning - indices, barriers, queries to two terms:
 // 4 us - and by its chain of three to seven tiles.
 // Every wait is bounded; on a timeout the flag is raised, all roles drain, the copies in flight are waited for.
+#include <float.h>
 #include <math.h>
 
 #include <algorithm>
@@ -418,11 +419,11 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
         for (int u = 0; u < FLY; ++u) {
           const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&raw[u]);
           const float top = fmaxf(__low2float(top2[u]), __high2float(top2[u]));
-          const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 100);
+          const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 127);
           const float up = pow2i(7 - e);
           const int f = f0 + (i0 + u) * RPI;
           // (an infinite element would saturate: its row becomes NaN here, as its softmax is)
-          const float sc = pow2i(e - 7) * (1.4426950408889634f * rsqrtf((float)DH));
+          const float sc = fminf(pow2i(e - 7) * (1.4426950408889634f * rsqrtf((float)DH)), kMaxFactor);
           if (pl == 0) s_sc[x * 128 + f] = top < INFINITY ? sc : __int_as_float(0x7fffffff);
           unsigned hi[2] = {0u, 0u}, lo[2] = {0u, 0u};
 #pragma unroll
@@ -445,7 +446,7 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
     __syncwarp();
     if (lane == 0) mbar_arrive(bar(B_QFULL));
     const float sc = my_tiles > 0 ? s_sc[x * 128 + r] : 0.f;
-    float ref = -INFINITY, sum = 0.f;
+    float ref = -FLT_MAX, sum = 0.f;                         // (under any score but -inf, whose weight it makes 0)
     bool ok = true;
     // whole warps go on or give up: the tensor-memory instructions want all lanes
     auto wait = [&](int i, int phase) {
@@ -504,7 +505,7 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
           if (__any_sync(0xffffffffu, grow)) {
             float turn = 1.f;
             if (grow) {
-              turn = exp2_fast(ref - (top - kTcBias));       // 2^-inf = 0 on the first tile
+              turn = exp2_fast(ref - (top - kTcBias));       // 0 on the first tile
               ref = top - kTcBias;
               sum *= turn;
             }

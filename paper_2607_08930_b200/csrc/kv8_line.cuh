@@ -17,6 +17,11 @@ __device__ __forceinline__ float log2_fast(float x) {      // exact for powers o
   return y;
 }
 
+// Largest factor of a query row's scores: times a K scale of at most 2^40 it stays finite.  Rows held to it (their largest
+// element is 2^90 at least) have all their scores scaled down alike; any two that differ are still so far apart, by 2^14
+// at least, that the softmax is the larger one's alone.
+constexpr float kMaxFactor = 0x1p87f;
+
 // A cut item: the workers that hold parts of it, its first query token, number of query rows (0: nothing is cut) and
 // kv head; whether worker c0 began with it (its part is then in the even slot, as everybody else's is).
 struct alignas(16) Cut { int c0, c1, t0, nrows, head, even, pad0, pad1; };

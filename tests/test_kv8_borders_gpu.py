@@ -30,7 +30,7 @@ def check_winners(got, q, hq, dh, k, v):
     assert seen >= 0.8 * n * hq
 
 
-@pytest.mark.parametrize("power", [24, 30, 33, 36, 45, 60])
+@pytest.mark.parametrize("power", [24, 30, 33, 36, 45, 60, 102, 110, 116, 125])
 @pytest.mark.parametrize("hq,hkv,dh,rows", [(28, 4, 128, [(1, 300)]), (32, 32, 128, [(32, 129)] * 3), (8, 2, 64, [(12, 200)]),
                                             (14, 2, 128, [(40, 200), (40, 1100)]), (8, 2, 64, [(64, 333)]),
                                             (28, 4, 128, [(300, 500)] * 6)])
@@ -74,3 +74,31 @@ def test_scores_a_few_of_their_own_steps_apart(B, hq, hkv, dh, nq):
     for max_vis in (vis, 0):
         out = host(B.op_attention_kv8(q.cuda(), k8, v8, ks, vs, ints([0, nq]), ints([0]), ints([vis]), hq, max_nq=nq, max_vis=max_vis))
         assert np.isfinite(out).all() and out.min() >= 1 - 2.0 ** -8 and out.max() <= 2 * (1 + 2.0 ** -8)
+
+
+@pytest.mark.parametrize("nq", [1, 64])
+def test_large_queries_beside_small_ones_and_far_scales(B, nq):
+    """(2^110, 2^104) against the keys (1, 0) and (0, 4): the first wins.  Scores beyond fp32 to the negative side are keys
+    without weight, and a zero code meets a query and a scale whose product is beyond fp32 as a zero."""
+    hq, hkv, dh = 4, 1, 128
+    codes = np.zeros((3, 1, 32, dh), np.uint8)
+    one, four = K.encode(np.array([1.0, 4.0]))
+    codes[0, 0, 0, 0], codes[0, 0, 1, 1] = one, four
+    codes[1, 0, :, 2], codes[1, 0, 5, 2] = one + 128, 0    # block 1: -1, and 0 at key 37
+    vcodes = np.zeros((3, 1, 32, dh), np.uint8)
+    vals = np.arange(1, 97) % 29 + 1.0
+    vcodes[:, 0] = K.encode(np.floor(vals)).reshape(3, 32, 1)
+    scales = np.ones((3, 1))
+    q = torch.zeros(nq, hq * dh, dtype=torch.bfloat16)
+    q[0, 0], q[0, 1] = 2.0 ** 110, 2.0 ** 104              # head 0: key 0
+    q[0, dh + 2] = 2.0 ** 120                              # head 1: block 1 loses but for its zero
+    (k8, ks), (v8, vs) = to_gpu(codes, scales), to_gpu(vcodes, np.ones((3, 1)))
+    ks[1] = 2.0 ** 30                                      # head 1's products there: -2^150 and 0
+    v = K.decode(vcodes)[:, 0, :, 0].reshape(-1)
+    out = host(B.op_attention_kv8(q.cuda(), k8, v8, ks, vs, ints([0, nq]), ints([0]), ints([70]), hq, max_nq=nq, max_vis=0))
+    out = out.reshape(nq, hq, dh)
+    tol = lambda x: x * (HALF_BF16 + 2.0 ** -10)           # noqa: E731
+    assert (np.abs(out[0, 0] - v[0]) <= tol(v[0])).all()
+    tied = np.r_[0:32, 37, 64:70]                          # all of them score zero
+    assert (np.abs(out[0, 1] - v[tied].mean()) <= tol(v[tied].mean())).all()
+    assert (np.abs(out[0, 2:] - v[:70].mean()) <= tol(v[:70].mean())).all()
