@@ -419,7 +419,9 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
         for (int u = 0; u < FLY; ++u) {
           const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&raw[u]);
           const float top = fmaxf(__low2float(top2[u]), __high2float(top2[u]));
-          const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 127);
+          // (2^-60 at least, under which no score passes 2^-4: a factor times a K scale of 2^-40 stays a normal number, and
+          // masked scores of -inf stay that)
+          const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -60), 127);
           const float up = pow2i(7 - e);
           const int f = f0 + (i0 + u) * RPI;
           // (an infinite element would saturate: its row becomes NaN here, as its softmax is)

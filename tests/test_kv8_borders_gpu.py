@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from oracle import kv8_oracle as K
-from test_kv8_gpu import B, HALF_BF16, attn_bound, attn_inputs, bf16, host, ints, prefix, to_gpu  # noqa: F401
+from test_kv8_gpu import B, HALF_BF16, attn_bound, attn_inputs, bf16, check_attention, host, ints, prefix, to_gpu  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -102,3 +102,19 @@ def test_large_queries_beside_small_ones_and_far_scales(B, nq):
     tied = np.r_[0:32, 37, 64:70]                          # all of them score zero
     assert (np.abs(out[0, 1] - v[tied].mean()) <= tol(v[tied].mean())).all()
     assert (np.abs(out[0, 2:] - v[:70].mean()) <= tol(v[:70].mean())).all()
+
+
+@pytest.mark.parametrize("hq,hkv,dh,rows", [(28, 4, 128, [(1, 77)]), (14, 2, 128, [(40, 97), (40, 130)]), (8, 2, 64, [(64, 200)]),
+                                            (28, 4, 128, [(300, 330)] * 6)])
+def test_queries_of_next_to_nothing_average(B, hq, hkv, dh, rows):
+    """Zero query rows, and rows of 2^-120, over blocks of zeros (whose scale is the least, 2^-40) that end inside a tile."""
+    rng = np.random.default_rng(len(rows) + dh)
+    n, vis, base, kc, vc, q = attn_inputs(rng, hq, hkv, dh, rows)
+    kc[0][kc[0] != 127] = 0
+    kc[1][np.isfinite(kc[1])] = 2.0 ** -40
+    q[::3] = 0
+    q[1::3] = (q[1::3].double() * 2.0 ** -120).to(torch.bfloat16)
+    (k8, ks), (v8, vs) = to_gpu(*kc), to_gpu(*vc)
+    out = B.op_attention_kv8(q.cuda(), k8, v8, ks, vs, ints(prefix(n)), ints(base), ints(vis), hq, max_nq=int(n.max()),
+                             max_vis=0)
+    check_attention(host(out), q, hq, dh, n, vis, base, kc, vc)
