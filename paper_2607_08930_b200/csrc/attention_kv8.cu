@@ -650,10 +650,16 @@ Route route_of(int n_rows, int M, int hint_nq, int max_vis, int hq, int hkv, int
   // with 255 registers: 20 rows x 32 tokens, 32 heads 38.2 us against 32.0 with 16, 64 rows 121 and 122.)
   w.nq = widest <= 8 ? 1 : 2;
   w.tq = 8 * w.nq / G;
+  // Workers per (row, kv head), when every item has one: the tiles of the largest row.  A worker goes on to the next tile of
+  // its row, so fewer do as well, and those that the tokens cannot fill are launched for nothing: without a hint one more than
+  // the rows' mean (512 rows x 1 to 16 tokens of 32 heads over up to 64 keys: 2344 us by the largest row there could be, 94
+  // by the mean, 66 with the hint), with one at most eight times as many as there can be items (a hint of M: 236 us).
+  const long long filled = (long long)M / w.tq + n_rows;           // tiles of one kv head, at most
+  const long long cap = hint_nq > 0 ? 8 * filled / n_rows : ((long long)M / n_rows + w.tq - 1) / w.tq + 1;
+  const int tiles = (int)std::min<long long>((max_nq + w.tq - 1) / w.tq, cap);
   // Single-warp workers where there are many items and two query tiles make each of them work for a warp.  64 rows x 32
   // tokens, 32 heads, 4096 items: 200 to 512 keys 89 us (107 with four-warp workers), 96 to 1024 122 us (131); 1280 items:
   // 96 to 500 keys 31.9 us (34.4), but 500 to 3000 114 us (106); 800 items 29.4 us (26.2).
-  const int tiles = (max_nq + w.tq - 1) / w.tq;
   const long long items = (long long)n_rows * hkv * tiles;
   w.many = w.nq > 1 && items >= (max_vis > 0 && max_vis <= 512 ? 6 : 16) * 148;
   // Short rows have a worker per item and nothing to merge; so do rows of some length where there are about as many items

@@ -118,3 +118,32 @@ def test_queries_of_next_to_nothing_average(B, hq, hkv, dh, rows):
     out = B.op_attention_kv8(q.cuda(), k8, v8, ks, vs, ints(prefix(n)), ints(base), ints(vis), hq, max_nq=int(n.max()),
                              max_vis=0)
     check_attention(host(out), q, hq, dh, n, vis, base, kc, vc)
+
+
+# ---- many rows, missing hints --------------------------------------------------------------------------------
+
+def ms_of(fn):
+    for _ in range(3):
+        fn()
+    best = 1e9
+    for _ in range(7):
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        fn()
+        b.record()
+        torch.cuda.synchronize()
+        best = min(best, a.elapsed_time(b))
+    return best
+
+
+@pytest.mark.parametrize("hq,hkv,dh,n_rows,nq", [(32, 32, 64, 512, 16), (16, 1, 128, 300, 40)])
+def test_many_short_rows_without_a_query_hint(B, hq, hkv, dh, n_rows, nq):
+    """Work grows with the tokens, not with rows x tokens: without max_nq a call takes at most three times as long."""
+    rng = np.random.default_rng(n_rows)
+    rows = [(int(a), int(b)) for a, b in zip(rng.integers(1, nq + 1, n_rows), rng.integers(0, 65, n_rows))]
+    n, vis, base, kc, vc, q = attn_inputs(rng, hq, hkv, dh, rows)
+    (k8, ks), (v8, vs) = to_gpu(*kc), to_gpu(*vc)
+    a = (q.cuda(), k8, v8, ks, vs, ints(prefix(n)), ints(base), ints(vis), hq)
+    told, untold = (lambda m=m: B.op_attention_kv8(*a, max_nq=m, max_vis=64) for m in (nq, 0))
+    check_attention(host(untold()), q, hq, dh, n, vis, base, kc, vc)
+    assert ms_of(untold) <= 3 * ms_of(told) + 0.02
