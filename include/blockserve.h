@@ -335,7 +335,9 @@ int bs_op_lm_head_confidence(const void* hf, int lda, const void* W, int M, int 
  * 16-byte aligned (scratch 256); row i owns packed tokens [cu[i], cu[i+1]), cu[0] = 0, non-decreasing; tokens at and
  * behind cu[n_rows] belong to no row and their outputs are left as they were.  Indices are checked on the device: a
  * token or row whose position, cache row or span lies outside the stated sizes is skipped, and error_flag (device int,
- * nullable, only ever raised) gets 100 or more.  Calls allocate nothing and may be captured into graphs; calls that
+ * nullable, only ever raised) gets 100 or more.  A wait inside the attention kernel that runs out (none does in a working
+ * machine) raises it to 1 at least, and the outputs that it kept from being formed are NaN; in the bounds-checked build a
+ * flag of -1 - t before the call makes them run out at a row's t-th key tile.  Calls allocate nothing and may be captured into graphs; calls that
  * share scratch must be ordered (same stream, or events). */
 enum { BS_KV8_BLOCK = 32, BS_KV8_MAX_ROWS = 1024 };
 

@@ -27,7 +27,8 @@
 // the same way of issuing took 529, and 398 with products issued by an elected lane.  16 block steps of 32 tokens over 320
 // to 800 keys, one query tile per CTA, 17.9 us, are bound by a CTA's beginning - indices, barriers, queries to two terms:
 // 4 us - and by its chain of three to seven tiles.
-// Every wait is bounded; on a timeout the flag is raised, all roles drain, the copies in flight are waited for.
+// Every wait is bounded; when one runs out the flag is raised, all roles drain, the copies and products in flight are
+// waited for, and the CTA's outputs are NaN.
 #include <float.h>
 #include <math.h>
 
@@ -188,7 +189,7 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
   using L = TcLayout<DH, NT>;
   enum { B_KFULL = 0, B_KEMPTY = B_KFULL + kKStages, B_V8FULL = B_KEMPTY + kKStages, B_V8EMPTY = B_V8FULL + kV8Stages,
          B_VFULL = B_V8EMPTY + kV8Stages, B_VEMPTY = B_VFULL + kV16Stages, B_QFULL = B_VEMPTY + kV16Stages,
-         B_SFULL = B_QFULL + 1, B_PFULL = B_SFULL + 2 * NT, B_OFULL = B_PFULL + 2 * NT, B_COUNT = B_OFULL + 2 * NT };
+         B_SFULL = B_QFULL + 1, B_PFULL = B_SFULL + 2 * NT, B_OFULL = B_PFULL + 2 * NT, B_LAST = B_OFULL + 2 * NT, B_COUNT };
   extern __shared__ unsigned char smem_dyn[];
   __shared__ __align__(8) unsigned long long bars[B_COUNT];
   __shared__ unsigned tmem_base_slot;
@@ -236,6 +237,7 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
       mbar_init(bar(B_PFULL + i), 4);
       mbar_init(bar(B_OFULL + i), 1);
     }
+    mbar_init(bar(B_LAST), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
@@ -252,6 +254,7 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
   constexpr unsigned tmem_base = 0;                         // the only place an allocation of all 512 columns can have
   volatile int* abort_flag = &s_abort;
   if (threadIdx.x == 0 && tmem_base_slot != 0) s_abort = 1;
+  auto wait = [&](unsigned b, unsigned parity) { return !(kBoundsCheck && *abort_flag) && mbar_wait(b, parity, abort_flag); };
   const int blk0 = base / kKv8Block + kt0 * (KT / kKv8Block);      // cache block of the chunk's first key
 
   // Two query tiles: 4 x 128 registers a thread at launch become 56 + 2 x 192 + 72.
@@ -262,10 +265,12 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
     // ------------------------------------------------------------------ TMA producer
     if (lane == 0 && n_tiles > 0) {
       int issued = 0;
+      const int give_up = kBoundsCheck && p.error_flag ? -1 - *(volatile int*)p.error_flag : -1;      // (for tests)
       for (int t = 0; t < n_tiles; ++t) {
+        if (kBoundsCheck && t == give_up) *abort_flag = 1;
         const int ks = t % kKStages, vs = t % kV8Stages;
-        if (!mbar_wait(bar(B_KEMPTY + ks), (unsigned)((t / kKStages) & 1) ^ 1u, abort_flag)) break;
-        if (!mbar_wait(bar(B_V8EMPTY + vs), (unsigned)((t / kV8Stages) & 1) ^ 1u, abort_flag)) break;
+        if (!wait(bar(B_KEMPTY + ks), (unsigned)((t / kKStages) & 1) ^ 1u)) break;
+        if (!wait(bar(B_V8EMPTY + vs), (unsigned)((t / kV8Stages) & 1) ^ 1u)) break;
         mbar_expect_tx(bar(B_KFULL + ks), (unsigned)L::k8);
         tma_load_4d(sK + ks * L::k8, &map_k, 0, 0, kh, blk0 + 4 * t, bar(B_KFULL + ks));
         mbar_expect_tx(bar(B_V8FULL + vs), (unsigned)L::k8);
@@ -289,7 +294,7 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
       // Scores of half h of key tile t for query tile x.  The place is free: the weights in it were read by the last
       // product issued before, and the tensor pipe runs one thread's instructions in order.
       auto scores = [&](int t, int x, int h) {
-        if (x == 0 && h == 0 && !mbar_wait(bar(B_KFULL + t % kKStages), (unsigned)(t / kKStages) & 1u, abort_flag)) return false;
+        if (x == 0 && h == 0 && !wait(bar(B_KFULL + t % kKStages), (unsigned)(t / kKStages) & 1u)) return false;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const unsigned q_hi = desc_lo(sQ + x * 2 * L::q_part), q_lo = desc_lo(sQ + x * 2 * L::q_part + L::q_part);
         const unsigned k_lo = desc_lo(sK + (t % kKStages) * L::k8 + h * (L::k8 / 2)), d = tmem_base + x * 128 + h * 64;
@@ -302,15 +307,15 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
         if (h == 1 && x == n_qt - 1) umma_commit(bar(B_KEMPTY + t % kKStages));
         return true;
       };
-      ok = mbar_wait(bar(B_QFULL), 0, abort_flag);
+      ok = wait(bar(B_QFULL), 0);
       for (int i = 0; i < 2 * n_qt && ok; ++i) ok = scores(0, NT == 1 ? 0 : i % n_qt, NT == 1 ? i : i / n_qt);
       for (int t = 0; t < n_tiles && ok; ++t) {
-        ok = mbar_wait(bar(B_VFULL + t % kV16Stages), (unsigned)(t / kV16Stages) & 1u, abort_flag);
+        ok = wait(bar(B_VFULL + t % kV16Stages), (unsigned)(t / kV16Stages) & 1u);
         const unsigned v_lo = desc_lo(sV16 + (t % kV16Stages) * L::v16, KT * 128);
 #pragma unroll 1
         for (int i = 0; i < 2 * n_qt && ok; ++i) {           // first halves of all query tiles, then the second ones
           const int x = NT == 1 || n_qt == 1 ? 0 : i & 1, h = NT == 1 || n_qt == 1 ? i : i >> 1;
-          ok = mbar_wait(bar(B_PFULL + 2 * x + h), (unsigned)t & 1u, abort_flag);
+          ok = wait(bar(B_PFULL + 2 * x + h), (unsigned)t & 1u);
           if (!ok) break;
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           const unsigned d = tmem_base + kOCol + x * 128, a = tmem_base + x * 128 + h * 64, v = v_lo + h * (KT / 32) * (2048 >> 4);
@@ -319,6 +324,12 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
           umma_commit(bar(B_OFULL + 2 * x + h));
           if (h == 1 && x == n_qt - 1) umma_commit(bar(B_VEMPTY + t % kV16Stages));
           if (t + 1 < n_tiles) ok = scores(t + 1, x, h);
+        }
+      }
+      if (!ok) {                    // products in flight end before their operands and the tensor memory are given up
+        umma_commit(bar(B_LAST));
+        const long long begin = clock64();
+        while (!mbar_try_wait(bar(B_LAST), 0) && clock64() - begin < kWaitCycles / 64) {
         }
       }
     }
@@ -331,8 +342,8 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
     const int j = c % LPK;
     for (int t = 0; t < n_tiles; ++t) {
       const int a = t % kV8Stages, b = t % kV16Stages;
-      if (!mbar_wait(bar(B_V8FULL + a), (unsigned)(t / kV8Stages) & 1u, abort_flag)) break;
-      if (!mbar_wait(bar(B_VEMPTY + b), (unsigned)((t / kV16Stages) & 1) ^ 1u, abort_flag)) break;
+      if (!wait(bar(B_V8FULL + a), (unsigned)(t / kV8Stages) & 1u)) break;
+      if (!wait(bar(B_VEMPTY + b), (unsigned)((t / kV16Stages) & 1) ^ 1u)) break;
       const int left = vis - (kt0 + t) * KT;
       const unsigned src = sV8 + a * L::k8 + c * 16, dst = sV16 + b * L::v16 + (j >> 2) * (KT * 128);
 #pragma unroll 1
@@ -451,9 +462,9 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
     float ref = -FLT_MAX, sum = 0.f;                         // (under any score but -inf, whose weight it makes 0)
     bool ok = true;
     // whole warps go on or give up: the tensor-memory instructions want all lanes
-    auto wait = [&](int i, int phase) {
-      if (__all_sync(0xffffffffu, mbar_try_wait(bar(i), (unsigned)phase & 1u))) return true;
-      return __all_sync(0xffffffffu, mbar_wait(bar(i), (unsigned)phase & 1u, abort_flag)) != 0;
+    auto warp_wait = [&](int i, int phase) {
+      if (__all_sync(0xffffffffu, !(kBoundsCheck && *abort_flag) && mbar_try_wait(bar(i), (unsigned)phase & 1u))) return true;
+      return __all_sync(0xffffffffu, wait(bar(i), (unsigned)phase & 1u)) != 0;
     };
     // The tile's four pairs of scales: lane l looks after block l % 4, one tile ahead.
     float ksn = 1.f, vsn = 1.f;
@@ -475,7 +486,7 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
       for (int h = 0; h < 2; ++h) {                          // 64 keys at a time: their scores fit the registers, read once
         // (These scores were issued after the weights that stood in their place were used, so no warp of the group - one
         // without query rows has nothing to hold it up - publishes here before all four have published there.)
-        if (!wait(B_SFULL + 2 * x + h, t)) return false;
+        if (!warp_wait(B_SFULL + 2 * x + h, t)) return false;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         if (warp_has_rows) {
           unsigned y[64];
@@ -513,7 +524,7 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
             }
             if (t > 0 || h > 0) {
               // the output stands still once the product issued last is in it
-              if (!wait(B_OFULL + 2 * x + (h ^ 1), t - 1 + h)) return false;
+              if (!warp_wait(B_OFULL + 2 * x + (h ^ 1), t - 1 + h)) return false;
               asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll 1
               for (int c = 0; c < DH / 32; ++c) {
@@ -569,7 +580,7 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
       const int left = vis - (kt0 + t) * KT;
       ok = __any_sync(0xffffffffu, !(f * sc_top < 0.5f)) ? tile(std::true_type(), t, f, lv, left) : tile(std::false_type(), t, f, lv, left);
     }
-    const bool have = ok && my_tiles > 0 && wait(B_OFULL + 2 * x + 1, my_tiles - 1);
+    const bool have = ok && my_tiles > 0 && warp_wait(B_OFULL + 2 * x + 1, my_tiles - 1);
     if (warp_has_rows) {
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       const bool valid = r < nrows;
@@ -577,8 +588,10 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
       const size_t tok = (size_t)(t0 + x * p.tq + rr / G);
       const size_t at = (tok * p.hq + kh * G + rr % G) * DH;
       const size_t ml_at = ((size_t)chunk * p.M + tok) * p.hq + kh * G + rr % G;
-      if (p.chunks > 1 && valid) p.part_ml[ml_at] = make_float2(have ? ref : -INFINITY, have ? sum : 0.f);
-      const float inv = have ? 1.0f / sum : 0.f;
+      // no keys: zeros; a wait that ran out: NaN, here and in what is merged of it
+      const float none = my_tiles > 0 ? __int_as_float(0x7fffffff) : 0.f;
+      if (p.chunks > 1 && valid) p.part_ml[ml_at] = make_float2(have ? ref : -INFINITY, have ? sum : none);
+      const float inv = have ? 1.0f / sum : 1.f;
       float* pdst = p.part_o + (size_t)chunk * p.M * p.hq * DH + at;
 #pragma unroll 1
       for (int c = 0; c < DH / 32; ++c) {
@@ -588,7 +601,7 @@ k_attention_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_const
           tmem_ld_wait();
         } else {
 #pragma unroll
-          for (int j = 0; j < 32; ++j) o[j] = 0u;        // no keys: zeros
+          for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(none);
         }
         if (!valid) continue;
         if (p.chunks > 1) {

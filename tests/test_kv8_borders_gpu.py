@@ -147,3 +147,45 @@ def test_many_short_rows_without_a_query_hint(B, hq, hkv, dh, n_rows, nq):
     told, untold = (lambda m=m: B.op_attention_kv8(*a, max_nq=m, max_vis=64) for m in (nq, 0))
     check_attention(host(untold()), q, hq, dh, n, vis, base, kc, vc)
     assert ms_of(untold) <= 3 * ms_of(told) + 0.02
+
+
+# ---- waits that run out --------------------------------------------------------------------------------------
+
+@pytest.fixture()
+def debug_lib(B, monkeypatch):
+    from paper_2607_08930_b200 import build
+    path = build.build(debug=True)
+    regular = B.lib()
+    monkeypatch.setattr(B, "LIB_PATH", path)
+    monkeypatch.setattr(B, "_lib", None)
+    assert B.lib() is not regular
+    return B
+
+
+@pytest.mark.parametrize("after", [0, 1, 2])
+@pytest.mark.parametrize("hq,hkv,dh,rows,alone", [
+    (14, 1, 128, [(9, 300)], True),                        # one CTA: everything it has is lost
+    (8, 1, 64, [(16, 290)], True),
+    (14, 1, 128, [(9, 1400)], False),                      # one tile of queries, its keys in chunks
+    (14, 2, 128, [(40, 300), (30, 0), (40, 700)], False),
+    (28, 4, 128, [(300, 500)] * 6, False)])                # two query tiles a CTA
+def test_a_wait_that_runs_out_leaves_no_result(debug_lib, hq, hkv, dh, rows, alone, after):
+    """In the bounds-checked build the waits of a CTA run out at key tile t when the flag holds -1 - t (the first one raises
+    it, so later CTAs may go on): the flag says so, outputs are NaN or right, rows without keys zeros, and the next call is
+    right."""
+    rng = np.random.default_rng(len(rows) + dh)
+    n, vis, base, kc, vc, q = attn_inputs(rng, hq, hkv, dh, rows)
+    (k8, ks), (v8, vs) = to_gpu(*kc), to_gpu(*vc)
+    flag = torch.full((1,), -1 - after, dtype=torch.int32, device="cuda")
+    run = lambda: host(debug_lib.op_attention_kv8(q.cuda(), k8, v8, ks, vs, ints(prefix(n)), ints(base), ints(vis), hq,   # noqa: E731
+                                                  max_nq=int(n.max()), max_vis=int(vis.max()), error_flag=flag))
+    got = run()
+    assert int(flag.item()) == 1
+    flag.zero_()
+    want = run()
+    assert int(flag.item()) == 0
+    check_attention(want, q, hq, dh, n, vis, base, kc, vc)
+    lost = np.isnan(got)
+    assert lost.any() and (got[~lost] == want[~lost]).all()
+    assert not lost[np.repeat(vis == 0, n)].any()
+    assert lost.all() or not alone
