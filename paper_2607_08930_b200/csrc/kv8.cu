@@ -113,9 +113,10 @@ constexpr int kWarps = 4;       // of a CTA of the bf16 pass
 constexpr int kUnroll = 3;      // heads in flight per lane
 
 // One warp: heads [h0, h1) of token t.  BF16KV: k and v heads go to cache row `kv_row` of kc / vc; else h1 <= hq.
-template <int DH, bool BF16KV>
+// wanted(): whether the token is to be handled, asked while its heads and position are on their way.
+template <int DH, bool BF16KV, typename Wanted>
 __device__ __forceinline__ void token_heads(const QkNormArgs& a, int t, int h0, int h1, size_t kv_row,
-                                            bf16* kc, bf16* vc) {
+                                            bf16* kc, bf16* vc, Wanted wanted) {
   constexpr int LPH = DH / 16, HPW = 32 / LPH;     // lanes per head, heads per warp pass
   const int lane = threadIdx.x & 31, p = lane % LPH, mine = lane / LPH;
   const int heads = a.hq + 2 * a.hkv;
@@ -127,6 +128,7 @@ __device__ __forceinline__ void token_heads(const QkNormArgs& a, int t, int h0, 
     for (int u = 0; u < kUnroll; ++u) raw[u] = h + u * HPW < h1 ? load_head<DH>(src + (size_t)(h + u * HPW) * DH, p) : no_head();
   };
   fetch(h0 + mine);                                // on its way beside the position and the angles
+  if (!wanted()) return;
   if (pos < 0 || pos >= a.max_pos) {               // warp-uniform
     if (lane == 0) bad_index(a.error_flag, SITE_QK_NORM);
     return;
@@ -175,7 +177,8 @@ __global__ void __launch_bounds__(kWarps * 32, 5) k_qk_norm_rope_kv(QkNormArgs a
     return;
   }
   const int heads = a.hq + 2 * a.hkv;
-  token_heads<DH, true>(a, t, part * per_share, min(heads, (part + 1) * per_share), (size_t)row, kc, vc);
+  token_heads<DH, true>(a, t, part * per_share, min(heads, (part + 1) * per_share), (size_t)row, kc, vc,
+                        [] { return true; });
 }
 
 // ---- 8-bit cache -------------------------------------------------------------------------------------------
@@ -185,6 +188,27 @@ struct Slot {
   int row, t0, n, at, base, len;     // len: kv_len of the row (0 where the caller has none)
   long long block;     // cache block
   int first;           // cache position (offset from the row's base) of the block's row 0
+};
+// Whether a row of n > 0 tokens from t0 on fits its slab and the call.
+__device__ __forceinline__ bool span_fits(int t0, int n, int base, int at, int M, long long n_blocks) {
+  return t0 >= 0 && n > 0 && (long long)t0 + n <= M && base >= 0 && base % kKv8Block == 0 && at >= 0 &&
+         (long long)base + at + n <= n_blocks * kKv8Block;
+}
+// Whether token t belongs to a row that fits, asked once by every warp of a CTA, as whole warps.  One warp looks the rows up
+// for its CTA, the 32 around the first token's, all at once (by every warp, the same few lines of the L2 hold all of them up:
+// 16 block steps 7.3 us, 6.8 so); a token behind those is looked up by its own warp.
+struct RowSpan {
+  int t0, t1, base, at;
+  __device__ __forceinline__ void load(int r, const int* __restrict__ cu, const int* __restrict__ kv_base,
+                                       const int* __restrict__ kv_at) {
+    t0 = __ldcg(cu + r);
+    t1 = __ldcg(cu + r + 1);
+    base = __ldcg(kv_base + r);
+    at = __ldcg(kv_at + r);
+  }
+  __device__ __forceinline__ int2 tokens(int M, long long n_blocks) const {       // none of a row that does not fit
+    return span_fits(t0, t1 - t0, base, at, M, n_blocks) ? make_int2(t0, t1) : make_int2(0, 0);
+  }
 };
 // false: the slot holds nothing (or indices that do not fit: flagged).  Every lane of the warp gets the same answer.
 __device__ __forceinline__ bool find_slot(int slot, const int* __restrict__ cu, const int* __restrict__ kv_base,
@@ -199,9 +223,7 @@ __device__ __forceinline__ bool find_slot(int slot, const int* __restrict__ cu, 
   s.at = __ldcg(kv_at + r);
   s.len = kv_len ? __ldcg(kv_len + r) : 0;
   if (s.n == 0) return false;
-  const bool ok = s.t0 >= 0 && s.n > 0 && t1 <= M && s.base >= 0 && s.base % kKv8Block == 0 && s.at >= 0 &&
-                  (long long)s.base + s.at + s.n <= n_blocks * kKv8Block;
-  if (!ok) {
+  if (!span_fits(s.t0, s.n, s.base, s.at, M, n_blocks)) {
     if ((threadIdx.x & 31) == 0) bad_index(flag, SITE_KV8);
     return false;
   }
@@ -391,14 +413,37 @@ __global__ void __launch_bounds__(kTileThreads<DH>, 768 / kTileThreads<DH>) k_qk
                                                                        Kv8Cache c, int q_ctas, int shares, int per_share,
                                                                        int per_cta) {
   __shared__ unsigned s_max[2][2][kTileThreads<DH> / 32];
+  __shared__ int2 s_rows[32];
+  __shared__ int s_first;
   __shared__ float4 s_gain[DH / 4];      // k_gain as floats, by the lanes' order: [four dims of a lane][lane]
   pdl_wait();
   pdl_trigger();
   if ((int)blockIdx.x < q_ctas) {
     const long long unit = (long long)blockIdx.x * (kTileThreads<DH> / 32) + (threadIdx.x >> 5);
-    const int t = (int)(unit / shares), part = (int)(unit % shares);
-    if (t >= min(a.M, __ldcg(cu_q + n_rows))) return;      // tokens behind the last row are left alone
-    token_heads<DH, false>(a, t, part * per_share, min(a.hq, (part + 1) * per_share), 0, nullptr, nullptr);
+    const int t = (int)(unit / shares), part = (int)(unit % shares), lane = threadIdx.x & 31;
+    RowSpan mine = {0, 0, 0, 0};
+    int first = 0;
+    auto look = [&](int token) {
+      if (n_rows > 32) first = 32 * warp_search((n_rows + 31) >> 5, token, [&](int i) { return __ldcg(cu_q + 32 * i); });
+      if (first + lane < n_rows) mine.load(first + lane, cu_q, kv_base, kv_at);
+    };
+    if (threadIdx.x < 32) look((int)((long long)blockIdx.x * (kTileThreads<DH> / 32) / shares));
+    auto holds = [&](int2 v) { return __any_sync(0xffffffffu, t >= v.x && t < v.y) != 0; };
+    auto wanted = [&] {
+      if (threadIdx.x < 32) s_rows[lane] = mine.tokens(a.M, c.n_blocks);
+      if (threadIdx.x == 0) s_first = first;
+      __syncthreads();
+      if (holds(s_rows[lane])) return true;
+      if (s_first + 32 >= n_rows) return false;
+      mine = {0, 0, 0, 0};
+      look(t);
+      return holds(mine.tokens(a.M, c.n_blocks));
+    };
+    // Tokens behind the last row are left alone, and so are those of rows that do not fit (the tiles' CTAs flag them).
+    if (t >= a.M)
+      wanted();                                            // (for the barrier)
+    else
+      token_heads<DH, false>(a, t, part * per_share, min(a.hq, (part + 1) * per_share), 0, nullptr, nullptr, wanted);
     return;
   }
   const int unit = (int)blockIdx.x - q_ctas;

@@ -4,7 +4,8 @@ import pytest
 import torch
 
 from oracle import kv8_oracle as K
-from test_kv8_gpu import B, HALF_BF16, attn_bound, attn_inputs, bf16, check_attention, host, ints, prefix, to_gpu  # noqa: F401
+from test_kv8_gpu import (B, EPS, HALF_BF16, THETA, attn_bound, attn_inputs, bf16, chain_tol, check_attention, host, ints,  # noqa: F401
+                          prefix, random_cache, to_gpu)
 
 pytestmark = pytest.mark.gpu
 
@@ -147,6 +148,46 @@ def test_many_short_rows_without_a_query_hint(B, hq, hkv, dh, n_rows, nq):
     told, untold = (lambda m=m: B.op_attention_kv8(*a, max_nq=m, max_vis=64) for m in (nq, 0))
     check_attention(host(untold()), q, hq, dh, n, vis, base, kc, vc)
     assert ms_of(untold) <= 3 * ms_of(told) + 0.02
+
+
+# ---- indices that do not fit ---------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("many", [0, 33, 250])
+def test_write_skips_the_queries_of_rows_that_do_not_fit(B, many):
+    """A row whose span does not fit is skipped whole, as a token with a bad cache row of the bf16 cache is: its queries stay
+    as they were, in place too, so that the call can be made again."""
+    hq, hkv, dh = 4, 2, 64
+    rng = np.random.default_rng(3)
+    n = np.array([2, 1, 3, 1, 2, 1, 0, 5])
+    base = np.array([16, -32, 128, 64, 0, 32, 7, 0])       # rows 0, 1, 2, 3, 4 do not fit (row 6 has no token)
+    at = np.array([0, 0, 0, 64, -1, 2, 0, 20])
+    bad = np.array([True] * 5 + [False] * 3)
+    if many:                                               # more rows than a CTA looks up at once, long stretches of empty ones
+        n = np.where(rng.random(many) < 0.5, 0, rng.integers(1, 4, many))
+        n[10:many // 3] = 0
+        bad = rng.random(many) < 0.3
+        base = 32 * np.arange(many)
+        at = np.where(bad, 32 * many, rng.integers(0, 29, many))
+    M, cu = int(n.sum()), prefix(n)
+    pad = 2
+    qkv = bf16(rng.normal(size=(M + pad, (hq + 2 * hkv) * dh)))
+    table = B.rope_table(50, dh, THETA)
+    pos = np.r_[np.arange(M) % 50, 3, 3]
+    (k8, ks), (v8, vs) = to_gpu(*random_cache(rng, max(4, many), hkv, dh)), to_gpu(*random_cache(rng, max(4, many), hkv, dh))
+    want = K.norm_rope(host(qkv)[:, :hq * dh].reshape(-1, hq, dh), None, EPS, pos, THETA).reshape(-1, hq * dh)
+    skipped = np.r_[np.repeat(bad, n), True, True]
+    for inplace in (False, True):
+        flag = torch.zeros(1, dtype=torch.int32, device="cuda")
+        x = qkv.cuda()
+        q_out = x if inplace else torch.full((M + pad, hq * dh), 9.0, dtype=torch.bfloat16, device="cuda")
+        before = host(q_out)
+        B.op_qk_norm_rope_kv8(x, None, None, EPS, ints(pos), ints(cu), ints(base), ints(at), ints(at), k8, v8, ks, vs, hq, hkv, dh,
+                              table, q_out=q_out, error_flag=flag)
+        assert int(flag.item()) >= 100
+        got = host(q_out)
+        assert (got[skipped] == before[skipped]).all()
+        g, w = got[~skipped, :hq * dh], want[~skipped]
+        assert (np.abs(g - w).reshape(-1, hq, dh) <= (np.abs(w) * HALF_BF16).reshape(-1, hq, dh) + 2 * chain_tol(w.reshape(-1, hq, dh), dh)).all()
 
 
 # ---- waits that run out --------------------------------------------------------------------------------------
