@@ -349,7 +349,7 @@ int bs_rope_table(float* host_table, int max_pos, int head_dim, float theta);
  *   y = gain * x / sqrt(mean(x^2) + eps) over the head's dims, then the pairs (y_j, y_{j + head_dim/2}) turned by the
  *   angle of the token's position id (rope_table, device memory), all in fp32 and rounded once to bf16.
  * Query heads go to q_out (row stride q_ld elements, a multiple of 8; q_out = qkv with q_ld = (Hq + 2 Hkv) * head_dim
- * rotates in place), k and v to cache row tok_kv[t] of the bf16 caches [kv_rows][Hkv][head_dim]; tok_kv[t] < 0: the
+ * rotates in place; any other overlap with qkv is refused), k and v to cache row tok_kv[t] of the bf16 caches [kv_rows][Hkv][head_dim]; tok_kv[t] < 0: the
  * token belongs to no row and is skipped.  q_gain / k_gain: bf16 [head_dim], or both NULL (rotation only).
  * Tokens of one call must name different cache rows. */
 int bs_op_qk_norm_rope_kv(const void* qkv, const void* q_gain, const void* k_gain, float eps, const int* tok_pos,
@@ -378,7 +378,7 @@ int bs_op_kv8_read(const void* k8, const void* v8, const float* k_scale, const f
 /* Ragged bidirectional attention over the 8-bit cache: the queries of row i attend to cache positions [0, vis[i]) of
  * its slab (no causal or padding mask); out bf16 [M][Hq * head_dim]; vis[i] = 0 gives zeros.  Codes behind vis[i] may
  * be anything, NaN included.  q bf16, row stride q_ld elements (a multiple of 8): q_out of the operators above, or
- * the query part of a qkv buffer.  max_nq (0: unknown) and max_vis (0: unknown) are the largest query count and vis of
+ * the query part of a qkv buffer; out may be q where q_ld = Hq * head_dim, other overlaps are refused.  max_nq (0: unknown) and max_vis (0: unknown) are the largest query count and vis of
  * a row; they choose the kernel, not the result's meaning.  At most BS_KV8_MAX_ROWS rows and 32 query heads per kv
  * head.  scratch: bs_op_attention_kv8_scratch_bytes bytes of device memory, overwritten; may be NULL for sizes of which
  * bs_op_attention_kv8_uses_scratch says 0 (whole items by workers of their own, keys that are not cut). */

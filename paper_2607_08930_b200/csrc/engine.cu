@@ -971,6 +971,12 @@ static bool aligned16(std::initializer_list<const void*> ps) {
     if (!p || ((uintptr_t)p & 15)) return false;
   return true;
 }
+// Whether `rows` rows of `width` bf16 elements, `ld` apart, from `a` on meet [b, b + b_elements).
+static bool rows_meet(const void* a, int rows, long long ld, long long width, const void* b, long long b_elements) {
+  const long long at = ((const char*)b - (const char*)a) / 2;            // of b in a's elements
+  const long long r = at < width ? 0 : (at - width) / ld + 1;            // the first row that ends behind b
+  return r < rows && r * ld < at + b_elements;
+}
 static bool kv8_cache_of(const void* k8, const void* v8, const float* ks, const float* vs, long long kv_rows, Kv8Cache* c) {
   if (!aligned16({k8, v8, ks, vs}) || kv_rows < kKv8Block || kv_rows % kKv8Block || kv_rows > 0x7fffffffll) return false;
   *c = Kv8Cache{(unsigned char*)k8, (unsigned char*)v8, (float*)ks, (float*)vs, kv_rows / kKv8Block};
@@ -982,6 +988,9 @@ static bool qk_norm_args(const void* qkv, const void* q_gain, const void* k_gain
   if (M < 0 || !kv8_shape_ok(hq, hkv, dh) || max_pos < 1 || !(eps >= 0.f) || !tok_pos) return false;
   if (!aligned16({qkv, q_out, table}) || q_ld < hq * dh || q_ld % 8 || (!q_gain != !k_gain)) return false;
   if (q_gain && !aligned16({q_gain, k_gain})) return false;
+  // every token's heads are read and written by several warps: in place is right, over other tokens' rows is not
+  const long long width = (long long)(hq + 2 * hkv) * dh;
+  if (!(q_out == qkv && (M == 1 || q_ld == width)) && rows_meet(q_out, M, q_ld, (long long)hq * dh, qkv, M * width)) return false;
   *a = QkNormArgs{(const bf16*)qkv, (bf16*)q_out, q_ld, (const bf16*)q_gain, (const bf16*)k_gain, eps, tok_pos,
                   table, max_pos, M, hq, hkv, dh, error_flag};
   return true;
@@ -1056,6 +1065,8 @@ int bs_op_attention_kv8(const void* q, int q_ld, const void* k8, const void* v8,
       !aligned16({q, out}) || ((uintptr_t)scratch & 255) || !cu_q || !kv_base || !vis ||
       ((!scratch || scratch_bytes < attention_kv8_scratch_bytes(n_q_heads, n_kv_heads, head_dim)) &&
        attention_kv8_uses_scratch(n_rows, M, max_nq, max_vis, n_q_heads, n_kv_heads, head_dim)) ||
+      (!(out == q && (M == 1 || q_ld == n_q_heads * head_dim)) &&
+       rows_meet(q, M, q_ld, (long long)n_q_heads * head_dim, out, (long long)M * n_q_heads * head_dim)) ||
       !kv8_cache_of(k8, v8, k_scale, v_scale, kv_rows, &a.cache))
     return BS_E_ARG;
   a.q = (const bf16*)q; a.q_ld = q_ld; a.out = (bf16*)out;

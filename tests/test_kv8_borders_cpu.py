@@ -1,0 +1,42 @@
+"""Refusals of the 8-bit cache operators that need no GPU: buffers that overlap, numbers of rows."""
+import pytest
+
+from test_kv8_cpu import B, P, _attn, _norm8  # noqa: F401
+
+E = 2            # bytes of an element
+
+
+# qkv of two tokens, 1024 elements each, at P; 512 elements of queries per token
+@pytest.mark.parametrize("at,ld", [(0, 512), (0, 2048), (8, 1024), (512, 512), (1024, 1024), (1536, 512), (2040, 512), (-8, 512),
+                                   (-1016, 512), (-512 + 8, 4096), (-4096, 4096), (-4096 + 2040, 4096)])
+def test_queries_over_other_tokens_inputs_are_refused(B, at, ld):
+    assert _norm8(B, q_out=P + E * at, ld=ld) == B.BS_E_ARG
+    rc = B.lib().bs_op_qk_norm_rope_kv(P, P, P, 1e-6, P, P, P + E * at, ld, 2 * P, 2 * P, 64, 2, 4, 2, 128, P, 9, None, None)
+    assert rc == B.BS_E_ARG
+
+
+# q rows of 3584 elements
+@pytest.mark.parametrize("at,ld", [(0, 4096), (8, 3584), (3584, 3584), (-8, 3584), (7160, 3584), (4096, 4096), (512 - 3584, 4096)])
+def test_outputs_over_other_tokens_queries_are_refused(B, at, ld):
+    assert _attn(B, out=P + E * at, q_ld=ld) == B.BS_E_ARG
+
+
+OVERS = {}
+for _name in ("test_write_refuses", "test_norm_refuses"):
+    import test_kv8_cpu
+    OVERS[_name] = getattr(test_kv8_cpu, _name).pytestmark[0].args[1]
+
+
+@pytest.mark.parametrize("over", OVERS["test_write_refuses"], ids=str)
+def test_write_refuses_with_queries_of_their_own(B, over):
+    assert _norm8(B, **{"q_out": 4 * P, **over}) == B.BS_E_ARG
+
+
+@pytest.mark.parametrize("over", OVERS["test_norm_refuses"], ids=str)
+def test_norm_refuses_with_queries_of_their_own(B, over):
+    a = dict(qkv=P, gq=P, gk=P, eps=1e-6, pos=P, tok_kv=P, q_out=4 * P, ld=512, kc=P, vc=P, rows=64, M=2, hq=4, hkv=2, dh=128,
+             table=P, max_pos=9)
+    a.update(over)
+    assert B.lib().bs_op_qk_norm_rope_kv(a["qkv"], a["gq"], a["gk"], a["eps"], a["pos"], a["tok_kv"], a["q_out"], a["ld"],
+                                         a["kc"], a["vc"], a["rows"], a["M"], a["hq"], a["hkv"], a["dh"], a["table"],
+                                         a["max_pos"], None, None) == B.BS_E_ARG

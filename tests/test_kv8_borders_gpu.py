@@ -230,3 +230,44 @@ def test_a_wait_that_runs_out_leaves_no_result(debug_lib, hq, hkv, dh, rows, alo
     assert lost.any() and (got[~lost] == want[~lost]).all()
     assert not lost[np.repeat(vis == 0, n)].any()
     assert lost.all() or not alone
+
+
+# ---- buffers that share memory -------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("hq,hkv,dh,rows,told", [
+    (28, 4, 128, [(1, 300), (1, 0), (1, 77)], True), (28, 4, 128, [(1, 3000), (1, 20)], False), (32, 32, 128, [(32, 200)] * 9, True),
+    (14, 2, 128, [(40, 300), (9, 0), (64, 90)], True), (28, 4, 128, [(300, 500)] * 6, True), (14, 1, 128, [(9, 1400)], True)])
+def test_attention_in_place(B, hq, hkv, dh, rows, told):
+    rng = np.random.default_rng(len(rows))
+    n, vis, base, kc, vc, q = attn_inputs(rng, hq, hkv, dh, rows)
+    (k8, ks), (v8, vs) = to_gpu(*kc), to_gpu(*vc)
+    a = (k8, v8, ks, vs, ints(prefix(n)), ints(base), ints(vis), hq)
+    kw = dict(max_nq=int(n.max()), max_vis=int(vis.max()) if told else 0)
+    want = B.op_attention_kv8(q.cuda(), *a, **kw)
+    x = q.cuda()
+    assert B.op_attention_kv8(x, *a, out=x, **kw) is x and torch.equal(x, want)
+
+
+def test_buffers_side_by_side_in_one_allocation(B):
+    """Queries right before and right behind their inputs, and two rows of them around the inputs, are no overlap."""
+    hq, hkv, dh, M = 4, 2, 64, 2
+    width, wq = (hq + 2 * hkv) * dh, hq * dh
+    rng = np.random.default_rng(1)
+    qkv = bf16(rng.normal(size=(M, width)))
+    table = B.rope_table(8, dh, THETA)
+    mem = torch.empty(4 * M * width, dtype=torch.bfloat16, device="cuda")
+    x = mem[M * width:2 * M * width].view(M, width)
+    kc = torch.zeros(8, hkv, dh, dtype=torch.bfloat16, device="cuda")
+    call = lambda q: B.op_qk_norm_rope_kv(x, None, None, EPS, ints([3, 4]), ints([0, 1]), kc, torch.zeros_like(kc), hq, hkv, dh,   # noqa: E731
+                                          table, q_out=q)
+    x.copy_(qkv)
+    want = call(None)
+    for q in (mem[M * width - M * wq:M * width].view(M, wq), mem[2 * M * width:2 * M * width + M * wq].view(M, wq),
+              mem.as_strided((M, wq), (M * width + wq, 1), M * width - wq)):
+        assert torch.equal(call(q), want) and torch.equal(x.cpu(), qkv)
+    with pytest.raises(B.BlockServeError):
+        call(mem.as_strided((M, wq), (M * width + wq - 8, 1), M * width - wq))
+    k8, v8, ks, vs = B.kv8_cache(32, hkv, dh)
+    with pytest.raises(B.BlockServeError):
+        B.op_qk_norm_rope_kv8(x, None, None, EPS, ints([3, 4]), ints([0, 2]), ints([0]), ints([0]), ints([0]), k8, v8, ks, vs, hq, hkv,
+                              dh, table, q_out=x[:, dh:])
