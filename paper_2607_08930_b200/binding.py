@@ -449,7 +449,7 @@ def op_confidence(logits: torch.Tensor, mask_id: int):
 
 # ---- per-head norms with the rotation, and the 8-bit KV cache -----------------------------------------------------
 
-KV8_BLOCK, KV8_MAX_ROWS = 32, 1024
+KV8_BLOCK, KV8_MAX_ROWS = 32, 1024      # BS_KV8_BLOCK, BS_KV8_MAX_ROWS
 _BF16, _F32, _I32, _E4M3, _U8 = torch.bfloat16, torch.float32, torch.int32, torch.float8_e4m3fn, torch.uint8
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda dev: torch.cuda.current_stream(dev).cuda_stream)      # the handle alone: a fiftieth of the Stream object's cost
@@ -652,6 +652,8 @@ def op_attention_kv8(q, k8, v8, k_scale, v_scale, cu_q, kv_base, vis, hq: int, m
     M = q.shape[0]
     ld = _row_stride(name, dev, "q", q, M, hq * dh)
     n = _rows_of(name, dev, "cu_q kv_base vis", cu_q, kv_base, vis)
+    if n > KV8_MAX_ROWS:
+        _refuse(name, f"at most {KV8_MAX_ROWS} rows, got {n}")
     if out is None:
         out = torch.empty(M, hq * dh, dtype=_BF16, device=q.device)
     else:

@@ -962,6 +962,7 @@ int bs_op_confidence(const float* logits, int n_rows, int vocab, int mask_id, in
 
 // ---- per-head norms with the rotation, and the 8-bit KV cache -------------------------------------------------
 
+static_assert(BS_KV8_BLOCK == kKv8Block, "the header's block and the kernels'");
 static bool kv8_shape_ok(int hq, int hkv, int dh) {
   return hkv >= 1 && hkv <= 65535 && hq >= 1 && hq % hkv == 0 && hq / hkv <= 32 && (dh == 64 || dh == 128) &&
          (long long)(hq + 2ll * hkv) * dh <= (1 << 24);
@@ -1060,7 +1061,7 @@ int bs_op_attention_kv8(const void* q, int q_ld, const void* k8, const void* v8,
                         int head_dim, void* scratch, size_t scratch_bytes, int* error_flag, void* stream) {
   if (M == 0 || n_rows == 0) return BS_OK;
   AttnKv8Args a;
-  if (M < 0 || n_rows < 1 || n_rows > kAttnKv8MaxRows || max_nq < 0 || max_vis < 0 ||
+  if (M < 0 || n_rows < 1 || n_rows > BS_KV8_MAX_ROWS || max_nq < 0 || max_vis < 0 ||
       !kv8_shape_ok(n_q_heads, n_kv_heads, head_dim) || q_ld < n_q_heads * head_dim || q_ld % 8 ||
       !aligned16({q, out}) || ((uintptr_t)scratch & 255) || !cu_q || !kv_base || !vis ||
       ((!scratch || scratch_bytes < attention_kv8_scratch_bytes(n_q_heads, n_kv_heads, head_dim)) &&

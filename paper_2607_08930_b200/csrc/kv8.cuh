@@ -119,7 +119,6 @@ struct AttnKv8Args {
   size_t scratch_bytes;
   int* error_flag;
 };
-constexpr int kAttnKv8MaxRows = 1024;
 size_t attention_kv8_scratch_bytes(int hq, int hkv, int dh);
 // Whether a call of these sizes puts anything there.
 bool attention_kv8_uses_scratch(int n_rows, int M, int max_nq, int max_vis, int hq, int hkv, int dh);

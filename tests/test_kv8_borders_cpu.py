@@ -1,5 +1,9 @@
 """Refusals of the 8-bit cache operators that need no GPU: buffers that overlap, numbers of rows."""
+import os
+import re
+
 import pytest
+import torch
 
 from test_kv8_cpu import B, P, _attn, _norm8  # noqa: F401
 
@@ -40,3 +44,16 @@ def test_norm_refuses_with_queries_of_their_own(B, over):
     assert B.lib().bs_op_qk_norm_rope_kv(a["qkv"], a["gq"], a["gk"], a["eps"], a["pos"], a["tok_kv"], a["q_out"], a["ld"],
                                          a["kc"], a["vc"], a["rows"], a["M"], a["hq"], a["hkv"], a["dh"], a["table"],
                                          a["max_pos"], None, None) == B.BS_E_ARG
+
+
+def test_the_row_limit_is_one_number_and_named(B):
+    header = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "blockserve.h")).read()
+    block, rows = map(int, re.search(r"BS_KV8_BLOCK = (\d+), BS_KV8_MAX_ROWS = (\d+)", header).groups())
+    assert (B.KV8_BLOCK, B.KV8_MAX_ROWS) == (block, rows)
+    q = torch.zeros(4, 256, dtype=torch.bfloat16)
+    cache = B.kv8_cache(64, 2, 64, device="cpu")
+    for n, why in ((rows, "CUDA"), (rows + 1, str(rows))):
+        idx = torch.zeros(n + 1, dtype=torch.int32)
+        with pytest.raises(B.BlockServeError, match=why):
+            B.op_attention_kv8(q, *cache, idx, idx, idx, 4, scratch=torch.empty(256, dtype=torch.uint8))
+    assert _attn(B, n_rows=rows + 1) == B.BS_E_ARG
