@@ -1,11 +1,15 @@
 """Calls at the borders of what the 8-bit cache operators take, against the 64-bit oracle (needs a B200)."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
 
 from oracle import kv8_oracle as K
 from test_kv8_gpu import (B, EPS, HALF_BF16, THETA, attn_bound, attn_inputs, bf16, chain_tol, check_attention, host, ints,  # noqa: F401
-                          prefix, random_cache, to_gpu)
+                          prefix, random_cache, slabs, to_gpu)
 
 pytestmark = pytest.mark.gpu
 
@@ -150,6 +154,41 @@ def test_many_short_rows_without_a_query_hint(B, hq, hkv, dh, n_rows, nq):
     assert ms_of(untold) <= 3 * ms_of(told) + 0.02
 
 
+@pytest.mark.parametrize("hq,hkv,dh,nq,top,hint", [(28, 4, 128, 1, 300, 300), (4, 2, 64, 2, 700, 0), (14, 2, 128, 10, 200, 200)])
+def test_as_many_rows_as_a_call_takes(B, hq, hkv, dh, nq, top, hint):
+    rng = np.random.default_rng(top)
+    rows = [(int(a), int(b)) for a, b in zip(rng.integers(0, nq + 1, 1024), rng.integers(0, top + 1, 1024))]
+    n, vis, base, kc, vc, q = attn_inputs(rng, hq, hkv, dh, rows)
+    (k8, ks), (v8, vs) = to_gpu(*kc), to_gpu(*vc)
+    out = B.op_attention_kv8(q.cuda(), k8, v8, ks, vs, ints(prefix(n)), ints(base), ints(vis), hq, max_nq=nq, max_vis=hint)
+    check_attention(host(out), q, hq, dh, n, vis, base, kc, vc)
+
+
+def test_write_and_read_of_many_rows(B):
+    """More rows than two rounds of the search over them reach: writes bit for bit (V), and read back."""
+    hq, hkv, dh = 2, 1, 64
+    rng = np.random.default_rng(9)
+    n, at = rng.integers(0, 4, 1500), rng.integers(0, 70, 1500)
+    base, blocks = slabs(rng, at + n, gap=False)
+    M, cu = int(n.sum()), prefix(n)
+    qkv = bf16(rng.normal(size=(M, 4 * dh)))
+    row = np.repeat(np.arange(1500), n)
+    pos = at[row] + np.arange(M) - cu[row]
+    cv, sv = random_cache(rng, blocks, hkv, dh)
+    (k8, ks), (v8, vs) = to_gpu(*random_cache(rng, blocks, hkv, dh)), to_gpu(cv, sv)
+    flag = torch.zeros(1, dtype=torch.int32, device="cuda")
+    q = B.op_qk_norm_rope_kv8(qkv.cuda(), None, None, EPS, ints(pos), ints(cu), ints(base), ints(at), ints(at), k8, v8, ks, vs,
+                              hq, hkv, dh, B.rope_table(100, dh, THETA), error_flag=flag)
+    x = host(qkv).reshape(M, 4, dh)
+    ref = K.norm_rope(x[:, :hq], None, EPS, pos, THETA)
+    assert (np.abs(host(q).reshape(M, hq, dh) - ref) <= np.abs(ref) * HALF_BF16 + 2 * chain_tol(ref, dh)).all()
+    rv, rsv = K.write(cv, sv, list(zip(cu[:-1], n, base, at, at)), x[:, 3:])
+    assert (vs.cpu().numpy() == rsv).all() and (v8.view(torch.uint8).cpu().numpy() == rv).all()
+    _, vo = B.op_kv8_read(k8, v8, ks, vs, ints(cu), ints(base), ints(at), M, error_flag=flag)
+    assert (host(vo) == np.concatenate([K.span(rv, rsv, base[i], at[i], n[i]) for i in range(1500)])).all()
+    assert int(flag.item()) == 0
+
+
 # ---- indices that do not fit ---------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("many", [0, 33, 250])
@@ -271,3 +310,72 @@ def test_buffers_side_by_side_in_one_allocation(B):
     with pytest.raises(B.BlockServeError):
         B.op_qk_norm_rope_kv8(x, None, None, EPS, ints([3, 4]), ints([0, 2]), ints([0]), ints([0]), ints([0]), k8, v8, ks, vs, hq, hkv,
                               dh, table, q_out=x[:, dh:])
+
+
+# ---- small caches, tight bounds, first calls -----------------------------------------------------------------
+
+@pytest.mark.parametrize("blocks", [1, 2, 3, 4])
+@pytest.mark.parametrize("hq,hkv,dh,nq", [(14, 2, 128, 40), (8, 2, 64, 64), (28, 4, 128, 1)])
+def test_caches_of_less_than_a_key_tile(B, hq, hkv, dh, nq, blocks):
+    rng = np.random.default_rng(blocks)
+    vis = blocks * 32 - 5
+    ck, sk = random_cache(rng, blocks, hkv, dh, spread=0)
+    cv, sv = random_cache(rng, blocks, hkv, dh)
+    ck[-1, :, 27:], cv[-1, :, 27:] = 127, 127
+    q = bf16(rng.normal(size=(nq, hq * dh)))
+    (k8, ks), (v8, vs) = to_gpu(ck, sk), to_gpu(cv, sv)
+    out = B.op_attention_kv8(q.cuda(), k8, v8, ks, vs, ints([0, nq]), ints([0]), ints([vis]), hq, max_nq=nq)
+    check_attention(host(out), q, hq, dh, np.array([nq]), np.array([vis]), np.array([0]), (ck, sk), (cv, sv))
+
+
+@pytest.mark.parametrize("hq,hkv,dh,nq,vis", [(28, 4, 128, 1, 500), (28, 4, 128, 1, 3000), (32, 32, 128, 32, 300), (8, 2, 64, 12, 400)])
+def test_streamed_queries_keep_their_small_elements(B, hq, hkv, dh, nq, vis):
+    """One channel of the queries is 2^12 times the others and meets keys of zero there.  The streaming kernel holds a query
+    in fp16 after its row's largest element has come to [1, 2): an element is off by 2^-25 of that one at most (bf16's 8
+    bits fit fp16's 11; half its least step is 2^-25), so the bound has that in place of the two-term 2^-17."""
+    rng = np.random.default_rng(nq + vis)
+    n, at, base, kc, vc, q = attn_inputs(rng, hq, hkv, dh, [(nq, vis)])
+    q = q.reshape(nq, hq, dh)
+    q[:, :, 7] = 2.0 ** 12
+    q = q.reshape(nq, hq * dh)
+    seen = kc[0] != 127
+    kc[0][..., 7] = np.where(seen[..., 7], 0, 127)
+    (k8, ks), (v8, vs) = to_gpu(*kc), to_gpu(*vc)
+    out = B.op_attention_kv8(q.cuda(), k8, v8, ks, vs, ints([0, nq]), ints(base), ints([vis]), hq, max_nq=nq, max_vis=vis)
+    k, v = K.span(*kc, base[0], 0, vis), K.span(*vc, base[0], 0, vis)
+    ref, mag, dot, flat = K.attention(host(q).reshape(nq, hq, dh), k, v)
+    tol = attn_bound(ref, mag, dot, flat * 2.0 ** -8, np.abs(v).max(), vis, dh)
+    assert (np.abs(host(out).reshape(nq, hq, dh) - ref) <= tol).all()
+
+
+FIRST_CALL = """
+import sys, torch
+from paper_2607_08930_b200 import binding as B
+hq, hkv, dh, nq = 14, 2, 128, int(sys.argv[1])
+torch.manual_seed(0)
+ints = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+k8, v8, ks, vs = B.kv8_cache(2048, hkv, dh)
+qkv = torch.randn(2 * nq, (hq + 2 * hkv) * dh, device="cuda").bfloat16()
+idx = ints(0, nq, 2 * nq), ints(0, 1024), ints(0, 0), ints(0, 0)
+pos, vis = torch.arange(2 * nq, dtype=torch.int32, device="cuda") % nq, ints(nq, nq)
+table = B.rope_table(nq, dh, 1e4)
+def step():
+    q = B.op_qk_norm_rope_kv8(qkv, None, None, 1e-6, pos, *idx, k8, v8, ks, vs, hq, hkv, dh, table)
+    return B.op_attention_kv8(q, k8, v8, ks, vs, idx[0], idx[1], vis, hq), B.op_kv8_read(k8, v8, ks, vs, idx[0], idx[1], idx[2], 2 * nq)[1]
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    got = step()
+g.replay()
+torch.cuda.synchronize()
+want = step()
+assert all(torch.equal(a, b) for a, b in zip(got, want)) and torch.isfinite(got[0].float()).all()
+print("same")
+"""
+
+
+@pytest.mark.parametrize("nq", ["1", "70"])
+def test_the_first_call_of_a_process_may_be_captured(B, nq):
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST_CALL, nq], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "same" in r.stdout, r.stderr[-2000:]
