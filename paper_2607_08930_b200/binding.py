@@ -533,7 +533,10 @@ def _row_stride(name: str, dev: int, arg: str, t: torch.Tensor, rows: int, width
             (t.stride(1) != 1 and t.numel() > 0):
         _refuse(name, f"{arg} must be a bfloat16 matrix of at least {rows} rows of {width} adjacent elements on the "
                       f"operator's device, got {tuple(t.shape)} {t.dtype} on {t.device}")
-    return t.stride(0) if rows > 1 else max(t.stride(0), shape[1])
+    ld = t.stride(0) if rows > 1 else max(t.stride(0), shape[1])
+    if ld > 0x7fffffff:                       # (ctypes would pass its low bits on)
+        _refuse(name, f"{arg}'s row stride of {ld} elements does not fit 31 bits")
+    return ld
 
 
 def _norm_inputs(name: str, dev: int, qkv, q_gain, k_gain, tok_pos, hq, hkv, dh, rope, q_out, error_flag):

@@ -57,3 +57,18 @@ def test_the_row_limit_is_one_number_and_named(B):
         with pytest.raises(B.BlockServeError, match=why):
             B.op_attention_kv8(q, *cache, idx, idx, idx, 4, scratch=torch.empty(256, dtype=torch.uint8))
     assert _attn(B, n_rows=rows + 1) == B.BS_E_ARG
+
+
+def test_row_strides_beyond_31_bits_are_refused(B):
+    """Passed on as they are, their low 32 bits would read other rows."""
+    hq, hkv, dh, M = 4, 2, 64, 2
+    far = torch.empty_strided((M, hq * dh), ((1 << 32) + hq * dh, 1), dtype=torch.bfloat16, device="meta")
+    cache = B.kv8_cache(64, hkv, dh, device="cpu")
+    idx = torch.zeros(M + 1, dtype=torch.int32)
+    with pytest.raises(B.BlockServeError, match="row stride"):
+        B.op_attention_kv8(far, *cache, idx[:2], idx, idx, hq, scratch=torch.empty(256, dtype=torch.uint8))
+    qkv = torch.zeros(M, (hq + 2 * hkv) * dh, dtype=torch.bfloat16)
+    kc = torch.zeros(64, hkv, dh, dtype=torch.bfloat16)
+    with pytest.raises(B.BlockServeError, match="row stride"):
+        B.op_qk_norm_rope_kv(qkv, None, None, 1e-6, idx, idx, kc, kc.clone(), hq, hkv, dh, B.rope_table(8, dh, 1e4, device="cpu"),
+                             q_out=far)
