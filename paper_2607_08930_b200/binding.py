@@ -533,7 +533,9 @@ def _row_stride(name: str, dev: int, arg: str, t: torch.Tensor, rows: int, width
             (t.stride(1) != 1 and t.numel() > 0):
         _refuse(name, f"{arg} must be a bfloat16 matrix of at least {rows} rows of {width} adjacent elements on the "
                       f"operator's device, got {tuple(t.shape)} {t.dtype} on {t.device}")
-    ld = t.stride(0) if rows > 1 else max(t.stride(0), shape[1])
+    if rows <= 1:
+        return width
+    ld = t.stride(0)
     if ld > 0x7fffffff:                       # (ctypes would pass its low bits on)
         _refuse(name, f"{arg}'s row stride of {ld} elements does not fit 31 bits")
     return ld

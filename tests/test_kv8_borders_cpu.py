@@ -72,3 +72,11 @@ def test_row_strides_beyond_31_bits_are_refused(B):
     with pytest.raises(B.BlockServeError, match="row stride"):
         B.op_qk_norm_rope_kv(qkv, None, None, 1e-6, idx, idx, kc, kc.clone(), hq, hkv, dh, B.rope_table(8, dh, 1e4, device="cpu"),
                              q_out=far)
+
+
+@pytest.mark.parametrize("extra", [0, 3, 8])
+def test_a_single_row_has_no_stride(B, extra):
+    """One row wider than its queries by any number of elements: only the width counts."""
+    q = torch.zeros(1, 256 + extra, dtype=torch.bfloat16)
+    assert B._row_stride("x", -1, "q", q, 1, 256) == 256
+    assert B._row_stride("x", -1, "q", torch.zeros(2, 256 + extra, dtype=torch.bfloat16), 2, 256) == 256 + extra
