@@ -335,10 +335,10 @@ int bs_op_lm_head_confidence(const void* hf, int lda, const void* W, int M, int 
  * 16-byte aligned (scratch 256); row i owns packed tokens [cu[i], cu[i+1]), cu[0] = 0, non-decreasing; tokens at and
  * behind cu[n_rows] belong to no row and their outputs are left as they were.  Indices are checked on the device: a
  * token or row whose position, cache row or span lies outside the stated sizes is skipped, and error_flag (device int,
- * nullable, only ever raised) gets 100 or more.  A wait inside the attention kernel that runs out (none does in a working
- * machine) raises it to 1 at least, and the outputs that it kept from being formed are NaN; in the bounds-checked build a
- * flag of -1 - t before the call makes them run out at a row's t-th key tile.  Calls allocate nothing and may be captured into graphs; calls that
- * share scratch must be ordered (same stream, or events). */
+ * nullable, only ever raised) gets 100 or more.  A wait inside the attention kernel that runs out (none does in a
+ * working machine) raises it to 1 at least, and the outputs that it kept from being formed are NaN; in the
+ * bounds-checked build a flag of -1 - t before the call makes them run out at a row's t-th key tile.  Calls allocate
+ * nothing and may be captured into graphs; calls that share scratch must be ordered (same stream, or events). */
 enum { BS_KV8_BLOCK = 32, BS_KV8_MAX_ROWS = 1024 };
 
 /* cos / sin table of the rotation, [max_pos][head_dim / 2][2], evaluated in double and rounded once, into HOST memory
@@ -349,9 +349,9 @@ int bs_rope_table(float* host_table, int max_pos, int head_dim, float theta);
  *   y = gain * x / sqrt(mean(x^2) + eps) over the head's dims, then the pairs (y_j, y_{j + head_dim/2}) turned by the
  *   angle of the token's position id (rope_table, device memory), all in fp32 and rounded once to bf16.
  * Query heads go to q_out (row stride q_ld elements, a multiple of 8; q_out = qkv with q_ld = (Hq + 2 Hkv) * head_dim
- * rotates in place; any other overlap with qkv is refused), k and v to cache row tok_kv[t] of the bf16 caches [kv_rows][Hkv][head_dim]; tok_kv[t] < 0: the
- * token belongs to no row and is skipped.  q_gain / k_gain: bf16 [head_dim], or both NULL (rotation only).
- * Tokens of one call must name different cache rows. */
+ * rotates in place; any other overlap with qkv is refused), k and v to cache row tok_kv[t] of the bf16 caches
+ * [kv_rows][Hkv][head_dim]; tok_kv[t] < 0: the token belongs to no row and is skipped.  q_gain / k_gain: bf16
+ * [head_dim], or both NULL (rotation only). Tokens of one call must name different cache rows. */
 int bs_op_qk_norm_rope_kv(const void* qkv, const void* q_gain, const void* k_gain, float eps, const int* tok_pos,
                           const int* tok_kv, void* q_out, int q_ld, void* kcache, void* vcache, long long kv_rows, int M,
                           int n_q_heads, int n_kv_heads, int head_dim, const float* rope_table, int max_pos,
@@ -377,10 +377,14 @@ int bs_op_kv8_read(const void* k8, const void* v8, const float* k_scale, const f
 
 /* Ragged bidirectional attention over the 8-bit cache: the queries of row i attend to cache positions [0, vis[i]) of
  * its slab (no causal or padding mask); out bf16 [M][Hq * head_dim]; vis[i] = 0 gives zeros.  Codes behind vis[i] may
- * be anything, NaN included.  q bf16, row stride q_ld elements (a multiple of 8): q_out of the operators above, or
- * the query part of a qkv buffer; out may be q where q_ld = Hq * head_dim, other overlaps are refused.  max_nq (0: unknown) and max_vis (0: unknown) are the largest query count and vis of
- * a row; they choose the kernel, not the result's meaning.  At most BS_KV8_MAX_ROWS rows and 32 query heads per kv
- * head.  scratch: bs_op_attention_kv8_scratch_bytes bytes of device memory, overwritten; may be NULL for sizes of which
+ * be anything, NaN included.  Sums, references and the softmax are fp32; scores meet queries held to 2^-17 of their
+ * row's largest element at worst, products with V meet weights rounded to fp16 (their sum does not).  q bf16, row
+ * stride q_ld elements (a multiple of 8): q_out of the operators above, or the query part of a qkv buffer; out may be q
+ * where q_ld = Hq * head_dim, other overlaps are refused.  max_nq (0: unknown) and max_vis (0: unknown) are the largest
+ * query count and vis of a row; they choose the kernel, not the result's meaning: without max_nq a row is taken to hold
+ * all M tokens, without max_vis its keys are not cut over several CTAs on the tensor-core kernel, and a call can take
+ * several times as long.  At most BS_KV8_MAX_ROWS rows and 32 query heads per kv head.  scratch:
+ * bs_op_attention_kv8_scratch_bytes bytes of device memory, overwritten; may be NULL for sizes of which
  * bs_op_attention_kv8_uses_scratch says 0 (whole items by workers of their own, keys that are not cut). */
 size_t bs_op_attention_kv8_scratch_bytes(int n_q_heads, int n_kv_heads, int head_dim);
 int bs_op_attention_kv8_uses_scratch(int n_rows, int M, int max_nq, int max_vis, int n_q_heads, int n_kv_heads, int head_dim);

@@ -651,7 +651,8 @@ def op_attention_kv8(q, k8, v8, k_scale, v_scale, cu_q, kv_base, vis, hq: int, m
                      error_flag: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Attention of packed queries (q [M, >= hq * dh]: q_out of the operators above, or a qkv buffer) over their rows'
     cache positions [0, vis[i]) of the 8-bit cache; rows with vis = 0 give zeros.  max_nq / max_vis (0: unknown): the
-    largest number of query tokens and of visible positions of a row.  Without `scratch` it comes from torch's allocator."""
+    largest number of query tokens and of visible positions of a row: any value gives the same result, but calls without
+    them can take several times as long.  Without `scratch` it comes from torch's allocator."""
     name, dev = "bs_op_attention_kv8", q.get_device()
     rows, hkv, dh = _kv8_shape(name, dev, k8, v8, k_scale, v_scale)
     M = q.shape[0]

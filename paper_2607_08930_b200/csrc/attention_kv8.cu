@@ -75,10 +75,11 @@ __device__ __forceinline__ uint2 lds64(unsigned at) {
 // no other warp touches (cp.async, no barrier): the next blocks are on their way while this one is computed.  Rows
 // behind the row's end arrive as zeros, whatever the cache holds there.
 //
-// What it reaches: 64 single-token rows of 1024 to 4096 keys (28 / 4 heads, 175 MB) 32 us of streaming, 5.5 TB/s of the
-// 6.5 measured for a copy, and 5 us of merge; two rows of 50,001 and 65,536 keys 23 us and 6.  64 rows x 32 tokens over
-// up to 1024 keys of 32 heads, 117 us, are bound by the instructions around the products instead: a block of 32 keys is
-// decoded (about 500 clk) for only 16 query rows' 64 products (520 clk), with two warps per scheduler to overlap.
+// What it reaches: 64 single-token rows of 1024 to 4096 keys (28 / 4 heads, 175 MB) 38.7 us, of which the merge takes 5 to 6;
+// two rows of 50,001 and 65,536 keys 29.0 us, 6 of them merge.  64 rows x 32 tokens over up to 1024 keys of 32 heads, 116 us,
+// wait on one another's instructions instead: with 16 query rows per item every block is fetched and decoded twice (530 MB
+// read where 306 would do), each time for only 64 products, and two warps per scheduler fill 39 % of the issue slots and
+// 32 % of the tensor pipe.
 //
 // Keys are the rows (M) of both products and the queries their columns (N), so that 8 query rows - a group of heads of
 // one token - fill an instruction.  Codes go to the tensor cores as fp16, which holds every e4m3 value (the warp-level
@@ -637,17 +638,17 @@ Route route_of(int n_rows, int M, int hint_nq, int max_vis, int hq, int hkv, int
   const int G = hq / hkv;
   const int max_nq = hint_nq > 0 ? std::min(hint_nq, M) : M;
   const long long widest = (long long)max_nq * G;
-  // From 48 (head_dim 64: 96) query rows per kv head on the 128-row tensor-core tiles pay (16 rows of 320 to 800 keys, 7
-  // heads a group: 35 query rows 18.1 us, 15.4 by the streaming kernel, 112 19.4 and 24.7; 32 heads: 40 query rows 62 and
-  // 58, 64 63 and 71; head_dim 64, 96 query rows 14.6 and 12.0).  The streaming kernel's tiles hold a token's group of up to
-  // 16 heads.
+  // Beyond 48 (head_dim 64: 96) query rows per kv head the 128-row tensor-core tiles pay (16 rows of 320 to 800 keys, 7
+  // heads a group: 35 query rows 16.5 us, 14.6 by the streaming kernel, 49 16.8 and 16.2, 112 17.6 and 23.3; 32 heads: 48 query
+  // rows 56 and 52, 64 57 and 66; head_dim 64: 96 query rows 14.5 and 12.8, 128 14.6 and 16.8).  The streaming kernel's tiles
+  // hold a token's group of up to 16 heads.
   // Rows of up to 96 keys do not fill a key tile and are streamed whatever the width (16 rows x 32 tokens, 7 heads a group: 43
-  // keys 8.6 us, tcgen05 11.5, 100 keys 10.6 and 11.8; 200 rows: 64 keys 82 and 105, 128 keys 108 and 106).
+  // keys 8.4 us, tcgen05 10.8, 100 keys 11.3 and 10.8; 200 rows: 64 keys 81 and 102, 96 keys 90 and 102, 128 keys 103 and 99).
   const bool brief = max_vis > 0 && max_vis <= 96;
   w.tensor = G > 16 || (!brief && widest > (dh == 128 ? 48 : 96));
   if (w.tensor) return w;
   // 8 or 16 query rows per item.  (32, which reads a block once for all of a 32-token step, leaves two warps per scheduler
-  // with 255 registers: 20 rows x 32 tokens, 32 heads 38.2 us against 32.0 with 16, 64 rows 121 and 122.)
+  // with 255 registers: a fifth slower on 20 rows x 32 tokens of 32 heads, no faster on 64 rows when it was tried.)
   w.nq = widest <= 8 ? 1 : 2;
   w.tq = 8 * w.nq / G;
   // Workers per (row, kv head), when every item has one: the tiles of the largest row.  A worker goes on to the next tile of
@@ -658,14 +659,15 @@ Route route_of(int n_rows, int M, int hint_nq, int max_vis, int hq, int hkv, int
   const long long cap = hint_nq > 0 ? 8 * filled / n_rows : ((long long)M / n_rows + w.tq - 1) / w.tq + 1;
   const int tiles = (int)std::min<long long>((max_nq + w.tq - 1) / w.tq, cap);
   // Single-warp workers where there are many items and two query tiles make each of them work for a warp.  64 rows x 32
-  // tokens, 32 heads, 4096 items: 200 to 512 keys 89 us (107 with four-warp workers), 96 to 1024 122 us (131); 1280 items:
-  // 96 to 500 keys 31.9 us (34.4), but 500 to 3000 114 us (106); 800 items 29.4 us (26.2).
+  // tokens, 32 heads, 4096 items: 200 to 512 keys 86 us (102 with four-warp workers), 96 to 1024 118 us (125); 1280 items: 96
+  // to 500 keys 31 us (33), but 500 to 3000 110 us (98); 768 items of 96 to 500 keys 28 us (23).
   const long long items = (long long)n_rows * hkv * tiles;
   w.many = w.nq > 1 && items >= (max_vis > 0 && max_vis <= 512 ? 6 : 16) * 148;
   // Short rows have a worker per item and nothing to merge; so do rows of some length where there are about as many items
-  // as workers fit the machine.  Four-warp workers: 2 rows of up to 1524 keys 10.1 us, 15.5 by the line; 2 rows of up to
-  // 15,778 60 and 13; 480 items of up to 3000 59 and 66; 256 items of up to 4000 41 and 38.  Single-warp workers: 4096
-  // items of up to 512 keys 89 us, 95 by the line; of up to 1024 130 and 122.
+  // as workers fit the machine.  Four-warp workers, 4 items a row: 2 rows of up to 500 keys 7.1 us, 11.7 by the line; 1100 8.9
+  // and 11.5; 2000 15.8 and 11.8; 15,778 68 and 14; 30 rows of up to 2000 18.0 and 18.0; 4000 29 and 24; 110 rows of up to
+  // 2000 33 and 34; 4000 58 and 54.  Single-warp workers: 4096 items of up to 512 keys 86 us, 92 by the line; of up to 1024
+  // 124 and 118.
   const int reach = w.many ? 512 : items >= 400 ? 4096 : 2048;
   w.direct = max_vis > 0 && max_vis <= reach ? tiles : 0;
   return w;
@@ -701,10 +703,10 @@ cudaError_t launch_attention_kv8(const AttnKv8Args& a, cudaStream_t s) {
   }
   const int nq = w.nq;
   const bool many = w.many;
-  // Stages and CTAs per SM.  One query tile, head_dim 128: three stages on two CTAs, 64 rows of 1024 to 4096 keys 37.0 us
-  // (two on three 38.7); head_dim 64: two on three, 60 rows of 1000 to 8000 keys 30.6 us (three on three 34.7).  Two query
-  // tiles, head_dim 128, four-warp: two on three, 200 rows x 2 tokens 26.4 us (three on two 33.3); single-warp: two on two,
-  // 64 rows x 32 tokens 122 us (two on three, which spills, 125).
+  // Stages and CTAs per SM.  One query tile, head_dim 128: three stages on two CTAs, 64 rows of 1000 to 4000 keys 36.8 us
+  // (two on three 38.0); head_dim 64: two on three, 60 rows of 1000 to 8000 keys, 8 heads, 49 us (three on three 59).  Two query
+  // tiles, head_dim 128, four-warp: two on three, 200 rows x 2 tokens 36 us (three on two 43); single-warp: two on two, 64
+  // rows x 32 tokens 119 us (two on three, which spills, 127).
   if (a.dh == 128) {
     if (nq == 1) return run_stream<128, 1, 3, 4, 2>(p, s);
     return many ? run_stream<128, 2, 2, 1, 2>(p, s) : run_stream<128, 2, 2, 4, 3>(p, s);

@@ -19,13 +19,13 @@
 // Weights are formed against a running reference that lags the maximum (kTcBias, kTcGrow): the output is rescaled only
 // when a row's maximum has outgrown it.
 //
-// What bounds it: 6 rows of 1200 to 2304 tokens (28 / 4 heads, head_dim 128) 361 us, 793 TFLOP/s counted as a 16-bit
+// What bounds it: 6 rows of 1200 to 2304 tokens (28 / 4 heads, head_dim 128) 367 us, 782 TFLOP/s counted as a 16-bit
 // attention, 47 % of the measured matrix rate.  Of a 128-key step of two query tiles, about 3900 clk, the tensor pipe
 // works for 2600 (1024 per tile at the full rate; the halves of the scores, 128 x 64 x 32 from shared memory, take 49 clk
 // instead of 32) and each scheduler's exponentials take 2048; the two softmax warps of a scheduler overlap them with their
 // other work only in part.  Scores of 128 keys at once (two passes over them, no spare half) took 480 us where halves with
 // the same way of issuing took 529, and 398 with products issued by an elected lane.  16 block steps of 32 tokens over 320
-// to 800 keys, one query tile per CTA, 17.9 us, are bound by a CTA's beginning - indices, barriers, queries to two terms:
+// to 800 keys, one query tile per CTA, 18.2 us, are bound by a CTA's beginning - indices, barriers, queries to two terms:
 // 4 us - and by its chain of three to seven tiles.
 // Every wait is bounded; when one runs out the flag is raised, all roles drain, the copies and products in flight are
 // waited for, and the CTA's outputs are NaN.
@@ -725,14 +725,14 @@ cudaError_t run_tc(const AttnKv8Args& a, float* part, size_t part_floats, int sm
   p.out = a.out; p.cu_q = a.cu_q; p.kv_base = a.kv_base; p.vis = a.vis;
   p.n_rows = a.n_rows; p.M = a.M; p.hq = a.hq; p.hkv = a.hkv; p.G = G; p.error_flag = a.error_flag;
   p.tq = 128 / G;
-  // Two query tiles per CTA share every key tile it loads and converts (6 rows of 1200 to 2304 tokens, 7 heads a group: 379
-  // us, 552 with one; 3 rows of 600 to 700 49 and 72); one per CTA fills the SMs when there are few.
+  // Two query tiles per CTA share every key tile it loads and converts (6 rows of 1200 to 2304 tokens, 7 heads a group: 388
+  // us, 546 with one; 3 rows of 600 to 700 48 and 67); one per CTA fills the SMs when there are few.
   const int nq = a.max_nq > 0 ? std::min(a.max_nq, a.M) : a.M;
   const long long singles = (long long)((nq + p.tq - 1) / p.tq) * a.n_rows * a.hkv;       // most query tiles there can be
   const bool two = singles > 2ll * sms && nq > p.tq;
   const int key_tiles = a.max_vis > 0 ? (a.max_vis + KT - 1) / KT : 1;
   // Few CTAs: the keys are cut, too, as long as a chunk keeps four key tiles (32 tokens, 4 kv heads: a row of 30,000 to 40,000
-  // keys 45 us, 369 uncut, 4 rows of 1000 to 2000 26 and 34; 9 rows of 500 to 800 25 us in two chunks, 20 uncut).
+  // keys 45 us, 376 uncut, 4 rows of 1000 to 2000 24 and 33; 9 rows of 500 to 800 29 us in two chunks, 18 uncut).
   int chunks = 1;
   if (!two)
     while (chunks < kMaxChunks && singles * (chunks + 1) <= sms && key_tiles / (chunks + 1) >= kAttnKv8CutTiles / 2 &&

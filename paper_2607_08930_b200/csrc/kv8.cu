@@ -8,10 +8,10 @@
 // norm's sum moves by shuffles inside those lanes, everything between the load and the one rounding at the end is fp32.
 //
 // Measured against a copy's 6.5 TB/s: norms and rotation into the bf16 cache, 16 rows of 320 to 1024 tokens (28 / 4 heads,
-// head_dim 128, 191 MB) 35.4 us, 5.4 TB/s (three heads in flight per lane and CTAs of four warps; four heads 39 us, eight
-// warps 40 us); the same pass into the 8-bit cache, 32 heads, 308 MB, 63 us, 4.9 TB/s (a tile waits for its scale, and the
-// instructions of norm, rotation, maximum and encoding take two thirds of the issue slots); reading back, 617 MB, 102 us, 6.0 TB/s (a whole tile in flight per warp; half of
-// one 108 us).  A single-token batch is latency: 64 tokens 2.7 us, three trips to memory.
+// head_dim 128, 191 MB) 35.6 us, 5.4 TB/s (three heads in flight per lane and CTAs of four warps; four heads 38 us, eight
+// warps 40 us); the same pass into the 8-bit cache, 32 heads, 308 MB, 64 us, 4.8 TB/s (a tile waits for its scale and for its
+// loads, and the instructions of norm, rotation, maximum and encoding take 62 % of the issue slots); reading back, 617 MB, 102
+// us, 6.0 TB/s (a whole tile in flight per warp).  A single-token batch is latency: 64 tokens 2.7 us, three trips to memory.
 #include <math.h>
 
 #include <algorithm>
@@ -299,7 +299,7 @@ __device__ __forceinline__ float largest16(const HeadLoad& v) {
   return fmaxf(__low2float(top), __high2float(top));
 }
 
-// Three CTAs of 256 threads per SM (80 registers; two of 110 measured 76 us where three took 66, 16 whole rows of 32 heads).
+// Three CTAs of 256 threads per SM (80 registers; with two 16 whole rows of 32 heads take 87 us where three take 76).
 // One CTA: the K and V tiles of kv heads [g0, g1) of one cache block.  A thread owns one row of the block and keeps its
 // angles in registers from head to head; the next head's rows are fetched while this one's are turned.  New rows are
 // formed in registers, kept rows decoded beside them, the largest magnitude of both gives the scale, and all are encoded
@@ -518,7 +518,7 @@ void head_shares(int M, int heads, int dh, int warps, int* shares, int* per_shar
   *shares = (passes + each - 1) / each;
 }
 // Of `n` items of each of `slots` work slots: how many one CTA takes, so that a slot's indices and angles are fetched for
-// as many as leave eight CTAs per SM (three: 16 whole rows written in 69.5 us where eight took 66, read in 107 and 102).
+// as many as leave eight CTAs per SM (with three 16 whole rows are written in 81 us where eight take 76, read in 106 and 103).
 int items_per_cta(long long slots, int n, int least) {
   int per = n;
   while (per > least && slots * ((n + per - 1) / per) < 148 * 8) per = (per + 1) / 2;
