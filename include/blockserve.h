@@ -393,6 +393,95 @@ int bs_op_attention_kv8(const void* q, int q_ld, const void* k8, const void* v8,
                         const int* vis, int n_rows, int M, int max_nq, int max_vis, int n_q_heads, int n_kv_heads,
                         int head_dim, void* scratch, size_t scratch_bytes, int* error_flag, void* stream);
 
+/* ---- projections in 8-bit integers --------------------------------------- *
+ * No counterpart in the paper (its runs hold weights and activations in 16 bits): for models whose weights have to
+ * stream, or multiply, in half the bytes.
+ *
+ * A row (a token's activations, an output channel's weights) is K signed 8-bit codes and one fp32 scale: value = code *
+ * scale.  Rows of codes start at multiples of 16 bytes (row strides in bytes, multiples of 16, of at least K); the bytes
+ * between K and the stride are neither read nor written.  Device pointers are 16-byte aligned (scales and indices:
+ * 4-byte).  Outputs must not overlap inputs, from an array's first element to its last (BS_E_ARG).  Calls allocate
+ * nothing, keep nothing, use no scratch and may be captured into graphs. */
+enum { BS_BF16 = 0, BS_F32 = 1 };            /* element types of x and of logits */
+enum { BS_I8_MAX_K = 131071 };               /* sums of K products of codes fit 32 bits */
+
+/* Codes and scales of rows x [x_rows][ldx] (type BS_BF16 or BS_F32, stride in elements; any alignment of the rows):
+ *   y = x, or with `gain` (bf16 [K]) gain * x / sqrt(mean(x^2) + eps) in fp32;
+ *   scale = max(fp32(max |y| / 127), 2^-126);  code = y / scale to the nearest integer, halves to the even one, decided on
+ *   the exact quotient.
+ * Row m is row idx[m] of x (idx NULL: row m, x_rows >= M).  An idx[m] outside [0, x_rows) raises error_flag (device int,
+ * nullable, only ever raised) to 100 or more and leaves the row's outputs as they were.  A row with an infinite or NaN
+ * element gets the scale NaN and zero codes. */
+int bs_op_quant_i8(const void* x, int type, long long ldx, const int* idx, int x_rows, const void* gain, float eps,
+                   void* codes, long long ldc, float* scale, int M, int K, int* error_flag, void* stream);
+
+/* z[m, n] = (sum over k < K of A[m, k] * W[n, k]) * w_scale[n] * a_scale[m]; the sum is exact (int32), then fp32.
+ * mode 0: C bf16 = z;  1: C fp32 += z;  2: C fp32 = z;  3: C bf16 = silu(z) * z2, z2 from W2 and w2_scale (ldw too).
+ * A int8 [M][lda], W int8 [N][ldw], C [M][ldc] (stride in elements, at least N).  Codes may take all values from -128 to
+ * 127.  1 <= K <= BS_I8_MAX_K.  The results do not depend on how the call is cut over the device.  A wait inside the
+ * kernel that runs out (none does in a working machine) raises error_flag to 1 at least, and the outputs that it kept
+ * from being formed are NaN; in the bounds-checked build a flag of -1 - b before the call makes them run out at the b-th
+ * 128 codes of a tile's K range. */
+int bs_op_gemm_i8(const void* A, long long lda, const float* a_scale, const void* W, long long ldw, const float* w_scale,
+                  const void* W2, const float* w2_scale, void* C, long long ldc, int M, int N, int K, int mode,
+                  int* error_flag, void* stream);
+
+/* ---- constrained decoding: rules on logits ------------------------------- *
+ * The paper commits by confidence alone; these rules come between the LM head and the confidence pass.  For a logit z of
+ * token v in a row of request i, each step rounded to fp32:
+ *   1. v occurs in the request's context:            z = z > 0 ? z / repetition[i] : z * repetition[i]
+ *   2. v occurs c > 0 times in its generated part:   z = z - (frequency[i] * c + presence[i])
+ *   3. biases of the request for v:                  z = z + bias, in their order
+ *   4. v not allowed by the row's grammar mask, or v = mask_id:  z = -infinity, whatever it was (NaN included)
+ * The struct is host memory, consumed before a call returns; its members are device memory, read by the call's kernel, so
+ * that a program may fill them once and update their contents between calls.  NULL members are rules that do not apply.
+ * Indices are checked on the device: what is out of range raises error_flag to 100 or more and is skipped, as said
+ * below.  Calls allocate nothing, keep nothing, use no scratch and may be captured into graphs. */
+enum { BS_RULES_MAX_VOCAB = 393216 };
+typedef struct {
+  int vocab, n_reqs;
+  int mask_id;               /* never chosen, never counted as context; -1: there is none */
+  const int* row_req;        /* [n_rows] request of a row, -1: only the grammar applies; NULL: row r is request r.  A row
+                                whose request or mask is out of range is skipped.  Rows of one request next to each other
+                                share the work of counting its context. */
+  /* request i's context: tokens ctx[ctx_begin[i]] .. ctx[ctx_end[i] - 1], from ctx_gen[i] on the generated part.  Ids
+     outside [0, vocab) are skipped (and raise the flag), the mask id is skipped; a request whose bounds are not
+     0 <= begin <= gen <= end <= ctx_total has no context (and raises the flag). */
+  const int* ctx;
+  long long ctx_total;       /* < 2^31 */
+  const int* ctx_begin;      /* [n_reqs], like the next two; needed with ctx */
+  const int* ctx_gen;
+  const int* ctx_end;
+  const float* repetition;   /* [n_reqs], nullable: 1 */
+  const float* presence;     /* [n_reqs], nullable: 0 */
+  const float* frequency;    /* [n_reqs], nullable: 0 */
+  /* request i's biases: tokens bias_tok[bias_at[i]] .. bias_tok[bias_at[i + 1] - 1] in ascending order (equal ones add up,
+     in order).  A token that is out of range or below the one before it raises the flag, and which of the request's
+     biases then count is not defined. */
+  const int* bias_at;        /* [n_reqs + 1], values in [0, bias_total] */
+  const int* bias_tok;
+  const float* bias_val;
+  long long bias_total;      /* < 2^31 */
+  const unsigned* allowed;   /* [n_masks][allowed_ld]: bit v mod 32 of word v / 32 set: token v is allowed */
+  long long allowed_ld;      /* words, at least ceil(vocab / 32) */
+  int n_masks;
+  const int* row_mask;       /* [n_rows] mask of a row, -1: every token is allowed; NULL: row r has mask r */
+} bs_logit_rules;
+
+/* out[r, v] = the logit after the rules, rounded to the logits' type once.  logits [n_rows][ld] of type BS_F32 or BS_BF16
+ * (stride in elements, at least vocab), 16-byte aligned; out the same with out_ld.  out = logits with out_ld = ld works in
+ * place (only the entries that change are written); any other overlap is refused.  Entries at and behind vocab are left
+ * as they were, and so are skipped rows. */
+int bs_op_logit_rules(const void* logits, int type, long long ld, void* out, long long out_ld, int n_rows,
+                      const bs_logit_rules* rules, int* error_flag, void* stream);
+
+/* bs_op_confidence under the rules, in one pass that stores no logits: tok = argmax after the rules (lowest id on ties),
+ * conf = exp(max - logsumexp).  A row of which nothing is left (every logit -infinity), and a skipped row, gives tok = -1
+ * and conf = 0.  Rows with a NaN among the logits that are left give conf = NaN, and tok the best of the others (or -1);
+ * k logits of +infinity share the row: conf = 1 / k. */
+int bs_op_rules_confidence(const void* logits, int type, long long ld, int n_rows, const bs_logit_rules* rules, int* tok,
+                           float* conf, int* error_flag, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -63,13 +63,22 @@ class BsStats(C.Structure):
                 ("kernel_launches", C.c_longlong), ("row_steps", C.c_longlong), ("active_row_steps", C.c_longlong)]
 
 
+class BsLogitRules(C.Structure):
+    _fields_ = [("vocab", C.c_int), ("n_reqs", C.c_int), ("mask_id", C.c_int), ("row_req", C.c_void_p), ("ctx", C.c_void_p),
+                ("ctx_total", C.c_longlong), ("ctx_begin", C.c_void_p), ("ctx_gen", C.c_void_p), ("ctx_end", C.c_void_p),
+                ("repetition", C.c_void_p), ("presence", C.c_void_p), ("frequency", C.c_void_p), ("bias_at", C.c_void_p),
+                ("bias_tok", C.c_void_p), ("bias_val", C.c_void_p), ("bias_total", C.c_longlong), ("allowed", C.c_void_p),
+                ("allowed_ld", C.c_longlong), ("n_masks", C.c_int), ("row_mask", C.c_void_p)]
+
+
 EXPORTS = ["bs_query_sizes", "bs_init_model", "bs_admit", "bs_evict_refill", "bs_denoise_step", "bs_block_done",
            "bs_read_tokens", "bs_get_stats", "bs_set_profiling", "bs_get_profile", "bs_destroy", "bs_last_error", "bs_build_flags", "bs_debug_read", "bs_debug_inject_timeout",
            "bs_debug_force_commit", "bs_debug_snapshot", "bs_debug_restore", "bs_op_gemm", "bs_op_gemm_cluster_splits",
            "bs_op_rmsnorm", "bs_op_rope_kv", "bs_op_rope_kv_static", "bs_op_attention_q_tile", "bs_op_attention", "bs_op_confidence",
            "bs_op_lm_head_confidence", "bs_op_lm_head_confidence_scratch_bytes", "bs_rope_table", "bs_op_qk_norm_rope_kv",
            "bs_op_qk_norm_rope_kv8", "bs_op_kv8_read", "bs_op_attention_kv8", "bs_op_attention_kv8_scratch_bytes",
-           "bs_op_attention_kv8_uses_scratch"]
+           "bs_op_attention_kv8_uses_scratch", "bs_op_quant_i8", "bs_op_gemm_i8", "bs_op_logit_rules",
+           "bs_op_rules_confidence"]
 
 _lib = None
 
@@ -125,6 +134,10 @@ def lib() -> C.CDLL:
         L.bs_op_attention_kv8_uses_scratch.argtypes = [i] * 7
         L.bs_op_attention_kv8.argtypes = [vp, i, vp, vp, vp, vp, ll, vp, vp, vp, vp, i, i, i, i, i, i, i, vp, C.c_size_t,
                                           vp, vp]
+        L.bs_op_quant_i8.argtypes = [vp, i, ll, vp, i, vp, f, vp, ll, vp, i, i, vp, vp]
+        L.bs_op_gemm_i8.argtypes = [vp, ll, vp, vp, ll, vp, vp, vp, vp, ll, i, i, i, i, vp, vp]
+        L.bs_op_logit_rules.argtypes = [vp, i, ll, vp, ll, i, vp, vp, vp]
+        L.bs_op_rules_confidence.argtypes = [vp, i, ll, i, vp, vp, vp, vp, vp]
         _lib = L
     return _lib
 
@@ -675,3 +688,230 @@ def op_attention_kv8(q, k8, v8, k_scale, v_scale, cu_q, kv_base, vis, hq: int, m
           n, M, max_nq, max_vis, hq, hkv, dh, _ptr(scratch),
           0 if scratch is None else scratch.numel(), _ptr(error_flag))
     return out
+
+
+# ---- projections in 8-bit integers --------------------------------------------------------------------------------
+
+I8_MAX_K, RULES_MAX_VOCAB = 131071, 393216      # BS_I8_MAX_K, BS_RULES_MAX_VOCAB
+_I8 = torch.int8
+_TYPES = {torch.bfloat16: 0, torch.float32: 1}  # BS_BF16, BS_F32
+
+
+def _stride_of(t: torch.Tensor) -> int:
+    """Row stride of a matrix of adjacent elements (a single row has the width's)."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _rows_of_codes(name: str, dev: int, arg: str, t: torch.Tensor) -> int:
+    """Row stride of an int8 matrix whose rows start at multiples of 16 bytes."""
+    shape = t.shape
+    if len(shape) != 2 or t.dtype is not _I8 or t.get_device() != dev or (shape[1] > 1 and t.stride(1) != 1):
+        _refuse(name, f"{arg} must be an int8 matrix of adjacent elements on the operator's device, got {tuple(shape)} "
+                      f"{t.dtype} on {t.device}")
+    if shape[0] <= 1:
+        return (shape[1] + 15) // 16 * 16
+    return t.stride(0)
+
+
+def i8_codes(rows: int, K: int, device="cuda") -> torch.Tensor:
+    """Uninitialised int8 codes [rows, K] whose rows start at multiples of 16 bytes."""
+    ld = (K + 15) // 16 * 16
+    t = torch.empty(rows, ld, dtype=_I8, device=device)
+    return t if ld == K else t[:, :K]
+
+
+def op_quant_i8(x: torch.Tensor, gain: Optional[torch.Tensor] = None, eps: float = 1e-6, idx: Optional[torch.Tensor] = None,
+                codes: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
+                error_flag: Optional[torch.Tensor] = None):
+    """(codes int8 [M, K], scale fp32 [M]) of the rows of x (bf16 or fp32 [rows, K], any row stride), or of its rows
+    idx[m]; with `gain` (bf16 [K]) of their RMS norms.  Weights are laid out by the same call: a row is an output channel.
+    error_flag (int32 [1]) gets >= 100 where an idx was out of range (the row is left as it was)."""
+    name, dev = "bs_op_quant_i8", x.get_device()
+    type_ = _TYPES.get(x.dtype)
+    if type_ is None or x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
+        _refuse(name, f"x must be a bfloat16 or float32 matrix of adjacent elements, got {tuple(x.shape)} {x.dtype}")
+    rows, K = x.shape
+    M = rows
+    if idx is not None:
+        _need(name, dev, _I32, 0, "idx", idx)
+        M = idx.numel()
+    if gain is not None:
+        _need(name, dev, _BF16, K, "gain", gain)
+    if codes is None:
+        codes = i8_codes(M, K, x.device)
+    elif codes.shape != (M, K):
+        _refuse(name, f"codes must be [{M}, {K}], got {tuple(codes.shape)}")
+    ldc = _rows_of_codes(name, dev, "codes", codes)
+    if scale is None:
+        scale = torch.empty(M, dtype=_F32, device=x.device)
+    else:
+        _need(name, dev, _F32, M, "scale", scale)
+    if error_flag is not None:
+        _need(name, dev, _I32, 1, "error_flag", error_flag)
+    _call(name, dev, (_lib or lib()).bs_op_quant_i8, x.data_ptr(), type_, _stride_of(x), _ptr(idx), rows, _ptr(gain), eps,
+          codes.data_ptr(), ldc, scale.data_ptr(), M, K, _ptr(error_flag))
+    return codes, scale
+
+
+def op_gemm_i8(a: torch.Tensor, a_scale: torch.Tensor, W: torch.Tensor, w_scale: torch.Tensor, mode: int = 0,
+               W2: Optional[torch.Tensor] = None, w2_scale: Optional[torch.Tensor] = None,
+               C_out: Optional[torch.Tensor] = None, error_flag: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """z = (a @ W.T) * w_scale * a_scale[:, None] of int8 codes a [M, K], W [N, K] (rows at multiples of 16 bytes, as
+    op_quant_i8 gives them), with the modes of op_gemm: 0 bf16, 1 added to fp32 C_out, 2 fp32, 3 bf16 silu(z) * z2 with
+    W2 [N, K] and w2_scale."""
+    name, dev = "bs_op_gemm_i8", a.get_device()
+    lda, ldw = _rows_of_codes(name, dev, "a", a), _rows_of_codes(name, dev, "W", W)
+    (M, K), N = a.shape, W.shape[0]
+    if W.shape[1] != K or (mode == 3) != (W2 is not None):
+        _refuse(name, f"W must be [N, {K}], and W2 is given in mode 3 only")
+    if a_scale.dtype is not _F32 or a_scale.get_device() != dev or not a_scale.is_contiguous() or a_scale.numel() < M:
+        _need(name, dev, _F32, M, "a_scale", a_scale)
+    if w_scale.dtype is not _F32 or w_scale.get_device() != dev or not w_scale.is_contiguous() or w_scale.numel() < N:
+        _need(name, dev, _F32, N, "w_scale", w_scale)
+    if W2 is not None:
+        if w2_scale is None or W2.shape != W.shape or _rows_of_codes(name, dev, "W2", W2) != ldw:
+            _refuse(name, "W2 must have W's shape and strides, with w2_scale")
+        _need(name, dev, _F32, N, "w2_scale", w2_scale)
+    dtype = _F32 if mode in (1, 2) else _BF16
+    if C_out is None:
+        if mode == 1:
+            _refuse(name, "mode 1 adds to C_out")
+        C_out = torch.empty(M, N, dtype=dtype, device=a.device)
+    elif C_out.shape != (M, N) or C_out.dtype is not dtype or C_out.get_device() != dev or (N > 1 and C_out.stride(1) != 1):
+        _refuse(name, f"C_out must be a {dtype} matrix [{M}, {N}] of adjacent elements on the operator's device, got "
+                      f"{tuple(C_out.shape)} {C_out.dtype} on {C_out.device}")
+    if error_flag is not None:
+        _need(name, dev, _I32, 1, "error_flag", error_flag)
+    _call(name, dev, (_lib or lib()).bs_op_gemm_i8, a.data_ptr(), lda, a_scale.data_ptr(), W.data_ptr(), ldw, w_scale.data_ptr(),
+          _ptr(W2), _ptr(w2_scale), C_out.data_ptr(), _stride_of(C_out), M, N, K, mode, _ptr(error_flag))
+    return C_out
+
+
+# ---- constrained decoding: rules on logits ------------------------------------------------------------------------
+
+class LogitRules:
+    """The rules of a batch, made once by logit_rules(); the tensors that it names are read at every call, so their
+    contents may be updated in between."""
+
+    __slots__ = ("struct", "ref", "tensors", "dev", "rows", "vocab")
+
+    def __init__(self, struct: BsLogitRules, tensors, dev: int, rows: Optional[int]):
+        self.struct, self.ref, self.tensors, self.dev, self.rows = struct, C.addressof(struct), tensors, dev, rows
+        self.vocab = struct.vocab
+
+
+def logit_rules(vocab: int, row_req: Optional[torch.Tensor], n_reqs: int, mask_id: int = -1, ctx: Optional[torch.Tensor] = None,
+                ctx_begin: Optional[torch.Tensor] = None, ctx_gen: Optional[torch.Tensor] = None,
+                ctx_end: Optional[torch.Tensor] = None, repetition: Optional[torch.Tensor] = None,
+                presence: Optional[torch.Tensor] = None, frequency: Optional[torch.Tensor] = None,
+                bias_at: Optional[torch.Tensor] = None, bias_tok: Optional[torch.Tensor] = None,
+                bias_val: Optional[torch.Tensor] = None, allowed: Optional[torch.Tensor] = None,
+                row_mask: Optional[torch.Tensor] = None) -> LogitRules:
+    """Rules of constrained decoding for rows of logits [rows, vocab].
+
+    row_req int32 [rows]: request of a row (-1: only the grammar applies; None: row r is request r).  Request i's context
+    is ctx[ctx_begin[i] : ctx_end[i]] (int32), generated from ctx_gen[i] on; repetition, presence and frequency penalties
+    fp32 [n_reqs]; its biases bias_val at the ascending tokens bias_tok, entries bias_at[i] .. bias_at[i + 1].  allowed
+    int32 [masks, ceil(vocab / 32)]: bit v % 32 of word v // 32 set where token v is allowed; row_mask int32 [rows]: mask of
+    a row (-1: none; None: row r has mask r).  mask_id is never chosen and not counted as context."""
+    name = "logit_rules"
+    given = [t for t in (row_req, ctx, ctx_begin, ctx_gen, ctx_end, repetition, presence, frequency, bias_at, bias_tok, bias_val,
+                         allowed, row_mask) if t is not None]
+    dev = given[0].get_device() if given else -1
+    if dev < 0 and given:
+        _refuse(name, "the rules' tensors are CUDA tensors")
+    if not 1 <= vocab <= RULES_MAX_VOCAB or n_reqs < 0 or not -1 <= mask_id < vocab:
+        _refuse(name, f"vocab must lie in [1, {RULES_MAX_VOCAB}], mask_id in [-1, vocab), got {vocab} and {mask_id}")
+    rows = None                                   # most rows that the rules know, where they are listed by row
+    for arg, t in (("row_req", row_req), ("row_mask", row_mask)):
+        if t is not None:
+            _need(name, dev, _I32, 0, arg, t)
+            rows = t.numel() if rows is None else min(rows, t.numel())
+    if row_req is None:
+        rows = n_reqs if rows is None else min(rows, n_reqs)
+    if ctx is not None:
+        _need(name, dev, _I32, 0, "ctx", ctx)
+        if ctx_begin is None or ctx_gen is None or ctx_end is None:
+            _refuse(name, "ctx needs ctx_begin, ctx_gen and ctx_end")
+        _need(name, dev, _I32, n_reqs, "ctx_begin ctx_gen ctx_end", ctx_begin, ctx_gen, ctx_end)
+        _need(name, dev, _F32, n_reqs, "repetition presence frequency", *[t for t in (repetition, presence, frequency) if t is not None])
+    elif not (ctx_begin is ctx_gen is ctx_end is repetition is presence is frequency is None):
+        _refuse(name, "penalties need a context (ctx)")
+    if bias_at is not None:
+        if bias_tok is None or bias_val is None or bias_tok.numel() != bias_val.numel():
+            _refuse(name, "bias_at needs bias_tok and bias_val of one length")
+        _need(name, dev, _I32, n_reqs + 1, "bias_at", bias_at)
+        _need(name, dev, _I32, 0, "bias_tok", bias_tok)
+        _need(name, dev, _F32, 0, "bias_val", bias_val)
+    elif bias_tok is not None or bias_val is not None:
+        _refuse(name, "biases need bias_at")
+    if allowed is not None:
+        words = (vocab + 31) // 32
+        if allowed.dim() != 2 or allowed.dtype is not _I32 or allowed.get_device() != dev or allowed.shape[1] < words or \
+                allowed.stride(1) != 1:
+            _refuse(name, f"allowed must be an int32 matrix of at least {words} adjacent words a mask on the operator's device")
+        if row_mask is None:
+            rows = allowed.shape[0] if rows is None else min(rows, allowed.shape[0])
+    elif row_mask is not None:
+        _refuse(name, "row_mask needs allowed")
+    p = _ptr
+    s = BsLogitRules(vocab, n_reqs, mask_id, p(row_req), p(ctx), 0 if ctx is None else ctx.numel(), p(ctx_begin), p(ctx_gen),
+                     p(ctx_end), p(repetition), p(presence), p(frequency), p(bias_at), p(bias_tok), p(bias_val),
+                     0 if bias_tok is None else bias_tok.numel(), p(allowed),
+                     0 if allowed is None else (allowed.stride(0) if allowed.shape[0] > 1 else allowed.shape[1]),
+                     0 if allowed is None else allowed.shape[0], p(row_mask))
+    return LogitRules(s, given, dev, rows)
+
+
+def _ruled_logits(name: str, logits: torch.Tensor, rules: LogitRules):
+    """(device, type, row stride, rows) of logits that the rules fit."""
+    dev, shape = logits.get_device(), logits.shape
+    type_ = _TYPES.get(logits.dtype)
+    if type_ is None or len(shape) != 2 or shape[1] != rules.vocab or (shape[1] > 1 and logits.stride(1) != 1):
+        _refuse(name, f"logits must be a bfloat16 or float32 matrix [rows, {rules.vocab}] of adjacent elements, got "
+                      f"{tuple(shape)} {logits.dtype}")
+    if rules.dev not in (-1, dev):
+        _refuse(name, "the rules' tensors are on another device than the logits")
+    if rules.rows is not None and shape[0] > rules.rows:
+        _refuse(name, f"{shape[0]} rows of logits, but rules for {rules.rows}")
+    return dev, type_, _stride_of(logits), shape[0]
+
+
+def op_logit_rules(logits: torch.Tensor, rules: LogitRules, out: Optional[torch.Tensor] = None,
+                   error_flag: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The logits (fp32 or bf16 [rows, vocab]) after the rules: repetition, frequency and presence penalties, biases, then
+    -inf where the grammar or mask_id forbids.  In place, or to `out` (the same type).  error_flag (int32 [1]) gets >= 100
+    where an index was out of range."""
+    name = "bs_op_logit_rules"
+    dev, type_, ld, rows = _ruled_logits(name, logits, rules)
+    if out is None:
+        out = logits
+    elif out.shape != logits.shape or out.dtype is not logits.dtype or out.get_device() != dev or \
+            (out.shape[1] > 1 and out.stride(1) != 1):
+        _refuse(name, f"out must be a {logits.dtype} matrix {tuple(logits.shape)} of adjacent elements on the operator's device")
+    if error_flag is not None:
+        _need(name, dev, _I32, 1, "error_flag", error_flag)
+    _call(name, dev, (_lib or lib()).bs_op_logit_rules, logits.data_ptr(), type_, ld, out.data_ptr(), _stride_of(out), rows,
+          rules.ref, _ptr(error_flag))
+    return out
+
+
+def op_rules_confidence(logits: torch.Tensor, rules: LogitRules, tok: Optional[torch.Tensor] = None,
+                        conf: Optional[torch.Tensor] = None, error_flag: Optional[torch.Tensor] = None):
+    """op_confidence under the rules, without storing logits: (tok int32 [rows], conf fp32 [rows]); a row of which nothing
+    is left gives -1 and 0."""
+    name = "bs_op_rules_confidence"
+    dev, type_, ld, rows = _ruled_logits(name, logits, rules)
+    if tok is None:
+        tok = torch.empty(rows, dtype=_I32, device=logits.device)
+    else:
+        _need(name, dev, _I32, rows, "tok", tok)
+    if conf is None:
+        conf = torch.empty(rows, dtype=_F32, device=logits.device)
+    else:
+        _need(name, dev, _F32, rows, "conf", conf)
+    if error_flag is not None:
+        _need(name, dev, _I32, 1, "error_flag", error_flag)
+    _call(name, dev, (_lib or lib()).bs_op_rules_confidence, logits.data_ptr(), type_, ld, rows, rules.ref, tok.data_ptr(),
+          conf.data_ptr(), _ptr(error_flag))
+    return tok, conf

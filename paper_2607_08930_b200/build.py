@@ -10,7 +10,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libblockserve.so")
 SOURCES = ["engine.cu", "sched_index.cu", "elementwise.cu", "gemm_tcgen05.cu", "attention.cu", "attention_tc.cu",
            "rope_static.cu", "kv8.cu", "attention_kv8.cu",
-           "attention_kv8_tc.cu"]
+           "attention_kv8_tc.cu", "quant_i8.cu", "gemm_i8.cu", "logit_rules.cu"]
 NVCC_FLAGS = ["-std=c++17", "-O3", "-lineinfo", "-gencode", "arch=compute_100a,code=sm_100a",
               "-Xcompiler", "-fPIC", "-Xptxas", "-v"]
 

@@ -67,7 +67,9 @@ enum BoundsSite {
   SITE_EMBED = 1, SITE_FILL_TOKENS = 2, SITE_ROPE_KV = 3, SITE_FINISH_QKV = 4, SITE_COMMIT = 5, SITE_INDEX = 6,
   SITE_SCHED = 7, SITE_NORM_GATHER = 8,
   // checked in every build: the 8-bit cache operators and the per-head norm take their indices from the caller
-  SITE_QK_NORM = 9, SITE_KV8 = 10, SITE_ATTN_KV8 = 11
+  SITE_QK_NORM = 9, SITE_KV8 = 10, SITE_ATTN_KV8 = 11,
+  // likewise: 8-bit row codes, logit rules
+  SITE_QUANT_I8 = 12, SITE_RULES = 13
 };
 
 constexpr int kHdrInts = 32;

@@ -9,6 +9,7 @@
 #include <vector>
 
 #include "../../include/blockserve.h"
+#include "decode_ops.cuh"
 #include "kv8.cuh"
 
 using namespace bs;
@@ -1076,6 +1077,122 @@ int bs_op_attention_kv8(const void* q, int q_ld, const void* k8, const void* v8,
   a.hq = n_q_heads; a.hkv = n_kv_heads; a.dh = head_dim;
   a.scratch = scratch; a.scratch_bytes = scratch ? scratch_bytes : 0; a.error_flag = error_flag;
   return launch_attention_kv8(a, (cudaStream_t)stream) == cudaSuccess ? BS_OK : BS_E_CUDA;
+}
+
+// ---- projections in 8-bit integers, rules on logits ------------------------------------------------------------
+
+static_assert(BS_I8_MAX_K == kGemmI8MaxK && BS_RULES_MAX_VOCAB == kRulesMaxVocab, "the header's bounds and the kernels'");
+
+// An array in memory: rows of `width` bytes, `ld` bytes apart.
+struct Extent {
+  uintptr_t lo, hi;
+};
+static Extent extent(const void* p, long long rows, long long ld, long long width) {
+  const uintptr_t at = (uintptr_t)p;
+  return p && rows > 0 ? Extent{at, at + (uintptr_t)((rows - 1) * ld + width)} : Extent{at, at};
+}
+static bool meets(const Extent& out, std::initializer_list<Extent> in) {
+  for (const Extent& e : in)
+    if (out.lo < e.hi && e.lo < out.hi) return true;
+  return false;
+}
+static bool aligned4(std::initializer_list<const void*> ps) {           // where given
+  for (const void* p : ps)
+    if ((uintptr_t)p & 3) return false;
+  return true;
+}
+constexpr long long kMaxStride = 1ll << 36;                              // of a row, in bytes: extents stay below 2^63
+static int status_of(cudaError_t r) {
+  return r == cudaSuccess ? BS_OK : (r == cudaErrorNotSupported ? BS_E_ARG : BS_E_CUDA);
+}
+
+int bs_op_quant_i8(const void* x, int type, long long ldx, const int* idx, int x_rows, const void* gain, float eps,
+                   void* codes, long long ldc, float* scale, int M, int K, int* error_flag, void* stream) {
+  if (M == 0) return BS_OK;
+  const int size = type == BS_F32 ? 4 : 2;
+  if (M < 0 || K < 1 || K > BS_I8_MAX_K || (type != BS_BF16 && type != BS_F32) || !x || !scale || !aligned16({codes}) ||
+      ((uintptr_t)x & (size - 1)) || !aligned4({idx, scale, error_flag}) || ((uintptr_t)gain & 15) || !(eps >= 0.f) ||
+      x_rows < (idx ? 1 : M) || ldx < K || ldx > kMaxStride / 4 || ldc < K || ldc % 16 || ldc > kMaxStride)
+    return BS_E_ARG;
+  const Extent from = extent(x, x_rows, ldx * size, (long long)K * size), list = extent(idx, M, 4, 4), g = extent(gain, 1, 0, 2ll * K);
+  const Extent out = extent(codes, M, ldc, K), sc = extent(scale, M, 4, 4);
+  if (meets(out, {from, list, g, sc}) || meets(sc, {from, list, g})) return BS_E_ARG;
+  return status_of(launch_quant_i8(QuantI8Args{x, ldx, type == BS_F32, idx, x_rows, (const bf16*)gain, eps, (int8_t*)codes, ldc,
+                                               scale, M, K, error_flag}, (cudaStream_t)stream));
+}
+
+int bs_op_gemm_i8(const void* A, long long lda, const float* a_scale, const void* W, long long ldw, const float* w_scale,
+                  const void* W2, const float* w2_scale, void* C, long long ldc, int M, int N, int K, int mode,
+                  int* error_flag, void* stream) {
+  if (M == 0 || N == 0) return BS_OK;
+  if (M < 0 || N < 0 || K < 1 || K > BS_I8_MAX_K || mode < 0 || mode > 3 || !aligned16({A, W, C}) || !a_scale || !w_scale ||
+      !aligned4({a_scale, w_scale, w2_scale, error_flag}) || lda < K || lda % 16 || lda > kMaxStride || ldw < K || ldw % 16 ||
+      ldw > kMaxStride || ldc < N || ldc > kMaxStride / 4 || (mode == 3) != (W2 != nullptr) || (W2 && (!w2_scale || ((uintptr_t)W2 & 15))))
+    return BS_E_ARG;
+  const int size = mode == 1 || mode == 2 ? 4 : 2;
+  if (meets(extent(C, M, ldc * size, (long long)N * size),
+            {extent(A, M, lda, K), extent(W, N, ldw, K), extent(W2, N, ldw, K), extent(a_scale, M, 4, 4), extent(w_scale, N, 4, 4),
+             extent(W2 ? w2_scale : nullptr, N, 4, 4)}))
+    return BS_E_ARG;
+  return status_of(launch_gemm_i8(GemmI8Args{(const int8_t*)A, lda, a_scale, (const int8_t*)W, (const int8_t*)W2, ldw, w_scale,
+                                             w2_scale, C, ldc, M, N, K, mode, error_flag}, (cudaStream_t)stream));
+}
+
+// Checks the rules and lays them out for the kernels; `out` and `out2` must not meet what they read.
+static bool rules_args(const void* logits, int type, long long ld, int n_rows, const bs_logit_rules* r, int* error_flag,
+                       const Extent& out, const Extent& out2, bool inplace, RulesArgs* a) {
+  if (n_rows < 0 || !r || (type != BS_BF16 && type != BS_F32) || !aligned16({logits}) || !aligned4({error_flag})) return false;
+  if (r->vocab < 1 || r->vocab > BS_RULES_MAX_VOCAB || r->n_reqs < 0 || r->mask_id < -1 || r->mask_id >= r->vocab ||
+      ld < r->vocab || ld > kMaxStride / 4 || (!r->row_req && r->n_reqs < n_rows))
+    return false;
+  if (!aligned4({r->row_req, r->ctx, r->ctx_begin, r->ctx_gen, r->ctx_end, r->repetition, r->presence, r->frequency, r->bias_at,
+                 r->bias_tok, r->bias_val, r->allowed, r->row_mask}))
+    return false;
+  if (r->ctx && (r->ctx_total < 0 || r->ctx_total > 0x7fffffffll || !r->ctx_begin || !r->ctx_gen || !r->ctx_end)) return false;
+  if (r->bias_at && (r->bias_total < 0 || r->bias_total > 0x7fffffffll || (r->bias_total && (!r->bias_tok || !r->bias_val))))
+    return false;
+  if (r->allowed && (r->n_masks < 0 || r->allowed_ld < (r->vocab + 31) / 32 || r->allowed_ld > kMaxStride / 4 ||
+                     (!r->row_mask && r->n_masks < n_rows)))
+    return false;
+  const int size = type == BS_F32 ? 4 : 2;
+  const long long n = r->n_reqs;
+  const std::initializer_list<Extent> in = {
+      extent(r->row_req, n_rows, 4, 4), extent(r->ctx, 1, 0, 4 * r->ctx_total), extent(r->ctx_begin, n, 4, 4),
+      extent(r->ctx_gen, n, 4, 4), extent(r->ctx_end, n, 4, 4), extent(r->repetition, n, 4, 4), extent(r->presence, n, 4, 4),
+      extent(r->frequency, n, 4, 4), extent(r->bias_at, n + 1, 4, 4), extent(r->bias_at ? r->bias_tok : nullptr, 1, 0, 4 * r->bias_total),
+      extent(r->bias_at ? r->bias_val : nullptr, 1, 0, 4 * r->bias_total),
+      extent(r->allowed, r->n_masks, 4 * r->allowed_ld, 4ll * ((r->vocab + 31) / 32)),
+      extent(r->allowed ? r->row_mask : nullptr, n_rows, 4, 4)};
+  const Extent z = extent(logits, n_rows, ld * size, (long long)r->vocab * size);
+  if (meets(out, in) || meets(out2, in) || (!inplace && meets(out, {z})) || meets(out2, {z, out})) return false;
+  *a = RulesArgs{logits, ld, type == BS_BF16, n_rows, r->vocab, r->n_reqs, r->mask_id, r->row_req, r->ctx, r->ctx_total,
+                 r->ctx_begin, r->ctx_gen, r->ctx_end, r->repetition, r->presence, r->frequency, r->bias_at, r->bias_tok,
+                 r->bias_val, r->bias_total, r->allowed, r->allowed_ld, r->n_masks, r->row_mask, error_flag};
+  return true;
+}
+
+int bs_op_logit_rules(const void* logits, int type, long long ld, void* out, long long out_ld, int n_rows,
+                      const bs_logit_rules* rules, int* error_flag, void* stream) {
+  if (n_rows == 0) return BS_OK;
+  if (n_rows < 0 || !rules || !aligned16({out}) || rules->vocab < 1 || out_ld < rules->vocab || out_ld > kMaxStride / 4)
+    return BS_E_ARG;
+  const int size = type == BS_F32 ? 4 : 2;
+  const bool inplace = out == logits && out_ld == ld;
+  RulesArgs a;
+  if (!rules_args(logits, type, ld, n_rows, rules, error_flag, extent(out, n_rows, out_ld * size, (long long)rules->vocab * size),
+                  Extent{0, 0}, inplace, &a))
+    return BS_E_ARG;
+  return status_of(launch_logit_rules(a, out, out_ld, (cudaStream_t)stream));
+}
+
+int bs_op_rules_confidence(const void* logits, int type, long long ld, int n_rows, const bs_logit_rules* rules, int* tok,
+                           float* conf, int* error_flag, void* stream) {
+  if (n_rows == 0) return BS_OK;
+  RulesArgs a;
+  if (n_rows < 0 || !tok || !conf || !aligned4({tok, conf}) ||
+      !rules_args(logits, type, ld, n_rows, rules, error_flag, extent(tok, n_rows, 4, 4), extent(conf, n_rows, 4, 4), false, &a))
+    return BS_E_ARG;
+  return status_of(launch_rules_confidence(a, tok, conf, (cudaStream_t)stream));
 }
 
 }  // extern "C"

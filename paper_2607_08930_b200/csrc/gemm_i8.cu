@@ -1,0 +1,598 @@
+// Projections in 8-bit integers on the 5th-generation tensor cores:
+//   z[m, n] = (sum over k of A[m, k] W[n, k]) * w_scale[n] * a_scale[m],  codes int8, sums int32 (exact), scales fp32,
+// stored as bf16 (mode 0), added to fp32 (1), stored as fp32 (2), or silu(z) * z2 as bf16 with a second weight (3).
+//
+// Weight rows sit on the 128-row side of the tcgen05.mma tile and tokens on its N side, as in the bf16 projections: a
+// block step with a few dozen tokens wastes no tensor-core rows, and every CTA streams weights of its own.  A k step is
+// 128 codes (one 128-byte swizzle span, four kind::i8 instructions of 32).  One CTA per SM, warp-specialised:
+//   warp 0       TMA producer
+//   warp 1       MMA issuer (one thread)
+//   warps 2..9   epilogue: warp w reads TMEM lanes 32 (w mod 4) ..; its two groups of four take alternate token chunks
+// CG = 2: two CTAs of a cluster share every instruction (256 weight rows) and each stages half of the tokens, which
+// takes a quarter off the bytes a CTA loads for an operation.
+// SPLIT: a projection with fewer tiles than SMs has the k range of each tile shared by the CTAs (pairs) of one cluster;
+// they add their partial sums over distributed shared memory.  Integer sums are exact, so the order does not matter and
+// the result does not depend on the split.
+// Every wait is bounded: one that runs out raises the error flag and leaves NaN in the outputs that it kept from being
+// formed; all roles drain and TMEM is freed.
+#include <math.h>
+
+#include <mutex>
+
+#include "decode_ops.cuh"
+#include "tc_common.cuh"
+
+namespace bs {
+
+namespace {
+
+using namespace tc;
+
+constexpr int BKB = 128;                  // bytes = codes of a k step
+constexpr int kTileRows = 128;            // weight rows of a CTA
+constexpr int kThreads = 320;
+constexpr int kRing = 196 * 1024;         // operand stages
+constexpr int kMaxStages = 12;
+constexpr int kAccCols = 256;             // TMEM columns of an accumulator buffer (two of them)
+
+struct Params {
+  int M, N, K;
+  int tn;                   // tokens of a tile
+  int n_tiles, m_tiles, splits, kblocks, stages;
+  int nbuf;                 // accumulator buffers
+  int mgroup;               // token tiles per group of the item order (0: token tile fastest over all)
+  int vec;                  // bf16 rows take 16-byte stores
+  void* C;
+  long long ldc;
+  const float *sa, *sw, *sw2;
+  int* error_flag;
+};
+
+__device__ __forceinline__ unsigned cluster_rank() {
+  unsigned r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ unsigned in_cta(unsigned addr, unsigned rank) {
+  unsigned r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ void cluster_barrier() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+template <int CG>
+__device__ __forceinline__ void load_tile(unsigned dst, const CUtensorMap* map, int c0, int c1, unsigned bar) {
+  if (CG == 1)
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(bar) : "memory");
+  else
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes "
+                 "[%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(bar) : "memory");
+}
+// kind::i8: signed 8-bit A and B, both K-major, 32-bit integer accumulator, shape (128 CG) x n x 32.
+template <int CG>
+__device__ __forceinline__ unsigned instruction(int n) {
+  return (2u << 4) | (1u << 7) | (1u << 10) | ((unsigned)(n >> 3) << 17) | ((unsigned)((kTileRows * CG) >> 4) << 24);
+}
+template <int CG>
+__device__ __forceinline__ void mma_i8(unsigned d, unsigned a_lo, unsigned b_lo, unsigned idesc, unsigned accumulate) {
+  if (CG == 1)
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "mov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %5};\n\t"
+                 "tcgen05.mma.cta_group::1.kind::i8 [%0], da, db, %3, p;\n\t}"
+                 ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kDescHi) : "memory");
+  else
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "mov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %5};\n\t"
+                 "tcgen05.mma.cta_group::2.kind::i8 [%0], da, db, %3, p;\n\t}"
+                 ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kDescHi) : "memory");
+}
+// Arrives on the barrier once the MMAs issued before have completed (CG = 2: on the one at this offset in both CTAs).
+template <int CG>
+__device__ __forceinline__ void commit(unsigned bar, unsigned short both) {
+  if (CG == 1)
+    umma_commit(bar);
+  else
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                 ::"r"(bar), "h"(both) : "memory");
+}
+// What is in flight when a wait has run out gets 10 ms to arrive.
+constexpr long long kDrainCycles = 20000000ll;
+__device__ __forceinline__ void wait_briefly(unsigned bar, unsigned parity, long long until) {
+  while (!mbar_try_wait(bar, parity) && clock64() < until) {
+  }
+}
+__device__ __forceinline__ void tmem_ld8(unsigned taddr, int* r) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr));
+  tmem_ld_wait();
+}
+
+// Output tiles are numbered token tile fastest (the CTAs of a round then share weight tiles in L2); with mgroup the
+// token tiles are taken in groups, all weight tiles within one before the next, so that the group's activations stay in
+// L2 while the weights pass.
+__device__ __forceinline__ void tile_of(const Params& p, int tile, int* mt, int* nt) {
+  if (p.mgroup <= 0) {
+    *mt = tile % p.m_tiles;
+    *nt = tile / p.m_tiles;
+    return;
+  }
+  const int per = p.mgroup * p.n_tiles, g = tile / per, r = tile - g * per;
+  const int size = min(p.mgroup, p.m_tiles - g * p.mgroup);
+  *nt = r / size;
+  *mt = g * p.mgroup + r % size;
+}
+
+__device__ __forceinline__ float silu(float x) {         // as in the bf16 SwiGLU: relative error about 2^-21
+  float e, r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x * -1.4426950408889634f));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+  return x * r;
+}
+
+// Stores the finished values v[j] of (feature n, token t0 + j), j < jmax; `tile` (bf16 modes): 32 x 32 transposition
+// space of the warp, through which the rows leave in 16-byte pieces.
+template <int MODE>
+__device__ __forceinline__ void store_chunk(const Params& p, const float* v, int n, int t0, int jmax, bf16* tile) {
+  const int lane = threadIdx.x & 31;
+  if (MODE == 0 || MODE == 3) {
+    bf16* C = static_cast<bf16*>(p.C);
+    if (p.vec) {
+      __syncwarp();
+#pragma unroll
+      for (int j = 0; j < 32; ++j) tile[j * 32 + lane] = __float2bfloat16_rn(v[j]);
+      __syncwarp();
+      const int piece = lane & 3, nb = n - lane + piece * 8;
+      if (nb < p.N) {                                     // N is a multiple of 8 here
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int tok = i * 8 + (lane >> 2);
+          if (tok < jmax)
+            *reinterpret_cast<uint4*>(C + (long long)(t0 + tok) * p.ldc + nb) =
+                *reinterpret_cast<const uint4*>(tile + tok * 32 + piece * 8);
+        }
+      }
+      return;
+    }
+    if (n >= p.N) return;
+    bf16* c = C + (long long)t0 * p.ldc + n;
+#pragma unroll
+    for (int j = 0; j < 32; ++j)
+      if (j < jmax) c[(long long)j * p.ldc] = __float2bfloat16_rn(v[j]);
+  } else {
+    if (n >= p.N) return;
+    float* c = static_cast<float*>(p.C) + (long long)t0 * p.ldc + n;
+    if (MODE == 1) {
+      float u[32];
+#pragma unroll
+      for (int j = 0; j < 32; ++j) u[j] = j < jmax ? c[(long long)j * p.ldc] : 0.f;
+#pragma unroll
+      for (int j = 0; j < 32; ++j)
+        if (j < jmax) c[(long long)j * p.ldc] = u[j] + v[j];
+    } else {
+#pragma unroll
+      for (int j = 0; j < 32; ++j)
+        if (j < jmax) c[(long long)j * p.ldc] = v[j];
+    }
+  }
+}
+
+template <int CG, int MODE, bool SPLIT>
+__global__ void __launch_bounds__(kThreads, 1)
+k_gemm_i8(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_w2,
+          const __grid_constant__ CUtensorMap map_x, const Params p) {
+  constexpr bool kDual = MODE == 3;
+  constexpr int kW = kDual ? 2 : 1;
+  constexpr int kWBytes = kTileRows * BKB;
+  extern __shared__ unsigned char smem_dyn[];
+  __shared__ __align__(8) unsigned long long bars[2 * kMaxStages + 5];    // full, empty, accumulator full, empty; drain
+  __shared__ __align__(16) bf16 out_tile[(MODE == 0 || MODE == 3) ? 8 : 1][32 * 32];
+  __shared__ __align__(16) float tok_scale[8][32];
+  __shared__ unsigned tmem_slot;
+  __shared__ int s_abort;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const unsigned rank = (CG == 2 || SPLIT) ? cluster_rank() : 0u;
+  const unsigned half = CG == 2 ? rank & 1u : 0u;           // place in the pair
+  const unsigned lead = CG == 2 ? rank & ~1u : rank;        // the pair's leader
+  const int split = SPLIT ? (int)(rank / CG) : 0;
+  const int group_ctas = CG * (SPLIT ? p.splits : 1);
+  const int worker = (int)blockIdx.x / group_ctas, workers = (int)gridDim.x / group_ctas;
+  const unsigned smem0 = (smem_u32(smem_dyn) + 1023u) & ~1023u;
+  const int x_rows = p.tn / CG;
+  const int stage_bytes = kW * kWBytes + x_rows * BKB;
+  const unsigned full0 = smem_u32(&bars[0]), empty0 = smem_u32(&bars[kMaxStages]);
+  const unsigned tfull0 = smem_u32(&bars[2 * kMaxStages]), tempty0 = smem_u32(&bars[2 * kMaxStages + 2]);
+  const unsigned drain = smem_u32(&bars[2 * kMaxStages + 4]);
+  const unsigned full_lead0 = CG == 2 ? in_cta(full0, lead) : full0;
+  const unsigned tempty_lead0 = CG == 2 ? in_cta(tempty0, lead) : tempty0;
+  const unsigned peer_abort = CG == 2 ? in_cta(smem_u32(&s_abort), rank ^ 1u) : 0u;
+  const unsigned short both = (unsigned short)(3u << lead);
+  const int items = p.n_tiles * p.m_tiles;
+  const int kb0 = SPLIT ? (int)((long long)p.kblocks * split / p.splits) : 0;
+  const int kb1 = SPLIT ? (int)((long long)p.kblocks * (split + 1) / p.splits) : p.kblocks;
+
+  if (threadIdx.x == 0) {
+    s_abort = 0;
+    for (int i = 0; i < p.stages; ++i) {
+      mbar_init(full0 + 8 * i, 1);
+      mbar_init(empty0 + 8 * i, 1);
+    }
+    mbar_init(drain, 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(tfull0 + 8 * i, 1);
+      mbar_init(tempty0 + 8 * i, 8 * CG);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    if (CG == 1) {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tmem_slot)) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tmem_slot)) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  if (CG == 2) cluster_barrier();                           // the partner's barriers exist before anything signals them
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const unsigned tmem = tmem_slot;
+  volatile int* abort_flag = &s_abort;
+  // (the tensor memory is held: a kernel behind that allocates its own before it waits cannot keep this one from it)
+  pdl_trigger();
+  pdl_wait();                                               // codes, scales and outputs may come from the kernel before
+
+  if (warp == 0) {
+    // ---------------------------------------------------------------- TMA producer
+    if (lane == 0) {
+      int stage = 0, filled = 0;
+      unsigned phase = 0;
+      bool ok = true;
+      for (int it = worker; it < items && ok; it += workers) {
+        int mt, nt;
+        tile_of(p, it, &mt, &nt);
+        const int wrow = (nt * CG + (int)half) * kTileRows;
+        const int xrow = mt * p.tn + (int)half * x_rows;
+        for (int kb = kb0; kb < kb1; ++kb) {
+          if (!mbar_wait(empty0 + 8 * stage, phase ^ 1u, abort_flag)) { ok = false; break; }
+          if (half == 0) mbar_expect_tx(full0 + 8 * stage, (unsigned)(CG * stage_bytes));
+          const unsigned at = smem0 + stage * stage_bytes;
+          load_tile<CG>(at, &map_w, kb * BKB, wrow, full_lead0 + 8 * stage);
+          if (kDual) load_tile<CG>(at + kWBytes, &map_w2, kb * BKB, wrow, full_lead0 + 8 * stage);
+          load_tile<CG>(at + kW * kWBytes, &map_x, kb * BKB, xrow, full_lead0 + 8 * stage);
+          ++filled;
+          if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+        }
+      }
+      if ((!ok || *abort_flag) && half == 0) {              // copies in flight land before this CTA leaves
+        const long long until = clock64() + kDrainCycles;
+        for (int f = max(0, filled - p.stages); f < filled; ++f)
+          wait_briefly(full0 + 8 * (f % p.stages), (unsigned)(f / p.stages) & 1u, until);
+      }
+      if (CG == 2 && !ok) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(peer_abort), "r"(1) : "memory");
+    }
+  } else if (warp == 1) {
+    // ---------------------------------------------------------------- MMA issuer (of a pair: the leader)
+    if (lane == 0 && half == 0) {
+      int stage = 0, local = 0;
+      unsigned phase = 0;
+      bool ok = true;
+      const unsigned idesc = instruction<CG>(p.tn);
+      const unsigned lo0 = desc_lo(smem0), step = (unsigned)stage_bytes >> 4;
+      // debugging build: an error flag of -1 - b before the call makes the wait for k step b run out
+      const int fail_at = kBoundsCheck && p.error_flag ? -1 - *static_cast<volatile int*>(p.error_flag) : -1;
+      unsigned lo = lo0;
+      for (int it = worker; it < items && ok; it += workers, ++local) {
+        const int acc = p.nbuf == 2 ? local & 1 : 0;
+        const unsigned acc_phase = (unsigned)(p.nbuf == 2 ? local >> 1 : local) & 1u;
+        if (!mbar_wait(tempty0 + 8 * acc, acc_phase ^ 1u, abort_flag)) { ok = false; break; }
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const unsigned d0 = tmem + acc * kAccCols, d1 = d0 + (p.nbuf == 2 ? kAccCols / 2 : kAccCols);
+        unsigned accumulate = 0u;
+        for (int kb = kb0; kb < kb1; ++kb) {
+          if (kBoundsCheck && kb == fail_at) *abort_flag = 1;
+          if ((kBoundsCheck && kb == fail_at) || !mbar_wait(full0 + 8 * stage, phase, abort_flag)) { ok = false; break; }
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const unsigned b = lo + kW * (kWBytes >> 4);
+#pragma unroll
+          for (int k = 0; k < BKB / 32; ++k) {
+            mma_i8<CG>(d0, lo + 2 * k, b + 2 * k, idesc, k == 0 ? accumulate : 1u);
+            if (kDual) mma_i8<CG>(d1, lo + (kWBytes >> 4) + 2 * k, b + 2 * k, idesc, k == 0 ? accumulate : 1u);
+          }
+          accumulate = 1u;
+          commit<CG>(empty0 + 8 * stage, both);
+          lo += step;
+          if (++stage == p.stages) { stage = 0; phase ^= 1u; lo = lo0; }
+        }
+        if (ok) commit<CG>(tfull0 + 8 * acc, both);
+      }
+      if (!ok) {                                            // products in flight end before tensor memory is freed
+        commit<CG>(drain, both);
+        wait_briefly(drain, 0u, clock64() + kDrainCycles);
+      }
+      if (CG == 2 && !ok) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(peer_abort), "r"(1) : "memory");
+    }
+  } else if (!SPLIT) {
+    // ---------------------------------------------------------------- epilogue
+    const int q = warp & 3, group = (warp - 2) >> 2;
+    float* const scales = tok_scale[warp - 2];
+    int local = 0;
+    bool ok = true;
+    for (int it = worker; it < items; it += workers, ++local) {
+      int mt, nt;
+      tile_of(p, it, &mt, &nt);
+      const int n = (nt * CG + (int)half) * kTileRows + q * 32 + lane;
+      const float w = n < p.N ? __ldg(p.sw + n) : 0.f;
+      const float w2 = kDual && n < p.N ? __ldg(p.sw2 + n) : 0.f;
+      const int acc = p.nbuf == 2 ? local & 1 : 0;
+      const unsigned acc_phase = (unsigned)(p.nbuf == 2 ? local >> 1 : local) & 1u;
+      ok = ok && mbar_wait(tfull0 + 8 * acc, acc_phase, abort_flag);
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      const unsigned row = tmem + ((unsigned)(q * 32) << 16) + acc * kAccCols;
+      const unsigned second = p.nbuf == 2 ? kAccCols / 2 : kAccCols;
+      const int limit = min(p.tn, p.M - mt * p.tn);
+      for (int c0 = group * 32; c0 < limit; c0 += 64) {
+        const int t0 = mt * p.tn + c0, jmax = min(32, limit - c0);
+        unsigned z[32], y[kDual ? 32 : 1];
+        if (ok) {
+          tmem_ld32_nowait(row + c0, z);
+          if (kDual) tmem_ld32_nowait(row + second + c0, y);
+        }
+        const float s = lane < jmax ? __ldg(p.sa + t0 + lane) : 0.f;
+        __syncwarp();
+        scales[lane] = s;
+        __syncwarp();
+        if (ok) tmem_ld_wait();
+        float v[32];
+#pragma unroll
+        for (int j = 0; j < 32; j += 4) {
+          const float4 t = *reinterpret_cast<const float4*>(scales + j);
+          const float ts[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float g = (float)(int)z[j + i] * w * ts[i];
+            v[j + i] = kDual ? silu(g) * ((float)(int)y[kDual ? j + i : 0] * w2 * ts[i]) : g;
+          }
+        }
+        if (!ok) {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(0x7fffffffu);
+        }
+        store_chunk<MODE>(p, v, n, t0, jmax, out_tile[(MODE == 0 || MODE == 3) ? warp - 2 : 0]);
+      }
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) {
+        if (CG == 1) mbar_arrive(tempty0 + 8 * acc);
+        else asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(tempty_lead0 + 8 * acc) : "memory");
+      }
+    }
+    if (CG == 2 && !ok && lane == 0) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(peer_abort), "r"(1) : "memory");
+  }
+
+  if (SPLIT) {
+    // One item per cluster.  Chunk c (8 tokens) of the tile belongs to split c mod S: every CTA sends its partial sums of
+    // the others' chunks into their idle operand rings, and finishes its own.  All threads reach both barriers whatever
+    // happened before, so no CTA is left waiting.
+    const int S = p.splits;
+    int mt, nt;
+    tile_of(p, worker, &mt, &nt);
+    const int limit = min(p.tn, p.M - mt * p.tn);
+    const int chunks = (limit + 7) / 8, own = (chunks + S - 1) / S;       // chunks a CTA may own
+    const int q = warp & 3, group = (warp - 2) >> 2;
+    const int feature = q * 32 + lane;
+    const unsigned row = tmem + ((unsigned)(q * 32) << 16);
+    bool ok = true;
+    __syncwarp();                                           // the role branches above end here
+    if (warp >= 2) {
+      ok = mbar_wait(tfull0, 0u, abort_flag);
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    }
+    __syncthreads();
+    cluster_barrier();
+    if (warp >= 2) {
+      for (int c = group; c < chunks; c += 2) {
+        const int owner = c % S;
+        if (owner == split) continue;
+        int z[8];
+        tmem_ld8(row + c * 8, z);
+        // a partial sum that is not there is sent as the least integer: no sum of fewer than 131072 products reaches it
+        if (!ok) z[0] = z[1] = z[2] = z[3] = z[4] = z[5] = z[6] = z[7] = (int)0x80000000;
+        const int slot = split < owner ? split : split - 1;
+        const unsigned to = in_cta(smem0 + (unsigned)(((slot * own + c / S) * kTileRows + feature) * 32),
+                                   (unsigned)(owner * CG) + half);
+        asm volatile("st.shared::cluster.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(z[0]), "r"(z[1]), "r"(z[2]), "r"(z[3]) : "memory");
+        asm volatile("st.shared::cluster.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(to + 16), "r"(z[4]), "r"(z[5]), "r"(z[6]), "r"(z[7]) : "memory");
+      }
+    }
+    cluster_barrier();
+    if (warp >= 2) {
+      const int n = (nt * CG + (int)half) * kTileRows + feature;
+      const float w = n < p.N ? __ldg(p.sw + n) : 0.f;
+      for (int i = group; i * S + split < chunks; i += 2) {
+        const int c = i * S + split, t0 = mt * p.tn + c * 8, jmax = min(8, limit - c * 8);
+        int z[8];
+        tmem_ld8(row + c * 8, z);
+        bool whole = ok;
+        for (int slot = 0; slot < S - 1; ++slot) {
+          const unsigned from = smem0 + (unsigned)(((slot * own + i) * kTileRows + feature) * 32);
+          int y[8];
+          asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(y[0]), "=r"(y[1]), "=r"(y[2]), "=r"(y[3]) : "r"(from) : "memory");
+          asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(y[4]), "=r"(y[5]), "=r"(y[6]), "=r"(y[7]) : "r"(from + 16) : "memory");
+          whole = whole && y[0] != (int)0x80000000;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) z[j] += y[j];
+        }
+        if (n < p.N) {
+          float v[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            v[j] = whole ? (float)z[j] * w * (j < jmax ? __ldg(p.sa + t0 + j) : 0.f) : __uint_as_float(0x7fffffffu);
+          if (MODE == 0) {
+            bf16* o = static_cast<bf16*>(p.C) + (long long)t0 * p.ldc + n;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              if (j < jmax) o[(long long)j * p.ldc] = __float2bfloat16_rn(v[j]);
+          } else {
+            float* o = static_cast<float*>(p.C) + (long long)t0 * p.ldc + n;
+            if (MODE == 1) {
+#pragma unroll
+              for (int j = 0; j < 8; ++j)
+                if (j < jmax) v[j] += o[(long long)j * p.ldc];
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              if (j < jmax) o[(long long)j * p.ldc] = v[j];
+          }
+        }
+      }
+    }
+  }
+
+  // Neither CTA of a pair may leave (or free its tensor memory) while the partner can still reach it.
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  if (CG == 2) cluster_barrier();
+  if (s_abort && threadIdx.x == 0 && p.error_flag) atomicMax(p.error_flag, 1);
+  if (warp == 1) {
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    if (CG == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  }
+}
+
+using Kernel = void (*)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const Params);
+template <int CG, bool SPLIT>
+Kernel kernel_of(int mode) {
+  switch (mode) {
+    case 0: return k_gemm_i8<CG, 0, SPLIT>;
+    case 1: return k_gemm_i8<CG, 1, SPLIT>;
+    case 2: return k_gemm_i8<CG, 2, SPLIT>;
+    default: return k_gemm_i8<CG, 3, false>;
+  }
+}
+
+constexpr int kSmem = kRing + 1024;
+
+// One-time set-up per device: SM count, shared-memory attributes, how many clusters of each size are resident at once.
+struct DevInfo {
+  int num_sms;
+  int ok;
+  int clusters[9];           // by cluster size (single-CTA kernel for sizes without pairs: 3, 5, 6, 7)
+};
+DevInfo g_dev[kMaxDevices];
+std::mutex g_mutex;
+
+const DevInfo* dev_info() {
+  DevInfo* d = device_slot(g_dev);
+  if (!d) return nullptr;
+  std::lock_guard<std::mutex> lock(g_mutex);
+  if (!d->num_sms) {
+    int dev = 0, n = 0;
+    cudaGetDevice(&dev);
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) return nullptr;
+    bool ok = true;
+    for (int m = 0; m < 4 && ok; ++m)
+      for (Kernel k : {kernel_of<1, false>(m), kernel_of<1, true>(m), kernel_of<2, false>(m), kernel_of<2, true>(m)})
+        ok = ok && cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) == cudaSuccess;
+    for (int c = 1; c <= 8 && ok; ++c) {
+      cudaLaunchConfig_t cfg = {};
+      cfg.gridDim = dim3((unsigned)(n / c * c));
+      cfg.blockDim = dim3(kThreads);
+      cfg.dynamicSmemBytes = kSmem;
+      cudaLaunchAttribute at[1];
+      at[0].id = cudaLaunchAttributeClusterDimension;
+      at[0].val.clusterDim.x = (unsigned)c; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+      cfg.attrs = at; cfg.numAttrs = 1;
+      int most = 0;
+      if (cudaOccupancyMaxActiveClusters(&most, c == 2 ? kernel_of<2, false>(0) : kernel_of<1, true>(0), &cfg) != cudaSuccess) {
+        cudaGetLastError();
+        most = 0;
+      }
+      d->clusters[c] = most;
+    }
+    if (!ok) cudaGetLastError();
+    d->ok = ok;
+    d->num_sms = n;
+  }
+  return d;
+}
+
+// [rows][cols] int8, `ld` bytes apart; boxes of `box` rows by 128 bytes, 128B-swizzled, zeros outside.
+bool encode(const void* base, long long rows, long long cols, long long ld, int box, CUtensorMap* out) {
+  const auto fn = tensor_map_encoder();
+  if (!fn) return false;
+  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)ld};
+  const cuuint32_t b[2] = {BKB, (cuuint32_t)box}, e[2] = {1, 1};
+  return fn(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, b, e, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+struct Plan {
+  int cg, splits, tn, m_tiles, n_tiles, workers, stages, nbuf;
+};
+
+}  // namespace
+
+cudaError_t launch_gemm_i8(const GemmI8Args& a, cudaStream_t s) {
+  if (a.M <= 0 || a.N <= 0) return cudaSuccess;
+  const DevInfo* dv = dev_info();
+  if (!dv || !dv->ok) return cudaErrorNotSupported;
+  const bool dual = a.mode == 3;
+  Plan pl;
+  pl.cg = a.M > 128 && dv->clusters[2] > 0 ? 2 : 1;
+  pl.m_tiles = (a.M + 255) / 256;
+  const int per = (a.M + pl.m_tiles - 1) / pl.m_tiles, unit = pl.cg == 2 ? 32 : 16;
+  pl.tn = (per + unit - 1) / unit * unit;
+  pl.n_tiles = (a.N + kTileRows * pl.cg - 1) / (kTileRows * pl.cg);
+  const int kblocks = (a.K + BKB - 1) / BKB;
+  const long long items = (long long)pl.n_tiles * pl.m_tiles;
+  pl.splits = 1;
+  if (!dual) {
+    for (int sp = 8 / pl.cg; sp > 1; --sp) {
+      if (pl.cg == 2 && (sp & (sp - 1))) continue;
+      if (items <= dv->clusters[sp * pl.cg] && kblocks / sp >= 2) { pl.splits = sp; break; }
+    }
+  }
+  pl.nbuf = dual && pl.tn > 128 ? 1 : 2;
+  const int stage_bytes = (dual ? 2 : 1) * kTileRows * BKB + pl.tn / pl.cg * BKB;
+  pl.stages = kRing / stage_bytes;
+  if (pl.stages > kMaxStages) pl.stages = kMaxStages;
+  const int most = pl.cg == 2 ? dv->clusters[2] : dv->num_sms;
+  pl.workers = (int)(items < most ? items : most);
+
+  Params p;
+  p.M = a.M; p.N = a.N; p.K = a.K; p.tn = pl.tn; p.n_tiles = pl.n_tiles; p.m_tiles = pl.m_tiles; p.splits = pl.splits;
+  p.kblocks = kblocks; p.stages = pl.stages; p.nbuf = pl.nbuf;
+  p.mgroup = (long long)a.M * a.K > (56ll << 20) && pl.m_tiles > 16 ? 16 : 0;
+  p.vec = a.ldc % 8 == 0 && a.N % 8 == 0 && ((uintptr_t)a.C & 15) == 0;
+  p.C = a.C; p.ldc = a.ldc; p.sa = a.sa; p.sw = a.sw; p.sw2 = a.sw2; p.error_flag = a.error_flag;
+  CUtensorMap mw, mw2, mx;
+  if (!encode(a.W, a.N, a.K, a.ldw, kTileRows, &mw) || !encode(a.A, a.M, a.K, a.lda, pl.tn / pl.cg, &mx))
+    return cudaErrorNotSupported;
+  mw2 = mw;
+  if (dual && !encode(a.W2, a.N, a.K, a.ldw, kTileRows, &mw2)) return cudaErrorNotSupported;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(pl.workers * pl.cg * pl.splits));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kSmem;
+  cfg.stream = s;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = (unsigned)(pl.cg * pl.splits); at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 2;
+  Kernel k = pl.cg == 2 ? (pl.splits > 1 ? kernel_of<2, true>(a.mode) : kernel_of<2, false>(a.mode))
+                        : (pl.splits > 1 ? kernel_of<1, true>(a.mode) : kernel_of<1, false>(a.mode));
+  return cudaLaunchKernelEx(&cfg, k, mw, mw2, mx, p);
+}
+
+}  // namespace bs

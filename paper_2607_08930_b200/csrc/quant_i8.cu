@@ -1,0 +1,207 @@
+// Rows (activations of a token, weights of an output channel) as 8-bit integer codes with one scale each.
+//
+//   y = x, or gain * x / sqrt(mean(x^2) + eps) with a gain;  s = max(fp32(max |y| / 127), 2^-126);
+//   code = y / s rounded to the nearest integer, halves to the even one - of the exact quotient, not of a rounded one.
+//
+// Bound by memory: x is read once, a byte an element is written.  One CTA per row keeps the row in registers (32 elements
+// a thread, all loads in flight before the first use) between the maximum and the rounding; rows too long for that are
+// read twice, the second time from L2.
+// A row with an infinite or NaN element has no scale: NaN, with zero codes, so that every product of it is NaN.
+#include "decode_ops.cuh"
+
+namespace bs {
+
+namespace {
+
+constexpr int kUnit = 8;            // elements a thread loads and rounds at a time
+constexpr int kUnits = 4;           // units a thread keeps
+
+// The eight elements from element `at` of a row on; those at and behind K are zero.
+template <bool F32, bool VEC>
+__device__ __forceinline__ void load_unit(const void* row, int at, int K, float* v) {
+  if (VEC && at + kUnit <= K) {
+    if (F32) {
+      const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(row) + at);
+      const float4 a = __ldg(p), b = __ldg(p + 1);
+      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+      v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    } else {
+      const uint4 u = __ldg(reinterpret_cast<const uint4*>(static_cast<const bf16*>(row) + at));
+      const unsigned w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kUnit; ++i) {
+      v[i] = 0.f;
+      if (at + i < K)
+        v[i] = F32 ? __ldg(static_cast<const float*>(row) + at + i)
+                   : __bfloat162float(__ldg(static_cast<const bf16*>(row) + at + i));
+    }
+  }
+}
+
+// v *= gain, and this unit's share of the sum of squares of v before that.
+__device__ __forceinline__ float apply_gain(const bf16* gain, int at, int K, float* v) {
+  float ss = 0.f;
+#pragma unroll
+  for (int i = 0; i < kUnit; ++i) ss = fmaf(v[i], v[i], ss);
+  float g[kUnit];
+  load_unit<false, true>(gain, at, K, g);
+#pragma unroll
+  for (int i = 0; i < kUnit; ++i) v[i] *= g[i];
+  return ss;
+}
+
+// |v| as an integer orders as the value does, with infinities and NaN above all numbers.
+__device__ __forceinline__ unsigned magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+
+// Codes of eight elements, y = v * r.  Adding 1.5 * 2^23 leaves the nearest integer of y * inv in the low bits; where the
+// remainder y - q s (exact: a multiple of half a step of s, no larger than s) reaches half of s the quotient's own rounding
+// may have decided, and the remainder decides instead.
+template <bool NORM>
+__device__ __forceinline__ uint2 round_unit(const float* v, float r, float s, float inv) {
+  constexpr float kMagic = 12582912.f;
+  unsigned b[kUnit];
+  float most = 0.f;
+#pragma unroll
+  for (int i = 0; i < kUnit; ++i) {
+    const float y = NORM ? v[i] * r : v[i];
+    const float t = fmaf(y, inv, kMagic);
+    most = fmaxf(most, fabsf(fmaf(kMagic - t, s, y)));
+    b[i] = __float_as_uint(t);
+  }
+  if (most + most >= s) {
+#pragma unroll
+    for (int i = 0; i < kUnit; ++i) {
+      const float y = NORM ? v[i] * r : v[i];
+      const float q = __uint_as_float(b[i]) - kMagic;
+      const float rest = fmaf(-q, s, y), twice = fabsf(rest) + fabsf(rest);
+      if (twice > s || (twice == s && (b[i] & 1u))) b[i] += rest > 0.f ? 1u : 0xffffffffu;
+    }
+  }
+  uint2 out;
+  out.x = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+  out.y = __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410);
+  return out;
+}
+
+__device__ __forceinline__ void store_unit(int8_t* row, int at, int K, uint2 c) {
+  if (at + kUnit <= K) {
+    *reinterpret_cast<uint2*>(row + at) = c;
+  } else {
+    for (int i = 0; at + i < K; ++i) row[at + i] = (int8_t)((i < 4 ? c.x >> (8 * i) : c.y >> (8 * (i - 4))) & 0xffu);
+  }
+}
+
+template <bool F32, bool VEC, bool NORM, bool LONG>
+__global__ void __launch_bounds__(1024) k_quant_i8(const QuantI8Args a) {
+  __shared__ unsigned s_max[32];
+  __shared__ float s_sum[32];
+  pdl_wait();
+  pdl_trigger();
+  const int m = blockIdx.x;
+  long long from = m;
+  if (a.idx) {
+    from = __ldg(a.idx + m);
+    if (from < 0 || from >= a.x_rows) {
+      if (threadIdx.x == 0 && a.error_flag) atomicMax(a.error_flag, 100 + SITE_QUANT_I8);
+      return;
+    }
+  }
+  const void* row = static_cast<const char*>(a.x) + from * a.ldx * (F32 ? 4 : 2);
+  const int step = blockDim.x * kUnit;
+  float v[kUnits][kUnit];
+  unsigned top = 0;
+  float ss = 0.f;
+  if (!LONG) {
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      const int at = threadIdx.x * kUnit + u * step;
+      if (at < a.K) load_unit<F32, VEC>(row, at, a.K, v[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      const int at = threadIdx.x * kUnit + u * step;
+      if (at < a.K) {
+        if (NORM) ss += apply_gain(a.gain, at, a.K, v[u]);
+#pragma unroll
+        for (int i = 0; i < kUnit; ++i) top = max(top, magnitude(v[u][i]));
+      }
+    }
+  } else {
+    for (int at = threadIdx.x * kUnit; at < a.K; at += step) {
+      load_unit<F32, VEC>(row, at, a.K, v[0]);
+      if (NORM) ss += apply_gain(a.gain, at, a.K, v[0]);
+#pragma unroll
+      for (int i = 0; i < kUnit; ++i) top = max(top, magnitude(v[0][i]));
+    }
+  }
+  top = __reduce_max_sync(0xffffffffu, top);
+  if (NORM) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+  }
+  const int warps = blockDim.x >> 5, lane = threadIdx.x & 31;
+  if (warps > 1) {
+    if (lane == 0) {
+      s_max[threadIdx.x >> 5] = top;
+      if (NORM) s_sum[threadIdx.x >> 5] = ss;
+    }
+    __syncthreads();
+    top = __reduce_max_sync(0xffffffffu, lane < warps ? s_max[lane] : 0u);
+    if (NORM) {
+      ss = lane < warps ? s_sum[lane] : 0.f;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+    }
+  }
+  // rounding is monotonic: the largest |gain x| times r is the largest |y|
+  const float r = NORM ? rsqrtf(ss / (float)a.K + a.eps) : 1.f;
+  const float big = NORM ? __uint_as_float(top) * r : __uint_as_float(top);
+  const bool real = top < 0x7f800000u && big < INFINITY;
+  const float s = fmaxf(__fdiv_rn(big, 127.f), 0x1p-126f);
+  const float inv = __frcp_rn(s);
+  if (threadIdx.x == 0) a.scale[m] = real ? s : __uint_as_float(0x7fffffffu);
+  int8_t* out = a.codes + (long long)m * a.ldc;
+  if (!LONG) {
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      const int at = threadIdx.x * kUnit + u * step;
+      if (at < a.K) store_unit(out, at, a.K, real ? round_unit<NORM>(v[u], r, s, inv) : make_uint2(0u, 0u));
+    }
+  } else {
+    for (int at = threadIdx.x * kUnit; at < a.K; at += step) {
+      load_unit<F32, VEC>(row, at, a.K, v[0]);
+      if (NORM) apply_gain(a.gain, at, a.K, v[0]);
+      store_unit(out, at, a.K, real ? round_unit<NORM>(v[0], r, s, inv) : make_uint2(0u, 0u));
+    }
+  }
+}
+
+template <bool F32, bool VEC>
+cudaError_t launch_typed(const QuantI8Args& a, cudaStream_t s) {
+  const int units = (a.K + kUnit - 1) / kUnit;
+  int threads = ((units + kUnits - 1) / kUnits + 31) / 32 * 32;
+  const bool lng = threads > 1024;
+  if (lng) threads = 1024;
+  void (*k)(const QuantI8Args);
+  if (a.gain) k = lng ? k_quant_i8<F32, VEC, true, true> : k_quant_i8<F32, VEC, true, false>;
+  else k = lng ? k_quant_i8<F32, VEC, false, true> : k_quant_i8<F32, VEC, false, false>;
+  return launch_pdl(k, dim3(a.M), dim3(threads), 0, s, a);
+}
+
+}  // namespace
+
+cudaError_t launch_quant_i8(const QuantI8Args& a, cudaStream_t s) {
+  if (a.M <= 0 || a.K <= 0) return cudaSuccess;
+  const bool vec = ((uintptr_t)a.x & 15) == 0 && (a.ldx * (a.f32 ? 4 : 2)) % 16 == 0;
+  if (a.f32) return vec ? launch_typed<true, true>(a, s) : launch_typed<true, false>(a, s);
+  return vec ? launch_typed<false, true>(a, s) : launch_typed<false, false>(a, s);
+}
+
+}  // namespace bs
