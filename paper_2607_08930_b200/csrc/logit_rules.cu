@@ -28,6 +28,8 @@ constexpr int kRowsAtOnce = 32;            // rows whose parts are kept before t
 constexpr int kMaxChunks = 8;
 constexpr unsigned kInPrompt = 0x80000000u;
 
+constexpr int kListed = 4096;              // touched entries that a table lists (those beyond are found by their bits)
+
 struct Part {
   float m, s;
   int at;
@@ -63,9 +65,12 @@ __device__ __forceinline__ void widen(const uint4& u, float* v, const bf16*) {
 
 // The table of one request's rules over the entries [c0, c0 + n) of a CTA.
 struct Table {
-  unsigned* plain;       // bit set: only the grammar decides about this entry; word -1 and word `words` are zero
+  unsigned* plain;       // bit set: only the grammar decides about this entry; the word behind the last is zero
   unsigned* biased;      // bit set: the request has a bias for this entry
   unsigned* count;       // kInPrompt | times generated
+  unsigned* list;        // the touched entries in ascending order: entry | (1 + place of its first bias, or 0) << 16
+  int listed;            // how many of them
+  int cut;               // the touched entries of words from this one on are not listed
   int c0, n, words;
   int bias_lo, bias_hi;  // the request's biases (all of them)
   float rho, alpha, phi;
@@ -83,8 +88,29 @@ __device__ void raise(const RulesArgs& a) {
   if (a.error_flag) atomicMax(a.error_flag, 100 + SITE_RULES);
 }
 
+// The place of the first bias of token id (ids ascend), bias_hi if there is none.
+__device__ __forceinline__ int find_bias(const RulesArgs& a, const Table& t, int id) {
+  int lo = t.bias_lo, hi = t.bias_hi;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (__ldg(a.bias_tok + mid) < id) lo = mid + 1;
+    else hi = mid;
+  }
+  return lo;
+}
+
 // All threads of the CTA; req < 0: no rules but the grammar.
 __device__ void build_table(const RulesArgs& a, Table& t, int req) {
+  __shared__ int s_first[kWarps + 1], s_cut;
+  int begin = 0, gen = 0, end = 0, lo = 0, hi = 0;
+  t.rho = 1.f; t.alpha = 0.f; t.phi = 0.f;
+  if (req >= 0 && a.ctx) {
+    begin = __ldg(a.ctx_begin + req); gen = __ldg(a.ctx_gen + req); end = __ldg(a.ctx_end + req);
+    if (a.repetition) t.rho = __ldg(a.repetition + req);
+    if (a.presence) t.alpha = __ldg(a.presence + req);
+    if (a.frequency) t.phi = __ldg(a.frequency + req);
+  }
+  if (req >= 0 && a.bias_at) { lo = __ldg(a.bias_at + req); hi = __ldg(a.bias_at + req + 1); }
   __syncthreads();                                           // the rows before are done with the table
   for (int w = threadIdx.x; w < t.words; w += kThreads) {
     t.plain[w] = in_range(t, w, a.mask_id);
@@ -92,54 +118,78 @@ __device__ void build_table(const RulesArgs& a, Table& t, int req) {
   }
   if (a.ctx)
     for (int i = threadIdx.x * 4; i < t.words * 32; i += kThreads * 4) *reinterpret_cast<uint4*>(t.count + i) = make_uint4(0, 0, 0, 0);
-  t.bias_lo = t.bias_hi = 0;
-  t.rho = 1.f; t.alpha = 0.f; t.phi = 0.f;
+  if (threadIdx.x == 0) s_cut = t.words;
+  if (begin < 0 || gen < begin || end < gen || end > a.ctx_total || lo < 0 || hi < lo || hi > a.bias_total) {
+    if (threadIdx.x == 0 && t.c0 == 0) raise(a);
+    if (begin < 0 || gen < begin || end < gen || end > a.ctx_total) begin = gen = end = 0;
+    if (lo < 0 || hi < lo || hi > a.bias_total) lo = hi = 0;
+  }
+  t.bias_lo = lo; t.bias_hi = hi;
   __syncthreads();
-  if (req >= 0) {
-    const bool tells = threadIdx.x == 0 && t.c0 == 0;
-    if (a.ctx) {
-      const int begin = __ldg(a.ctx_begin + req), gen = __ldg(a.ctx_gen + req), end = __ldg(a.ctx_end + req);
-      if (begin < 0 || gen < begin || end < gen || end > a.ctx_total) {
-        if (tells) raise(a);
-      } else {
-        for (int i = begin + threadIdx.x; i < end; i += kThreads) {
-          const int id = __ldg(a.ctx + i), e = id - t.c0;
-          if ((unsigned)id >= (unsigned)a.vocab) {
-            if (t.c0 == 0) raise(a);
-          } else if (e >= 0 && e < t.n && id != a.mask_id) {
-            if (i >= gen) atomicAdd(t.count + e, 1u);
-            else atomicOr(t.count + e, kInPrompt);
-            atomicAnd(t.plain + (e >> 5), ~(1u << (e & 31)));
-          }
-        }
-        if (a.repetition) t.rho = __ldg(a.repetition + req);
-        if (a.presence) t.alpha = __ldg(a.presence + req);
-        if (a.frequency) t.phi = __ldg(a.frequency + req);
-      }
+  for (int i = begin + threadIdx.x; i < end; i += kThreads) {
+    const int id = __ldg(a.ctx + i), e = id - t.c0;
+    if ((unsigned)id >= (unsigned)a.vocab) {
+      if (t.c0 == 0) raise(a);
+    } else if (e >= 0 && e < t.n && id != a.mask_id) {
+      if (i >= gen) atomicAdd(t.count + e, 1u);
+      else atomicOr(t.count + e, kInPrompt);
+      atomicAnd(t.plain + (e >> 5), ~(1u << (e & 31)));
     }
-    if (a.bias_at) {
-      const int lo = __ldg(a.bias_at + req), hi = __ldg(a.bias_at + req + 1);
-      if (lo < 0 || hi < lo || hi > a.bias_total) {
-        if (tells) raise(a);
-      } else {
-        t.bias_lo = lo; t.bias_hi = hi;
-        for (int i = lo + threadIdx.x; i < hi; i += kThreads) {
-          const int id = __ldg(a.bias_tok + i), e = id - t.c0;
-          if ((unsigned)id >= (unsigned)a.vocab || (i > lo && __ldg(a.bias_tok + i - 1) > id)) {
-            if (t.c0 == 0) raise(a);
-          } else if (e >= 0 && e < t.n && id != a.mask_id) {
-            atomicOr(t.biased + (e >> 5), 1u << (e & 31));
-            atomicAnd(t.plain + (e >> 5), ~(1u << (e & 31)));
-          }
-        }
-      }
+  }
+  for (int i = lo + threadIdx.x; i < hi; i += kThreads) {
+    const int id = __ldg(a.bias_tok + i), e = id - t.c0;
+    if ((unsigned)id >= (unsigned)a.vocab || (i > lo && __ldg(a.bias_tok + i - 1) > id)) {
+      if (t.c0 == 0) raise(a);
+    } else if (e >= 0 && e < t.n && id != a.mask_id) {
+      atomicOr(t.biased + (e >> 5), 1u << (e & 31));
+      atomicAnd(t.plain + (e >> 5), ~(1u << (e & 31)));
     }
   }
   __syncthreads();
+  // list the touched entries in order: thread i takes `each` words
+  const int each = (t.words + kThreads - 1) / kThreads, lane = threadIdx.x & 31;
+  int mine = 0;
+  for (int w = threadIdx.x * each; w < min(t.words, (int)(threadIdx.x + 1) * each); ++w)
+    mine += __popc(in_range(t, w, a.mask_id) & ~t.plain[w]);
+  int upto = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int v = __shfl_up_sync(0xffffffffu, upto, o);
+    if (lane >= o) upto += v;
+  }
+  if (lane == 31) s_first[threadIdx.x >> 5] = upto;
+  __syncthreads();
+  int before = lane < kWarps ? s_first[lane] : 0;
+  const int total = __reduce_add_sync(0xffffffffu, before);
+  before = __reduce_add_sync(0xffffffffu, lane < (int)(threadIdx.x >> 5) ? before : 0);
+  int at = before + upto - mine;
+  if (mine)
+    for (int w = threadIdx.x * each; w < min(t.words, (int)(threadIdx.x + 1) * each); ++w) {
+      unsigned bits = in_range(t, w, a.mask_id) & ~t.plain[w];
+      const unsigned with = t.biased[w];
+      if (at + __popc(bits) > kListed) {
+        if (bits) atomicMin(&s_cut, w);
+        break;
+      }
+      for (; bits; bits &= bits - 1) {
+        const int b = __ffs(bits) - 1, e = w * 32 + b;
+        unsigned place = 0u;
+        if ((with >> b) & 1u) place = (unsigned)min(find_bias(a, t, t.c0 + e) - t.bias_lo + 1, 0xffff);
+        t.list[at++] = (unsigned)e | place << 16;
+      }
+    }
+  __syncthreads();
+  t.cut = s_cut;
+  t.listed = total;
+  if (t.cut < t.words) {                                     // entries of the words before: count them again
+    int n = 0;
+    for (int w = lane; w < t.cut; w += 32) n += __popc(in_range(t, w, a.mask_id) & ~t.plain[w]);
+    t.listed = __reduce_add_sync(0xffffffffu, n);
+  }
 }
 
-// y of entry e (of the chunk), which some rule touches, from its logit.
-__device__ __forceinline__ float touched(const RulesArgs& a, const Table& t, int e, float z) {
+// y of entry e (of the chunk), which some rule touches, from its logit; place: where its first bias is, as listed.
+__device__ __forceinline__ float touched(const RulesArgs& a, const Table& t, int e, unsigned place, float z) {
   float y = z;
   if (a.ctx) {
     const unsigned c = t.count[e];
@@ -149,25 +199,55 @@ __device__ __forceinline__ float touched(const RulesArgs& a, const Table& t, int
       if (made) y = __fsub_rn(y, __fadd_rn(__fmul_rn(t.phi, (float)made), t.alpha));
     }
   }
-  if ((t.biased[e >> 5] >> (e & 31)) & 1u) {
+  if (place) {
     const int id = t.c0 + e;
-    int lo = t.bias_lo, hi = t.bias_hi;                      // the first bias of this id (ids ascend)
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (__ldg(a.bias_tok + mid) < id) lo = mid + 1;
-      else hi = mid;
-    }
-    for (; lo < t.bias_hi && __ldg(a.bias_tok + lo) == id; ++lo) y = __fadd_rn(y, __ldg(a.bias_val + lo));
+    for (int i = place < 0xffffu ? t.bias_lo + (int)place - 1 : find_bias(a, t, id); i < t.bias_hi && __ldg(a.bias_tok + i) == id; ++i)
+      y = __fadd_rn(y, __ldg(a.bias_val + i));
   }
   return y;
 }
 
-// The bits of E entries from entry p of the chunk on (p >= -E): words w and w + 1 of a row of bits.
+// Calls f(entry, place) for the touched entries that the mask (nullable) allows, each by one thread of the CTA.
+template <typename F>
+__device__ __forceinline__ void each_touched(const RulesArgs& a, const Table& t, const unsigned* mask, F f) {
+  for (int i = threadIdx.x; i < t.listed; i += kThreads) {
+    const unsigned r = t.list[i], e = r & 0xffffu;
+    if (!mask || ((__ldg(mask + (e >> 5)) >> (e & 31)) & 1u)) f((int)e, r >> 16);
+  }
+  for (int w = t.cut + threadIdx.x; w < t.words; w += kThreads) {
+    unsigned bits = in_range(t, w, a.mask_id) & ~t.plain[w];
+    if (mask && bits) bits &= __ldg(mask + w);
+    for (; bits; bits &= bits - 1) {
+      const int b = __ffs(bits) - 1;
+      f(w * 32 + b, (t.biased[w] >> b) & 1u ? 0xffffu : 0u);
+    }
+  }
+}
+
+// E bits from entry p of the chunk on, of a row of bits with a word behind the last.
 template <bool ALIGNED, typename F>
 __device__ __forceinline__ unsigned bits_at(int p, F word) {
   const int w = p >> 5;
   if (ALIGNED) return word(w) >> (p & 31);
   return __funnelshift_r(word(w), word(w + 1), p & 31);
+}
+
+// A row's chunk as vectors: entries [first, first + E nv) start at 16-byte boundaries; up to 2 E - 2 are left over.
+struct Cut {
+  int first, nv;
+};
+template <typename T, bool ALIGNED>
+__device__ __forceinline__ Cut cut_of(const T* z, int n) {
+  constexpr int E = Vec<T>::E;
+  const int shift = ALIGNED ? 0 : (int)(((uintptr_t)z & 15) / sizeof(T));
+  const int first = min(n, (E - shift) % E);
+  return Cut{first, (n - first) / E};
+}
+// The i-th entry left over, or -1.
+template <int E>
+__device__ __forceinline__ int left_over(const Cut& c, int n, int i) {
+  const int e = i < c.first ? i : c.first + c.nv * E + i - c.first;
+  return e < n ? e : -1;
 }
 
 __device__ __forceinline__ unsigned cluster_rank() {
@@ -176,13 +256,15 @@ __device__ __forceinline__ unsigned cluster_rank() {
   return r;
 }
 
-// Request and grammar mask of a row: false where an index is out of range.
-__device__ __forceinline__ bool row_of(const RulesArgs& a, int row, int* req, const unsigned** mask) {
-  *req = a.row_req ? __ldg(a.row_req + row) : row;
-  int m = a.allowed ? (a.row_mask ? __ldg(a.row_mask + row) : row) : -1;
-  const bool ok = *req >= -1 && *req < a.n_reqs && m >= -1 && m < a.n_masks;
-  *mask = ok && m >= 0 ? a.allowed + (long long)m * a.allowed_ld : nullptr;
-  return ok;
+// Request and grammar mask of a row, -1: none.
+struct Row {
+  int req, mask;
+};
+__device__ __forceinline__ Row row_of(const RulesArgs& a, int row) {
+  return Row{a.row_req ? __ldg(a.row_req + row) : row, a.allowed ? (a.row_mask ? __ldg(a.row_mask + row) : row) : -1};
+}
+__device__ __forceinline__ bool valid(const RulesArgs& a, const Row& r) {
+  return r.req >= -1 && r.req < a.n_reqs && r.mask >= -1 && r.mask < a.n_masks;
 }
 
 __device__ __forceinline__ unsigned ordered(float m) {       // unsigned order of floats (no NaN)
@@ -210,21 +292,28 @@ __device__ Table make_table(const RulesArgs& a, const Plan& pl, int chunk, unsig
   t.c0 = chunk * pl.chunk;
   t.n = max(0, min(pl.chunk, a.vocab - t.c0));
   t.words = pl.chunk / 32;
-  t.count = smem;
-  t.plain = smem + (a.ctx ? pl.chunk : 0) + 4;
+  t.list = smem;
+  t.count = smem + kListed;
+  t.plain = t.count + (a.ctx ? pl.chunk : 0);
   t.biased = t.plain + t.words + 4;
-  t.bias_lo = t.bias_hi = 0;
-  t.rho = 1.f; t.alpha = 0.f; t.phi = 0.f;
-  if (threadIdx.x < 4) {
-    t.plain[-1 - (int)threadIdx.x] = 0u;
-    t.plain[t.words + threadIdx.x] = 0u;
-  }
+  if (threadIdx.x < 4) t.plain[t.words + threadIdx.x] = 0u;
   return t;
+}
+
+// Joins one more value into a running (max, sum, argmax) whose entries come in ascending order.
+__device__ __forceinline__ void join_one(Part& p, float y, int at) {
+  if (y > p.m) {
+    p.s = p.s * weight(p.m, y) + 1.f;
+    p.m = y;
+    p.at = at;
+  } else if (y > -INFINITY || y != y) {
+    p.s += weight(y, p.m);
+  }
 }
 
 template <typename T, bool ALIGNED>
 __global__ void __launch_bounds__(kThreads, 2) k_rules_confidence(const RulesArgs a, const Plan pl, int* tok, float* conf) {
-  constexpr int E = Vec<T>::E, kBatch = 16 / E;              // 16 elements a thread at a time
+  constexpr int E = Vec<T>::E, kBatch = E == 4 ? 5 : 3;      // vectors a thread has in flight
   extern __shared__ __align__(16) unsigned smem[];
   __shared__ Part parts[kRowsAtOnce][kWarps];
   pdl_wait();
@@ -236,56 +325,54 @@ __global__ void __launch_bounds__(kThreads, 2) k_rules_confidence(const RulesArg
   Table t = make_table(a, pl, chunk, smem);
   const T* logits = static_cast<const T*>(a.logits);
   int cur = -2;
+  Row next = row_of(a, r0);
   for (int rb = r0; rb < r1; rb += kRowsAtOnce) {
     const int re = min(r1, rb + kRowsAtOnce);
     for (int row = rb; row < re; ++row) {
-      int req;
-      const unsigned* mask;
-      if (!row_of(a, row, &req, &mask)) {
+      const Row me = next;
+      if (row + 1 < r1) next = row_of(a, row + 1);
+      if (!valid(a, me)) {
         if (threadIdx.x == 0 && chunk == 0) raise(a);
         if (lane == 0) parts[row - rb][warp] = Part{-INFINITY, 0.f, 0x7fffffff};
         continue;
       }
-      if (req != cur) {
-        build_table(a, t, req);
-        cur = req;
-      }
       const T* z = logits + (long long)row * a.ld + t.c0;
-      const int shift = ALIGNED ? 0 : (int)(((uintptr_t)z & 15) / sizeof(T));
-      if (mask) mask += t.c0 >> 5;
+      if (me.req != cur) {
+        build_table(a, t, me.req);
+        cur = me.req;
+      }
+      const unsigned* mask = me.mask < 0 ? nullptr : a.allowed + me.mask * a.allowed_ld + (t.c0 >> 5);
+      const Cut c = cut_of<T, ALIGNED>(z, t.n);
       auto usable = [&](int w) -> unsigned {
         const unsigned p = t.plain[w];
         return mask && p ? p & __ldg(mask + w) : p;
       };
       float m = -INFINITY, s = 0.f;
       int best = 0;                                          // first entry of the vector that holds m
-      const int last = t.n + shift;                          // entries from the first vector's beginning
-      for (int i0 = threadIdx.x * E; i0 < last; i0 += kThreads * E * kBatch) {
+      for (int j0 = threadIdx.x; j0 < c.nv; j0 += kThreads * kBatch) {
+        unsigned bits[kBatch];
+        uint4 u[kBatch];
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) {
+          const int j = j0 + b * kThreads;
+          bits[b] = 0u;
+          u[b] = make_uint4(0u, 0u, 0u, 0u);
+          if (j < c.nv) u[b] = __ldcs(reinterpret_cast<const uint4*>(z + c.first) + j);
+          if (j < c.nv) bits[b] = bits_at<ALIGNED>(c.first + j * E, usable);
+        }
         float v[kBatch][E];
         float top = m;
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) {
-          const int p = i0 + b * kThreads * E - shift;
-          unsigned bits = 0u;
-          if (p + shift < last) bits = bits_at<ALIGNED>(p, usable);
-          if (p >= -t.c0 && t.c0 + p + E <= a.vocab && p + shift < last) {
-            const uint4 u = __ldcs(reinterpret_cast<const uint4*>(z + p));
-            widen(u, v[b], z);
+          widen(u[b], v[b], z);
 #pragma unroll
-            for (int e = 0; e < E; ++e) v[b][e] = (bits >> e) & 1u ? v[b][e] : -INFINITY;
-          } else {
-#pragma unroll
-            for (int e = 0; e < E; ++e) v[b][e] = (bits >> e) & 1u ? value(z + p + e) : -INFINITY;
-          }
-        }
-#pragma unroll
-        for (int b = 0; b < kBatch; ++b) {
+          for (int e = 0; e < E; ++e) v[b][e] = (bits[b] >> e) & 1u ? v[b][e] : -INFINITY;
           float vm = v[b][0];
 #pragma unroll
           for (int e = 1; e < E; ++e) vm = fmaxf(vm, v[b][e]);
           if (vm > top) {
             top = vm;
-            best = i0 + b * kThreads * E - shift;
+            best = c.first + (j0 + b * kThreads) * E;
           }
         }
         if (top > m) {
@@ -305,37 +392,27 @@ __global__ void __launch_bounds__(kThreads, 2) k_rules_confidence(const RulesArg
             for (int e = 0; e < E; ++e) s += __expf(v[b][e] - ref);
         }
       }
-      // the touched entries
-      float tm = -INFINITY, ts = 0.f;
-      int tat = 0x7fffffff;
-      for (int w = threadIdx.x; w < t.words; w += kThreads) {
-        unsigned bits = in_range(t, w, a.mask_id) & ~t.plain[w];
-        if (mask && bits) bits &= __ldg(mask + w);
-        while (bits) {
-          const int e = w * 32 + __ffs(bits) - 1;
-          bits &= bits - 1;
-          const float y = touched(a, t, e, value(z + e));
-          if (y > tm) {
-            ts = ts * weight(tm, y) + 1.f;
-            tm = y;
-            tat = t.c0 + e;
-          } else if (y > -INFINITY || y != y) {
-            ts += weight(y, tm);
-          }
-        }
+      Part one{-INFINITY, 0.f, 0x7fffffff};
+      if (threadIdx.x < 2 * E) {
+        const int e = left_over<E>(c, t.n, threadIdx.x);
+        if (e >= 0 && ((usable(e >> 5) >> (e & 31)) & 1u)) join_one(one, value(z + e), t.c0 + e);
       }
-      // warp's part: the lowest entry among the lanes that hold the maximum
-      const float top = unordered(__reduce_max_sync(0xffffffffu, ordered(fmaxf(m, tm))));
+      Part some{-INFINITY, 0.f, 0x7fffffff};
+      each_touched(a, t, mask, [&](int e, unsigned place) { join_one(some, touched(a, t, e, place, value(z + e)), t.c0 + e); });
+      // the warp's part: the lowest entry among the lanes that hold the maximum
+      const float top = unordered(__reduce_max_sync(0xffffffffu, ordered(fmaxf(m, fmaxf(one.m, some.m)))));
       unsigned at = 0x7fffffffu;
       if (m == top && top > -INFINITY) {
+#pragma unroll
         for (int e = E - 1; e >= 0; --e) {
           const int p = best + e;
-          if (p >= 0 && p < t.n && ((usable(p >> 5) >> (p & 31)) & 1u) && value(z + p) == top) at = (unsigned)(t.c0 + p);
+          if (((usable(p >> 5) >> (p & 31)) & 1u) && value(z + p) == top) at = (unsigned)(t.c0 + p);
         }
       }
-      if (tm == top) at = min(at, (unsigned)tat);
+      if (one.m == top) at = min(at, (unsigned)one.at);
+      if (some.m == top) at = min(at, (unsigned)some.at);
       at = __reduce_min_sync(0xffffffffu, at);
-      s = s * weight(m, top) + ts * weight(tm, top);
+      s = s * weight(m, top) + one.s * weight(one.m, top) + some.s * weight(some.m, top);
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
       if (lane == 0) parts[row - rb][warp] = Part{top, s, (int)at};
@@ -374,10 +451,24 @@ __global__ void __launch_bounds__(kThreads, 2) k_rules_confidence(const RulesArg
   }
 }
 
+__device__ __forceinline__ uint4 narrow(const float* v, const float*) {
+  return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+}
+__device__ __forceinline__ uint4 narrow(const float* v, const bf16*) {
+  unsigned w[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
+    w[k] = *reinterpret_cast<const unsigned*>(&h);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 // Stores y.  In place only entries that change are written: the touched ones and those that are not allowed.
 template <typename T, bool ALIGNED, bool INPLACE>
 __global__ void __launch_bounds__(kThreads, 2) k_logit_rules(const RulesArgs a, const Plan pl, T* out, long long out_ld) {
-  constexpr int E = Vec<T>::E;
+  constexpr int E = Vec<T>::E, kBatch = INPLACE ? 1 : 4;
+  constexpr unsigned kAll = (1u << E) - 1u;
   extern __shared__ __align__(16) unsigned smem[];
   pdl_wait();
   pdl_trigger();
@@ -385,78 +476,68 @@ __global__ void __launch_bounds__(kThreads, 2) k_logit_rules(const RulesArgs a, 
   const int r0 = (int)((long long)a.n_rows * span / pl.spans), r1 = (int)((long long)a.n_rows * (span + 1) / pl.spans);
   Table t = make_table(a, pl, chunk, smem);
   int cur = -2;
+  Row next = row_of(a, r0);
   for (int row = r0; row < r1; ++row) {
-    int req;
-    const unsigned* mask;
-    if (!row_of(a, row, &req, &mask)) {
+    const Row me = next;
+    if (row + 1 < r1) next = row_of(a, row + 1);
+    if (!valid(a, me)) {
       if (threadIdx.x == 0 && chunk == 0) raise(a);
       continue;
     }
-    if (req != cur) {
-      build_table(a, t, req);
-      cur = req;
-    }
     const T* z = static_cast<const T*>(a.logits) + (long long)row * a.ld + t.c0;
     T* y = out + (long long)row * out_ld + t.c0;
-    const int shift = ALIGNED ? 0 : (int)(((uintptr_t)z & 15) / sizeof(T));
-    if (mask) mask += t.c0 >> 5;
-    const int last = t.n + shift;
-    auto inside = [&](int w) -> unsigned { return w < 0 ? 0u : in_range(t, w, -1); };
-    auto plain = [&](int w) -> unsigned { return t.plain[w]; };
+    if (me.req != cur) {
+      build_table(a, t, me.req);
+      cur = me.req;
+    }
+    const unsigned* mask = me.mask < 0 ? nullptr : a.allowed + me.mask * a.allowed_ld + (t.c0 >> 5);
+    const Cut c = cut_of<T, ALIGNED>(z, t.n);
+    // bits of the entries that may stay, and of those that no other rule touches
     auto allow = [&](int w) -> unsigned {
-      if (w < 0 || w * 32 >= t.n) return 0u;
       const unsigned in = in_range(t, w, a.mask_id);
-      return mask ? in & __ldg(mask + w) : in;
+      return mask && in ? in & __ldg(mask + w) : in;
     };
-    for (int i = threadIdx.x * E; i < last; i += kThreads * E) {
-      const int p = i - shift;
-      const unsigned all = (1u << E) - 1u;
-      const unsigned own = bits_at<ALIGNED>(p, inside) & all;            // entries of this chunk
-      const unsigned keep = bits_at<ALIGNED>(p, allow) & own;            // entries with a finite chance
-      const unsigned calm = bits_at<ALIGNED>(p, plain) & keep;           // ... that no other rule touches
-      if (INPLACE && calm == own) continue;
-      const bool whole = own == all && ALIGNED;
-      float v[E];
-      if (!INPLACE || keep != calm) {
-        if (own == all) {
-          widen(__ldcs(reinterpret_cast<const uint4*>(z + p)), v, z);
-        } else {
+    auto plain = [&](int w) -> unsigned { return t.plain[w]; };
+    for (int j0 = threadIdx.x; j0 < c.nv; j0 += kThreads * kBatch) {
+      uint4 u[kBatch];
+      unsigned keep[kBatch], calm[kBatch];
 #pragma unroll
-          for (int e = 0; e < E; ++e) v[e] = (own >> e) & 1u ? value(z + p + e) : 0.f;
+      for (int b = 0; b < kBatch; ++b) {
+        const int j = j0 + b * kThreads;
+        keep[b] = calm[b] = 0u;
+        if (j < c.nv) {
+          if (!INPLACE) u[b] = __ldcs(reinterpret_cast<const uint4*>(z + c.first) + j);
+          keep[b] = bits_at<ALIGNED>(c.first + j * E, allow) & kAll;
+          calm[b] = bits_at<ALIGNED>(c.first + j * E, plain) & keep[b];
         }
       }
-      for (unsigned some = keep & ~calm; some; some &= some - 1) {
-        const int at = __ffs(some) - 1;
-        float x = 0.f;
 #pragma unroll
-        for (int e = 0; e < E; ++e) x = e == at ? v[e] : x;
-        x = touched(a, t, p + at, x);
+      for (int b = 0; b < kBatch; ++b) {
+        const int j = j0 + b * kThreads, p = c.first + j * E;
+        if (j >= c.nv) break;
+        const unsigned put_now = (INPLACE ? 0u : calm[b]) | (kAll & ~keep[b]);    // the others come below
+        float v[E];
+        if (!INPLACE) widen(u[b], v, z);
 #pragma unroll
-        for (int e = 0; e < E; ++e) v[e] = e == at ? x : v[e];
-      }
+        for (int e = 0; e < E; ++e) v[e] = !INPLACE && ((keep[b] >> e) & 1u) ? v[e] : -INFINITY;
+        if (put_now == kAll && (ALIGNED || INPLACE)) {
+          __stcs(reinterpret_cast<uint4*>(y + p), narrow(v, z));
+        } else if (put_now) {
 #pragma unroll
-      for (int e = 0; e < E; ++e)
-        if (!((keep >> e) & 1u)) v[e] = -INFINITY;
-      if (!INPLACE && whole) {
-        uint4 u;
-        if (sizeof(T) == 4) {
-          u = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
-        } else {
-          unsigned w[4];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const __nv_bfloat162 h = __floats2bfloat162_rn(v[(2 * k) % E], v[(2 * k + 1) % E]);
-            w[k] = *reinterpret_cast<const unsigned*>(&h);
-          }
-          u = make_uint4(w[0], w[1], w[2], w[3]);
+          for (int e = 0; e < E; ++e)
+            if ((put_now >> e) & 1u) put(y + p + e, v[e]);
         }
-        *reinterpret_cast<uint4*>(y + p) = u;
-      } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (((INPLACE ? own & ~calm : own) >> e) & 1u) put(y + p + e, v[e]);
       }
     }
+    if (threadIdx.x < 2 * E) {
+      const int e = left_over<E>(c, t.n, threadIdx.x);
+      if (e >= 0) {
+        const bool stays = (allow(e >> 5) >> (e & 31)) & 1u, alone = (t.plain[e >> 5] >> (e & 31)) & 1u;
+        if (!stays) put(y + e, -INFINITY);
+        else if (alone && !INPLACE) put(y + e, value(z + e));
+      }
+    }
+    each_touched(a, t, mask, [&](int e, unsigned place) { put(y + e, touched(a, t, e, place, value(z + e))); });
   }
 }
 
@@ -468,7 +549,7 @@ struct DevInfo {
 DevInfo g_dev[kMaxDevices];
 std::mutex g_mutex;
 
-constexpr int kMaxSmem = 208 * 1024;
+constexpr int kMaxSmem = 208 * 1024;         // the table of an eighth of the largest vocabulary
 
 template <typename T>
 using ConfKernel = void (*)(const RulesArgs, const Plan, int*, float*);
@@ -500,7 +581,7 @@ const DevInfo* dev_info() {
   return d;
 }
 
-size_t smem_of(const RulesArgs& a, int chunk) { return ((a.ctx ? (size_t)chunk : 0) + 2 * (size_t)(chunk / 32) + 16) * 4; }
+size_t smem_of(const RulesArgs& a, int chunk) { return (kListed + (a.ctx ? (size_t)chunk : 0) + 2 * (size_t)(chunk / 32) + 8) * 4; }
 
 Plan plan_of(const RulesArgs& a, int num_sms) {
   Plan pl;

@@ -16,42 +16,52 @@ namespace {
 constexpr int kUnit = 8;            // elements a thread loads and rounds at a time
 constexpr int kUnits = 4;           // units a thread keeps
 
-// The eight elements from element `at` of a row on; those at and behind K are zero.
+// Eight elements as they are stored; those at and behind K are zero.
+template <bool F32>
+struct Unit {
+  uint4 u[F32 ? 2 : 1];
+};
 template <bool F32, bool VEC>
-__device__ __forceinline__ void load_unit(const void* row, int at, int K, float* v) {
+__device__ __forceinline__ Unit<F32> load_unit(const void* row, int at, int K) {
+  Unit<F32> r;
   if (VEC && at + kUnit <= K) {
-    if (F32) {
-      const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(row) + at);
-      const float4 a = __ldg(p), b = __ldg(p + 1);
-      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-      v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-    } else {
-      const uint4 u = __ldg(reinterpret_cast<const uint4*>(static_cast<const bf16*>(row) + at));
-      const unsigned w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __uint_as_float(w[i] << 16);
-        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-      }
-    }
+    const uint4* p = reinterpret_cast<const uint4*>(static_cast<const char*>(row) + (size_t)at * (F32 ? 4 : 2));
+    r.u[0] = __ldg(p);
+    if (F32) r.u[F32 ? 1 : 0] = __ldg(p + 1);
   } else {
+    unsigned w[8];
 #pragma unroll
     for (int i = 0; i < kUnit; ++i) {
-      v[i] = 0.f;
+      w[i] = 0u;
       if (at + i < K)
-        v[i] = F32 ? __ldg(static_cast<const float*>(row) + at + i)
-                   : __bfloat162float(__ldg(static_cast<const bf16*>(row) + at + i));
+        w[i] = F32 ? __ldg(static_cast<const unsigned*>(row) + at + i) : __ldg(static_cast<const unsigned short*>(row) + at + i);
+    }
+    if (F32) {
+      r.u[0] = make_uint4(w[0], w[1], w[2], w[3]);
+      r.u[F32 ? 1 : 0] = make_uint4(w[4], w[5], w[6], w[7]);
+    } else {
+      r.u[0] = make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
     }
   }
+  return r;
+}
+template <bool F32>
+__device__ __forceinline__ void widen(const Unit<F32>& r, float* v) {
+  const unsigned w[8] = {r.u[0].x, r.u[0].y, r.u[0].z, r.u[0].w, r.u[F32 ? 1 : 0].x, r.u[F32 ? 1 : 0].y, r.u[F32 ? 1 : 0].z,
+                         r.u[F32 ? 1 : 0].w};
+#pragma unroll
+  for (int i = 0; i < kUnit; ++i)
+    v[i] = F32 ? __uint_as_float(w[i]) : __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
 }
 
-// v *= gain, and this unit's share of the sum of squares of v before that.
-__device__ __forceinline__ float apply_gain(const bf16* gain, int at, int K, float* v) {
-  float ss = 0.f;
+// This unit's elements times the gain, and its share of the sum of squares before that.
+template <bool F32>
+__device__ __forceinline__ float gained(const Unit<F32>& r, const bf16* gain, int at, int K, float* v) {
+  widen<F32>(r, v);
+  float ss = 0.f, g[kUnit];
 #pragma unroll
   for (int i = 0; i < kUnit; ++i) ss = fmaf(v[i], v[i], ss);
-  float g[kUnit];
-  load_unit<false, true>(gain, at, K, g);
+  widen<false>(load_unit<false, true>(gain, at, K), g);
 #pragma unroll
   for (int i = 0; i < kUnit; ++i) v[i] *= g[i];
   return ss;
@@ -98,6 +108,27 @@ __device__ __forceinline__ void store_unit(int8_t* row, int at, int K, uint2 c) 
   }
 }
 
+// The largest magnitude of a unit (joined with `top`), and its share of the sum of squares.
+template <bool F32, bool NORM>
+__device__ __forceinline__ unsigned largest(const Unit<F32>& r, const bf16* gain, int at, int K, unsigned top, float* ss) {
+  if (NORM) {
+    float v[kUnit];
+    *ss += gained<F32>(r, gain, at, K, v);
+#pragma unroll
+    for (int i = 0; i < kUnit; ++i) top = max(top, magnitude(v[i]));
+  } else if (F32) {
+    float v[kUnit];
+    widen<F32>(r, v);
+#pragma unroll
+    for (int i = 0; i < kUnit; ++i) top = max(top, magnitude(v[i]));
+  } else {                                                  // two to a word: the same order, in 16 bits
+    const unsigned w[4] = {r.u[0].x, r.u[0].y, r.u[0].z, r.u[0].w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = __vmaxu2(top, w[i] & 0x7fff7fffu);
+  }
+  return top;
+}
+
 template <bool F32, bool VEC, bool NORM, bool LONG>
 __global__ void __launch_bounds__(1024) k_quant_i8(const QuantI8Args a) {
   __shared__ unsigned s_max[32];
@@ -115,32 +146,25 @@ __global__ void __launch_bounds__(1024) k_quant_i8(const QuantI8Args a) {
   }
   const void* row = static_cast<const char*>(a.x) + from * a.ldx * (F32 ? 4 : 2);
   const int step = blockDim.x * kUnit;
-  float v[kUnits][kUnit];
+  Unit<F32> r[kUnits];
   unsigned top = 0;
   float ss = 0.f;
   if (!LONG) {
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
       const int at = threadIdx.x * kUnit + u * step;
-      if (at < a.K) load_unit<F32, VEC>(row, at, a.K, v[u]);
+      if (at < a.K) r[u] = load_unit<F32, VEC>(row, at, a.K);
     }
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
       const int at = threadIdx.x * kUnit + u * step;
-      if (at < a.K) {
-        if (NORM) ss += apply_gain(a.gain, at, a.K, v[u]);
-#pragma unroll
-        for (int i = 0; i < kUnit; ++i) top = max(top, magnitude(v[u][i]));
-      }
+      if (at < a.K) top = largest<F32, NORM>(r[u], a.gain, at, a.K, top, &ss);
     }
   } else {
-    for (int at = threadIdx.x * kUnit; at < a.K; at += step) {
-      load_unit<F32, VEC>(row, at, a.K, v[0]);
-      if (NORM) ss += apply_gain(a.gain, at, a.K, v[0]);
-#pragma unroll
-      for (int i = 0; i < kUnit; ++i) top = max(top, magnitude(v[0][i]));
-    }
+    for (int at = threadIdx.x * kUnit; at < a.K; at += step)
+      top = largest<F32, NORM>(load_unit<F32, VEC>(row, at, a.K), a.gain, at, a.K, top, &ss);
   }
+  if (!F32 && !NORM) top = max(top & 0xffffu, top >> 16) << 16;
   top = __reduce_max_sync(0xffffffffu, top);
   if (NORM) {
 #pragma unroll
@@ -161,25 +185,27 @@ __global__ void __launch_bounds__(1024) k_quant_i8(const QuantI8Args a) {
     }
   }
   // rounding is monotonic: the largest |gain x| times r is the largest |y|
-  const float r = NORM ? rsqrtf(ss / (float)a.K + a.eps) : 1.f;
-  const float big = NORM ? __uint_as_float(top) * r : __uint_as_float(top);
+  const float rms = NORM ? rsqrtf(ss / (float)a.K + a.eps) : 1.f;
+  const float big = NORM ? __uint_as_float(top) * rms : __uint_as_float(top);
   const bool real = top < 0x7f800000u && big < INFINITY;
   const float s = fmaxf(__fdiv_rn(big, 127.f), 0x1p-126f);
   const float inv = __frcp_rn(s);
   if (threadIdx.x == 0) a.scale[m] = real ? s : __uint_as_float(0x7fffffffu);
   int8_t* out = a.codes + (long long)m * a.ldc;
+  auto finish = [&](const Unit<F32>& u, int at) {
+    float v[kUnit];
+    if (NORM) gained<F32>(u, a.gain, at, a.K, v);
+    else widen<F32>(u, v);
+    store_unit(out, at, a.K, real ? round_unit<NORM>(v, rms, s, inv) : make_uint2(0u, 0u));
+  };
   if (!LONG) {
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
       const int at = threadIdx.x * kUnit + u * step;
-      if (at < a.K) store_unit(out, at, a.K, real ? round_unit<NORM>(v[u], r, s, inv) : make_uint2(0u, 0u));
+      if (at < a.K) finish(r[u], at);
     }
   } else {
-    for (int at = threadIdx.x * kUnit; at < a.K; at += step) {
-      load_unit<F32, VEC>(row, at, a.K, v[0]);
-      if (NORM) apply_gain(a.gain, at, a.K, v[0]);
-      store_unit(out, at, a.K, real ? round_unit<NORM>(v[0], r, s, inv) : make_uint2(0u, 0u));
-    }
+    for (int at = threadIdx.x * kUnit; at < a.K; at += step) finish(load_unit<F32, VEC>(row, at, a.K), at);
   }
 }
 
