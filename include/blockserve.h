@@ -437,7 +437,7 @@ int bs_op_gemm_i8(const void* A, long long lda, const float* a_scale, const void
  * that a program may fill them once and update their contents between calls.  NULL members are rules that do not apply.
  * Indices are checked on the device: what is out of range raises error_flag to 100 or more and is skipped, as said
  * below.  Calls allocate nothing, keep nothing, use no scratch and may be captured into graphs. */
-enum { BS_RULES_MAX_VOCAB = 360448 };
+enum { BS_RULES_MAX_VOCAB = 524288 };
 typedef struct {
   int vocab, n_reqs;
   int mask_id;               /* never chosen, never counted as context; -1: there is none */

@@ -692,7 +692,7 @@ def op_attention_kv8(q, k8, v8, k_scale, v_scale, cu_q, kv_base, vis, hq: int, m
 
 # ---- projections in 8-bit integers --------------------------------------------------------------------------------
 
-I8_MAX_K, RULES_MAX_VOCAB = 131071, 360448      # BS_I8_MAX_K, BS_RULES_MAX_VOCAB
+I8_MAX_K, RULES_MAX_VOCAB = 131071, 524288      # BS_I8_MAX_K, BS_RULES_MAX_VOCAB
 _I8 = torch.int8
 _TYPES = {torch.bfloat16: 0, torch.float32: 1}  # BS_BF16, BS_F32
 

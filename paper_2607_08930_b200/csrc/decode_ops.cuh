@@ -59,7 +59,7 @@ struct RulesArgs {
   const int* row_mask;    // nullable: row r has mask r
   int* error_flag;
 };
-constexpr int kRulesMaxVocab = 360448;
+constexpr int kRulesMaxVocab = 524288;
 cudaError_t launch_logit_rules(const RulesArgs& a, void* out, long long out_ld, cudaStream_t s);
 cudaError_t launch_rules_confidence(const RulesArgs& a, int* tok, float* conf, cudaStream_t s);
 

@@ -5,13 +5,15 @@
 // ones) and conf = exp(max - logsumexp) without storing it.
 //
 // Bound by memory: a row of logits is read once.  The rules touch few entries of a row (the context's tokens, the
-// biases), so a pass over all entries only looks up one bit an entry, and the touched ones are taken one by one.  A
-// vocabulary is cut into up to eight chunks; the CTA of a chunk keeps, for one request at a time, a count for every entry
-// of the chunk in shared memory (context tokens are counted by shared-memory atomics: integers, so their order does not
-// matter) and the bits of the entries that no rule but the grammar touches.  It walks the consecutive rows of its span
-// and builds the table anew when the request changes.  For the confidence the CTAs of a span are a cluster; every warp
-// leaves (max, sum, argmax) of its part of a row in shared memory, and these are joined in a fixed order over distributed
-// shared memory, so that one launch without scratch does.
+// biases), so the pass over all entries only looks up one bit an entry, and the touched ones are taken one by one from a
+// list.  A vocabulary is dealt in blocks of 512 entries to up to eight CTAs (in turn, because the frequent tokens of a
+// vocabulary have its low ids).  A CTA keeps a table of one request at a time in shared memory: the bits of the entries
+// that some rule touches, and a list of those entries with how often each was generated.  The context's tokens first set
+// their bits, a prefix sum over the words makes the bits places in the list, and the tokens are counted there
+// (shared-memory atomics: integers, so their order does not matter).  The CTA walks the consecutive rows of its span and
+// builds the table anew when the request changes.  For the confidence the CTAs of a span are a cluster; every warp
+// leaves (max, sum, argmax) of its part of a row in shared memory without waiting for the others, and the parts of up to
+// 32 rows are joined at a time, in a fixed order, over distributed shared memory: one launch without scratch.
 #include <math.h>
 
 #include <mutex>
@@ -23,12 +25,16 @@ namespace bs {
 
 namespace {
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kBlock = 512;                // entries dealt to a CTA at a time
+constexpr int kBlockWords = kBlock / 32;
 constexpr int kRowsAtOnce = 32;            // rows whose parts are kept before they are joined
+constexpr int kPerSm = 4;                  // CTAs of an SM
 constexpr int kMaxChunks = 8;
+constexpr int kListed = 4096;              // touched entries that are listed at a time
+constexpr int kTokens = 8;                 // context tokens a thread has in flight
 constexpr unsigned kInPrompt = 0x80000000u;
-
-constexpr int kListed = 4096;              // touched entries that a table lists (those beyond are found by their bits)
+constexpr float kLog2e = 1.4426950408889634f;
 
 struct Part {
   float m, s;
@@ -36,8 +42,9 @@ struct Part {
 };
 
 struct Plan {
-  int chunks;            // CTAs that share a row (a cluster for the confidence)
-  int chunk;             // entries of a chunk: a multiple of 32
+  int chunks, lg;        // CTAs that share a row (a cluster for the confidence): 1 << lg
+  int blocks;            // blocks of a CTA's share (the last may lie behind the vocabulary)
+  int listed;            // room in the list
   int spans;
 };
 
@@ -46,62 +53,123 @@ __device__ __forceinline__ float value(const bf16* p) { return __bfloat162float(
 __device__ __forceinline__ void put(float* p, float y) { *p = y; }
 __device__ __forceinline__ void put(bf16* p, float y) { *p = __float2bfloat16_rn(y); }
 
-// E elements of 16 bytes, as fp32.
-template <typename T>
-struct Vec {
-  static constexpr int E = 16 / sizeof(T);
-};
-__device__ __forceinline__ void widen(const uint4& u, float* v, const float*) {
-  v[0] = __uint_as_float(u.x); v[1] = __uint_as_float(u.y); v[2] = __uint_as_float(u.z); v[3] = __uint_as_float(u.w);
+__device__ __forceinline__ float exp2_fast(float x) {        // relative error 2^-22; results below 2^-126 are zero
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
 }
-__device__ __forceinline__ void widen(const uint4& u, float* v, const bf16*) {
-  const unsigned w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[2 * i] = __uint_as_float(w[i] << 16);
-    v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-  }
+// Loads that happen only if `on`, without a branch: a loop's loads then all leave before the first is waited for.
+__device__ __forceinline__ uint4 load4_if(const void* p, bool on, unsigned otherwise) {
+  uint4 u = make_uint4(otherwise, otherwise, otherwise, otherwise);
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %5, 0;\n\t@p ld.global.cs.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
+               : "+r"(u.x), "+r"(u.y), "+r"(u.z), "+r"(u.w) : "l"(p), "r"((unsigned)on));
+  return u;
+}
+__device__ __forceinline__ unsigned load1_if(const void* p, bool on, unsigned otherwise) {
+  unsigned u = otherwise;
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p ld.global.nc.u32 %0, [%1];\n\t}"
+               : "+r"(u) : "l"(p), "r"((unsigned)on));
+  return u;
+}
+__device__ __forceinline__ unsigned cluster_rank() {
+  unsigned r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_barrier() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// The table of one request's rules over the entries [c0, c0 + n) of a CTA.
+// ---- a request's table ---------------------------------------------------------------------------------------
+
+// Entry e of a CTA's share is token id_of(e).
 struct Table {
-  unsigned* plain;       // bit set: only the grammar decides about this entry; the word behind the last is zero
-  unsigned* biased;      // bit set: the request has a bias for this entry
-  unsigned* count;       // kInPrompt | times generated
-  unsigned* list;        // the touched entries in ascending order: entry | (1 + place of its first bias, or 0) << 16
-  int listed;            // how many of them
-  int cut;               // the touched entries of words from this one on are not listed
-  int c0, n, words;
-  int bias_lo, bias_hi;  // the request's biases (all of them)
+  unsigned* plain;       // bit set: only the grammar decides about this entry
+  unsigned* touched;     // bit set: some other rule does
+  unsigned short* place; // of a word's first touched entry among all of them
+  unsigned* list;        // touched entries in ascending order: entry | (1 + place of its first bias, or 0) << 16
+  unsigned* count;       // of a listed entry: kInPrompt | times generated
+  int total;             // touched entries
+  int begin, gen, end;   // the request's context
+  int bias_lo, bias_hi;  // its biases
+  int chunk, lg, words, vocab, mask_id;
   float rho, alpha, phi;
-};
 
-__device__ __forceinline__ unsigned in_range(const Table& t, int w, int mask_id) {
-  const int left = t.n - w * 32;
-  unsigned bits = left >= 32 ? 0xffffffffu : (left <= 0 ? 0u : (1u << left) - 1u);
-  const int m = mask_id - t.c0;
-  if (m >= 0 && (m >> 5) == w) bits &= ~(1u << (m & 31));
-  return bits;
-}
+  __device__ __forceinline__ int id_of(int e) const {
+    return ((((e >> 9) << lg) | chunk) << 9) | (e & (kBlock - 1));
+  }
+  __device__ __forceinline__ bool owns(int id) const { return ((id >> 9) & ((1 << lg) - 1)) == chunk; }
+  __device__ __forceinline__ int entry_of(int id) const { return ((id >> 9) >> lg) << 9 | (id & (kBlock - 1)); }
+  // the bits of word w that are entries of the vocabulary and not the mask id
+  __device__ __forceinline__ unsigned in_range(int w) const {
+    const int id = id_of(w * 32), left = vocab - id;
+    unsigned bits = left >= 32 ? 0xffffffffu : (left <= 0 ? 0u : (1u << left) - 1u);
+    if ((mask_id >> 5) == (id >> 5)) bits &= ~(1u << (mask_id & 31));
+    return bits;
+  }
+  // whether a rule for token id is this CTA's to keep
+  __device__ __forceinline__ bool takes(int id) const { return (unsigned)id < (unsigned)vocab && owns(id) && id != mask_id; }
+};
 
 __device__ void raise(const RulesArgs& a) {
   if (a.error_flag) atomicMax(a.error_flag, 100 + SITE_RULES);
 }
 
-// The place of the first bias of token id (ids ascend), bias_hi if there is none.
-__device__ __forceinline__ int find_bias(const RulesArgs& a, const Table& t, int id) {
-  int lo = t.bias_lo, hi = t.bias_hi;
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (__ldg(a.bias_tok + mid) < id) lo = mid + 1;
-    else hi = mid;
-  }
-  return lo;
+__device__ Table make_table(const RulesArgs& a, const Plan& pl, int chunk, unsigned* smem) {
+  Table t;
+  t.chunk = chunk; t.lg = pl.lg; t.vocab = a.vocab; t.mask_id = a.mask_id;
+  t.words = pl.blocks * kBlockWords;
+  t.list = smem;
+  t.count = t.list + pl.listed;
+  t.plain = t.count + pl.listed;
+  t.touched = t.plain + t.words;
+  t.place = reinterpret_cast<unsigned short*>(t.touched + t.words);
+  t.total = 0;
+  return t;
 }
 
-// All threads of the CTA; req < 0: no rules but the grammar.
-__device__ void build_table(const RulesArgs& a, Table& t, int req) {
-  __shared__ int s_first[kWarps + 1], s_cut;
+// Lists the touched entries from the `from`-th on, as many as there is room for.  All threads of the CTA.
+__device__ __forceinline__ void list_touched(const RulesArgs& a, const Table& t, const Plan& pl, int from) {
+  const int to = min(t.total, from + pl.listed);
+  for (int i = threadIdx.x; i < to - from; i += kThreads) t.count[i] = 0u;
+  for (int w = threadIdx.x; w < t.words; w += kThreads) {
+    unsigned bits = t.touched[w];
+    for (int at = t.place[w]; bits; bits &= bits - 1, ++at)
+      if (at >= from && at < to) t.list[at - from] = (unsigned)(w * 32 + __ffs(bits) - 1);
+  }
+  __syncthreads();
+  // the tokens of the context and of the biases, several in flight
+  auto place_of = [&](int id) {
+    const int e = t.entry_of(id);
+    return t.place[e >> 5] + __popc(t.touched[e >> 5] & ((1u << (e & 31)) - 1u)) - from;
+  };
+  for (int i0 = t.begin + threadIdx.x; i0 < t.end; i0 += kThreads * kTokens) {
+    int id[kTokens];
+#pragma unroll
+    for (int k = 0; k < kTokens; ++k) id[k] = (int)load1_if(a.ctx + i0 + k * kThreads, i0 + k * kThreads < t.end, 0xffffffffu);
+#pragma unroll
+    for (int k = 0; k < kTokens; ++k)
+      if (t.takes(id[k])) {
+        const int at = place_of(id[k]);
+        if (at >= 0 && at < to - from) {
+          if (i0 + k * kThreads >= t.gen) atomicAdd(t.count + at, 1u);
+          else atomicOr(t.count + at, kInPrompt);
+        }
+      }
+  }
+  for (int i = t.bias_lo + threadIdx.x; i < t.bias_hi; i += kThreads) {
+    const int id = __ldg(a.bias_tok + i);
+    if (t.takes(id) && (i == t.bias_lo || __ldg(a.bias_tok + i - 1) < id)) {
+      const int at = place_of(id);
+      if (at >= 0 && at < to - from) atomicOr(t.list + at, (unsigned)min(i - t.bias_lo + 1, 0xffff) << 16);
+    }
+  }
+  __syncthreads();
+}
+
+// The table of a request (req < 0: no rules but the grammar).  All threads of the CTA.
+__device__ __forceinline__ void build_table(const RulesArgs& a, Table& t, const Plan& pl, int req) {
+  __shared__ int s_first[kWarps];
   int begin = 0, gen = 0, end = 0, lo = 0, hi = 0;
   t.rho = 1.f; t.alpha = 0.f; t.phi = 0.f;
   if (req >= 0 && a.ctx) {
@@ -112,45 +180,46 @@ __device__ void build_table(const RulesArgs& a, Table& t, int req) {
   }
   if (req >= 0 && a.bias_at) { lo = __ldg(a.bias_at + req); hi = __ldg(a.bias_at + req + 1); }
   __syncthreads();                                           // the rows before are done with the table
-  for (int w = threadIdx.x; w < t.words; w += kThreads) {
-    t.plain[w] = in_range(t, w, a.mask_id);
-    t.biased[w] = 0u;
-  }
-  if (a.ctx)
-    for (int i = threadIdx.x * 4; i < t.words * 32; i += kThreads * 4) *reinterpret_cast<uint4*>(t.count + i) = make_uint4(0, 0, 0, 0);
-  if (threadIdx.x == 0) s_cut = t.words;
-  if (begin < 0 || gen < begin || end < gen || end > a.ctx_total || lo < 0 || hi < lo || hi > a.bias_total) {
-    if (threadIdx.x == 0 && t.c0 == 0) raise(a);
-    if (begin < 0 || gen < begin || end < gen || end > a.ctx_total) begin = gen = end = 0;
-    if (lo < 0 || hi < lo || hi > a.bias_total) lo = hi = 0;
-  }
-  t.bias_lo = lo; t.bias_hi = hi;
+  for (int w = threadIdx.x; w < t.words; w += kThreads) t.touched[w] = 0u;
+  const bool bad_ctx = begin < 0 || gen < begin || end < gen || end > a.ctx_total;
+  const bool bad_bias = lo < 0 || hi < lo || hi > a.bias_total;
+  if (bad_ctx) begin = gen = end = 0;
+  if (bad_bias) lo = hi = 0;
+  if ((bad_ctx || bad_bias) && threadIdx.x == 0 && t.chunk == 0) raise(a);
+  t.begin = begin; t.gen = gen; t.end = end; t.bias_lo = lo; t.bias_hi = hi;
   __syncthreads();
-  for (int i = begin + threadIdx.x; i < end; i += kThreads) {
-    const int id = __ldg(a.ctx + i), e = id - t.c0;
-    if ((unsigned)id >= (unsigned)a.vocab) {
-      if (t.c0 == 0) raise(a);
-    } else if (e >= 0 && e < t.n && id != a.mask_id) {
-      if (i >= gen) atomicAdd(t.count + e, 1u);
-      else atomicOr(t.count + e, kInPrompt);
-      atomicAnd(t.plain + (e >> 5), ~(1u << (e & 31)));
-    }
+  bool bad = false;
+  auto touch = [&](int id, bool there) {
+    const int e = t.entry_of(id);
+    if (t.takes(id)) atomicOr(t.touched + (e >> 5), 1u << (e & 31));
+    bad = bad || (there && (unsigned)id >= (unsigned)t.vocab);
+  };
+  // (a thread's first biases are fetched along with the first tokens)
+  int b_id = (int)load1_if(a.bias_tok + lo + threadIdx.x, lo + (int)threadIdx.x < hi, 0xffffffffu);
+  int b_before = (int)load1_if(a.bias_tok + lo + threadIdx.x - 1, threadIdx.x > 0 && lo + (int)threadIdx.x < hi, 0xffffffffu);
+  for (int i0 = begin + threadIdx.x; i0 < end; i0 += kThreads * kTokens) {
+    int id[kTokens];
+#pragma unroll
+    for (int k = 0; k < kTokens; ++k) id[k] = (int)load1_if(a.ctx + i0 + k * kThreads, i0 + k * kThreads < end, 0xffffffffu);
+#pragma unroll
+    for (int k = 0; k < kTokens; ++k) touch(id[k], i0 + k * kThreads < end);
   }
   for (int i = lo + threadIdx.x; i < hi; i += kThreads) {
-    const int id = __ldg(a.bias_tok + i), e = id - t.c0;
-    if ((unsigned)id >= (unsigned)a.vocab || (i > lo && __ldg(a.bias_tok + i - 1) > id)) {
-      if (t.c0 == 0) raise(a);
-    } else if (e >= 0 && e < t.n && id != a.mask_id) {
-      atomicOr(t.biased + (e >> 5), 1u << (e & 31));
-      atomicAnd(t.plain + (e >> 5), ~(1u << (e & 31)));
-    }
+    touch(b_id, true);
+    bad = bad || b_before > b_id;
+    b_id = (int)load1_if(a.bias_tok + i + kThreads, i + kThreads < hi, 0xffffffffu);
+    b_before = (int)load1_if(a.bias_tok + i + kThreads - 1, i + kThreads < hi, 0xffffffffu);
   }
+  if (bad && t.chunk == 0) raise(a);
   __syncthreads();
-  // list the touched entries in order: thread i takes `each` words
   const int each = (t.words + kThreads - 1) / kThreads, lane = threadIdx.x & 31;
+  const int w0 = threadIdx.x * each, w1 = min(t.words, w0 + each);
   int mine = 0;
-  for (int w = threadIdx.x * each; w < min(t.words, (int)(threadIdx.x + 1) * each); ++w)
-    mine += __popc(in_range(t, w, a.mask_id) & ~t.plain[w]);
+  for (int w = w0; w < w1; ++w) {
+    const unsigned bits = t.touched[w];
+    t.plain[w] = t.in_range(w) & ~bits;
+    mine += __popc(bits);
+  }
   int upto = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -159,102 +228,58 @@ __device__ void build_table(const RulesArgs& a, Table& t, int req) {
   }
   if (lane == 31) s_first[threadIdx.x >> 5] = upto;
   __syncthreads();
-  int before = lane < kWarps ? s_first[lane] : 0;
-  const int total = __reduce_add_sync(0xffffffffu, before);
-  before = __reduce_add_sync(0xffffffffu, lane < (int)(threadIdx.x >> 5) ? before : 0);
-  int at = before + upto - mine;
-  if (mine)
-    for (int w = threadIdx.x * each; w < min(t.words, (int)(threadIdx.x + 1) * each); ++w) {
-      unsigned bits = in_range(t, w, a.mask_id) & ~t.plain[w];
-      const unsigned with = t.biased[w];
-      if (at + __popc(bits) > kListed) {
-        if (bits) atomicMin(&s_cut, w);
-        break;
-      }
-      for (; bits; bits &= bits - 1) {
-        const int b = __ffs(bits) - 1, e = w * 32 + b;
-        unsigned place = 0u;
-        if ((with >> b) & 1u) place = (unsigned)min(find_bias(a, t, t.c0 + e) - t.bias_lo + 1, 0xffff);
-        t.list[at++] = (unsigned)e | place << 16;
-      }
-    }
-  __syncthreads();
-  t.cut = s_cut;
-  t.listed = total;
-  if (t.cut < t.words) {                                     // entries of the words before: count them again
-    int n = 0;
-    for (int w = lane; w < t.cut; w += 32) n += __popc(in_range(t, w, a.mask_id) & ~t.plain[w]);
-    t.listed = __reduce_add_sync(0xffffffffu, n);
+  const int sum = lane < kWarps ? s_first[lane] : 0;
+  t.total = __reduce_add_sync(0xffffffffu, sum);
+  int at = __reduce_add_sync(0xffffffffu, lane < (int)(threadIdx.x >> 5) ? sum : 0) + upto - mine;
+  for (int w = w0; w < w1; ++w) {
+    t.place[w] = (unsigned short)at;
+    at += __popc(t.touched[w]);
   }
+  __syncthreads();
+  if (t.total > 0 && t.total <= pl.listed) list_touched(a, t, pl, 0);
 }
 
-// y of entry e (of the chunk), which some rule touches, from its logit; place: where its first bias is, as listed.
-__device__ __forceinline__ float touched(const RulesArgs& a, const Table& t, int e, unsigned place, float z) {
+// y of the i-th listed entry from its logit.
+__device__ __forceinline__ float ruled(const RulesArgs& a, const Table& t, int i, float z) {
   float y = z;
-  if (a.ctx) {
-    const unsigned c = t.count[e];
-    if (c) {
-      y = y > 0.f ? __fdiv_rn(y, t.rho) : __fmul_rn(y, t.rho);
-      const unsigned made = c & ~kInPrompt;
-      if (made) y = __fsub_rn(y, __fadd_rn(__fmul_rn(t.phi, (float)made), t.alpha));
-    }
+  const unsigned c = t.count[i], place = t.list[i] >> 16;
+  if (c) {
+    y = y > 0.f ? __fdiv_rn(y, t.rho) : __fmul_rn(y, t.rho);
+    const unsigned made = c & ~kInPrompt;
+    if (made) y = __fsub_rn(y, __fadd_rn(__fmul_rn(t.phi, (float)made), t.alpha));
   }
   if (place) {
-    const int id = t.c0 + e;
-    for (int i = place < 0xffffu ? t.bias_lo + (int)place - 1 : find_bias(a, t, id); i < t.bias_hi && __ldg(a.bias_tok + i) == id; ++i)
-      y = __fadd_rn(y, __ldg(a.bias_val + i));
+    const int id = t.id_of((int)(t.list[i] & 0xffffu));
+    int k = t.bias_lo + (int)place - 1;
+    if (place == 0xffffu)                                    // or behind that: ids ascend
+      for (int hi = t.bias_hi; k < hi;) {
+        const int mid = (k + hi) >> 1;
+        if (__ldg(a.bias_tok + mid) < id) k = mid + 1;
+        else hi = mid;
+      }
+    for (; k < t.bias_hi && __ldg(a.bias_tok + k) == id; ++k) y = __fadd_rn(y, __ldg(a.bias_val + k));
   }
   return y;
 }
 
-// Calls f(entry, place) for the touched entries that the mask (nullable) allows, each by one thread of the CTA.
+// Calls f(i, entry) for the touched entries that the mask (nullable) allows, listed as the i-th, each by one thread of the
+// CTA.  More of them than there is room for are listed in turns, anew for every row.
 template <typename F>
-__device__ __forceinline__ void each_touched(const RulesArgs& a, const Table& t, const unsigned* mask, F f) {
-  for (int i = threadIdx.x; i < t.listed; i += kThreads) {
-    const unsigned r = t.list[i], e = r & 0xffffu;
-    if (!mask || ((__ldg(mask + (e >> 5)) >> (e & 31)) & 1u)) f((int)e, r >> 16);
-  }
-  for (int w = t.cut + threadIdx.x; w < t.words; w += kThreads) {
-    unsigned bits = in_range(t, w, a.mask_id) & ~t.plain[w];
-    if (mask && bits) bits &= __ldg(mask + w);
-    for (; bits; bits &= bits - 1) {
-      const int b = __ffs(bits) - 1;
-      f(w * 32 + b, (t.biased[w] >> b) & 1u ? 0xffffu : 0u);
+__device__ __forceinline__ void each_touched(const RulesArgs& a, const Table& t, const Plan& pl, const unsigned* mask, F f) {
+  for (int from = 0; from < t.total; from += pl.listed) {
+    if (t.total > pl.listed) {
+      __syncthreads();
+      list_touched(a, t, pl, from);
+    }
+    const int n = min(pl.listed, t.total - from);
+    for (int i = threadIdx.x; i < n; i += kThreads) {
+      const int e = (int)(t.list[i] & 0xffffu), id = t.id_of(e);
+      if (!mask || ((__ldg(mask + (id >> 5)) >> (id & 31)) & 1u)) f(i, id);
     }
   }
 }
 
-// E bits from entry p of the chunk on, of a row of bits with a word behind the last.
-template <bool ALIGNED, typename F>
-__device__ __forceinline__ unsigned bits_at(int p, F word) {
-  const int w = p >> 5;
-  if (ALIGNED) return word(w) >> (p & 31);
-  return __funnelshift_r(word(w), word(w + 1), p & 31);
-}
-
-// A row's chunk as vectors: entries [first, first + E nv) start at 16-byte boundaries; up to 2 E - 2 are left over.
-struct Cut {
-  int first, nv;
-};
-template <typename T, bool ALIGNED>
-__device__ __forceinline__ Cut cut_of(const T* z, int n) {
-  constexpr int E = Vec<T>::E;
-  const int shift = ALIGNED ? 0 : (int)(((uintptr_t)z & 15) / sizeof(T));
-  const int first = min(n, (E - shift) % E);
-  return Cut{first, (n - first) / E};
-}
-// The i-th entry left over, or -1.
-template <int E>
-__device__ __forceinline__ int left_over(const Cut& c, int n, int i) {
-  const int e = i < c.first ? i : c.first + c.nv * E + i - c.first;
-  return e < n ? e : -1;
-}
-
-__device__ __forceinline__ unsigned cluster_rank() {
-  unsigned r;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
+// ---- rows ----------------------------------------------------------------------------------------------------
 
 // Request and grammar mask of a row, -1: none.
 struct Row {
@@ -267,6 +292,42 @@ __device__ __forceinline__ bool valid(const RulesArgs& a, const Row& r) {
   return r.req >= -1 && r.req < a.n_reqs && r.mask >= -1 && r.mask < a.n_masks;
 }
 
+// A block of a row as vectors of 16 bytes.  Rows at 16-byte boundaries: all of it.  Others: kPer vectors from entry
+// `first` of the block on, and E entries (before and behind) one by one.  Vectors that do not end within the vocabulary
+// are taken one by one, too.
+template <typename T, bool ALIGNED>
+struct Walk {
+  static constexpr int E = 16 / sizeof(T), kPer = kBlock / E - (ALIGNED ? 0 : 1);
+  int first;
+  __device__ __forceinline__ explicit Walk(const T* row)
+      : first(ALIGNED ? 0 : (int)((E - (((uintptr_t)row & 15) / sizeof(T))) % E)) {}
+  __device__ __forceinline__ int vectors(const Plan& pl) const { return pl.blocks * kPer; }
+  // first entry of vector j of the CTA's share
+  __device__ __forceinline__ int entry(int j) const { return ALIGNED ? j * E : j / kPer * kBlock + first + j % kPer * E; }
+  // entry i of those taken one by one, -1: none (i < singles)
+  __device__ __forceinline__ int singles(const Plan& pl) const { return ALIGNED ? E : (pl.blocks + 1) * E; }
+  __device__ __forceinline__ int single(const Plan& pl, const Table& t, int i) const {
+    int e;
+    if (i < E) {                                             // the end of the vocabulary, where it is in a vector's middle
+      const int last = (t.vocab - 1) & ~(kBlock - 1);        // the block that holds it
+      const int begin = last + first, id = begin + (t.vocab - begin) / E * E + i;
+      if (t.vocab < begin || !t.owns(last) || id >= t.vocab || id - last >= first + kPer * E) return -1;
+      return t.entry_of(id);
+    }
+    const int k = i % E;
+    e = (i / E - 1) * kBlock + (k < first ? k : kPer * E + k);
+    return t.id_of(e) < t.vocab ? e : -1;
+  }
+};
+
+// E bits (at least) from entry e on, of the CTA's words.
+template <int E, bool ALIGNED, typename F>
+__device__ __forceinline__ unsigned bits_at(int e, F word) {
+  const int w = e >> 5;
+  if (ALIGNED) return word(w) >> (e & 31);
+  return __funnelshift_r(word(w), (e & 31) > 32 - E ? word(w + 1) : 0u, e & 31);
+}
+
 __device__ __forceinline__ unsigned ordered(float m) {       // unsigned order of floats (no NaN)
   const unsigned u = __float_as_uint(m);
   return u ^ ((unsigned)((int)u >> 31) | 0x80000000u);
@@ -275,30 +336,7 @@ __device__ __forceinline__ float unordered(unsigned u) {
   return __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u);
 }
 // exp(m - top) of a part's maximum, 1 where they are equal (infinities too).
-__device__ __forceinline__ float weight(float m, float top) { return m == top ? 1.f : __expf(m - top); }
-
-// Joins (m, s, at) over the lanes of a warp; at = lowest index among the parts that hold the maximum.
-__device__ __forceinline__ Part join_lanes(Part p) {
-  const float top = unordered(__reduce_max_sync(0xffffffffu, ordered(p.m)));
-  float s = p.s * weight(p.m, top);
-  const unsigned at = __reduce_min_sync(0xffffffffu, p.m == top ? (unsigned)p.at : 0x7fffffffu);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-  return Part{top, s, (int)at};
-}
-
-__device__ Table make_table(const RulesArgs& a, const Plan& pl, int chunk, unsigned* smem) {
-  Table t;
-  t.c0 = chunk * pl.chunk;
-  t.n = max(0, min(pl.chunk, a.vocab - t.c0));
-  t.words = pl.chunk / 32;
-  t.list = smem;
-  t.count = smem + kListed;
-  t.plain = t.count + (a.ctx ? pl.chunk : 0);
-  t.biased = t.plain + t.words + 4;
-  if (threadIdx.x < 4) t.plain[t.words + threadIdx.x] = 0u;
-  return t;
-}
+__device__ __forceinline__ float weight(float m, float top) { return m == top ? 1.f : exp2_fast((m - top) * kLog2e); }
 
 // Joins one more value into a running (max, sum, argmax) whose entries come in ascending order.
 __device__ __forceinline__ void join_one(Part& p, float y, int at) {
@@ -311,11 +349,79 @@ __device__ __forceinline__ void join_one(Part& p, float y, int at) {
   }
 }
 
+// ---- vectors -------------------------------------------------------------------------------------------------
+
+template <typename T>
+constexpr unsigned kLeast = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;     // a word of -inf
+
+// Entries without their bit become -inf.
+template <typename T>
+__device__ __forceinline__ uint4 only(uint4 u, unsigned bits) {
+  unsigned w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (sizeof(T) == 4) {
+      w[i] = (bits >> i) & 1u ? w[i] : kLeast<T>;
+    } else {
+      const unsigned keep = ((bits >> (2 * i)) & 1u ? 0x0000ffffu : 0u) | ((bits >> (2 * i + 1)) & 1u ? 0xffff0000u : 0u);
+      w[i] = (w[i] & keep) | (kLeast<T> & ~keep);
+    }
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// The largest entry (NaN are passed over).
+__device__ __forceinline__ float largest(const uint4& u, const float*) {
+  return fmaxf(fmaxf(__uint_as_float(u.x), __uint_as_float(u.y)), fmaxf(__uint_as_float(u.z), __uint_as_float(u.w)));
+}
+__device__ __forceinline__ float largest(const uint4& u, const bf16*) {
+  const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&u);
+  const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+  return fmaxf(__low2float(m), __high2float(m));
+}
+__device__ __forceinline__ void widen(const uint4& u, float* v, const float*) {
+  v[0] = __uint_as_float(u.x); v[1] = __uint_as_float(u.y); v[2] = __uint_as_float(u.z); v[3] = __uint_as_float(u.w);
+}
+__device__ __forceinline__ void widen(const uint4& u, float* v, const bf16*) {
+  const unsigned w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = __uint_as_float(w[i] << 16);
+    v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+}
+// s (two partial sums) += exp(v - ref), two entries an instruction up to the exponential.  The difference comes first: one
+// product v log2(e) - ref log2(e) would leave the rounding of ref log2(e), common to all terms, in the sum.
+template <int E>
+__device__ __forceinline__ void add_exps(const float* v, unsigned long long minus_ref, unsigned long long log2e,
+                                         unsigned long long& s) {
+#pragma unroll
+  for (int e = 0; e < E; e += 2) {
+    unsigned long long x;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(v[e]), "f"(v[e + 1]));
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(x) : "l"(x), "l"(minus_ref));
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(x) : "l"(x), "l"(log2e));
+    float a, b;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x));
+    asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(exp2_fast(a)), "f"(exp2_fast(b)));
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(s) : "l"(s), "l"(x));
+  }
+}
+__device__ __forceinline__ unsigned long long pair_of(float x) {
+  unsigned long long r;
+  asm("mov.b64 %0, {%1, %1};" : "=l"(r) : "f"(x));
+  return r;
+}
+
+// ---- the confidence ------------------------------------------------------------------------------------------
+
 template <typename T, bool ALIGNED>
-__global__ void __launch_bounds__(kThreads, 2) k_rules_confidence(const RulesArgs a, const Plan pl, int* tok, float* conf) {
-  constexpr int E = Vec<T>::E, kBatch = E == 4 ? 5 : 3;      // vectors a thread has in flight
+__global__ void __launch_bounds__(kThreads, kPerSm) k_rules_confidence(const RulesArgs a, const Plan pl, int* tok, float* conf) {
+  using W = Walk<T, ALIGNED>;
+  constexpr int E = W::E, kBatch = E == 4 ? 5 : 4;           // vectors a thread has in flight
+  constexpr unsigned kAll = (1u << E) - 1u;
   extern __shared__ __align__(16) unsigned smem[];
   __shared__ Part parts[kRowsAtOnce][kWarps];
+  __shared__ unsigned s_top[kRowsAtOnce];                    // the largest maximum that a warp has left so far, ordered
   pdl_wait();
   pdl_trigger();
   const int chunk = pl.chunks > 1 ? (int)cluster_rank() : 0;
@@ -323,11 +429,13 @@ __global__ void __launch_bounds__(kThreads, 2) k_rules_confidence(const RulesArg
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int r0 = (int)((long long)a.n_rows * span / pl.spans), r1 = (int)((long long)a.n_rows * (span + 1) / pl.spans);
   Table t = make_table(a, pl, chunk, smem);
-  const T* logits = static_cast<const T*>(a.logits);
+  const unsigned long long log2e = pair_of(kLog2e);
   int cur = -2;
   Row next = row_of(a, r0);
   for (int rb = r0; rb < r1; rb += kRowsAtOnce) {
     const int re = min(r1, rb + kRowsAtOnce);
+    if (threadIdx.x < kRowsAtOnce) s_top[threadIdx.x] = 0u;
+    __syncthreads();
     for (int row = rb; row < re; ++row) {
       const Row me = next;
       if (row + 1 < r1) next = row_of(a, row + 1);
@@ -336,89 +444,114 @@ __global__ void __launch_bounds__(kThreads, 2) k_rules_confidence(const RulesArg
         if (lane == 0) parts[row - rb][warp] = Part{-INFINITY, 0.f, 0x7fffffff};
         continue;
       }
-      const T* z = logits + (long long)row * a.ld + t.c0;
+      const T* z = static_cast<const T*>(a.logits) + (long long)row * a.ld;
       if (me.req != cur) {
-        build_table(a, t, me.req);
+        build_table(a, t, pl, me.req);
         cur = me.req;
       }
-      const unsigned* mask = me.mask < 0 ? nullptr : a.allowed + me.mask * a.allowed_ld + (t.c0 >> 5);
-      const Cut c = cut_of<T, ALIGNED>(z, t.n);
+      const unsigned* mask = me.mask < 0 ? nullptr : a.allowed + me.mask * a.allowed_ld;
+      const W walk(z);
       auto usable = [&](int w) -> unsigned {
         const unsigned p = t.plain[w];
-        return mask && p ? p & __ldg(mask + w) : p;
+        return p & load1_if(mask + (t.id_of(w * 32) >> 5), mask && p, 0xffffffffu);
       };
-      float m = -INFINITY, s = 0.f;
+      float m = -INFINITY;
+      unsigned long long s2 = 0ull;
       int best = 0;                                          // first entry of the vector that holds m
-      for (int j0 = threadIdx.x; j0 < c.nv; j0 += kThreads * kBatch) {
-        unsigned bits[kBatch];
+      const int nv = walk.vectors(pl);
+      for (int j0 = threadIdx.x; j0 < nv; j0 += kThreads * kBatch) {
+        unsigned bits[kBatch], every = kAll;
         uint4 u[kBatch];
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) {
-          const int j = j0 + b * kThreads;
-          bits[b] = 0u;
-          u[b] = make_uint4(0u, 0u, 0u, 0u);
-          if (j < c.nv) u[b] = __ldcs(reinterpret_cast<const uint4*>(z + c.first) + j);
-          if (j < c.nv) bits[b] = bits_at<ALIGNED>(c.first + j * E, usable);
+          const int e = walk.entry(min(j0 + b * kThreads, nv - 1)), id = t.id_of(e);
+          const bool there = j0 + b * kThreads < nv && id + E <= t.vocab;
+          u[b] = load4_if(z + id, there, kLeast<T>);         // (what is not there is -inf)
+          bits[b] = bits_at<E, ALIGNED>(e, usable) | (there ? 0u : kAll);
         }
-        float v[kBatch][E];
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) every &= bits[b];
+        if ((every & kAll) != kAll) {
+#pragma unroll
+          for (int b = 0; b < kBatch; ++b) u[b] = only<T>(u[b], bits[b]);
+        }
         float top = m;
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) {
-          widen(u[b], v[b], z);
-#pragma unroll
-          for (int e = 0; e < E; ++e) v[b][e] = (bits[b] >> e) & 1u ? v[b][e] : -INFINITY;
-          float vm = v[b][0];
-#pragma unroll
-          for (int e = 1; e < E; ++e) vm = fmaxf(vm, v[b][e]);
+          const float vm = largest(u[b], z);
           if (vm > top) {
             top = vm;
-            best = c.first + (j0 + b * kThreads) * E;
+            best = walk.entry(j0 + b * kThreads);
           }
         }
         if (top > m) {
-          s *= weight(m, top);
+          const unsigned long long w = pair_of(weight(m, top));
+          asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(s2) : "l"(s2), "l"(w));
           m = top;
         }
-        if (m == INFINITY) {
+        if (m == INFINITY) {                                 // k of them share the row
+          float n = 0.f;
 #pragma unroll
-          for (int b = 0; b < kBatch; ++b)
+          for (int b = 0; b < kBatch; ++b) {
+            float v[E];
+            widen(u[b], v, z);
 #pragma unroll
-            for (int e = 0; e < E; ++e) s += v[b][e] == INFINITY ? 1.f : (v[b][e] == v[b][e] ? 0.f : v[b][e]);
+            for (int e = 0; e < E; ++e) n += v[e] == INFINITY ? 1.f : (v[e] == v[e] ? 0.f : v[e]);
+          }
+          unsigned long long x;
+          asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(n), "f"(0.f));
+          asm("add.rn.f32x2 %0, %1, %2;" : "=l"(s2) : "l"(s2), "l"(x));
         } else {
-          const float ref = m > -INFINITY ? m : 0.f;
+          const unsigned long long minus = pair_of(m > -INFINITY ? -m : 0.f);
 #pragma unroll
-          for (int b = 0; b < kBatch; ++b)
-#pragma unroll
-            for (int e = 0; e < E; ++e) s += __expf(v[b][e] - ref);
+          for (int b = 0; b < kBatch; ++b) {
+            float v[E];
+            widen(u[b], v, z);
+            add_exps<E>(v, minus, log2e, s2);
+          }
         }
       }
-      Part one{-INFINITY, 0.f, 0x7fffffff};
-      if (threadIdx.x < 2 * E) {
-        const int e = left_over<E>(c, t.n, threadIdx.x);
-        if (e >= 0 && ((usable(e >> 5) >> (e & 31)) & 1u)) join_one(one, value(z + e), t.c0 + e);
-      }
-      Part some{-INFINITY, 0.f, 0x7fffffff};
-      each_touched(a, t, mask, [&](int e, unsigned place) { join_one(some, touched(a, t, e, place, value(z + e)), t.c0 + e); });
-      // the warp's part: the lowest entry among the lanes that hold the maximum
-      const float top = unordered(__reduce_max_sync(0xffffffffu, ordered(fmaxf(m, fmaxf(one.m, some.m)))));
-      unsigned at = 0x7fffffffu;
-      if (m == top && top > -INFINITY) {
-#pragma unroll
-        for (int e = E - 1; e >= 0; --e) {
-          const int p = best + e;
-          if (((usable(p >> 5) >> (p & 31)) & 1u) && value(z + p) == top) at = (unsigned)(t.c0 + p);
+      float s, s_odd;
+      asm("mov.b64 {%0, %1}, %2;" : "=f"(s), "=f"(s_odd) : "l"(s2));
+      s += s_odd;
+      Part one{-INFINITY, 0.f, 0x7fffffff};                  // entries beside the vectors
+      for (int i = threadIdx.x; i < walk.singles(pl); i += kThreads) {
+        const int e = walk.single(pl, t, i);
+        if (e >= 0 && ((usable(e >> 5) >> (e & 31)) & 1u)) {
+          const int id = t.id_of(e);
+          const float y = value(z + id);
+          // (the end of the vocabulary comes before the blocks' ends here: equal values keep the lower entry)
+          if (y == one.m) one.at = min(one.at, id);
+          join_one(one, y, id);
         }
       }
-      if (one.m == top) at = min(at, (unsigned)one.at);
-      if (some.m == top) at = min(at, (unsigned)some.at);
-      at = __reduce_min_sync(0xffffffffu, at);
+      Part some{-INFINITY, 0.f, 0x7fffffff};                 // the touched entries
+      each_touched(a, t, pl, mask, [&](int i, int id) { join_one(some, ruled(a, t, i, value(z + id)), id); });
+      // the warp's part: the lowest entry among the lanes that hold the maximum (where no warp has left a larger one)
+      const unsigned highest = __reduce_max_sync(0xffffffffu, ordered(fmaxf(m, fmaxf(one.m, some.m))));
+      const float top = unordered(highest);
       s = s * weight(m, top) + one.s * weight(one.m, top) + some.s * weight(some.m, top);
+      unsigned before = 0u;
+      if (lane == 0) before = atomicMax(&s_top[row - rb], highest);
+      unsigned at = 0x7fffffffu;
+      if (__shfl_sync(0xffffffffu, before, 0) <= highest && top > -INFINITY) {
+        if (m == top) {
+          const int id = t.id_of(best);
+          const unsigned bits = bits_at<E, ALIGNED>(best, usable);
+#pragma unroll
+          for (int e = E - 1; e >= 0; --e)
+            if (((bits >> e) & 1u) && value(z + id + e) == top) at = (unsigned)(id + e);
+        }
+        if (one.m == top) at = min(at, (unsigned)one.at);
+        if (some.m == top) at = min(at, (unsigned)some.at);
+        at = __reduce_min_sync(0xffffffffu, at);
+      }
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
       if (lane == 0) parts[row - rb][warp] = Part{top, s, (int)at};
     }
     // join the parts of these rows: row i by CTA i mod chunks
-    if (pl.chunks > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (pl.chunks > 1) cluster_barrier();
     else __syncthreads();
     for (int i = chunk + warp * pl.chunks; i < re - rb; i += kWarps * pl.chunks) {
       Part p{-INFINITY, 0.f, 0x7fffffff};
@@ -426,9 +559,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_rules_confidence(const RulesArg
         const int c = k / kWarps, w = k % kWarps;
         Part o;
         if (pl.chunks > 1) {
-          const unsigned from = tc::smem_u32(&parts[i][w]);
           unsigned far;
-          asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(far) : "r"(from), "r"(c));
+          asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(far) : "r"(tc::smem_u32(&parts[i][w])), "r"(c));
           asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(o.m) : "r"(far) : "memory");
           asm volatile("ld.shared::cluster.f32 %0, [%1+4];" : "=f"(o.s) : "r"(far) : "memory");
           asm volatile("ld.shared::cluster.s32 %0, [%1+8];" : "=r"(o.at) : "r"(far) : "memory");
@@ -440,39 +572,33 @@ __global__ void __launch_bounds__(kThreads, 2) k_rules_confidence(const RulesArg
         p.s = p.s * weight(p.m, top) + o.s * weight(o.m, top);
         p.m = top;
       }
-      p = join_lanes(p);
+      const float top = unordered(__reduce_max_sync(0xffffffffu, ordered(p.m)));
+      const unsigned at = __reduce_min_sync(0xffffffffu, p.m == top ? (unsigned)p.at : 0x7fffffffu);
+      float s = p.s * weight(p.m, top);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
       if (lane == 0) {
-        tok[rb + i] = p.m > -INFINITY ? p.at : -1;
-        conf[rb + i] = p.m > -INFINITY ? __fdiv_rn(1.f, p.s) : (p.s == p.s ? 0.f : p.s);
+        tok[rb + i] = top > -INFINITY ? (int)at : -1;
+        conf[rb + i] = top > -INFINITY ? __fdiv_rn(1.f, s) : (s == s ? 0.f : s);
       }
     }
-    if (pl.chunks > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (pl.chunks > 1) cluster_barrier();                    // nobody overwrites or leaves parts that others still read
     else __syncthreads();
   }
 }
 
-__device__ __forceinline__ uint4 narrow(const float* v, const float*) {
-  return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
-}
-__device__ __forceinline__ uint4 narrow(const float* v, const bf16*) {
-  unsigned w[4];
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
-    w[k] = *reinterpret_cast<const unsigned*>(&h);
-  }
-  return make_uint4(w[0], w[1], w[2], w[3]);
-}
+// ---- the rules on the logits themselves ----------------------------------------------------------------------
 
 // Stores y.  In place only entries that change are written: the touched ones and those that are not allowed.
 template <typename T, bool ALIGNED, bool INPLACE>
-__global__ void __launch_bounds__(kThreads, 2) k_logit_rules(const RulesArgs a, const Plan pl, T* out, long long out_ld) {
-  constexpr int E = Vec<T>::E, kBatch = INPLACE ? 1 : 4;
+__global__ void __launch_bounds__(kThreads, kPerSm) k_logit_rules(const RulesArgs a, const Plan pl, T* out, long long out_ld) {
+  using W = Walk<T, ALIGNED>;
+  constexpr int E = W::E, kBatch = 4;
   constexpr unsigned kAll = (1u << E) - 1u;
   extern __shared__ __align__(16) unsigned smem[];
   pdl_wait();
   pdl_trigger();
-  const int chunk = (int)blockIdx.x % pl.chunks, span = (int)blockIdx.x / pl.chunks;
+  const int chunk = (int)blockIdx.x & (pl.chunks - 1), span = (int)blockIdx.x >> pl.lg;
   const int r0 = (int)((long long)a.n_rows * span / pl.spans), r1 = (int)((long long)a.n_rows * (span + 1) / pl.spans);
   Table t = make_table(a, pl, chunk, smem);
   int cur = -2;
@@ -484,133 +610,144 @@ __global__ void __launch_bounds__(kThreads, 2) k_logit_rules(const RulesArgs a, 
       if (threadIdx.x == 0 && chunk == 0) raise(a);
       continue;
     }
-    const T* z = static_cast<const T*>(a.logits) + (long long)row * a.ld + t.c0;
-    T* y = out + (long long)row * out_ld + t.c0;
+    const T* z = static_cast<const T*>(a.logits) + (long long)row * a.ld;
+    T* y = out + (long long)row * out_ld;
     if (me.req != cur) {
-      build_table(a, t, me.req);
+      build_table(a, t, pl, me.req);
       cur = me.req;
     }
-    const unsigned* mask = me.mask < 0 ? nullptr : a.allowed + me.mask * a.allowed_ld + (t.c0 >> 5);
-    const Cut c = cut_of<T, ALIGNED>(z, t.n);
-    // bits of the entries that may stay, and of those that no other rule touches
-    auto allow = [&](int w) -> unsigned {
-      const unsigned in = in_range(t, w, a.mask_id);
-      return mask && in ? in & __ldg(mask + w) : in;
-    };
+    const unsigned* mask = me.mask < 0 ? nullptr : a.allowed + me.mask * a.allowed_ld;
+    const W walk(z);
     auto plain = [&](int w) -> unsigned { return t.plain[w]; };
-    for (int j0 = threadIdx.x; j0 < c.nv; j0 += kThreads * kBatch) {
+    auto allow = [&](int w) -> unsigned {                    // entries that may stay
+      const unsigned in = t.in_range(w);
+      return in & load1_if(mask + (t.id_of(w * 32) >> 5), mask && in, 0xffffffffu);
+    };
+    const int nv = walk.vectors(pl);
+    for (int j0 = threadIdx.x; j0 < nv; j0 += kThreads * kBatch) {
       uint4 u[kBatch];
       unsigned keep[kBatch], calm[kBatch];
 #pragma unroll
       for (int b = 0; b < kBatch; ++b) {
-        const int j = j0 + b * kThreads;
-        keep[b] = calm[b] = 0u;
-        if (j < c.nv) {
-          if (!INPLACE) u[b] = __ldcs(reinterpret_cast<const uint4*>(z + c.first) + j);
-          keep[b] = bits_at<ALIGNED>(c.first + j * E, allow) & kAll;
-          calm[b] = bits_at<ALIGNED>(c.first + j * E, plain) & keep[b];
-        }
+        const int e = walk.entry(min(j0 + b * kThreads, nv - 1)), id = t.id_of(e);
+        u[b] = load4_if(z + id, !INPLACE && j0 + b * kThreads < nv && id + E <= t.vocab, 0u);
+        keep[b] = bits_at<E, ALIGNED>(e, allow) & kAll;
+        calm[b] = bits_at<E, ALIGNED>(e, plain) & kAll;
       }
 #pragma unroll
       for (int b = 0; b < kBatch; ++b) {
-        const int j = j0 + b * kThreads, p = c.first + j * E;
-        if (j >= c.nv) break;
-        const unsigned put_now = (INPLACE ? 0u : calm[b]) | (kAll & ~keep[b]);    // the others come below
-        float v[E];
-        if (!INPLACE) widen(u[b], v, z);
-#pragma unroll
-        for (int e = 0; e < E; ++e) v[e] = !INPLACE && ((keep[b] >> e) & 1u) ? v[e] : -INFINITY;
-        if (put_now == kAll && (ALIGNED || INPLACE)) {
-          __stcs(reinterpret_cast<uint4*>(y + p), narrow(v, z));
-        } else if (put_now) {
+        const int id = t.id_of(walk.entry(j0 + b * kThreads));
+        if (j0 + b * kThreads >= nv || id + E > t.vocab) continue;
+        const unsigned now = (INPLACE ? 0u : calm[b] & keep[b]) | (kAll & ~keep[b]);      // the others are written below
+        const uint4 x = keep[b] == kAll ? u[b] : only<T>(u[b], keep[b]);
+        if (now == kAll && (ALIGNED || INPLACE)) {
+          __stcs(reinterpret_cast<uint4*>(y + id), x);
+        } else if (now) {
+          float v[E];
+          widen(x, v, z);
 #pragma unroll
           for (int e = 0; e < E; ++e)
-            if ((put_now >> e) & 1u) put(y + p + e, v[e]);
+            if ((now >> e) & 1u) put(y + id + e, v[e]);
         }
       }
     }
-    if (threadIdx.x < 2 * E) {
-      const int e = left_over<E>(c, t.n, threadIdx.x);
+    for (int i = threadIdx.x; i < walk.singles(pl); i += kThreads) {
+      const int e = walk.single(pl, t, i);
       if (e >= 0) {
+        const int id = t.id_of(e);
         const bool stays = (allow(e >> 5) >> (e & 31)) & 1u, alone = (t.plain[e >> 5] >> (e & 31)) & 1u;
-        if (!stays) put(y + e, -INFINITY);
-        else if (alone && !INPLACE) put(y + e, value(z + e));
+        if (!stays) put(y + id, -INFINITY);
+        else if (alone && !INPLACE) put(y + id, value(z + id));
       }
     }
-    each_touched(a, t, mask, [&](int e, unsigned place) { put(y + e, touched(a, t, e, place, value(z + e))); });
+    each_touched(a, t, pl, mask, [&](int i, int id) { put(y + id, ruled(a, t, i, value(z + id))); });
   }
 }
 
-// One-time set-up per device.
+// ---- launches ------------------------------------------------------------------------------------------------
+
+using ConfKernel = void (*)(const RulesArgs, const Plan, int*, float*);
+template <typename T>
+ConfKernel conf_kernel(bool aligned) { return aligned ? k_rules_confidence<T, true> : k_rules_confidence<T, false>; }
+template <typename T>
+using RuleKernel = void (*)(const RulesArgs, const Plan, T*, long long);
+
+// One-time set-up per device; how many spans the device holds at once, by cluster size and by the table's size (in steps of
+// 1 KB), asked when first needed.
+constexpr int kMaxSmem = 56 * 1024;
 struct DevInfo {
   int num_sms;
   int ok;
+  int spans[4][kMaxSmem / 1024 + 1];
 };
 DevInfo g_dev[kMaxDevices];
 std::mutex g_mutex;
 
-constexpr int kMaxSmem = 208 * 1024;         // the table of an eighth of the largest vocabulary
-
-template <typename T>
-using ConfKernel = void (*)(const RulesArgs, const Plan, int*, float*);
-template <typename T>
-using RuleKernel = void (*)(const RulesArgs, const Plan, T*, long long);
-
 template <typename T>
 bool allow_smem() {
   bool ok = true;
-  for (ConfKernel<T> k : {k_rules_confidence<T, true>, k_rules_confidence<T, false>})
+  for (ConfKernel k : {conf_kernel<T>(true), conf_kernel<T>(false)})
     ok = ok && cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem) == cudaSuccess;
   for (RuleKernel<T> k : {k_logit_rules<T, true, true>, k_logit_rules<T, true, false>, k_logit_rules<T, false, true>, k_logit_rules<T, false, false>})
     ok = ok && cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem) == cudaSuccess;
   return ok;
 }
 
-const DevInfo* dev_info() {
+void cluster_config(cudaLaunchConfig_t* cfg, cudaLaunchAttribute* at, int ctas, int chunks, size_t smem, cudaStream_t s) {
+  cfg->gridDim = dim3((unsigned)ctas);
+  cfg->blockDim = dim3(kThreads);
+  cfg->dynamicSmemBytes = smem;
+  cfg->stream = s;
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = (unsigned)chunks; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+  at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg->attrs = at;
+  cfg->numAttrs = 2;
+}
+
+size_t smem_of(const Plan& pl) { return ((size_t)pl.listed * 2 + (size_t)pl.blocks * kBlockWords * 2) * 4 + (size_t)pl.blocks * kBlockWords * 2; }
+
+// The plan of a call, spans excepted.  Shares of at least 32 blocks: with fewer the join would cost more than the row.
+Plan plan_of(const RulesArgs& a) {
+  Plan pl;
+  const int blocks = (a.vocab + kBlock - 1) / kBlock;
+  pl.lg = 0;
+  while ((1 << pl.lg) < kMaxChunks && blocks > 32 << pl.lg) ++pl.lg;
+  pl.chunks = 1 << pl.lg;
+  pl.blocks = (blocks + pl.chunks - 1) >> pl.lg;
+  pl.listed = pl.blocks * kBlock < kListed ? pl.blocks * kBlock : kListed;
+  return pl;
+}
+
+// Sets pl->spans: as many as the device holds at once, since a second round of them would double the time.
+bool plan_spans(const RulesArgs& a, Plan* pl) {
   DevInfo* d = device_slot(g_dev);
-  if (!d) return nullptr;
+  if (!d) return false;
+  const size_t smem = smem_of(*pl);
   std::lock_guard<std::mutex> lock(g_mutex);
   if (!d->num_sms) {
     int dev = 0, n = 0;
     cudaGetDevice(&dev);
-    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) return nullptr;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) return false;
     d->ok = allow_smem<float>() && allow_smem<bf16>();
     if (!d->ok) cudaGetLastError();
     d->num_sms = n;
   }
-  return d;
-}
-
-size_t smem_of(const RulesArgs& a, int chunk) { return (kListed + (a.ctx ? (size_t)chunk : 0) + 2 * (size_t)(chunk / 32) + 8) * 4; }
-
-Plan plan_of(const RulesArgs& a, int num_sms) {
-  Plan pl;
-  pl.chunks = 1;
-  while (pl.chunks < kMaxChunks && a.vocab > 16384 * pl.chunks) pl.chunks *= 2;
-  pl.chunk = ((a.vocab + pl.chunks - 1) / pl.chunks + 31) / 32 * 32;
-  int per_sm = (int)(225 * 1024 / (smem_of(a, pl.chunk) + 8 * 1024));
-  if (per_sm > 2) per_sm = 2;
-  int spans = num_sms * per_sm / pl.chunks;
-  pl.spans = spans < a.n_rows ? spans : a.n_rows;
-  return pl;
-}
-
-template <typename T>
-cudaError_t launch_conf(const RulesArgs& a, const Plan& pl, int* tok, float* conf, cudaStream_t s) {
-  const bool aligned = (a.ld * sizeof(T)) % 16 == 0;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(pl.spans * pl.chunks));
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = smem_of(a, pl.chunk);
-  cfg.stream = s;
-  cudaLaunchAttribute at[2];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  at[1].id = cudaLaunchAttributeClusterDimension;
-  at[1].val.clusterDim.x = (unsigned)pl.chunks; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, aligned ? k_rules_confidence<T, true> : k_rules_confidence<T, false>, a, pl, tok, conf);
+  if (!d->ok || smem > kMaxSmem) return false;
+  int& spans = d->spans[pl->lg][smem / 1024];
+  if (spans == 0) {
+    spans = d->num_sms * kPerSm >> pl->lg;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute at[2];
+    cluster_config(&cfg, at, spans << pl->lg, pl->chunks, (smem + 1023) / 1024 * 1024, nullptr);
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, conf_kernel<float>(true), &cfg) == cudaSuccess && n > 0) spans = n;
+    else cudaGetLastError();
+  }
+  pl->spans = spans < a.n_rows ? spans : a.n_rows;
+  return true;
 }
 
 template <typename T>
@@ -618,24 +755,26 @@ cudaError_t launch_rules(const RulesArgs& a, const Plan& pl, T* out, long long o
   const bool aligned = (a.ld * sizeof(T)) % 16 == 0 && (out_ld * sizeof(T)) % 16 == 0, inplace = out == a.logits;
   RuleKernel<T> k = inplace ? (aligned ? k_logit_rules<T, true, true> : k_logit_rules<T, false, true>)
                             : (aligned ? k_logit_rules<T, true, false> : k_logit_rules<T, false, false>);
-  return launch_pdl(k, dim3((unsigned)(pl.spans * pl.chunks)), dim3(kThreads), smem_of(a, pl.chunk), s, a, pl, out, out_ld);
+  return launch_pdl(k, dim3((unsigned)(pl.spans * pl.chunks)), dim3(kThreads), smem_of(pl), s, a, pl, out, out_ld);
 }
 
 }  // namespace
 
 cudaError_t launch_rules_confidence(const RulesArgs& a, int* tok, float* conf, cudaStream_t s) {
   if (a.n_rows <= 0) return cudaSuccess;
-  const DevInfo* d = dev_info();
-  if (!d || !d->ok) return cudaErrorNotSupported;
-  const Plan pl = plan_of(a, d->num_sms);
-  return a.bf16_logits ? launch_conf<bf16>(a, pl, tok, conf, s) : launch_conf<float>(a, pl, tok, conf, s);
+  Plan pl = plan_of(a);
+  if (!plan_spans(a, &pl)) return cudaErrorNotSupported;
+  const bool aligned = (a.ld * (a.bf16_logits ? 2 : 4)) % 16 == 0;
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute at[2];
+  cluster_config(&cfg, at, pl.spans * pl.chunks, pl.chunks, smem_of(pl), s);
+  return cudaLaunchKernelEx(&cfg, a.bf16_logits ? conf_kernel<bf16>(aligned) : conf_kernel<float>(aligned), a, pl, tok, conf);
 }
 
 cudaError_t launch_logit_rules(const RulesArgs& a, void* out, long long out_ld, cudaStream_t s) {
   if (a.n_rows <= 0) return cudaSuccess;
-  const DevInfo* d = dev_info();
-  if (!d || !d->ok) return cudaErrorNotSupported;
-  const Plan pl = plan_of(a, d->num_sms);
+  Plan pl = plan_of(a);
+  if (!plan_spans(a, &pl)) return cudaErrorNotSupported;
   return a.bf16_logits ? launch_rules<bf16>(a, pl, (bf16*)out, out_ld, s) : launch_rules<float>(a, pl, (float*)out, out_ld, s);
 }
 
