@@ -17,6 +17,7 @@
 #include <math.h>
 
 #include <mutex>
+#include <type_traits>
 
 #include "decode_ops.cuh"
 #include "tc_common.cuh"
@@ -40,12 +41,18 @@ struct Part {
   float m, s;
   int at;
 };
+struct __align__(16) Slot {
+  Part part;
+  int unused;
+};
 
 struct Plan {
   int chunks, lg;        // CTAs that share a row (a cluster for the confidence): 1 << lg
   int blocks;            // blocks of a CTA's share (the last may lie behind the vocabulary)
   int listed;            // room in the list
   int spans;
+  int early;             // the launch may overlap the kernel before: clusters that fill the device do not all fit beside
+                         // one that is leaving, and the last would wait for a first to end (16 x 32 rows: 72 us, else 56)
 };
 
 __device__ __forceinline__ float value(const float* p) { return *p; }
@@ -71,13 +78,48 @@ __device__ __forceinline__ unsigned load1_if(const void* p, bool on, unsigned ot
                : "+r"(u) : "l"(p), "r"((unsigned)on));
   return u;
 }
+// One logit as it is stored, and its value.  (An ordinary load: in place, other entries of its sector are being written.)
+__device__ __forceinline__ unsigned load_bits(const float* p, bool on) {
+  unsigned u = 0u;
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p ld.global.u32 %0, [%1];\n\t}" : "+r"(u) : "l"(p), "r"((unsigned)on) : "memory");
+  return u;
+}
+__device__ __forceinline__ unsigned load_bits(const bf16* p, bool on) {
+  unsigned u = 0u;
+  asm volatile("{\n\t.reg .pred p;\n\t.reg .u16 h;\n\tsetp.ne.u32 p, %2, 0;\n\tmov.u16 h, 0;\n\t@p ld.global.u16 h, [%1];\n\tcvt.u32.u16 %0, h;\n\t}"
+               : "=r"(u) : "l"(p), "r"((unsigned)on) : "memory");
+  return u;
+}
+__device__ __forceinline__ float from_bits(unsigned u, const float*) { return __uint_as_float(u); }
+__device__ __forceinline__ float from_bits(unsigned u, const bf16*) { return __uint_as_float(u << 16); }
 __device__ __forceinline__ unsigned cluster_rank() {
   unsigned r;
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
   return r;
 }
-__device__ __forceinline__ void cluster_barrier() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ unsigned in_cta(unsigned addr, unsigned rank) {
+  unsigned r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
+}
+// Writes a slot of CTA `rank` of the cluster, which counts its 16 bytes on its barrier.
+__device__ __forceinline__ void send(const Slot* to, unsigned long long* bar, unsigned rank, float m, float s, unsigned at) {
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];"
+               ::"r"(in_cta(tc::smem_u32(to), rank)), "r"(__float_as_uint(m)), "r"(__float_as_uint(s)), "r"(at), "r"(0u),
+                 "r"(in_cta(tc::smem_u32(bar), rank)) : "memory");
+}
+// Bounded: false if the parts do not arrive in time.
+__device__ __forceinline__ bool wait_parts(unsigned long long* bar, unsigned parity) {
+  const long long t0 = clock64();
+  for (;;) {
+    unsigned ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(tc::smem_u32(bar)), "r"(parity) : "memory");
+    if (ok) return true;
+    if (clock64() - t0 > tc::kWaitCycles) return false;
+  }
 }
 
 // ---- a request's table ---------------------------------------------------------------------------------------
@@ -87,8 +129,9 @@ struct Table {
   unsigned* plain;       // bit set: only the grammar decides about this entry
   unsigned* touched;     // bit set: some other rule does
   unsigned short* place; // of a word's first touched entry among all of them
-  unsigned* list;        // touched entries in ascending order: entry | (1 + place of its first bias, or 0) << 16
-  unsigned* count;       // of a listed entry: kInPrompt | times generated
+  unsigned* count;       // of a listed entry (touched, in ascending order): kInPrompt | times generated
+  unsigned short* list;  // the entry
+  unsigned short* bias;  // 1 + place of its first bias, or 0
   int total;             // touched entries
   int begin, gen, end;   // the request's context
   int bias_lo, bias_hi;  // its biases
@@ -119,29 +162,29 @@ __device__ Table make_table(const RulesArgs& a, const Plan& pl, int chunk, unsig
   Table t;
   t.chunk = chunk; t.lg = pl.lg; t.vocab = a.vocab; t.mask_id = a.mask_id;
   t.words = pl.blocks * kBlockWords;
-  t.list = smem;
-  t.count = t.list + pl.listed;
+  t.count = smem;
   t.plain = t.count + pl.listed;
   t.touched = t.plain + t.words;
-  t.place = reinterpret_cast<unsigned short*>(t.touched + t.words);
+  t.list = reinterpret_cast<unsigned short*>(t.touched + t.words);
+  t.bias = t.list + pl.listed;
+  t.place = t.bias + pl.listed;
   t.total = 0;
   return t;
 }
 
 // Lists the touched entries from the `from`-th on, as many as there is room for.  All threads of the CTA.
 __device__ __forceinline__ void list_touched(const RulesArgs& a, const Table& t, const Plan& pl, int from) {
-  const int to = min(t.total, from + pl.listed);
-  for (int i = threadIdx.x; i < to - from; i += kThreads) t.count[i] = 0u;
-  for (int w = threadIdx.x; w < t.words; w += kThreads) {
-    unsigned bits = t.touched[w];
-    for (int at = t.place[w]; bits; bits &= bits - 1, ++at)
-      if (at >= from && at < to) t.list[at - from] = (unsigned)(w * 32 + __ffs(bits) - 1);
+  const int n = min(t.total - from, pl.listed);
+  for (int i = threadIdx.x; i < n; i += kThreads) {
+    t.count[i] = 0u;
+    t.bias[i] = 0;
   }
   __syncthreads();
-  // the tokens of the context and of the biases, several in flight
-  auto place_of = [&](int id) {
-    const int e = t.entry_of(id);
-    return t.place[e >> 5] + __popc(t.touched[e >> 5] & ((1u << (e & 31)) - 1u)) - from;
+  // the place of entry e (tokens that occur often write the same entry), or something out of [0, n)
+  auto listed = [&](int e) {
+    const int at = t.place[e >> 5] + __popc(t.touched[e >> 5] & ((1u << (e & 31)) - 1u)) - from;
+    if (at >= 0 && at < n) t.list[at] = (unsigned short)e;
+    return at;
   };
   for (int i0 = t.begin + threadIdx.x; i0 < t.end; i0 += kThreads * kTokens) {
     int id[kTokens];
@@ -150,8 +193,8 @@ __device__ __forceinline__ void list_touched(const RulesArgs& a, const Table& t,
 #pragma unroll
     for (int k = 0; k < kTokens; ++k)
       if (t.takes(id[k])) {
-        const int at = place_of(id[k]);
-        if (at >= 0 && at < to - from) {
+        const int at = listed(t.entry_of(id[k]));
+        if (at >= 0 && at < n) {
           if (i0 + k * kThreads >= t.gen) atomicAdd(t.count + at, 1u);
           else atomicOr(t.count + at, kInPrompt);
         }
@@ -160,8 +203,8 @@ __device__ __forceinline__ void list_touched(const RulesArgs& a, const Table& t,
   for (int i = t.bias_lo + threadIdx.x; i < t.bias_hi; i += kThreads) {
     const int id = __ldg(a.bias_tok + i);
     if (t.takes(id) && (i == t.bias_lo || __ldg(a.bias_tok + i - 1) < id)) {
-      const int at = place_of(id);
-      if (at >= 0 && at < to - from) atomicOr(t.list + at, (unsigned)min(i - t.bias_lo + 1, 0xffff) << 16);
+      const int at = listed(t.entry_of(id));
+      if (at >= 0 && at < n) t.bias[at] = (unsigned short)min(i - t.bias_lo + 1, 0xffff);
     }
   }
   __syncthreads();
@@ -242,14 +285,14 @@ __device__ __forceinline__ void build_table(const RulesArgs& a, Table& t, const 
 // y of the i-th listed entry from its logit.
 __device__ __forceinline__ float ruled(const RulesArgs& a, const Table& t, int i, float z) {
   float y = z;
-  const unsigned c = t.count[i], place = t.list[i] >> 16;
+  const unsigned c = t.count[i], place = t.bias[i];
   if (c) {
     y = y > 0.f ? __fdiv_rn(y, t.rho) : __fmul_rn(y, t.rho);
     const unsigned made = c & ~kInPrompt;
     if (made) y = __fsub_rn(y, __fadd_rn(__fmul_rn(t.phi, (float)made), t.alpha));
   }
   if (place) {
-    const int id = t.id_of((int)(t.list[i] & 0xffffu));
+    const int id = t.id_of(t.list[i]);
     int k = t.bias_lo + (int)place - 1;
     if (place == 0xffffu)                                    // or behind that: ids ascend
       for (int hi = t.bias_hi; k < hi;) {
@@ -262,22 +305,38 @@ __device__ __forceinline__ float ruled(const RulesArgs& a, const Table& t, int i
   return y;
 }
 
-// Calls f(i, entry) for the touched entries that the mask (nullable) allows, listed as the i-th, each by one thread of the
-// CTA.  More of them than there is room for are listed in turns, anew for every row.
-template <typename F>
-__device__ __forceinline__ void each_touched(const RulesArgs& a, const Table& t, const Plan& pl, const unsigned* mask, F f) {
-  for (int from = 0; from < t.total; from += pl.listed) {
-    if (t.total > pl.listed) {
-      __syncthreads();
-      list_touched(a, t, pl, from);
-    }
-    const int n = min(pl.listed, t.total - from);
-    for (int i = threadIdx.x; i < n; i += kThreads) {
-      const int e = (int)(t.list[i] & 0xffffu), id = t.id_of(e);
-      if (!mask || ((__ldg(mask + (id >> 5)) >> (id & 31)) & 1u)) f(i, id);
+// Calls f(i, z) for the touched entries of a row that the mask (nullable) allows, listed as the i-th, with their logits,
+// each by one thread of the CTA.  More of them than there is room for are listed in turns, anew for every row.
+template <typename T>
+struct Touched {
+  int id = 0;
+  unsigned word = 0u;      // of the mask
+  unsigned z = 0u;
+  // fetches what the thread needs for the first of its entries
+  __device__ __forceinline__ void begin(const Table& t, const Plan& pl, const unsigned* mask, const T* row) {
+    if (t.total <= pl.listed) fetch(t, mask, row, threadIdx.x, t.total);
+  }
+  __device__ __forceinline__ void fetch(const Table& t, const unsigned* mask, const T* row, int i, int n) {
+    id = t.id_of(i < n ? t.list[i] : 0);
+    word = load1_if(mask + (id >> 5), i < n && mask, i < n ? 0xffffffffu : 0u);
+    z = load_bits(row + id, i < n);
+  }
+  template <typename F>
+  __device__ __forceinline__ void finish(const RulesArgs& a, const Table& t, const Plan& pl, const unsigned* mask, const T* row, F f) {
+    for (int from = 0; from < t.total; from += pl.listed) {
+      const int n = min(pl.listed, t.total - from);
+      if (t.total > pl.listed) {
+        __syncthreads();
+        list_touched(a, t, pl, from);
+        fetch(t, mask, row, threadIdx.x, n);
+      }
+      for (int i = threadIdx.x; i < n; i += kThreads) {
+        if ((word >> (id & 31)) & 1u) f(i, id, from_bits(z, row));
+        if (i + kThreads < n) fetch(t, mask, row, i + kThreads, n);
+      }
     }
   }
-}
+};
 
 // ---- rows ----------------------------------------------------------------------------------------------------
 
@@ -286,7 +345,8 @@ struct Row {
   int req, mask;
 };
 __device__ __forceinline__ Row row_of(const RulesArgs& a, int row) {
-  return Row{a.row_req ? __ldg(a.row_req + row) : row, a.allowed ? (a.row_mask ? __ldg(a.row_mask + row) : row) : -1};
+  return Row{(int)load1_if(a.row_req + row, a.row_req != nullptr, (unsigned)row),
+             (int)load1_if(a.row_mask + row, a.allowed && a.row_mask, a.allowed ? (unsigned)row : 0xffffffffu)};
 }
 __device__ __forceinline__ bool valid(const RulesArgs& a, const Row& r) {
   return r.req >= -1 && r.req < a.n_reqs && r.mask >= -1 && r.mask < a.n_masks;
@@ -354,18 +414,18 @@ __device__ __forceinline__ void join_one(Part& p, float y, int at) {
 template <typename T>
 constexpr unsigned kLeast = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;     // a word of -inf
 
-// Entries without their bit become -inf.
+// Entries without their bit (of the low E) become -inf.  A product puts four bits at the tops of four bytes (the shifted
+// copies do not meet), from where a byte permutation spreads them over a word: two instructions an entry instead of three.
 template <typename T>
 __device__ __forceinline__ uint4 only(uint4 u, unsigned bits) {
   unsigned w[4] = {u.x, u.y, u.z, u.w};
+  const unsigned lo = (bits & 15u) * 0x10204080u, hi = sizeof(T) == 4 ? lo : (bits >> 4 & 15u) * 0x10204080u;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    if (sizeof(T) == 4) {
-      w[i] = (bits >> i) & 1u ? w[i] : kLeast<T>;
-    } else {
-      const unsigned keep = ((bits >> (2 * i)) & 1u ? 0x0000ffffu : 0u) | ((bits >> (2 * i + 1)) & 1u ? 0xffff0000u : 0u);
-      w[i] = (w[i] & keep) | (kLeast<T> & ~keep);
-    }
+    unsigned keep;                                           // (the permutation's upper selectors repeat a byte's top bit)
+    if (sizeof(T) == 4) asm("prmt.b32 %0, %1, %1, %2;" : "=r"(keep) : "r"(lo), "r"(0x8888u + 0x1111u * i));
+    else asm("prmt.b32 %0, %1, %1, %2;" : "=r"(keep) : "r"(i < 2 ? lo : hi), "r"(i & 1 ? 0xbbaau : 0x9988u));
+    w[i] = (w[i] & keep) | (kLeast<T> & ~keep);
   }
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
@@ -420,28 +480,47 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_rules_confidence(const Rul
   constexpr int E = W::E, kBatch = E == 4 ? 5 : 4;           // vectors a thread has in flight
   constexpr unsigned kAll = (1u << E) - 1u;
   extern __shared__ __align__(16) unsigned smem[];
-  __shared__ Part parts[kRowsAtOnce][kWarps];
+  __shared__ Slot parts[kRowsAtOnce * kWarps];               // of the rows that this CTA joins: [row][chunk][warp]
+  __shared__ __align__(8) unsigned long long s_bar;
   __shared__ unsigned s_top[kRowsAtOnce];                    // the largest maximum that a warp has left so far, ordered
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (threadIdx.x == 0) {
+    tc::mbar_init(tc::smem_u32(&s_bar), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncwarp();
+  cluster_arrive();
   pdl_wait();
   pdl_trigger();
-  const int chunk = pl.chunks > 1 ? (int)cluster_rank() : 0;
-  const int span = blockIdx.x / pl.chunks;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int chunk = (int)cluster_rank();
+  const int span = (int)blockIdx.x >> pl.lg;
+  unsigned turn = 0u;
   const int r0 = (int)((long long)a.n_rows * span / pl.spans), r1 = (int)((long long)a.n_rows * (span + 1) / pl.spans);
   Table t = make_table(a, pl, chunk, smem);
   const unsigned long long log2e = pair_of(kLog2e);
+  const int step = (kThreads * E) << pl.lg;                  // tokens between two vectors of a thread
   int cur = -2;
   Row next = row_of(a, r0);
-  for (int rb = r0; rb < r1; rb += kRowsAtOnce) {
+  cluster_wait();                                            // the others' barriers are there
+  for (int rb = r0; rb < r1; rb += kRowsAtOnce, turn ^= 1u) {
     const int re = min(r1, rb + kRowsAtOnce);
+    const int joins = (re - rb - chunk + pl.chunks - 1) >> pl.lg;                // rows that this CTA joins: chunk, chunk + chunks, ..
+    if (rb > r0) {                                           // the parts of the rows before have been read everywhere
+      __syncthreads();
+      cluster_arrive();
+      cluster_wait();
+    }
+    if (threadIdx.x == 0 && joins > 0) tc::mbar_expect_tx(tc::smem_u32(&s_bar), (unsigned)(joins * pl.chunks * kWarps * sizeof(Slot)));
     if (threadIdx.x < kRowsAtOnce) s_top[threadIdx.x] = 0u;
     __syncthreads();
     for (int row = rb; row < re; ++row) {
       const Row me = next;
       if (row + 1 < r1) next = row_of(a, row + 1);
+      const unsigned joiner = (unsigned)(row - rb) & (unsigned)(pl.chunks - 1);
+      const Slot* slot = &parts[(((row - rb) >> pl.lg << pl.lg) + chunk) * kWarps + warp];
       if (!valid(a, me)) {
         if (threadIdx.x == 0 && chunk == 0) raise(a);
-        if (lane == 0) parts[row - rb][warp] = Part{-INFINITY, 0.f, 0x7fffffff};
+        if (lane == 0) send(slot, &s_bar, joiner, -INFINITY, 0.f, 0x7fffffffu);
         continue;
       }
       const T* z = static_cast<const T*>(a.logits) + (long long)row * a.ld;
@@ -455,62 +534,78 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_rules_confidence(const Rul
         const unsigned p = t.plain[w];
         return p & load1_if(mask + (t.id_of(w * 32) >> 5), mask && p, 0xffffffffu);
       };
+      Touched<T> entries;
+      entries.begin(t, pl, mask, z);
       float m = -INFINITY;
       unsigned long long s2 = 0ull;
-      int best = 0;                                          // first entry of the vector that holds m
+      int best = threadIdx.x;                                // the batch that holds m: its first vector
       const int nv = walk.vectors(pl);
-      for (int j0 = threadIdx.x; j0 < nv; j0 += kThreads * kBatch) {
-        unsigned bits[kBatch], every = kAll;
-        uint4 u[kBatch];
-#pragma unroll
-        for (int b = 0; b < kBatch; ++b) {
-          const int e = walk.entry(min(j0 + b * kThreads, nv - 1)), id = t.id_of(e);
-          const bool there = j0 + b * kThreads < nv && id + E <= t.vocab;
-          u[b] = load4_if(z + id, there, kLeast<T>);         // (what is not there is -inf)
-          bits[b] = bits_at<E, ALIGNED>(e, usable) | (there ? 0u : kAll);
-        }
-#pragma unroll
-        for (int b = 0; b < kBatch; ++b) every &= bits[b];
-        if ((every & kAll) != kAll) {
-#pragma unroll
-          for (int b = 0; b < kBatch; ++b) u[b] = only<T>(u[b], bits[b]);
-        }
-        float top = m;
-#pragma unroll
-        for (int b = 0; b < kBatch; ++b) {
-          const float vm = largest(u[b], z);
-          if (vm > top) {
-            top = vm;
-            best = walk.entry(j0 + b * kThreads);
-          }
-        }
-        if (top > m) {
-          const unsigned long long w = pair_of(weight(m, top));
-          asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(s2) : "l"(s2), "l"(w));
-          m = top;
-        }
-        if (m == INFINITY) {                                 // k of them share the row
-          float n = 0.f;
+      auto dense = [&](auto masked) {
+        int e0 = walk.entry(threadIdx.x), id0 = t.id_of(e0);
+        const unsigned shift = ALIGNED ? e0 & 31 : 0;        // (the same for all of a thread's vectors)
+        const unsigned* words = mask + (id0 >> 5);
+        for (int j0 = threadIdx.x; j0 < nv; j0 += kThreads * kBatch, e0 += kThreads * E * kBatch, id0 += step * kBatch, words += (step >> 5) * kBatch) {
+          unsigned bits[kBatch], every = 0xffffffffu;
+          uint4 u[kBatch];
+          // aligned rows: a thread's vectors are whole blocks apart, those that are not there lie behind the vocabulary
+          const int left = ALIGNED ? t.vocab - E - id0 : 0;
 #pragma unroll
           for (int b = 0; b < kBatch; ++b) {
-            float v[E];
-            widen(u[b], v, z);
-#pragma unroll
-            for (int e = 0; e < E; ++e) n += v[e] == INFINITY ? 1.f : (v[e] == v[e] ? 0.f : v[e]);
+            const int e = ALIGNED ? e0 + b * kThreads * E : walk.entry(min(j0 + b * kThreads, nv - 1));
+            const int id = ALIGNED ? id0 + b * step : t.id_of(e);
+            const bool there = ALIGNED ? b * step <= left : id <= t.vocab - E && j0 + b * kThreads < nv;
+            u[b] = make_uint4(kLeast<T>, kLeast<T>, kLeast<T>, kLeast<T>);      // (what is not there is -inf)
+            if (there) u[b] = __ldcs(reinterpret_cast<const uint4*>(z + id));
+            if (ALIGNED) {
+              bits[b] = masked.value ? 0u : 0xffffffffu;
+              if (masked.value && there) bits[b] = __ldg(words + b * (step >> 5));
+              if (masked.value || there) bits[b] &= t.plain[e >> 5];
+            } else {
+              bits[b] = bits_at<E, false>(e, usable) | (there ? 0u : kAll);
+            }
           }
-          unsigned long long x;
-          asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(n), "f"(0.f));
-          asm("add.rn.f32x2 %0, %1, %2;" : "=l"(s2) : "l"(s2), "l"(x));
-        } else {
-          const unsigned long long minus = pair_of(m > -INFINITY ? -m : 0.f);
+          if (!masked.value) {
 #pragma unroll
-          for (int b = 0; b < kBatch; ++b) {
-            float v[E];
-            widen(u[b], v, z);
-            add_exps<E>(v, minus, log2e, s2);
+            for (int b = 0; b < kBatch; ++b) every &= bits[b];
+          }
+          if (masked.value || ((every >> shift) & kAll) != kAll) {
+#pragma unroll
+            for (int b = 0; b < kBatch; ++b) u[b] = only<T>(u[b], bits[b] >> shift);
+          }
+          float top = largest(u[0], z);
+#pragma unroll
+          for (int b = 1; b < kBatch; ++b) top = fmaxf(top, largest(u[b], z));
+          if (top > m) {
+            const unsigned long long w = pair_of(weight(m, top));
+            asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(s2) : "l"(s2), "l"(w));
+            m = top;
+            best = j0;
+          }
+          if (m == INFINITY) {                               // k of them share the row
+            float n = 0.f;
+#pragma unroll
+            for (int b = 0; b < kBatch; ++b) {
+              float v[E];
+              widen(u[b], v, z);
+#pragma unroll
+              for (int e = 0; e < E; ++e) n += v[e] == INFINITY ? 1.f : (v[e] == v[e] ? 0.f : v[e]);
+            }
+            unsigned long long x;
+            asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(n), "f"(0.f));
+            asm("add.rn.f32x2 %0, %1, %2;" : "=l"(s2) : "l"(s2), "l"(x));
+          } else {
+            const unsigned long long minus = pair_of(m > -INFINITY ? -m : 0.f);
+#pragma unroll
+            for (int b = 0; b < kBatch; ++b) {
+              float v[E];
+              widen(u[b], v, z);
+              add_exps<E>(v, minus, log2e, s2);
+            }
           }
         }
-      }
+      };
+      if (mask) dense(std::true_type());
+      else dense(std::false_type());
       float s, s_odd;
       asm("mov.b64 {%0, %1}, %2;" : "=f"(s), "=f"(s_odd) : "l"(s2));
       s += s_odd;
@@ -526,7 +621,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_rules_confidence(const Rul
         }
       }
       Part some{-INFINITY, 0.f, 0x7fffffff};                 // the touched entries
-      each_touched(a, t, pl, mask, [&](int i, int id) { join_one(some, ruled(a, t, i, value(z + id)), id); });
+      entries.finish(a, t, pl, mask, z, [&](int i, int id, float v) { join_one(some, ruled(a, t, i, v), id); });
       // the warp's part: the lowest entry among the lanes that hold the maximum (where no warp has left a larger one)
       const unsigned highest = __reduce_max_sync(0xffffffffu, ordered(fmaxf(m, fmaxf(one.m, some.m))));
       const float top = unordered(highest);
@@ -536,11 +631,14 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_rules_confidence(const Rul
       unsigned at = 0x7fffffffu;
       if (__shfl_sync(0xffffffffu, before, 0) <= highest && top > -INFINITY) {
         if (m == top) {
-          const int id = t.id_of(best);
-          const unsigned bits = bits_at<E, ALIGNED>(best, usable);
+          for (int j = best; j < min(nv, best + kThreads * kBatch) && at == 0x7fffffffu; j += kThreads) {
+            const int first = walk.entry(j), id = t.id_of(first);
+            if (id > t.vocab - E) break;
+            const unsigned bits = bits_at<E, ALIGNED>(first, usable);
 #pragma unroll
-          for (int e = E - 1; e >= 0; --e)
-            if (((bits >> e) & 1u) && value(z + id + e) == top) at = (unsigned)(id + e);
+            for (int e = E - 1; e >= 0; --e)
+              if (((bits >> e) & 1u) && value(z + id + e) == top) at = (unsigned)(id + e);
+          }
         }
         if (one.m == top) at = min(at, (unsigned)one.at);
         if (some.m == top) at = min(at, (unsigned)some.at);
@@ -548,42 +646,33 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_rules_confidence(const Rul
       }
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-      if (lane == 0) parts[row - rb][warp] = Part{top, s, (int)at};
+      if (lane == 0) send(slot, &s_bar, joiner, top, s, at);
     }
     // join the parts of these rows: row i by CTA i mod chunks
-    if (pl.chunks > 1) cluster_barrier();
-    else __syncthreads();
-    for (int i = chunk + warp * pl.chunks; i < re - rb; i += kWarps * pl.chunks) {
-      Part p{-INFINITY, 0.f, 0x7fffffff};
-      for (int k = lane; k < kWarps * pl.chunks; k += 32) {
-        const int c = k / kWarps, w = k % kWarps;
-        Part o;
-        if (pl.chunks > 1) {
-          unsigned far;
-          asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(far) : "r"(tc::smem_u32(&parts[i][w])), "r"(c));
-          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(o.m) : "r"(far) : "memory");
-          asm volatile("ld.shared::cluster.f32 %0, [%1+4];" : "=f"(o.s) : "r"(far) : "memory");
-          asm volatile("ld.shared::cluster.s32 %0, [%1+8];" : "=r"(o.at) : "r"(far) : "memory");
-        } else {
-          o = parts[i][w];
+    if (warp < joins) {
+      const bool here = wait_parts(&s_bar, turn);
+      if (!here && lane == 0 && a.error_flag) atomicMax(a.error_flag, 1);
+      for (int k = warp; k < joins; k += kWarps) {
+        Part p{-INFINITY, 0.f, 0x7fffffff};
+        for (int i = lane; i < kWarps << pl.lg; i += 32) {
+          const Part o = parts[(k << pl.lg) * kWarps + i].part;
+          const float top = fmaxf(p.m, o.m);
+          p.at = o.m > p.m ? o.at : (o.m == p.m ? min(p.at, o.at) : p.at);
+          p.s = p.s * weight(p.m, top) + o.s * weight(o.m, top);
+          p.m = top;
         }
-        const float top = fmaxf(p.m, o.m);
-        p.at = o.m > p.m ? o.at : (o.m == p.m ? min(p.at, o.at) : p.at);
-        p.s = p.s * weight(p.m, top) + o.s * weight(o.m, top);
-        p.m = top;
-      }
-      const float top = unordered(__reduce_max_sync(0xffffffffu, ordered(p.m)));
-      const unsigned at = __reduce_min_sync(0xffffffffu, p.m == top ? (unsigned)p.at : 0x7fffffffu);
-      float s = p.s * weight(p.m, top);
+        const float top = unordered(__reduce_max_sync(0xffffffffu, ordered(p.m)));
+        const unsigned at = __reduce_min_sync(0xffffffffu, p.m == top ? (unsigned)p.at : 0x7fffffffu);
+        float s = p.s * weight(p.m, top);
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-      if (lane == 0) {
-        tok[rb + i] = top > -INFINITY ? (int)at : -1;
-        conf[rb + i] = top > -INFINITY ? __fdiv_rn(1.f, s) : (s == s ? 0.f : s);
+        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        if (lane == 0) {
+          const int row = rb + (k << pl.lg) + chunk;
+          tok[row] = here && top > -INFINITY ? (int)at : -1;
+          conf[row] = !here ? __uint_as_float(0x7fffffffu) : top > -INFINITY ? __fdiv_rn(1.f, s) : (s == s ? 0.f : s);
+        }
       }
     }
-    if (pl.chunks > 1) cluster_barrier();                    // nobody overwrites or leaves parts that others still read
-    else __syncthreads();
   }
 }
 
@@ -600,6 +689,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logit_rules(const RulesArg
   pdl_trigger();
   const int chunk = (int)blockIdx.x & (pl.chunks - 1), span = (int)blockIdx.x >> pl.lg;
   const int r0 = (int)((long long)a.n_rows * span / pl.spans), r1 = (int)((long long)a.n_rows * (span + 1) / pl.spans);
+  const int step = (kThreads * E) << pl.lg;                  // tokens between two vectors of a thread
   Table t = make_table(a, pl, chunk, smem);
   int cur = -2;
   Row next = row_of(a, r0);
@@ -623,21 +713,32 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logit_rules(const RulesArg
       const unsigned in = t.in_range(w);
       return in & load1_if(mask + (t.id_of(w * 32) >> 5), mask && in, 0xffffffffu);
     };
+    Touched<T> entries;
+    entries.begin(t, pl, mask, z);
     const int nv = walk.vectors(pl);
-    for (int j0 = threadIdx.x; j0 < nv; j0 += kThreads * kBatch) {
+    int e0 = walk.entry(threadIdx.x), id0 = t.id_of(e0);
+    for (int j0 = threadIdx.x; j0 < nv; j0 += kThreads * kBatch, e0 += kThreads * E * kBatch, id0 += step * kBatch) {
       uint4 u[kBatch];
       unsigned keep[kBatch], calm[kBatch];
 #pragma unroll
       for (int b = 0; b < kBatch; ++b) {
-        const int e = walk.entry(min(j0 + b * kThreads, nv - 1)), id = t.id_of(e);
-        u[b] = load4_if(z + id, !INPLACE && j0 + b * kThreads < nv && id + E <= t.vocab, 0u);
-        keep[b] = bits_at<E, ALIGNED>(e, allow) & kAll;
-        calm[b] = bits_at<E, ALIGNED>(e, plain) & kAll;
+        const int e = ALIGNED ? e0 + b * kThreads * E : walk.entry(min(j0 + b * kThreads, nv - 1));
+        const int id = ALIGNED ? id0 + b * step : t.id_of(e);
+        const bool there = id <= t.vocab - E && (ALIGNED || j0 + b * kThreads < nv);
+        u[b] = load4_if(z + id, !INPLACE && there, 0u);
+        if (ALIGNED) {
+          const unsigned m = load1_if(mask + (id >> 5), mask && there, 0xffffffffu);
+          calm[b] = (t.plain[e >> 5] >> (e & 31)) & kAll;
+          keep[b] = ((t.plain[e >> 5] | t.touched[e >> 5]) & m) >> (e & 31) & kAll;
+        } else {
+          keep[b] = bits_at<E, false>(e, allow) & kAll;
+          calm[b] = bits_at<E, false>(e, plain) & kAll;
+        }
       }
 #pragma unroll
       for (int b = 0; b < kBatch; ++b) {
-        const int id = t.id_of(walk.entry(j0 + b * kThreads));
-        if (j0 + b * kThreads >= nv || id + E > t.vocab) continue;
+        const int id = ALIGNED ? id0 + b * step : t.id_of(walk.entry(min(j0 + b * kThreads, nv - 1)));
+        if (id > t.vocab - E || (!ALIGNED && j0 + b * kThreads >= nv)) continue;
         const unsigned now = (INPLACE ? 0u : calm[b] & keep[b]) | (kAll & ~keep[b]);      // the others are written below
         const uint4 x = keep[b] == kAll ? u[b] : only<T>(u[b], keep[b]);
         if (now == kAll && (ALIGNED || INPLACE)) {
@@ -660,7 +761,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logit_rules(const RulesArg
         else if (alone && !INPLACE) put(y + id, value(z + id));
       }
     }
-    each_touched(a, t, pl, mask, [&](int i, int id) { put(y + id, ruled(a, t, i, value(z + id))); });
+    entries.finish(a, t, pl, mask, z, [&](int i, int id, float v) { put(y + id, ruled(a, t, i, v)); });
   }
 }
 
@@ -693,7 +794,7 @@ bool allow_smem() {
   return ok;
 }
 
-void cluster_config(cudaLaunchConfig_t* cfg, cudaLaunchAttribute* at, int ctas, int chunks, size_t smem, cudaStream_t s) {
+void cluster_config(cudaLaunchConfig_t* cfg, cudaLaunchAttribute* at, int ctas, int chunks, size_t smem, bool early, cudaStream_t s) {
   cfg->gridDim = dim3((unsigned)ctas);
   cfg->blockDim = dim3(kThreads);
   cfg->dynamicSmemBytes = smem;
@@ -703,10 +804,10 @@ void cluster_config(cudaLaunchConfig_t* cfg, cudaLaunchAttribute* at, int ctas, 
   at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[1].val.programmaticStreamSerializationAllowed = 1;
   cfg->attrs = at;
-  cfg->numAttrs = 2;
+  cfg->numAttrs = early ? 2 : 1;
 }
 
-size_t smem_of(const Plan& pl) { return ((size_t)pl.listed * 2 + (size_t)pl.blocks * kBlockWords * 2) * 4 + (size_t)pl.blocks * kBlockWords * 2; }
+size_t smem_of(const Plan& pl) { return (size_t)pl.listed * 8 + (size_t)pl.blocks * kBlockWords * 10; }
 
 // The plan of a call, spans excepted.  Shares of at least 32 blocks: with fewer the join would cost more than the row.
 Plan plan_of(const RulesArgs& a) {
@@ -740,13 +841,13 @@ bool plan_spans(const RulesArgs& a, Plan* pl) {
     spans = d->num_sms * kPerSm >> pl->lg;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute at[2];
-    cluster_config(&cfg, at, spans << pl->lg, pl->chunks, (smem + 1023) / 1024 * 1024, nullptr);
-    cfg.numAttrs = 1;
+    cluster_config(&cfg, at, spans << pl->lg, pl->chunks, (smem + 1023) / 1024 * 1024, false, nullptr);
     int n = 0;
     if (cudaOccupancyMaxActiveClusters(&n, conf_kernel<float>(true), &cfg) == cudaSuccess && n > 0) spans = n;
     else cudaGetLastError();
   }
   pl->spans = spans < a.n_rows ? spans : a.n_rows;
+  pl->early = 2 * pl->spans <= spans;
   return true;
 }
 
@@ -767,7 +868,7 @@ cudaError_t launch_rules_confidence(const RulesArgs& a, int* tok, float* conf, c
   const bool aligned = (a.ld * (a.bf16_logits ? 2 : 4)) % 16 == 0;
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute at[2];
-  cluster_config(&cfg, at, pl.spans * pl.chunks, pl.chunks, smem_of(pl), s);
+  cluster_config(&cfg, at, pl.spans * pl.chunks, pl.chunks, smem_of(pl), pl.early, s);
   return cudaLaunchKernelEx(&cfg, a.bf16_logits ? conf_kernel<bf16>(aligned) : conf_kernel<float>(aligned), a, pl, tok, conf);
 }
 
