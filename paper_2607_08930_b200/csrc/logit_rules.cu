@@ -65,13 +65,7 @@ __device__ __forceinline__ float exp2_fast(float x) {        // relative error 2
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
-// Loads that happen only if `on`, without a branch: a loop's loads then all leave before the first is waited for.
-__device__ __forceinline__ uint4 load4_if(const void* p, bool on, unsigned otherwise) {
-  uint4 u = make_uint4(otherwise, otherwise, otherwise, otherwise);
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %5, 0;\n\t@p ld.global.cs.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
-               : "+r"(u.x), "+r"(u.y), "+r"(u.z), "+r"(u.w) : "l"(p), "r"((unsigned)on));
-  return u;
-}
+// A load that happens only if `on`, without a branch: a loop's loads then all leave before the first is waited for.
 __device__ __forceinline__ unsigned load1_if(const void* p, bool on, unsigned otherwise) {
   unsigned u = otherwise;
   asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p ld.global.nc.u32 %0, [%1];\n\t}"
@@ -345,19 +339,18 @@ struct Row {
   int req, mask;
 };
 __device__ __forceinline__ Row row_of(const RulesArgs& a, int row) {
-  return Row{(int)load1_if(a.row_req + row, a.row_req != nullptr, (unsigned)row),
-             (int)load1_if(a.row_mask + row, a.allowed && a.row_mask, a.allowed ? (unsigned)row : 0xffffffffu)};
+  return Row{a.row_req ? __ldg(a.row_req + row) : row, a.allowed ? (a.row_mask ? __ldg(a.row_mask + row) : row) : -1};
 }
 __device__ __forceinline__ bool valid(const RulesArgs& a, const Row& r) {
   return r.req >= -1 && r.req < a.n_reqs && r.mask >= -1 && r.mask < a.n_masks;
 }
 
-// A block of a row as vectors of 16 bytes.  Rows at 16-byte boundaries: all of it.  Others: kPer vectors from entry
-// `first` of the block on, and E entries (before and behind) one by one.  Vectors that do not end within the vocabulary
-// are taken one by one, too.
+// A block of a row as vectors.  Rows at 32-byte boundaries: vectors of 32 bytes, all of it.  Others: kPer vectors of 16
+// bytes from entry `first` of the block on, and E entries (before and behind) one by one.  A vector that does not end
+// within the vocabulary is taken one by one, too.
 template <typename T, bool ALIGNED>
 struct Walk {
-  static constexpr int E = 16 / sizeof(T), kPer = kBlock / E - (ALIGNED ? 0 : 1);
+  static constexpr int kW = ALIGNED ? 8 : 4, E = kW * 4 / sizeof(T), kPer = kBlock / E - (ALIGNED ? 0 : 1);
   int first;
   __device__ __forceinline__ explicit Walk(const T* row)
       : first(ALIGNED ? 0 : (int)((E - (((uintptr_t)row & 15) / sizeof(T))) % E)) {}
@@ -365,7 +358,7 @@ struct Walk {
   // first entry of vector j of the CTA's share
   __device__ __forceinline__ int entry(int j) const { return ALIGNED ? j * E : j / kPer * kBlock + first + j % kPer * E; }
   // entry i of those taken one by one, -1: none (i < singles)
-  __device__ __forceinline__ int singles(const Plan& pl) const { return ALIGNED ? E : (pl.blocks + 1) * E; }
+  __device__ __forceinline__ int singles(const Plan& pl, const Table& t) const { return ALIGNED ? (t.vocab % E ? E : 0) : (pl.blocks + 1) * E; }
   __device__ __forceinline__ int single(const Plan& pl, const Table& t, int i) const {
     int e;
     if (i < E) {                                             // the end of the vocabulary, where it is in a vector's middle
@@ -411,42 +404,73 @@ __device__ __forceinline__ void join_one(Part& p, float y, int at) {
 
 // ---- vectors -------------------------------------------------------------------------------------------------
 
+template <int N>
+struct Vec {
+  unsigned w[N];
+};
+__device__ __forceinline__ void load(const void* p, Vec<4>& u) {
+  asm volatile("ld.global.cs.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(u.w[0]), "=r"(u.w[1]), "=r"(u.w[2]), "=r"(u.w[3]) : "l"(p));
+}
+__device__ __forceinline__ void load(const void* p, Vec<8>& u) {
+  asm volatile("ld.global.cs.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(u.w[0]), "=r"(u.w[1]), "=r"(u.w[2]), "=r"(u.w[3]), "=r"(u.w[4]), "=r"(u.w[5]), "=r"(u.w[6]), "=r"(u.w[7])
+               : "l"(p));
+}
+__device__ __forceinline__ void store(void* p, const Vec<4>& u) {
+  asm volatile("st.global.cs.v4.b32 [%0], {%1, %2, %3, %4};" ::"l"(p), "r"(u.w[0]), "r"(u.w[1]), "r"(u.w[2]), "r"(u.w[3]) : "memory");
+}
+__device__ __forceinline__ void store(void* p, const Vec<8>& u) {
+  asm volatile("st.global.cs.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"l"(p), "r"(u.w[0]), "r"(u.w[1]), "r"(u.w[2]), "r"(u.w[3]), "r"(u.w[4]), "r"(u.w[5]), "r"(u.w[6]), "r"(u.w[7]) : "memory");
+}
+
 template <typename T>
 constexpr unsigned kLeast = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;     // a word of -inf
 
-// Entries without their bit (of the low E) become -inf.  A product puts four bits at the tops of four bytes (the shifted
-// copies do not meet), from where a byte permutation spreads them over a word: two instructions an entry instead of three.
-template <typename T>
-__device__ __forceinline__ uint4 only(uint4 u, unsigned bits) {
-  unsigned w[4] = {u.x, u.y, u.z, u.w};
-  const unsigned lo = (bits & 15u) * 0x10204080u, hi = sizeof(T) == 4 ? lo : (bits >> 4 & 15u) * 0x10204080u;
+// Entries without their bit (the lowest is the first's) become -inf.  A product puts four bits at the tops of four bytes
+// (the shifted copies do not meet), from where a byte permutation spreads them over a word: two instructions a word.
+template <typename T, int N>
+__device__ __forceinline__ void only(Vec<N>& u, unsigned bits) {
+  constexpr int kPerWord = 4 / sizeof(T), kGroup = 4 / kPerWord;             // words that four bits decide about
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    unsigned keep;                                           // (the permutation's upper selectors repeat a byte's top bit)
-    if (sizeof(T) == 4) asm("prmt.b32 %0, %1, %1, %2;" : "=r"(keep) : "r"(lo), "r"(0x8888u + 0x1111u * i));
-    else asm("prmt.b32 %0, %1, %1, %2;" : "=r"(keep) : "r"(i < 2 ? lo : hi), "r"(i & 1 ? 0xbbaau : 0x9988u));
-    w[i] = (w[i] & keep) | (kLeast<T> & ~keep);
+  for (int g = 0; g < N / kGroup; ++g) {
+    const unsigned tops = (bits >> (4 * g) & 15u) * 0x10204080u;
+#pragma unroll
+    for (int i = 0; i < kGroup; ++i) {
+      unsigned keep;                                         // (the permutation's selectors repeat a byte's top bit)
+      asm("prmt.b32 %0, %1, %1, %2;" : "=r"(keep) : "r"(tops), "r"(sizeof(T) == 4 ? 0x8888u + 0x1111u * i : (i ? 0xbbaau : 0x9988u)));
+      unsigned& w = u.w[g * kGroup + i];
+      w = (w & keep) | (kLeast<T> & ~keep);
+    }
   }
-  return make_uint4(w[0], w[1], w[2], w[3]);
 }
 // The largest entry (NaN are passed over).
-__device__ __forceinline__ float largest(const uint4& u, const float*) {
-  return fmaxf(fmaxf(__uint_as_float(u.x), __uint_as_float(u.y)), fmaxf(__uint_as_float(u.z), __uint_as_float(u.w)));
+template <int N>
+__device__ __forceinline__ float largest(const Vec<N>& u, const float*) {
+  float m = __uint_as_float(u.w[0]);
+#pragma unroll
+  for (int i = 1; i < N; ++i) m = fmaxf(m, __uint_as_float(u.w[i]));
+  return m;
 }
-__device__ __forceinline__ float largest(const uint4& u, const bf16*) {
-  const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&u);
-  const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+template <int N>
+__device__ __forceinline__ float largest(const Vec<N>& u, const bf16*) {
+  const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(u.w);
+  __nv_bfloat162 m = h[0];
+#pragma unroll
+  for (int i = 1; i < N; ++i) m = __hmax2(m, h[i]);
   return fmaxf(__low2float(m), __high2float(m));
 }
-__device__ __forceinline__ void widen(const uint4& u, float* v, const float*) {
-  v[0] = __uint_as_float(u.x); v[1] = __uint_as_float(u.y); v[2] = __uint_as_float(u.z); v[3] = __uint_as_float(u.w);
-}
-__device__ __forceinline__ void widen(const uint4& u, float* v, const bf16*) {
-  const unsigned w[4] = {u.x, u.y, u.z, u.w};
+template <int N>
+__device__ __forceinline__ void widen(const Vec<N>& u, float* v, const float*) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[2 * i] = __uint_as_float(w[i] << 16);
-    v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  for (int i = 0; i < N; ++i) v[i] = __uint_as_float(u.w[i]);
+}
+template <int N>
+__device__ __forceinline__ void widen(const Vec<N>& u, float* v, const bf16*) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    v[2 * i] = __uint_as_float(u.w[i] << 16);
+    v[2 * i + 1] = __uint_as_float(u.w[i] & 0xffff0000u);
   }
 }
 // s (two partial sums) += exp(v - ref), two entries an instruction up to the exponential.  The difference comes first: one
@@ -477,12 +501,13 @@ __device__ __forceinline__ unsigned long long pair_of(float x) {
 template <typename T, bool ALIGNED>
 __global__ void __launch_bounds__(kThreads, kPerSm) k_rules_confidence(const RulesArgs a, const Plan pl, int* tok, float* conf) {
   using W = Walk<T, ALIGNED>;
-  constexpr int E = W::E, kBatch = E == 4 ? 5 : 4;           // vectors a thread has in flight
+  constexpr int E = W::E, kBatch = ALIGNED ? 2 : 4;          // vectors a thread has in flight
   constexpr unsigned kAll = (1u << E) - 1u;
   extern __shared__ __align__(16) unsigned smem[];
   __shared__ Slot parts[kRowsAtOnce * kWarps];               // of the rows that this CTA joins: [row][chunk][warp]
   __shared__ __align__(8) unsigned long long s_bar;
   __shared__ unsigned s_top[kRowsAtOnce];                    // the largest maximum that a warp has left so far, ordered
+  __shared__ Row s_rows[kRowsAtOnce];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if (threadIdx.x == 0) {
     tc::mbar_init(tc::smem_u32(&s_bar), 1);
@@ -500,7 +525,6 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_rules_confidence(const Rul
   const unsigned long long log2e = pair_of(kLog2e);
   const int step = (kThreads * E) << pl.lg;                  // tokens between two vectors of a thread
   int cur = -2;
-  Row next = row_of(a, r0);
   cluster_wait();                                            // the others' barriers are there
   for (int rb = r0; rb < r1; rb += kRowsAtOnce, turn ^= 1u) {
     const int re = min(r1, rb + kRowsAtOnce);
@@ -511,11 +535,13 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_rules_confidence(const Rul
       cluster_wait();
     }
     if (threadIdx.x == 0 && joins > 0) tc::mbar_expect_tx(tc::smem_u32(&s_bar), (unsigned)(joins * pl.chunks * kWarps * sizeof(Slot)));
-    if (threadIdx.x < kRowsAtOnce) s_top[threadIdx.x] = 0u;
+    if (threadIdx.x < kRowsAtOnce) {
+      s_top[threadIdx.x] = 0u;
+      if (rb + (int)threadIdx.x < re) s_rows[threadIdx.x] = row_of(a, rb + threadIdx.x);
+    }
     __syncthreads();
     for (int row = rb; row < re; ++row) {
-      const Row me = next;
-      if (row + 1 < r1) next = row_of(a, row + 1);
+      const Row me = s_rows[row - rb];
       const unsigned joiner = (unsigned)(row - rb) & (unsigned)(pl.chunks - 1);
       const Slot* slot = &parts[(((row - rb) >> pl.lg << pl.lg) + chunk) * kWarps + warp];
       if (!valid(a, me)) {
@@ -546,7 +572,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_rules_confidence(const Rul
         const unsigned* words = mask + (id0 >> 5);
         for (int j0 = threadIdx.x; j0 < nv; j0 += kThreads * kBatch, e0 += kThreads * E * kBatch, id0 += step * kBatch, words += (step >> 5) * kBatch) {
           unsigned bits[kBatch], every = 0xffffffffu;
-          uint4 u[kBatch];
+          Vec<W::kW> u[kBatch];
           // aligned rows: a thread's vectors are whole blocks apart, those that are not there lie behind the vocabulary
           const int left = ALIGNED ? t.vocab - E - id0 : 0;
 #pragma unroll
@@ -554,8 +580,9 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_rules_confidence(const Rul
             const int e = ALIGNED ? e0 + b * kThreads * E : walk.entry(min(j0 + b * kThreads, nv - 1));
             const int id = ALIGNED ? id0 + b * step : t.id_of(e);
             const bool there = ALIGNED ? b * step <= left : id <= t.vocab - E && j0 + b * kThreads < nv;
-            u[b] = make_uint4(kLeast<T>, kLeast<T>, kLeast<T>, kLeast<T>);      // (what is not there is -inf)
-            if (there) u[b] = __ldcs(reinterpret_cast<const uint4*>(z + id));
+#pragma unroll
+            for (int i = 0; i < W::kW; ++i) u[b].w[i] = kLeast<T>;               // (what is not there is -inf)
+            if (there) load(z + id, u[b]);
             if (ALIGNED) {
               bits[b] = masked.value ? 0u : 0xffffffffu;
               if (masked.value && there) bits[b] = __ldg(words + b * (step >> 5));
@@ -570,7 +597,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_rules_confidence(const Rul
           }
           if (masked.value || ((every >> shift) & kAll) != kAll) {
 #pragma unroll
-            for (int b = 0; b < kBatch; ++b) u[b] = only<T>(u[b], bits[b] >> shift);
+            for (int b = 0; b < kBatch; ++b) only<T>(u[b], bits[b] >> shift);
           }
           float top = largest(u[0], z);
 #pragma unroll
@@ -610,7 +637,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_rules_confidence(const Rul
       asm("mov.b64 {%0, %1}, %2;" : "=f"(s), "=f"(s_odd) : "l"(s2));
       s += s_odd;
       Part one{-INFINITY, 0.f, 0x7fffffff};                  // entries beside the vectors
-      for (int i = threadIdx.x; i < walk.singles(pl); i += kThreads) {
+      for (int i = threadIdx.x; i < walk.singles(pl, t); i += kThreads) {
         const int e = walk.single(pl, t, i);
         if (e >= 0 && ((usable(e >> 5) >> (e & 31)) & 1u)) {
           const int id = t.id_of(e);
@@ -682,7 +709,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_rules_confidence(const Rul
 template <typename T, bool ALIGNED, bool INPLACE>
 __global__ void __launch_bounds__(kThreads, kPerSm) k_logit_rules(const RulesArgs a, const Plan pl, T* out, long long out_ld) {
   using W = Walk<T, ALIGNED>;
-  constexpr int E = W::E, kBatch = 4;
+  constexpr int E = W::E, kBatch = ALIGNED ? 2 : 4;
   constexpr unsigned kAll = (1u << E) - 1u;
   extern __shared__ __align__(16) unsigned smem[];
   pdl_wait();
@@ -691,11 +718,15 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logit_rules(const RulesArg
   const int r0 = (int)((long long)a.n_rows * span / pl.spans), r1 = (int)((long long)a.n_rows * (span + 1) / pl.spans);
   const int step = (kThreads * E) << pl.lg;                  // tokens between two vectors of a thread
   Table t = make_table(a, pl, chunk, smem);
+  __shared__ Row s_rows[kRowsAtOnce];
   int cur = -2;
-  Row next = row_of(a, r0);
   for (int row = r0; row < r1; ++row) {
-    const Row me = next;
-    if (row + 1 < r1) next = row_of(a, row + 1);
+    if ((row - r0) % kRowsAtOnce == 0) {
+      __syncthreads();
+      if (threadIdx.x < kRowsAtOnce && row + (int)threadIdx.x < r1) s_rows[threadIdx.x] = row_of(a, row + threadIdx.x);
+      __syncthreads();
+    }
+    const Row me = s_rows[(row - r0) % kRowsAtOnce];
     if (!valid(a, me)) {
       if (threadIdx.x == 0 && chunk == 0) raise(a);
       continue;
@@ -718,14 +749,14 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logit_rules(const RulesArg
     const int nv = walk.vectors(pl);
     int e0 = walk.entry(threadIdx.x), id0 = t.id_of(e0);
     for (int j0 = threadIdx.x; j0 < nv; j0 += kThreads * kBatch, e0 += kThreads * E * kBatch, id0 += step * kBatch) {
-      uint4 u[kBatch];
+      Vec<W::kW> u[kBatch];
       unsigned keep[kBatch], calm[kBatch];
 #pragma unroll
       for (int b = 0; b < kBatch; ++b) {
         const int e = ALIGNED ? e0 + b * kThreads * E : walk.entry(min(j0 + b * kThreads, nv - 1));
         const int id = ALIGNED ? id0 + b * step : t.id_of(e);
         const bool there = id <= t.vocab - E && (ALIGNED || j0 + b * kThreads < nv);
-        u[b] = load4_if(z + id, !INPLACE && there, 0u);
+        if (!INPLACE && there) load(z + id, u[b]);
         if (ALIGNED) {
           const unsigned m = load1_if(mask + (id >> 5), mask && there, 0xffffffffu);
           calm[b] = (t.plain[e >> 5] >> (e & 31)) & kAll;
@@ -740,19 +771,24 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logit_rules(const RulesArg
         const int id = ALIGNED ? id0 + b * step : t.id_of(walk.entry(min(j0 + b * kThreads, nv - 1)));
         if (id > t.vocab - E || (!ALIGNED && j0 + b * kThreads >= nv)) continue;
         const unsigned now = (INPLACE ? 0u : calm[b] & keep[b]) | (kAll & ~keep[b]);      // the others are written below
-        const uint4 x = keep[b] == kAll ? u[b] : only<T>(u[b], keep[b]);
+        if (INPLACE) {
+#pragma unroll
+          for (int i = 0; i < W::kW; ++i) u[b].w[i] = kLeast<T>;
+        } else if (keep[b] != kAll) {
+          only<T>(u[b], keep[b]);
+        }
         if (now == kAll && (ALIGNED || INPLACE)) {
-          __stcs(reinterpret_cast<uint4*>(y + id), x);
+          store(y + id, u[b]);
         } else if (now) {
           float v[E];
-          widen(x, v, z);
+          widen(u[b], v, z);
 #pragma unroll
           for (int e = 0; e < E; ++e)
             if ((now >> e) & 1u) put(y + id + e, v[e]);
         }
       }
     }
-    for (int i = threadIdx.x; i < walk.singles(pl); i += kThreads) {
+    for (int i = threadIdx.x; i < walk.singles(pl, t); i += kThreads) {
       const int e = walk.single(pl, t, i);
       if (e >= 0) {
         const int id = t.id_of(e);
@@ -853,7 +889,8 @@ bool plan_spans(const RulesArgs& a, Plan* pl) {
 
 template <typename T>
 cudaError_t launch_rules(const RulesArgs& a, const Plan& pl, T* out, long long out_ld, cudaStream_t s) {
-  const bool aligned = (a.ld * sizeof(T)) % 16 == 0 && (out_ld * sizeof(T)) % 16 == 0, inplace = out == a.logits;
+  const bool aligned = (((uintptr_t)a.logits | (uintptr_t)out | (uintptr_t)(a.ld * sizeof(T)) | (uintptr_t)(out_ld * sizeof(T))) & 31) == 0;
+  const bool inplace = out == a.logits;
   RuleKernel<T> k = inplace ? (aligned ? k_logit_rules<T, true, true> : k_logit_rules<T, false, true>)
                             : (aligned ? k_logit_rules<T, true, false> : k_logit_rules<T, false, false>);
   return launch_pdl(k, dim3((unsigned)(pl.spans * pl.chunks)), dim3(kThreads), smem_of(pl), s, a, pl, out, out_ld);
@@ -865,7 +902,7 @@ cudaError_t launch_rules_confidence(const RulesArgs& a, int* tok, float* conf, c
   if (a.n_rows <= 0) return cudaSuccess;
   Plan pl = plan_of(a);
   if (!plan_spans(a, &pl)) return cudaErrorNotSupported;
-  const bool aligned = (a.ld * (a.bf16_logits ? 2 : 4)) % 16 == 0;
+  const bool aligned = (((uintptr_t)a.logits | (uintptr_t)(a.ld * (a.bf16_logits ? 2 : 4))) & 31) == 0;
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute at[2];
   cluster_config(&cfg, at, pl.spans * pl.chunks, pl.chunks, smem_of(pl), pl.early, s);
