@@ -570,8 +570,13 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_rules_confidence(const Rul
         int e0 = walk.entry(threadIdx.x), id0 = t.id_of(e0);
         const unsigned shift = ALIGNED ? e0 & 31 : 0;        // (the same for all of a thread's vectors)
         const unsigned* words = mask + (id0 >> 5);
+        unsigned ahead[kBatch];                              // the mask's words of the next batch
+        if (ALIGNED && masked.value) {
+#pragma unroll
+          for (int b = 0; b < kBatch; ++b) ahead[b] = load1_if(words + b * (step >> 5), b * step <= t.vocab - E - id0, 0u);
+        }
         for (int j0 = threadIdx.x; j0 < nv; j0 += kThreads * kBatch, e0 += kThreads * E * kBatch, id0 += step * kBatch, words += (step >> 5) * kBatch) {
-          unsigned bits[kBatch], every = 0xffffffffu;
+          unsigned bits[kBatch], every = 0xffffffffu, any = 0u;
           Vec<W::kW> u[kBatch];
           // aligned rows: a thread's vectors are whole blocks apart, those that are not there lie behind the vocabulary
           const int left = ALIGNED ? t.vocab - E - id0 : 0;
@@ -582,14 +587,24 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_rules_confidence(const Rul
             const bool there = ALIGNED ? b * step <= left : id <= t.vocab - E && j0 + b * kThreads < nv;
 #pragma unroll
             for (int i = 0; i < W::kW; ++i) u[b].w[i] = kLeast<T>;               // (what is not there is -inf)
-            if (there) load(z + id, u[b]);
             if (ALIGNED) {
-              bits[b] = masked.value ? 0u : 0xffffffffu;
-              if (masked.value && there) bits[b] = __ldg(words + b * (step >> 5));
+              bits[b] = masked.value ? ahead[b] : 0xffffffffu;
               if (masked.value || there) bits[b] &= t.plain[e >> 5];
+              if (masked.value) bits[b] = bits[b] >> shift & kAll;
+              // a grammar often leaves a handful of tokens: vectors without any are not read
+              if (masked.value ? bits[b] != 0u : there) load(z + id, u[b]);
             } else {
+              if (there) load(z + id, u[b]);
               bits[b] = bits_at<E, false>(e, usable) | (there ? 0u : kAll);
             }
+          }
+          if (ALIGNED && masked.value) {
+#pragma unroll
+            for (int b = 0; b < kBatch; ++b) {
+              any |= bits[b];
+              ahead[b] = load1_if(words + (kBatch + b) * (step >> 5), (kBatch + b) * step <= left && j0 + (kBatch + b) * kThreads < nv, 0u);
+            }
+            if (!any) continue;
           }
           if (!masked.value) {
 #pragma unroll
@@ -597,7 +612,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_rules_confidence(const Rul
           }
           if (masked.value || ((every >> shift) & kAll) != kAll) {
 #pragma unroll
-            for (int b = 0; b < kBatch; ++b) only<T>(u[b], bits[b] >> shift);
+            for (int b = 0; b < kBatch; ++b) only<T>(u[b], masked.value ? bits[b] : bits[b] >> shift);
           }
           float top = largest(u[0], z);
 #pragma unroll
