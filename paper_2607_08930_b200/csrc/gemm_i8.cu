@@ -10,9 +10,10 @@
 //   warps 2..9   epilogue: warp w reads TMEM lanes 32 (w mod 4) ..; its two groups of four take alternate token chunks
 // CG = 2: two CTAs of a cluster share every instruction (256 weight rows) and each stages half of the tokens, which
 // takes a quarter off the bytes a CTA loads for an operation.
-// SPLIT: a projection with fewer tiles than SMs has the k range of each tile shared by the CTAs (pairs) of one cluster;
-// they add their partial sums over distributed shared memory.  Integer sums are exact, so the order does not matter and
-// the result does not depend on the split.
+// SPLIT: a projection with fewer tiles than SMs has the k range of each tile shared by the CTAs (pairs) of one cluster.
+// Chunk c (8 tokens) of the tile is finished by split c mod S: the others write their partial sums of it to that CTA's
+// shared memory, which counts the bytes on a barrier.  Integer sums are exact, so the order does not matter and the result
+// does not depend on the split.
 // Every wait is bounded: one that runs out raises the error flag and leaves NaN in the outputs that it kept from being
 // formed; all roles drain and TMEM is freed.
 #include <math.h>
@@ -31,7 +32,8 @@ using namespace tc;
 constexpr int BKB = 128;                  // bytes = codes of a k step
 constexpr int kTileRows = 128;            // weight rows of a CTA
 constexpr int kThreads = 320;
-constexpr int kRing = 196 * 1024;         // operand stages
+constexpr int kRing = 196 * 1024;         // operand stages and, behind them, received partial sums
+constexpr int kChunk = 8;                 // tokens of a chunk that one split finishes
 constexpr int kMaxStages = 12;
 constexpr int kAccCols = 256;             // TMEM columns of an accumulator buffer (two of them)
 
@@ -39,6 +41,7 @@ struct Params {
   int M, N, K;
   int tn;                   // tokens of a tile
   int n_tiles, m_tiles, splits, kblocks, stages;
+  int received;             // offset of the received partial sums
   int nbuf;                 // accumulator buffers
   int mgroup;               // token tiles per group of the item order (0: token tile fastest over all)
   int vec;                  // bf16 rows take 16-byte stores
@@ -70,6 +73,9 @@ __device__ __forceinline__ void load_tile(unsigned dst, const CUtensorMap* map, 
     asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes "
                  "[%0], [%1, {%2, %3}], [%4];"
                  ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void prefetch_tile(const CUtensorMap* map, int c0, int c1) {
+  asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global [%0, {%1, %2}];" ::"l"(map), "r"(c0), "r"(c1) : "memory");
 }
 // kind::i8: signed 8-bit A and B, both K-major, 32-bit integer accumulator, shape (128 CG) x n x 32.
 template <int CG>
@@ -109,6 +115,24 @@ __device__ __forceinline__ void tmem_ld8(unsigned taddr, int* r) {
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
                : "r"(taddr));
   tmem_ld_wait();
+}
+// Writes 16 bytes to a CTA of the cluster and counts them on its barrier.
+__device__ __forceinline__ void send16(unsigned to, unsigned bar, const int* v) {
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];"
+               ::"r"(to), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(bar) : "memory");
+}
+__device__ __forceinline__ bool wait_received(unsigned bar, volatile int* abort_flag) {
+  const long long t0 = clock64();
+  for (;;) {
+    unsigned ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], 0;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(bar) : "memory");
+    if (ok) return true;
+    if (clock64() - t0 > 3 * kWaitCycles) {                 // (the others' own waits come first)
+      *abort_flag = 1;
+      return false;
+    }
+  }
 }
 
 // Output tiles are numbered token tile fastest (the CTAs of a round then share weight tiles in L2); with mgroup the
@@ -188,8 +212,8 @@ k_gemm_i8(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUt
   constexpr int kW = kDual ? 2 : 1;
   constexpr int kWBytes = kTileRows * BKB;
   extern __shared__ unsigned char smem_dyn[];
-  __shared__ __align__(8) unsigned long long bars[2 * kMaxStages + 5];    // full, empty, accumulator full, empty; drain
-  __shared__ __align__(16) bf16 out_tile[(MODE == 0 || MODE == 3) ? 8 : 1][32 * 32];
+  __shared__ __align__(8) unsigned long long bars[2 * kMaxStages + 6];    // full, empty, accumulator full, empty; drain, received
+  __shared__ __align__(16) bf16 out_tile[(MODE == 0 || MODE == 3) ? 8 : 1][(SPLIT ? kChunk : 32) * 32];
   __shared__ __align__(16) float tok_scale[8][32];
   __shared__ unsigned tmem_slot;
   __shared__ int s_abort;
@@ -206,7 +230,7 @@ k_gemm_i8(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUt
   const int stage_bytes = kW * kWBytes + x_rows * BKB;
   const unsigned full0 = smem_u32(&bars[0]), empty0 = smem_u32(&bars[kMaxStages]);
   const unsigned tfull0 = smem_u32(&bars[2 * kMaxStages]), tempty0 = smem_u32(&bars[2 * kMaxStages + 2]);
-  const unsigned drain = smem_u32(&bars[2 * kMaxStages + 4]);
+  const unsigned drain = smem_u32(&bars[2 * kMaxStages + 4]), got = smem_u32(&bars[2 * kMaxStages + 5]);
   const unsigned full_lead0 = CG == 2 ? in_cta(full0, lead) : full0;
   const unsigned tempty_lead0 = CG == 2 ? in_cta(tempty0, lead) : tempty0;
   const unsigned peer_abort = CG == 2 ? in_cta(smem_u32(&s_abort), rank ^ 1u) : 0u;
@@ -222,6 +246,7 @@ k_gemm_i8(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUt
       mbar_init(empty0 + 8 * i, 1);
     }
     mbar_init(drain, 1);
+    mbar_init(got, 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(tfull0 + 8 * i, 1);
       mbar_init(tempty0 + 8 * i, 8 * CG);
@@ -239,12 +264,19 @@ k_gemm_i8(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUt
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
-  if (CG == 2) cluster_barrier();                           // the partner's barriers exist before anything signals them
+  if (CG == 2 || SPLIT) cluster_barrier();                  // the others' barriers exist before anything signals them
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const unsigned tmem = tmem_slot;
   volatile int* abort_flag = &s_abort;
   // (the tensor memory is held: a kernel behind that allocates its own before it waits cannot keep this one from it)
   pdl_trigger();
+  if (warp == 0 && lane < p.stages && kb0 + lane < kb1 && worker < items) {
+    // the first weight tiles come to L2 meanwhile (the kernel before may write them: they are not read before it ends)
+    int mt, nt;
+    tile_of(p, worker, &mt, &nt);
+    prefetch_tile(&map_w, (kb0 + lane) * BKB, (nt * CG + (int)half) * kTileRows);
+    if (kDual) prefetch_tile(&map_w2, (kb0 + lane) * BKB, (nt * CG + (int)half) * kTileRows);
+  }
   pdl_wait();                                               // codes, scales and outputs may come from the kernel before
 
   if (warp == 0) {
@@ -375,80 +407,86 @@ k_gemm_i8(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUt
     if (CG == 2 && !ok && lane == 0) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(peer_abort), "r"(1) : "memory");
   }
 
-  if (SPLIT) {
-    // One item per cluster.  Chunk c (8 tokens) of the tile belongs to split c mod S: every CTA sends its partial sums of
-    // the others' chunks into their idle operand rings, and finishes its own.  All threads reach both barriers whatever
-    // happened before, so no CTA is left waiting.
+  if (SPLIT && warp >= 2) {
+    // ---------------------------------------------------------------- epilogue of a split tile (one for each cluster)
     const int S = p.splits;
     int mt, nt;
     tile_of(p, worker, &mt, &nt);
     const int limit = min(p.tn, p.M - mt * p.tn);
-    const int chunks = (limit + 7) / 8, own = (chunks + S - 1) / S;       // chunks a CTA may own
-    const int q = warp & 3, group = (warp - 2) >> 2;
-    const int feature = q * 32 + lane;
+    const int chunks = (limit + kChunk - 1) / kChunk;
+    const int mine = (chunks - split + S - 1) / S;           // chunks that this CTA finishes
+    const int own = (chunks + S - 1) / S;                    // and the most that one does
+    const int q = warp & 3, group = (warp - 2) >> 2, feature = q * 32 + lane;
     const unsigned row = tmem + ((unsigned)(q * 32) << 16);
-    bool ok = true;
-    __syncwarp();                                           // the role branches above end here
-    if (warp >= 2) {
-      ok = mbar_wait(tfull0, 0u, abort_flag);
-      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    if (warp == 2 && lane == 0) mbar_expect_tx(got, (unsigned)((S - 1) * mine * kChunk * kTileRows * 4));
+    bool ok = mbar_wait(tfull0, 0u, abort_flag);
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    for (int c = group; c < chunks; c += 2) {
+      const int owner = c % S;
+      if (owner == split) continue;
+      int z[8];
+      tmem_ld8(row + c * kChunk, z);
+      // a partial sum that is not there is sent as the least integer: no sum of fewer than 131072 products reaches it
+      if (!ok) z[0] = (int)0x80000000;
+      const int slot = split < owner ? split : split - 1;
+      const unsigned rank_of = (unsigned)(owner * CG) + half;
+      const unsigned to = in_cta(smem0 + (unsigned)p.received + (unsigned)(((slot * own + c / S) * 2 * kTileRows + feature) * 16), rank_of);
+      const unsigned bar = in_cta(got, rank_of);
+      send16(to, bar, z);
+      send16(to + kTileRows * 16, bar, z + 4);
     }
-    __syncthreads();
-    cluster_barrier();
-    if (warp >= 2) {
-      for (int c = group; c < chunks; c += 2) {
-        const int owner = c % S;
-        if (owner == split) continue;
-        int z[8];
-        tmem_ld8(row + c * 8, z);
-        // a partial sum that is not there is sent as the least integer: no sum of fewer than 131072 products reaches it
-        if (!ok) z[0] = z[1] = z[2] = z[3] = z[4] = z[5] = z[6] = z[7] = (int)0x80000000;
-        const int slot = split < owner ? split : split - 1;
-        const unsigned to = in_cta(smem0 + (unsigned)(((slot * own + c / S) * kTileRows + feature) * 32),
-                                   (unsigned)(owner * CG) + half);
-        asm volatile("st.shared::cluster.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(z[0]), "r"(z[1]), "r"(z[2]), "r"(z[3]) : "memory");
-        asm volatile("st.shared::cluster.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(to + 16), "r"(z[4]), "r"(z[5]), "r"(z[6]), "r"(z[7]) : "memory");
-      }
-    }
-    cluster_barrier();
-    if (warp >= 2) {
-      const int n = (nt * CG + (int)half) * kTileRows + feature;
-      const float w = n < p.N ? __ldg(p.sw + n) : 0.f;
-      for (int i = group; i * S + split < chunks; i += 2) {
-        const int c = i * S + split, t0 = mt * p.tn + c * 8, jmax = min(8, limit - c * 8);
-        int z[8];
-        tmem_ld8(row + c * 8, z);
-        bool whole = ok;
-        for (int slot = 0; slot < S - 1; ++slot) {
-          const unsigned from = smem0 + (unsigned)(((slot * own + i) * kTileRows + feature) * 32);
-          int y[8];
-          asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(y[0]), "=r"(y[1]), "=r"(y[2]), "=r"(y[3]) : "r"(from) : "memory");
-          asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(y[4]), "=r"(y[5]), "=r"(y[6]), "=r"(y[7]) : "r"(from + 16) : "memory");
-          whole = whole && y[0] != (int)0x80000000;
+    const int n = (nt * CG + (int)half) * kTileRows + feature;
+    const float w = n < p.N ? __ldg(p.sw + n) : 0.f;
+    const bool here = mine == 0 || wait_received(got, abort_flag);
+    for (int i = group; i < mine; i += 2) {
+      const int c = i * S + split, t0 = mt * p.tn + c * kChunk, jmax = min(kChunk, limit - c * kChunk);
+      const float s = lane < jmax ? __ldg(p.sa + t0 + lane) : 0.f;
+      int z[8];
+      tmem_ld8(row + c * kChunk, z);
+      bool whole = ok && here;
+      for (int slot = 0; slot < S - 1; ++slot) {
+        const unsigned from = smem0 + (unsigned)p.received + (unsigned)(((slot * own + i) * 2 * kTileRows + feature) * 16);
+        int y[8];
+        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(y[0]), "=r"(y[1]), "=r"(y[2]), "=r"(y[3]) : "r"(from) : "memory");
+        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(y[4]), "=r"(y[5]), "=r"(y[6]), "=r"(y[7]) : "r"(from + kTileRows * 16) : "memory");
+        whole = whole && y[0] != (int)0x80000000;
 #pragma unroll
-          for (int j = 0; j < 8; ++j) z[j] += y[j];
-        }
-        if (n < p.N) {
-          float v[8];
+        for (int j = 0; j < 8; ++j) z[j] += y[j];
+      }
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        v[j] = (float)z[j] * w * __shfl_sync(0xffffffffu, s, j);
+        if (!whole) v[j] = __uint_as_float(0x7fffffffu);
+      }
+      if (MODE == 0 && p.vec) {
+        bf16* tile = out_tile[warp - 2];
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 8; ++j) tile[j * 32 + lane] = __float2bfloat16_rn(v[j]);
+        __syncwarp();
+        const int tok = lane >> 2, piece = lane & 3, nb = n - lane + piece * 8;
+        if (nb < p.N && tok < jmax)                          // N is a multiple of 8 here
+          *reinterpret_cast<uint4*>(static_cast<bf16*>(p.C) + (long long)(t0 + tok) * p.ldc + nb) =
+              *reinterpret_cast<const uint4*>(tile + tok * 32 + piece * 8);
+      } else if (n < p.N) {
+        if (MODE == 0) {
+          bf16* o = static_cast<bf16*>(p.C) + (long long)t0 * p.ldc + n;
 #pragma unroll
           for (int j = 0; j < 8; ++j)
-            v[j] = whole ? (float)z[j] * w * (j < jmax ? __ldg(p.sa + t0 + j) : 0.f) : __uint_as_float(0x7fffffffu);
-          if (MODE == 0) {
-            bf16* o = static_cast<bf16*>(p.C) + (long long)t0 * p.ldc + n;
+            if (j < jmax) o[(long long)j * p.ldc] = __float2bfloat16_rn(v[j]);
+        } else {
+          float* o = static_cast<float*>(p.C) + (long long)t0 * p.ldc + n;
+          if (MODE == 1) {
+            float u[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-              if (j < jmax) o[(long long)j * p.ldc] = __float2bfloat16_rn(v[j]);
-          } else {
-            float* o = static_cast<float*>(p.C) + (long long)t0 * p.ldc + n;
-            if (MODE == 1) {
+            for (int j = 0; j < 8; ++j) u[j] = j < jmax ? o[(long long)j * p.ldc] : 0.f;
 #pragma unroll
-              for (int j = 0; j < 8; ++j)
-                if (j < jmax) v[j] += o[(long long)j * p.ldc];
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-              if (j < jmax) o[(long long)j * p.ldc] = v[j];
+            for (int j = 0; j < 8; ++j) v[j] += u[j];
           }
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (j < jmax) o[(long long)j * p.ldc] = v[j];
         }
       }
     }
@@ -562,14 +600,16 @@ cudaError_t launch_gemm_i8(const GemmI8Args& a, cudaStream_t s) {
   }
   pl.nbuf = dual && pl.tn > 128 ? 1 : 2;
   const int stage_bytes = (dual ? 2 : 1) * kTileRows * BKB + pl.tn / pl.cg * BKB;
-  pl.stages = kRing / stage_bytes;
+  const int own = (pl.tn / kChunk + pl.splits - 1) / pl.splits;
+  const int received = (pl.splits - 1) * own * kChunk * kTileRows * 4;
+  pl.stages = (kRing - received) / stage_bytes;
   if (pl.stages > kMaxStages) pl.stages = kMaxStages;
   const int most = pl.cg == 2 ? dv->clusters[2] : dv->num_sms;
   pl.workers = (int)(items < most ? items : most);
 
   Params p;
   p.M = a.M; p.N = a.N; p.K = a.K; p.tn = pl.tn; p.n_tiles = pl.n_tiles; p.m_tiles = pl.m_tiles; p.splits = pl.splits;
-  p.kblocks = kblocks; p.stages = pl.stages; p.nbuf = pl.nbuf;
+  p.kblocks = kblocks; p.stages = pl.stages; p.nbuf = pl.nbuf; p.received = pl.stages * stage_bytes;
   p.mgroup = (long long)a.M * a.K > (56ll << 20) && pl.m_tiles > 16 ? 16 : 0;
   p.vec = a.ldc % 8 == 0 && a.N % 8 == 0 && ((uintptr_t)a.C & 15) == 0;
   p.C = a.C; p.ldc = a.ldc; p.sa = a.sa; p.sw = a.sw; p.sw2 = a.sw2; p.error_flag = a.error_flag;
