@@ -368,6 +368,15 @@ k_gemm_i8(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUt
       const unsigned row = tmem + ((unsigned)(q * 32) << 16) + acc * kAccCols;
       const unsigned second = p.nbuf == 2 ? kAccCols / 2 : kAccCols;
       const int limit = min(p.tn, p.M - mt * p.tn);
+      auto release = [&]() {
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+          if (CG == 1) mbar_arrive(tempty0 + 8 * acc);
+          else asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(tempty_lead0 + 8 * acc) : "memory");
+        }
+      };
+      if (group * 32 >= limit) release();
       for (int c0 = group * 32; c0 < limit; c0 += 64) {
         const int t0 = mt * p.tn + c0, jmax = min(32, limit - c0);
         unsigned z[32], y[kDual ? 32 : 1];
@@ -380,6 +389,7 @@ k_gemm_i8(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUt
         scales[lane] = s;
         __syncwarp();
         if (ok) tmem_ld_wait();
+        if (c0 + 64 >= limit) release();                     // the accumulator has been read: the next item may have it
         float v[32];
 #pragma unroll
         for (int j = 0; j < 32; j += 4) {
@@ -396,12 +406,6 @@ k_gemm_i8(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUt
           for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(0x7fffffffu);
         }
         store_chunk<MODE>(p, v, n, t0, jmax, out_tile[(MODE == 0 || MODE == 3) ? warp - 2 : 0]);
-      }
-      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-      __syncwarp();
-      if (lane == 0) {
-        if (CG == 1) mbar_arrive(tempty0 + 8 * acc);
-        else asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(tempty_lead0 + 8 * acc) : "memory");
       }
     }
     if (CG == 2 && !ok && lane == 0) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(peer_abort), "r"(1) : "memory");
@@ -576,6 +580,54 @@ struct Plan {
   int cg, splits, tn, m_tiles, n_tiles, workers, stages, nbuf;
 };
 
+// Clocks that a plan takes, from what was measured over QKV, O, gate/up, down and LM-head shapes at 1 to 8192 tokens.  A k
+// step costs its products (2 tn clocks a weight tile, 1.2 times that in practice) or its loads (62 bytes a clock, 50 for a
+// CTA of a pair); a call no less than its weights from HBM, 1.4 times that where token tiles fetch them side by side.  An
+// epilogue takes 6 clocks a token, 18 with silu, behind the next item's products where there are two buffers.  A split
+// costs 1200 clocks and its exchange, pairs 2500 for their barriers.
+float cost_of(const Plan& p, int kblocks, bool dual, float weight_bytes) {
+  const int w = dual ? 2 : 1, kb = (kblocks + p.splits - 1) / p.splits;
+  const float step = fmaxf(2.4f * p.tn * w, (kTileRows * w + p.tn / p.cg) * (float)BKB / (p.cg == 1 ? 62.f : 50.f));
+  const int rounds = (int)(((long long)p.n_tiles * p.m_tiles + p.workers - 1) / p.workers);
+  const float epilogue = (dual ? 18.f : 6.f) * p.tn, loop = kb * step * (p.cg == 1 ? 1.05f : 1.f);
+  float c = rounds * loop + (rounds - 1) * (p.nbuf == 1 ? epilogue : fmaxf(0.f, epilogue - loop));
+  c = fmaxf(c, weight_bytes * (p.m_tiles > 1 ? 1.4f : 1.f) / 3400.f) + epilogue;
+  if (p.splits > 1) c += 1200.f + p.tn * (8.f + 10.f / p.splits) * p.cg;
+  return c + (p.cg == 2 ? 2500.f : 0.f);
+}
+
+// The cheapest plan: single CTAs or pairs, tiles of equal width that cover the tokens, k ranges shared by up to eight CTAs
+// where the tiles leave SMs idle (one wave of clusters; two k steps each at least).
+Plan plan_of(const DevInfo& dv, int M, int N, int kblocks, bool dual) {
+  Plan best = {};
+  float least = INFINITY;
+  const float weight_bytes = (float)N * kblocks * BKB * (dual ? 2 : 1);
+  for (int cg = 1; cg <= (dv.clusters[2] > 0 ? 2 : 1); ++cg) {
+    const int unit = cg == 2 ? 32 : 16;                      // widths that kind::i8 has at 128 and at 256 rows
+    int last = 0;
+    for (int want = 256; want >= unit; want -= want > 128 ? 32 : want > 64 ? 16 : unit) {
+      Plan p = {};
+      p.cg = cg;
+      p.m_tiles = (M + want - 1) / want;
+      p.tn = ((M + p.m_tiles - 1) / p.m_tiles + unit - 1) / unit * unit;
+      if (p.tn == last) continue;
+      last = p.tn;
+      p.n_tiles = (N + kTileRows * cg - 1) / (kTileRows * cg);
+      p.nbuf = dual && p.tn > 128 ? 1 : 2;
+      const long long items = (long long)p.n_tiles * p.m_tiles;
+      for (int sp = 1; sp <= (dual ? 1 : 8 / cg); ++sp) {
+        const int most = sp == 1 ? (cg == 2 ? dv.clusters[2] : dv.num_sms) : dv.clusters[sp * cg];
+        if (sp > 1 && (items > most || kblocks < 2 * sp)) break;
+        p.splits = sp;
+        p.workers = (int)(items < most ? items : most);
+        const float c = cost_of(p, kblocks, dual, weight_bytes);
+        if (c < least) { least = c; best = p; }
+      }
+    }
+  }
+  return best;
+}
+
 }  // namespace
 
 cudaError_t launch_gemm_i8(const GemmI8Args& a, cudaStream_t s) {
@@ -583,30 +635,13 @@ cudaError_t launch_gemm_i8(const GemmI8Args& a, cudaStream_t s) {
   const DevInfo* dv = dev_info();
   if (!dv || !dv->ok) return cudaErrorNotSupported;
   const bool dual = a.mode == 3;
-  Plan pl;
-  pl.cg = a.M > 128 && dv->clusters[2] > 0 ? 2 : 1;
-  pl.m_tiles = (a.M + 255) / 256;
-  const int per = (a.M + pl.m_tiles - 1) / pl.m_tiles, unit = pl.cg == 2 ? 32 : 16;
-  pl.tn = (per + unit - 1) / unit * unit;
-  pl.n_tiles = (a.N + kTileRows * pl.cg - 1) / (kTileRows * pl.cg);
   const int kblocks = (a.K + BKB - 1) / BKB;
-  const long long items = (long long)pl.n_tiles * pl.m_tiles;
-  pl.splits = 1;
-  if (!dual) {
-    for (int sp = 8 / pl.cg; sp > 1; --sp) {
-      if (pl.cg == 2 && (sp & (sp - 1))) continue;
-      if (items <= dv->clusters[sp * pl.cg] && kblocks / sp >= 2) { pl.splits = sp; break; }
-    }
-  }
-  pl.nbuf = dual && pl.tn > 128 ? 1 : 2;
+  Plan pl = plan_of(*dv, a.M, a.N, kblocks, dual);
   const int stage_bytes = (dual ? 2 : 1) * kTileRows * BKB + pl.tn / pl.cg * BKB;
   const int own = (pl.tn / kChunk + pl.splits - 1) / pl.splits;
   const int received = (pl.splits - 1) * own * kChunk * kTileRows * 4;
   pl.stages = (kRing - received) / stage_bytes;
   if (pl.stages > kMaxStages) pl.stages = kMaxStages;
-  const int most = pl.cg == 2 ? dv->clusters[2] : dv->num_sms;
-  pl.workers = (int)(items < most ? items : most);
-
   Params p;
   p.M = a.M; p.N = a.N; p.K = a.K; p.tn = pl.tn; p.n_tiles = pl.n_tiles; p.m_tiles = pl.m_tiles; p.splits = pl.splits;
   p.kblocks = kblocks; p.stages = pl.stages; p.nbuf = pl.nbuf; p.received = pl.stages * stage_bytes;
