@@ -3,9 +3,9 @@
 //   y = x, or gain * x / sqrt(mean(x^2) + eps) with a gain;  s = max(fp32(max |y| / 127), 2^-126);
 //   code = y / s rounded to the nearest integer, halves to the even one - of the exact quotient, not of a rounded one.
 //
-// Bound by memory: x is read once, a byte an element is written.  One CTA per row keeps the row in registers (32 elements
-// a thread, all loads in flight before the first use) between the maximum and the rounding; rows too long for that are
-// read twice, the second time from L2.
+// Bound by memory: x is read once, a byte an element is written.  The threads of a row keep it in registers as it is stored
+// (32 elements each, all loads in flight before the first use) between the maximum and the rounding; rows too long for that
+// are read twice, the second time from L2.  Short rows share a CTA of up to 256 threads.
 // A row with an infinite or NaN element has no scale: NaN, with zero codes, so that every product of it is NaN.
 #include "decode_ops.cuh"
 
@@ -70,20 +70,37 @@ __device__ __forceinline__ float gained(const Unit<F32>& r, const bf16* gain, in
 // |v| as an integer orders as the value does, with infinities and NaN above all numbers.
 __device__ __forceinline__ unsigned magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 
+__device__ __forceinline__ unsigned long long pair(float a, float b) {
+  unsigned long long r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
+  unsigned long long r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+
 // Codes of eight elements, y = v * r.  Adding 1.5 * 2^23 leaves the nearest integer of y * inv in the low bits; where the
 // remainder y - q s (exact: a multiple of half a step of s, no larger than s) reaches half of s the quotient's own rounding
-// may have decided, and the remainder decides instead.
+// may have decided, and the remainder decides instead.  Two elements an instruction.
 template <bool NORM>
 __device__ __forceinline__ uint2 round_unit(const float* v, float r, float s, float inv) {
   constexpr float kMagic = 12582912.f;
+  const unsigned long long inv2 = pair(inv, inv), s2 = pair(-s, -s), magic = pair(kMagic, kMagic), one = pair(1.f, 1.f),
+                           back = pair(-kMagic, -kMagic), zero = pair(-0.f, -0.f), r2 = pair(r, r);
   unsigned b[kUnit];
   float most = 0.f;
 #pragma unroll
-  for (int i = 0; i < kUnit; ++i) {
-    const float y = NORM ? v[i] * r : v[i];
-    const float t = fmaf(y, inv, kMagic);
-    most = fmaxf(most, fabsf(fmaf(kMagic - t, s, y)));
-    b[i] = __float_as_uint(t);
+  for (int i = 0; i < kUnit; i += 2) {
+    unsigned long long y = pair(v[i], v[i + 1]);
+    if (NORM) y = fma2(y, r2, zero);
+    const unsigned long long t = fma2(y, inv2, magic);
+    const unsigned long long rest = fma2(fma2(t, one, back), s2, y);
+    float lo, hi;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(rest));
+    most = fmaxf(fmaxf(most, fabsf(lo)), fabsf(hi));
+    asm("mov.b64 {%0, %1}, %2;" : "=r"(b[i]), "=r"(b[i + 1]) : "l"(t));
   }
   if (most + most >= s) {
 #pragma unroll
@@ -129,21 +146,23 @@ __device__ __forceinline__ unsigned largest(const Unit<F32>& r, const bf16* gain
   return top;
 }
 
+// (plain bf16 rows: two CTAs of up to 1024 threads an SM, 32 registers a thread, three of the longest rows in flight instead
+// of two: 4096 x 18944 47 -> 42 us; the others would spill)
 template <bool F32, bool VEC, bool NORM, bool LONG>
-__global__ void __launch_bounds__(1024) k_quant_i8(const QuantI8Args a) {
+__global__ void __launch_bounds__(1024, F32 || NORM || !VEC || LONG ? 1 : 2) k_quant_i8(const QuantI8Args a) {
   __shared__ unsigned s_max[32];
   __shared__ float s_sum[32];
   pdl_wait();
   pdl_trigger();
-  const int m = blockIdx.x;
+  const int m = blockIdx.x * blockDim.y + threadIdx.y;       // (a row has whole warps)
+  bool here = m < a.M;
   long long from = m;
-  if (a.idx) {
+  if (a.idx && here) {
     from = __ldg(a.idx + m);
-    if (from < 0 || from >= a.x_rows) {
-      if (threadIdx.x == 0 && a.error_flag) atomicMax(a.error_flag, 100 + SITE_QUANT_I8);
-      return;
-    }
+    here = from >= 0 && from < a.x_rows;
+    if (!here && threadIdx.x == 0 && a.error_flag) atomicMax(a.error_flag, 100 + SITE_QUANT_I8);
   }
+  const int K = here ? a.K : 0;
   const void* row = static_cast<const char*>(a.x) + from * a.ldx * (F32 ? 4 : 2);
   const int step = blockDim.x * kUnit;
   Unit<F32> r[kUnits];
@@ -153,16 +172,16 @@ __global__ void __launch_bounds__(1024) k_quant_i8(const QuantI8Args a) {
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
       const int at = threadIdx.x * kUnit + u * step;
-      if (at < a.K) r[u] = load_unit<F32, VEC>(row, at, a.K);
+      if (at < K) r[u] = load_unit<F32, VEC>(row, at, K);
     }
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
       const int at = threadIdx.x * kUnit + u * step;
-      if (at < a.K) top = largest<F32, NORM>(r[u], a.gain, at, a.K, top, &ss);
+      if (at < K) top = largest<F32, NORM>(r[u], a.gain, at, K, top, &ss);
     }
   } else {
-    for (int at = threadIdx.x * kUnit; at < a.K; at += step)
-      top = largest<F32, NORM>(load_unit<F32, VEC>(row, at, a.K), a.gain, at, a.K, top, &ss);
+    for (int at = threadIdx.x * kUnit; at < K; at += step)
+      top = largest<F32, NORM>(load_unit<F32, VEC>(row, at, K), a.gain, at, K, top, &ss);
   }
   if (!F32 && !NORM) top = max(top & 0xffffu, top >> 16) << 16;
   top = __reduce_max_sync(0xffffffffu, top);
@@ -173,17 +192,18 @@ __global__ void __launch_bounds__(1024) k_quant_i8(const QuantI8Args a) {
   const int warps = blockDim.x >> 5, lane = threadIdx.x & 31;
   if (warps > 1) {
     if (lane == 0) {
-      s_max[threadIdx.x >> 5] = top;
-      if (NORM) s_sum[threadIdx.x >> 5] = ss;
+      s_max[threadIdx.y * warps + (threadIdx.x >> 5)] = top;
+      if (NORM) s_sum[threadIdx.y * warps + (threadIdx.x >> 5)] = ss;
     }
     __syncthreads();
-    top = __reduce_max_sync(0xffffffffu, lane < warps ? s_max[lane] : 0u);
+    top = __reduce_max_sync(0xffffffffu, lane < warps ? s_max[threadIdx.y * warps + lane] : 0u);
     if (NORM) {
-      ss = lane < warps ? s_sum[lane] : 0.f;
+      ss = lane < warps ? s_sum[threadIdx.y * warps + lane] : 0.f;
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
     }
   }
+  if (!here) return;
   // rounding is monotonic: the largest |gain x| times r is the largest |y|
   const float rms = NORM ? rsqrtf(ss / (float)a.K + a.eps) : 1.f;
   const float big = NORM ? __uint_as_float(top) * rms : __uint_as_float(top);
@@ -194,18 +214,18 @@ __global__ void __launch_bounds__(1024) k_quant_i8(const QuantI8Args a) {
   int8_t* out = a.codes + (long long)m * a.ldc;
   auto finish = [&](const Unit<F32>& u, int at) {
     float v[kUnit];
-    if (NORM) gained<F32>(u, a.gain, at, a.K, v);
+    if (NORM) gained<F32>(u, a.gain, at, K, v);
     else widen<F32>(u, v);
-    store_unit(out, at, a.K, real ? round_unit<NORM>(v, rms, s, inv) : make_uint2(0u, 0u));
+    store_unit(out, at, K, real ? round_unit<NORM>(v, rms, s, inv) : make_uint2(0u, 0u));
   };
   if (!LONG) {
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
       const int at = threadIdx.x * kUnit + u * step;
-      if (at < a.K) finish(r[u], at);
+      if (at < K) finish(r[u], at);
     }
   } else {
-    for (int at = threadIdx.x * kUnit; at < a.K; at += step) finish(load_unit<F32, VEC>(row, at, a.K), at);
+    for (int at = threadIdx.x * kUnit; at < K; at += step) finish(load_unit<F32, VEC>(row, at, K), at);
   }
 }
 
@@ -218,7 +238,10 @@ cudaError_t launch_typed(const QuantI8Args& a, cudaStream_t s) {
   void (*k)(const QuantI8Args);
   if (a.gain) k = lng ? k_quant_i8<F32, VEC, true, true> : k_quant_i8<F32, VEC, true, false>;
   else k = lng ? k_quant_i8<F32, VEC, false, true> : k_quant_i8<F32, VEC, false, false>;
-  return launch_pdl(k, dim3(a.M), dim3(threads), 0, s, a);
+  // 256 threads to a CTA where there are rows enough (a CTA of one warp a row: 16384 x 384 18 us)
+  int rows = threads < 256 ? 256 / threads : 1;
+  while (rows > 1 && a.M < 512 * rows) --rows;
+  return launch_pdl(k, dim3((unsigned)((a.M + rows - 1) / rows)), dim3((unsigned)threads, (unsigned)rows), 0, s, a);
 }
 
 }  // namespace
