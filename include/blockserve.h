@@ -407,8 +407,8 @@ enum { BS_I8_MAX_K = 131071 };               /* sums of K products of codes fit 
 
 /* Codes and scales of rows x [x_rows][ldx] (type BS_BF16 or BS_F32, stride in elements; any alignment of the rows):
  *   y = x, or with `gain` (bf16 [K]) gain * x / sqrt(mean(x^2) + eps) in fp32;
- *   scale = max(fp32(max |y| / 127), 2^-126);  code = y / scale to the nearest integer, halves to the even one, decided on
- *   the exact quotient.
+ *   scale = max(max |y| * (1 / 127), 2^-126) in fp32, with 1 / 127 rounded to fp32;  code = y / scale to the nearest
+ *   integer, halves to the even one, decided on the exact quotient: -127 to 127.
  * Row m is row idx[m] of x (idx NULL: row m, x_rows >= M).  An idx[m] outside [0, x_rows) raises error_flag (device int,
  * nullable, only ever raised) to 100 or more and leaves the row's outputs as they were.  A row with an infinite or NaN
  * element gets the scale NaN and zero codes. */

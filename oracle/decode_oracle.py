@@ -8,12 +8,12 @@ LEAST_SCALE = 2.0 ** -126
 
 
 def quant(x, gain=None, eps=0.0):
-    """(y, codes as floats, scale) of rows x in float64: y = x or its RMS norm; the scale is held in fp32, the codes are the
-    exact quotients rounded half to even.  Rows with an infinite or NaN element: scale NaN, codes 0."""
+    """(y, codes as floats, scale) of rows x in float64: y = x or its RMS norm; the scale is the fp32
+    product of max |y| and 1 / 127, the codes are the exact quotients rounded half to even.  Rows with an infinite or NaN element: scale NaN, codes 0."""
     x = np.asarray(x, np.float64)
     with np.errstate(all="ignore"):
         y = x if gain is None else x * gain / np.sqrt((x * x).mean(1, keepdims=True) + eps)
-        scale = np.maximum((np.abs(y).max(1) / 127).astype(np.float32).astype(np.float64), LEAST_SCALE)
+        scale = np.maximum((np.abs(y).max(1).astype(np.float32) * np.float32(1 / 127)).astype(np.float64), LEAST_SCALE)
         bad = ~np.isfinite(x).all(1)
         codes = np.rint(y / scale[:, None])
     codes[bad] = 0

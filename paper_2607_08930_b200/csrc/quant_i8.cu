@@ -1,6 +1,6 @@
 // Rows (activations of a token, weights of an output channel) as 8-bit integer codes with one scale each.
 //
-//   y = x, or gain * x / sqrt(mean(x^2) + eps) with a gain;  s = max(fp32(max |y| / 127), 2^-126);
+//   y = x, or gain * x / sqrt(mean(x^2) + eps) with a gain;  s = max(max |y| * fp32(1 / 127), 2^-126) in fp32;
 //   code = y / s rounded to the nearest integer, halves to the even one - of the exact quotient, not of a rounded one.
 //
 // Bound by memory: x is read once, a byte an element is written.  The threads of a row keep it in registers as it is stored
@@ -208,7 +208,7 @@ __global__ void __launch_bounds__(1024, F32 || NORM || !VEC || LONG ? 1 : 2) k_q
   const float rms = NORM ? rsqrtf(ss / (float)a.K + a.eps) : 1.f;
   const float big = NORM ? __uint_as_float(top) * rms : __uint_as_float(top);
   const bool real = top < 0x7f800000u && big < INFINITY;
-  const float s = fmaxf(__fdiv_rn(big, 127.f), 0x1p-126f);
+  const float s = fmaxf(__fmul_rn(big, 1.f / 127.f), 0x1p-126f);
   const float inv = __frcp_rn(s);
   if (threadIdx.x == 0) a.scale[m] = real ? s : __uint_as_float(0x7fffffffu);
   int8_t* out = a.codes + (long long)m * a.ldc;

@@ -65,7 +65,7 @@ def test_quotients_at_and_next_to_halves(B):
     for _ in range(64):
         s = np.float32(rng.uniform(1, 2)) * np.float32(2.0) ** rng.integers(-100, 100)
         top = np.float32(127 * np.float64(s))
-        s = np.float32(np.float64(top) / 127)
+        s = top * np.float32(1 / 127)
         half = ((np.arange(-127, 127) + 0.5) * np.float64(s)).astype(np.float32)
         near = [half]
         for _ in range(2):
