@@ -726,11 +726,11 @@ def op_quant_i8(x: torch.Tensor, gain: Optional[torch.Tensor] = None, eps: float
     """(codes int8 [M, K], scale fp32 [M]) of the rows of x (bf16 or fp32 [rows, K], any row stride), or of its rows
     idx[m]; with `gain` (bf16 [K]) of their RMS norms.  Weights are laid out by the same call: a row is an output channel.
     error_flag (int32 [1]) gets >= 100 where an idx was out of range (the row is left as it was)."""
-    name, dev = "bs_op_quant_i8", x.get_device()
+    name, dev, shape = "bs_op_quant_i8", x.get_device(), x.shape
     type_ = _TYPES.get(x.dtype)
-    if type_ is None or x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
-        _refuse(name, f"x must be a bfloat16 or float32 matrix of adjacent elements, got {tuple(x.shape)} {x.dtype}")
-    rows, K = x.shape
+    if type_ is None or len(shape) != 2 or (shape[1] > 1 and x.stride(1) != 1):
+        _refuse(name, f"x must be a bfloat16 or float32 matrix of adjacent elements, got {tuple(shape)} {x.dtype}")
+    rows, K = shape
     M = rows
     if idx is not None:
         _need(name, dev, _I32, 0, "idx", idx)
@@ -738,18 +738,22 @@ def op_quant_i8(x: torch.Tensor, gain: Optional[torch.Tensor] = None, eps: float
     if gain is not None:
         _need(name, dev, _BF16, K, "gain", gain)
     if codes is None:
-        codes = i8_codes(M, K, x.device)
-    elif codes.shape != (M, K):
-        _refuse(name, f"codes must be [{M}, {K}], got {tuple(codes.shape)}")
-    ldc = _rows_of_codes(name, dev, "codes", codes)
+        ldc = (K + 15) // 16 * 16
+        codes = torch.empty((M, ldc), dtype=_I8, device=x.device)
+        if ldc != K:
+            codes = codes[:, :K]
+    else:
+        if codes.shape != (M, K):
+            _refuse(name, f"codes must be [{M}, {K}], got {tuple(codes.shape)}")
+        ldc = _rows_of_codes(name, dev, "codes", codes)
     if scale is None:
         scale = torch.empty(M, dtype=_F32, device=x.device)
-    else:
+    elif scale.dtype is not _F32 or scale.get_device() != dev or not scale.is_contiguous() or scale.numel() < M:
         _need(name, dev, _F32, M, "scale", scale)
     if error_flag is not None:
         _need(name, dev, _I32, 1, "error_flag", error_flag)
-    _call(name, dev, (_lib or lib()).bs_op_quant_i8, x.data_ptr(), type_, _stride_of(x), _ptr(idx), rows, _ptr(gain), eps,
-          codes.data_ptr(), ldc, scale.data_ptr(), M, K, _ptr(error_flag))
+    _call(name, dev, (_lib or lib()).bs_op_quant_i8, x.data_ptr(), type_, x.stride(0) if rows > 1 else K, _ptr(idx), rows,
+          _ptr(gain), eps, codes.data_ptr(), ldc, scale.data_ptr(), M, K, _ptr(error_flag))
     return codes, scale
 
 
@@ -761,12 +765,12 @@ def op_gemm_i8(a: torch.Tensor, a_scale: torch.Tensor, W: torch.Tensor, w_scale:
     W2 [N, K] and w2_scale."""
     name, dev = "bs_op_gemm_i8", a.get_device()
     lda, ldw = _rows_of_codes(name, dev, "a", a), _rows_of_codes(name, dev, "W", W)
-    (M, K), N = a.shape, W.shape[0]
-    if W.shape[1] != K or (mode == 3) != (W2 is not None):
+    (M, K), (N, width) = a.shape, W.shape
+    if width != K or (mode == 3) != (W2 is not None):
         _refuse(name, f"W must be [N, {K}], and W2 is given in mode 3 only")
-    if a_scale.dtype is not _F32 or a_scale.get_device() != dev or not a_scale.is_contiguous() or a_scale.numel() < M:
+    if not (a_scale.dtype is w_scale.dtype is _F32 and a_scale.get_device() == w_scale.get_device() == dev and
+            a_scale.is_contiguous() and w_scale.is_contiguous() and a_scale.numel() >= M and w_scale.numel() >= N):
         _need(name, dev, _F32, M, "a_scale", a_scale)
-    if w_scale.dtype is not _F32 or w_scale.get_device() != dev or not w_scale.is_contiguous() or w_scale.numel() < N:
         _need(name, dev, _F32, N, "w_scale", w_scale)
     if W2 is not None:
         if w2_scale is None or W2.shape != W.shape or _rows_of_codes(name, dev, "W2", W2) != ldw:
@@ -776,14 +780,17 @@ def op_gemm_i8(a: torch.Tensor, a_scale: torch.Tensor, W: torch.Tensor, w_scale:
     if C_out is None:
         if mode == 1:
             _refuse(name, "mode 1 adds to C_out")
-        C_out = torch.empty(M, N, dtype=dtype, device=a.device)
-    elif C_out.shape != (M, N) or C_out.dtype is not dtype or C_out.get_device() != dev or (N > 1 and C_out.stride(1) != 1):
-        _refuse(name, f"C_out must be a {dtype} matrix [{M}, {N}] of adjacent elements on the operator's device, got "
-                      f"{tuple(C_out.shape)} {C_out.dtype} on {C_out.device}")
+        C_out = torch.empty((M, N), dtype=dtype, device=a.device)
+        ldc = N
+    else:
+        if C_out.shape != (M, N) or C_out.dtype is not dtype or C_out.get_device() != dev or (N > 1 and C_out.stride(1) != 1):
+            _refuse(name, f"C_out must be a {dtype} matrix [{M}, {N}] of adjacent elements on the operator's device, got "
+                          f"{tuple(C_out.shape)} {C_out.dtype} on {C_out.device}")
+        ldc = _stride_of(C_out)
     if error_flag is not None:
         _need(name, dev, _I32, 1, "error_flag", error_flag)
     _call(name, dev, (_lib or lib()).bs_op_gemm_i8, a.data_ptr(), lda, a_scale.data_ptr(), W.data_ptr(), ldw, w_scale.data_ptr(),
-          _ptr(W2), _ptr(w2_scale), C_out.data_ptr(), _stride_of(C_out), M, N, K, mode, _ptr(error_flag))
+          _ptr(W2), _ptr(w2_scale), C_out.data_ptr(), ldc, M, N, K, mode, _ptr(error_flag))
     return C_out
 
 

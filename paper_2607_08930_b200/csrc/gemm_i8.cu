@@ -239,6 +239,11 @@ k_gemm_i8(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUt
   const int kb0 = SPLIT ? (int)((long long)p.kblocks * split / p.splits) : 0;
   const int kb1 = SPLIT ? (int)((long long)p.kblocks * (split + 1) / p.splits) : p.kblocks;
 
+  if (threadIdx.x == 32) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_w) : "memory");
+    if (kDual) asm volatile("prefetch.tensormap [%0];" ::"l"(&map_w2) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_x) : "memory");
+  }
   if (threadIdx.x == 0) {
     s_abort = 0;
     for (int i = 0; i < p.stages; ++i) {

@@ -145,7 +145,7 @@ struct Table {
     return bits;
   }
   // whether a rule for token id is this CTA's to keep
-  __device__ __forceinline__ bool takes(int id) const { return (unsigned)id < (unsigned)vocab && owns(id) && id != mask_id; }
+  __device__ __forceinline__ bool takes(int id) const { return owns(id) && (unsigned)id < (unsigned)vocab && id != mask_id; }
 };
 
 __device__ void raise(const RulesArgs& a) {
@@ -589,7 +589,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_rules_confidence(const Rul
             for (int i = 0; i < W::kW; ++i) u[b].w[i] = kLeast<T>;               // (what is not there is -inf)
             if (ALIGNED) {
               bits[b] = masked.value ? ahead[b] : 0xffffffffu;
-              if (masked.value || there) bits[b] &= t.plain[e >> 5];
+              if (there) bits[b] &= t.plain[e >> 5];         // (others lie behind the table)
               if (masked.value) bits[b] = bits[b] >> shift & kAll;
               // a grammar often leaves a handful of tokens: vectors without any are not read
               if (masked.value ? bits[b] != 0u : there) load(z + id, u[b]);
@@ -774,8 +774,9 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logit_rules(const RulesArg
         if (!INPLACE && there) load(z + id, u[b]);
         if (ALIGNED) {
           const unsigned m = load1_if(mask + (id >> 5), mask && there, 0xffffffffu);
-          calm[b] = (t.plain[e >> 5] >> (e & 31)) & kAll;
-          keep[b] = ((t.plain[e >> 5] | t.touched[e >> 5]) & m) >> (e & 31) & kAll;
+          const unsigned p = there ? t.plain[e >> 5] : 0u, some = there ? t.touched[e >> 5] : 0u;      // (others lie behind the table)
+          calm[b] = (p >> (e & 31)) & kAll;
+          keep[b] = ((p | some) & m) >> (e & 31) & kAll;
         } else {
           keep[b] = bits_at<E, false>(e, allow) & kAll;
           calm[b] = bits_at<E, false>(e, plain) & kAll;
