@@ -8,9 +8,9 @@
 // biases), so the pass over all entries only looks up one bit an entry, and the touched ones are taken one by one from a
 // list.  A vocabulary is dealt in blocks of 512 entries to up to eight CTAs (in turn, because the frequent tokens of a
 // vocabulary have its low ids).  A CTA keeps a table of one request at a time in shared memory: the bits of the entries
-// that some rule touches, and a list of those entries with how often each was generated.  The context's tokens first set
-// their bits, a prefix sum over the words makes the bits places in the list, and the tokens are counted there
-// (shared-memory atomics: integers, so their order does not matter).  The CTA walks the consecutive rows of its span and
+// that some rule touches, and a list of those entries with how often each was generated.  Every warp queues the context
+// tokens of the CTA's share among those it reads; they first set their bits, a prefix sum over the words makes the bits
+// places in the list, and the tokens are counted there (shared-memory atomics: integers, so their order does not matter).  The CTA walks the consecutive rows of its span and
 // builds the table anew when the request changes.  For the confidence the CTAs of a span are a cluster; every warp
 // leaves (max, sum, argmax) of its part of a row in shared memory without waiting for the others, and the parts of up to
 // 32 rows are joined at a time, in a fixed order, over distributed shared memory: one launch without scratch.
@@ -32,9 +32,10 @@ constexpr int kBlockWords = kBlock / 32;
 constexpr int kRowsAtOnce = 32;            // rows whose parts are kept before they are joined
 constexpr int kPerSm = 4;                  // CTAs of an SM
 constexpr int kMaxChunks = 8;
-constexpr int kListed = 4096;              // touched entries that are listed at a time
+constexpr int kListed = 3072;              // touched entries that are listed at a time
 constexpr int kTokens = 8;                 // context tokens a thread has in flight
-constexpr unsigned kInPrompt = 0x80000000u;
+constexpr int kQueue = 192;                // tokens of a CTA's share that a warp keeps (if it reads more, it reads them twice)
+constexpr unsigned kInPrompt = 0x80000000u, kGenerated = 0x80000000u;
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct Part {
@@ -126,6 +127,8 @@ struct Table {
   unsigned* count;       // of a listed entry (touched, in ascending order): kInPrompt | times generated
   unsigned short* list;  // the entry
   unsigned short* bias;  // 1 + place of its first bias, or 0
+  unsigned* queue;       // this warp's tokens of the share: entry | kGenerated
+  int queued;            // how many (more than kQueue: they are not all there)
   int total;             // touched entries
   int begin, gen, end;   // the request's context
   int bias_lo, bias_hi;  // its biases
@@ -162,7 +165,8 @@ __device__ Table make_table(const RulesArgs& a, const Plan& pl, int chunk, unsig
   t.list = reinterpret_cast<unsigned short*>(t.touched + t.words);
   t.bias = t.list + pl.listed;
   t.place = t.bias + pl.listed;
-  t.total = 0;
+  t.queue = reinterpret_cast<unsigned*>(t.place + t.words) + (threadIdx.x >> 5) * kQueue;
+  t.total = t.queued = 0;
   return t;
 }
 
@@ -180,19 +184,20 @@ __device__ __forceinline__ void list_touched(const RulesArgs& a, const Table& t,
     if (at >= 0 && at < n) t.list[at] = (unsigned short)e;
     return at;
   };
-  for (int i0 = t.begin + threadIdx.x; i0 < t.end; i0 += kThreads * kTokens) {
-    int id[kTokens];
-#pragma unroll
-    for (int k = 0; k < kTokens; ++k) id[k] = (int)load1_if(a.ctx + i0 + k * kThreads, i0 + k * kThreads < t.end, 0xffffffffu);
-#pragma unroll
-    for (int k = 0; k < kTokens; ++k)
-      if (t.takes(id[k])) {
-        const int at = listed(t.entry_of(id[k]));
-        if (at >= 0 && at < n) {
-          if (i0 + k * kThreads >= t.gen) atomicAdd(t.count + at, 1u);
-          else atomicOr(t.count + at, kInPrompt);
-        }
-      }
+  auto counted = [&](int e, bool generated) {
+    const int at = listed(e);
+    if (at >= 0 && at < n) {
+      if (generated) atomicAdd(t.count + at, 1u);
+      else atomicOr(t.count + at, kInPrompt);
+    }
+  };
+  if (t.queued <= kQueue) {
+    for (int i = threadIdx.x & 31; i < t.queued; i += 32) counted((int)(t.queue[i] & 0xffffu), t.queue[i] & kGenerated);
+  } else {
+    for (int i = t.begin + threadIdx.x; i < t.end; i += kThreads) {
+      const int id = __ldg(a.ctx + i);
+      if (t.takes(id)) counted(t.entry_of(id), i >= t.gen);
+    }
   }
   for (int i = t.bias_lo + threadIdx.x; i < t.bias_hi; i += kThreads) {
     const int id = __ldg(a.bias_tok + i);
@@ -226,30 +231,41 @@ __device__ __forceinline__ void build_table(const RulesArgs& a, Table& t, const 
   t.begin = begin; t.gen = gen; t.end = end; t.bias_lo = lo; t.bias_hi = hi;
   __syncthreads();
   bool bad = false;
-  auto touch = [&](int id, bool there) {
-    const int e = t.entry_of(id);
-    if (t.takes(id)) atomicOr(t.touched + (e >> 5), 1u << (e & 31));
-    bad = bad || (there && (unsigned)id >= (unsigned)t.vocab);
-  };
+  const int lane = threadIdx.x & 31;
+  auto touch = [&](int e) { atomicOr(t.touched + (e >> 5), 1u << (e & 31)); };
   // (a thread's first biases are fetched along with the first tokens)
   int b_id = (int)load1_if(a.bias_tok + lo + threadIdx.x, lo + (int)threadIdx.x < hi, 0xffffffffu);
   int b_before = (int)load1_if(a.bias_tok + lo + threadIdx.x - 1, threadIdx.x > 0 && lo + (int)threadIdx.x < hi, 0xffffffffu);
-  for (int i0 = begin + threadIdx.x; i0 < end; i0 += kThreads * kTokens) {
+  t.queued = 0;
+  for (int i0 = begin + threadIdx.x; i0 - lane < end; i0 += kThreads * kTokens) {
     int id[kTokens];
 #pragma unroll
-    for (int k = 0; k < kTokens; ++k) id[k] = (int)load1_if(a.ctx + i0 + k * kThreads, i0 + k * kThreads < end, 0xffffffffu);
+    for (int k = 0; k < kTokens; ++k) id[k] = i0 + k * kThreads < end ? __ldg(a.ctx + i0 + k * kThreads) : -1;
 #pragma unroll
-    for (int k = 0; k < kTokens; ++k) touch(id[k], i0 + k * kThreads < end);
+    for (int k = 0; k < kTokens; ++k) {
+      const bool mine = t.takes(id[k]);
+      const unsigned all = __ballot_sync(0xffffffffu, mine);
+      const int at = t.queued + __popc(all & ((1u << lane) - 1u));
+      if (mine) {
+        const int e = t.entry_of(id[k]);
+        if (at < kQueue) t.queue[at] = (unsigned)e | (i0 + k * kThreads >= gen ? kGenerated : 0u);
+        else touch(e);
+      }
+      t.queued += __popc(all);
+      bad = bad || (i0 + k * kThreads < end && (unsigned)id[k] >= (unsigned)t.vocab);
+    }
   }
+  __syncwarp();
+  for (int i = lane; i < min(t.queued, kQueue); i += 32) touch((int)(t.queue[i] & 0xffffu));
   for (int i = lo + threadIdx.x; i < hi; i += kThreads) {
-    touch(b_id, true);
-    bad = bad || b_before > b_id;
+    if (t.takes(b_id)) touch(t.entry_of(b_id));
+    bad = bad || (unsigned)b_id >= (unsigned)t.vocab || b_before > b_id;
     b_id = (int)load1_if(a.bias_tok + i + kThreads, i + kThreads < hi, 0xffffffffu);
     b_before = (int)load1_if(a.bias_tok + i + kThreads - 1, i + kThreads < hi, 0xffffffffu);
   }
   if (bad && t.chunk == 0) raise(a);
   __syncthreads();
-  const int each = (t.words + kThreads - 1) / kThreads, lane = threadIdx.x & 31;
+  const int each = (t.words + kThreads - 1) / kThreads;
   const int w0 = threadIdx.x * each, w1 = min(t.words, w0 + each);
   int mine = 0;
   for (int w = w0; w < w1; ++w) {
@@ -589,7 +605,8 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_rules_confidence(const Rul
             for (int i = 0; i < W::kW; ++i) u[b].w[i] = kLeast<T>;               // (what is not there is -inf)
             if (ALIGNED) {
               bits[b] = masked.value ? ahead[b] : 0xffffffffu;
-              if (there) bits[b] &= t.plain[e >> 5];         // (others lie behind the table)
+              bits[b] &= t.plain[there ? e >> 5 : 0];        // (others lie behind the table)
+              if (!masked.value && !there) bits[b] = 0xffffffffu;
               if (masked.value) bits[b] = bits[b] >> shift & kAll;
               // a grammar often leaves a handful of tokens: vectors without any are not read
               if (masked.value ? bits[b] != 0u : there) load(z + id, u[b]);
@@ -827,7 +844,7 @@ using RuleKernel = void (*)(const RulesArgs, const Plan, T*, long long);
 
 // One-time set-up per device; how many spans the device holds at once, by cluster size and by the table's size (in steps of
 // 1 KB), asked when first needed.
-constexpr int kMaxSmem = 56 * 1024;
+constexpr int kMaxSmem = 64 * 1024;
 struct DevInfo {
   int num_sms;
   int ok;
@@ -859,7 +876,7 @@ void cluster_config(cudaLaunchConfig_t* cfg, cudaLaunchAttribute* at, int ctas, 
   cfg->numAttrs = early ? 2 : 1;
 }
 
-size_t smem_of(const Plan& pl) { return (size_t)pl.listed * 8 + (size_t)pl.blocks * kBlockWords * 10; }
+size_t smem_of(const Plan& pl) { return (size_t)pl.listed * 8 + (size_t)pl.blocks * kBlockWords * 10 + kWarps * kQueue * 4; }
 
 // The plan of a call, spans excepted.  Shares of at least 32 blocks: with fewer the join would cost more than the row.
 Plan plan_of(const RulesArgs& a) {
