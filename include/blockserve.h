@@ -448,7 +448,7 @@ typedef struct {
      outside [0, vocab) are skipped (and raise the flag), the mask id is skipped; a request whose bounds are not
      0 <= begin <= gen <= end <= ctx_total has no context (and raises the flag). */
   const int* ctx;
-  long long ctx_total;       /* < 2^31 */
+  long long ctx_total;       /* <= 2^30 */
   const int* ctx_begin;      /* [n_reqs], like the next two; needed with ctx */
   const int* ctx_gen;
   const int* ctx_end;
@@ -461,7 +461,7 @@ typedef struct {
   const int* bias_at;        /* [n_reqs + 1], values in [0, bias_total] */
   const int* bias_tok;
   const float* bias_val;
-  long long bias_total;      /* < 2^31 */
+  long long bias_total;      /* <= 2^30 */
   const unsigned* allowed;   /* [n_masks][allowed_ld]: bit v mod 32 of word v / 32 set: token v is allowed */
   long long allowed_ld;      /* words, at least ceil(vocab / 32) */
   int n_masks;
@@ -469,8 +469,8 @@ typedef struct {
 } bs_logit_rules;
 
 /* out[r, v] = the logit after the rules, rounded to the logits' type once.  logits [n_rows][ld] of type BS_F32 or BS_BF16
- * (stride in elements, at least vocab), 16-byte aligned; out the same with out_ld.  out = logits with out_ld = ld works in
- * place (only the entries that change are written); any other overlap is refused.  Entries at and behind vocab are left
+ * (stride in elements, at least vocab), 16-byte aligned; out the same with out_ld.  out = logits with out_ld = ld (or a
+ * single row) works in place (only the entries that change are written); any other overlap is refused.  Entries at and behind vocab are left
  * as they were, and so are skipped rows. */
 int bs_op_logit_rules(const void* logits, int type, long long ld, void* out, long long out_ld, int n_rows,
                       const bs_logit_rules* rules, int* error_flag, void* stream);
@@ -478,7 +478,8 @@ int bs_op_logit_rules(const void* logits, int type, long long ld, void* out, lon
 /* bs_op_confidence under the rules, in one pass that stores no logits: tok = argmax after the rules (lowest id on ties),
  * conf = exp(max - logsumexp).  A row of which nothing is left (every logit -infinity), and a skipped row, gives tok = -1
  * and conf = 0.  Rows with a NaN among the logits that are left give conf = NaN, and tok the best of the others (or -1);
- * k logits of +infinity share the row: conf = 1 / k. */
+ * k logits of +infinity share the row: conf = 1 / k.  A row's result does not depend on the call's other rows.  A wait inside
+ * the kernel that runs out (none does in a working machine) raises error_flag to 1 at least; its rows get -1 and NaN. */
 int bs_op_rules_confidence(const void* logits, int type, long long ld, int n_rows, const bs_logit_rules* rules, int* tok,
                            float* conf, int* error_flag, void* stream);
 

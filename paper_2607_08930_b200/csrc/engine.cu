@@ -1101,6 +1101,7 @@ static bool aligned4(std::initializer_list<const void*> ps) {           // where
     if ((uintptr_t)p & 3) return false;
   return true;
 }
+constexpr long long kMaxListed = 1ll << 30;                              // context tokens, biases: their indices step beyond
 constexpr long long kMaxStride = 1ll << 36;                              // of a row, in bytes: extents stay below 2^63
 static int status_of(cudaError_t r) {
   return r == cudaSuccess ? BS_OK : (r == cudaErrorNotSupported ? BS_E_ARG : BS_E_CUDA);
@@ -1148,8 +1149,8 @@ static bool rules_args(const void* logits, int type, long long ld, int n_rows, c
   if (!aligned4({r->row_req, r->ctx, r->ctx_begin, r->ctx_gen, r->ctx_end, r->repetition, r->presence, r->frequency, r->bias_at,
                  r->bias_tok, r->bias_val, r->allowed, r->row_mask}))
     return false;
-  if (r->ctx && (r->ctx_total < 0 || r->ctx_total > 0x7fffffffll || !r->ctx_begin || !r->ctx_gen || !r->ctx_end)) return false;
-  if (r->bias_at && (r->bias_total < 0 || r->bias_total > 0x7fffffffll || (r->bias_total && (!r->bias_tok || !r->bias_val))))
+  if (r->ctx && (r->ctx_total < 0 || r->ctx_total > kMaxListed || !r->ctx_begin || !r->ctx_gen || !r->ctx_end)) return false;
+  if (r->bias_at && (r->bias_total < 0 || r->bias_total > kMaxListed || (r->bias_total && (!r->bias_tok || !r->bias_val))))
     return false;
   if (r->allowed && (r->n_masks < 0 || r->allowed_ld < (r->vocab + 31) / 32 || r->allowed_ld > kMaxStride / 4 ||
                      (!r->row_mask && r->n_masks < n_rows)))
@@ -1177,7 +1178,7 @@ int bs_op_logit_rules(const void* logits, int type, long long ld, void* out, lon
   if (n_rows < 0 || !rules || !aligned16({out}) || rules->vocab < 1 || out_ld < rules->vocab || out_ld > kMaxStride / 4)
     return BS_E_ARG;
   const int size = type == BS_F32 ? 4 : 2;
-  const bool inplace = out == logits && out_ld == ld;
+  const bool inplace = out == logits && (out_ld == ld || n_rows == 1);
   RulesArgs a;
   if (!rules_args(logits, type, ld, n_rows, rules, error_flag, extent(out, n_rows, out_ld * size, (long long)rules->vocab * size),
                   Extent{0, 0}, inplace, &a))

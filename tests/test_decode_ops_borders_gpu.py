@@ -1,5 +1,9 @@
 """Calls at the borders of what the 8-bit projections and the logit rules take, and runs of the operators together, against
 the 64-bit oracle (needs a B200)."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -233,6 +237,37 @@ def test_captured_calls_read_what_the_tensors_hold_then(B):
         assert torch.equal(out, B.op_logit_rules(buf, fresh, out=torch.empty_like(buf)))
         assert torch.equal(y, B.op_gemm_i8(*B.op_quant_i8(x), w, sw))
         assert np.array_equal(out.cpu().numpy(), D.rules(zz, r["row_req"], vocab, **{k: v for k, v in r.items() if k != "row_req"}))
+
+
+FIRST_CALL = """
+import torch
+from paper_2607_08930_b200 import binding as B
+torch.manual_seed(0)
+x, w = torch.randn(200, 700, device="cuda"), torch.randn(900, 700, device="cuda")
+ints = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+rules = B.logit_rules(900, None, 200, mask_id=7, ctx=ints(3, 4, 4, 9), ctx_begin=torch.zeros(200, dtype=torch.int32, device="cuda"),
+                      ctx_gen=torch.ones(200, dtype=torch.int32, device="cuda"),
+                      ctx_end=torch.full((200,), 4, dtype=torch.int32, device="cuda"), frequency=torch.ones(200, device="cuda"))
+def step():
+    wq, sw = B.op_quant_i8(w)
+    y = B.op_gemm_i8(*B.op_quant_i8(x), wq, sw, mode=2)
+    return (y, *B.op_rules_confidence(y, rules), B.op_logit_rules(y, rules, out=torch.empty_like(y)))
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    got = step()
+g.replay()
+torch.cuda.synchronize()
+want = step()
+assert all(torch.equal(a, b) for a, b in zip(got, want)) and torch.isfinite(got[0]).all()
+print("same")
+"""
+
+
+def test_the_first_call_of_a_process_may_be_captured(B):
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST_CALL], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "same" in r.stdout, r.stderr[-2000:]
 
 
 def test_calls_on_two_streams_at_once(B):

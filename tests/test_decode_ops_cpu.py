@@ -96,8 +96,8 @@ def _rules(B, call, **over):
 @pytest.mark.parametrize("over", [dict(z=None), dict(z=P + 13 * G + 8), dict(type=2), dict(ld=99), dict(n=-1), dict(vocab=0),
                                   dict(vocab=524289, ld=1 << 20, out_ld=1 << 20, allowed_ld=1 << 20), dict(n_reqs=-1), dict(mask_id=100),
                                   dict(mask_id=-2), dict(row_req=None), dict(row_req=P + 2), dict(ctx_total=-1),
-                                  dict(ctx_total=1 << 31), dict(ctx_begin=None), dict(ctx_gen=None), dict(ctx_end=None),
-                                  dict(repetition=P + 5 * G + 1), dict(bias_total=-1), dict(bias_total=1 << 31), dict(bias_tok=None),
+                                  dict(ctx_total=(1 << 30) + 1), dict(ctx_begin=None), dict(ctx_gen=None), dict(ctx_end=None),
+                                  dict(repetition=P + 5 * G + 1), dict(bias_total=-1), dict(bias_total=(1 << 30) + 1), dict(bias_tok=None),
                                   dict(bias_val=None), dict(allowed_ld=3), dict(n_masks=-1), dict(row_mask=None), dict(flag=P + 2)])
 def test_rules_refuse(B, call, over):
     assert _rules(B, call, **over) == B.BS_E_ARG
