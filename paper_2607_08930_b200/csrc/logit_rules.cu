@@ -10,10 +10,16 @@
 // vocabulary have its low ids).  A CTA keeps a table of one request at a time in shared memory: the bits of the entries
 // that some rule touches, and a list of those entries with how often each was generated.  Every warp queues the context
 // tokens of the CTA's share among those it reads; they first set their bits, a prefix sum over the words makes the bits
-// places in the list, and the tokens are counted there (shared-memory atomics: integers, so their order does not matter).  The CTA walks the consecutive rows of its span and
-// builds the table anew when the request changes.  For the confidence the CTAs of a span are a cluster; every warp
-// leaves (max, sum, argmax) of its part of a row in shared memory without waiting for the others, and the parts of up to
-// 32 rows are joined at a time, in a fixed order, over distributed shared memory: one launch without scratch.
+// places in the list, and the tokens are counted there (shared-memory atomics: integers, so their order does not matter).
+// The CTA walks the consecutive rows of its span and builds the table anew when the request changes.  For the confidence
+// the CTAs of a span are a cluster; every warp sends (max, sum, argmax) of its part of a row to the CTA that joins the row
+// (st.async: nobody waits in between), and the parts of up to 32 rows are joined at a time, in a fixed order: one launch
+// without scratch.
+//
+// Measured on logits [rows][vocabulary]: the confidence of 317 rows of 152064 (16 requests, a grammar on nine rows of ten)
+// takes 50 us, 41 without any rule (29 at the copy rate), of 64 single rows of 126464 with contexts of 512 to 4096 tokens
+// 18 us; the logits of 64 such rows of 152064 take 23 us (12), of 318 rows of 126464 in 16 bits 45 us (30).  A row's warps
+// issue on 55 % of the clocks: tables, the ends of rows and the spans' unequal lengths are what memory waits for.
 #include <math.h>
 
 #include <mutex>
@@ -32,7 +38,7 @@ constexpr int kBlockWords = kBlock / 32;
 constexpr int kRowsAtOnce = 32;            // rows whose parts are kept before they are joined
 constexpr int kPerSm = 4;                  // CTAs of an SM
 constexpr int kMaxChunks = 8;
-constexpr int kListed = 3072;              // touched entries that are listed at a time
+constexpr int kListed = 2944;              // touched entries that are listed at a time
 constexpr int kTokens = 8;                 // context tokens a thread has in flight
 constexpr int kQueue = 192;                // tokens of a CTA's share that a warp keeps (if it reads more, it reads them twice)
 constexpr unsigned kInPrompt = 0x80000000u, kGenerated = 0x80000000u;
