@@ -5,8 +5,8 @@
 // ones) and conf = exp(max - logsumexp) without storing it.
 //
 // Bound by memory: a row of logits is read once.  The rules touch few entries of a row (the context's tokens, the
-// biases), so the pass over all entries only looks up one bit an entry, and the touched ones are taken one by one from a
-// list.  A vocabulary is dealt in blocks of 512 entries to up to eight CTAs (in turn, because the frequent tokens of a
+// biases): the touched ones are taken one by one from a list, and the pass over all entries passes them over (one bit an
+// entry) for the confidence; for the logits it writes them as if no rule touched them, and they are written again.  A vocabulary is dealt in blocks of 512 entries to up to eight CTAs (in turn, because the frequent tokens of a
 // vocabulary have its low ids).  A CTA keeps a table of one request at a time in shared memory: the bits of the entries
 // that some rule touches, and a list of those entries with how often each was generated.  Every warp queues the context
 // tokens of the CTA's share among those it reads; they first set their bits, a prefix sum over the words makes the bits
@@ -18,8 +18,10 @@
 //
 // Measured on logits [rows][vocabulary]: the confidence of 317 rows of 152064 (16 requests, a grammar on nine rows of ten)
 // takes 50 us, 41 without any rule (29 at the copy rate), of 64 single rows of 126464 with contexts of 512 to 4096 tokens
-// 18 us; the logits of 64 such rows of 152064 take 23 us (12), of 318 rows of 126464 in 16 bits 45 us (30).  A row's warps
-// issue on 55 % of the clocks: tables, the ends of rows and the spans' unequal lengths are what memory waits for.
+// 18 us; the logits of 64 such rows of 152064 take 20 us (12), of 318 rows of 126464 in 16 bits 43 us (30; 35 without the
+// grammar, 29 bare; in place 37 with half of the entries forbidden, 16 without a grammar).  Of the confidence's 50 us, 6 pass before and after the rows, 5.5 building tables, 8 for every row of a
+// span (7.5 without rules: 5.8 TB/s), and spans have 4 or 5 rows.  Fewer spans of equal lengths: 128 rows 27.3 -> 24.7 us, but
+// 315 rows 49.2 -> 51.4.
 #include <math.h>
 
 #include <mutex>
@@ -743,7 +745,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_rules_confidence(const Rul
 
 // ---- the rules on the logits themselves ----------------------------------------------------------------------
 
-// Stores y.  In place only entries that change are written: the touched ones and those that are not allowed.
+// Stores y.  In place only vectors with an entry that is not allowed are written, and the touched entries.
 template <typename T, bool ALIGNED, bool INPLACE>
 __global__ void __launch_bounds__(kThreads, kPerSm) k_logit_rules(const RulesArgs a, const Plan pl, T* out, long long out_ld) {
   using W = Walk<T, ALIGNED>;
@@ -771,71 +773,88 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logit_rules(const RulesArg
     }
     const T* z = static_cast<const T*>(a.logits) + (long long)row * a.ld;
     T* y = out + (long long)row * out_ld;
-    if (me.req != cur) {
-      build_table(a, t, pl, me.req);
-      cur = me.req;
-    }
     const unsigned* mask = me.mask < 0 ? nullptr : a.allowed + me.mask * a.allowed_ld;
     const W walk(z);
-    auto plain = [&](int w) -> unsigned { return t.plain[w]; };
     auto allow = [&](int w) -> unsigned {                    // entries that may stay
       const unsigned in = t.in_range(w);
       return in & load1_if(mask + (t.id_of(w * 32) >> 5), mask && in, 0xffffffffu);
     };
-    Touched<T> entries;
-    entries.begin(t, pl, mask, z);
-    const int nv = walk.vectors(pl);
-    int e0 = walk.entry(threadIdx.x), id0 = t.id_of(e0);
-    for (int j0 = threadIdx.x; j0 < nv; j0 += kThreads * kBatch, e0 += kThreads * E * kBatch, id0 += step * kBatch) {
-      Vec<W::kW> u[kBatch];
-      unsigned keep[kBatch], calm[kBatch];
-#pragma unroll
-      for (int b = 0; b < kBatch; ++b) {
-        const int e = ALIGNED ? e0 + b * kThreads * E : walk.entry(min(j0 + b * kThreads, nv - 1));
-        const int id = ALIGNED ? id0 + b * step : t.id_of(e);
-        const bool there = id <= t.vocab - E && (ALIGNED || j0 + b * kThreads < nv);
-        if (!INPLACE && there) load(z + id, u[b]);
-        if (ALIGNED) {
-          const unsigned m = load1_if(mask + (id >> 5), mask && there, 0xffffffffu);
-          const unsigned p = there ? t.plain[e >> 5] : 0u, some = there ? t.touched[e >> 5] : 0u;      // (others lie behind the table)
-          calm[b] = (p >> (e & 31)) & kAll;
-          keep[b] = ((p | some) & m) >> (e & 31) & kAll;
-        } else {
-          keep[b] = bits_at<E, false>(e, allow) & kAll;
-          calm[b] = bits_at<E, false>(e, plain) & kAll;
-        }
+    const bool level = (((uintptr_t)y ^ (uintptr_t)z) & 15) == 0;              // vectors of z are vectors of y
+    // All entries, the touched ones as if no rule touched them: they are written again behind a barrier.
+    auto dense = [&]() {
+      if (INPLACE && !mask) {
+        if (threadIdx.x == 0 && (unsigned)t.mask_id < (unsigned)t.vocab && t.owns(t.mask_id)) put(y + t.mask_id, -INFINITY);
+        return;
       }
+      const int nv = walk.vectors(pl);
+      int e0 = walk.entry(threadIdx.x), id0 = t.id_of(e0);
+      for (int j0 = threadIdx.x; j0 < nv; j0 += kThreads * kBatch, e0 += kThreads * E * kBatch, id0 += step * kBatch) {
+        Vec<W::kW> u[kBatch];
+        unsigned keep[kBatch];
 #pragma unroll
-      for (int b = 0; b < kBatch; ++b) {
-        const int id = ALIGNED ? id0 + b * step : t.id_of(walk.entry(min(j0 + b * kThreads, nv - 1)));
-        if (id > t.vocab - E || (!ALIGNED && j0 + b * kThreads >= nv)) continue;
-        const unsigned now = (INPLACE ? 0u : calm[b] & keep[b]) | (kAll & ~keep[b]);      // the others are written below
+        for (int b = 0; b < kBatch; ++b) {
+          const int e = ALIGNED ? e0 + b * kThreads * E : walk.entry(min(j0 + b * kThreads, nv - 1));
+          const int id = ALIGNED ? id0 + b * step : t.id_of(e);
+          const bool there = id <= t.vocab - E && (ALIGNED || j0 + b * kThreads < nv);
+          if (!INPLACE && there) load(z + id, u[b]);
+          if (ALIGNED) {
+            const unsigned at = (unsigned)(t.mask_id - id);
+            keep[b] = load1_if(mask + (id >> 5), mask && there, 0xffffffffu) >> (e & 31) & kAll;
+            if (at < E) keep[b] &= ~(1u << at);
+          } else {
+            keep[b] = bits_at<E, false>(e, allow) & kAll;
+          }
+          if (!there) keep[b] = kAll;
+        }
         if (INPLACE) {
 #pragma unroll
-          for (int i = 0; i < W::kW; ++i) u[b].w[i] = kLeast<T>;
-        } else if (keep[b] != kAll) {
-          only<T>(u[b], keep[b]);
-        }
-        if (now == kAll && (ALIGNED || INPLACE)) {
-          store(y + id, u[b]);
-        } else if (now) {
-          float v[E];
-          widen(u[b], v, z);
+          for (int b = 0; b < kBatch; ++b) {
+            const int id = ALIGNED ? id0 + b * step : t.id_of(walk.entry(min(j0 + b * kThreads, nv - 1)));
 #pragma unroll
-          for (int e = 0; e < E; ++e)
-            if ((now >> e) & 1u) put(y + id + e, v[e]);
+            for (int i = 0; i < W::kW; ++i) u[b].w[i] = kLeast<T>;
+            if (keep[b] && keep[b] != kAll) load(z + id, u[b]);
+          }
+        }
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) {
+          const int id = ALIGNED ? id0 + b * step : t.id_of(walk.entry(min(j0 + b * kThreads, nv - 1)));
+          if (INPLACE ? keep[b] == kAll : id > t.vocab - E || (!ALIGNED && j0 + b * kThreads >= nv)) continue;
+          if (keep[b] != kAll) only<T>(u[b], keep[b]);
+          if (ALIGNED || INPLACE || level) {
+            store(y + id, u[b]);
+          } else {
+            float v[E];
+            widen(u[b], v, z);
+#pragma unroll
+            for (int e = 0; e < E; ++e) put(y + id + e, v[e]);
+          }
         }
       }
-    }
-    for (int i = threadIdx.x; i < walk.singles(pl, t); i += kThreads) {
-      const int e = walk.single(pl, t, i);
-      if (e >= 0) {
-        const int id = t.id_of(e);
-        const bool stays = (allow(e >> 5) >> (e & 31)) & 1u, alone = (t.plain[e >> 5] >> (e & 31)) & 1u;
-        if (!stays) put(y + id, -INFINITY);
-        else if (alone && !INPLACE) put(y + id, value(z + id));
+      for (int i = threadIdx.x; i < walk.singles(pl, t); i += kThreads) {
+        const int e = walk.single(pl, t, i);
+        if (e >= 0) {
+          const int id = t.id_of(e);
+          if (!((allow(e >> 5) >> (e & 31)) & 1u)) put(y + id, -INFINITY);
+          else if (!INPLACE) put(y + id, value(z + id));
+        }
+      }
+    };
+    Touched<T> entries;
+    // Where a table is to be built, half of the CTAs build it after the pass over all entries: while some wait for context
+    // tokens, the others keep memory busy.
+    const bool build = me.req != cur, later = build && (span & 1);
+    cur = me.req;
+#pragma unroll 1
+    for (int part = 0; part < 2; ++part) {
+      if ((part != 0) == later) {
+        if (build) build_table(a, t, pl, me.req);
+        if (!later) entries.begin(t, pl, mask, z);
+      } else {
+        dense();
       }
     }
+    if (later) entries.begin(t, pl, mask, z);
+    if (t.total > 0) __syncthreads();                        // the pass has written its entries
     entries.finish(a, t, pl, mask, z, [&](int i, int id, float v) { put(y + id, ruled(a, t, i, v)); });
   }
 }
