@@ -470,8 +470,8 @@ typedef struct {
 
 /* out[r, v] = the logit after the rules, rounded to the logits' type once.  logits [n_rows][ld] of type BS_F32 or BS_BF16
  * (stride in elements, at least vocab), 16-byte aligned; out the same with out_ld.  out = logits with out_ld = ld (or a
- * single row) works in place (only the touched entries and vectors of 16 or 32 bytes with a forbidden one are written); any other overlap is refused.  Entries at and behind vocab are left
- * as they were, and so are skipped rows. */
+ * single row) works in place (only the touched entries and vectors of 16 or 32 bytes with a forbidden one are written);
+ * any other overlap is refused.  Entries at and behind vocab are left as they were, and so are skipped rows. */
 int bs_op_logit_rules(const void* logits, int type, long long ld, void* out, long long out_ld, int n_rows,
                       const bs_logit_rules* rules, int* error_flag, void* stream);
 

@@ -19,9 +19,10 @@
 // Measured on logits [rows][vocabulary]: the confidence of 317 rows of 152064 (16 requests, a grammar on nine rows of ten)
 // takes 50 us, 41 without any rule (29 at the copy rate), of 64 single rows of 126464 with contexts of 512 to 4096 tokens
 // 18 us; the logits of 64 such rows of 152064 take 20 us (12), of 318 rows of 126464 in 16 bits 43 us (30; 35 without the
-// grammar, 29 bare; in place 37 with half of the entries forbidden, 16 without a grammar).  Of the confidence's 50 us, 6 pass before and after the rows, 5.5 building tables, 8 for every row of a
-// span (7.5 without rules: 5.8 TB/s), and spans have 4 or 5 rows.  Fewer spans of equal lengths: 128 rows 27.3 -> 24.7 us, but
-// 315 rows 49.2 -> 51.4.
+// grammar, 29 bare; in place 37 with half of the entries forbidden, 16 without a grammar).  Of the confidence's 50 us, 6 pass
+// before and after the rows, 5.5 building tables, 8 for every row of a span (7.5 without rules: 5.8 TB/s), and spans have 4
+// or 5 rows.  Fewer spans of equal lengths: 128 rows 27.3 -> 24.7 us, but 315 rows 49.2 -> 51.4.  Rows that are not
+// aligned, 317 of 152063: confidence 54 us without rules, logits 79 (aligned 42 and 69).
 #include <math.h>
 
 #include <mutex>
@@ -369,30 +370,36 @@ __device__ __forceinline__ bool valid(const RulesArgs& a, const Row& r) {
   return r.req >= -1 && r.req < a.n_reqs && r.mask >= -1 && r.mask < a.n_masks;
 }
 
-// A block of a row as vectors.  Rows at 32-byte boundaries: vectors of 32 bytes, all of it.  Others: kPer vectors of 16
-// bytes from entry `first` of the block on, and E entries (before and behind) one by one.  A vector that does not end
-// within the vocabulary is taken one by one, too.
+// A block of a row as vectors.  Rows at 32-byte boundaries: vectors of 32 bytes, all of it.  Others: vectors of 16 bytes
+// from entry `first` of the block on; the one that would pass the block's end is not taken (unless first is 0), and the
+// entries before and behind are taken one by one.  So is a vector that does not end within the vocabulary.  The vectors of
+// a thread are whole blocks apart.
 template <typename T, bool ALIGNED>
 struct Walk {
-  static constexpr int kW = ALIGNED ? 8 : 4, E = kW * 4 / sizeof(T), kPer = kBlock / E - (ALIGNED ? 0 : 1);
+  static constexpr int kW = ALIGNED ? 8 : 4, E = kW * 4 / sizeof(T), kSlots = kBlock / E;
   int first;
   __device__ __forceinline__ explicit Walk(const T* row)
       : first(ALIGNED ? 0 : (int)((E - (((uintptr_t)row & 15) / sizeof(T))) % E)) {}
-  __device__ __forceinline__ int vectors(const Plan& pl) const { return pl.blocks * kPer; }
+  __device__ __forceinline__ int vectors(const Plan& pl) const { return pl.blocks * kSlots; }
+  __device__ __forceinline__ int per() const { return kSlots - (first != 0); }
   // first entry of vector j of the CTA's share
-  __device__ __forceinline__ int entry(int j) const { return ALIGNED ? j * E : j / kPer * kBlock + first + j % kPer * E; }
+  __device__ __forceinline__ int entry(int j) const { return j * E + first; }
+  // the largest token with which a vector of this thread begins
+  __device__ __forceinline__ int reach(const Table& t) const { return (int)(threadIdx.x & (kSlots - 1)) < per() ? t.vocab - E : -1; }
   // entry i of those taken one by one, -1: none (i < singles)
-  __device__ __forceinline__ int singles(const Plan& pl, const Table& t) const { return ALIGNED ? (t.vocab % E ? E : 0) : (pl.blocks + 1) * E; }
+  __device__ __forceinline__ int singles(const Plan& pl, const Table& t) const {
+    return first == 0 ? (t.vocab % E ? E : 0) : (pl.blocks + 1) * E;
+  }
   __device__ __forceinline__ int single(const Plan& pl, const Table& t, int i) const {
     int e;
     if (i < E) {                                             // the end of the vocabulary, where it is in a vector's middle
       const int last = (t.vocab - 1) & ~(kBlock - 1);        // the block that holds it
       const int begin = last + first, id = begin + (t.vocab - begin) / E * E + i;
-      if (t.vocab < begin || !t.owns(last) || id >= t.vocab || id - last >= first + kPer * E) return -1;
+      if (t.vocab < begin || !t.owns(last) || id >= t.vocab || id - last >= first + per() * E) return -1;
       return t.entry_of(id);
     }
     const int k = i % E;
-    e = (i / E - 1) * kBlock + (k < first ? k : kPer * E + k);
+    e = (i / E - 1) * kBlock + (k < first ? k : per() * E + k);
     return t.id_of(e) < t.vocab ? e : -1;
   }
 };
@@ -525,7 +532,7 @@ __device__ __forceinline__ unsigned long long pair_of(float x) {
 template <typename T, bool ALIGNED>
 __global__ void __launch_bounds__(kThreads, kPerSm) k_rules_confidence(const RulesArgs a, const Plan pl, int* tok, float* conf) {
   using W = Walk<T, ALIGNED>;
-  constexpr int E = W::E, kBatch = ALIGNED ? 2 : 4;          // vectors a thread has in flight
+  constexpr int E = W::E, kBatch = ALIGNED ? 2 : 3;          // vectors a thread has in flight (four: spills)
   constexpr unsigned kAll = (1u << E) - 1u;
   extern __shared__ __align__(16) unsigned smem[];
   __shared__ Slot parts[kRowsAtOnce * kWarps];               // of the rows that this CTA joins: [row][chunk][warp]
@@ -592,23 +599,24 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_rules_confidence(const Rul
       const int nv = walk.vectors(pl);
       auto dense = [&](auto masked) {
         int e0 = walk.entry(threadIdx.x), id0 = t.id_of(e0);
+        const int reach = walk.reach(t);
         const unsigned shift = ALIGNED ? e0 & 31 : 0;        // (the same for all of a thread's vectors)
+        const unsigned low = e0 & 31;
+        const bool two = low > 32 - E;                       // its bits are in two words
         const unsigned* words = mask + (id0 >> 5);
         unsigned ahead[kBatch];                              // the mask's words of the next batch
         if (ALIGNED && masked.value) {
 #pragma unroll
-          for (int b = 0; b < kBatch; ++b) ahead[b] = load1_if(words + b * (step >> 5), b * step <= t.vocab - E - id0, 0u);
+          for (int b = 0; b < kBatch; ++b) ahead[b] = load1_if(words + b * (step >> 5), b * step <= reach - id0, 0u);
         }
         for (int j0 = threadIdx.x; j0 < nv; j0 += kThreads * kBatch, e0 += kThreads * E * kBatch, id0 += step * kBatch, words += (step >> 5) * kBatch) {
           unsigned bits[kBatch], every = 0xffffffffu, any = 0u;
           Vec<W::kW> u[kBatch];
-          // aligned rows: a thread's vectors are whole blocks apart, those that are not there lie behind the vocabulary
-          const int left = ALIGNED ? t.vocab - E - id0 : 0;
+          const int left = reach - id0;                      // vectors that are not there lie behind the vocabulary
 #pragma unroll
           for (int b = 0; b < kBatch; ++b) {
-            const int e = ALIGNED ? e0 + b * kThreads * E : walk.entry(min(j0 + b * kThreads, nv - 1));
-            const int id = ALIGNED ? id0 + b * step : t.id_of(e);
-            const bool there = ALIGNED ? b * step <= left : id <= t.vocab - E && j0 + b * kThreads < nv;
+            const int e = e0 + b * kThreads * E, id = id0 + b * step;
+            const bool there = b * step <= left;
 #pragma unroll
             for (int i = 0; i < W::kW; ++i) u[b].w[i] = kLeast<T>;               // (what is not there is -inf)
             if (ALIGNED) {
@@ -620,7 +628,12 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_rules_confidence(const Rul
               if (masked.value ? bits[b] != 0u : there) load(z + id, u[b]);
             } else {
               if (there) load(z + id, u[b]);
-              bits[b] = bits_at<E, false>(e, usable) | (there ? 0u : kAll);
+              unsigned lo = there ? t.plain[e >> 5] : 0xffffffffu, hi = there && two ? t.plain[(e >> 5) + 1] : 0xffffffffu;
+              if (masked.value) {
+                lo &= load1_if(words + b * (step >> 5), there, 0xffffffffu);
+                hi &= load1_if(words + b * (step >> 5) + 1, there && two, 0xffffffffu);
+              }
+              bits[b] = __funnelshift_r(lo, hi, low) & kAll;
             }
           }
           if (ALIGNED && masked.value) {
@@ -786,39 +799,37 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logit_rules(const RulesArg
         if (threadIdx.x == 0 && (unsigned)t.mask_id < (unsigned)t.vocab && t.owns(t.mask_id)) put(y + t.mask_id, -INFINITY);
         return;
       }
-      const int nv = walk.vectors(pl);
-      int e0 = walk.entry(threadIdx.x), id0 = t.id_of(e0);
-      for (int j0 = threadIdx.x; j0 < nv; j0 += kThreads * kBatch, e0 += kThreads * E * kBatch, id0 += step * kBatch) {
+      const int nv = walk.vectors(pl), reach = walk.reach(t);
+      int id0 = t.id_of(walk.entry(threadIdx.x));
+      const unsigned low = id0 & 31;
+      const bool two = !ALIGNED && low > 32 - E;             // a vector's bits are in two words
+      for (int j0 = threadIdx.x; j0 < nv; j0 += kThreads * kBatch, id0 += step * kBatch) {
         Vec<W::kW> u[kBatch];
         unsigned keep[kBatch];
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) {
-          const int e = ALIGNED ? e0 + b * kThreads * E : walk.entry(min(j0 + b * kThreads, nv - 1));
-          const int id = ALIGNED ? id0 + b * step : t.id_of(e);
-          const bool there = id <= t.vocab - E && (ALIGNED || j0 + b * kThreads < nv);
+          const int id = id0 + b * step;
+          const bool there = id <= reach;
           if (!INPLACE && there) load(z + id, u[b]);
-          if (ALIGNED) {
-            const unsigned at = (unsigned)(t.mask_id - id);
-            keep[b] = load1_if(mask + (id >> 5), mask && there, 0xffffffffu) >> (e & 31) & kAll;
-            if (at < E) keep[b] &= ~(1u << at);
-          } else {
-            keep[b] = bits_at<E, false>(e, allow) & kAll;
-          }
+          const unsigned at = (unsigned)(t.mask_id - id);
+          const unsigned word = load1_if(mask + (id >> 5), mask && there, 0xffffffffu);
+          const unsigned more = ALIGNED ? 0u : load1_if(mask + (id >> 5) + 1, mask && there && two, 0xffffffffu);
+          keep[b] = (ALIGNED ? word >> low : __funnelshift_r(word, more, low)) & kAll;
+          if (at < E) keep[b] &= ~(1u << at);
           if (!there) keep[b] = kAll;
         }
         if (INPLACE) {
 #pragma unroll
           for (int b = 0; b < kBatch; ++b) {
-            const int id = ALIGNED ? id0 + b * step : t.id_of(walk.entry(min(j0 + b * kThreads, nv - 1)));
 #pragma unroll
             for (int i = 0; i < W::kW; ++i) u[b].w[i] = kLeast<T>;
-            if (keep[b] && keep[b] != kAll) load(z + id, u[b]);
+            if (keep[b] && keep[b] != kAll) load(z + id0 + b * step, u[b]);
           }
         }
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) {
-          const int id = ALIGNED ? id0 + b * step : t.id_of(walk.entry(min(j0 + b * kThreads, nv - 1)));
-          if (INPLACE ? keep[b] == kAll : id > t.vocab - E || (!ALIGNED && j0 + b * kThreads >= nv)) continue;
+          const int id = id0 + b * step;
+          if (INPLACE ? keep[b] == kAll : id > reach) continue;
           if (keep[b] != kAll) only<T>(u[b], keep[b]);
           if (ALIGNED || INPLACE || level) {
             store(y + id, u[b]);
