@@ -6,7 +6,7 @@
 // Bound by memory: x is read once, a byte an element is written.  The threads of a row keep it in registers as it is stored
 // (32 elements each, all loads in flight before the first use) between the maximum and the rounding; rows too long for that
 // are read twice, the second time from L2.  Short rows share a CTA of up to 256 threads.  Measured: 4096 rows of 18944 bf16 in
-// 42 us (5.5 TB/s of 6.56 copied), 16384 rows of 4096 fp32 in 50 us (6.7), 16 rows of 3584 in 2.2 us.
+// 42 us (5.5 TB/s of 6.56 copied), in fp32 in 58 (6.6), 16 rows of 3584 in 2.2 us.
 // A row with an infinite or NaN element has no scale: NaN, with zero codes, so that every product of it is NaN.
 #include "decode_ops.cuh"
 
@@ -147,10 +147,13 @@ __device__ __forceinline__ unsigned largest(const Unit<F32>& r, const bf16* gain
   return top;
 }
 
-// (plain bf16 rows: two CTAs of up to 1024 threads an SM, 32 registers a thread, three of the longest rows in flight instead
-// of two: 4096 x 18944 47 -> 42 us; the others would spill)
+// Two CTAs an SM at least: of up to 1024 threads with 32 registers each for plain bf16 rows (three of 592: 4096 x
+// 18944 47 -> 42 us), where the others would spill; those have up to 640 threads (4096 x 18944 fp32 with 1024: one CTA, 81 us,
+// so 58; norms of bf16 rows 106 and 73, unaligned ones 133 and 79).
 template <bool F32, bool VEC, bool NORM, bool LONG>
-__global__ void __launch_bounds__(1024, F32 || NORM || !VEC || LONG ? 1 : 2) k_quant_i8(const QuantI8Args a) {
+constexpr int kMost = F32 || NORM || !VEC || LONG ? 640 : 1024;
+template <bool F32, bool VEC, bool NORM, bool LONG>
+__global__ void __launch_bounds__(kMost<F32, VEC, NORM, LONG>, 2) k_quant_i8(const QuantI8Args a) {
   __shared__ unsigned s_max[32];
   __shared__ float s_sum[32];
   pdl_wait();
@@ -234,8 +237,8 @@ template <bool F32, bool VEC>
 cudaError_t launch_typed(const QuantI8Args& a, cudaStream_t s) {
   const int units = (a.K + kUnit - 1) / kUnit;
   int threads = ((units + kUnits - 1) / kUnits + 31) / 32 * 32;
-  const bool lng = threads > 1024;
-  if (lng) threads = 1024;
+  const bool lng = threads > (a.gain ? kMost<F32, VEC, true, false> : kMost<F32, VEC, false, false>);
+  if (lng) threads = kMost<F32, VEC, false, true>;
   void (*k)(const QuantI8Args);
   if (a.gain) k = lng ? k_quant_i8<F32, VEC, true, true> : k_quant_i8<F32, VEC, true, false>;
   else k = lng ? k_quant_i8<F32, VEC, false, true> : k_quant_i8<F32, VEC, false, false>;
