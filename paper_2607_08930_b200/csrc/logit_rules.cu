@@ -17,12 +17,12 @@
 // without scratch.
 //
 // Measured on logits [rows][vocabulary]: the confidence of 317 rows of 152064 (16 requests, a grammar on nine rows of ten)
-// takes 50 us, 41 without any rule (29 at the copy rate), of 64 single rows of 126464 with contexts of 512 to 4096 tokens
-// 18 us; the logits of 64 such rows of 152064 take 20 us (12), of 318 rows of 126464 in 16 bits 43 us (30; 35 without the
-// grammar, 29 bare; in place 37 with half of the entries forbidden, 16 without a grammar).  Of the confidence's 50 us, 6 pass
-// before and after the rows, 5.5 building tables, 8 for every row of a span (7.5 without rules: 5.8 TB/s), and spans have 4
-// or 5 rows.  Fewer spans of equal lengths: 128 rows 27.3 -> 24.7 us, but 315 rows 49.2 -> 51.4.  Rows that are not
-// aligned, 317 of 152063: confidence 54 us without rules, logits 79 (aligned 42 and 69).
+// takes 48 us, 41 without any rule (29 at the copy rate), of 64 single rows of 126464 with contexts of 512 to 4096 tokens
+// 17 us; the logits of 64 such rows of 152064 take 20 us (12), of 318 rows of 126464 in 16 bits 43 us (30; 35 without the
+// grammar, 29 bare; in place 37 with half of the entries forbidden, 16 without a grammar).  Of the confidence's 48 us, 6 pass
+// before and after the rows, 5 building tables, 7.5 for every row of a span (5.8 TB/s), and spans have 4 or 5 rows.  Fewer
+// spans of equal lengths: 128 rows 27.3 -> 24.7 us, but 315 rows 49.2 -> 51.4.  Rows that are not aligned, 317 of 152063:
+// confidence 51 us without rules, logits 79 (aligned 41 and 69).
 #include <math.h>
 
 #include <mutex>
@@ -458,29 +458,38 @@ __device__ __forceinline__ void store(void* p, const Vec<8>& u) {
 template <typename T>
 constexpr unsigned kLeast = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;     // a word of -inf
 
-// Entries without their bit (the lowest is the first's) become -inf.  A product puts four bits at the tops of four bytes
-// (the shifted copies do not meet), from where a byte permutation spreads them over a word: two instructions a word.
+// Entries without their bit (the lowest is the first's) become -inf.  In 16 bits a product puts four bits at the tops of
+// four bytes (the shifted copies do not meet), from where a byte permutation spreads them over a word.
 template <typename T, int N>
 __device__ __forceinline__ void only(Vec<N>& u, unsigned bits) {
-  constexpr int kPerWord = 4 / sizeof(T), kGroup = 4 / kPerWord;             // words that four bits decide about
+  if constexpr (sizeof(T) == 4) {
 #pragma unroll
-  for (int g = 0; g < N / kGroup; ++g) {
-    const unsigned tops = (bits >> (4 * g) & 15u) * 0x10204080u;
+    for (int i = 0; i < N; ++i) u.w[i] = (bits >> i) & 1u ? u.w[i] : kLeast<T>;
+  } else {
 #pragma unroll
-    for (int i = 0; i < kGroup; ++i) {
-      unsigned keep;                                         // (the permutation's selectors repeat a byte's top bit)
-      asm("prmt.b32 %0, %1, %1, %2;" : "=r"(keep) : "r"(tops), "r"(sizeof(T) == 4 ? 0x8888u + 0x1111u * i : (i ? 0xbbaau : 0x9988u)));
-      unsigned& w = u.w[g * kGroup + i];
-      w = (w & keep) | (kLeast<T> & ~keep);
+    for (int g = 0; g < N / 2; ++g) {
+      const unsigned tops = (bits >> (4 * g) & 15u) * 0x10204080u;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        unsigned keep;                                       // (the permutation's selectors repeat a byte's top bit)
+        asm("prmt.b32 %0, %1, %1, %2;" : "=r"(keep) : "r"(tops), "r"(i ? 0xbbaau : 0x9988u));
+        unsigned& w = u.w[g * 2 + i];
+        w = (w & keep) | (kLeast<T> & ~keep);
+      }
     }
   }
 }
 // The largest entry (NaN are passed over).
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
 template <int N>
 __device__ __forceinline__ float largest(const Vec<N>& u, const float*) {
-  float m = __uint_as_float(u.w[0]);
+  float m = fmaxf(__uint_as_float(u.w[0]), __uint_as_float(u.w[1]));
 #pragma unroll
-  for (int i = 1; i < N; ++i) m = fmaxf(m, __uint_as_float(u.w[i]));
+  for (int i = 2; i < N; i += 2) m = max3(m, __uint_as_float(u.w[i]), __uint_as_float(u.w[i + 1]));
   return m;
 }
 template <int N>
@@ -596,7 +605,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_rules_confidence(const Rul
       float m = -INFINITY;
       unsigned long long s2 = 0ull;
       int best = threadIdx.x;                                // the batch that holds m: its first vector
-      const int nv = walk.vectors(pl);
+      const int nv = t.vocab < walk.first + E ? 0 : walk.vectors(pl);
       auto dense = [&](auto masked) {
         int e0 = walk.entry(threadIdx.x), id0 = t.id_of(e0);
         const int reach = walk.reach(t);
@@ -617,21 +626,20 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_rules_confidence(const Rul
           for (int b = 0; b < kBatch; ++b) {
             const int e = e0 + b * kThreads * E, id = id0 + b * step;
             const bool there = b * step <= left;
-#pragma unroll
-            for (int i = 0; i < W::kW; ++i) u[b].w[i] = kLeast<T>;               // (what is not there is -inf)
             if (ALIGNED) {
               bits[b] = masked.value ? ahead[b] : 0xffffffffu;
               bits[b] &= t.plain[there ? e >> 5 : 0];        // (others lie behind the table)
-              if (!masked.value && !there) bits[b] = 0xffffffffu;
+              if (!masked.value && !there) bits[b] = 0u;     // (without bits: -inf)
               if (masked.value) bits[b] = bits[b] >> shift & kAll;
-              // a grammar often leaves a handful of tokens: vectors without any are not read
-              if (masked.value ? bits[b] != 0u : there) load(z + id, u[b]);
+              // a grammar often leaves a handful of tokens: vectors without any are not read (the row's first is, instead:
+              // a load under a condition would keep the registers' old values alive)
+              load(z + ((masked.value ? bits[b] != 0u : there) ? id : walk.first), u[b]);
             } else {
-              if (there) load(z + id, u[b]);
-              unsigned lo = there ? t.plain[e >> 5] : 0xffffffffu, hi = there && two ? t.plain[(e >> 5) + 1] : 0xffffffffu;
+              load(z + (there ? id : walk.first), u[b]);
+              unsigned lo = there ? t.plain[e >> 5] : 0u, hi = there && two ? t.plain[(e >> 5) + 1] : 0u;
               if (masked.value) {
-                lo &= load1_if(words + b * (step >> 5), there, 0xffffffffu);
-                hi &= load1_if(words + b * (step >> 5) + 1, there && two, 0xffffffffu);
+                lo &= load1_if(words + b * (step >> 5), there, 0u);
+                hi &= load1_if(words + b * (step >> 5) + 1, there && two, 0u);
               }
               bits[b] = __funnelshift_r(lo, hi, low) & kAll;
             }
