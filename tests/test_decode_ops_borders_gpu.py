@@ -55,6 +55,23 @@ def test_odd_values_and_masks(B, dtype, vocab):
         check_rules(B, z, r, vocab, reqs, dtype)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("vocab,pad,out_pad", [(7, 0, 2), (1000, 0, 5), (1000, 1, 0), (2003, 5, 2), (40001, 2, 3), (40001, 7, 15)])
+def test_outputs_at_other_alignments_than_the_logits(B, dtype, vocab, pad, out_pad):
+    """Rows of logits and of outputs start at different places within 16 bytes; what is stored is exact."""
+    rng = np.random.default_rng(vocab + pad)
+    rows, reqs = 21, 4
+    r = make_rules(rng, rows, vocab, reqs, min(300, vocab), 10, 5)
+    z = torch.from_numpy((3 * rng.normal(size=(rows, vocab))).astype(np.float32)).to(dtype)
+    y = D.rules(z.float().numpy(), r["row_req"], vocab, **{k: v for k, v in r.items() if k != "row_req"})
+    store = torch.full((rows, vocab + pad), 2.5, dtype=dtype, device="cuda")
+    store[:, :vocab] = z.cuda()
+    out = torch.full((rows, vocab + out_pad), 1.5, dtype=dtype, device="cuda")
+    B.op_logit_rules(store[:, :vocab], to_rules(B, r, vocab, reqs), out=out[:, :vocab])
+    assert torch.equal(out[:, :vocab].cpu(), torch.from_numpy(y).to(dtype))
+    assert (out[:, vocab:] == 1.5).all()
+
+
 @pytest.mark.parametrize("drop", ["ctx", "bias", "allowed", "row_req", "row_mask", "repetition", "presence", "frequency", "mask_id", "all"])
 def test_rules_that_are_absent(B, drop):
     rng = np.random.default_rng(3)
