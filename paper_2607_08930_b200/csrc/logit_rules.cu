@@ -252,6 +252,7 @@ __device__ __forceinline__ void build_table(const RulesArgs& a, Table& t, const 
     for (int k = 0; k < kTokens; ++k) id[k] = i0 + k * kThreads < end ? __ldg(a.ctx + i0 + k * kThreads) : -1;
 #pragma unroll
     for (int k = 0; k < kTokens; ++k) {
+      if (i0 - lane + k * kThreads >= end) break;            // (the same for a warp)
       const bool mine = t.takes(id[k]);
       const unsigned all = __ballot_sync(0xffffffffu, mine);
       const int at = t.queued + __popc(all & ((1u << lane) - 1u));
@@ -458,25 +459,31 @@ __device__ __forceinline__ void store(void* p, const Vec<8>& u) {
 template <typename T>
 constexpr unsigned kLeast = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;     // a word of -inf
 
-// Entries without their bit (the lowest is the first's) become -inf.  In 16 bits a product puts four bits at the tops of
-// four bytes (the shifted copies do not meet), from where a byte permutation spreads them over a word.
+// Entries without their bit (the lowest is the first's) become -inf.  A product puts four bits at the tops of four bytes
+// (the shifted copies do not meet), from where a byte permutation spreads them over a word.
 template <typename T, int N>
 __device__ __forceinline__ void only(Vec<N>& u, unsigned bits) {
+  constexpr int kPerWord = 4 / sizeof(T), kGroup = 4 / kPerWord;             // words that four bits decide about
+#pragma unroll
+  for (int g = 0; g < N / kGroup; ++g) {
+    const unsigned tops = (bits >> (4 * g) & 15u) * 0x10204080u;
+#pragma unroll
+    for (int i = 0; i < kGroup; ++i) {
+      unsigned keep;                                         // (the permutation's selectors repeat a byte's top bit)
+      asm("prmt.b32 %0, %1, %1, %2;" : "=r"(keep) : "r"(tops), "r"(sizeof(T) == 4 ? 0x8888u + 0x1111u * i : (i ? 0xbbaau : 0x9988u)));
+      unsigned& w = u.w[g * kGroup + i];
+      w = (w & keep) | (kLeast<T> & ~keep);
+    }
+  }
+}
+// The same with a select an entry where they are words: fewer instructions, but more registers where stores follow.
+template <typename T, int N>
+__device__ __forceinline__ void only_selected(Vec<N>& u, unsigned bits) {
   if constexpr (sizeof(T) == 4) {
 #pragma unroll
     for (int i = 0; i < N; ++i) u.w[i] = (bits >> i) & 1u ? u.w[i] : kLeast<T>;
   } else {
-#pragma unroll
-    for (int g = 0; g < N / 2; ++g) {
-      const unsigned tops = (bits >> (4 * g) & 15u) * 0x10204080u;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        unsigned keep;                                       // (the permutation's selectors repeat a byte's top bit)
-        asm("prmt.b32 %0, %1, %1, %2;" : "=r"(keep) : "r"(tops), "r"(i ? 0xbbaau : 0x9988u));
-        unsigned& w = u.w[g * 2 + i];
-        w = (w & keep) | (kLeast<T> & ~keep);
-      }
-    }
+    only<T>(u, bits);
   }
 }
 // The largest entry (NaN are passed over).
@@ -658,7 +665,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_rules_confidence(const Rul
           }
           if (masked.value || ((every >> shift) & kAll) != kAll) {
 #pragma unroll
-            for (int b = 0; b < kBatch; ++b) only<T>(u[b], masked.value ? bits[b] : bits[b] >> shift);
+            for (int b = 0; b < kBatch; ++b) only_selected<T>(u[b], masked.value ? bits[b] : bits[b] >> shift);
           }
           float top = largest(u[0], z);
 #pragma unroll
