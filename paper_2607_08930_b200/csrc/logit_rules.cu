@@ -268,7 +268,8 @@ __device__ __forceinline__ void build_table(const RulesArgs& a, Table& t, const 
   __syncwarp();
   for (int i = lane; i < min(t.queued, kQueue); i += 32) touch((int)(t.queue[i] & 0xffffu));
   for (int i = lo + threadIdx.x; i < hi; i += kThreads) {
-    if (t.takes(b_id)) touch(t.entry_of(b_id));
+    // (the first of equal ones, as list_touched has it: each place of the list has a writer whatever the order is)
+    if (t.takes(b_id) && b_before < b_id) touch(t.entry_of(b_id));
     bad = bad || (unsigned)b_id >= (unsigned)t.vocab || b_before > b_id;
     b_id = (int)load1_if(a.bias_tok + i + kThreads, i + kThreads < hi, 0xffffffffu);
     b_before = (int)load1_if(a.bias_tok + i + kThreads - 1, i + kThreads < hi, 0xffffffffu);

@@ -1,0 +1,101 @@
+"""What the 8-bit row codes, the 8-bit projections and the logit rules do at the edges of what they accept, against the
+64-bit oracle (needs a B200)."""
+import itertools
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import decode_oracle as D
+from test_decode_ops_gpu import B, CONF_TOL, f32, host, ints  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def new_flag():
+    return torch.zeros(1, dtype=torch.int32, device="cuda")
+
+
+# ---- bias lists that do not ascend, or name what is no token ----------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("vocab,pad", [(700, 0), (701, 0), (40001, 0), (126464, 64)])
+@pytest.mark.parametrize("tok", [[5, 4], [7, 3, 9], [2, 1 << 20, 5], [600, 5, 600, 5], [-1, 3], [3, 3, 2, 2], [9, 8, 7, 6]])
+def test_biases_out_of_order_touch_nothing_else(B, dtype, vocab, pad, tok):
+    """The request's rows lie in the middle of a larger buffer.  Of its biases some count (which is not defined); every
+    other entry, the other requests' rows and the memory around them are as without the list."""
+    rng = np.random.default_rng(vocab + len(tok))
+    rows, mid = 5, [1, 2, 3]
+    row_req = np.array([0, 1, 1, 1, 2])
+    ctx = rng.integers(0, vocab, 60)
+    ctx[:3] = [3, 5, 600]
+    r = dict(mask_id=vocab - 1, ctx=ctx, begin=[0, 0, 20], gen=[5, 9, 30], end=[20, 20, 60],
+             repetition=np.array([1.2, 1.3, 1.1], np.float32), presence=np.array([0.3, 0.2, 0.1], np.float32))
+    val = np.linspace(0.5, 2.0, len(tok)).astype(np.float32)
+    z = torch.from_numpy((3 * rng.normal(size=(rows, vocab))).astype(np.float32)).to(dtype)
+    plain = D.rules(z.float().numpy(), row_req, vocab, **r)
+    rules = B.logit_rules(vocab, ints(row_req), 3, mask_id=vocab - 1, ctx=ints(ctx), ctx_begin=ints(r["begin"]),
+                          ctx_gen=ints(r["gen"]), ctx_end=ints(r["end"]), repetition=f32(r["repetition"]),
+                          presence=f32(r["presence"]), bias_at=ints([0, 0, len(tok), len(tok)]), bias_tok=ints(tok),
+                          bias_val=f32(val))
+    named = sorted({t for t in tok if 0 <= t < vocab - 1})
+    rest = np.setdiff1d(np.arange(vocab), named)
+    guard = 16                                               # rows of it on either side
+
+    def buffer():
+        store = torch.full((rows + 2 * guard, vocab + pad), 77.0, dtype=dtype, device="cuda")
+        return store, store[guard:guard + rows, :vocab]
+
+    def check(store, view):
+        got, want = view.cpu(), torch.from_numpy(plain).to(dtype)
+        assert torch.equal(got[[0, 4]], want[[0, 4]])
+        assert torch.equal(got[:, rest], want[:, rest])
+        view.fill_(77.0)
+        assert (store == 77.0).all()
+
+    store, view = buffer()
+    view.copy_(z.cuda())
+    flag = new_flag()
+    tok_out, conf = torch.full((rows + 8,), -9, dtype=torch.int32, device="cuda"), torch.full((rows + 8,), -9.0, device="cuda")
+    B.op_rules_confidence(view, rules, tok=tok_out[4:4 + rows], conf=conf[4:4 + rows], error_flag=flag)
+    assert int(flag) >= 100
+    assert (tok_out[[0, 1, 2, 3, -1]] == -9).all() and (conf[[0, 1, 2, 3, -1]] == -9).all()
+    # the outcomes that some of the biases could give
+    some = [D.confidence(plain)]
+    for n in range(1, len(tok) + 1):
+        for which in itertools.combinations([i for i, t in enumerate(tok) if t in named], n):
+            y = plain.copy()
+            for i in which:
+                y[mid, tok[i]] += val[i]
+            some.append(D.confidence(y))
+    t, c = tok_out[4:4 + rows].cpu().numpy(), host(conf[4:4 + rows])
+    for row in range(rows):
+        assert any(t[row] == tt[row] and abs(c[row] - cc[row]) <= cc[row] * CONF_TOL for tt, cc in some), row
+    flag.zero_()
+    out_store, out = buffer()
+    B.op_logit_rules(view, rules, out=out, error_flag=flag)
+    assert int(flag) >= 100
+    check(out_store, out)
+    flag.zero_()
+    B.op_logit_rules(view, rules, error_flag=flag)           # in place
+    assert int(flag) >= 100
+    check(store, view)
+
+
+@pytest.mark.parametrize("vocab,length", [(2003, 300), (9000, 9000), (40001, 30000)])
+def test_long_lists_of_biases_in_any_order(B, vocab, length):
+    rng = np.random.default_rng(length)
+    tok = rng.integers(-5, vocab // 2, length)               # the upper half is not named
+    store = torch.full((24, vocab), 77.0, device="cuda")
+    z = torch.randn(4, vocab, device="cuda")
+    store[12:16] = z
+    flag = new_flag()
+    rules = B.logit_rules(vocab, None, 4, bias_at=ints([0, 0, length, length, length]), bias_tok=ints(tok),
+                          bias_val=torch.ones(length, device="cuda"))
+    _, conf = B.op_rules_confidence(store[12:16].clone(), rules)
+    B.op_logit_rules(store[12:16], rules, error_flag=flag)
+    assert int(flag) >= 100 and torch.isfinite(conf).all()
+    assert torch.equal(store[12:16][[0, 2, 3]], z[[0, 2, 3]])
+    rest = np.setdiff1d(np.arange(vocab), tok)
+    assert torch.equal(store[13, rest], z[1, rest]) and torch.isfinite(store[13]).all()
+    assert (store[:12] == 77.0).all() and (store[16:] == 77.0).all()
