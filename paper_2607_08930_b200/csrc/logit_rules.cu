@@ -414,8 +414,8 @@ __device__ __forceinline__ unsigned bits_at(int e, F word) {
   return __funnelshift_r(word(w), (e & 31) > 32 - E ? word(w + 1) : 0u, e & 31);
 }
 
-__device__ __forceinline__ unsigned ordered(float m) {       // unsigned order of floats (no NaN)
-  const unsigned u = __float_as_uint(m);
+__device__ __forceinline__ unsigned ordered(float m) {       // unsigned order of floats (no NaN); -0 counts as +0
+  const unsigned u = __float_as_uint(__fadd_rn(m, 0.f));
   return u ^ ((unsigned)((int)u >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float unordered(unsigned u) {

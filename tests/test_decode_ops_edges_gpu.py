@@ -99,3 +99,30 @@ def test_long_lists_of_biases_in_any_order(B, vocab, length):
     rest = np.setdiff1d(np.arange(vocab), tok)
     assert torch.equal(store[13, rest], z[1, rest]) and torch.isfinite(store[13]).all()
     assert (store[:12] == 77.0).all() and (store[16:] == 77.0).all()
+
+
+# ---- zeros of both signs ----------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("vocab,pad", [(1000, 0), (1001, 2), (40001, 0), (126464, 0)])
+@pytest.mark.parametrize("masked", [False, True])
+def test_the_lowest_of_zeros_of_both_signs(B, dtype, vocab, pad, masked):
+    """Rows whose largest logits are a zero of one sign and, in another warp's entries, a zero of the other: the lower id
+    every time, whichever warp is first."""
+    rng = np.random.default_rng(vocab)
+    rows = 256
+    z = np.full((rows, vocab), -4.0, np.float32)
+    low = rng.integers(0, vocab - 300, rows)
+    high = low + rng.integers(100, np.minimum(vocab - low, 5000))
+    z[np.arange(rows), low] = np.where(np.arange(rows) % 4 < 3, -0.0, 0.0)
+    z[np.arange(rows), high] = np.where(np.arange(rows) % 4 < 3, 0.0, -0.0)
+    store = torch.zeros(rows, vocab + pad, dtype=dtype, device="cuda")
+    store[:, :vocab] = f32(z).to(dtype)
+    every = torch.full((1, (vocab + 31) // 32), -1, dtype=torch.int32, device="cuda")
+    # (request 0's context holds the lower zero of a few rows, which a repetition penalty keeps)
+    rules = B.logit_rules(vocab, torch.zeros(rows, dtype=torch.int32, device="cuda"), 1, ctx=ints(low[:5]), ctx_begin=ints([0]),
+                          ctx_gen=ints([5]), ctx_end=ints([5]), repetition=f32([1.25]), allowed=every if masked else None,
+                          row_mask=torch.zeros(rows, dtype=torch.int32, device="cuda") if masked else None)
+    for _ in range(30):
+        tok, _ = B.op_rules_confidence(store[:, :vocab], rules)
+        assert np.array_equal(tok.cpu().numpy(), low)
