@@ -1166,9 +1166,11 @@ static bool rules_args(const void* logits, int type, long long ld, int n_rows, c
       extent(r->allowed ? r->row_mask : nullptr, n_rows, 4, 4)};
   const Extent z = extent(logits, n_rows, ld * size, (long long)r->vocab * size);
   if (meets(out, in) || meets(out2, in) || (!inplace && meets(out, {z})) || meets(out2, {z, out})) return false;
-  *a = RulesArgs{logits, ld, type == BS_BF16, n_rows, r->vocab, r->n_reqs, r->mask_id, r->row_req, r->ctx, r->ctx_total,
-                 r->ctx_begin, r->ctx_gen, r->ctx_end, r->repetition, r->presence, r->frequency, r->bias_at, r->bias_tok,
-                 r->bias_val, r->bias_total, r->allowed, r->allowed_ld, r->n_masks, r->row_mask, error_flag};
+  // (the counts of absent rules may hold anything)
+  *a = RulesArgs{logits, ld, type == BS_BF16, n_rows, r->vocab, r->n_reqs, r->mask_id, r->row_req, r->ctx,
+                 r->ctx ? r->ctx_total : 0, r->ctx_begin, r->ctx_gen, r->ctx_end, r->repetition, r->presence, r->frequency,
+                 r->bias_at, r->bias_tok, r->bias_val, r->bias_at ? r->bias_total : 0, r->allowed, r->allowed_ld,
+                 r->allowed ? r->n_masks : 0, r->row_mask, error_flag};
   return true;
 }
 

@@ -126,3 +126,22 @@ def test_the_lowest_of_zeros_of_both_signs(B, dtype, vocab, pad, masked):
     for _ in range(30):
         tok, _ = B.op_rules_confidence(store[:, :vocab], rules)
         assert np.array_equal(tok.cpu().numpy(), low)
+
+
+# ---- members of rules that are absent ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("left", [dict(n_masks=-5), dict(ctx_total=-1), dict(bias_total=-(1 << 40)), dict(allowed_ld=-3),
+                                  dict(ctx_total=1 << 50, bias_total=1 << 50)])
+def test_counts_of_absent_rules_do_not_matter(B, left):
+    """What a program leaves in the counts that belong to NULL members."""
+    z = torch.randn(6, 500, device="cuda")
+    rules = B.logit_rules(500, None, 6, mask_id=9)
+    want, want_conf = B.op_rules_confidence(z, rules)
+    for k, v in left.items():
+        setattr(rules.struct, k, v)
+    flag = new_flag()
+    tok, conf = B.op_rules_confidence(z, rules, error_flag=flag)
+    assert torch.equal(tok, want) and torch.equal(conf, want_conf) and int(flag) == 0
+    out = B.op_logit_rules(z, rules, out=torch.empty_like(z), error_flag=flag)
+    z[:, 9] = -float("inf")
+    assert torch.equal(out, z) and int(flag) == 0
