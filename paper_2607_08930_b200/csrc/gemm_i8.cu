@@ -646,7 +646,7 @@ Plan plan_of(const DevInfo& dv, int M, int N, int kblocks, bool dual) {
 cudaError_t launch_gemm_i8(const GemmI8Args& a, cudaStream_t s) {
   if (a.M <= 0 || a.N <= 0) return cudaSuccess;
   const DevInfo* dv = dev_info();
-  if (!dv || !dv->ok) return cudaErrorNotSupported;
+  if (!dv || !dv->ok) return cudaErrorInitializationError;             // of the device, not of the arguments
   const bool dual = a.mode == 3;
   const int kblocks = (a.K + BKB - 1) / BKB;
   Plan pl = plan_of(*dv, a.M, a.N, kblocks, dual);

@@ -942,7 +942,8 @@ Plan plan_of(const RulesArgs& a) {
   return pl;
 }
 
-// Sets pl->spans: as many as the device holds at once, since a second round of them would double the time.
+// Sets pl->spans: as many as the device holds at once, since a second round of them would double the time.  False: the
+// device cannot be asked.
 bool plan_spans(const RulesArgs& a, Plan* pl) {
   DevInfo* d = device_slot(g_dev);
   if (!d) return false;
@@ -986,7 +987,7 @@ cudaError_t launch_rules(const RulesArgs& a, const Plan& pl, T* out, long long o
 cudaError_t launch_rules_confidence(const RulesArgs& a, int* tok, float* conf, cudaStream_t s) {
   if (a.n_rows <= 0) return cudaSuccess;
   Plan pl = plan_of(a);
-  if (!plan_spans(a, &pl)) return cudaErrorNotSupported;
+  if (!plan_spans(a, &pl)) return cudaErrorInitializationError;
   const bool aligned = (((uintptr_t)a.logits | (uintptr_t)(a.ld * (a.bf16_logits ? 2 : 4))) & 31) == 0;
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute at[2];
@@ -997,7 +998,7 @@ cudaError_t launch_rules_confidence(const RulesArgs& a, int* tok, float* conf, c
 cudaError_t launch_logit_rules(const RulesArgs& a, void* out, long long out_ld, cudaStream_t s) {
   if (a.n_rows <= 0) return cudaSuccess;
   Plan pl = plan_of(a);
-  if (!plan_spans(a, &pl)) return cudaErrorNotSupported;
+  if (!plan_spans(a, &pl)) return cudaErrorInitializationError;
   return a.bf16_logits ? launch_rules<bf16>(a, pl, (bf16*)out, out_ld, s) : launch_rules<float>(a, pl, (float*)out, out_ld, s);
 }
 
