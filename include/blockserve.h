@@ -404,6 +404,7 @@ int bs_op_attention_kv8(const void* q, int q_ld, const void* k8, const void* v8,
  * nothing, keep nothing, use no scratch and may be captured into graphs. */
 enum { BS_BF16 = 0, BS_F32 = 1 };            /* element types of x and of logits */
 enum { BS_I8_MAX_K = 131071 };               /* sums of K products of codes fit 32 bits */
+enum { BS_I8_MAX_ROWS = 0x7fffff00 };        /* M and N: indices of a tile that begins before the last row fit 31 bits */
 
 /* Codes and scales of rows x [x_rows][ldx] (type BS_BF16 or BS_F32, stride in elements; any alignment of the rows):
  *   y = x, or with `gain` (bf16 [K]) gain * x / sqrt(mean(x^2) + eps) in fp32;
@@ -437,7 +438,7 @@ int bs_op_gemm_i8(const void* A, long long lda, const float* a_scale, const void
  * that a program may fill them once and update their contents between calls.  NULL members are rules that do not apply.
  * Indices are checked on the device: what is out of range raises error_flag to 100 or more and is skipped, as said
  * below.  Calls allocate nothing, keep nothing, use no scratch and may be captured into graphs. */
-enum { BS_RULES_MAX_VOCAB = 524288 };
+enum { BS_RULES_MAX_VOCAB = 524288, BS_RULES_MAX_ROWS = 0x7fffff00 };
 typedef struct {
   int vocab, n_reqs;
   int mask_id;               /* never chosen, never counted as context; -1: there is none */

@@ -1111,7 +1111,7 @@ int bs_op_quant_i8(const void* x, int type, long long ldx, const int* idx, int x
                    void* codes, long long ldc, float* scale, int M, int K, int* error_flag, void* stream) {
   if (M == 0) return BS_OK;
   const int size = type == BS_F32 ? 4 : 2;
-  if (M < 0 || K < 1 || K > BS_I8_MAX_K || (type != BS_BF16 && type != BS_F32) || !x || !scale || !aligned16({codes}) ||
+  if (M < 0 || M > BS_I8_MAX_ROWS || K < 1 || K > BS_I8_MAX_K || (type != BS_BF16 && type != BS_F32) || !x || !scale || !aligned16({codes}) ||
       ((uintptr_t)x & (size - 1)) || !aligned4({idx, scale, error_flag}) || ((uintptr_t)gain & 15) || !(eps >= 0.f) ||
       x_rows < (idx ? 1 : M) || ldx < K || ldx > kMaxStride / 4 || ldc < K || ldc % 16 || ldc > kMaxStride)
     return BS_E_ARG;
@@ -1126,7 +1126,7 @@ int bs_op_gemm_i8(const void* A, long long lda, const float* a_scale, const void
                   const void* W2, const float* w2_scale, void* C, long long ldc, int M, int N, int K, int mode,
                   int* error_flag, void* stream) {
   if (M == 0 || N == 0) return BS_OK;
-  if (M < 0 || N < 0 || K < 1 || K > BS_I8_MAX_K || mode < 0 || mode > 3 || !aligned16({A, W, C}) || !a_scale || !w_scale ||
+  if (M < 0 || N < 0 || M > BS_I8_MAX_ROWS || N > BS_I8_MAX_ROWS || K < 1 || K > BS_I8_MAX_K || mode < 0 || mode > 3 || !aligned16({A, W, C}) || !a_scale || !w_scale ||
       !aligned4({a_scale, w_scale, w2_scale, error_flag}) || lda < K || lda % 16 || lda > kMaxStride || ldw < K || ldw % 16 ||
       ldw > kMaxStride || ldc < N || ldc > kMaxStride / 4 || (mode == 3) != (W2 != nullptr) || (W2 && (!w2_scale || ((uintptr_t)W2 & 15))))
     return BS_E_ARG;
@@ -1142,7 +1142,7 @@ int bs_op_gemm_i8(const void* A, long long lda, const float* a_scale, const void
 // Checks the rules and lays them out for the kernels; `out` and `out2` must not meet what they read.
 static bool rules_args(const void* logits, int type, long long ld, int n_rows, const bs_logit_rules* r, int* error_flag,
                        const Extent& out, const Extent& out2, bool inplace, RulesArgs* a) {
-  if (n_rows < 0 || !r || (type != BS_BF16 && type != BS_F32) || !aligned16({logits}) || !aligned4({error_flag})) return false;
+  if (n_rows < 0 || n_rows > BS_RULES_MAX_ROWS || !r || (type != BS_BF16 && type != BS_F32) || !aligned16({logits}) || !aligned4({error_flag})) return false;
   if (r->vocab < 1 || r->vocab > BS_RULES_MAX_VOCAB || r->n_reqs < 0 || r->mask_id < -1 || r->mask_id >= r->vocab ||
       ld < r->vocab || ld > kMaxStride / 4 || (!r->row_req && r->n_reqs < n_rows))
     return false;

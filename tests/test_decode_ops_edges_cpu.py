@@ -12,3 +12,30 @@ def test_a_missing_device_is_not_an_argument_error(B):
              _rules(B, "rules", out=P + 13 * G), _rules(B, "conf", row_req=None, n_reqs=6, row_mask=None, n_masks=6)]
     valid += [_gemm(B, mode=m) for m in range(3)] + [_gemm(B, mode=3, W2=P + 5 * G, sw2=P + 6 * G)]
     assert valid == [B.BS_E_CUDA] * len(valid)
+
+
+# ---- numbers of rows next to 2^31 -------------------------------------------------------------------------------
+
+MOST = 0x7fffff00
+
+
+@pytest.mark.parametrize("n", [MOST + 1, 2 ** 31 - 1])
+def test_rows_whose_tiles_would_pass_31_bits_are_refused(B, n):
+    far = dict(ldx=64, scale=P + 90 * G, codes=P + 40 * G)
+    assert _quant(B, M=n, rows=n, **far) == B.BS_E_ARG
+    wide = dict(A=P, W=P + 40 * G, C=P + 90 * G, sa=P + 300 * G, sw=P + 310 * G)
+    assert _gemm(B, M=n, **wide) == B.BS_E_ARG
+    assert _gemm(B, N=n, ldc=n, **wide) == B.BS_E_ARG
+    rows = dict(n=n, z=P + 100 * G, out=P + 300 * G, tok=P + 500 * G, conf=P + 510 * G, row_req=P + 520 * G, row_mask=P + 530 * G)
+    assert _rules(B, "rules", **rows) == B.BS_E_ARG and _rules(B, "conf", **rows) == B.BS_E_ARG
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the calls have made-up pointers: they must not reach a device")
+def test_the_largest_numbers_of_rows_are_accepted(B):
+    far = dict(ldx=64, scale=P + 90 * G, codes=P + 40 * G)
+    assert _quant(B, M=MOST, rows=2 ** 31 - 1, **far) == B.BS_E_CUDA
+    wide = dict(A=P, W=P + 40 * G, C=P + 90 * G, sa=P + 300 * G, sw=P + 310 * G)
+    assert _gemm(B, M=MOST, **wide) == B.BS_E_CUDA
+    assert _gemm(B, N=MOST, ldc=MOST, **wide) == B.BS_E_CUDA
+    rows = dict(n=MOST, z=P + 100 * G, out=P + 300 * G, tok=P + 500 * G, conf=P + 510 * G, row_req=P + 520 * G, row_mask=P + 530 * G)
+    assert _rules(B, "rules", **rows) == B.BS_E_CUDA and _rules(B, "conf", **rows) == B.BS_E_CUDA
