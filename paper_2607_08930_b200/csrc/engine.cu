@@ -1089,7 +1089,9 @@ struct Extent {
 };
 static Extent extent(const void* p, long long rows, long long ld, long long width) {
   const uintptr_t at = (uintptr_t)p;
-  return p && rows > 0 ? Extent{at, at + (uintptr_t)((rows - 1) * ld + width)} : Extent{at, at};
+  if (!p || rows <= 0) return Extent{at, at};
+  const unsigned __int128 end = (unsigned __int128)(rows - 1) * (unsigned __int128)ld + (unsigned __int128)width + at;
+  return Extent{at, end > UINTPTR_MAX ? UINTPTR_MAX : (uintptr_t)end};
 }
 static bool meets(const Extent& out, std::initializer_list<Extent> in) {
   for (const Extent& e : in)
@@ -1102,7 +1104,7 @@ static bool aligned4(std::initializer_list<const void*> ps) {           // where
   return true;
 }
 constexpr long long kMaxListed = 1ll << 30;                              // context tokens, biases: their indices step beyond
-constexpr long long kMaxStride = 1ll << 36;                              // of a row, in bytes: extents stay below 2^63
+constexpr long long kMaxStride = 1ll << 36;                              // of a row, in bytes
 static int status_of(cudaError_t r) {
   return r == cudaSuccess ? BS_OK : (r == cudaErrorNotSupported ? BS_E_ARG : BS_E_CUDA);
 }

@@ -39,3 +39,14 @@ def test_the_largest_numbers_of_rows_are_accepted(B):
     assert _gemm(B, N=MOST, ldc=MOST, **wide) == B.BS_E_CUDA
     rows = dict(n=MOST, z=P + 100 * G, out=P + 300 * G, tok=P + 500 * G, conf=P + 510 * G, row_req=P + 520 * G, row_mask=P + 530 * G)
     assert _rules(B, "rules", **rows) == B.BS_E_CUDA and _rules(B, "conf", **rows) == B.BS_E_CUDA
+
+
+@pytest.mark.parametrize("rows,ld", [(2 ** 31 - 1, 1 << 34), (2 ** 31 - 1, 1 << 33), (1 << 30, 1 << 34)])
+def test_overlap_is_seen_whatever_the_strides(B, rows, ld):
+    """Strides and rows that are allowed each, with an extent of up to 2^66 bytes."""
+    assert _quant(B, x=P, ldx=ld, rows=rows, idx=P - 64) == B.BS_E_ARG          # the codes lie in it
+    far = 1 << 60
+    assert _quant(B, x=P + far, ldx=ld, rows=rows, idx=P - 64, codes=P + far + G) == B.BS_E_ARG
+    n = min(rows, MOST)
+    assert _gemm(B, A=P, lda=2 * ld, M=n) == B.BS_E_ARG                         # the outputs lie in A
+    assert _rules(B, "rules", z=P, ld=ld, n=n, row_req=16, row_mask=16) == B.BS_E_ARG
