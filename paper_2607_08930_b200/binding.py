@@ -862,9 +862,10 @@ def logit_rules(vocab: int, row_req: Optional[torch.Tensor], n_reqs: int, mask_i
     elif row_mask is not None:
         _refuse(name, "row_mask needs allowed")
     p = _ptr
-    s = BsLogitRules(vocab, n_reqs, mask_id, p(row_req), p(ctx), 0 if ctx is None else ctx.numel(), p(ctx_begin), p(ctx_gen),
-                     p(ctx_end), p(repetition), p(presence), p(frequency), p(bias_at), p(bias_tok), p(bias_val),
-                     0 if bias_tok is None else bias_tok.numel(), p(allowed),
+    # (a tensor without elements has no address of its own, and NULL would be an absent rule)
+    s = BsLogitRules(vocab, n_reqs, mask_id, p(row_req), p(ctx) or p(ctx_begin), 0 if ctx is None else ctx.numel(), p(ctx_begin),
+                     p(ctx_gen), p(ctx_end), p(repetition), p(presence), p(frequency), p(bias_at), p(bias_tok), p(bias_val),
+                     0 if bias_tok is None else bias_tok.numel(), p(allowed) or p(row_mask),
                      0 if allowed is None else (allowed.stride(0) if allowed.shape[0] > 1 else allowed.shape[1]),
                      0 if allowed is None else allowed.shape[0], p(row_mask))
     return LogitRules(s, given, dev, rows)

@@ -145,3 +145,24 @@ def test_counts_of_absent_rules_do_not_matter(B, left):
     out = B.op_logit_rules(z, rules, out=torch.empty_like(z), error_flag=flag)
     z[:, 9] = -float("inf")
     assert torch.equal(out, z) and int(flag) == 0
+
+
+def test_tensors_without_elements_are_rules_all_the_same(B):
+    """A grammar of no masks, of which rows name one, and a context of no tokens, of which a request has some: both are out
+    of range, not absent."""
+    z = torch.randn(4, 500, device="cuda")
+    words = torch.empty(0, 16, dtype=torch.int32, device="cuda")
+    rules = B.logit_rules(500, None, 4, allowed=words, row_mask=ints([-1, 0, -1, 3]))
+    flag = new_flag()
+    tok, conf = B.op_rules_confidence(z, rules, error_flag=flag)
+    assert int(flag) >= 100 and tok.tolist()[1::2] == [-1, -1] and conf.tolist()[1::2] == [0, 0]
+    assert torch.equal(tok[::2].long(), z[::2].argmax(1))
+    flag.zero_()
+    out = torch.full_like(z, 7.0)
+    B.op_logit_rules(z, rules, out=out, error_flag=flag)
+    assert int(flag) >= 100 and torch.equal(out[::2], z[::2]) and (out[1::2] == 7).all()
+    none, zeros = torch.empty(0, dtype=torch.int32, device="cuda"), ints([0, 0, 0, 0])
+    for end, raised in ((zeros, False), (ints([0, 0, 1, 0]), True)):
+        rules = B.logit_rules(500, None, 4, ctx=none, ctx_begin=zeros, ctx_gen=zeros, ctx_end=end, presence=f32([1, 1, 1, 1]))
+        flag.zero_()
+        assert torch.equal(B.op_logit_rules(z, rules, out=out, error_flag=flag), z) and (int(flag) >= 100) == raised
