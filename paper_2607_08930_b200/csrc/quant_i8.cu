@@ -147,6 +147,61 @@ __device__ __forceinline__ unsigned largest(const Unit<F32>& r, const bf16* gain
   return top;
 }
 
+// Whether fp32 holds a row's sum of squares and its products with the gains: the mean of the squares (with eps) and the
+// largest product lie where neither has overflowed, nor lost bits to the least numbers.  A row of zeros is one, too.
+__device__ __forceinline__ bool in_range(float mean, float ss, unsigned top) {
+  return mean >= 0x1p-100f && mean < INFINITY && top < 0x7f800000u &&
+         (top >= __float_as_uint(0x1p-100f) || (top == 0u && ss == 0.f));
+}
+
+// A row that is not: its elements are scaled by a power of two to below one first, and the squares are summed in 64 bits.
+// Every warp reads the whole row for itself (no barriers, for rows that share the CTA), and rounds its own units.
+template <bool F32, bool VEC>
+__device__ __noinline__ void far_row(const void* row, const bf16* gain, float eps, int8_t* out, float* scale, int K) {
+  const int lane = threadIdx.x & 31;
+  float v[kUnit], g[kUnit];
+  unsigned top = 0u;
+  for (int at = lane * kUnit; at < K; at += 32 * kUnit) {
+    widen<F32>(load_unit<F32, VEC>(row, at, K), v);
+#pragma unroll
+    for (int i = 0; i < kUnit; ++i) top = max(top, magnitude(v[i]));
+  }
+  top = __reduce_max_sync(0xffffffffu, top);
+  const int e = max((int)(top >> 23), 1) - 126;              // the largest |x| is below 2^e
+  const float f = e > 126 ? __uint_as_float(1u << (149 - e)) : __uint_as_float((unsigned)(127 - e) << 23);      // 2^-e
+  auto scaled = [&](int at) {                                // v = gain x 2^-e; its share of the sum of squares
+    double ss = 0.0;
+    widen<F32>(load_unit<F32, VEC>(row, at, K), v);
+    widen<false>(load_unit<false, true>(gain, at, K), g);
+#pragma unroll
+    for (int i = 0; i < kUnit; ++i) {
+      v[i] *= f;
+      ss += (double)v[i] * v[i];
+      v[i] *= g[i];
+    }
+    return ss;
+  };
+  unsigned most = 0u;
+  double ss = 0.0;
+  for (int at = lane * kUnit; at < K; at += 32 * kUnit) {
+    ss += scaled(at);
+#pragma unroll
+    for (int i = 0; i < kUnit; ++i) most = max(most, magnitude(v[i]));
+  }
+  most = __reduce_max_sync(0xffffffffu, most);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+  const float rms = (float)(1.0 / sqrt(ss / K + ldexp((double)eps, -2 * e)));
+  const float big = __uint_as_float(most) * rms;
+  const bool real = top < 0x7f800000u && most < 0x7f800000u && big < INFINITY;
+  const float s = fmaxf(__fmul_rn(big, 1.f / 127.f), 0x1p-126f);
+  if (threadIdx.x == 0) *scale = real ? s : __uint_as_float(0x7fffffffu);
+  for (int at = threadIdx.x * kUnit; at < K; at += blockDim.x * kUnit) {
+    scaled(at);
+    store_unit(out, at, K, real ? round_unit<true>(v, rms, s, __frcp_rn(s)) : make_uint2(0u, 0u));
+  }
+}
+
 // Two CTAs an SM at least: of up to 1024 threads with 32 registers each for plain bf16 rows (three of 592: 4096 x
 // 18944 47 -> 42 us), where the others would spill; those have up to 640 threads (4096 x 18944 fp32 with 1024: one CTA, 81 us,
 // so 58; norms of bf16 rows 106 and 73, unaligned ones 133 and 79).
@@ -208,8 +263,13 @@ __global__ void __launch_bounds__(kMost<F32, VEC, NORM, LONG>, 2) k_quant_i8(con
     }
   }
   if (!here) return;
+  const float mean = ss / (float)a.K + a.eps;
+  if (NORM && !in_range(mean, ss, top)) {
+    far_row<F32, VEC>(row, a.gain, a.eps, a.codes + (long long)m * a.ldc, a.scale + m, K);
+    return;
+  }
   // rounding is monotonic: the largest |gain x| times r is the largest |y|
-  const float rms = NORM ? rsqrtf(ss / (float)a.K + a.eps) : 1.f;
+  const float rms = NORM ? rsqrtf(mean) : 1.f;
   const float big = NORM ? __uint_as_float(top) * rms : __uint_as_float(top);
   const bool real = top < 0x7f800000u && big < INFINITY;
   const float s = fmaxf(__fmul_rn(big, 1.f / 127.f), 0x1p-126f);

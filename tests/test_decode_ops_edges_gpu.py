@@ -7,7 +7,7 @@ import pytest
 import torch
 
 from oracle import decode_oracle as D
-from test_decode_ops_gpu import B, CONF_TOL, f32, host, ints  # noqa: F401
+from test_decode_ops_gpu import B, CONF_TOL, HALF_F32, f32, host, ints  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -166,3 +166,51 @@ def test_tensors_without_elements_are_rules_all_the_same(B):
         rules = B.logit_rules(500, None, 4, ctx=none, ctx_begin=zeros, ctx_gen=zeros, ctx_end=end, presence=f32([1, 1, 1, 1]))
         flag.zero_()
         assert torch.equal(B.op_logit_rules(z, rules, out=out, error_flag=flag), z) and (int(flag) >= 100) == raised
+
+
+# ---- RMS norms of rows far from one -----------------------------------------------------------------------------
+
+POWERS = [0, 126, 100, 65, 63, 61, 30, -30, -45, -49, -51, -60, -74, -80, -99, -101, -120, -133]      # of the rows
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("k,pad", [(1, 0), (9, 0), (384, 0), (385, 0), (3584, 8), (18944, 0), (40001, 0)])
+@pytest.mark.parametrize("eps", [1e-5, 1e-38, 0.0])
+@pytest.mark.parametrize("power", [0, 100, -60])
+def test_codes_of_rms_norms_far_from_one(B, dtype, k, pad, eps, power):
+    """Squares, or products with the gains, beyond what fp32 holds at either end, beside ordinary rows, rows of zeros and
+    rows without a scale.  Bounds as for ordinary rows: the sum of at most 32 terms a thread (long rows: k / 1024) and ten
+    joins, its root and the products, relative error below delta; a code within 127 * 2 delta of a rounded quotient."""
+    rng = np.random.default_rng((k + power) % 2 ** 32)
+    x = rng.uniform(0.5, 1, size=(3 * len(POWERS), k)) * rng.choice([-1, 1], size=(3 * len(POWERS), k))
+    x = x * 2.0 ** np.repeat(POWERS, 3)[:, None]
+    x[::7, k // 2:] *= 2.0 ** -10                             # a smaller half
+    x[10] = 0.0
+    x[20, 0], x[30, k - 1], x[40, 0] = np.inf, np.nan, -np.inf
+    x = torch.from_numpy(x).to(dtype)
+    gain = torch.from_numpy((1 + 0.2 * rng.uniform(-1, 1, size=k)) * 2.0 ** power).bfloat16()
+    store = torch.zeros(x.shape[0], k + pad, dtype=dtype, device="cuda")
+    store[:, :k] = x.cuda()
+    got, s = B.op_quant_i8(store[:, :k], gain=gain.cuda(), eps=eps)
+    with np.errstate(all="ignore"):
+        e = np.float64(np.float32(eps))
+        y, _, scale = D.quant(host(x), host(gain), e)
+        none = ~np.isfinite(y).all(1)
+    assert none[[20, 30, 40]].all() and none.sum() == 3 + (eps == 0)
+    got, s = host(got), host(s)
+    assert np.array_equal(np.isnan(s), none) and (got[none] == 0).all()
+    y, scale, got, s = y[~none], scale[~none], got[~none], s[~none]
+    delta = (max(32, k / 1024) + 10 + 8) * HALF_F32
+    assert (np.abs(s - scale) <= scale * (delta + 2 * HALF_F32)).all()
+    assert (np.abs(got - y / s[:, None]) <= 0.5 + 127 * 2 * delta).all()
+
+
+def test_a_norm_beyond_fp32_has_no_scale(B):
+    """The row's y itself is too large: 127 elements of zero and one whose y is sqrt(128) * 2^125."""
+    x = torch.zeros(2, 128, device="cuda")
+    x[:, 5] = 1.0
+    gain = torch.ones(128, dtype=torch.bfloat16, device="cuda")
+    codes, s = B.op_quant_i8(x, gain=gain * 2.0 ** 125, eps=0.0)
+    assert torch.isnan(s).all() and (codes == 0).all()
+    codes, s = B.op_quant_i8(x, gain=gain * 2.0 ** 123, eps=0.0)
+    assert torch.isfinite(s).all() and (codes[:, 5] == 127).all() and (codes.sum(1) == 127).all()
