@@ -412,7 +412,8 @@ enum { BS_I8_MAX_ROWS = 0x7fffff00 };        /* M and N: indices of a tile that 
  *   integer, halves to the even one, decided on the exact quotient: -127 to 127.
  * Row m is row idx[m] of x (idx NULL: row m, x_rows >= M).  An idx[m] outside [0, x_rows) raises error_flag (device int,
  * nullable, only ever raised) to 100 or more and leaves the row's outputs as they were.  A row with an infinite or NaN
- * element gets the scale NaN and zero codes. */
+ * element gets the scale NaN and zero codes, and so does one whose y is (an infinite gain, a y beyond fp32, zeros with an
+ * eps of 0).  Squares, or products with the gain, that leave fp32's range on the way make no difference. */
 int bs_op_quant_i8(const void* x, int type, long long ldx, const int* idx, int x_rows, const void* gain, float eps,
                    void* codes, long long ldc, float* scale, int M, int K, int* error_flag, void* stream);
 
