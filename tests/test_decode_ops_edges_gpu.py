@@ -7,7 +7,7 @@ import pytest
 import torch
 
 from oracle import decode_oracle as D
-from test_decode_ops_gpu import B, CONF_TOL, HALF_F32, f32, host, ints  # noqa: F401
+from test_decode_ops_gpu import B, CONF_TOL, HALF_F32, f32, host, ints, random_codes  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -214,3 +214,28 @@ def test_a_norm_beyond_fp32_has_no_scale(B):
     assert torch.isnan(s).all() and (codes == 0).all()
     codes, s = B.op_quant_i8(x, gain=gain * 2.0 ** 123, eps=0.0)
     assert torch.isfinite(s).all() and (codes[:, 5] == 127).all() and (codes.sum(1) == 127).all()
+
+
+# ---- products: each rounding, and no other ----------------------------------------------------------------------
+
+@pytest.mark.parametrize("mode", [0, 1, 2])
+@pytest.mark.parametrize("m,n,k,cpad", [(1, 130, 20000, 0), (3, 130, 33, 6), (16, 640, 9000, 0), (64, 4608, 3584, 0),
+                                        (64, 128, 131071, 0), (128, 520, 6000, 3), (200, 384, 18944, 0), (256, 2048, 16384, 0),
+                                        (300, 520, 777, 24), (512, 1024, 8192, 0), (512, 3584, 2000, 0), (1025, 1300, 513, 1),
+                                        (3000, 2500, 300, 0)])
+def test_products_have_the_stated_roundings_alone(B, mode, m, n, k, cpad):
+    """The exact sum to fp32, times w_scale, times a_scale, then to bf16 or added in fp32: equal, however the call is cut."""
+    rng = np.random.default_rng(m + n + k)
+    a, ta = random_codes(rng, m, k)
+    w, tw = random_codes(rng, n, k)
+    sa, sw = rng.uniform(0.5, 2, m).astype(np.float32), (rng.uniform(0.5, 2, n) / k).astype(np.float32)
+    z = (a.astype(np.float64) @ w.astype(np.float64).T).astype(np.float32) * sw * sa[:, None]
+    assert z.dtype == np.float32
+    out = torch.full((m, n + cpad), 3.0, dtype=torch.bfloat16 if mode == 0 else torch.float32, device="cuda")
+    if mode == 1:
+        base = (40 * rng.normal(size=(m, n))).astype(np.float32)
+        out[:, :n] = f32(base)
+        z = base + z
+    B.op_gemm_i8(ta, f32(sa), tw, f32(sw), mode=mode, C_out=out[:, :n])
+    assert torch.equal(out[:, :n].cpu(), torch.from_numpy(z).to(out.dtype))
+    assert (out[:, n:] == 3.0).all()
