@@ -590,8 +590,16 @@ bool encode(const void* base, long long rows, long long cols, long long ld, int 
 }
 
 struct Plan {
-  int cg, splits, tn, m_tiles, n_tiles, workers, stages, nbuf;
+  int cg, splits, tn, m_tiles, n_tiles, workers, nbuf;
+  int stage_bytes, stages;   // operand stages, in what the received partial sums leave of the ring
 };
+
+void set_stages(Plan* p, bool dual) {
+  const int own = (p->tn / kChunk + p->splits - 1) / p->splits;
+  p->stage_bytes = (dual ? 2 : 1) * kTileRows * BKB + p->tn / p->cg * BKB;
+  p->stages = (kRing - (p->splits - 1) * own * kChunk * kTileRows * 4) / p->stage_bytes;
+  if (p->stages > kMaxStages) p->stages = kMaxStages;
+}
 
 // Clocks that a plan takes, from what was measured over QKV, O, gate/up, down and LM-head shapes at 1 to 8192 tokens.  A k
 // step costs its products (2 tn clocks a weight tile, 1.2 times that in practice) or its loads (62 bytes a clock, 50 for a
@@ -610,7 +618,9 @@ float cost_of(const Plan& p, int kblocks, bool dual, float weight_bytes) {
 }
 
 // The cheapest plan: single CTAs or pairs, tiles of equal width that cover the tokens, k ranges shared by up to eight CTAs
-// where the tiles leave SMs idle (one wave of clusters; two k steps each at least).
+// where the tiles leave SMs idle (one wave of clusters; two k steps each at least).  Three stages at least, without which
+// products and loads take turns, and the cost above does not hold (512 x 2048 x 8192 on two 17.2 us, 13.8 on the three or
+// more of the plan that is then cheapest; 256 x 3584 x 3584 10.8 and 8.9; 1024 x 1024 x 16384 29.5 and 25.1).
 Plan plan_of(const DevInfo& dv, int M, int N, int kblocks, bool dual) {
   Plan best = {};
   float least = INFINITY;
@@ -632,6 +642,8 @@ Plan plan_of(const DevInfo& dv, int M, int N, int kblocks, bool dual) {
         const int most = sp == 1 ? (cg == 2 ? dv.clusters[2] : dv.num_sms) : dv.clusters[sp * cg];
         if (sp > 1 && (items > most || kblocks < 2 * sp)) break;
         p.splits = sp;
+        set_stages(&p, dual);
+        if (p.stages < 3) continue;
         p.workers = (int)(items < most ? items : most);
         const float c = cost_of(p, kblocks, dual, weight_bytes);
         if (c < least) { least = c; best = p; }
@@ -649,15 +661,10 @@ cudaError_t launch_gemm_i8(const GemmI8Args& a, cudaStream_t s) {
   if (!dv || !dv->ok) return cudaErrorInitializationError;             // of the device, not of the arguments
   const bool dual = a.mode == 3;
   const int kblocks = (a.K + BKB - 1) / BKB;
-  Plan pl = plan_of(*dv, a.M, a.N, kblocks, dual);
-  const int stage_bytes = (dual ? 2 : 1) * kTileRows * BKB + pl.tn / pl.cg * BKB;
-  const int own = (pl.tn / kChunk + pl.splits - 1) / pl.splits;
-  const int received = (pl.splits - 1) * own * kChunk * kTileRows * 4;
-  pl.stages = (kRing - received) / stage_bytes;
-  if (pl.stages > kMaxStages) pl.stages = kMaxStages;
+  const Plan pl = plan_of(*dv, a.M, a.N, kblocks, dual);
   Params p;
   p.M = a.M; p.N = a.N; p.K = a.K; p.tn = pl.tn; p.n_tiles = pl.n_tiles; p.m_tiles = pl.m_tiles; p.splits = pl.splits;
-  p.kblocks = kblocks; p.stages = pl.stages; p.nbuf = pl.nbuf; p.received = pl.stages * stage_bytes;
+  p.kblocks = kblocks; p.stages = pl.stages; p.nbuf = pl.nbuf; p.received = pl.stages * pl.stage_bytes;
   p.mgroup = (long long)a.M * a.K > (56ll << 20) && pl.m_tiles > 16 ? 16 : 0;
   p.vec = a.ldc % 8 == 0 && a.N % 8 == 0 && ((uintptr_t)a.C & 15) == 0;
   p.C = a.C; p.ldc = a.ldc; p.sa = a.sa; p.sw = a.sw; p.sw2 = a.sw2; p.error_flag = a.error_flag;
