@@ -410,6 +410,8 @@ enum { BS_I8_MAX_ROWS = 0x7fffff00 };        /* M and N: indices of a tile that 
  *   y = x, or with `gain` (bf16 [K]) gain * x / sqrt(mean(x^2) + eps) in fp32;
  *   scale = max(max |y| * (1 / 127), 2^-126) in fp32, with 1 / 127 rounded to fp32;  code = y / scale to the nearest
  *   integer, halves to the even one, decided on the exact quotient: -127 to 127.
+ * (The scale is that product, not the rounded quotient max |y| / 127: fp32(1 / 127) is 2^-28 of itself too small, so that one
+ * largest magnitude in 21 - in bf16, 6 mantissas of 128 - has the fp32 value just below the quotient's.)
  * Row m is row idx[m] of x (idx NULL: row m, x_rows >= M).  An idx[m] outside [0, x_rows) raises error_flag (device int,
  * nullable, only ever raised) to 100 or more and leaves the row's outputs as they were.  A row with an infinite or NaN
  * element gets the scale NaN and zero codes, and so does one whose y is (an infinite gain, a y beyond fp32, zeros with an
@@ -459,7 +461,7 @@ typedef struct {
   const float* frequency;    /* [n_reqs], nullable: 0 */
   /* request i's biases: tokens bias_tok[bias_at[i]] .. bias_tok[bias_at[i + 1] - 1] in ascending order (equal ones add up,
      in order).  A token that is out of range or below the one before it raises the flag, and which of the request's
-     biases then count is not defined. */
+     biases then count is not defined; entries that the list does not name are as without it. */
   const int* bias_at;        /* [n_reqs + 1], values in [0, bias_total] */
   const int* bias_tok;
   const float* bias_val;
