@@ -679,12 +679,12 @@ cudaError_t launch_gemm_i8(const GemmI8Args& a, cudaStream_t s) {
   cfg.dynamicSmemBytes = kSmem;
   cfg.stream = s;
   cudaLaunchAttribute at[2];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  at[1].id = cudaLaunchAttributeClusterDimension;
-  at[1].val.clusterDim.x = (unsigned)(pl.cg * pl.splits); at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = (unsigned)(pl.cg * pl.splits); at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+  at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
-  cfg.numAttrs = 2;
+  cfg.numAttrs = pdl_disabled() ? 1 : 2;
   Kernel k = pl.cg == 2 ? (pl.splits > 1 ? kernel_of<2, true>(a.mode) : kernel_of<2, false>(a.mode))
                         : (pl.splits > 1 ? kernel_of<1, true>(a.mode) : kernel_of<1, false>(a.mode));
   return cudaLaunchKernelEx(&cfg, k, mw, mw2, mx, p);

@@ -925,7 +925,7 @@ void cluster_config(cudaLaunchConfig_t* cfg, cudaLaunchAttribute* at, int ctas, 
   at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[1].val.programmaticStreamSerializationAllowed = 1;
   cfg->attrs = at;
-  cfg->numAttrs = early ? 2 : 1;
+  cfg->numAttrs = early && !pdl_disabled() ? 2 : 1;
 }
 
 size_t smem_of(const Plan& pl) { return (size_t)pl.listed * 8 + (size_t)pl.blocks * kBlockWords * 10 + kWarps * kQueue * 4; }

@@ -1,6 +1,9 @@
 """What the 8-bit row codes, the 8-bit projections and the logit rules do at the edges of what they accept, against the
 64-bit oracle (needs a B200)."""
 import itertools
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -239,3 +242,37 @@ def test_products_have_the_stated_roundings_alone(B, mode, m, n, k, cpad):
     B.op_gemm_i8(ta, f32(sa), tw, f32(sw), mode=mode, C_out=out[:, :n])
     assert torch.equal(out[:, :n].cpu(), torch.from_numpy(z).to(out.dtype))
     assert (out[:, n:] == 3.0).all()
+
+
+# ---- launches ---------------------------------------------------------------------------------------------------
+
+EDGES = """
+import ctypes as C
+import torch
+from paper_2607_08930_b200 import binding as B
+x, w = torch.randn(40, 256, device="cuda"), torch.randn(700, 256, device="cuda")
+rules = B.logit_rules(700, None, 40, mask_id=7)
+codes, wq, y = B.op_quant_i8(x), B.op_quant_i8(w), torch.randn(40, 700, device="cuda")
+rt = C.CDLL("libcudart.so.12")
+for op in (lambda: B.op_quant_i8(x), lambda: B.op_gemm_i8(*codes, *wq, mode=2), lambda: B.op_rules_confidence(y, rules),
+           lambda: B.op_logit_rules(y, rules)):
+    g = torch.cuda.CUDAGraph(keep_graph=True)
+    with torch.cuda.graph(g):
+        op(), op(), op()
+    n, tail, head, data = C.c_size_t(8), (C.c_void_p * 8)(), (C.c_void_p * 8)(), (C.c_ubyte * 8 * 8)()
+    assert rt.cudaGraphGetEdges_v2(C.c_void_p(g.raw_cuda_graph()), tail, head, data, C.byref(n)) == 0
+    print(n.value, sum(data[i][2] == 1 for i in range(n.value)))          # (from port, to port, type, ..): 1 is programmatic
+"""
+
+
+@pytest.mark.parametrize("off", [False, True])
+def test_the_switch_for_plain_launches(B, off):
+    """Three calls in a row depend on one another, through programmatic edges unless BS_NO_PDL is set."""
+    env = {k: v for k, v in os.environ.items() if k != "BS_NO_PDL"}
+    if off:
+        env["BS_NO_PDL"] = "1"
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", EDGES], cwd=root, env=env, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-2000:]
+    edges = [tuple(map(int, line.split())) for line in r.stdout.splitlines()]
+    assert edges == [(2, 0 if off else 2)] * 4
