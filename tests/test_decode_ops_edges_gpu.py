@@ -10,7 +10,7 @@ import pytest
 import torch
 
 from oracle import decode_oracle as D
-from test_decode_ops_gpu import B, CONF_TOL, HALF_F32, f32, host, ints, random_codes  # noqa: F401
+from test_decode_ops_gpu import B, CONF_TOL, HALF_F32, check_rules, f32, host, ints, random_codes  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -276,3 +276,24 @@ def test_the_switch_for_plain_launches(B, off):
     assert r.returncode == 0, r.stderr[-2000:]
     edges = [tuple(map(int, line.split())) for line in r.stdout.splitlines()]
     assert edges == [(2, 0 if off else 2)] * 4
+
+
+# ---- the largest vocabulary -------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("all_of_it", [False, True])
+def test_the_largest_vocabulary(B, dtype, all_of_it):
+    """Shares of 65536 entries, of which a few or all are touched; a bias for each token of one request."""
+    vocab = B.RULES_MAX_VOCAB
+    rng = np.random.default_rng(vocab)
+    n = np.array([0, vocab + 1000 if all_of_it else 900])
+    ctx = np.concatenate([rng.permutation(vocab), rng.integers(0, vocab, 1000)])[:n[1]]
+    biases = np.array([vocab - 1 if all_of_it else 70, 3])
+    tok = np.concatenate([np.sort(rng.permutation(vocab)[:b]) for b in biases])
+    bits = rng.random((2, vocab)) < np.array([[0.5], [0.00001]])
+    r = dict(row_req=np.array([0, 1, 1, -1]), mask_id=vocab - 1, ctx=ctx, begin=np.array([0, 0]), gen=np.array([0, 500]), end=n,
+             repetition=np.array([1.5, 1.25], np.float32), presence=np.array([0.25, 0.5], np.float32),
+             frequency=np.array([0.5, 0.125], np.float32), bias_at=np.concatenate([[0], np.cumsum(biases)]), bias_tok=tok,
+             bias_val=rng.normal(size=len(tok)).astype(np.float32), row_mask=np.array([-1, 0, 1, 0]),
+             allowed=np.packbits(bits, axis=1, bitorder="little").view(np.int32))
+    check_rules(B, (3 * rng.normal(size=(4, vocab))).astype(np.float32), r, vocab, 2, dtype)
