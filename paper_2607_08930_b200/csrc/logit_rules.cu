@@ -114,15 +114,17 @@ __device__ __forceinline__ void send(const Slot* to, unsigned long long* bar, un
                ::"r"(in_cta(tc::smem_u32(to), rank)), "r"(__float_as_uint(m)), "r"(__float_as_uint(s)), "r"(at), "r"(0u),
                  "r"(in_cta(tc::smem_u32(bar), rank)) : "memory");
 }
-// Bounded: false if the parts do not arrive in time.
-__device__ __forceinline__ bool wait_parts(unsigned long long* bar, unsigned parity) {
-  const long long t0 = clock64();
+// Bounded: false if the parts do not arrive in time.  The CTAs of a cluster read the same lists but need not have the same
+// work: a list's tokens may all be in one CTA's share, and equal biases are added one by one (a million of them in one row:
+// 0.11 s).  So the limit grows with the longest list (context and biases), by a thousand clocks a token and row.
+__device__ __forceinline__ bool wait_parts(unsigned long long* bar, unsigned parity, unsigned longest) {
+  const long long t0 = clock64(), limit = tc::kWaitCycles + 1024ll * kRowsAtOnce * longest;
   for (;;) {
     unsigned ok;
     asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
                  : "=r"(ok) : "r"(tc::smem_u32(bar)), "r"(parity) : "memory");
     if (ok) return true;
-    if (clock64() - t0 > tc::kWaitCycles) return false;
+    if (clock64() - t0 > limit) return false;
   }
 }
 
@@ -556,7 +558,9 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_rules_confidence(const Rul
   __shared__ __align__(8) unsigned long long s_bar;
   __shared__ unsigned s_top[kRowsAtOnce];                    // the largest maximum that a warp has left so far, ordered
   __shared__ Row s_rows[kRowsAtOnce];
+  __shared__ unsigned s_longest[kWarps];                     // the longest list so far (a copy for each warp)
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (lane == 0) s_longest[warp] = 0u;
   if (threadIdx.x == 0) {
     tc::mbar_init(tc::smem_u32(&s_bar), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -601,6 +605,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_rules_confidence(const Rul
       if (me.req != cur) {
         build_table(a, t, pl, me.req);
         cur = me.req;
+        if (lane == 0) s_longest[warp] = max(s_longest[warp], (unsigned)(t.end - t.begin) + (unsigned)(t.bias_hi - t.bias_lo));
       }
       const unsigned* mask = me.mask < 0 ? nullptr : a.allowed + me.mask * a.allowed_ld;
       const W walk(z);
@@ -746,7 +751,8 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_rules_confidence(const Rul
     }
     // join the parts of these rows: row i by CTA i mod chunks
     if (warp < joins) {
-      const bool here = wait_parts(&s_bar, turn);
+      __syncwarp();
+      const bool here = wait_parts(&s_bar, turn, s_longest[warp]);
       if (!here && lane == 0 && a.error_flag) atomicMax(a.error_flag, 1);
       for (int k = warp; k < joins; k += kWarps) {
         Part p{-INFINITY, 0.f, 0x7fffffff};

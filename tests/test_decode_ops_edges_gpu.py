@@ -297,3 +297,19 @@ def test_the_largest_vocabulary(B, dtype, all_of_it):
              bias_val=rng.normal(size=len(tok)).astype(np.float32), row_mask=np.array([-1, 0, 1, 0]),
              allowed=np.packbits(bits, axis=1, bitorder="little").view(np.int32))
     check_rules(B, (3 * rng.normal(size=(4, vocab))).astype(np.float32), r, vocab, 2, dtype)
+
+
+def test_a_list_that_keeps_one_share_busy_for_seconds(B):
+    """2^25 equal biases, which one thread adds one after the other: the CTAs that join the row wait for it."""
+    vocab, n = 126464, 1 << 25
+    z = torch.randn(2, vocab, device="cuda")
+    val = torch.ones(n, device="cuda")
+    val[1::2] = -1.0
+    z[:, 5] = 3.0
+    rules = B.logit_rules(vocab, None, 2, bias_at=ints([0, n, n]), bias_tok=torch.full((n,), 5, dtype=torch.int32, device="cuda"),
+                          bias_val=val)
+    flag = new_flag()
+    tok, conf = B.op_rules_confidence(z, rules, error_flag=flag)
+    want, want_conf = B.op_rules_confidence(z, B.logit_rules(vocab, None, 2))
+    assert int(flag) == 0 and torch.equal(tok, want)
+    assert (np.abs(host(conf) - host(want_conf)) <= host(want_conf) * 2 * CONF_TOL).all()
