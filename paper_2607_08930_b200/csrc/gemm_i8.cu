@@ -16,8 +16,8 @@
 // does not depend on the split.
 // Measured: 8192 tokens x 3584 x 18944 in 360 us (3.1 POP/s; the bf16 projection of the same size takes 866), the SwiGLU of
 // 512 x 18944 x 3584 in 52 us, of which its products take 44 (the arithmetic and stores of an epilogue that nothing hides,
-// its accumulators fill TMEM, the rest); 64 tokens x 4608 x 3584 in 7.1 us, the LM head of 128 tokens in 106 us (weights
-// and logits from and to HBM: 95).
+// its accumulators fill TMEM, the rest); 64 tokens x 4608 x 3584 in 7.3 us (7.0 out of the L2), the LM head of 128
+// tokens in 108 us (weights and logits from and to HBM: 95).
 // Every wait is bounded: one that runs out raises the error flag and leaves NaN in the outputs that it kept from being
 // formed; all roles drain and TMEM is freed.
 #include <math.h>
