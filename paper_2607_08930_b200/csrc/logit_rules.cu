@@ -17,12 +17,12 @@
 // without scratch.
 //
 // Measured on logits [rows][vocabulary]: the confidence of 317 rows of 152064 (16 requests, a grammar on nine rows of ten)
-// takes 48 us, 40 without any rule (29 at the copy rate), of 64 single rows of 126464 with contexts of 512 to 4096 tokens
-// 19 us (17.5 out of the L2); the logits of 64 such rows of 152064 take 20 us (12), of 318 rows of 126464 in 16 bits 43 us (30; 35 without the
-// grammar, 29 bare; in place 37 with half of the entries forbidden, 16 without a grammar).  Of the confidence's 48 us, 6 pass
-// before and after the rows, 5 building tables, 7.5 for every row of a span (5.8 TB/s), and spans have 4 or 5 rows.  Fewer
-// spans of equal lengths: 128 rows 27.3 -> 24.7 us, but 315 rows 49.2 -> 51.4.  Rows that are not aligned, 317 of 152063:
-// confidence 50 us without rules, logits 81 (aligned 40 and 69).
+// takes 48 us, 40 without any rule (29 at the copy rate), of 64 single rows of 126464 with contexts of 512 to 4096 tokens 19
+// us (17.5 out of the L2); the logits of 64 such rows of 152064 take 20 us (12), of 318 rows of 126464 in 16 bits 43 us (30;
+// 35 without the grammar, 29 bare; in place 37 with half of the entries forbidden, 16 without a grammar).  Of the
+// confidence's 48 us, 6 pass before and after the rows, 5 building tables, 7.5 for every row of a span (5.8 TB/s), and spans
+// have 4 or 5 rows.  Fewer spans of equal lengths: 128 rows 27.3 -> 24.7 us, but 315 rows 49.2 -> 51.4.  Rows that are not
+// aligned, 317 of 152063: confidence 50 us without rules, logits 81 (aligned 40 and 69).
 #include <math.h>
 
 #include <mutex>
